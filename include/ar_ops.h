@@ -1,0 +1,103 @@
+/*
+ * ar_ops.h -- C ABI of the operators around libar's collectives (gfx950).
+ *
+ * A rank of a tensor-parallel program computes a block on its shard, has the
+ * ranks' results joined, and adds the join to its residual stream between two
+ * norms.  The joins are ar.h's collectives; around them:
+ *   ar_residual_norm   norm of a block's output, gate, scaled residual, norm
+ *                      before the next block, and its backward pass
+ *
+ * Conventions.  As in ar.h: device pointers on the current device, sizes in
+ * elements unless named *_bytes, `stream` a hipStream_t as void* (NULL = the
+ * null stream), AR_OK or an AR_ERR_* code returned, the code of a failure also
+ * left in ar_last_error().  Calls are asynchronous on `stream`, allocate
+ * nothing, create no stream or event and issue no memset, so they may be
+ * captured into a HIP graph and replayed.  They keep nothing between calls and
+ * may be made from several host threads.  Matrices are row-major with a row
+ * stride (`ld_*`, elements; 0 = the number of columns; at least that number);
+ * elements of a row are contiguous.  Pointers need the alignment of their
+ * elements and no more.  Where a function takes a workspace, it is device
+ * memory of at least the bytes that the matching *_workspace function names
+ * for the same description, 256-byte aligned, owned by the caller and used
+ * until the call's work on `stream` is done (AR_ERR_SCRATCH: too small or
+ * absent).  Calls that overlap in time need workspaces of their own.
+ *
+ * Aliasing.  An output must not overlap another output or an input, but where
+ * a function says that it may be an input itself: then with the same pointer
+ * and row stride.  Column ranges of one buffer that share no element do not
+ * overlap.  AR_ERR_ARG otherwise.
+ *
+ * Arithmetic.  fp32 throughout; outputs are rounded to their type once, to
+ * nearest even.  Results
+ * depend on the inputs alone: sums are taken in a fixed order and no atomics
+ * are used, so repeated calls give the same bits.
+ */
+#ifndef AR_OPS_H
+#define AR_OPS_H
+
+#include "ar.h"
+
+#ifdef __cplusplus
+extern "C" {
+#endif
+
+/* ---- residual norm ------------------------------------------------------ */
+
+/* Per row t, with rms(v) = sqrt(mean_j v_j^2 + eps):
+ *     n = y / rms(y) * post_weight           (without AR_NORM_POST: n = y)
+ *     s = alpha * residual + gate * n        (without a gate: gate = 1)
+ *     x = s / rms(s) * pre_weight            (without AR_NORM_PRE: no x)
+ * y is a block's output (joined over the ranks), s the new residual stream, x
+ * the next block's input.  x is computed from the unrounded s.  A NULL weight
+ * stands for ones. */
+enum { AR_NORM_POST = 1, AR_NORM_PRE = 2 };
+
+typedef struct ar_norm_desc {
+    size_t rows;           /* 0 is a valid no-op (backward: zero parameter gradients) */
+    size_t cols;           /* 1 or more */
+    int dtype;             /* AR_FLOAT32 or AR_BFLOAT16: y, residual, s, x and
+                              their gradients */
+    int param_dtype;       /* the same choice for weights, gate and their gradients */
+    int flags;             /* AR_NORM_* */
+    float alpha;           /* scale of the residual; finite */
+    float eps;             /* > 0 and finite; used with AR_NORM_* */
+    size_t gate_rows;      /* 0: no gate; otherwise it divides rows, and row k
+                              of the gate (gate_rows x cols, contiguous) holds for
+                              rows / gate_rows consecutive rows: 1 = one gate for
+                              all, one per sequence, rows = one per row */
+    size_t ld_y, ld_residual, ld_s, ld_x;  /* row strides (ld_residual: also of dresidual) */
+    size_t ld_ds, ld_dx, ld_dy;            /* backward only */
+} ar_norm_desc;
+
+/* Forward.  s may be y or residual, x may be y or residual (not both the
+ * same).  Errors: AR_ERR_ARG (NULL or misaligned pointer, range, stride,
+ * overlap, gate_rows that does not divide rows), AR_ERR_UNSUPPORTED (data
+ * type), AR_ERR_HIP. */
+int ar_residual_norm(const ar_norm_desc *desc, const void *y, const void *residual, const void *post_weight,
+                     const void *gate, const void *pre_weight, void *s, void *x, void *stream);
+
+/* Backward.  From y and s of the forward, ds (gradient of s from its later
+ * uses; NULL = zero) and dx (gradient of x; NULL without AR_NORM_PRE):
+ *     G         = ds + gradient of x with regard to s, times dx
+ *     dresidual = alpha * G
+ *     dgate     = sum over the gate row's rows of G * n
+ *     dn        = G * gate
+ *     dy        = gradient of n with regard to y, times dn
+ *     dpost_weight = sum_t dn * y / rms(y),  dpre_weight = sum_t dx * s / rms(s)
+ * The norms are taken of y and s again; nothing else is kept by the forward.
+ * dpost_weight, dgate and dpre_weight may be NULL (not wanted), and must be
+ * where what they belong to is absent from the forward: a gradient for a norm
+ * without its flag, or for a gate with gate_rows 0, is AR_ERR_ARG.  A weight
+ * that stands for ones (NULL) may have a gradient.  dy and dresidual may each
+ * be y, s, ds or dx.  Workspace: partial sums of the parameter gradients. */
+int ar_residual_norm_backward(const ar_norm_desc *desc, const void *y, const void *s, const void *ds, const void *dx,
+                              const void *post_weight, const void *gate, const void *pre_weight, void *dy,
+                              void *dresidual, void *dpost_weight, void *dgate, void *dpre_weight, void *workspace,
+                              size_t workspace_bytes, void *stream);
+size_t ar_residual_norm_backward_workspace(const ar_norm_desc *desc);
+
+#ifdef __cplusplus
+}
+#endif
+
+#endif /* AR_OPS_H */

@@ -697,3 +697,7 @@ def ring_bytes(msg_bytes: int, nranks: int, dtype="f32", proto="simple", peer_di
 def compulsory_bytes(msg_bytes: int, nranks: int) -> float:
     """Lower bound for any AllReduce of N buffers in one memory: read and write each once."""
     return 2.0 * nranks * msg_bytes
+
+
+# The operators around the collectives (include/ar_ops.h).
+from .ops import residual_norm, residual_norm_backward, residual_norm_backward_workspace  # noqa: E402,F401

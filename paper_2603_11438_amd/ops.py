@@ -1,0 +1,248 @@
+"""Operators around the collectives, for torch tensors on one GPU: a thin
+layer over the C ABI in include/ar_ops.h (formulas and roundings there).
+
+    residual_norm, residual_norm_backward   norm, gate, scaled residual, norm
+
+Every step runs in the HIP library; torch provides device memory and streams.
+Tensors are checked on every call (ValueError, TypeError); what the library
+itself refuses is an ARError.  Results and workspaces are allocated by torch
+on the stream of the call (``stream``, or torch's current one); a result given
+as ``out`` is written in place.  Rows must be contiguous; the stride between
+rows is free.
+"""
+from __future__ import annotations
+
+import ctypes
+from typing import Optional
+
+import paper_2603_11438_amd as _ar
+
+AR_NORM_POST, AR_NORM_PRE = 1, 2
+
+_P, _S, _I, _F = ctypes.c_void_p, ctypes.c_size_t, ctypes.c_int, ctypes.c_float
+
+
+class ar_norm_desc(ctypes.Structure):
+    _fields_ = [("rows", _S), ("cols", _S), ("dtype", _I), ("param_dtype", _I), ("flags", _I), ("alpha", _F),
+                ("eps", _F), ("gate_rows", _S), ("ld_y", _S), ("ld_residual", _S), ("ld_s", _S), ("ld_x", _S),
+                ("ld_ds", _S), ("ld_dx", _S), ("ld_dy", _S)]
+
+
+# Every symbol include/ar_ops.h declares, with (restype, argtypes).
+SIGNATURES = {
+    "ar_residual_norm": (_I, [ctypes.POINTER(ar_norm_desc)] + [_P] * 8),
+    "ar_residual_norm_backward": (_I, [ctypes.POINTER(ar_norm_desc)] + [_P] * 13 + [_S, _P]),
+    "ar_residual_norm_backward_workspace": (_S, [ctypes.POINTER(ar_norm_desc)]),
+}
+
+_bound = None
+
+
+def _lib() -> ctypes.CDLL:
+    global _bound
+    if _bound is None:
+        L = _ar.lib()
+        for name, (res, args) in SIGNATURES.items():
+            f = getattr(L, name)
+            f.restype, f.argtypes = res, args
+        _bound = L
+    return _bound
+
+
+# ---- tensors ----------------------------------------------------------------
+
+class _On:
+    """The device and stream of a call: makes them current where they are not,
+    so that what torch allocates belongs to the call's stream."""
+
+    def __init__(self, t, stream):
+        import torch
+
+        if not t.is_cuda:
+            raise ValueError("tensors must be on the GPU")
+        self.index = t.device.index
+        if stream is not None and stream.device.index != self.index:
+            raise ValueError(f"the stream is on {stream.device}, the tensors are on {t.device}")
+        self.guard = None
+        if stream is not None:
+            self.guard = torch.cuda.stream(stream)
+        elif torch._C._cuda_getDevice() != self.index:
+            self.guard = torch.cuda.device(self.index)
+
+    def __enter__(self):
+        import torch
+
+        if self.guard is not None:
+            self.guard.__enter__()
+        self.ptr = torch._C._cuda_getCurrentRawStream(self.index)
+        return self
+
+    def __exit__(self, *exc):
+        if self.guard is not None:
+            self.guard.__exit__(*exc)
+
+
+def _rows(t, name, cols=None, rows=None, dtype=None, device=None):
+    """(rows, cols, row stride) of a tensor whose leading dimensions count rows."""
+    if not t.is_cuda or (device is not None and t.device.index != device):
+        raise ValueError(f"{name} must be on the GPU of the call")
+    if dtype is not None and t.dtype != dtype:
+        raise TypeError(f"{name} is {t.dtype}, expected {dtype}")
+    shape = t.shape
+    if not shape:
+        raise ValueError(f"{name} must have at least one dimension")
+    n, stride = shape[-1], t.stride()
+    m = 1
+    for k in shape[:-1]:
+        m *= k
+    if (cols is not None and n != cols) or (rows is not None and m != rows):
+        raise ValueError(f"{name} is {m} x {n}, expected {m if rows is None else rows} x {n if cols is None else cols}")
+    if m == 0 or n == 0:
+        return m, n, n
+    if n > 1 and stride[-1] != 1:
+        raise ValueError(f"the rows of {name} must be contiguous")
+    ld, span = n, None
+    for k, s in zip(reversed(shape[:-1]), reversed(stride[:-1])):
+        if k == 1:
+            continue
+        if span is None:
+            ld = s
+        elif s != span:
+            raise ValueError(f"the leading dimensions of {name} must have one stride between rows")
+        span = s * k
+    if ld < n:
+        raise ValueError(f"the rows of {name} must not overlap")
+    return m, n, ld
+
+
+def _param(t, name, shape, dtype, device):
+    if t is None:
+        return None
+    if not t.is_cuda or t.device.index != device or not t.is_contiguous() or tuple(t.shape) != shape:
+        raise ValueError(f"{name} must be a contiguous tensor of shape {shape} on the GPU of the call")
+    if t.dtype != dtype:
+        raise TypeError(f"{name} is {t.dtype}, expected {dtype}")
+    return t.data_ptr()
+
+
+def _ptr(t):
+    return None if t is None else t.data_ptr()
+
+
+def _workspace(nbytes, like):
+    import torch
+
+    return torch.empty(nbytes, dtype=torch.uint8, device=like.device) if nbytes else None
+
+
+# ---- residual norm ------------------------------------------------------------
+
+def _norm_desc(y, post_weight, pre_weight, gate, alpha, eps, post, pre):
+    """Description, and the pointers of the parameters (post, gate, pre)."""
+    import torch
+
+    rows, cols, ld = _rows(y, "y")
+    dev = y.device.index
+    given = [t for t in (post_weight, gate, pre_weight) if t is not None]
+    pdt = given[0].dtype if given else y.dtype
+    d = ar_norm_desc(rows=rows, cols=cols, dtype=_ar._dtype_of(y), param_dtype=_ar.AR_FLOAT32 if pdt == torch.float32 else
+                     _ar.AR_BFLOAT16, flags=(AR_NORM_POST if post else 0) | (AR_NORM_PRE if pre else 0), alpha=alpha,
+                     eps=eps, gate_rows=0, ld_y=ld)
+    if pdt not in (torch.float32, torch.bfloat16):
+        raise TypeError(f"unsupported dtype {pdt}")
+    if gate is not None:
+        d.gate_rows = 1 if gate.dim() == 1 else gate.shape[0]
+        if d.gate_rows == 0 or rows % d.gate_rows:
+            raise ValueError(f"{rows} rows cannot be shared by {d.gate_rows} rows of the gate")
+    if (post_weight is not None and not post) or (pre_weight is not None and not pre):
+        raise ValueError("a weight is given for a norm that is switched off")
+    gshape = None if gate is None else ((cols,) if gate.dim() == 1 else (d.gate_rows, cols))
+    return d, pdt, (_param(post_weight, "post_weight", (cols,), pdt, dev), _param(gate, "gate", gshape, pdt, dev),
+                    _param(pre_weight, "pre_weight", (cols,), pdt, dev))
+
+
+def residual_norm(y, residual, *, post_weight=None, pre_weight=None, gate=None, alpha: float = 1.0, eps: float = 1e-6,
+                  post: bool = True, pre: bool = True, out=None, stream=None):
+    """s = alpha * residual + gate * norm(y), x = norm(s); returns (s, x).
+
+    y and residual: (..., cols), f32 or bf16.  Weights (cols) and gate (cols, or
+    (k, cols) with row i for the i-th rows / k consecutive rows) share one type
+    of their own; one left out is ones.  post / pre switch the norm of y and
+    the norm of s off; without the latter x is None.  out: (s, x) to write to;
+    s may be y or residual, and so may x."""
+    import torch
+
+    with _On(y, stream) as on:
+        d, _, (w1, g, w2) = _norm_desc(y, post_weight, pre_weight, gate, alpha, eps, post, pre)
+        dev = on.index
+        _, _, d.ld_residual = _rows(residual, "residual", d.cols, d.rows, y.dtype, dev)
+        if out is None:
+            s, x = torch.empty_like(y, memory_format=torch.contiguous_format), None
+            if pre:
+                x = torch.empty_like(s)
+        else:
+            s, x = out
+            if (x is None) == pre:
+                raise ValueError("out is (s, x), x None where the norm of s is switched off")
+        _, _, d.ld_s = _rows(s, "s", d.cols, d.rows, y.dtype, dev)
+        if x is not None:
+            _, _, d.ld_x = _rows(x, "x", d.cols, d.rows, y.dtype, dev)
+        rc = _lib().ar_residual_norm(ctypes.byref(d), y.data_ptr(), residual.data_ptr(), w1, g, w2, s.data_ptr(), _ptr(x),
+                                     on.ptr)
+        _ar._check(rc, "ar_residual_norm")
+    return s, x
+
+
+def residual_norm_backward(y, s, ds, dx, *, post_weight=None, pre_weight=None, gate=None, alpha: float = 1.0,
+                           eps: float = 1e-6, post: bool = True, pre: bool = True, param_grads: bool = True, out=None,
+                           workspace=None, stream=None) -> dict:
+    """Gradients of residual_norm: {"dy", "dresidual", "dpost_weight",
+    "dpre_weight", "dgate"}; those of parameters that are absent, or not wanted
+    (param_grads False), are left out.
+
+    y: as in the forward call, s: its result; ds (None = zero) and dx (None
+    where x was not computed): the gradients of s and x.  out: (dy, dresidual)
+    to write to; each may be y, s, ds or dx.  workspace: a uint8 tensor to use
+    in place of a new one (residual_norm_backward_workspace)."""
+    import torch
+
+    with _On(y, stream) as on:
+        d, pdt, (w1, g, w2) = _norm_desc(y, post_weight, pre_weight, gate, alpha, eps, post, pre)
+        dev = on.index
+        _, _, d.ld_s = _rows(s, "s", d.cols, d.rows, y.dtype, dev)
+        if ds is not None:
+            _, _, d.ld_ds = _rows(ds, "ds", d.cols, d.rows, y.dtype, dev)
+        if (dx is not None) != pre:
+            raise ValueError("dx is given exactly where the norm of s is not switched off")
+        if pre:
+            _, _, d.ld_dx = _rows(dx, "dx", d.cols, d.rows, y.dtype, dev)
+        if out is None:
+            dy = torch.empty_like(y, memory_format=torch.contiguous_format)
+            dr = torch.empty_like(dy)
+        else:
+            dy, dr = out
+        _, _, d.ld_dy = _rows(dy, "dy", d.cols, d.rows, y.dtype, dev)
+        _, _, d.ld_residual = _rows(dr, "dresidual", d.cols, d.rows, y.dtype, dev)
+        grads = {"dy": dy, "dresidual": dr}
+        if param_grads:
+            for key, t in (("dpost_weight", post_weight), ("dpre_weight", pre_weight), ("dgate", gate)):
+                if t is not None:
+                    grads[key] = torch.empty_like(t)
+        ws = workspace
+        need = _lib().ar_residual_norm_backward_workspace(ctypes.byref(d)) if len(grads) > 2 else 0
+        if ws is None:
+            ws = _workspace(need, y)
+        elif not ws.is_cuda or ws.device.index != dev or not ws.is_contiguous():
+            raise ValueError("workspace must be a contiguous tensor on the GPU of the call")
+        rc = _lib().ar_residual_norm_backward(
+            ctypes.byref(d), y.data_ptr(), s.data_ptr(), _ptr(ds), _ptr(dx), w1, g, w2, dy.data_ptr(), dr.data_ptr(),
+            _ptr(grads.get("dpost_weight")), _ptr(grads.get("dgate")), _ptr(grads.get("dpre_weight")), _ptr(ws),
+            0 if ws is None else ws.numel() * ws.element_size(), on.ptr)
+        _ar._check(rc, "ar_residual_norm_backward")
+    return grads
+
+
+def residual_norm_backward_workspace(rows: int, cols: int, dtype="f32") -> int:
+    """Bytes of residual_norm_backward's workspace."""
+    d = ar_norm_desc(rows=rows, cols=cols, dtype=_ar.DTYPES[dtype], param_dtype=0, flags=3, alpha=1.0, eps=1.0)
+    return _lib().ar_residual_norm_backward_workspace(ctypes.byref(d))

@@ -1,0 +1,111 @@
+"""Host-side checks of the operators around the collectives that need no GPU:
+every call of include/ar_ops.h is exported and bound, wrong requests are
+refused before anything is launched, and the plain forms' gradients agree with
+differences."""
+from __future__ import annotations
+
+import ctypes
+import os
+import re
+
+import pytest
+import torch
+
+import paper_2603_11438_amd as ar
+from oracle import ops_oracle as oo
+from paper_2603_11438_amd import ops
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+
+
+@pytest.fixture(scope="module", autouse=True)
+def built_lib():
+    if not os.path.exists(ar.LIB_PATH):
+        import __graft_entry__
+
+        __graft_entry__.build()
+    ops._lib()
+
+
+def test_every_declared_symbol_is_exported():
+    text = open(os.path.join(ROOT, "include", "ar_ops.h")).read()
+    text = re.sub(r"/\*.*?\*/", "", text, flags=re.S)
+    names = set(re.findall(r"\b(ar_[a-z0-9_]+)\s*\(", text))
+    L = ctypes.CDLL(ar.LIB_PATH)
+    assert names == set(ops.SIGNATURES)
+    for n in names:
+        assert hasattr(L, n), n
+
+
+# Addresses that are checked and never followed: every call below is refused.
+A, B, C, D = (0x10000000 * k for k in range(1, 5))
+
+
+def norm(s=C, x=D, y=A, residual=B, w1=None, gate=None, w2=None, **kw):
+    f = dict(rows=4, cols=64, dtype=0, param_dtype=0, flags=3, alpha=1.0, eps=1e-6)
+    f.update(kw)
+    return ops._lib().ar_residual_norm(ctypes.byref(ops.ar_norm_desc(**f)), y, residual, w1, gate, w2, s, x, None)
+
+
+@pytest.mark.parametrize("kw,code", [
+    (dict(dtype=2), ar.AR_ERR_UNSUPPORTED), (dict(param_dtype=-1), ar.AR_ERR_UNSUPPORTED), (dict(cols=0), ar.AR_ERR_ARG),
+    (dict(flags=4), ar.AR_ERR_ARG), (dict(eps=0.0), ar.AR_ERR_ARG), (dict(eps=float("nan")), ar.AR_ERR_ARG),
+    (dict(alpha=float("inf")), ar.AR_ERR_ARG), (dict(gate_rows=3, gate=0x90000000), ar.AR_ERR_ARG),
+    (dict(gate_rows=2), ar.AR_ERR_ARG), (dict(ld_y=63), ar.AR_ERR_ARG), (dict(y=None), ar.AR_ERR_ARG),
+    (dict(x=None), ar.AR_ERR_ARG), (dict(s=C + 2), ar.AR_ERR_ARG), (dict(s=A + 4), ar.AR_ERR_ARG), (dict(x=C), ar.AR_ERR_ARG),
+    (dict(x=A, ld_x=65), ar.AR_ERR_ARG), (dict(w2=C + 64), ar.AR_ERR_ARG), (dict(rows=1 << 60), ar.AR_ERR_ARG)])
+def test_norm_refusals(kw, code):
+    assert norm(**kw) == code
+    assert ar.ar_last_error() == code
+
+
+def test_norm_without_rows_is_done():
+    assert norm(rows=0, y=None, s=None, x=None, residual=None) == ar.AR_OK
+
+
+def norm_bwd(ws=0xE0000000, nbytes=None, y=A, s=B, ds=None, dx=C, w1=None, gate=None, w2=None, dy=D, dr=0x50000000,
+             dw1=None, dgate=None, dw2=None, **kw):
+    f = dict(rows=4, cols=64, dtype=0, param_dtype=0, flags=3, alpha=1.0, eps=1e-6)
+    f.update(kw)
+    d = ops.ar_norm_desc(**f)
+    L = ops._lib()
+    n = L.ar_residual_norm_backward_workspace(ctypes.byref(d)) if nbytes is None else nbytes
+    return L.ar_residual_norm_backward(ctypes.byref(d), y, s, ds, dx, w1, gate, w2, dy, dr, dw1, dgate, dw2, ws, n, None)
+
+
+@pytest.mark.parametrize("kw,code", [
+    (dict(dx=None), ar.AR_ERR_ARG), (dict(dw1=0x60000000, flags=2), ar.AR_ERR_ARG), (dict(dw2=0x60000000, flags=1), ar.AR_ERR_ARG),
+    (dict(dgate=0x60000000), ar.AR_ERR_ARG), (dict(dw1=0x60000000, nbytes=8), ar.AR_ERR_SCRATCH),
+    (dict(dw1=0x60000000, ws=None), ar.AR_ERR_SCRATCH), (dict(dw1=0x60000000, ws=0xE0000010), ar.AR_ERR_ARG),
+    (dict(dw1=0x60000000, dw2=0x60000080), ar.AR_ERR_ARG), (dict(dw1=A), ar.AR_ERR_ARG), (dict(dy=A + 16), ar.AR_ERR_ARG),
+    (dict(dr=D), ar.AR_ERR_ARG), (dict(dw1=0xE0000000), ar.AR_ERR_ARG)])
+def test_norm_backward_refusals(kw, code):
+    assert norm_bwd(**kw) == code
+
+
+def test_norm_tensor_checks():
+    """CPU tensors never reach the library."""
+    t = torch.zeros(4, 8)
+    with pytest.raises(ValueError, match="GPU"):
+        ar.residual_norm(t, t)
+    with pytest.raises(ValueError, match="GPU"):
+        ar.residual_norm_backward(t, t, t, t)
+
+
+def test_norm_plain_gradient_is_the_difference():
+    torch.manual_seed(0)
+    t, d, h = 6, 16, 1e-5
+    rnd = lambda *s: torch.randn(*s, dtype=torch.float64)  # noqa: E731
+    v = dict(y=rnd(t, d), residual=rnd(t, d), w1=rnd(d), w2=rnd(d), gate=rnd(3, d))
+    ds, dx = rnd(t, d), rnd(t, d)
+
+    def loss(**u):
+        s, x, _, _ = oo.residual_norm(u["y"], u["residual"], u["w1"], u["w2"], u["gate"], 0.7, 1e-3)
+        return float((s * ds).sum() + (x * dx).sum())
+
+    s = oo.residual_norm(v["y"], v["residual"], v["w1"], v["w2"], v["gate"], 0.7, 1e-3)[0]
+    g = oo.residual_norm_backward(v["y"], s, ds, dx, v["w1"], v["w2"], v["gate"], 0.7, 1e-3)
+    for name, key in {"y": "dy", "residual": "dresidual", "w1": "dpost_weight", "w2": "dpre_weight", "gate": "dgate"}.items():
+        e = rnd(*v[name].shape)
+        fd = (loss(**{**v, name: v[name] + h * e}) - loss(**{**v, name: v[name] - h * e})) / (2 * h)
+        assert abs(fd - float((g[key][0] * e).sum())) < 1e-6 * (1 + abs(fd)), name

@@ -3,7 +3,8 @@
  *
  * A rank of a tensor-parallel program computes a block on its shard, has the
  * ranks' results joined, and adds the join to its residual stream between two
- * norms.  The joins are ar.h's collectives; around them:
+ * norms.  The joins are ar.h's collectives; the rest is here:
+ *   ar_gated_ffn       act(x Wg^T) * (x Wu^T), and its backward pass
  *   ar_residual_norm   norm of a block's output, gate, scaled residual, norm
  *                      before the next block, and its backward pass
  *
@@ -27,8 +28,8 @@
  * and row stride.  Column ranges of one buffer that share no element do not
  * overlap.  AR_ERR_ARG otherwise.
  *
- * Arithmetic.  fp32 throughout; outputs are rounded to their type once, to
- * nearest even.  Results
+ * Arithmetic.  fp32 throughout; outputs are rounded to their type once, to nearest even.  Where an operand
+ * of a matrix product is rounded on the way, the function says so.  Results
  * depend on the inputs alone: sums are taken in a fixed order and no atomics
  * are used, so repeated calls give the same bits.
  */
@@ -95,6 +96,44 @@ int ar_residual_norm_backward(const ar_norm_desc *desc, const void *y, const voi
                               void *dresidual, void *dpost_weight, void *dgate, void *dpre_weight, void *workspace,
                               size_t workspace_bytes, void *stream);
 size_t ar_residual_norm_backward_workspace(const ar_norm_desc *desc);
+
+/* ---- gated feed-forward block ------------------------------------------- */
+
+/* Activations: silu g / (1 + e^-g); gelu, the form with tanh,
+ * g/2 (1 + tanh(sqrt(2/pi) (g + 0.044715 g^3))); relu max(g, 0). */
+enum { AR_ACT_SILU = 0, AR_ACT_GELU = 1, AR_ACT_RELU = 2 };
+
+/* With G = x Wg^T and U = x Wu^T (x: tokens x dim; weights: hidden x dim):
+ *     h = act(G) * U */
+typedef struct ar_ffn_desc {
+    size_t tokens;         /* 0 is a valid no-op (backward: zero weight gradients) */
+    size_t dim, hidden;    /* 1 or more */
+    int dtype;             /* AR_BFLOAT16 */
+    int act;               /* AR_ACT_* */
+    size_t ld_x, ld_w_gate, ld_w_up, ld_h;  /* row strides (ld_h: also of dh) */
+    size_t ld_dx, ld_dw_gate, ld_dw_up;     /* backward only */
+} ar_ffn_desc;
+
+/* Forward, one kernel for both products, the activation and their product
+ * (operands that are not laid out for it, by alignment or a dim that is no
+ * multiple of 64, are first copied into the workspace).  saved: NULL, or
+ * 2 * tokens * hidden floats (16-byte aligned) that receive G and U for the
+ * backward pass, in fp32.  Errors: AR_ERR_ARG, AR_ERR_UNSUPPORTED,
+ * AR_ERR_SCRATCH, AR_ERR_HIP. */
+int ar_gated_ffn(const ar_ffn_desc *desc, const void *x, const void *w_gate, const void *w_up, void *h, float *saved,
+                 void *workspace, size_t workspace_bytes, void *stream);
+size_t ar_gated_ffn_workspace(const ar_ffn_desc *desc);
+
+/* Backward.  From `saved` of the forward and dh:
+ *     dG = dh * U * act'(G),  dU = dh * act(G)
+ *     dx = dG Wg + dU Wu,  dWg = dG^T x,  dWu = dU^T x
+ * dG and dU are computed in fp32 and rounded to bf16 as operands of these
+ * products (the matrix units' operand type).  dx, or both weight gradients,
+ * may be NULL (not wanted). */
+int ar_gated_ffn_backward(const ar_ffn_desc *desc, const void *dh, const void *x, const void *w_gate,
+                          const void *w_up, const float *saved, void *dx, void *dw_gate, void *dw_up,
+                          void *workspace, size_t workspace_bytes, void *stream);
+size_t ar_gated_ffn_backward_workspace(const ar_ffn_desc *desc);
 
 #ifdef __cplusplus
 }

@@ -1,6 +1,7 @@
 """Operators around the collectives, for torch tensors on one GPU: a thin
 layer over the C ABI in include/ar_ops.h (formulas and roundings there).
 
+    gated_ffn, gated_ffn_backward           act(x Wg^T) * (x Wu^T)
     residual_norm, residual_norm_backward   norm, gate, scaled residual, norm
 
 Every step runs in the HIP library; torch provides device memory and streams.
@@ -18,6 +19,8 @@ from typing import Optional
 import paper_2603_11438_amd as _ar
 
 AR_NORM_POST, AR_NORM_PRE = 1, 2
+AR_ACT_SILU, AR_ACT_GELU, AR_ACT_RELU = 0, 1, 2
+ACTS = {"silu": AR_ACT_SILU, "gelu": AR_ACT_GELU, "relu": AR_ACT_RELU}
 
 _P, _S, _I, _F = ctypes.c_void_p, ctypes.c_size_t, ctypes.c_int, ctypes.c_float
 
@@ -28,11 +31,20 @@ class ar_norm_desc(ctypes.Structure):
                 ("ld_ds", _S), ("ld_dx", _S), ("ld_dy", _S)]
 
 
+class ar_ffn_desc(ctypes.Structure):
+    _fields_ = [("tokens", _S), ("dim", _S), ("hidden", _S), ("dtype", _I), ("act", _I), ("ld_x", _S),
+                ("ld_w_gate", _S), ("ld_w_up", _S), ("ld_h", _S), ("ld_dx", _S), ("ld_dw_gate", _S), ("ld_dw_up", _S)]
+
+
 # Every symbol include/ar_ops.h declares, with (restype, argtypes).
 SIGNATURES = {
     "ar_residual_norm": (_I, [ctypes.POINTER(ar_norm_desc)] + [_P] * 8),
     "ar_residual_norm_backward": (_I, [ctypes.POINTER(ar_norm_desc)] + [_P] * 13 + [_S, _P]),
     "ar_residual_norm_backward_workspace": (_S, [ctypes.POINTER(ar_norm_desc)]),
+    "ar_gated_ffn": (_I, [ctypes.POINTER(ar_ffn_desc)] + [_P] * 6 + [_S, _P]),
+    "ar_gated_ffn_workspace": (_S, [ctypes.POINTER(ar_ffn_desc)]),
+    "ar_gated_ffn_backward": (_I, [ctypes.POINTER(ar_ffn_desc)] + [_P] * 9 + [_S, _P]),
+    "ar_gated_ffn_backward_workspace": (_S, [ctypes.POINTER(ar_ffn_desc)]),
 }
 
 _bound = None
@@ -246,3 +258,91 @@ def residual_norm_backward_workspace(rows: int, cols: int, dtype="f32") -> int:
     """Bytes of residual_norm_backward's workspace."""
     d = ar_norm_desc(rows=rows, cols=cols, dtype=_ar.DTYPES[dtype], param_dtype=0, flags=3, alpha=1.0, eps=1.0)
     return _lib().ar_residual_norm_backward_workspace(ctypes.byref(d))
+
+
+# ---- gated feed-forward block -------------------------------------------------
+
+def _ffn_desc(x, w_gate, w_up, act):
+    if act not in ACTS:
+        raise ValueError(f"unknown activation {act!r}: one of {sorted(ACTS)}")
+    tokens, dim, ld_x = _rows(x, "x")
+    dev = x.device.index
+    if w_gate.dim() != 2 or w_up.dim() != 2:
+        raise ValueError("the weights must be matrices")
+    hidden, _, ld_g = _rows(w_gate, "w_gate", dim, None, x.dtype, dev)
+    _, _, ld_u = _rows(w_up, "w_up", dim, hidden, x.dtype, dev)
+    return ar_ffn_desc(tokens=tokens, dim=dim, hidden=hidden, dtype=_ar._dtype_of(x), act=ACTS[act], ld_x=ld_x,
+                       ld_w_gate=ld_g, ld_w_up=ld_u)
+
+
+def gated_ffn(x, w_gate, w_up, *, act: str = "silu", save: bool = False, out=None, stream=None):
+    """h = act(x w_gate^T) * (x w_up^T), bf16; with save also what
+    gated_ffn_backward needs: (h, saved).
+
+    x: (..., dim); weights: (hidden, dim), which may be halves of one tensor;
+    act: "silu", "gelu" (the form with tanh) or "relu"; out: h to write to.
+    saved: (2, tokens, hidden) fp32, both projections."""
+    import torch
+
+    with _On(x, stream) as on:
+        d = _ffn_desc(x, w_gate, w_up, act)
+        h = out
+        if h is None:
+            h = torch.empty(*x.shape[:-1], d.hidden, dtype=x.dtype, device=x.device)
+        _, _, d.ld_h = _rows(h, "h", d.hidden, d.tokens, x.dtype, on.index)
+        saved = torch.empty(2, d.tokens, d.hidden, dtype=torch.float32, device=x.device) if save else None
+        L = _lib()
+        ws = None
+        rc = L.ar_gated_ffn(ctypes.byref(d), x.data_ptr(), w_gate.data_ptr(), w_up.data_ptr(), h.data_ptr(), _ptr(saved),
+                            None, 0, on.ptr)
+        if rc == _ar.AR_ERR_SCRATCH:  # only operands that have to be laid out need one
+            ws = _workspace(L.ar_gated_ffn_workspace(ctypes.byref(d)), x)
+            rc = L.ar_gated_ffn(ctypes.byref(d), x.data_ptr(), w_gate.data_ptr(), w_up.data_ptr(), h.data_ptr(), _ptr(saved),
+                                _ptr(ws), ws.numel(), on.ptr)
+        _ar._check(rc, "ar_gated_ffn")
+    return (h, saved) if save else h
+
+
+def gated_ffn_backward(dh, x, w_gate, w_up, saved, *, act: str = "silu", need_dx: bool = True, need_dw: bool = True,
+                       out=None, workspace=None, stream=None):
+    """Gradients of gated_ffn with regard to x and both weights: (dx, dw_gate,
+    dw_up); None for those not needed (need_dx, need_dw).
+
+    saved: from gated_ffn(save=True) on the same x and weights.  out: the three
+    results to write to.  workspace: a uint8 tensor to use in place of a new one
+    (gated_ffn_backward_workspace)."""
+    import torch
+
+    with _On(x, stream) as on:
+        d = _ffn_desc(x, w_gate, w_up, act)
+        dev = on.index
+        _, _, d.ld_h = _rows(dh, "dh", d.hidden, d.tokens, x.dtype, dev)
+        if (not saved.is_cuda or saved.device.index != dev or saved.dtype != torch.float32 or not saved.is_contiguous()
+                or tuple(saved.shape) != (2, d.tokens, d.hidden)):
+            raise ValueError("saved must be what gated_ffn(save=True) returned for this x and these weights")
+        dx, dg, du = (None, None, None) if out is None else out
+        if need_dx:
+            dx = torch.empty_like(x, memory_format=torch.contiguous_format) if dx is None else dx
+            _, _, d.ld_dx = _rows(dx, "dx", d.dim, d.tokens, x.dtype, dev)
+        if need_dw:
+            dg = torch.empty(d.hidden, d.dim, dtype=x.dtype, device=x.device) if dg is None else dg
+            du = torch.empty_like(dg, memory_format=torch.contiguous_format) if du is None else du
+            _, _, d.ld_dw_gate = _rows(dg, "dw_gate", d.dim, d.hidden, x.dtype, dev)
+            _, _, d.ld_dw_up = _rows(du, "dw_up", d.dim, d.hidden, x.dtype, dev)
+        L, ws = _lib(), workspace
+        if ws is None:
+            ws = _workspace(L.ar_gated_ffn_backward_workspace(ctypes.byref(d)), x)
+        elif not ws.is_cuda or ws.device.index != dev or not ws.is_contiguous():
+            raise ValueError("workspace must be a contiguous tensor on the GPU of the call")
+        rc = L.ar_gated_ffn_backward(
+            ctypes.byref(d), dh.data_ptr(), x.data_ptr(), w_gate.data_ptr(), w_up.data_ptr(), saved.data_ptr(),
+            _ptr(dx) if need_dx else None, _ptr(dg) if need_dw else None, _ptr(du) if need_dw else None, _ptr(ws),
+            0 if ws is None else ws.numel() * ws.element_size(), on.ptr)
+        _ar._check(rc, "ar_gated_ffn_backward")
+    return dx if need_dx else None, dg if need_dw else None, du if need_dw else None
+
+
+def gated_ffn_backward_workspace(tokens: int, dim: int, hidden: int) -> int:
+    """Bytes of gated_ffn_backward's workspace."""
+    d = ar_ffn_desc(tokens=tokens, dim=dim, hidden=hidden, dtype=_ar.AR_BFLOAT16)
+    return _lib().ar_gated_ffn_backward_workspace(ctypes.byref(d))

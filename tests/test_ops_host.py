@@ -109,3 +109,67 @@ def test_norm_plain_gradient_is_the_difference():
         e = rnd(*v[name].shape)
         fd = (loss(**{**v, name: v[name] + h * e}) - loss(**{**v, name: v[name] - h * e})) / (2 * h)
         assert abs(fd - float((g[key][0] * e).sum())) < 1e-6 * (1 + abs(fd)), name
+
+
+def ffn(x=A, wg=B, wu=C, h=D, saved=None, ws=None, nbytes=0, **kw):
+    f = dict(tokens=4, dim=64, hidden=32, dtype=1, act=0)
+    f.update(kw)
+    return ops._lib().ar_gated_ffn(ctypes.byref(ops.ar_ffn_desc(**f)), x, wg, wu, h, saved, ws, nbytes, None)
+
+
+@pytest.mark.parametrize("kw,code", [
+    (dict(dtype=0), ar.AR_ERR_UNSUPPORTED), (dict(dtype=7), ar.AR_ERR_UNSUPPORTED), (dict(act=3), ar.AR_ERR_ARG),
+    (dict(dim=0), ar.AR_ERR_ARG), (dict(hidden=0), ar.AR_ERR_ARG), (dict(tokens=1 << 31), ar.AR_ERR_ARG),
+    (dict(ld_x=60), ar.AR_ERR_ARG), (dict(ld_h=31), ar.AR_ERR_ARG), (dict(x=None), ar.AR_ERR_ARG), (dict(wu=C + 1), ar.AR_ERR_ARG),
+    (dict(h=A), ar.AR_ERR_ARG), (dict(h=C + 2), ar.AR_ERR_ARG), (dict(saved=0x90000004), ar.AR_ERR_ARG), (dict(saved=A), ar.AR_ERR_ARG),
+    (dict(saved=D), ar.AR_ERR_ARG), (dict(dim=60), ar.AR_ERR_SCRATCH), (dict(x=A + 2), ar.AR_ERR_SCRATCH),
+    (dict(ld_w_up=65), ar.AR_ERR_SCRATCH), (dict(dim=60, ws=0x90000000, nbytes=100), ar.AR_ERR_SCRATCH),
+    (dict(dim=60, ws=0x90000008, nbytes=1 << 20), ar.AR_ERR_ARG), (dict(dim=60, ws=A, nbytes=1 << 20), ar.AR_ERR_ARG)])
+def test_ffn_refusals(kw, code):
+    assert ffn(**kw) == code
+    assert ar.ar_last_error() == code
+
+
+def ffn_bwd(dh=A, x=B, wg=C, wu=D, saved=0x50000000, dx=0x60000000, dwg=0x70000000, dwu=0x80000000, ws=0x90000000,
+            nbytes=None, **kw):
+    f = dict(tokens=4, dim=64, hidden=32, dtype=1, act=0)
+    f.update(kw)
+    d = ops.ar_ffn_desc(**f)
+    L = ops._lib()
+    n = L.ar_gated_ffn_backward_workspace(ctypes.byref(d)) if nbytes is None else nbytes
+    return L.ar_gated_ffn_backward(ctypes.byref(d), dh, x, wg, wu, saved, dx, dwg, dwu, ws, n, None)
+
+
+@pytest.mark.parametrize("kw,code", [
+    (dict(saved=None), ar.AR_ERR_ARG), (dict(dwg=None), ar.AR_ERR_ARG), (dict(ws=None), ar.AR_ERR_SCRATCH),
+    (dict(nbytes=1024), ar.AR_ERR_SCRATCH), (dict(ws=0x90000010), ar.AR_ERR_ARG), (dict(dx=B), ar.AR_ERR_ARG),
+    (dict(dwg=0x80000800), ar.AR_ERR_ARG), (dict(dx=0x90000000), ar.AR_ERR_ARG), (dict(saved=0x90000000), ar.AR_ERR_ARG),
+    (dict(ld_dx=63), ar.AR_ERR_ARG), (dict(dh=A + 1), ar.AR_ERR_ARG)])
+def test_ffn_backward_refusals(kw, code):
+    assert ffn_bwd(**kw) == code
+
+
+def test_ffn_without_tokens_is_done():
+    assert ffn(tokens=0, x=None, h=None) == ar.AR_OK
+    assert ffn_bwd(tokens=0, dx=None, dwg=None, dwu=None, ws=None) == ar.AR_OK
+
+
+def test_ffn_tensor_checks():
+    t = torch.zeros(4, 8, dtype=torch.bfloat16)
+    with pytest.raises(ValueError, match="GPU"):
+        ar.gated_ffn(t, t, t)
+    with pytest.raises(ValueError, match="GPU"):
+        ar.gated_ffn_backward(t, t, t, t, t)
+
+
+@pytest.mark.parametrize("act", ("silu", "gelu", "relu"))
+def test_ffn_plain_gradient_is_the_difference(act):
+    torch.manual_seed(1)
+    rnd = lambda *s: torch.randn(*s, dtype=torch.float64)  # noqa: E731
+    v, dh, h = dict(x=rnd(5, 8), wg=rnd(6, 8), wu=rnd(6, 8)), rnd(5, 6), 1e-6
+    loss = lambda u: float((dh * oo.gated_ffn(u["x"], u["wg"], u["wu"], act)[0]).sum())  # noqa: E731
+    grads = oo.gated_ffn_backward(dh, v["x"], v["wg"], v["wu"], act)
+    for name, g in zip(("x", "wg", "wu"), grads):
+        e = rnd(*v[name].shape)
+        fd = (loss({**v, name: v[name] + h * e}) - loss({**v, name: v[name] - h * e})) / (2 * h)
+        assert abs(fd - float((g * e).sum())) < 1e-6 * (1 + abs(fd)), name

@@ -1,12 +1,14 @@
 /*
  * ar_ops.h -- C ABI of the operators around libar's collectives (gfx950).
  *
- * A rank of a tensor-parallel program computes a block on its shard, has the
- * ranks' results joined, and adds the join to its residual stream between two
- * norms.  The joins are ar.h's collectives; the rest is here:
+ * A rank of a tensor- or data-parallel program computes a block on its shard,
+ * has the ranks' results joined, adds the join to its residual stream between
+ * two norms, and turns joined gradients into weight updates.  The joins are
+ * ar.h's collectives; the rest is here:
  *   ar_gated_ffn       act(x Wg^T) * (x Wu^T), and its backward pass
  *   ar_residual_norm   norm of a block's output, gate, scaled residual, norm
  *                      before the next block, and its backward pass
+ *   ar_orthogonalize   Newton-Schulz products that orthogonalise an update
  *
  * Conventions.  As in ar.h: device pointers on the current device, sizes in
  * elements unless named *_bytes, `stream` a hipStream_t as void* (NULL = the
@@ -28,7 +30,8 @@
  * and row stride.  Column ranges of one buffer that share no element do not
  * overlap.  AR_ERR_ARG otherwise.
  *
- * Arithmetic.  fp32 throughout; outputs are rounded to their type once, to nearest even.  Where an operand
+ * Arithmetic.  fp32 throughout (sums of squares of ar_orthogonalize in fp64);
+ * outputs are rounded to their type once, to nearest even.  Where an operand
  * of a matrix product is rounded on the way, the function says so.  Results
  * depend on the inputs alone: sums are taken in a fixed order and no atomics
  * are used, so repeated calls give the same bits.
@@ -134,6 +137,44 @@ int ar_gated_ffn_backward(const ar_ffn_desc *desc, const void *dh, const void *x
                           const void *w_up, const float *saved, void *dx, void *dw_gate, void *dw_up,
                           void *workspace, size_t workspace_bytes, void *stream);
 size_t ar_gated_ffn_backward_workspace(const ar_ffn_desc *desc);
+
+/* ---- orthogonalised updates --------------------------------------------- */
+
+#define AR_ORTHO_MAX_STEPS 16
+
+/* For each of `batch` matrices M (rows x cols):
+ *     X = M / (|M|_F + eps)                       (of M^T where rows > cols)
+ *     steps times, with the step's (a, b, c):
+ *         A = X X^T,  B = b A + c A A,  X = a X + B X
+ *     out = scale * X                              (its transpose there)
+ * Each step takes every singular value v to a v + b v^3 + c v^5; with the
+ * usual coefficients all come near 1 within five steps. */
+typedef struct ar_ortho_desc {
+    size_t batch;          /* matrices; 0 is a valid no-op */
+    size_t rows, cols;     /* 1 .. 65536 */
+    int dtype;             /* AR_FLOAT32 or AR_BFLOAT16: input and output */
+    int steps;             /* 1 .. AR_ORTHO_MAX_STEPS */
+    const float *coefs;    /* host memory: a, b, c of each step (3 * steps) */
+    float eps;             /* 0 or more; finite */
+    float scale;           /* finite */
+    size_t ld_in, ld_out;  /* row strides */
+    size_t stride_in, stride_out;  /* elements between matrices; 0 = rows * ld */
+} ar_ortho_desc;
+
+/* out may be `in`.  Operands of the products are held in fp16 planes with
+ * power-of-two scales.  fp32, and bf16 with a short side of at most 256: two
+ * planes (22 bits) and three products, about fp32's accuracy.  Other bf16:
+ * products of one plane (11 bits), with the diagonals of A and B and the a X
+ * term kept apart from it in fp32 and in two planes; the result's error before
+ * its rounding to bf16 is below half a bf16 unit.  A matrix of zeros gives
+ * zeros; one with an infinity or NaN gives NaN throughout.  AR_ERR_ARG also
+ * for coefficients that are not finite or take singular values in [0, 1]
+ * beyond 2^12 on the way.  Matrices of a batch may lie one after another or
+ * side by side in shared rows, without sharing elements.  Workspace: the
+ * planes. */
+int ar_orthogonalize(const ar_ortho_desc *desc, const void *in, void *out, void *workspace, size_t workspace_bytes,
+                     void *stream);
+size_t ar_orthogonalize_workspace(const ar_ortho_desc *desc);
 
 #ifdef __cplusplus
 }

@@ -700,5 +700,5 @@ def compulsory_bytes(msg_bytes: int, nranks: int) -> float:
 
 
 # The operators around the collectives (include/ar_ops.h).
-from .ops import (gated_ffn, gated_ffn_backward, gated_ffn_backward_workspace, residual_norm, residual_norm_backward,  # noqa: E402,F401
-                  residual_norm_backward_workspace)
+from .ops import (gated_ffn, gated_ffn_backward, gated_ffn_backward_workspace, orthogonalize,  # noqa: E402,F401
+                  orthogonalize_workspace, residual_norm, residual_norm_backward, residual_norm_backward_workspace)

@@ -269,8 +269,8 @@ template <typename O, int COLS, typename V, typename R>
 __device__ __forceinline__ void store_32_rows(char *lds, uint32_t cols, V value, R row)
 {
     constexpr int E = sizeof(O), PITCH = COLS * E + 16, PER = 16 / E;  // elements a lane stores at once
-    constexpr int LANES = COLS / PER, ROWS = 64 / LANES;
-    static_assert(COLS % PER == 0 && 64 % LANES == 0, "whole rows of lanes");
+    constexpr int LANES = COLS / PER;  // of a row
+    static_assert(COLS % PER == 0 && 32 * LANES % 64 == 0, "whole rows and waves");
     const uint32_t lane = threadIdx.x & 63u;
     typedef O O4 __attribute__((ext_vector_type(4)));
 #pragma unroll
@@ -283,10 +283,9 @@ __device__ __forceinline__ void store_32_rows(char *lds, uint32_t cols, V value,
             *(O4 *)(lds + (lane & 31u) * PITCH + (j * 32 + q * 8 + (lane >> 5) * 4) * E) = v;
         }
     asm volatile("" ::: "memory");
-    const uint32_t c = lane % LANES * PER;
 #pragma unroll
-    for (int r0 = 0; r0 < 32; r0 += ROWS) {
-        const uint32_t r = r0 + lane / LANES;
+    for (int k0 = 0; k0 < 32 * LANES; k0 += 64) {
+        const uint32_t r = (k0 + lane) / LANES, c = (k0 + lane) % LANES * PER;
         O *to = row(r);
         const O *from = (const O *)(lds + r * PITCH) + c;
         if (to) {

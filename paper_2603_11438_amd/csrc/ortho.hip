@@ -1,0 +1,635 @@
+// Newton-Schulz orthogonalisation (gfx950): steps of three matrix products,
+//     A = X X^T,  B = b A + c A A,  X = a X + B X   (ar_ops.h),
+// on the matrix units through gemm_nt.h, with fp16 operands and fp32 sums.
+//
+// Operands.  A value v is held as hi = fp16(v s) and lo = fp16(v s - hi) with a
+// power of two s chosen from a bound on |v|: 11 bits, or 22 with lo.
+//   fp32 matrices: products of hi and lo, hi hi + hi lo + lo hi, and X also in
+//   fp32 for the a X term.
+//   bf16 matrices: products of hi alone, one third of the work.  What a single
+//   plane would lose is kept out of the products: X itself has both planes for
+//   the a X term (a strong direction's rounding error would otherwise swamp
+//   weak directions, which the steps amplify up to a^steps = 485 times), and
+//   the diagonals of A and B, on which most of their norm sits, stay in fp32:
+//   with A = D + O, D diagonal,
+//     A A = D D + D O + O D + O O,   a X + B X = (a + diag B) X + (B - diag B) X.
+//   The result's error before its rounding to bf16 is 0.5e-3 to 0.9e-3 of its
+//   norm (bf16's own rounding 1.7e-3); without the two measures up to 1.8e-2.
+//   Small matrices, whose few singular values do not average such errors, take
+//   two planes in bf16 too.
+//
+// A and B are symmetric: only tiles on and below the diagonal are computed and
+// written to both places.  X is also kept transposed, as the second operand of
+// B X; tall matrices are transposed on the way in and out.
+#include <type_traits>
+
+#include "gemm_nt.h"
+
+#pragma clang fp contract(fast)
+
+namespace ar {
+namespace dev {
+
+constexpr uint32_t kNormParts = 256;  // partial sums of squares of a matrix, at most
+
+// Scales of one step: X in (2^14 for the input), A, B, and the factor that the
+// step's X planes stand to the true X (1 but for the first step).
+struct Scales {
+    float x, a, b, tau;
+};
+
+// One matrix' part of the workspace, in bytes.
+struct OrthoSpace {
+    size_t xh, xl, xf, xt[2], xt_lo, a, a_lo, b, b_lo, diag_a, diag_b, scales, norms, bytes;
+};
+
+struct OrthoArgs {
+    const void *in;
+    void *out;
+    char *ws;
+    OrthoSpace at;
+    uint64_t ld_in, ld_out, stride_in, stride_out;
+    uint32_t m, n, mp, np;       // rows <= columns, and both in multiples of 64
+    uint32_t batch, norm_parts, step, steps;
+    int tall;                    // the matrix is the transpose
+    float a, b, c, eps, scale;
+    // bound of |X| after k steps, and of its growth from |X| = tau, for
+    // singular values up to 1 (tau)
+    float bound[AR_ORTHO_MAX_STEPS + 1], growth[AR_ORTHO_MAX_STEPS + 1];
+    float abs_b[AR_ORTHO_MAX_STEPS], abs_c[AR_ORTHO_MAX_STEPS];
+};
+
+// ---- the norm ---------------------------------------------------------------
+
+// Sums of squares in fp64: any fp32 matrix' norm is in range.  One wave a row.
+template <typename T> __global__ __launch_bounds__(256) void ortho_norm_kernel(const OrthoArgs o)
+{
+    constexpr int VEC = 16 / (int)sizeof(T);
+    __shared__ double sums[4];
+    const uint32_t rows = o.tall ? o.n : o.m, cols = o.tall ? o.m : o.n;
+    const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6;
+    const T *in = (const T *)o.in + blockIdx.y * o.stride_in;
+    double sum = 0.0;
+    for (uint32_t r = blockIdx.x * 4 + wave; r < rows; r += gridDim.x * 4) {
+        const T *row = in + (uint64_t)r * o.ld_in;
+        for (uint32_t c = lane * VEC; c < cols; c += 64 * VEC) {
+            float v[VEC];
+            if (c + VEC <= cols) load_vec<T, VEC>(row + c, v);
+            else load_part<T, VEC>(row + c, (int)(cols - c), v);
+#pragma unroll
+            for (int k = 0; k < VEC; ++k) sum += (double)v[k] * (double)v[k];
+        }
+    }
+#pragma unroll
+    for (int d = 32; d; d >>= 1) sum += __shfl_xor(sum, d);
+    if (lane == 0) sums[wave] = sum;
+    __syncthreads();
+    if (threadIdx.x == 0)
+        ((double *)(o.ws + blockIdx.y * o.at.bytes + o.at.norms))[blockIdx.x] = sums[0] + sums[1] + sums[2] + sums[3];
+}
+
+// 2^(14 - e) for the least e with bound <= 2^e, the exponent kept within what
+// an fp32 scale and its inverse hold.
+__device__ __forceinline__ float scale_for(float bound)
+{
+    int e = bound > 0.0f ? ilogbf(bound) + 1 : -100;
+    e = e < -100 ? -100 : e > 100 ? 100 : e;
+    return ldexpf(1.0f, 14 - e);
+}
+
+// X's planes, both ways round, from the input: X = M / 2^e with the norm of M
+// between 2^(e-1) and 2^e, which is exact; the rest of the normalisation is the
+// first step's tau.  Tiles of 64 x 64.
+template <typename T, int PLANES> __global__ __launch_bounds__(256) void ortho_enter_kernel(const OrthoArgs o)
+{
+    __shared__ float tile[64][65];
+    __shared__ double total[4];
+    char *ws = o.ws + blockIdx.z * o.at.bytes;
+    const double *parts = (const double *)(ws + o.at.norms);
+    double sum = threadIdx.x < o.norm_parts ? parts[threadIdx.x] : 0.0;
+#pragma unroll
+    for (int d = 32; d; d >>= 1) sum += __shfl_xor(sum, d);
+    if ((threadIdx.x & 63u) == 0) total[threadIdx.x >> 6] = sum;
+    __syncthreads();
+    const double norm = sqrt(total[0] + total[1] + total[2] + total[3]);
+    int e = 0;
+    if (norm > 0.0) frexp(norm, &e);  // norm = f 2^e, f in [1/2, 1)
+    const bool finite = norm <= 1.7976931348623157e308;
+    if (blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x <= o.steps) {
+        const int k = (int)threadIdx.x;
+        const float tau = !finite ? __builtin_nanf("") : norm > 0.0 ? (float)(ldexp(1.0, e) / (norm + (double)o.eps)) : 1.0f;
+        const float bound = fminf(o.bound[k], tau * o.growth[k]);
+        const float sq = bound * bound;
+        Scales s;
+        s.x = k == 0 ? 16384.0f : scale_for(bound);
+        s.a = scale_for(sq);
+        s.b = k < (int)o.steps ? scale_for(o.abs_b[k] * sq + o.abs_c[k] * sq * sq) : 1.0f;
+        s.tau = k == 0 ? tau : 1.0f;
+        ((Scales *)(ws + o.at.scales))[k] = s;
+    }
+    // the tile of the input that becomes rows i0.., columns j0.. of X
+    const uint32_t i0 = blockIdx.y * 64, j0 = blockIdx.x * 64;
+    const uint32_t r0 = o.tall ? j0 : i0, c0 = o.tall ? i0 : j0, rows = o.tall ? o.n : o.m, cols = o.tall ? o.m : o.n;
+    const T *in = (const T *)o.in + blockIdx.z * o.stride_in;
+    for (uint32_t k = threadIdx.x; k < 512; k += 256) {
+        const uint32_t r = k / 8, c = k % 8 * 8;
+        float v[8];
+        const T *from = in + (uint64_t)(r0 + r) * o.ld_in + c0 + c;
+        if (r0 + r < rows && c0 + c + 8 <= cols) load_vec<T, 8>(from, v);
+        else load_part<T, 8>(from, r0 + r < rows && c0 + c < cols ? (int)(cols - c0 - c) : 0, v);
+#pragma unroll
+        for (int q = 0; q < 8; ++q) {
+            // in two factors: 2^(14-e) alone may leave fp32's range
+            const float x = finite ? ldexpf(ldexpf(v[q], -e / 2), 14 - e + e / 2) : __builtin_nanf("");
+            if (o.tall) tile[c + q][r] = x;
+            else tile[r][c + q] = x;
+        }
+    }
+    __syncthreads();
+    for (uint32_t k = threadIdx.x; k < 512; k += 256) {
+        const uint32_t r = k / 8, c = k % 8 * 8;
+        f16x8 h, l, th, tl;
+#pragma unroll
+        for (int q = 0; q < 8; ++q) {
+            const float x = tile[r][c + q], t = tile[c + q][r];
+            h[q] = (f16)x, l[q] = (f16)(x - (float)h[q]);
+            th[q] = (f16)t, tl[q] = (f16)(t - (float)th[q]);
+        }
+        const size_t x_at = ((size_t)(i0 + r) * o.np + j0 + c) * 2, t_at = ((size_t)(j0 + r) * o.mp + i0 + c) * 2;
+        *(f16x8 *)(ws + o.at.xh + x_at) = h;
+        *(f16x8 *)(ws + o.at.xl + x_at) = l;
+        *(f16x8 *)(ws + o.at.xt[0] + t_at) = th;
+        if (PLANES == 2) {
+            *(f16x8 *)(ws + o.at.xt[0] + o.at.xt_lo + t_at) = tl;
+            store_vec<float, 8>((float *)(ws + o.at.xf + x_at * 2), &tile[r][c]);
+        }
+    }
+}
+
+// ---- the products -----------------------------------------------------------
+
+// Writes a wave's 32 x COLS block transposed: value(j, r) as in store_32_rows,
+// row(c): where column c goes (its element of the block's first row) or null;
+// `rows` of the 32 are written.
+template <typename O, int COLS, typename V, typename R>
+__device__ __forceinline__ void store_32_cols(char *lds, uint32_t rows, V value, R row)
+{
+    constexpr int E = sizeof(O), PER = 16 / E, PITCH = 32 * E + 16, LANES = 32 / PER;
+    const uint32_t lane = threadIdx.x & 63u;
+#pragma unroll
+    for (int j = 0; j < COLS / 32; ++j)
+#pragma unroll
+        for (int r = 0; r < 16; ++r)
+            *(O *)(lds + (j * 32 + r / 4 * 8 + (lane >> 5) * 4 + r % 4) * PITCH + (lane & 31u) * E) = (O)value(j, r);
+    asm volatile("" ::: "memory");
+    const uint32_t c = lane % LANES * PER;
+    static_assert(64 % LANES == 0 && COLS % (64 / LANES) == 0, "whole waves");
+#pragma unroll
+    for (int k0 = 0; k0 < COLS; k0 += 64 / LANES) {
+        const uint32_t k = k0 + lane / LANES;
+        O *to = row(k);
+        const O *from = (const O *)(lds + k * PITCH) + c;
+        if (to) {
+            if (c + PER <= rows) {
+                typedef O OV __attribute__((ext_vector_type(PER)));
+                typedef O OU __attribute__((ext_vector_type(PER), aligned(E)));
+                *(OU *)(to + c) = *(const OV *)from;
+            } else {
+                for (uint32_t q = c; q < rows; ++q) to[q] = from[q - c];
+            }
+        }
+    }
+    asm volatile("" ::: "memory");
+}
+template <typename O, int COLS> constexpr int kStageColBytes = COLS * (32 * (int)sizeof(O) + 16);
+
+// A wave's place in its tile.
+template <int T> struct WaveAt {
+    uint32_t row0, col0, row, half;
+    __device__ __forceinline__ WaveAt(const TileAt at)
+    {
+        const uint32_t lane = threadIdx.x & 63u, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+        row0 = at.m * T * 64 + (wave >> 1) * T * 32, col0 = at.n * T * 64 + (wave & 1u) * T * 32;
+        row = lane & 31u, half = (lane >> 5) * 4;
+    }
+    __device__ __forceinline__ uint32_t i(int bi) const { return row0 + bi * 32 + row; }
+    __device__ __forceinline__ uint32_t j(int bj, int r) const { return col0 + bj * 32 + r / 4 * 8 + half + r % 4; }
+};
+
+// The planes of a scaled matrix from the accumulators, rows and columns up to
+// the padded sizes.
+template <int T, int PLANES>
+__device__ __forceinline__ void store_planes(char *stage, const f32x16 (&acc)[T][T], const WaveAt<T> &w, char *hi, char *lo,
+                                             uint32_t rows, uint32_t cols, uint32_t ld)
+{
+    if (w.col0 >= cols) return;
+#pragma unroll
+    for (int bi = 0; bi < T; ++bi) {
+        auto to = [&](char *base) {
+            return [=](uint32_t r) {
+                const uint32_t i = w.row0 + bi * 32 + r;
+                return i < rows ? (f16 *)base + (uint64_t)i * ld + w.col0 : nullptr;
+            };
+        };
+        store_32_rows<f16, T * 32>(stage, cols - w.col0, [&](int j, int r) { return acc[bi][j][r]; }, to(hi));
+        if (PLANES == 2)
+            store_32_rows<f16, T * 32>(stage, cols - w.col0,
+                                       [&](int j, int r) { return acc[bi][j][r] - (float)(f16)acc[bi][j][r]; }, to(lo));
+    }
+}
+template <int T, int PLANES>
+__device__ __forceinline__ void store_planes_transposed(char *stage, const f32x16 (&acc)[T][T], const WaveAt<T> &w, char *hi,
+                                                        char *lo, uint32_t rows, uint32_t cols, uint32_t ld)
+{
+    // cols: of the result, that is rows of the block
+#pragma unroll
+    for (int bi = 0; bi < T; ++bi) {
+        const uint32_t first = w.row0 + bi * 32;
+        if (first >= cols) break;
+        auto to = [&](char *base) {
+            return [=](uint32_t c) {
+                const uint32_t j = w.col0 + c;
+                return j < rows ? (f16 *)base + (uint64_t)j * ld + first : nullptr;
+            };
+        };
+        store_32_cols<f16, T * 32>(stage, cols - first, [&](int j, int r) { return acc[bi][j][r]; }, to(hi));
+        if (PLANES == 2)
+            store_32_cols<f16, T * 32>(stage, cols - first,
+                                       [&](int j, int r) { return acc[bi][j][r] - (float)(f16)acc[bi][j][r]; }, to(lo));
+    }
+}
+
+template <int T> constexpr int kOrthoStage = kStageColBytes<float, T * 32> > kStageBytes<float, T * 32>
+                                                 ? kStageColBytes<float, T * 32> : kStageBytes<float, T * 32>;
+template <int T> constexpr int kOrthoLds = kGemmLds<T, T> > 4 * kOrthoStage<T> ? kGemmLds<T, T> : 4 * kOrthoStage<T>;
+
+// A = X X^T (SECOND false) or B = b A + c A A (true): tiles on and below the
+// diagonal, written to both places; the diagonal goes to its fp32 vector and
+// is zero in the planes.
+template <int T, int PLANES, bool SECOND>
+__global__ __launch_bounds__(256, 1) void ortho_square_kernel(const GemmArgs g, const OrthoArgs o)
+{
+    extern __shared__ __attribute__((aligned(16))) char lds[];
+    const TileAt at = tile_at_lower(g.tiles_m, g.batch);
+    f32x16 acc[T][T];
+    gemm_tile<f16, T, T, false>(g, at, lds, acc);
+    const WaveAt<T> w(at);
+    char *ws = o.ws + at.batch * o.at.bytes;
+    const Scales s = ((const Scales *)(ws + o.at.scales))[o.step];
+    float *diag_a = (float *)(ws + o.at.diag_a), *diag_b = (float *)(ws + o.at.diag_b);
+    const float sx = s.tau / s.x, ia = 1.0f / s.a;
+#pragma unroll
+    for (int bi = 0; bi < T; ++bi) {
+        const uint32_t i = w.i(bi);
+        const float di = SECOND && i < o.m ? diag_a[i] : 0.0f;
+#pragma unroll
+        for (int bj = 0; bj < T; ++bj)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const uint32_t j0 = w.j(bj, q * 4);
+                float off[4] = {0.0f, 0.0f, 0.0f, 0.0f}, dj[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+                if (SECOND && i < o.m && j0 < o.mp) {
+                    load_vec<float, 4>(diag_a + j0, dj);
+                    const f16 *p = (const f16 *)(ws + o.at.a) + (uint64_t)i * o.mp + j0;
+                    typedef f16 f16x4 __attribute__((ext_vector_type(4)));
+                    const f16x4 h = *(const f16x4 *)p;
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) off[k] = (float)h[k];
+                    if (PLANES == 2) {
+                        const f16x4 l = *(const f16x4 *)((const char *)p + o.at.a_lo);
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) off[k] += (float)l[k];
+                    }
+                }
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const uint32_t j = j0 + k;
+                    float v = acc[bi][bj][q * 4 + k];
+                    if (!SECOND) {
+                        v = v * sx * sx;
+                        if (i == j && i < o.m) diag_a[i] = v;
+                        v *= s.a;
+                    } else {
+                        v = v * ia * ia;
+                        if (i == j && i < o.m) diag_b[i] = o.b * di + o.c * (v + di * di);
+                        const float t = off[k] * ia;
+                        v = (o.b * t + o.c * (v + (di + dj[k]) * t)) * s.b;
+                    }
+                    acc[bi][bj][q * 4 + k] = i < o.m && j < o.m && i != j ? v : 0.0f;
+                }
+            }
+    }
+    char *stage = lds + (threadIdx.x >> 6) * kOrthoStage<T>;
+    char *hi = ws + (SECOND ? o.at.b : o.at.a), *lo = hi + (SECOND ? o.at.b_lo : o.at.a_lo);
+    store_planes<T, PLANES>(stage, acc, w, hi, lo, o.m, o.mp, o.mp);
+    if (at.m != at.n) store_planes_transposed<T, PLANES>(stage, acc, w, hi, lo, o.m, o.mp, o.mp);
+}
+
+// X = a X + B X; after the last step the result in the output's type.
+template <int T, int PLANES, typename O>
+__global__ __launch_bounds__(256, 1) void ortho_update_kernel(const GemmArgs g, const OrthoArgs o)
+{
+    extern __shared__ __attribute__((aligned(16))) char lds[];
+    const TileAt at = tile_at(g.tiles_m, g.tiles_n, g.batch);
+    f32x16 acc[T][T];
+    gemm_tile<f16, T, T, false>(g, at, lds, acc);
+    const WaveAt<T> w(at);
+    char *ws = o.ws + at.batch * o.at.bytes;
+    const Scales s = ((const Scales *)(ws + o.at.scales))[o.step], next = ((const Scales *)(ws + o.at.scales))[o.step + 1];
+    const float *diag_b = (const float *)(ws + o.at.diag_b);
+    const bool last = o.step + 1 == o.steps;
+    const float to = last ? o.scale : next.x, ib = 1.0f / s.b, ix = s.tau / s.x;
+#pragma unroll
+    for (int bi = 0; bi < T; ++bi) {
+        const uint32_t i = w.i(bi);
+        const float d = i < o.m ? o.a + diag_b[i] : 0.0f;
+#pragma unroll
+        for (int bj = 0; bj < T; ++bj)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const uint32_t j0 = w.j(bj, q * 4);
+                float x[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+                if (i < o.m && j0 < o.np) {
+                    const size_t x_at = ((size_t)i * o.np + j0) * 2;
+                    if (PLANES == 2) {
+                        load_vec<float, 4>((const float *)(ws + o.at.xf + x_at * 2), x);
+                    } else {
+                        typedef f16 f16x4 __attribute__((ext_vector_type(4)));
+                        const f16x4 h = *(const f16x4 *)(ws + o.at.xh + x_at), l = *(const f16x4 *)(ws + o.at.xl + x_at);
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) x[k] = (float)h[k] + (float)l[k];
+                    }
+                }
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const float v = (d * x[k] + acc[bi][bj][q * 4 + k] * ib) * ix;
+                    acc[bi][bj][q * 4 + k] = i < o.m && j0 + k < o.n ? v * to : 0.0f;
+                }
+            }
+    }
+    char *stage = lds + (threadIdx.x >> 6) * kOrthoStage<T>;
+    if (!last) {
+        // X's own planes are read by no other tile; the transposed ones are, so they alternate.
+        char *xt = ws + o.at.xt[(o.step + 1) & 1u];
+        store_planes<T, 2>(stage, acc, w, ws + o.at.xh, ws + o.at.xl, o.m, o.np, o.np);
+        if (PLANES == 2 && w.col0 < o.np)
+#pragma unroll
+            for (int bi = 0; bi < T; ++bi)
+                store_32_rows<float, T * 32>(stage, o.np - w.col0, [&](int j, int r) { return acc[bi][j][r]; }, [&](uint32_t r) {
+                    const uint32_t i = w.row0 + bi * 32 + r;
+                    return i < o.m ? (float *)(ws + o.at.xf) + (uint64_t)i * o.np + w.col0 : nullptr;
+                });
+        store_planes_transposed<T, PLANES>(stage, acc, w, xt, xt + o.at.xt_lo, o.n, o.mp, o.mp);
+        return;
+    }
+    O *out = (O *)o.out + at.batch * o.stride_out;
+#pragma unroll
+    for (int bi = 0; bi < T; ++bi) {
+        const uint32_t first = w.row0 + bi * 32;
+        if (first >= o.m || w.col0 >= o.n) break;
+        auto value = [&](int j, int r) { return acc[bi][j][r]; };
+        if (o.tall) {
+            store_32_cols<O, T * 32>(stage, o.m - first, value, [&](uint32_t c) {
+                return w.col0 + c < o.n ? out + (uint64_t)(w.col0 + c) * o.ld_out + first : nullptr;
+            });
+        } else {
+            store_32_rows<O, T * 32>(stage, o.n - w.col0, value, [&](uint32_t r) {
+                return first + r < o.m ? out + (uint64_t)(first + r) * o.ld_out + w.col0 : nullptr;
+            });
+        }
+    }
+}
+
+}  // namespace dev
+
+namespace {
+
+using namespace dev;
+
+int check_ortho(const ar_ortho_desc *d)
+{
+    if (!d) return AR_ERR_ARG;
+    if (!known_dtype(d->dtype)) return AR_ERR_UNSUPPORTED;
+    if (d->rows < 1 || d->cols < 1 || d->rows > 65536 || d->cols > 65536 || d->batch > 65535) return AR_ERR_ARG;
+    if (d->steps < 1 || d->steps > AR_ORTHO_MAX_STEPS) return AR_ERR_ARG;
+    if (!isfinite(d->eps) || d->eps < 0.0f || !isfinite(d->scale)) return AR_ERR_ARG;
+    for (size_t ld : {d->ld_in, d->ld_out})
+        if (ld && (ld < d->cols || ld > kOpsMaxSize / d->rows)) return AR_ERR_ARG;
+    for (size_t stride : {d->stride_in, d->stride_out})
+        if (stride > kOpsMaxSize) return AR_ERR_ARG;
+    return AR_OK;
+}
+
+// Bounds of |X| after each step for singular values in [0, 1], with 2 % for
+// rounding; false for coefficients that leave what the planes can scale.
+bool bounds(const ar_ortho_desc &d, OrthoArgs *o)
+{
+    double bound = 1.0, growth = 1.0;
+    o->bound[0] = 1.0f, o->growth[0] = 1.0f;
+    for (int k = 0; k < d.steps; ++k) {
+        const double a = d.coefs[3 * k], b = d.coefs[3 * k + 1], c = d.coefs[3 * k + 2];
+        if (!isfinite(a) || !isfinite(b) || !isfinite(c)) return false;
+        // |p(v)| and |p(v) / v| have their largest values at an end of [0, bound] or at a zero of a derivative
+        auto ratio = [&](double v2) { return fabs(a + b * v2 + c * v2 * v2); };
+        auto value = [&](double v2) { return sqrt(v2) * ratio(v2); };
+        const double top = bound * bound;
+        double most = value(top), slope = ratio(0.0) > ratio(top) ? ratio(0.0) : ratio(top);
+        auto consider = [&](double v2) {
+            if (!(v2 > 0.0 && v2 < top)) return;
+            most = value(v2) > most ? value(v2) : most;
+            slope = ratio(v2) > slope ? ratio(v2) : slope;
+        };
+        if (c != 0.0) {
+            const double disc = 9.0 * b * b - 20.0 * a * c;  // of a + 3 b w + 5 c w w, w = v v
+            if (disc >= 0.0) {
+                consider((-3.0 * b + sqrt(disc)) / (10.0 * c));
+                consider((-3.0 * b - sqrt(disc)) / (10.0 * c));
+            }
+            consider(-b / (2.0 * c));
+        } else if (b != 0.0) {
+            consider(-a / (3.0 * b));
+        }
+        bound = 1.02 * most, growth *= 1.02 * slope;
+        if (!(bound <= 4096.0)) return false;
+        if (growth > 1e30) growth = 1e30;
+        o->bound[k + 1] = (float)bound, o->growth[k + 1] = (float)growth;
+        o->abs_b[k] = (float)fabs(b), o->abs_c[k] = (float)fabs(c);
+    }
+    return true;
+}
+
+// Whether the products take two planes: fp32, and bf16 with a short side of at
+// most 256, where three products cost little beside the launches (see above).
+bool two_planes(const ar_ortho_desc &d)
+{
+    return d.dtype == AR_FLOAT32 || (d.rows < d.cols ? d.rows : d.cols) <= 256;
+}
+
+OrthoSpace ortho_space(const ar_ortho_desc &d, uint32_t mp, uint32_t np)
+{
+    OrthoSpace s{};
+    const bool two = two_planes(d);
+    size_t at = 0;
+    auto take = [&](size_t bytes) {
+        const size_t here = at;
+        at += round_up(bytes, 256);
+        return here;
+    };
+    const size_t x = (size_t)mp * np * 2, sq = (size_t)mp * mp * 2;
+    s.xh = take(x), s.xl = take(x), s.xf = take(two ? 2 * x : 0);
+    s.xt_lo = s.a_lo = s.b_lo = 0;
+    s.xt[0] = take(two ? 2 * x : x), s.xt[1] = take(two ? 2 * x : x);
+    s.a = take(two ? 2 * sq : sq), s.b = take(two ? 2 * sq : sq);
+    if (two) s.xt_lo = x, s.a_lo = s.b_lo = sq;
+    s.diag_a = take(mp * 4), s.diag_b = take(mp * 4);
+    s.scales = take(sizeof(Scales) * (AR_ORTHO_MAX_STEPS + 1));
+    s.norms = take(sizeof(double) * kNormParts);
+    s.bytes = at;
+    return s;
+}
+
+// The tile (64 * T rows and columns) that finishes first: rounds over the 256
+// compute units times a tile's time, which goes with its area over the rate
+// its size reaches.
+int tile_for(size_t m, size_t n, size_t batch, bool lower)
+{
+    static const double rate[5] = {0, 0.35, 0.75, 0.9, 1.0};
+    int best = 1;
+    double least = 0;
+    for (int t = 1; t <= 4; ++t) {
+        const size_t a = (m + 64 * t - 1) / (64 * t), b = (n + 64 * t - 1) / (64 * t);
+        const size_t tiles = batch * (lower ? a * (a + 1) / 2 : a * b);
+        const double time = (double)((tiles + 255) / 256) * t * t / rate[t];
+        if (t == 1 || time < least) best = t, least = time;
+    }
+    return best;
+}
+
+template <int T, int PLANES, bool SECOND> int launch_square(GemmArgs &g, const OrthoArgs &o, hipStream_t st)
+{
+    g.tiles_m = g.tiles_n = (o.m + T * 64 - 1) / (T * 64);
+    static const hipError_t set = hipFuncSetAttribute((const void *)ortho_square_kernel<T, PLANES, SECOND>,
+                                                      hipFuncAttributeMaxDynamicSharedMemorySize, kOrthoLds<T>);
+    if (set != hipSuccess) return AR_ERR_HIP;
+    const uint32_t tiles = g.tiles_m * (g.tiles_m + 1) / 2 * o.batch;
+    hipLaunchKernelGGL((ortho_square_kernel<T, PLANES, SECOND>), dim3(tiles), dim3(256), kOrthoLds<T>, st, g, o);
+    return launch_status();
+}
+template <int PLANES, bool SECOND> int square(GemmArgs &g, const OrthoArgs &o, hipStream_t st)
+{
+    switch (tile_for(o.m, o.m, o.batch, true)) {
+    case 1: return launch_square<1, PLANES, SECOND>(g, o, st);
+    case 2: return launch_square<2, PLANES, SECOND>(g, o, st);
+    case 3: return launch_square<3, PLANES, SECOND>(g, o, st);
+    default: return launch_square<4, PLANES, SECOND>(g, o, st);
+    }
+}
+
+template <int T, int PLANES, typename O> int launch_update(GemmArgs &g, const OrthoArgs &o, hipStream_t st)
+{
+    g.tiles_m = (o.m + T * 64 - 1) / (T * 64), g.tiles_n = (o.n + T * 64 - 1) / (T * 64);
+    static const hipError_t set = hipFuncSetAttribute((const void *)ortho_update_kernel<T, PLANES, O>,
+                                                      hipFuncAttributeMaxDynamicSharedMemorySize, kOrthoLds<T>);
+    if (set != hipSuccess) return AR_ERR_HIP;
+    hipLaunchKernelGGL((ortho_update_kernel<T, PLANES, O>), dim3(g.tiles_m * g.tiles_n * o.batch), dim3(256), kOrthoLds<T>, st, g, o);
+    return launch_status();
+}
+template <int PLANES, typename O> int update(GemmArgs &g, const OrthoArgs &o, hipStream_t st)
+{
+    switch (tile_for(o.m, o.n, o.batch, false)) {
+    case 1: return launch_update<1, PLANES, O>(g, o, st);
+    case 2: return launch_update<2, PLANES, O>(g, o, st);
+    case 3: return launch_update<3, PLANES, O>(g, o, st);
+    default: return launch_update<4, PLANES, O>(g, o, st);
+    }
+}
+
+// A product of planes: hi hi, with two planes hi lo and lo hi too.
+template <int PLANES>
+void operands(GemmArgs *g, const OrthoArgs &o, size_t a, size_t a_lo, size_t b, size_t b_lo, uint32_t k, uint32_t m, uint32_t n)
+{
+    *g = GemmArgs{};
+    g->segments = PLANES == 2 ? 3 : 1;
+    g->steps = k / kStepK;
+    const char *pa = o.ws + a, *pb = o.ws + b;
+    g->a[0] = pa, g->b[0] = pb;
+    g->a[1] = pa, g->b[1] = pb + b_lo;
+    g->a[2] = pa + a_lo, g->b[2] = pb;
+    g->lda = g->ldb = k * 2;
+    g->m = m, g->n = n, g->batch_a = g->batch_b = o.at.bytes, g->batch = o.batch, g->splits = 1;
+}
+
+template <typename O, int PLANES> int run_ortho(OrthoArgs &o, const float *coefs, hipStream_t st)
+{
+    hipLaunchKernelGGL((ortho_norm_kernel<O>), dim3(o.norm_parts, o.batch), dim3(256), 0, st, o);
+    int rc = launch_status();
+    if (rc != AR_OK) return rc;
+    hipLaunchKernelGGL((ortho_enter_kernel<O, PLANES>), dim3(o.np / 64, o.mp / 64, o.batch), dim3(256), 0, st, o);
+    if ((rc = launch_status()) != AR_OK) return rc;
+    for (o.step = 0; o.step < o.steps; ++o.step) {
+        o.a = coefs[3 * o.step], o.b = coefs[3 * o.step + 1], o.c = coefs[3 * o.step + 2];
+        GemmArgs g;
+        operands<PLANES>(&g, o, o.at.xh, o.at.xl - o.at.xh, o.at.xh, o.at.xl - o.at.xh, o.np, o.m, o.m);
+        if ((rc = square<PLANES, false>(g, o, st)) != AR_OK) return rc;
+        operands<PLANES>(&g, o, o.at.a, o.at.a_lo, o.at.a, o.at.a_lo, o.mp, o.m, o.m);
+        if ((rc = square<PLANES, true>(g, o, st)) != AR_OK) return rc;
+        operands<PLANES>(&g, o, o.at.b, o.at.b_lo, o.at.xt[o.step & 1u], o.at.xt_lo, o.mp, o.m, o.n);
+        if ((rc = update<PLANES, O>(g, o, st)) != AR_OK) return rc;
+    }
+    return AR_OK;
+}
+
+int ortho(const ar_ortho_desc *desc, const void *in, void *out, void *ws, size_t ws_bytes, void *stream)
+{
+    int rc = check_ortho(desc);
+    if (rc != AR_OK) return rc;
+    const ar_ortho_desc &d = *desc;
+    OrthoArgs o{};
+    if (!d.coefs || !bounds(d, &o)) return AR_ERR_ARG;
+    if (d.batch == 0) return AR_OK;
+    const size_t e = elem_bytes(d.dtype), ld_in = d.ld_in ? d.ld_in : d.cols, ld_out = d.ld_out ? d.ld_out : d.cols;
+    const size_t si = d.stride_in ? d.stride_in : d.rows * ld_in, so = d.stride_out ? d.stride_out : d.rows * ld_out;
+    // matrices of a batch must not share elements: one after another, or side by side in shared rows
+    auto apart = [&](size_t stride, size_t ld) {
+        return d.batch == 1 || stride >= (d.rows - 1) * ld + d.cols || (stride >= d.cols && stride * (d.batch - 1) + d.cols <= ld);
+    };
+    if (!apart(si, ld_in) || !apart(so, ld_out)) return AR_ERR_ARG;
+    if (!in || !out || (uintptr_t)in % e || (uintptr_t)out % e) return AR_ERR_ARG;
+    // the whole batch as one range
+    const Mat mi{in, 1, (d.batch - 1) * si + (d.rows - 1) * ld_in + d.cols, kOpsMaxSize, e};
+    const Mat mo{out, 1, (d.batch - 1) * so + (d.rows - 1) * ld_out + d.cols, kOpsMaxSize, e};
+    if (meet(mi, mo) && !(in == out && ld_in == ld_out && si == so)) return AR_ERR_ARG;
+    const size_t need = ar_orthogonalize_workspace(desc);
+    if (!ws || ws_bytes < need) return AR_ERR_SCRATCH;
+    if ((uintptr_t)ws % 256 != 0) return AR_ERR_ARG;
+    const Mat wsm{ws, 1, need, kOpsMaxSize, 1};
+    if (meet(wsm, mi) || meet(wsm, mo)) return AR_ERR_ARG;
+
+    o.tall = d.rows > d.cols;
+    o.m = (uint32_t)(o.tall ? d.cols : d.rows), o.n = (uint32_t)(o.tall ? d.rows : d.cols);
+    o.mp = (uint32_t)round_up(o.m, kStepK), o.np = (uint32_t)round_up(o.n, kStepK);
+    o.in = in, o.out = out, o.ws = (char *)ws, o.at = ortho_space(d, o.mp, o.np);
+    o.ld_in = ld_in, o.ld_out = ld_out, o.stride_in = si, o.stride_out = so;
+    o.batch = (uint32_t)d.batch, o.steps = (uint32_t)d.steps, o.eps = d.eps, o.scale = d.scale;
+    const size_t parts = (d.rows + 3) / 4;
+    o.norm_parts = (uint32_t)(parts < kNormParts ? parts : kNormParts);
+    hipStream_t st = (hipStream_t)stream;
+    if (d.dtype == AR_FLOAT32) return run_ortho<float, 2>(o, d.coefs, st);
+    return two_planes(d) ? run_ortho<bf16, 2>(o, d.coefs, st) : run_ortho<bf16, 1>(o, d.coefs, st);
+}
+
+}  // namespace
+}  // namespace ar
+
+extern "C" int ar_orthogonalize(const ar_ortho_desc *desc, const void *in, void *out, void *workspace, size_t workspace_bytes,
+                                void *stream)
+{
+    return ar::ops_ret(ar::ortho(desc, in, out, workspace, workspace_bytes, stream));
+}
+
+extern "C" size_t ar_orthogonalize_workspace(const ar_ortho_desc *desc)
+{
+    if (ar::check_ortho(desc) != AR_OK) return 0;
+    const size_t m = desc->rows < desc->cols ? desc->rows : desc->cols, n = desc->rows < desc->cols ? desc->cols : desc->rows;
+    return desc->batch * ar::ortho_space(*desc, (uint32_t)ar::round_up(m, ar::dev::kStepK), (uint32_t)ar::round_up(n, ar::dev::kStepK)).bytes;
+}

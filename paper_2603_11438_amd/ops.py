@@ -3,6 +3,7 @@ layer over the C ABI in include/ar_ops.h (formulas and roundings there).
 
     gated_ffn, gated_ffn_backward           act(x Wg^T) * (x Wu^T)
     residual_norm, residual_norm_backward   norm, gate, scaled residual, norm
+    orthogonalize                           Newton-Schulz steps on an update
 
 Every step runs in the HIP library; torch provides device memory and streams.
 Tensors are checked on every call (ValueError, TypeError); what the library
@@ -20,6 +21,7 @@ import paper_2603_11438_amd as _ar
 
 AR_NORM_POST, AR_NORM_PRE = 1, 2
 AR_ACT_SILU, AR_ACT_GELU, AR_ACT_RELU = 0, 1, 2
+AR_ORTHO_MAX_STEPS = 16
 ACTS = {"silu": AR_ACT_SILU, "gelu": AR_ACT_GELU, "relu": AR_ACT_RELU}
 
 _P, _S, _I, _F = ctypes.c_void_p, ctypes.c_size_t, ctypes.c_int, ctypes.c_float
@@ -36,6 +38,11 @@ class ar_ffn_desc(ctypes.Structure):
                 ("ld_w_gate", _S), ("ld_w_up", _S), ("ld_h", _S), ("ld_dx", _S), ("ld_dw_gate", _S), ("ld_dw_up", _S)]
 
 
+class ar_ortho_desc(ctypes.Structure):
+    _fields_ = [("batch", _S), ("rows", _S), ("cols", _S), ("dtype", _I), ("steps", _I), ("coefs", ctypes.POINTER(_F)),
+                ("eps", _F), ("scale", _F), ("ld_in", _S), ("ld_out", _S), ("stride_in", _S), ("stride_out", _S)]
+
+
 # Every symbol include/ar_ops.h declares, with (restype, argtypes).
 SIGNATURES = {
     "ar_residual_norm": (_I, [ctypes.POINTER(ar_norm_desc)] + [_P] * 8),
@@ -45,6 +52,8 @@ SIGNATURES = {
     "ar_gated_ffn_workspace": (_S, [ctypes.POINTER(ar_ffn_desc)]),
     "ar_gated_ffn_backward": (_I, [ctypes.POINTER(ar_ffn_desc)] + [_P] * 9 + [_S, _P]),
     "ar_gated_ffn_backward_workspace": (_S, [ctypes.POINTER(ar_ffn_desc)]),
+    "ar_orthogonalize": (_I, [ctypes.POINTER(ar_ortho_desc)] + [_P] * 3 + [_S, _P]),
+    "ar_orthogonalize_workspace": (_S, [ctypes.POINTER(ar_ortho_desc)]),
 }
 
 _bound = None
@@ -346,3 +355,70 @@ def gated_ffn_backward_workspace(tokens: int, dim: int, hidden: int) -> int:
     """Bytes of gated_ffn_backward's workspace."""
     d = ar_ffn_desc(tokens=tokens, dim=dim, hidden=hidden, dtype=_ar.AR_BFLOAT16)
     return _lib().ar_gated_ffn_backward_workspace(ctypes.byref(d))
+
+
+# ---- orthogonalised updates ---------------------------------------------------
+
+#: Coefficients (a, b, c) of a step that takes singular values in (0, 1] near 1
+#: within five steps.
+ORTHO_COEFS = (3.4445, -4.7750, 2.0315)
+
+
+def _matrices(t, name):
+    """(batch, rows, cols, row stride, stride between matrices)."""
+    if t.dim() not in (2, 3):
+        raise ValueError(f"{name} must be a matrix or a batch of matrices")
+    b, (m, n) = (1 if t.dim() == 2 else t.shape[0]), t.shape[-2:]
+    if m == 0 or n == 0:
+        raise ValueError(f"{name} must have rows and columns")
+    st = t.stride()
+    if n > 1 and st[-1] != 1:
+        raise ValueError(f"the rows of {name} must be contiguous")
+    ld = st[-2] if m > 1 else max(n, st[-2])
+    stride = st[0] if t.dim() == 3 and b > 1 else m * ld
+    if ld < n or stride <= 0:
+        raise ValueError(f"the rows of {name} must not overlap")
+    return b, m, n, ld, stride
+
+
+def orthogonalize(g, *, steps: int = 5, coefs=ORTHO_COEFS, eps: float = 1e-7, scale: float = 1.0, out=None,
+                  workspace=None, stream=None):
+    """scale times the orthogonalised g: X = g / (|g| + eps), then `steps` times
+    X = a X + (b A + c A A) X with A = X X^T (of g's transpose where it has more
+    rows than columns).
+
+    g: (rows, cols) or (batch, rows, cols), f32 or bf16; coefs: (a, b, c), or a
+    sequence of them, one for each step; out: the result to write to, which may
+    be g.  workspace: a uint8 tensor to use in place of a new one
+    (orthogonalize_workspace)."""
+    import torch
+
+    with _On(g, stream) as on:
+        dt = _ar._dtype_of(g)
+        b, m, n, ld, stride = _matrices(g, "g")
+        flat = [float(v) for c in coefs for v in (c if hasattr(c, "__len__") else (c,))]
+        if len(flat) == 3:
+            flat = flat * steps
+        if not 1 <= steps <= AR_ORTHO_MAX_STEPS or len(flat) != 3 * steps:
+            raise ValueError(f"steps is 1 .. {AR_ORTHO_MAX_STEPS}, with one (a, b, c) for all or one for each")
+        o = torch.empty(g.shape, dtype=g.dtype, device=g.device) if out is None else out
+        if o.shape != g.shape or o.dtype != g.dtype or not o.is_cuda or o.device.index != on.index:
+            raise ValueError("out must be like g")
+        _, _, _, ld_o, stride_o = _matrices(o, "out")
+        d = ar_ortho_desc(batch=b, rows=m, cols=n, dtype=dt, steps=steps, coefs=(_F * len(flat))(*flat), eps=eps, scale=scale,
+                          ld_in=ld, ld_out=ld_o, stride_in=stride, stride_out=stride_o)
+        L, ws = _lib(), workspace
+        if ws is None:
+            ws = _workspace(L.ar_orthogonalize_workspace(ctypes.byref(d)), g)
+        elif not ws.is_cuda or ws.device.index != on.index or not ws.is_contiguous():
+            raise ValueError("workspace must be a contiguous tensor on the GPU of the call")
+        rc = L.ar_orthogonalize(ctypes.byref(d), g.data_ptr(), o.data_ptr(), _ptr(ws),
+                                0 if ws is None else ws.numel() * ws.element_size(), on.ptr)
+        _ar._check(rc, "ar_orthogonalize")
+    return o
+
+
+def orthogonalize_workspace(batch: int, rows: int, cols: int, dtype="f32") -> int:
+    """Bytes of orthogonalize's workspace."""
+    d = ar_ortho_desc(batch=batch, rows=rows, cols=cols, dtype=_ar.DTYPES[dtype], steps=1, eps=0.0, scale=1.0)
+    return _lib().ar_orthogonalize_workspace(ctypes.byref(d))

@@ -1,0 +1,155 @@
+"""Orthogonalised updates on the GPU against the definition in 64 bits
+(oracle/ops_oracle.py).
+
+Tolerance, of the result's norm.  With every rounding of the planes, and no
+other error, modelled in 64 bits (square, wide and nearly square matrices of
+normal values, of a few strong directions over noise, and with singular values
+over four decades), the result was off by at most 0.95e-3 for bf16's single
+plane, and by 14 times the planes' unit for fp32's two, 2^-22.  bf16 then
+rounds the result: 1.7e-3 of a norm.  Together 1.95e-3; 2.3e-3 is asked.  fp32
+sums of n products are off by sqrt(n) u at random, which reaches the result
+like a plane's rounding: 14 (2^-22 + sqrt(n) 2^-24).  With a short side below 8
+the few singular values do not average: the model's worst over 60 matrices of
+each of 2 x 3, 3 x 5 and 4 x 4 is 33 units, and 40 stands in the place of 14."""
+from __future__ import annotations
+
+import math
+
+import pytest
+import torch
+
+import paper_2603_11438_amd as ar
+from gpu_helpers import say
+from oracle import ops_oracle as oo
+
+pytestmark = pytest.mark.gpu
+
+COEFS = (3.4445, -4.7750, 2.0315)
+TORCH = {"f32": torch.float32, "bf16": torch.bfloat16}
+
+
+def tolerance(m, n, dtype):
+    return 2.3e-3 if dtype == "bf16" else (14 if min(m, n) >= 8 else 40) * (2.0 ** -22 + math.sqrt(max(m, n)) * 2.0 ** -24)
+
+
+def make(kind, m, n, seed=0):
+    g = torch.Generator().manual_seed(seed + 1000 * m + n)
+    x = torch.randn(m, n, generator=g, dtype=torch.float64)
+    if kind == "strong":
+        k = max(1, min(m, n) // 16)
+        x = torch.randn(m, k, generator=g).double() @ torch.randn(k, n, generator=g).double() / math.sqrt(k) + 0.02 * x
+    elif kind == "decades":
+        u, s, v = torch.linalg.svd(x, full_matrices=False)
+        x = u @ torch.diag(torch.logspace(0, -4, len(s), dtype=torch.float64)) @ v
+    return x
+
+
+def check(got, m, coefs=(COEFS,) * 5, tol=None, scale=1.0, eps=1e-7):
+    dtype = "f32" if got.dtype == torch.float32 else "bf16"
+    want = oo.orthogonalize(m, coefs, eps, scale)
+    got = got.cpu().double()
+    assert bool(torch.isfinite(got).all())
+    off = float((got - want).norm() / want.norm())
+    tol = tol or tolerance(*m.shape, dtype)
+    if dtype == "bf16":
+        # a handful of elements can all be rounded by more than the usual share
+        tol = max(tol, 1.2 * float((want.bfloat16().double() - want).norm() / want.norm()))
+    assert off <= tol, f"off by {off:.3g}, {tol:.3g} allowed"
+
+
+SHAPES = [(1, 1), (1, 64), (64, 1), (2, 3), (33, 70), (70, 33), (64, 64), (65, 65), (128, 384), (127, 200), (200, 127), (256, 256),
+          (300, 129), (512, 1000), (1000, 520), (700, 701)]
+
+
+@pytest.mark.parametrize("dtype", ("f32", "bf16"))
+@pytest.mark.parametrize("m,n", SHAPES)
+def test_against_definition(m, n, dtype):
+    for kind in ("normal", "strong", "decades"):
+        for pad in (0, 5):
+            say(f"ortho {m} x {n} {dtype} {kind} pad {pad}")
+            x = torch.full((m, n + pad), float("nan"))
+            x[:, :n] = make(kind, m, n) * 1e-3
+            x = x.to(TORCH[dtype]).cuda()[:, :n]
+            check(ar.orthogonalize(x), x)
+
+
+@pytest.mark.parametrize("m,n,dtype", [(1536, 1536, "bf16"), (640, 4100, "f32"), (4100, 640, "bf16")])
+def test_larger(m, n, dtype):
+    say(f"ortho {m} x {n} {dtype}")
+    x = make("strong", m, n).to(TORCH[dtype]).cuda()
+    check(ar.orthogonalize(x), x)
+
+
+@pytest.mark.parametrize("dtype", ("f32", "bf16"))
+def test_batches_and_strides(dtype):
+    """Each matrix of a batch as by itself, in any arrangement of the batch."""
+    x = torch.stack([make(k, 90, 150, s) * 10.0 ** (3 * s - 3) for s, k in enumerate(("normal", "strong", "decades"))]).to(TORCH[dtype]).cuda()
+    alone = [ar.orthogonalize(m) for m in x]
+    for m, a in zip(x, alone):
+        check(a, m)
+    assert torch.equal(ar.orthogonalize(x), torch.stack(alone))
+    side = torch.zeros(90, 3, 170, dtype=x.dtype, device="cuda")  # matrices side by side in the same rows
+    side[:, :, :150] = x.permute(1, 0, 2)
+    view = side.permute(1, 0, 2)[:, :, :150]
+    got = ar.orthogonalize(view)
+    assert torch.equal(got, torch.stack(alone))
+    assert torch.equal(ar.orthogonalize(view, out=view), got) and torch.equal(view, got)
+    assert bool((side[:, :, 150:] == 0).all())
+
+
+@pytest.mark.parametrize("dtype", ("f32", "bf16"))
+def test_sizes_of_values(dtype):
+    """The normalisation is exact in powers of two, from the smallest norms to
+    the largest; below eps the result shrinks with the norm."""
+    x = make("strong", 60, 100).to(TORCH[dtype]).cuda()
+    base = ar.orthogonalize(x, eps=0.0)
+    for e in (-100, -60, 60, 100):
+        assert torch.equal(ar.orthogonalize(x * 2.0 ** e, eps=0.0), base), e
+    small = (x * 2.0 ** -40).contiguous()
+    check(ar.orthogonalize(small, eps=1e-3), small, eps=1e-3, tol=2 * tolerance(60, 100, dtype))
+
+
+def test_zero_and_bad_values():
+    for dtype in (torch.float32, torch.bfloat16):
+        x = make("normal", 70, 40).to(dtype).cuda()
+        batch = torch.stack([x, x * 0, x, x])
+        batch[2, 3, 5], batch[3, 69, 39] = float("nan"), float("inf")
+        got = ar.orthogonalize(batch)
+        assert torch.equal(got[0], ar.orthogonalize(x)) and bool((got[1] == 0).all())
+        assert bool(torch.isnan(got[2]).all()) and bool(torch.isnan(got[3]).all())
+
+
+def test_coefficients_scale_and_steps():
+    x = make("strong", 100, 130).float().cuda()
+    sched = [COEFS, COEFS, COEFS, (2.0, -1.5, 0.5), (1.875, -1.25, 0.375)]
+    check(ar.orthogonalize(x, steps=5, coefs=sched), x, sched)
+    check(ar.orthogonalize(x, steps=1, scale=0.25), x, (COEFS,), scale=0.25)
+    check(ar.orthogonalize(x, steps=3, coefs=(1.5, -0.5, 0.0)), x, ((1.5, -0.5, 0.0),) * 3)
+    check(ar.orthogonalize(x, steps=16, coefs=(1.875, -1.25, 0.375)), x, ((1.875, -1.25, 0.375),) * 16, tol=1e-3)
+
+
+def test_orthogonal_result():
+    """What it is for: with a convergent polynomial the rows come out orthonormal."""
+    x = make("normal", 96, 200).float().cuda()
+    o = ar.orthogonalize(x, steps=12, coefs=(1.875, -1.25, 0.375)).double()
+    assert float((o @ o.T - torch.eye(96, device="cuda", dtype=torch.float64)).abs().max()) < 1e-5
+
+
+def test_same_bits_stream_and_graph():
+    x = make("strong", 200, 300).bfloat16().cuda()
+    one = ar.orthogonalize(x)
+    st = torch.cuda.Stream()
+    st.wait_stream(torch.cuda.current_stream())
+    two = ar.orthogonalize(x, stream=st)
+    st.synchronize()
+    assert torch.equal(one, two)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = ar.orthogonalize(x)
+    for k in range(4):
+        x.copy_(make("normal", 200, 300, k + 1))
+        want = ar.orthogonalize(x)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(got, want), k

@@ -173,3 +173,37 @@ def test_ffn_plain_gradient_is_the_difference(act):
         e = rnd(*v[name].shape)
         fd = (loss({**v, name: v[name] + h * e}) - loss({**v, name: v[name] - h * e})) / (2 * h)
         assert abs(fd - float((g * e).sum())) < 1e-6 * (1 + abs(fd)), name
+
+
+def ortho(i=A, o=B, ws=0x90000000, nbytes=None, coefs=(3.4, -4.8, 2.0), **kw):
+    f = dict(batch=2, rows=8, cols=16, dtype=0, steps=1, eps=1e-7, scale=1.0)
+    f.update(kw)
+    d = ops.ar_ortho_desc(**f)
+    if coefs is not None:
+        d.coefs = (ctypes.c_float * (3 * 16))(*(tuple(coefs) * 16))
+    L = ops._lib()
+    n = L.ar_orthogonalize_workspace(ctypes.byref(d)) if nbytes is None else nbytes
+    return L.ar_orthogonalize(ctypes.byref(d), i, o, ws, n, None)
+
+
+@pytest.mark.parametrize("kw,code", [
+    (dict(dtype=3), ar.AR_ERR_UNSUPPORTED), (dict(rows=0), ar.AR_ERR_ARG), (dict(cols=65537), ar.AR_ERR_ARG),
+    (dict(steps=0), ar.AR_ERR_ARG), (dict(steps=17), ar.AR_ERR_ARG), (dict(coefs=None), ar.AR_ERR_ARG),
+    (dict(coefs=(float("nan"), 0, 0)), ar.AR_ERR_ARG), (dict(coefs=(5000.0, 0, 0)), ar.AR_ERR_ARG),
+    (dict(coefs=(20.0, 0, 0), steps=3), ar.AR_ERR_ARG), (dict(eps=-1.0), ar.AR_ERR_ARG), (dict(scale=float("inf")), ar.AR_ERR_ARG),
+    (dict(ld_in=15), ar.AR_ERR_ARG), (dict(stride_in=100), ar.AR_ERR_ARG), (dict(stride_out=16, ld_out=20), ar.AR_ERR_ARG),
+    (dict(i=None), ar.AR_ERR_ARG), (dict(o=B + 2), ar.AR_ERR_ARG), (dict(o=A + 64), ar.AR_ERR_ARG), (dict(o=A, ld_out=20), ar.AR_ERR_ARG),
+    (dict(ws=None), ar.AR_ERR_SCRATCH), (dict(nbytes=64), ar.AR_ERR_SCRATCH), (dict(ws=0x90000020), ar.AR_ERR_ARG),
+    (dict(ws=A), ar.AR_ERR_ARG)])
+def test_ortho_refusals(kw, code):
+    assert ortho(**kw) == code
+    assert ar.ar_last_error() == code
+
+
+def test_ortho_without_matrices_is_done():
+    assert ortho(batch=0, i=None, o=None, ws=None) == ar.AR_OK
+
+
+def test_ortho_tensor_checks():
+    with pytest.raises(ValueError, match="GPU"):
+        ar.orthogonalize(torch.zeros(4, 8))

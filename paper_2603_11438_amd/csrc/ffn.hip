@@ -38,33 +38,33 @@ struct FfnOut {
     uint64_t ld_h;
 };
 
-template <int MT, int NT, int ACT>
-__global__ __launch_bounds__(256, 1) void ffn_kernel(const GemmArgs g, const FfnOut o)
+template <typename S, int ACT> __global__ __launch_bounds__(S::THREADS) void ffn_kernel(const GemmArgs g, const FfnOut o)
 {
-    constexpr int HALF = NT * 16;
+    constexpr int NT = S::NT, HALF = NT * 16;
     extern __shared__ __attribute__((aligned(16))) char lds[];
     const TileAt at = tile_at(g.tiles_m, g.tiles_n, 1);
-    f32x16 acc[MT][NT];
-    gemm_tile<bf16, MT, NT, true>(g, at, lds, acc);
+    f32x16 acc[S::MT][NT];
+    gemm_tile<bf16, S, true>(g, at, lds, acc);
     const uint32_t wave = threadIdx.x >> 6;
-    const uint32_t row0 = at.m * MT * 64 + (wave >> 1) * MT * 32, col0 = at.n * NT * 32 + (wave & 1u) * HALF;
+    const uint32_t row0 = at.m * S::BM + (wave >> 1) * S::MT * 32, col0 = at.n * (S::BN / 2) + (wave & 1u) * HALF;
     if (col0 >= g.n) return;
     const uint32_t cols = g.n - col0;
     char *stage = lds + wave * kStageBytes<float, HALF>;
-#pragma unroll
-    for (int i = 0; i < MT; ++i) {
+    static_for<S::MT>([&](auto block) {
+        constexpr int i = block.value;
+        float v[NT][16];
+        take(acc[i], v);
         auto row_of = [&](auto *base, uint64_t ld) {
             return [=](uint32_t r) { return row0 + i * 32 + r < g.m ? base + (uint64_t)(row0 + i * 32 + r) * ld + col0 : nullptr; };
         };
         if (o.saved) {
-            store_32_rows<float, HALF>(stage, cols, [&](int j, int r) { return acc[i][j][r]; }, row_of(o.saved, g.n));
-            store_32_rows<float, HALF>(stage, cols, [&](int j, int r) { return acc[i][j + NT / 2][r]; },
+            store_32_rows<float, HALF>(stage, cols, [&](int j, int r) { return v[j][r]; }, row_of(o.saved, g.n));
+            store_32_rows<float, HALF>(stage, cols, [&](int j, int r) { return v[j + NT / 2][r]; },
                                        row_of(o.saved + (uint64_t)g.m * g.n, g.n));
         }
-        store_32_rows<bf16, HALF>(stage, cols,
-                                  [&](int j, int r) { return activation<ACT>(acc[i][j][r]) * acc[i][j + NT / 2][r]; },
+        store_32_rows<bf16, HALF>(stage, cols, [&](int j, int r) { return activation<ACT>(v[j][r]) * v[j + NT / 2][r]; },
                                   row_of(o.h, o.ld_h));
-    }
+    });
 }
 
 // Copies a matrix into rows of `to_ld` elements, zeros behind its columns.
@@ -195,20 +195,22 @@ struct ProductOut {
     uint64_t ld, ld2;
     uint32_t split;
 };
-template <int MT, int NT> __global__ __launch_bounds__(256, 1) void product_kernel(const GemmArgs g, const ProductOut o)
+template <typename S> __global__ __launch_bounds__(S::THREADS) void product_kernel(const GemmArgs g, const ProductOut o)
 {
-    constexpr int COLS = NT * 32;
+    constexpr int NT = S::NT, COLS = NT * 32;
     extern __shared__ __attribute__((aligned(16))) char lds[];
     const TileAt at = tile_at(g.tiles_m, g.tiles_n, 1);
-    f32x16 acc[MT][NT];
-    gemm_tile<bf16, MT, NT, false>(g, at, lds, acc);
+    f32x16 acc[S::MT][NT];
+    gemm_tile<bf16, S, false>(g, at, lds, acc);
     const uint32_t wave = threadIdx.x >> 6;
-    const uint32_t row0 = at.m * MT * 64 + (wave >> 1) * MT * 32, col0 = at.n * NT * 64 + (wave & 1u) * COLS;
+    const uint32_t row0 = at.m * S::BM + (wave >> 1) * S::MT * 32, col0 = at.n * S::BN + (wave & 1u) * COLS;
     if (col0 >= g.n) return;
     char *stage = lds + wave * kStageBytes<float, COLS>;
-#pragma unroll
-    for (int i = 0; i < MT; ++i) {
-        auto value = [&](int j, int r) { return acc[i][j][r]; };
+    static_for<S::MT>([&](auto block) {
+        constexpr int i = block.value;
+        float v[NT][16];
+        take(acc[i], v);
+        auto value = [&](int j, int r) { return v[j][r]; };
         if (g.splits > 1) {
             store_32_rows<float, COLS>(stage, g.n - col0, value, [&](uint32_t r) {
                 const uint32_t m = row0 + i * 32 + r;
@@ -221,7 +223,7 @@ template <int MT, int NT> __global__ __launch_bounds__(256, 1) void product_kern
                 return m < g.m ? to + col0 : nullptr;
             });
         }
-    }
+    });
 }
 
 // Adds the runs of a split product in their order.
@@ -288,22 +290,24 @@ int pack(const Mat &m, char *&ws, hipStream_t st, Operand *out)
     return launch_status();
 }
 
-template <int MT, int NT, int ACT> int launch_ffn(GemmArgs &g, const FfnOut &o, hipStream_t st)
+typedef Shape<4, 4, 1, 64, 2> Large;
+typedef Shape<2, 2, 1, 64, 2> Small;
+
+template <typename S, int ACT> int launch_ffn(GemmArgs &g, const FfnOut &o, hipStream_t st)
 {
-    g.tiles_m = (uint32_t)((g.m + MT * 64 - 1) / (MT * 64));
-    g.tiles_n = (uint32_t)((g.n + NT * 32 - 1) / (NT * 32));
-    constexpr int LDS = kGemmLds<MT, NT>;
-    static_assert(4 * kStageBytes<float, NT * 16> <= LDS, "the epilogue's staging fits");
-    static const hipError_t set = hipFuncSetAttribute((const void *)ffn_kernel<MT, NT, ACT>, hipFuncAttributeMaxDynamicSharedMemorySize, LDS);
+    g.tiles_m = (g.m + S::BM - 1) / S::BM;
+    g.tiles_n = (g.n + S::BN / 2 - 1) / (S::BN / 2);
+    static_assert(4 * kStageBytes<float, S::NT * 16> <= S::LDS, "the epilogue's staging fits");
+    static const hipError_t set = hipFuncSetAttribute((const void *)ffn_kernel<S, ACT>, hipFuncAttributeMaxDynamicSharedMemorySize, S::LDS);
     if (set != hipSuccess) return AR_ERR_HIP;
-    hipLaunchKernelGGL((ffn_kernel<MT, NT, ACT>), dim3(g.tiles_m * g.tiles_n), dim3(256), LDS, st, g, o);
+    hipLaunchKernelGGL((ffn_kernel<S, ACT>), dim3(g.tiles_m * g.tiles_n), dim3(S::THREADS), S::LDS, st, g, o);
     return launch_status();
 }
 
 template <int ACT> int launch_ffn_tiles(GemmArgs &g, const FfnOut &o, hipStream_t st)
 {
     const size_t large = (size_t)((g.m + 255) / 256) * ((g.n + 127) / 128);
-    return large >= 256 ? launch_ffn<4, 4, ACT>(g, o, st) : launch_ffn<2, 2, ACT>(g, o, st);
+    return large >= 256 ? launch_ffn<Large, ACT>(g, o, st) : launch_ffn<Small, ACT>(g, o, st);
 }
 
 struct FfnMats {
@@ -389,14 +393,14 @@ size_t part_bytes(size_t m, size_t n, size_t steps)
     return c.splits > 1 ? round_up(c.splits * m * n * sizeof(float), 256) : 0;
 }
 
-template <int MT, int NT> int launch_product(GemmArgs &g, const ProductOut &o, hipStream_t st)
+template <typename S> int launch_product(GemmArgs &g, const ProductOut &o, hipStream_t st)
 {
-    g.tiles_m = (uint32_t)((g.m + MT * 64 - 1) / (MT * 64));
-    g.tiles_n = (uint32_t)((g.n + NT * 64 - 1) / (NT * 64));
-    constexpr int LDS = kGemmLds<MT, NT> > 4 * kStageBytes<float, NT * 32> ? kGemmLds<MT, NT> : 4 * kStageBytes<float, NT * 32>;
-    static const hipError_t set = hipFuncSetAttribute((const void *)product_kernel<MT, NT>, hipFuncAttributeMaxDynamicSharedMemorySize, LDS);
+    g.tiles_m = (g.m + S::BM - 1) / S::BM;
+    g.tiles_n = (g.n + S::BN - 1) / S::BN;
+    constexpr int STAGE = 4 * kStageBytes<float, S::NT * 32>, LDS = S::LDS > STAGE ? S::LDS : STAGE;
+    static const hipError_t set = hipFuncSetAttribute((const void *)product_kernel<S>, hipFuncAttributeMaxDynamicSharedMemorySize, LDS);
     if (set != hipSuccess) return AR_ERR_HIP;
-    hipLaunchKernelGGL((product_kernel<MT, NT>), dim3(g.tiles_m * g.tiles_n, g.splits), dim3(256), LDS, st, g, o);
+    hipLaunchKernelGGL((product_kernel<S>), dim3(g.tiles_m * g.tiles_n, g.splits), dim3(S::THREADS), LDS, st, g, o);
     int rc = launch_status();
     if (rc != AR_OK || g.splits == 1) return rc;
     const uint64_t groups = ((uint64_t)g.m * g.n + 255) / 256;
@@ -408,7 +412,7 @@ int product(GemmArgs &g, const ProductOut &o, hipStream_t st)
 {
     const Cut c = cut_of(g.m, g.n, (size_t)g.steps * g.segments);
     g.splits = c.splits, g.batch = 1;
-    return c.tile == 4 ? launch_product<4, 4>(g, o, st) : launch_product<2, 2>(g, o, st);
+    return c.tile == 4 ? launch_product<Large>(g, o, st) : launch_product<Small>(g, o, st);
 }
 
 int transpose(const Mat &m, void *to, size_t to_ld, hipStream_t st)

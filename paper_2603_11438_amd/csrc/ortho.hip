@@ -204,86 +204,79 @@ __device__ __forceinline__ void store_32_cols(char *lds, uint32_t rows, V value,
 template <typename O, int COLS> constexpr int kStageColBytes = COLS * (32 * (int)sizeof(O) + 16);
 
 // A wave's place in its tile.
-template <int T> struct WaveAt {
+template <typename S> struct WaveAt {
     uint32_t row0, col0, row, half;
     __device__ __forceinline__ WaveAt(const TileAt at)
     {
         const uint32_t lane = threadIdx.x & 63u, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-        row0 = at.m * T * 64 + (wave >> 1) * T * 32, col0 = at.n * T * 64 + (wave & 1u) * T * 32;
+        row0 = at.m * S::BM + (wave >> 1) * S::MT * 32, col0 = at.n * S::BN + (wave & 1u) * S::NT * 32;
         row = lane & 31u, half = (lane >> 5) * 4;
     }
     __device__ __forceinline__ uint32_t i(int bi) const { return row0 + bi * 32 + row; }
     __device__ __forceinline__ uint32_t j(int bj, int r) const { return col0 + bj * 32 + r / 4 * 8 + half + r % 4; }
 };
 
-// The planes of a scaled matrix from the accumulators, rows and columns up to
-// the padded sizes.
-template <int T, int PLANES>
-__device__ __forceinline__ void store_planes(char *stage, const f32x16 (&acc)[T][T], const WaveAt<T> &w, char *hi, char *lo,
-                                             uint32_t rows, uint32_t cols, uint32_t ld)
+// The planes of a scaled matrix from 32 rows of a wave's block, rows and
+// columns up to the padded sizes: as they are, or transposed.
+template <int NT> __device__ __forceinline__ float plane_of(const float (&v)[NT][16], int plane, int j, int r)
 {
-    if (w.col0 >= cols) return;
-#pragma unroll
-    for (int bi = 0; bi < T; ++bi) {
-        auto to = [&](char *base) {
-            return [=](uint32_t r) {
-                const uint32_t i = w.row0 + bi * 32 + r;
-                return i < rows ? (f16 *)base + (uint64_t)i * ld + w.col0 : nullptr;
-            };
-        };
-        store_32_rows<f16, T * 32>(stage, cols - w.col0, [&](int j, int r) { return acc[bi][j][r]; }, to(hi));
-        if (PLANES == 2)
-            store_32_rows<f16, T * 32>(stage, cols - w.col0,
-                                       [&](int j, int r) { return acc[bi][j][r] - (float)(f16)acc[bi][j][r]; }, to(lo));
-    }
+    const float x = v[j][r];
+    return plane == 0 ? x : x - (float)(f16)x;
 }
-template <int T, int PLANES>
-__device__ __forceinline__ void store_planes_transposed(char *stage, const f32x16 (&acc)[T][T], const WaveAt<T> &w, char *hi,
-                                                        char *lo, uint32_t rows, uint32_t cols, uint32_t ld)
+template <typename S, int PLANES>
+__device__ __forceinline__ void store_planes(char *stage, const float (&v)[S::NT][16], uint32_t first, uint32_t col0, char *hi,
+                                             size_t lo, uint32_t rows, uint32_t cols, uint32_t ld)
 {
-    // cols: of the result, that is rows of the block
+    if (col0 >= cols) return;
 #pragma unroll
-    for (int bi = 0; bi < T; ++bi) {
-        const uint32_t first = w.row0 + bi * 32;
-        if (first >= cols) break;
-        auto to = [&](char *base) {
-            return [=](uint32_t c) {
-                const uint32_t j = w.col0 + c;
-                return j < rows ? (f16 *)base + (uint64_t)j * ld + first : nullptr;
-            };
-        };
-        store_32_cols<f16, T * 32>(stage, cols - first, [&](int j, int r) { return acc[bi][j][r]; }, to(hi));
-        if (PLANES == 2)
-            store_32_cols<f16, T * 32>(stage, cols - first,
-                                       [&](int j, int r) { return acc[bi][j][r] - (float)(f16)acc[bi][j][r]; }, to(lo));
-    }
+    for (int plane = 0; plane < PLANES; ++plane)
+        store_32_rows<f16, S::NT * 32>(stage, cols - col0, [&](int j, int r) { return plane_of(v, plane, j, r); }, [&](uint32_t r) {
+            return first + r < rows ? (f16 *)(hi + plane * lo) + (uint64_t)(first + r) * ld + col0 : nullptr;
+        });
+}
+template <typename S, int PLANES>
+__device__ __forceinline__ void store_planes_transposed(char *stage, const float (&v)[S::NT][16], uint32_t first, uint32_t col0,
+                                                        char *hi, size_t lo, uint32_t rows, uint32_t cols, uint32_t ld)
+{
+    if (first >= cols) return;
+#pragma unroll
+    for (int plane = 0; plane < PLANES; ++plane)
+        store_32_cols<f16, S::NT * 32>(stage, cols - first, [&](int j, int r) { return plane_of(v, plane, j, r); }, [&](uint32_t c) {
+            return col0 + c < rows ? (f16 *)(hi + plane * lo) + (uint64_t)(col0 + c) * ld + first : nullptr;
+        });
 }
 
-template <int T> constexpr int kOrthoStage = kStageColBytes<float, T * 32> > kStageBytes<float, T * 32>
-                                                 ? kStageColBytes<float, T * 32> : kStageBytes<float, T * 32>;
-template <int T> constexpr int kOrthoLds = kGemmLds<T, T> > 4 * kOrthoStage<T> ? kGemmLds<T, T> : 4 * kOrthoStage<T>;
+template <typename S> constexpr int kOrthoStage = kStageColBytes<float, S::NT * 32> > kStageBytes<float, S::NT * 32>
+                                                      ? kStageColBytes<float, S::NT * 32> : kStageBytes<float, S::NT * 32>;
+template <typename S> constexpr int kOrthoLds = S::LDS > 4 * kOrthoStage<S> ? S::LDS : 4 * kOrthoStage<S>;
 
 // A = X X^T (SECOND false) or B = b A + c A A (true): tiles on and below the
 // diagonal, written to both places; the diagonal goes to its fp32 vector and
 // is zero in the planes.
-template <int T, int PLANES, bool SECOND>
-__global__ __launch_bounds__(256, 1) void ortho_square_kernel(const GemmArgs g, const OrthoArgs o)
+template <typename S, bool SECOND>
+__global__ __launch_bounds__(S::THREADS) void ortho_square_kernel(const GemmArgs g, const OrthoArgs o)
 {
+    constexpr int NT = S::NT, PLANES = S::PLANES;
     extern __shared__ __attribute__((aligned(16))) char lds[];
     const TileAt at = tile_at_lower(g.tiles_m, g.batch);
-    f32x16 acc[T][T];
-    gemm_tile<f16, T, T, false>(g, at, lds, acc);
-    const WaveAt<T> w(at);
+    f32x16 acc[S::MT][NT];
+    gemm_tile<f16, S, false>(g, at, lds, acc);
+    const WaveAt<S> w(at);
     char *ws = o.ws + at.batch * o.at.bytes;
     const Scales s = ((const Scales *)(ws + o.at.scales))[o.step];
     float *diag_a = (float *)(ws + o.at.diag_a), *diag_b = (float *)(ws + o.at.diag_b);
     const float sx = s.tau / s.x, ia = 1.0f / s.a;
-#pragma unroll
-    for (int bi = 0; bi < T; ++bi) {
+    char *stage = lds + (threadIdx.x >> 6) * kOrthoStage<S>;
+    char *hi = ws + (SECOND ? o.at.b : o.at.a);
+    const size_t lo = SECOND ? o.at.b_lo : o.at.a_lo;
+    static_for<S::MT>([&](auto block) {
+        constexpr int bi = block.value;
+        float v[NT][16];
+        take(acc[bi], v);
         const uint32_t i = w.i(bi);
         const float di = SECOND && i < o.m ? diag_a[i] : 0.0f;
 #pragma unroll
-        for (int bj = 0; bj < T; ++bj)
+        for (int bj = 0; bj < NT; ++bj)
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
                 const uint32_t j0 = w.j(bj, q * 4);
@@ -304,47 +297,52 @@ __global__ __launch_bounds__(256, 1) void ortho_square_kernel(const GemmArgs g, 
 #pragma unroll
                 for (int k = 0; k < 4; ++k) {
                     const uint32_t j = j0 + k;
-                    float v = acc[bi][bj][q * 4 + k];
+                    float x = v[bj][q * 4 + k];
                     if (!SECOND) {
-                        v = v * sx * sx;
-                        if (i == j && i < o.m) diag_a[i] = v;
-                        v *= s.a;
+                        x = x * sx * sx;
+                        if (i == j && i < o.m) diag_a[i] = x;
+                        x *= s.a;
                     } else {
-                        v = v * ia * ia;
-                        if (i == j && i < o.m) diag_b[i] = o.b * di + o.c * (v + di * di);
+                        x = x * ia * ia;
+                        if (i == j && i < o.m) diag_b[i] = o.b * di + o.c * (x + di * di);
                         const float t = off[k] * ia;
-                        v = (o.b * t + o.c * (v + (di + dj[k]) * t)) * s.b;
+                        x = (o.b * t + o.c * (x + (di + dj[k]) * t)) * s.b;
                     }
-                    acc[bi][bj][q * 4 + k] = i < o.m && j < o.m && i != j ? v : 0.0f;
+                    v[bj][q * 4 + k] = i < o.m && j < o.m && i != j ? x : 0.0f;
                 }
             }
-    }
-    char *stage = lds + (threadIdx.x >> 6) * kOrthoStage<T>;
-    char *hi = ws + (SECOND ? o.at.b : o.at.a), *lo = hi + (SECOND ? o.at.b_lo : o.at.a_lo);
-    store_planes<T, PLANES>(stage, acc, w, hi, lo, o.m, o.mp, o.mp);
-    if (at.m != at.n) store_planes_transposed<T, PLANES>(stage, acc, w, hi, lo, o.m, o.mp, o.mp);
+        const uint32_t first = w.row0 + bi * 32;
+        store_planes<S, PLANES>(stage, v, first, w.col0, hi, lo, o.m, o.mp, o.mp);
+        if (at.m != at.n) store_planes_transposed<S, PLANES>(stage, v, first, w.col0, hi, lo, o.m, o.mp, o.mp);
+    });
 }
 
 // X = a X + B X; after the last step the result in the output's type.
-template <int T, int PLANES, typename O>
-__global__ __launch_bounds__(256, 1) void ortho_update_kernel(const GemmArgs g, const OrthoArgs o)
+template <typename S, typename O>
+__global__ __launch_bounds__(S::THREADS) void ortho_update_kernel(const GemmArgs g, const OrthoArgs o)
 {
+    constexpr int NT = S::NT, PLANES = S::PLANES;
     extern __shared__ __attribute__((aligned(16))) char lds[];
     const TileAt at = tile_at(g.tiles_m, g.tiles_n, g.batch);
-    f32x16 acc[T][T];
-    gemm_tile<f16, T, T, false>(g, at, lds, acc);
-    const WaveAt<T> w(at);
+    f32x16 acc[S::MT][NT];
+    gemm_tile<f16, S, false>(g, at, lds, acc);
+    const WaveAt<S> w(at);
     char *ws = o.ws + at.batch * o.at.bytes;
     const Scales s = ((const Scales *)(ws + o.at.scales))[o.step], next = ((const Scales *)(ws + o.at.scales))[o.step + 1];
     const float *diag_b = (const float *)(ws + o.at.diag_b);
     const bool last = o.step + 1 == o.steps;
     const float to = last ? o.scale : next.x, ib = 1.0f / s.b, ix = s.tau / s.x;
-#pragma unroll
-    for (int bi = 0; bi < T; ++bi) {
+    // X's own planes are read by no other tile; the transposed ones are, so they alternate.
+    char *stage = lds + (threadIdx.x >> 6) * kOrthoStage<S>, *xt = ws + o.at.xt[(o.step + 1) & 1u];
+    O *out = (O *)o.out + at.batch * o.stride_out;
+    static_for<S::MT>([&](auto block) {
+        constexpr int bi = block.value;
+        float v[NT][16];
+        take(acc[bi], v);
         const uint32_t i = w.i(bi);
         const float d = i < o.m ? o.a + diag_b[i] : 0.0f;
 #pragma unroll
-        for (int bj = 0; bj < T; ++bj)
+        for (int bj = 0; bj < NT; ++bj)
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
                 const uint32_t j0 = w.j(bj, q * 4);
@@ -362,42 +360,31 @@ __global__ __launch_bounds__(256, 1) void ortho_update_kernel(const GemmArgs g, 
                 }
 #pragma unroll
                 for (int k = 0; k < 4; ++k) {
-                    const float v = (d * x[k] + acc[bi][bj][q * 4 + k] * ib) * ix;
-                    acc[bi][bj][q * 4 + k] = i < o.m && j0 + k < o.n ? v * to : 0.0f;
+                    const float y = (d * x[k] + v[bj][q * 4 + k] * ib) * ix;
+                    v[bj][q * 4 + k] = i < o.m && j0 + k < o.n ? y * to : 0.0f;
                 }
             }
-    }
-    char *stage = lds + (threadIdx.x >> 6) * kOrthoStage<T>;
-    if (!last) {
-        // X's own planes are read by no other tile; the transposed ones are, so they alternate.
-        char *xt = ws + o.at.xt[(o.step + 1) & 1u];
-        store_planes<T, 2>(stage, acc, w, ws + o.at.xh, ws + o.at.xl, o.m, o.np, o.np);
-        if (PLANES == 2 && w.col0 < o.np)
-#pragma unroll
-            for (int bi = 0; bi < T; ++bi)
-                store_32_rows<float, T * 32>(stage, o.np - w.col0, [&](int j, int r) { return acc[bi][j][r]; }, [&](uint32_t r) {
-                    const uint32_t i = w.row0 + bi * 32 + r;
-                    return i < o.m ? (float *)(ws + o.at.xf) + (uint64_t)i * o.np + w.col0 : nullptr;
-                });
-        store_planes_transposed<T, PLANES>(stage, acc, w, xt, xt + o.at.xt_lo, o.n, o.mp, o.mp);
-        return;
-    }
-    O *out = (O *)o.out + at.batch * o.stride_out;
-#pragma unroll
-    for (int bi = 0; bi < T; ++bi) {
         const uint32_t first = w.row0 + bi * 32;
-        if (first >= o.m || w.col0 >= o.n) break;
-        auto value = [&](int j, int r) { return acc[bi][j][r]; };
-        if (o.tall) {
-            store_32_cols<O, T * 32>(stage, o.m - first, value, [&](uint32_t c) {
-                return w.col0 + c < o.n ? out + (uint64_t)(w.col0 + c) * o.ld_out + first : nullptr;
-            });
-        } else {
-            store_32_rows<O, T * 32>(stage, o.n - w.col0, value, [&](uint32_t r) {
-                return first + r < o.m ? out + (uint64_t)(first + r) * o.ld_out + w.col0 : nullptr;
-            });
+        auto value = [&](int j, int r) { return v[j][r]; };
+        if (!last) {
+            store_planes<S, 2>(stage, v, first, w.col0, ws + o.at.xh, o.at.xl - o.at.xh, o.m, o.np, o.np);
+            if (PLANES == 2 && w.col0 < o.np)
+                store_32_rows<float, NT * 32>(stage, o.np - w.col0, value, [&](uint32_t r) {
+                    return first + r < o.m ? (float *)(ws + o.at.xf) + (uint64_t)(first + r) * o.np + w.col0 : nullptr;
+                });
+            store_planes_transposed<S, PLANES>(stage, v, first, w.col0, xt, o.at.xt_lo, o.n, o.mp, o.mp);
+        } else if (first < o.m && w.col0 < o.n) {
+            if (o.tall) {
+                store_32_cols<O, NT * 32>(stage, o.m - first, value, [&](uint32_t c) {
+                    return w.col0 + c < o.n ? out + (uint64_t)(w.col0 + c) * o.ld_out + first : nullptr;
+                });
+            } else {
+                store_32_rows<O, NT * 32>(stage, o.n - w.col0, value, [&](uint32_t r) {
+                    return first + r < o.m ? out + (uint64_t)(first + r) * o.ld_out + w.col0 : nullptr;
+                });
+            }
         }
-    }
+    });
 }
 
 }  // namespace dev
@@ -488,73 +475,94 @@ OrthoSpace ortho_space(const ar_ortho_desc &d, uint32_t mp, uint32_t np)
     return s;
 }
 
-// The tile (64 * T rows and columns) that finishes first: rounds over the 256
-// compute units times a tile's time, which goes with its area over the rate
-// its size reaches.
-int tile_for(size_t m, size_t n, size_t batch, bool lower)
+// Tiles, by planes: rows and columns, and what they cost.  `busy`: us of a
+// compute unit for k = 64 of a tile while it has several to work on; `alone`:
+// us for the same when one tile has the unit to itself (its loads' way to the
+// L2 and back is then in the open); `fit`: tiles that share a unit; `ends`: us
+// before and after the products.  Measured on products of 1024 x 1024 x 4096
+// (alone) and 8192 x 8192 x 8192 (busy).
+struct TileCost {
+    int side;
+    double busy, alone, ends;
+    int fit;
+};
+constexpr TileCost kTiles[2][4] = {
+    {{64, 0.19, 0.26, 2.5, 2}, {128, 0.5, 0.68, 4.0, 2}, {192, 1.1, 1.1, 6.0, 1}, {256, 1.67, 1.67, 9.0, 1}},
+    {{64, 0.4, 0.5, 3.0, 1}, {128, 1.2, 1.3, 6.0, 1}, {192, 2.8, 2.8, 9.0, 1}, {256, 4.6, 4.6, 14.0, 1}},
+};
+
+// The tile that finishes a product of k = 64 * steps first.
+int tile_for(int planes, size_t m, size_t n, size_t steps, size_t batch, bool lower)
 {
-    static const double rate[5] = {0, 0.35, 0.75, 0.9, 1.0};
-    int best = 1;
+    int best = 0;
     double least = 0;
-    for (int t = 1; t <= 4; ++t) {
-        const size_t a = (m + 64 * t - 1) / (64 * t), b = (n + 64 * t - 1) / (64 * t);
-        const size_t tiles = batch * (lower ? a * (a + 1) / 2 : a * b);
-        const double time = (double)((tiles + 255) / 256) * t * t / rate[t];
-        if (t == 1 || time < least) best = t, least = time;
+    for (int t = 0; t < 4; ++t) {
+        const TileCost &c = kTiles[planes - 1][t];
+        const size_t a = (m + c.side - 1) / c.side, b = (n + c.side - 1) / c.side;
+        const size_t tiles = batch * (lower ? a * (a + 1) / 2 : a * b), per_unit = (tiles + 255) / 256;
+        const double busy = per_unit * c.busy, alone = (double)((per_unit + c.fit - 1) / c.fit) * c.alone;
+        const double time = steps * (busy > alone ? busy : alone) + c.ends * per_unit;
+        if (t == 0 || time < least) best = t, least = time;
     }
     return best;
 }
 
-template <int T, int PLANES, bool SECOND> int launch_square(GemmArgs &g, const OrthoArgs &o, hipStream_t st)
+// The shapes of kTiles' tiles.
+template <int PLANES, int TILE> struct ShapeOf;
+template <> struct ShapeOf<1, 0> { typedef Shape<1, 1, 1, 64, 4> type; };
+template <> struct ShapeOf<1, 1> { typedef Shape<2, 2, 1, 64, 2> type; };
+template <> struct ShapeOf<1, 2> { typedef Shape<3, 3, 1, 64, 2> type; };
+template <> struct ShapeOf<1, 3> { typedef Shape<4, 4, 1, 64, 2> type; };
+template <> struct ShapeOf<2, 0> { typedef Shape<1, 1, 2, 64, 3> type; };
+template <> struct ShapeOf<2, 1> { typedef Shape<2, 2, 2, 64, 2> type; };
+template <> struct ShapeOf<2, 2> { typedef Shape<3, 3, 2, 32, 2> type; };
+template <> struct ShapeOf<2, 3> { typedef Shape<4, 4, 2, 32, 2> type; };
+
+template <typename S, bool SECOND> int launch_square(GemmArgs &g, const OrthoArgs &o, hipStream_t st)
 {
-    g.tiles_m = g.tiles_n = (o.m + T * 64 - 1) / (T * 64);
-    static const hipError_t set = hipFuncSetAttribute((const void *)ortho_square_kernel<T, PLANES, SECOND>,
-                                                      hipFuncAttributeMaxDynamicSharedMemorySize, kOrthoLds<T>);
+    g.tiles_m = g.tiles_n = (o.m + S::BM - 1) / S::BM;
+    static const hipError_t set = hipFuncSetAttribute((const void *)ortho_square_kernel<S, SECOND>,
+                                                      hipFuncAttributeMaxDynamicSharedMemorySize, kOrthoLds<S>);
     if (set != hipSuccess) return AR_ERR_HIP;
     const uint32_t tiles = g.tiles_m * (g.tiles_m + 1) / 2 * o.batch;
-    hipLaunchKernelGGL((ortho_square_kernel<T, PLANES, SECOND>), dim3(tiles), dim3(256), kOrthoLds<T>, st, g, o);
+    hipLaunchKernelGGL((ortho_square_kernel<S, SECOND>), dim3(tiles), dim3(S::THREADS), kOrthoLds<S>, st, g, o);
     return launch_status();
 }
 template <int PLANES, bool SECOND> int square(GemmArgs &g, const OrthoArgs &o, hipStream_t st)
 {
-    switch (tile_for(o.m, o.m, o.batch, true)) {
-    case 1: return launch_square<1, PLANES, SECOND>(g, o, st);
-    case 2: return launch_square<2, PLANES, SECOND>(g, o, st);
-    case 3: return launch_square<3, PLANES, SECOND>(g, o, st);
-    default: return launch_square<4, PLANES, SECOND>(g, o, st);
+    switch (tile_for(PLANES, o.m, o.m, g.steps, o.batch, true)) {
+    case 0: return launch_square<typename ShapeOf<PLANES, 0>::type, SECOND>(g, o, st);
+    case 1: return launch_square<typename ShapeOf<PLANES, 1>::type, SECOND>(g, o, st);
+    case 2: return launch_square<typename ShapeOf<PLANES, 2>::type, SECOND>(g, o, st);
+    default: return launch_square<typename ShapeOf<PLANES, 3>::type, SECOND>(g, o, st);
     }
 }
 
-template <int T, int PLANES, typename O> int launch_update(GemmArgs &g, const OrthoArgs &o, hipStream_t st)
+template <typename S, typename O> int launch_update(GemmArgs &g, const OrthoArgs &o, hipStream_t st)
 {
-    g.tiles_m = (o.m + T * 64 - 1) / (T * 64), g.tiles_n = (o.n + T * 64 - 1) / (T * 64);
-    static const hipError_t set = hipFuncSetAttribute((const void *)ortho_update_kernel<T, PLANES, O>,
-                                                      hipFuncAttributeMaxDynamicSharedMemorySize, kOrthoLds<T>);
+    g.tiles_m = (o.m + S::BM - 1) / S::BM, g.tiles_n = (o.n + S::BN - 1) / S::BN;
+    static const hipError_t set = hipFuncSetAttribute((const void *)ortho_update_kernel<S, O>,
+                                                      hipFuncAttributeMaxDynamicSharedMemorySize, kOrthoLds<S>);
     if (set != hipSuccess) return AR_ERR_HIP;
-    hipLaunchKernelGGL((ortho_update_kernel<T, PLANES, O>), dim3(g.tiles_m * g.tiles_n * o.batch), dim3(256), kOrthoLds<T>, st, g, o);
+    hipLaunchKernelGGL((ortho_update_kernel<S, O>), dim3(g.tiles_m * g.tiles_n * o.batch), dim3(S::THREADS), kOrthoLds<S>, st, g, o);
     return launch_status();
 }
 template <int PLANES, typename O> int update(GemmArgs &g, const OrthoArgs &o, hipStream_t st)
 {
-    switch (tile_for(o.m, o.n, o.batch, false)) {
-    case 1: return launch_update<1, PLANES, O>(g, o, st);
-    case 2: return launch_update<2, PLANES, O>(g, o, st);
-    case 3: return launch_update<3, PLANES, O>(g, o, st);
-    default: return launch_update<4, PLANES, O>(g, o, st);
+    switch (tile_for(PLANES, o.m, o.n, g.steps, o.batch, false)) {
+    case 0: return launch_update<typename ShapeOf<PLANES, 0>::type, O>(g, o, st);
+    case 1: return launch_update<typename ShapeOf<PLANES, 1>::type, O>(g, o, st);
+    case 2: return launch_update<typename ShapeOf<PLANES, 2>::type, O>(g, o, st);
+    default: return launch_update<typename ShapeOf<PLANES, 3>::type, O>(g, o, st);
     }
 }
 
-// A product of planes: hi hi, with two planes hi lo and lo hi too.
-template <int PLANES>
+// A product of a's rows and b's rows in the workspace.
 void operands(GemmArgs *g, const OrthoArgs &o, size_t a, size_t a_lo, size_t b, size_t b_lo, uint32_t k, uint32_t m, uint32_t n)
 {
     *g = GemmArgs{};
-    g->segments = PLANES == 2 ? 3 : 1;
-    g->steps = k / kStepK;
-    const char *pa = o.ws + a, *pb = o.ws + b;
-    g->a[0] = pa, g->b[0] = pb;
-    g->a[1] = pa, g->b[1] = pb + b_lo;
-    g->a[2] = pa + a_lo, g->b[2] = pb;
+    g->segments = 1, g->steps = k / kStepK;
+    g->a[0] = o.ws + a, g->b[0] = o.ws + b, g->a_lo = a_lo, g->b_lo = b_lo;
     g->lda = g->ldb = k * 2;
     g->m = m, g->n = n, g->batch_a = g->batch_b = o.at.bytes, g->batch = o.batch, g->splits = 1;
 }
@@ -569,11 +577,11 @@ template <typename O, int PLANES> int run_ortho(OrthoArgs &o, const float *coefs
     for (o.step = 0; o.step < o.steps; ++o.step) {
         o.a = coefs[3 * o.step], o.b = coefs[3 * o.step + 1], o.c = coefs[3 * o.step + 2];
         GemmArgs g;
-        operands<PLANES>(&g, o, o.at.xh, o.at.xl - o.at.xh, o.at.xh, o.at.xl - o.at.xh, o.np, o.m, o.m);
+        operands(&g, o, o.at.xh, o.at.xl - o.at.xh, o.at.xh, o.at.xl - o.at.xh, o.np, o.m, o.m);
         if ((rc = square<PLANES, false>(g, o, st)) != AR_OK) return rc;
-        operands<PLANES>(&g, o, o.at.a, o.at.a_lo, o.at.a, o.at.a_lo, o.mp, o.m, o.m);
+        operands(&g, o, o.at.a, o.at.a_lo, o.at.a, o.at.a_lo, o.mp, o.m, o.m);
         if ((rc = square<PLANES, true>(g, o, st)) != AR_OK) return rc;
-        operands<PLANES>(&g, o, o.at.b, o.at.b_lo, o.at.xt[o.step & 1u], o.at.xt_lo, o.mp, o.m, o.n);
+        operands(&g, o, o.at.b, o.at.b_lo, o.at.xt[o.step & 1u], o.at.xt_lo, o.mp, o.m, o.n);
         if ((rc = update<PLANES, O>(g, o, st)) != AR_OK) return rc;
     }
     return AR_OK;

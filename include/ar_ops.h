@@ -110,7 +110,7 @@ enum { AR_ACT_SILU = 0, AR_ACT_GELU = 1, AR_ACT_RELU = 2 };
  *     h = act(G) * U */
 typedef struct ar_ffn_desc {
     size_t tokens;         /* 0 is a valid no-op (backward: zero weight gradients) */
-    size_t dim, hidden;    /* 1 or more */
+    size_t dim, hidden;    /* 1 .. 2^20 */
     int dtype;             /* AR_BFLOAT16 */
     int act;               /* AR_ACT_* */
     size_t ld_x, ld_w_gate, ld_w_up, ld_h;  /* row strides (ld_h: also of dh) */

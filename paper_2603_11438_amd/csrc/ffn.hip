@@ -54,107 +54,63 @@ template <typename S, int ACT> __global__ __launch_bounds__(S::THREADS) void ffn
         constexpr int i = block.value;
         float v[NT][16];
         take(acc[i], v);
-        auto row_of = [&](auto *base, uint64_t ld) {
-            return [=](uint32_t r) { return row0 + i * 32 + r < g.m ? base + (uint64_t)(row0 + i * 32 + r) * ld + col0 : nullptr; };
-        };
+        const uint32_t first = row0 + i * 32;
+        if (first >= g.m) return;
+        const uint32_t rows = g.m - first;
         if (o.saved) {
-            store_32_rows<float, HALF>(stage, cols, [&](int j, int r) { return v[j][r]; }, row_of(o.saved, g.n));
-            store_32_rows<float, HALF>(stage, cols, [&](int j, int r) { return v[j + NT / 2][r]; },
-                                       row_of(o.saved + (uint64_t)g.m * g.n, g.n));
+            float *to = o.saved + (uint64_t)first * g.n + col0;
+            stage_rows<float, HALF>(stage, [&](int j, int r) { return v[j][r]; });
+            write_rows<float, HALF>(stage, to, g.n, 0, rows, cols);
+            stage_rows<float, HALF>(stage, [&](int j, int r) { return v[j + NT / 2][r]; });
+            write_rows<float, HALF>(stage, to + (uint64_t)g.m * g.n, g.n, 0, rows, cols);
         }
-        store_32_rows<bf16, HALF>(stage, cols, [&](int j, int r) { return activation<ACT>(v[j][r]) * v[j + NT / 2][r]; },
-                                  row_of(o.h, o.ld_h));
+        stage_rows<bf16, HALF>(stage, [&](int j, int r) { return activation<ACT>(v[j][r]) * v[j + NT / 2][r]; });
+        write_rows<bf16, HALF>(stage, o.h + (uint64_t)first * o.ld_h + col0, o.ld_h, 0, rows, cols);
     });
 }
 
-// Copies a matrix into rows of `to_ld` elements, zeros behind its columns.
+// Copies a matrix into `to_rows` rows of `to_ld` elements, zeros behind its
+// rows and columns.
 struct PackArgs {
     const bf16 *from;
     bf16 *to;
-    uint64_t rows, ld, to_ld;
+    uint64_t rows, ld, to_rows, to_ld;
     uint32_t cols;
 };
-__global__ void pack_kernel(const PackArgs p)
+__global__ __launch_bounds__(256) void pack_kernel(const PackArgs p)
 {
-    const uint64_t n = p.rows * (p.to_ld / 8);
-    for (uint64_t i = (uint64_t)blockIdx.x * blockDim.x + threadIdx.x; i < n; i += (uint64_t)gridDim.x * blockDim.x) {
-        const uint64_t row = i / (p.to_ld / 8);
-        const uint32_t c = (uint32_t)(i % (p.to_ld / 8)) * 8;
+    const uint64_t per = p.to_ld / 8, n = p.to_rows * per;
+    for (uint64_t i = (uint64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (uint64_t)gridDim.x * 256) {
+        const uint64_t row = i / per;
+        const uint32_t c = (uint32_t)(i % per) * 8;
         const bf16 *from = p.from + row * p.ld + c;
-        bf16x8 v;
-        if (c + 8 <= p.cols) {
-            v = (bf16x8)*(const VecOf<bf16, 8>::type *)from;
-        } else {
-#pragma unroll
-            for (uint32_t k = 0; k < 8; ++k) v[k] = c + k < p.cols ? from[k] : (bf16)0.0f;
-        }
-        *(bf16x8 *)(p.to + row * p.to_ld + c) = v;
-    }
-}
-
-// The transpose of a matrix, with zeros behind the rows' end up to to_ld
-// columns: tiles of 64 x 64 through LDS.  The tile's rows are 66 elements apart
-// there, so that the columns read back lie in different banks.
-struct TransposeArgs {
-    const bf16 *from;
-    bf16 *to;
-    uint64_t ld, to_ld;
-    uint32_t rows, cols;
-};
-constexpr int kTile = 64, kTilePitch = 66;
-
-// Writes the transpose of a staged tile: to[c][r] for the tile's columns c
-// below `cols`, every r of the tile.
-__device__ __forceinline__ void store_transposed(const bf16 (*tile)[kTilePitch], bf16 *to, uint64_t to_ld, uint32_t cols)
-{
-    for (uint32_t i = threadIdx.x; i < kTile * kTile / 8; i += 256) {
-        const uint32_t c = i / 8, r = i % 8 * 8;
-        bf16x8 v;
-#pragma unroll
-        for (int k = 0; k < 8; ++k) v[k] = tile[r + k][c];
-        if (c < cols) *(bf16x8 *)(to + (uint64_t)c * to_ld + r) = v;
-    }
-}
-
-__global__ __launch_bounds__(256) void transpose_kernel(const TransposeArgs t)
-{
-    __shared__ bf16 tile[kTile][kTilePitch];
-    const uint32_t r0 = blockIdx.y * kTile, c0 = blockIdx.x * kTile;
-    for (uint32_t i = threadIdx.x; i < kTile * kTile / 8; i += 256) {
-        const uint32_t r = i / 8, c = i % 8 * 8;
-        const bf16 *from = t.from + (uint64_t)(r0 + r) * t.ld + c0 + c;
         float v[8];
-        if (r0 + r < t.rows && c0 + c + 8 <= t.cols) load_vec<bf16, 8>(from, v);
-        else load_part<bf16, 8>(from, r0 + r < t.rows && c0 + c < t.cols ? (int)(t.cols - c0 - c) : 0, v);
-#pragma unroll
-        for (int k = 0; k < 8; ++k) tile[r][c + k] = (bf16)v[k];
+        if (row < p.rows && c + 8 <= p.cols) load_vec<bf16, 8>(from, v);
+        else load_part<bf16, 8>(from, row < p.rows && c < p.cols ? (int)(p.cols - c) : 0, v);
+        store_vec<bf16, 8>(p.to + row * p.to_ld + c, v);
     }
-    __syncthreads();
-    store_transposed(tile, t.to + (uint64_t)c0 * t.to_ld + r0, t.to_ld, t.cols - c0 < kTile ? t.cols - c0 : kTile);
 }
 
 // dG = dh * U * act'(G) and dU = dh * act(G) from the saved projections, rounded
-// to bf16 as operands of the backward products: by rows for dx, transposed for
-// the weights' gradients, zeros in the padding of both.
+// to bf16 as operands of the backward products: rows of dG, then dU, with zeros
+// behind the columns of each and behind the rows.
 struct GradArgs {
     const float *saved;
     const bf16 *dh;
-    bf16 *by_rows;      // tokens x 2 hidden_ld: dG, then dU in each row; null: not wanted
-    bf16 *transposed;   // 2 hidden x tokens_ld: dG^T, then dU^T; null: not wanted
-    uint64_t ld_dh, hidden_ld, tokens_ld;
-    uint32_t tokens, hidden;
+    bf16 *to;
+    uint64_t ld_dh, tokens, to_tokens;
+    uint32_t hidden, to_hidden;
 };
 template <int ACT> __global__ __launch_bounds__(256) void ffn_grad_kernel(const GradArgs a)
 {
-    __shared__ bf16 tg[kTile][kTilePitch], tu[kTile][kTilePitch];
-    const uint32_t t0 = blockIdx.y * kTile, f0 = blockIdx.x * kTile;
-    const uint64_t half = (uint64_t)a.tokens * a.hidden;
-    for (uint32_t i = threadIdx.x; i < kTile * kTile / 8; i += 256) {
-        const uint32_t r = i / 8, c = i % 8 * 8, t = t0 + r, f = f0 + c;
+    const uint64_t per = a.to_hidden / 8, n = a.to_tokens * per, half = a.tokens * a.hidden;
+    for (uint64_t i = (uint64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (uint64_t)gridDim.x * 256) {
+        const uint64_t t = i / per;
+        const uint32_t f = (uint32_t)(i % per) * 8;
         float g[8], u[8], d[8];
         const int have = t < a.tokens && f < a.hidden ? (int)(a.hidden - f) : 0;
-        const float *from = a.saved + (uint64_t)t * a.hidden + f;
-        const bf16 *dh = a.dh + (uint64_t)t * a.ld_dh + f;
+        const float *from = a.saved + t * a.hidden + f;
+        const bf16 *dh = a.dh + t * a.ld_dh + f;
         if (have >= 8) {
             load_vec<float, 8>(from, g);
             load_vec<float, 8>(from + half, u);
@@ -164,78 +120,83 @@ template <int ACT> __global__ __launch_bounds__(256) void ffn_grad_kernel(const 
             load_part<float, 8>(from + half, have, u);
             load_part<bf16, 8>(dh, have, d);
         }
-        bf16x8 vg, vu;
 #pragma unroll
         for (int k = 0; k < 8; ++k) {
             float slope;
             const float act = activation<ACT>(g[k], &slope);
-            vg[k] = (bf16)(d[k] * u[k] * slope);
-            vu[k] = (bf16)(d[k] * act);
-            tg[r][c + k] = vg[k];
-            tu[r][c + k] = vu[k];
+            g[k] = d[k] * u[k] * slope;
+            u[k] = d[k] * act;
         }
-        if (a.by_rows && t < a.tokens) {
-            bf16 *to = a.by_rows + (uint64_t)t * 2 * a.hidden_ld + f;
-            *(bf16x8 *)to = vg;
-            *(bf16x8 *)(to + a.hidden_ld) = vu;
-        }
+        bf16 *to = a.to + t * 2 * a.to_hidden + f;
+        store_vec<bf16, 8>(to, g);
+        store_vec<bf16, 8>(to + a.to_hidden, u);
     }
-    if (!a.transposed) return;
-    __syncthreads();
-    const uint32_t cols = f0 >= a.hidden ? 0 : a.hidden - f0 < kTile ? a.hidden - f0 : kTile;
-    store_transposed(tg, a.transposed + (uint64_t)f0 * a.tokens_ld + t0, a.tokens_ld, cols);
-    store_transposed(tu, a.transposed + (uint64_t)(a.hidden + f0) * a.tokens_ld + t0, a.tokens_ld, cols);
 }
 
-// A plain product: rows below `split` of the result go to out, the others to
-// out2.  With k split, each run's sums go to `part` instead, [run][m][n].
+// A plain product.  Its rows belong to results of `half` rows each (a multiple
+// of 32), of which the first `rows` exist: one result, or dWg and then dWu.
+// With k split, each run's sums go to `part` instead, [run][m][cols].
 struct ProductOut {
-    bf16 *out, *out2;
+    bf16 *out[2];
     float *part;
-    uint64_t ld, ld2;
-    uint32_t split;
+    uint64_t ld[2];
+    uint32_t half, rows, cols;
 };
-template <typename S> __global__ __launch_bounds__(S::THREADS) void product_kernel(const GemmArgs g, const ProductOut o)
+template <typename S, bool ABYK> __global__ __launch_bounds__(S::THREADS) void product_kernel(const GemmArgs g, const ProductOut o)
 {
     constexpr int NT = S::NT, COLS = NT * 32;
     extern __shared__ __attribute__((aligned(16))) char lds[];
     const TileAt at = tile_at(g.tiles_m, g.tiles_n, 1);
     f32x16 acc[S::MT][NT];
-    gemm_tile<bf16, S, false>(g, at, lds, acc);
+    gemm_tile<bf16, S, false, ABYK, true>(g, at, lds, acc);
     const uint32_t wave = threadIdx.x >> 6;
     const uint32_t row0 = at.m * S::BM + (wave >> 1) * S::MT * 32, col0 = at.n * S::BN + (wave & 1u) * COLS;
-    if (col0 >= g.n) return;
+    if (col0 >= o.cols) return;
     char *stage = lds + wave * kStageBytes<float, COLS>;
     static_for<S::MT>([&](auto block) {
         constexpr int i = block.value;
         float v[NT][16];
         take(acc[i], v);
-        auto value = [&](int j, int r) { return v[j][r]; };
+        const uint32_t first = row0 + i * 32, which = first >= o.half, r = first - which * o.half;
+        if (first >= g.m || r >= o.rows) return;
+        auto value = [&](int j, int q) { return v[j][q]; };
         if (g.splits > 1) {
-            store_32_rows<float, COLS>(stage, g.n - col0, value, [&](uint32_t r) {
-                const uint32_t m = row0 + i * 32 + r;
-                return m < g.m ? o.part + ((uint64_t)blockIdx.y * g.m + m) * g.n + col0 : nullptr;
-            });
+            stage_rows<float, COLS>(stage, value);
+            write_rows<float, COLS>(stage, o.part + ((uint64_t)blockIdx.y * g.m + first) * o.cols + col0, o.cols, 0, o.rows - r,
+                                    o.cols - col0);
         } else {
-            store_32_rows<bf16, COLS>(stage, g.n - col0, value, [&](uint32_t r) {
-                const uint32_t m = row0 + i * 32 + r;
-                bf16 *to = m < o.split ? o.out + (uint64_t)m * o.ld : o.out2 + (uint64_t)(m - o.split) * o.ld2;
-                return m < g.m ? to + col0 : nullptr;
-            });
+            stage_rows<bf16, COLS>(stage, value);
+            write_rows<bf16, COLS>(stage, o.out[which] + (uint64_t)r * o.ld[which] + col0, o.ld[which], 0, o.rows - r, o.cols - col0);
         }
     });
 }
 
-// Adds the runs of a split product in their order.
-__global__ void join_kernel(const ProductOut o, uint32_t m, uint32_t n, uint32_t splits)
+// Adds the runs of a split product in their order, four columns a thread.
+__global__ __launch_bounds__(256) void join_kernel(const ProductOut o, uint32_t m, uint32_t splits)
 {
-    const uint64_t all = (uint64_t)m * n;
-    for (uint64_t i = (uint64_t)blockIdx.x * blockDim.x + threadIdx.x; i < all; i += (uint64_t)gridDim.x * blockDim.x) {
-        float v = o.part[i];
-        for (uint32_t s = 1; s < splits; ++s) v += o.part[s * all + i];
-        const uint32_t row = (uint32_t)(i / n), col = (uint32_t)(i % n);
-        bf16 *to = row < o.split ? o.out + (uint64_t)row * o.ld : o.out2 + (uint64_t)(row - o.split) * o.ld2;
-        to[col] = (bf16)v;
+    const uint64_t all = (uint64_t)m * o.cols, per = (o.cols + 3) / 4, n = m * per;
+    for (uint64_t i = (uint64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (uint64_t)gridDim.x * 256) {
+        const uint32_t row = (uint32_t)(i / per), c = (uint32_t)(i % per) * 4, which = row >= o.half, r = row - which * o.half;
+        if (r >= o.rows) continue;
+        const float *from = o.part + (uint64_t)row * o.cols + c;
+        bf16 *to = o.out[which] + (uint64_t)r * o.ld[which] + c;
+        float v[4], w[4];
+        if (c + 4 <= o.cols) {
+            load_vec<float, 4>(from, v);
+#pragma unroll 4
+            for (uint32_t s = 1; s < splits; ++s) {
+                load_vec<float, 4>(from + s * all, w);
+#pragma unroll
+                for (int k = 0; k < 4; ++k) v[k] += w[k];
+            }
+            store_vec<bf16, 4>(to, v);
+        } else {
+            for (uint32_t k = 0; k < o.cols - c; ++k) {
+                float t = from[k];
+                for (uint32_t s = 1; s < splits; ++s) t += from[s * all + k];
+                to[k] = (bf16)t;
+            }
+        }
     }
 }
 
@@ -250,8 +211,9 @@ int check_ffn(const ar_ffn_desc *d)
     if (!d) return AR_ERR_ARG;
     if (d->dtype != AR_BFLOAT16) return AR_ERR_UNSUPPORTED;
     if (d->act < AR_ACT_SILU || d->act > AR_ACT_RELU) return AR_ERR_ARG;
-    // rows and columns are counted in 32 bits on the device
-    if (d->dim < 1 || d->hidden < 1 || d->tokens > (1u << 30) || d->dim > (1u << 20) || d->hidden > (1u << 28)) return AR_ERR_ARG;
+    // rows and columns are counted in 32 bits on the device, and a tile's rows reached by 31
+    if (d->dim < 1 || d->hidden < 1 || d->tokens > (1u << 30) || d->dim > (1u << 20) || d->hidden > (1u << 20)) return AR_ERR_ARG;
+    if (d->tokens * d->hidden > kOpsMaxSize || d->tokens * d->dim > kOpsMaxSize || d->hidden * d->dim > kOpsMaxSize) return AR_ERR_ARG;
     const struct {
         size_t ld, cols, rows;
     } lds[] = {{d->ld_x, d->dim, d->tokens},       {d->ld_w_gate, d->dim, d->hidden}, {d->ld_w_up, d->dim, d->hidden},
@@ -262,36 +224,44 @@ int check_ffn(const ar_ffn_desc *d)
     return AR_OK;
 }
 
-// Whether the product kernel can read a matrix where it lies.
-bool direct(const Mat &m)
+// Whether the product kernel can read a matrix where it lies, by rows or by k.
+bool direct(const Mat &m, bool by_k)
 {
-    return m.cols % kStepK == 0 && (uintptr_t)m.p % 16 == 0 && m.ld % 8 == 0 && gemm_reaches(m.ld * 2, m.cols * 2);
+    if ((uintptr_t)m.p % 16 != 0 || m.ld % 8 != 0 || !gemm_reaches(m.ld * 2, m.cols * 2)) return false;
+    return by_k ? m.rows % kStepK == 0 && m.cols % 8 == 0 : m.cols % kStepK == 0;
 }
-size_t packed_bytes(size_t rows, size_t cols) { return round_up(rows * round_up(cols, kStepK) * 2, 256); }
+size_t packed_bytes(size_t rows, size_t cols, bool by_k)
+{
+    return round_up((by_k ? round_up(rows, kStepK) : rows) * round_up(cols, kStepK) * 2, 256);
+}
 
 // A matrix as the product kernel takes it: itself, or a copy in the workspace.
 struct Operand {
     const void *p;
-    uint32_t ld;  // bytes
+    uint32_t ld;    // bytes
+    uint32_t cols;  // that can be read
 };
 
-int pack(const Mat &m, char *&ws, hipStream_t st, Operand *out)
+int pack(const Mat &m, bool by_k, bool as_is, char *&ws, hipStream_t st, Operand *out)
 {
-    if (direct(m)) {
-        *out = {m.p, (uint32_t)(m.ld * 2)};
+    if (as_is) {
+        *out = {m.p, (uint32_t)(m.ld * 2), (uint32_t)m.cols};
         return AR_OK;
     }
-    const size_t to_ld = round_up(m.cols, kStepK);
-    PackArgs p{(const bf16 *)m.p, (bf16 *)ws, m.rows, m.ld, to_ld, (uint32_t)m.cols};
-    const uint64_t groups = (m.rows * (to_ld / 8) + 255) / 256;
+    const size_t to_ld = round_up(m.cols, kStepK), to_rows = by_k ? round_up(m.rows, kStepK) : m.rows;
+    PackArgs p{(const bf16 *)m.p, (bf16 *)ws, m.rows, m.ld, to_rows, to_ld, (uint32_t)m.cols};
+    const uint64_t groups = (to_rows * (to_ld / 8) + 255) / 256;
     hipLaunchKernelGGL(pack_kernel, dim3((uint32_t)(groups < 8192 ? groups : 8192)), dim3(256), 0, st, p);
-    *out = {ws, (uint32_t)(to_ld * 2)};
-    ws += packed_bytes(m.rows, m.cols);
+    *out = {ws, (uint32_t)(to_ld * 2), (uint32_t)to_ld};
+    ws += packed_bytes(m.rows, m.cols, by_k);
     return launch_status();
 }
 
 typedef Shape<4, 4, 1, 64, 2> Large;
+typedef Shape<3, 3, 1, 64, 2> Middle;
 typedef Shape<2, 2, 1, 64, 2> Small;
+typedef Shape<1, 1, 1, 64, 4> Tiny;
+typedef Shape<1, 2, 1, 64, 3> Flat;  // 64 tokens, both projections of 64 columns
 
 template <typename S, int ACT> int launch_ffn(GemmArgs &g, const FfnOut &o, hipStream_t st)
 {
@@ -306,8 +276,10 @@ template <typename S, int ACT> int launch_ffn(GemmArgs &g, const FfnOut &o, hipS
 
 template <int ACT> int launch_ffn_tiles(GemmArgs &g, const FfnOut &o, hipStream_t st)
 {
-    const size_t large = (size_t)((g.m + 255) / 256) * ((g.n + 127) / 128);
-    return large >= 256 ? launch_ffn<Large, ACT>(g, o, st) : launch_ffn<Small, ACT>(g, o, st);
+    // the pairs' columns count twice
+    if (g.m <= 64) return launch_ffn<Flat, ACT>(g, o, st);
+    return cut_for(1, g.m, 2 * (size_t)g.n, g.steps, 1, false, 1, 3, 1).tile == 1 ? launch_ffn<Small, ACT>(g, o, st)
+                                                                                  : launch_ffn<Large, ACT>(g, o, st);
 }
 
 struct FfnMats {
@@ -323,7 +295,7 @@ FfnMats ffn_mats(const ar_ffn_desc &d, const void *x, const void *wg, const void
 // before the call, so every operand counts.
 size_t ffn_workspace(const ar_ffn_desc &d)
 {
-    return packed_bytes(d.tokens, d.dim) + 2 * packed_bytes(d.hidden, d.dim);
+    return packed_bytes(d.tokens, d.dim, false) + 2 * packed_bytes(d.hidden, d.dim, false);
 }
 
 int ffn(const ar_ffn_desc *desc, const void *x, const void *wg, const void *wu, void *h, float *saved, void *ws,
@@ -341,7 +313,7 @@ int ffn(const ar_ffn_desc *desc, const void *x, const void *wg, const void *wu, 
     if (meet(m.h, sv)) return AR_ERR_ARG;
     size_t need = 0;
     for (const Mat &in : {m.x, m.wg, m.wu})
-        if (!direct(in)) need += packed_bytes(in.rows, in.cols);
+        if (!direct(in, false)) need += packed_bytes(in.rows, in.cols, false);
     if (need) {
         if (!ws || ws_bytes < need) return AR_ERR_SCRATCH;
         if ((uintptr_t)ws % 256 != 0) return AR_ERR_ARG;
@@ -352,8 +324,9 @@ int ffn(const ar_ffn_desc *desc, const void *x, const void *wg, const void *wu, 
     hipStream_t st = (hipStream_t)stream;
     char *at = (char *)ws;
     Operand px, pg, pu;
-    if ((rc = pack(m.x, at, st, &px)) != AR_OK || (rc = pack(m.wg, at, st, &pg)) != AR_OK || (rc = pack(m.wu, at, st, &pu)) != AR_OK)
-        return rc;
+    if ((rc = pack(m.x, false, direct(m.x, false), at, st, &px)) != AR_OK) return rc;
+    if ((rc = pack(m.wg, false, direct(m.wg, false), at, st, &pg)) != AR_OK) return rc;
+    if ((rc = pack(m.wu, false, direct(m.wu, false), at, st, &pu)) != AR_OK) return rc;
     GemmArgs g{};
     g.a[0] = px.p, g.b[0] = pg.p, g.b2 = pu.p;
     g.lda = px.ld, g.ldb = pg.ld, g.ldb2 = pu.ld;
@@ -369,88 +342,60 @@ int ffn(const ar_ffn_desc *desc, const void *x, const void *wg, const void *wu, 
 
 // ---- backward ---------------------------------------------------------------
 
-// A product's tile (64 * tile rows and columns) and the runs its k is split
-// into.  Large tiles where they fill the device, else small ones; where even
-// those leave most of it idle, k is split until they do not, in runs of at
-// least four steps.
-struct Cut {
-    int tile;
-    uint32_t splits;
-};
-Cut cut_of(size_t m, size_t n, size_t steps)
+constexpr uint32_t kMaxSplits = 32;
+size_t part_bytes(size_t m, size_t cols, size_t steps)
 {
-    const size_t large = ((m + 255) / 256) * ((n + 255) / 256), small = ((m + 127) / 128) * ((n + 127) / 128);
-    if (large >= 256) return {4, 1};
-    if (small >= 192) return {2, 1};
-    size_t splits = 512 / small;
-    if (splits > steps / 4) splits = steps / 4;
-    if (splits > 64) splits = 64;
-    return {2, (uint32_t)(splits ? splits : 1)};
-}
-size_t part_bytes(size_t m, size_t n, size_t steps)
-{
-    const Cut c = cut_of(m, n, steps);
-    return c.splits > 1 ? round_up(c.splits * m * n * sizeof(float), 256) : 0;
+    const Cut c = cut_for(1, m, cols, steps, 1, false, 0, 3, kMaxSplits);
+    return c.splits > 1 ? round_up(c.splits * m * cols * sizeof(float), 256) : 0;
 }
 
-template <typename S> int launch_product(GemmArgs &g, const ProductOut &o, hipStream_t st)
+template <typename S, bool ABYK> int launch_product(GemmArgs &g, const ProductOut &o, hipStream_t st)
 {
     g.tiles_m = (g.m + S::BM - 1) / S::BM;
-    g.tiles_n = (g.n + S::BN - 1) / S::BN;
+    g.tiles_n = (o.cols + S::BN - 1) / S::BN;
     constexpr int STAGE = 4 * kStageBytes<float, S::NT * 32>, LDS = S::LDS > STAGE ? S::LDS : STAGE;
-    static const hipError_t set = hipFuncSetAttribute((const void *)product_kernel<S>, hipFuncAttributeMaxDynamicSharedMemorySize, LDS);
+    static const hipError_t set = hipFuncSetAttribute((const void *)product_kernel<S, ABYK>, hipFuncAttributeMaxDynamicSharedMemorySize, LDS);
     if (set != hipSuccess) return AR_ERR_HIP;
-    hipLaunchKernelGGL((product_kernel<S>), dim3(g.tiles_m * g.tiles_n, g.splits), dim3(S::THREADS), LDS, st, g, o);
+    hipLaunchKernelGGL((product_kernel<S, ABYK>), dim3(g.tiles_m * g.tiles_n, g.splits), dim3(S::THREADS), LDS, st, g, o);
     int rc = launch_status();
     if (rc != AR_OK || g.splits == 1) return rc;
-    const uint64_t groups = ((uint64_t)g.m * g.n + 255) / 256;
-    hipLaunchKernelGGL(join_kernel, dim3((uint32_t)(groups < 4096 ? groups : 4096)), dim3(256), 0, st, o, g.m, g.n, g.splits);
+    const uint64_t groups = ((uint64_t)g.m * ((o.cols + 3) / 4) + 255) / 256;
+    hipLaunchKernelGGL(join_kernel, dim3((uint32_t)(groups < 8192 ? groups : 8192)), dim3(256), 0, st, o, g.m, g.splits);
     return launch_status();
 }
 
-int product(GemmArgs &g, const ProductOut &o, hipStream_t st)
+// B by k; A by rows (dx) or by k (the weights' gradients).
+template <bool ABYK> int product(GemmArgs &g, const ProductOut &o, hipStream_t st)
 {
-    const Cut c = cut_of(g.m, g.n, (size_t)g.steps * g.segments);
+    const Cut c = cut_for(1, g.m, o.cols, (size_t)g.steps * g.segments, 1, false, 0, 3, kMaxSplits);
     g.splits = c.splits, g.batch = 1;
-    return c.tile == 4 ? launch_product<Large>(g, o, st) : launch_product<Small>(g, o, st);
-}
-
-int transpose(const Mat &m, void *to, size_t to_ld, hipStream_t st)
-{
-    TransposeArgs t{(const bf16 *)m.p, (bf16 *)to, m.ld, to_ld, (uint32_t)m.rows, (uint32_t)m.cols};
-    hipLaunchKernelGGL(transpose_kernel, dim3((uint32_t)((m.cols + kTile - 1) / kTile), (uint32_t)(to_ld / kTile)), dim3(256), 0, st, t);
-    return launch_status();
+    switch (c.tile) {
+    case 0: return launch_product<Tiny, ABYK>(g, o, st);
+    case 1: return launch_product<Small, ABYK>(g, o, st);
+    case 2: return launch_product<Middle, ABYK>(g, o, st);
+    default: return launch_product<Large, ABYK>(g, o, st);
+    }
 }
 
 // Where the backward pass keeps what, in bytes from the workspace's start.
+// Copies of operands lie behind the rest, as many as there are.
 struct FfnBackwardSpace {
-    size_t tokens_ld, hidden_ld;
-    size_t by_rows, wg_t, wu_t, transposed, x_t, part, bytes;
+    size_t tokens, hidden;  // padded
+    size_t grads, part, copies;
 };
 FfnBackwardSpace ffn_backward_space(const ar_ffn_desc &d, bool dx, bool dw)
 {
     FfnBackwardSpace s{};
-    s.tokens_ld = round_up(d.tokens, kStepK), s.hidden_ld = round_up(d.hidden, kStepK);
-    size_t at = 0, parts = 0;
-    auto take = [&](size_t bytes) {
-        const size_t here = at;
-        at += round_up(bytes, 256);
-        return here;
-    };
-    if (dx) {
-        s.by_rows = take(d.tokens * 2 * s.hidden_ld * 2);
-        s.wg_t = take(d.dim * s.hidden_ld * 2);
-        s.wu_t = take(d.dim * s.hidden_ld * 2);
-        parts = part_bytes(d.tokens, d.dim, 2 * s.hidden_ld / kStepK);
-    }
+    s.tokens = round_up(d.tokens, kStepK), s.hidden = round_up(d.hidden, kStepK);
+    size_t parts = 0;
+    if (dx) parts = part_bytes(d.tokens, d.dim, 2 * s.hidden / kStepK);
     if (dw) {
-        s.transposed = take(2 * d.hidden * s.tokens_ld * 2);
-        s.x_t = take(d.dim * s.tokens_ld * 2);
-        const size_t p = part_bytes(2 * d.hidden, d.dim, s.tokens_ld / kStepK);
+        const size_t p = part_bytes(2 * s.hidden, d.dim, s.tokens / kStepK);
         parts = p > parts ? p : parts;
     }
-    s.part = take(parts);
-    s.bytes = at;
+    s.grads = 0;
+    s.part = round_up(s.tokens * 2 * s.hidden * 2, 256);
+    s.copies = s.part + parts;
     return s;
 }
 
@@ -485,23 +430,25 @@ int ffn_backward(const ar_ffn_desc *desc, const void *dh, const void *x, const v
         return rc != AR_OK ? rc : zero_rows(ou, st);
     }
     if (!m.x.ok() || !m.wg.ok() || !m.wu.ok() || !m.h.ok() || !saved || (uintptr_t)saved % 16 != 0) return AR_ERR_ARG;
+    if (!dx && !dwg) return AR_OK;  // nothing wanted
     const FfnBackwardSpace s = ffn_backward_space(d, dx != nullptr, dwg != nullptr);
-    if (s.bytes == 0) return AR_OK;  // nothing wanted
-    if (!ws || ws_bytes < s.bytes) return AR_ERR_SCRATCH;
+    // both weights are read with one row stride
+    const bool w_direct = direct(m.wg, true) && direct(m.wu, true) && m.wg.ld == m.wu.ld, x_direct = direct(m.x, true);
+    size_t need = s.copies;
+    if (dx && !w_direct) need += 2 * packed_bytes(d.hidden, d.dim, true);
+    if (dwg && !x_direct) need += packed_bytes(d.tokens, d.dim, true);
+    if (!ws || ws_bytes < need) return AR_ERR_SCRATCH;
     if ((uintptr_t)ws % 256 != 0) return AR_ERR_ARG;
-    const Mat wsm{ws, 1, s.bytes, s.bytes, 1};
+    const Mat wsm{ws, 1, need, need, 1};
     for (const Mat &in : {m.x, m.wg, m.wu, m.h, sv, wsm})
         if (meet(odx, in) || meet(og, in) || meet(ou, in)) return AR_ERR_ARG;
     for (const Mat &in : {m.x, m.wg, m.wu, m.h, sv})
         if (meet(wsm, in)) return AR_ERR_ARG;
 
-    char *w = (char *)ws;
-    GradArgs ga{};
-    ga.saved = saved, ga.dh = (const bf16 *)dh, ga.ld_dh = m.h.ld;
-    ga.by_rows = dx ? (bf16 *)(w + s.by_rows) : nullptr;
-    ga.transposed = dwg ? (bf16 *)(w + s.transposed) : nullptr;
-    ga.hidden_ld = s.hidden_ld, ga.tokens_ld = s.tokens_ld, ga.tokens = (uint32_t)d.tokens, ga.hidden = (uint32_t)d.hidden;
-    const dim3 grid((uint32_t)(s.hidden_ld / kTile), (uint32_t)(s.tokens_ld / kTile));
+    char *w = (char *)ws, *copies = w + s.copies;
+    const GradArgs ga{saved, (const bf16 *)dh, (bf16 *)(w + s.grads), m.h.ld, d.tokens, s.tokens, (uint32_t)d.hidden, (uint32_t)s.hidden};
+    const uint64_t groups = (s.tokens * (s.hidden / 8) + 255) / 256;
+    const dim3 grid((uint32_t)(groups < 16384 ? groups : 16384));
     switch (d.act) {
     case AR_ACT_SILU: hipLaunchKernelGGL((ffn_grad_kernel<AR_ACT_SILU>), grid, dim3(256), 0, st, ga); break;
     case AR_ACT_GELU: hipLaunchKernelGGL((ffn_grad_kernel<AR_ACT_GELU>), grid, dim3(256), 0, st, ga); break;
@@ -509,26 +456,28 @@ int ffn_backward(const ar_ffn_desc *desc, const void *dh, const void *x, const v
     }
     if ((rc = launch_status()) != AR_OK) return rc;
     if (dx) {
-        if ((rc = transpose(m.wg, w + s.wg_t, s.hidden_ld, st)) != AR_OK) return rc;
-        if ((rc = transpose(m.wu, w + s.wu_t, s.hidden_ld, st)) != AR_OK) return rc;
+        Operand pg, pu;
+        if ((rc = pack(m.wg, true, w_direct, copies, st, &pg)) != AR_OK) return rc;
+        if ((rc = pack(m.wu, true, w_direct, copies, st, &pu)) != AR_OK) return rc;
         GemmArgs g{};
-        g.segments = 2, g.steps = (uint32_t)(s.hidden_ld / kStepK);
-        g.a[0] = w + s.by_rows, g.a[1] = w + s.by_rows + s.hidden_ld * 2;
-        g.b[0] = w + s.wg_t, g.b[1] = w + s.wu_t;
-        g.lda = (uint32_t)(s.hidden_ld * 4), g.ldb = (uint32_t)(s.hidden_ld * 2);
-        g.m = (uint32_t)d.tokens, g.n = (uint32_t)d.dim;
-        const ProductOut o{(bf16 *)dx, nullptr, (float *)(w + s.part), odx.ld, 0, (uint32_t)d.tokens};
-        if ((rc = product(g, o, st)) != AR_OK) return rc;
+        g.segments = 2, g.steps = (uint32_t)(s.hidden / kStepK);
+        g.a[0] = w + s.grads, g.a[1] = w + s.grads + s.hidden * 2;
+        g.b[0] = pg.p, g.b[1] = pu.p;
+        g.lda = (uint32_t)(s.hidden * 4), g.ldb = pg.ld;
+        g.m = (uint32_t)d.tokens, g.n = pg.cols;
+        const ProductOut o{{(bf16 *)dx, nullptr}, (float *)(w + s.part), {odx.ld, 0}, 0x80000000u, (uint32_t)d.tokens, (uint32_t)d.dim};
+        if ((rc = product<false>(g, o, st)) != AR_OK) return rc;
     }
     if (dwg) {
-        if ((rc = transpose(m.x, w + s.x_t, s.tokens_ld, st)) != AR_OK) return rc;
+        Operand px;
+        if ((rc = pack(m.x, true, x_direct, copies, st, &px)) != AR_OK) return rc;
         GemmArgs g{};
-        g.segments = 1, g.steps = (uint32_t)(s.tokens_ld / kStepK);
-        g.a[0] = w + s.transposed, g.b[0] = w + s.x_t;
-        g.lda = g.ldb = (uint32_t)(s.tokens_ld * 2);
-        g.m = (uint32_t)(2 * d.hidden), g.n = (uint32_t)d.dim;
-        const ProductOut o{(bf16 *)dwg, (bf16 *)dwu, (float *)(w + s.part), og.ld, ou.ld, (uint32_t)d.hidden};
-        if ((rc = product(g, o, st)) != AR_OK) return rc;
+        g.segments = 1, g.steps = (uint32_t)(s.tokens / kStepK);
+        g.a[0] = w + s.grads, g.b[0] = px.p;
+        g.lda = (uint32_t)(s.hidden * 4), g.ldb = px.ld;
+        g.m = (uint32_t)(2 * s.hidden), g.n = px.cols;
+        const ProductOut o{{(bf16 *)dwg, (bf16 *)dwu}, (float *)(w + s.part), {og.ld, ou.ld}, (uint32_t)s.hidden, (uint32_t)d.hidden, (uint32_t)d.dim};
+        if ((rc = product<true>(g, o, st)) != AR_OK) return rc;
     }
     return AR_OK;
 }
@@ -545,7 +494,10 @@ extern "C" int ar_gated_ffn_backward(const ar_ffn_desc *desc, const void *dh, co
 
 extern "C" size_t ar_gated_ffn_backward_workspace(const ar_ffn_desc *desc)
 {
-    return ar::check_ffn(desc) == AR_OK && desc->tokens ? ar::ffn_backward_space(*desc, true, true).bytes : 0;
+    if (ar::check_ffn(desc) != AR_OK || !desc->tokens) return 0;
+    // pointers' alignment is not known before the call, so every copy counts
+    return ar::ffn_backward_space(*desc, true, true).copies + 2 * ar::packed_bytes(desc->hidden, desc->dim, true) +
+           ar::packed_bytes(desc->tokens, desc->dim, true);
 }
 
 extern "C" int ar_gated_ffn(const ar_ffn_desc *desc, const void *x, const void *w_gate, const void *w_up, void *h,

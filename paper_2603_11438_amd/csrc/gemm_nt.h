@@ -1,11 +1,13 @@
-// Matrix products C[m][n] = sum_k A[m][k] B[n][k] on gfx950's matrix units, for
+// Matrix products C[m][n] = sum_k A[m][k] B[k][n] on gfx950's matrix units, for
 // kernels that bring their own epilogue.
 //
-// Both operands are row-major with k contiguous ("NT"), 16-bit, rows 16-byte
-// aligned, k a multiple of 64; callers lay out what is not so.  A product may
-// run over several (A, B) pairs ("segments") of one k length one after another,
-// all into the same sums ([dG dU] times [Wg; Wu]).  Operands in two planes, hi
-// and lo, are multiplied as hi hi + hi lo + lo hi.
+// Operands are 16-bit and row-major, rows 16-byte aligned.  Each lies either by
+// rows, A[m][k] or B[n][k] with k contiguous, or by k, A[k][m] or B[k][n]; then
+// fragments are transposed on their way out of LDS, four k at a time.  k is a
+// multiple of 64; callers lay out what is not so.  A product may run over
+// several (A, B) pairs ("segments") of one k length one after another, all into
+// the same sums ([dG dU] times [Wg; Wu]).  Operands in two planes, hi and lo,
+// are multiplied as hi hi + hi lo + lo hi.
 //
 // A workgroup of four waves, one per SIMD, owns a tile; each wave holds MT x NT
 // accumulators of 32 x 32 in registers.  k advances in stages of BK through
@@ -20,7 +22,8 @@
 // 64 bytes: row >> 2 & 3), by permuting which chunk a lane loads: the sixteen
 // rows' equal chunks that a read touches together then lie in sixteen different
 // groups of four banks (SQ_LDS_BANK_CONFLICT: 0; with row & 7 a read took
-// twice as long).
+// twice as long).  By k, row k's chunks are rotated by 4 (k & 3) (64 columns: by
+// 4 (k >> 1 & 1)): a transposing read takes 64 bytes of each of four rows.
 //
 // Rate, bf16, 8192 x 8192 x 8192: 856 us, 1284 TFLOP/s with the 256 x 256 tile,
 // at 1.75 GHz: the board's power limit has the clock.  With every load an L2 hit
@@ -61,6 +64,52 @@ template <> struct Frag<bf16> {
 constexpr int kMaxSegments = 2;
 constexpr int kStepK = 64;  // k is a multiple of this
 
+// Tiles, by planes: rows and columns, and what they cost.  `busy`: us of a
+// compute unit for k = 64 of a tile while it has several to work on; `alone`:
+// us for the same when one tile has the unit to itself (its loads' way to the
+// L2 and back is then in the open); `fit`: tiles that share a unit; `ends`: us
+// before and after the products.  Measured on products of 1024 x 1024 x 4096
+// (alone) and 8192 x 8192 x 8192 (busy).
+struct TileCost {
+    int side;
+    double busy, alone, ends;
+    int fit;
+};
+constexpr int kTileSizes = 4;
+constexpr TileCost kTiles[2][kTileSizes] = {
+    {{64, 0.19, 0.26, 2.5, 2}, {128, 0.5, 0.68, 4.0, 2}, {192, 1.1, 1.1, 6.0, 1}, {256, 1.67, 1.67, 9.0, 1}},
+    {{64, 0.4, 0.5, 3.0, 1}, {128, 1.2, 1.3, 6.0, 1}, {192, 2.8, 2.8, 9.0, 1}, {256, 4.6, 4.6, 14.0, 1}},
+};
+
+// The tile (an index of kTiles) and the number of runs k is split into that
+// finish a product of k = 64 * steps first.  LOWER: tiles on and below the
+// diagonal alone.  `least` .. `most`: the tiles to choose from.  A split
+// product's runs write their sums, at about 3 TB/s, and a kernel of its own
+// adds them.
+struct Cut {
+    int tile;
+    uint32_t splits;
+};
+inline Cut cut_for(int planes, size_t m, size_t n, size_t steps, size_t batch, bool lower, int least, int most, uint32_t max_splits)
+{
+    Cut best{least, 1};
+    double time = 0;
+    for (int t = least; t <= most; ++t) {
+        const TileCost &c = kTiles[planes - 1][t];
+        const size_t a = (m + c.side - 1) / c.side, b = (n + c.side - 1) / c.side;
+        const size_t tiles = batch * (lower ? a * (a + 1) / 2 : a * b);
+        for (uint32_t s = 1; s <= max_splits && s * 2 <= (steps > 2 ? steps : 2); ++s) {
+            if (s > 1 && tiles * s > 1024) break;
+            const size_t units = (tiles * s + 255) / 256;
+            const double busy = units * c.busy, alone = (double)((units + c.fit - 1) / c.fit) * c.alone;
+            double sum = ((steps + s - 1) / s) * (busy > alone ? busy : alone) + c.ends * units;
+            if (s > 1) sum += 6.0 + 2.0 * s * tiles * c.side * c.side * 4 / 3e6;
+            if ((t == least && s == 1) || sum < time) best = {t, s}, time = sum;
+        }
+    }
+    return best;
+}
+
 // Rows of one tile are reached by 32-bit offsets from the tile's first row.
 inline bool gemm_reaches(uint64_t row_bytes, uint64_t k_bytes) { return row_bytes * 256 + k_bytes < (1ull << 31); }
 
@@ -70,19 +119,19 @@ struct GemmArgs {
     uint64_t a_lo, b_lo;        // two planes: bytes from the hi plane to the lo plane (one segment)
     uint32_t segments, steps;   // steps of 64 per segment
     uint32_t lda, ldb, ldb2;    // bytes
-    uint32_t m, n;              // rows of A and of B (paired: of each)
+    uint32_t m, n;              // of the result (paired: of each; by k: multiples of 8 that can be read)
     uint32_t tiles_m, tiles_n;
     uint64_t batch_a, batch_b;  // bytes between the matrices of a batch
     uint32_t batch;
     uint32_t splits;            // runs of stages that k is split into (grid.y); 1: not split
 };
 
-__device__ __forceinline__ u32x4v tile_resource(const void *p)
+// a: wave-uniform
+__device__ __forceinline__ u32x4v tile_resource(uint64_t a)
 {
-    const uint64_t a = (uint64_t)p;
     u32x4v r;
-    r.x = __builtin_amdgcn_readfirstlane((uint32_t)a);
-    r.y = __builtin_amdgcn_readfirstlane((uint32_t)(a >> 32) & 0xffffu);
+    r.x = (uint32_t)a;
+    r.y = (uint32_t)(a >> 32) & 0xffffu;
     r.z = 0x80000000u;  // offsets stay below 2^31 (gemm_reaches); rows are clamped to the matrix
     r.w = 0x00020000u;
     return r;
@@ -166,82 +215,119 @@ template <int MT_, int NT_, int PLANES_, int BK_, int BUFS_> struct Shape {
     static constexpr int ROW = BK * 2;                        // bytes of a row in a buffer
     static constexpr int PLANE = (BM + BN) * ROW;             // A's rows, then B's
     static constexpr int BUF = PLANES * PLANE, LDS = BUFS * BUF;
-    static constexpr int ROWS_PER_LOAD = 1024 / ROW, LOADS_A = BM / ROWS_PER_LOAD / WAVES, LOADS_B = BN / ROWS_PER_LOAD / WAVES;
-    static constexpr int LOADS_PLANE = LOADS_A + LOADS_B, LOADS = PLANES * LOADS_PLANE;  // of a wave and stage
-    static_assert(BM % (ROWS_PER_LOAD * WAVES) == 0 && BN % (ROWS_PER_LOAD * WAVES) == 0, "whole loads");
+    static_assert(BM * ROW % (1024 * WAVES) == 0 && BN * ROW % (1024 * WAVES) == 0, "whole loads");
 };
+
+// One operand of a tile: which of its bytes each lane loads, and where its
+// fragments lie in LDS.  R: rows (by rows) or columns (by k) of the tile; X:
+// those of a wave, in blocks of 32.
+template <typename S, bool BYK, int R> struct Side {
+    static constexpr int CHUNKS = BYK ? R / 8 : S::ROW / 16;  // of 16 bytes in a row of the buffer
+    static constexpr int LOADS = R * S::ROW / 1024 / S::WAVES;
+    uint32_t off[LOADS];  // a lane's loads: bytes from the tile's first element
+    uint64_t base;        // the tile's first element; by k, of this stage
+
+    static __device__ __forceinline__ uint32_t turn(uint32_t k) { return CHUNKS == 8 ? (k >> 1 & 1u) * 4 : (k & 3u) * 4; }
+    static __device__ __forceinline__ uint32_t swizzle(uint32_t row) { return CHUNKS == 8 ? row >> 1 & 7u : row >> 2 & 3u; }
+
+    // first: the tile's first row or column, of `count`
+    template <typename RowOf> __device__ __forceinline__ void place(uint32_t wave, uint32_t first, uint32_t count, RowOf row_of)
+    {
+        const uint32_t lane = threadIdx.x & 63u;
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i) {
+            const uint32_t q = (i * S::WAVES + wave) * 64 + lane, row = q / CHUNKS, at = q % CHUNKS;
+            if (BYK) {
+                // columns past the end repeat the last eight
+                uint32_t c = (at + CHUNKS - turn(row) % CHUNKS) % CHUNKS;
+                c = first / 8 + c < count / 8 ? c : count / 8 - 1 - first / 8;
+                off[i] = row_of(row, 0u) + c * 16;
+            } else {
+                off[i] = row_of(row, first) + (at ^ swizzle(row)) * 16;
+            }
+        }
+    }
+};
+
+__device__ __forceinline__ uint64_t uniform_address(const void *p)
+{
+    const uint64_t a = (uint64_t)p;
+    // the builtin returns int: without the casts the low half's sign would fill the high half
+    const uint32_t lo = (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)a);
+    const uint32_t hi = (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)(a >> 32));
+    return (uint64_t)hi << 32 | lo;
+}
 
 // The products of one tile.  acc[i][j][r], lane l: row i*32 + l%32 of the wave's
 // rows, column j*32 + 8*(r/4) + 4*(l/32) + r%4 of its columns (B's fragment is
 // the instruction's first operand, so a lane holds four neighbouring columns).
 //
-// PAIRED: of a wave's NT*32 rows of B the first half comes from b, the second
-// half from b2, both at the same rows: the wave then holds both products of the
-// same columns.
+// ABYK, BBYK: the operand lies by k.  PAIRED (B by rows): of a wave's NT*32 rows
+// of B the first half comes from b, the second half from b2, both at the same
+// rows: the wave then holds both products of the same columns.
 //
 // With k split, workgroup blockIdx.y of g.splits adds up its run of the stages
 // (never empty: there are at least as many steps as splits).
-template <typename T, typename S, bool PAIRED>
+template <typename T, typename S, bool PAIRED, bool ABYK = false, bool BBYK = false>
 __device__ __forceinline__ void gemm_tile(const GemmArgs &g, const TileAt at, char *lds, f32x16 (&acc)[S::MT][S::NT])
 {
-    constexpr int MT = S::MT, NT = S::NT, PLANES = S::PLANES, LOADS_A = S::LOADS_A, LOADS_B = S::LOADS_B, LOADS = S::LOADS;
-    constexpr int LOADS_PLANE = S::LOADS_PLANE, RPL = S::ROWS_PER_LOAD;
-    static_assert(PLANES == 1 || !PAIRED, "pairs have one plane");
-    constexpr int CHUNKS = S::ROW / 16, KQ = S::BK / 16, BUFS = S::BUFS;
+    constexpr int MT = S::MT, NT = S::NT, PLANES = S::PLANES, KQ = S::BK / 16, BUFS = S::BUFS;
+    typedef Side<S, ABYK, S::BM> SideA;
+    typedef Side<S, BBYK, S::BN> SideB;
+    constexpr int LOADS_A = SideA::LOADS, LOADS_B = SideB::LOADS, LOADS_PLANE = LOADS_A + LOADS_B, LOADS = PLANES * LOADS_PLANE;
+    static_assert((PLANES == 1 || !PAIRED) && (!PAIRED || !BBYK), "pairs have one plane and lie by rows");
     constexpr uint32_t A_BYTES = S::BM * S::ROW;
     typedef typename Frag<T>::type F;
     const uint32_t lane = threadIdx.x & 63u, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const uint32_t wm = wave / S::WN, wn = wave % S::WN;
     const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)lds;
-    auto swizzle = [](uint32_t row) { return CHUNKS == 8 ? (row >> 1) & 7u : (row >> 2) & 3u; };
-
-    // Loads of this wave: RPL rows each, from row RPL * (WAVES * i + wave) of the tile on.
-    const uint32_t lrow = lane / CHUNKS;
     const uint32_t m0 = at.m * S::BM, n0 = at.n * (PAIRED ? S::BN / 2 : S::BN);
     constexpr int HALF = NT * 16;  // paired: columns of a wave
-    uint32_t off[LOADS_PLANE];
-#pragma unroll
-    for (int i = 0; i < LOADS_A; ++i) {
-        const uint32_t t = (i * S::WAVES + wave) * RPL + lrow, r = m0 + t;
-        off[i] = ((r < g.m ? r : g.m - 1) - m0) * g.lda + ((lane % CHUNKS) ^ swizzle(t)) * 16;
-    }
-#pragma unroll
-    for (int i = 0; i < LOADS_B; ++i) {
-        const uint32_t t = (i * S::WAVES + wave) * RPL + lrow;
-        uint32_t r = t, ld = g.ldb;
+
+    SideA sa;
+    SideB sb;
+    sa.place(wave, m0, g.m, [&](uint32_t row, uint32_t first) {
+        return ABYK ? row * g.lda : ((first + row < g.m ? first + row : g.m - 1) - first) * g.lda;
+    });
+    sb.place(wave, n0, g.n, [&](uint32_t row, uint32_t first) {
+        if (BBYK) return row * g.ldb;
+        uint32_t ld = g.ldb, r = row;
         if (PAIRED) {
-            const uint32_t in = t % (2 * HALF);
+            const uint32_t in = row % (2 * HALF);
             ld = in < HALF ? g.ldb : g.ldb2;
-            r = t / (2 * HALF) * HALF + in % HALF;
+            r = row / (2 * HALF) * HALF + in % HALF;
         }
-        r += n0;
-        off[LOADS_A + i] = ((r < g.n ? r : g.n - 1) - n0) * ld + ((lane % CHUNKS) ^ swizzle(t)) * 16;
-    }
-    const uint32_t per = g.steps * (64 / S::BK), all = g.segments * per;
+        return ((first + r < g.n ? first + r : g.n - 1) - first) * ld;
+    });
+    const uint32_t per = g.steps * (kStepK / S::BK), all = g.segments * per;
     const uint32_t begin = (uint32_t)((uint64_t)all * blockIdx.y / g.splits);
     const uint32_t total = (uint32_t)((uint64_t)all * (blockIdx.y + 1) / g.splits) - begin;
     uint32_t segment = begin / per, step = begin % per, loaded = 0;  // of the next load
-    u32x4v ra, rb, rb2;  // rb2: the second of a pair; ra_lo, rb_lo: the lo planes
+    // by rows a stage is reached by `kbyte` behind the base, by k the base moves on
+    u32x4v ra, rb, rb2, ra_lo, rb_lo;
+    auto point = [&]() {
+        ra = tile_resource(sa.base), rb = tile_resource(sb.base);
+        if (PLANES == 2) ra_lo = tile_resource(sa.base + g.a_lo), rb_lo = tile_resource(sb.base + g.b_lo);
+    };
     auto enter = [&]() {
-        ra = tile_resource((const char *)g.a[segment] + at.batch * g.batch_a + (uint64_t)m0 * g.lda);
-        rb = tile_resource((const char *)g.b[segment] + at.batch * g.batch_b + (uint64_t)n0 * g.ldb);
+        sa.base = uniform_address((const char *)g.a[segment] + at.batch * g.batch_a +
+                                  (ABYK ? (uint64_t)step * S::BK * g.lda + m0 * 2 : (uint64_t)m0 * g.lda));
+        sb.base = uniform_address((const char *)g.b[segment] + at.batch * g.batch_b +
+                                  (BBYK ? (uint64_t)step * S::BK * g.ldb + n0 * 2 : (uint64_t)n0 * g.ldb));
+        point();
     };
     enter();
-    rb2 = PAIRED ? tile_resource((const char *)g.b2 + (uint64_t)n0 * g.ldb2) : rb;
-    u32x4v ra_lo = ra, rb_lo = rb;
-    if (PLANES == 2) {
-        ra_lo = tile_resource((const char *)g.a[0] + g.a_lo + at.batch * g.batch_a + (uint64_t)m0 * g.lda);
-        rb_lo = tile_resource((const char *)g.b[0] + g.b_lo + at.batch * g.batch_b + (uint64_t)n0 * g.ldb);
-    }
+    if (PAIRED) rb2 = tile_resource(uniform_address((const char *)g.b2 + (uint64_t)n0 * g.ldb2));
     uint32_t put = lds0 + wave * 1024, kbyte = step * S::ROW, slot = 0;
     auto load_one = [&](int n) {
         const int i = n % LOADS_PLANE, plane = n / LOADS_PLANE;
         if (i < LOADS_A) {
-            load_to_lds(put + plane * S::PLANE + i * S::WAVES * 1024, off[i], plane ? ra_lo : ra, kbyte);
+            load_to_lds(put + plane * S::PLANE + i * S::WAVES * 1024, sa.off[i], plane ? ra_lo : ra, ABYK ? 0u : kbyte);
         } else {
             const int k = i - LOADS_A;
-            const bool second = PAIRED && (((k * S::WAVES + wave) * RPL) % (2 * HALF)) >= HALF;
-            load_to_lds(put + plane * S::PLANE + A_BYTES + k * S::WAVES * 1024, off[i], plane ? rb_lo : second ? rb2 : rb, kbyte);
+            const bool second = PAIRED && (((k * S::WAVES + wave) * (1024 / S::ROW)) % (2 * HALF)) >= HALF;
+            load_to_lds(put + plane * S::PLANE + A_BYTES + k * S::WAVES * 1024, sb.off[k], plane ? rb_lo : second ? rb2 : rb,
+                        BBYK ? 0u : kbyte);
         }
     };
     auto next_stage = [&]() {
@@ -252,18 +338,48 @@ __device__ __forceinline__ void gemm_tile(const GemmArgs &g, const TileAt at, ch
         if (++step == per) {
             step = 0, kbyte = 0;
             if (++segment < g.segments) enter();
+        } else if (ABYK || BBYK) {
+            if (ABYK) sa.base += (uint64_t)S::BK * g.lda;
+            if (BBYK) sb.base += (uint64_t)S::BK * g.ldb;
+            point();
         }
     };
 
-    const uint32_t fr = lane & 31u, fc = lane >> 5, sw = swizzle(fr);
-    const char *pa = lds + (wm * MT * 32 + fr) * S::ROW, *pb = lds + A_BYTES + (wn * NT * 32 + fr) * S::ROW;
+    // Fragments: lane l holds row (by k: column) l%32 of a block and k = 16 *
+    // quarter + 8 * (l/32) + 0..7.  By k they come as two transposing reads,
+    // each of four k: sixteen lanes address four rows of sixteen columns.
+    const uint32_t fr = lane & 31u, fc = lane >> 5;
+    const uint32_t rows_a = (wm * MT * 32 + fr) * S::ROW, rows_b = A_BYTES + (wn * NT * 32 + fr) * S::ROW;
+    const uint32_t tk = 8 * fc + (lane & 15u) / 4, tc = 2 * (lane >> 4 & 1u) + (lane >> 1 & 1u), te = (lane & 1u) * 8;
+    uint32_t cols_a[MT], cols_b[NT];
+    if (ABYK)
+#pragma unroll
+        for (int i = 0; i < MT; ++i)
+            cols_a[i] = tk * (S::BM * 2) + ((wm * MT + i) * 4 + tc + SideA::turn(tk)) % SideA::CHUNKS * 16 + te;
+    if (BBYK)
+#pragma unroll
+        for (int j = 0; j < NT; ++j)
+            cols_b[j] = A_BYTES + tk * (S::BN * 2) + ((wn * NT + j) * 4 + tc + SideB::turn(tk)) % SideB::CHUNKS * 16 + te;
+    auto transposed = [&](uint32_t at_byte, uint32_t pitch) {
+        typedef short s16x4 __attribute__((ext_vector_type(4)));
+        typedef __attribute__((address_space(3))) s16x4 *P;
+        const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((P)(uintptr_t)(lds0 + at_byte));
+        const s16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((P)(uintptr_t)(lds0 + at_byte + 4 * pitch));
+        return __builtin_bit_cast(F, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
+    };
     constexpr int READS_PLANE = MT + NT, READS = PLANES * READS_PLANE;
     F fa[2][PLANES][MT], fb[2][PLANES][NT];
     auto read_one = [&](uint32_t at_buf, int quarter, int to, int n) {
         const int i = n % READS_PLANE, plane = n / READS_PLANE;
-        const uint32_t o = at_buf + plane * S::PLANE + (((2 * quarter + fc) ^ sw) * 16);
-        if (i < MT) fa[to][plane][i] = *(const F *)(pa + o + i * 32 * S::ROW);
-        else fb[to][plane][i - MT] = *(const F *)(pb + o + (i - MT) * 32 * S::ROW);
+        const uint32_t o = at_buf + plane * S::PLANE;
+        if (i < MT) {
+            if (ABYK) fa[to][plane][i] = transposed(o + quarter * 16 * (S::BM * 2) + cols_a[i], S::BM * 2);
+            else fa[to][plane][i] = *(const F *)(lds + o + rows_a + i * 32 * S::ROW + ((2 * quarter + fc) ^ SideA::swizzle(fr)) * 16);
+        } else {
+            const int j = i - MT;
+            if (BBYK) fb[to][plane][j] = transposed(o + quarter * 16 * (S::BN * 2) + cols_b[j], S::BN * 2);
+            else fb[to][plane][j] = *(const F *)(lds + o + rows_b + j * 32 * S::ROW + ((2 * quarter + fc) ^ SideB::swizzle(fr)) * 16);
+        }
     };
     // product k of a quarter: with two planes three rounds over the accumulators
     auto multiply = [&](int from, int k) {
@@ -344,18 +460,18 @@ template <int NT> __device__ __forceinline__ void take(const f32x16 (&acc)[NT], 
         for (int r = 0; r < 16; ++r) asm volatile("v_accvgpr_read_b32 %0, %1" : "=v"(v[j][r]) : "a"(acc[j][r]));
 }
 
-// Writes 32 rows of a wave's results through its own part of LDS, so that a
-// row's bytes leave together.  value(j, r): the lane's value at column
-// j*32 + 8*(r/4) + 4*(l/32) + r%4 of COLS, row l%32.  row(r): where row r goes
-// (its first column), or null for none; `cols` columns are written.
-template <typename O, int COLS, typename V, typename R>
-__device__ __forceinline__ void store_32_rows(char *lds, uint32_t cols, V value, R row)
+// 32 rows of a wave's results in its own part of LDS, so that a row's bytes can
+// leave together.  value(j, r): the lane's value at column j*32 + 8*(r/4) +
+// 4*(l/32) + r%4 of COLS, row l%32.
+template <typename O, int COLS> constexpr int kStagePitch = COLS * (int)sizeof(O) + 16;
+template <typename O, int COLS> constexpr int kStageBytes = 32 * kStagePitch<O, COLS>;
+template <typename O, int COLS, typename V> __device__ __forceinline__ void stage_rows(char *lds, V value)
 {
-    constexpr int E = sizeof(O), PITCH = COLS * E + 16, PER = 16 / E;  // elements a lane stores at once
-    constexpr int LANES = COLS / PER;  // of a row
-    static_assert(COLS % PER == 0 && 32 * LANES % 64 == 0, "whole rows and waves");
+    constexpr int E = sizeof(O), PITCH = kStagePitch<O, COLS>;
     const uint32_t lane = threadIdx.x & 63u;
     typedef O O4 __attribute__((ext_vector_type(4)));
+    char *at = lds + (lane & 31u) * PITCH + (lane >> 5) * 4 * E;
+    asm volatile("" ::: "memory");
 #pragma unroll
     for (int j = 0; j < COLS / 32; ++j)
 #pragma unroll
@@ -363,27 +479,60 @@ __device__ __forceinline__ void store_32_rows(char *lds, uint32_t cols, V value,
             O4 v;
 #pragma unroll
             for (int k = 0; k < 4; ++k) v[k] = (O)value(j, q * 4 + k);
-            *(O4 *)(lds + (lane & 31u) * PITCH + (j * 32 + q * 8 + (lane >> 5) * 4) * E) = v;
+            *(O4 *)(at + (j * 32 + q * 8) * E) = v;
         }
     asm volatile("" ::: "memory");
+}
+
+// Writes staged rows to `out` and the rows behind it: of the 32 rows those in
+// [from, until), of the columns the first `cols`.
+template <typename O, int COLS>
+__device__ __forceinline__ void write_rows(const char *lds, O *out, uint64_t ld, uint32_t from, uint32_t until, uint32_t cols)
+{
+    constexpr int E = sizeof(O), PITCH = kStagePitch<O, COLS>, PER = 16 / E, LANES = COLS / PER;  // of a row
+    static_assert(COLS % PER == 0 && 32 * LANES % 64 == 0, "whole rows and waves");
+    typedef O OV __attribute__((ext_vector_type(PER)));
+    typedef O OU __attribute__((ext_vector_type(PER), aligned(E)));
+    const uint32_t lane = threadIdx.x & 63u;
+    const bool whole = from == 0 && until >= 32 && cols >= COLS;
 #pragma unroll
     for (int k0 = 0; k0 < 32 * LANES; k0 += 64) {
         const uint32_t r = (k0 + lane) / LANES, c = (k0 + lane) % LANES * PER;
-        O *to = row(r);
-        const O *from = (const O *)(lds + r * PITCH) + c;
-        if (to) {
-            if (c + PER <= cols) {
-                typedef O OV __attribute__((ext_vector_type(PER)));
-                typedef O OU __attribute__((ext_vector_type(PER), aligned(E)));
-                *(OU *)(to + c) = *(const OV *)from;
-            } else {
-                for (uint32_t k = c; k < cols; ++k) to[k] = from[k - c];
-            }
+        O *to = out + r * ld + c;
+        const char *at = lds + r * PITCH + c * E;
+        if (whole) {
+            *(OU *)to = *(const OV *)at;
+        } else if (r >= from && r < until) {
+            if (c + PER <= cols) *(OU *)to = *(const OV *)at;
+            else
+                for (uint32_t k = c; k < cols; ++k) to[k - c] = ((const O *)at)[k - c];
         }
     }
-    asm volatile("" ::: "memory");
 }
-template <typename O, int COLS> constexpr int kStageBytes = 32 * (COLS * (int)sizeof(O) + 16);
+
+// Writes staged rows of a 16-bit type transposed: column c to row c of `out`, for
+// the first `cols` columns, `rows` of the 32 elements (a multiple of 8, or all).
+template <typename O, int COLS>
+__device__ __forceinline__ void write_columns(const char *lds, O *out, uint64_t ld, uint32_t rows, uint32_t cols)
+{
+    static_assert(sizeof(O) == 2, "a 16-bit type");
+    constexpr int PITCH = kStagePitch<O, COLS>;
+    typedef short s16x4 __attribute__((ext_vector_type(4)));
+    typedef short s16x8 __attribute__((ext_vector_type(8)));
+    typedef s16x8 Out __attribute__((aligned(2)));
+    typedef __attribute__((address_space(3))) s16x4 *P;
+    const uint32_t lane = threadIdx.x & 63u, r8 = (lane >> 4) * 8;
+    // sixteen lanes: rows r8..r8+3 of sixteen columns, then the next four rows
+    const uint32_t from = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const char *)lds +
+                          (r8 + (lane & 15u) / 4) * PITCH + (lane & 3u) * 8;
+#pragma unroll
+    for (int c0 = 0; c0 < COLS; c0 += 16) {
+        const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((P)(uintptr_t)(from + c0 * 2));
+        const s16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((P)(uintptr_t)(from + c0 * 2 + 4 * PITCH));
+        const uint32_t c = c0 + (lane & 15u);
+        if (c < cols && r8 < rows) *(Out *)(out + c * ld + r8) = __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
+    }
+}
 
 }  // namespace dev
 }  // namespace ar

@@ -19,8 +19,7 @@
 //   two planes in bf16 too.
 //
 // A and B are symmetric: only tiles on and below the diagonal are computed and
-// written to both places.  X is also kept transposed, as the second operand of
-// B X; tall matrices are transposed on the way in and out.
+// written to both places.  Tall matrices are transposed on the way in and out.
 #include <type_traits>
 
 #include "gemm_nt.h"
@@ -40,7 +39,7 @@ struct Scales {
 
 // One matrix' part of the workspace, in bytes.
 struct OrthoSpace {
-    size_t xh, xl, xf, xt[2], xt_lo, a, a_lo, b, b_lo, diag_a, diag_b, scales, norms, bytes;
+    size_t x[2], x_lo, xf, a, a_lo, b, b_lo, diag_a, diag_b, scales, norms, bytes;
 };
 
 struct OrthoArgs {
@@ -97,9 +96,9 @@ __device__ __forceinline__ float scale_for(float bound)
     return ldexpf(1.0f, 14 - e);
 }
 
-// X's planes, both ways round, from the input: X = M / 2^e with the norm of M
-// between 2^(e-1) and 2^e, which is exact; the rest of the normalisation is the
-// first step's tau.  Tiles of 64 x 64.
+// X's planes from the input: X = M / 2^e with the norm of M between 2^(e-1) and
+// 2^e, which is exact; the rest of the normalisation is the first step's tau.
+// Tiles of 64 x 64.
 template <typename T, int PLANES> __global__ __launch_bounds__(256) void ortho_enter_kernel(const OrthoArgs o)
 {
     __shared__ float tile[64][65];
@@ -148,27 +147,22 @@ template <typename T, int PLANES> __global__ __launch_bounds__(256) void ortho_e
     __syncthreads();
     for (uint32_t k = threadIdx.x; k < 512; k += 256) {
         const uint32_t r = k / 8, c = k % 8 * 8;
-        f16x8 h, l, th, tl;
+        f16x8 h, l;
 #pragma unroll
         for (int q = 0; q < 8; ++q) {
-            const float x = tile[r][c + q], t = tile[c + q][r];
+            const float x = tile[r][c + q];
             h[q] = (f16)x, l[q] = (f16)(x - (float)h[q]);
-            th[q] = (f16)t, tl[q] = (f16)(t - (float)th[q]);
         }
-        const size_t x_at = ((size_t)(i0 + r) * o.np + j0 + c) * 2, t_at = ((size_t)(j0 + r) * o.mp + i0 + c) * 2;
-        *(f16x8 *)(ws + o.at.xh + x_at) = h;
-        *(f16x8 *)(ws + o.at.xl + x_at) = l;
-        *(f16x8 *)(ws + o.at.xt[0] + t_at) = th;
-        if (PLANES == 2) {
-            *(f16x8 *)(ws + o.at.xt[0] + o.at.xt_lo + t_at) = tl;
-            store_vec<float, 8>((float *)(ws + o.at.xf + x_at * 2), &tile[r][c]);
-        }
+        const size_t x_at = ((size_t)(i0 + r) * o.np + j0 + c) * 2;
+        *(f16x8 *)(ws + o.at.x[0] + x_at) = h;
+        *(f16x8 *)(ws + o.at.x[0] + o.at.x_lo + x_at) = l;
+        if (PLANES == 2) store_vec<float, 8>((float *)(ws + o.at.xf + x_at * 2), &tile[r][c]);
     }
 }
 
 // ---- the products -----------------------------------------------------------
 
-// Writes a wave's 32 x COLS block transposed: value(j, r) as in store_32_rows,
+// Writes a wave's 32 x COLS block transposed: value(j, r) as in stage_rows,
 // row(c): where column c goes (its element of the block's first row) or null;
 // `rows` of the 32 are written.
 template <typename O, int COLS, typename V, typename R>
@@ -216,34 +210,21 @@ template <typename S> struct WaveAt {
     __device__ __forceinline__ uint32_t j(int bj, int r) const { return col0 + bj * 32 + r / 4 * 8 + half + r % 4; }
 };
 
-// The planes of a scaled matrix from 32 rows of a wave's block, rows and
-// columns up to the padded sizes: as they are, or transposed.
-template <int NT> __device__ __forceinline__ float plane_of(const float (&v)[NT][16], int plane, int j, int r)
-{
-    const float x = v[j][r];
-    return plane == 0 ? x : x - (float)(f16)x;
-}
-template <typename S, int PLANES>
+// The planes of a scaled matrix from 32 rows of a wave's block, for rows and
+// columns up to the padded sizes; MIRROR: also transposed, for a symmetric one.
+template <typename S, int PLANES, bool MIRROR>
 __device__ __forceinline__ void store_planes(char *stage, const float (&v)[S::NT][16], uint32_t first, uint32_t col0, char *hi,
-                                             size_t lo, uint32_t rows, uint32_t cols, uint32_t ld)
+                                             size_t lo, uint32_t rows, uint32_t cols)
 {
-    if (col0 >= cols) return;
+    constexpr int COLS = S::NT * 32;
+    if (first >= rows || col0 >= cols) return;
 #pragma unroll
-    for (int plane = 0; plane < PLANES; ++plane)
-        store_32_rows<f16, S::NT * 32>(stage, cols - col0, [&](int j, int r) { return plane_of(v, plane, j, r); }, [&](uint32_t r) {
-            return first + r < rows ? (f16 *)(hi + plane * lo) + (uint64_t)(first + r) * ld + col0 : nullptr;
-        });
-}
-template <typename S, int PLANES>
-__device__ __forceinline__ void store_planes_transposed(char *stage, const float (&v)[S::NT][16], uint32_t first, uint32_t col0,
-                                                        char *hi, size_t lo, uint32_t rows, uint32_t cols, uint32_t ld)
-{
-    if (first >= cols) return;
-#pragma unroll
-    for (int plane = 0; plane < PLANES; ++plane)
-        store_32_cols<f16, S::NT * 32>(stage, cols - first, [&](int j, int r) { return plane_of(v, plane, j, r); }, [&](uint32_t c) {
-            return col0 + c < rows ? (f16 *)(hi + plane * lo) + (uint64_t)(col0 + c) * ld + first : nullptr;
-        });
+    for (int plane = 0; plane < PLANES; ++plane) {
+        f16 *to = (f16 *)(hi + plane * lo);
+        stage_rows<f16, COLS>(stage, [&](int j, int r) { return plane == 0 ? v[j][r] : v[j][r] - (float)(f16)v[j][r]; });
+        write_rows<f16, COLS>(stage, to + (uint64_t)first * cols + col0, cols, 0, rows - first, cols - col0);
+        if (MIRROR) write_columns<f16, COLS>(stage, to + (uint64_t)col0 * cols + first, cols, rows - first, cols - col0);
+    }
 }
 
 template <typename S> constexpr int kOrthoStage = kStageColBytes<float, S::NT * 32> > kStageBytes<float, S::NT * 32>
@@ -265,7 +246,7 @@ __global__ __launch_bounds__(S::THREADS) void ortho_square_kernel(const GemmArgs
     char *ws = o.ws + at.batch * o.at.bytes;
     const Scales s = ((const Scales *)(ws + o.at.scales))[o.step];
     float *diag_a = (float *)(ws + o.at.diag_a), *diag_b = (float *)(ws + o.at.diag_b);
-    const float sx = s.tau / s.x, ia = 1.0f / s.a;
+    const float sx = s.tau / s.x, ia = 1.0f / s.a, to = SECOND ? s.b : s.a;  // powers of two but for tau
     char *stage = lds + (threadIdx.x >> 6) * kOrthoStage<S>;
     char *hi = ws + (SECOND ? o.at.b : o.at.a);
     const size_t lo = SECOND ? o.at.b_lo : o.at.a_lo;
@@ -300,20 +281,27 @@ __global__ __launch_bounds__(S::THREADS) void ortho_square_kernel(const GemmArgs
                     float x = v[bj][q * 4 + k];
                     if (!SECOND) {
                         x = x * sx * sx;
-                        if (i == j && i < o.m) diag_a[i] = x;
-                        x *= s.a;
                     } else {
-                        x = x * ia * ia;
-                        if (i == j && i < o.m) diag_b[i] = o.b * di + o.c * (x + di * di);
                         const float t = off[k] * ia;
-                        x = (o.b * t + o.c * (x + (di + dj[k]) * t)) * s.b;
+                        x = o.b * t + o.c * (x * ia * ia + (di + dj[k]) * t);
                     }
-                    v[bj][q * 4 + k] = i < o.m && j < o.m && i != j ? x : 0.0f;
+                    v[bj][q * 4 + k] = i < o.m && j < o.m ? x * to : 0.0f;
                 }
             }
+        if (at.m == at.n) {
+            // the diagonal goes to its vector (off and dj are zero there)
+#pragma unroll
+            for (int bj = 0; bj < NT; ++bj)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                    if (w.j(bj, r) != i) continue;
+                    if (i < o.m) (SECOND ? diag_b : diag_a)[i] = SECOND ? o.b * di + v[bj][r] / to + o.c * di * di : v[bj][r] / to;
+                    v[bj][r] = 0.0f;
+                }
+        }
         const uint32_t first = w.row0 + bi * 32;
-        store_planes<S, PLANES>(stage, v, first, w.col0, hi, lo, o.m, o.mp, o.mp);
-        if (at.m != at.n) store_planes_transposed<S, PLANES>(stage, v, first, w.col0, hi, lo, o.m, o.mp, o.mp);
+        if (at.m != at.n) store_planes<S, PLANES, true>(stage, v, first, w.col0, hi, lo, o.mp, o.mp);
+        else store_planes<S, PLANES, false>(stage, v, first, w.col0, hi, lo, o.mp, o.mp);
     });
 }
 
@@ -325,15 +313,17 @@ __global__ __launch_bounds__(S::THREADS) void ortho_update_kernel(const GemmArgs
     extern __shared__ __attribute__((aligned(16))) char lds[];
     const TileAt at = tile_at(g.tiles_m, g.tiles_n, g.batch);
     f32x16 acc[S::MT][NT];
-    gemm_tile<f16, S, false>(g, at, lds, acc);
+    gemm_tile<f16, S, false, false, true>(g, at, lds, acc);
     const WaveAt<S> w(at);
     char *ws = o.ws + at.batch * o.at.bytes;
     const Scales s = ((const Scales *)(ws + o.at.scales))[o.step], next = ((const Scales *)(ws + o.at.scales))[o.step + 1];
     const float *diag_b = (const float *)(ws + o.at.diag_b);
     const bool last = o.step + 1 == o.steps;
     const float to = last ? o.scale : next.x, ib = 1.0f / s.b, ix = s.tau / s.x;
-    // X's own planes are read by no other tile; the transposed ones are, so they alternate.
-    char *stage = lds + (threadIdx.x >> 6) * kOrthoStage<S>, *xt = ws + o.at.xt[(o.step + 1) & 1u];
+    // X's planes are read by other tiles too, so they alternate; its fp32 values are not.
+    char *stage = lds + (threadIdx.x >> 6) * kOrthoStage<S>;
+    const char *x_now = ws + o.at.x[o.step & 1u];
+    char *x_next = ws + o.at.x[(o.step + 1) & 1u];
     O *out = (O *)o.out + at.batch * o.stride_out;
     static_for<S::MT>([&](auto block) {
         constexpr int bi = block.value;
@@ -353,7 +343,7 @@ __global__ __launch_bounds__(S::THREADS) void ortho_update_kernel(const GemmArgs
                         load_vec<float, 4>((const float *)(ws + o.at.xf + x_at * 2), x);
                     } else {
                         typedef f16 f16x4 __attribute__((ext_vector_type(4)));
-                        const f16x4 h = *(const f16x4 *)(ws + o.at.xh + x_at), l = *(const f16x4 *)(ws + o.at.xl + x_at);
+                        const f16x4 h = *(const f16x4 *)(x_now + x_at), l = *(const f16x4 *)(x_now + o.at.x_lo + x_at);
 #pragma unroll
                         for (int k = 0; k < 4; ++k) x[k] = (float)h[k] + (float)l[k];
                     }
@@ -367,21 +357,19 @@ __global__ __launch_bounds__(S::THREADS) void ortho_update_kernel(const GemmArgs
         const uint32_t first = w.row0 + bi * 32;
         auto value = [&](int j, int r) { return v[j][r]; };
         if (!last) {
-            store_planes<S, 2>(stage, v, first, w.col0, ws + o.at.xh, o.at.xl - o.at.xh, o.m, o.np, o.np);
-            if (PLANES == 2 && w.col0 < o.np)
-                store_32_rows<float, NT * 32>(stage, o.np - w.col0, value, [&](uint32_t r) {
-                    return first + r < o.m ? (float *)(ws + o.at.xf) + (uint64_t)(first + r) * o.np + w.col0 : nullptr;
-                });
-            store_planes_transposed<S, PLANES>(stage, v, first, w.col0, xt, o.at.xt_lo, o.n, o.mp, o.mp);
+            store_planes<S, 2, false>(stage, v, first, w.col0, x_next, o.at.x_lo, o.mp, o.np);
+            if (PLANES == 2 && first < o.m && w.col0 < o.np) {
+                stage_rows<float, NT * 32>(stage, value);
+                write_rows<float, NT * 32>(stage, (float *)(ws + o.at.xf) + (uint64_t)first * o.np + w.col0, o.np, 0, o.m - first, o.np - w.col0);
+            }
         } else if (first < o.m && w.col0 < o.n) {
             if (o.tall) {
                 store_32_cols<O, NT * 32>(stage, o.m - first, value, [&](uint32_t c) {
                     return w.col0 + c < o.n ? out + (uint64_t)(w.col0 + c) * o.ld_out + first : nullptr;
                 });
             } else {
-                store_32_rows<O, NT * 32>(stage, o.n - w.col0, value, [&](uint32_t r) {
-                    return first + r < o.m ? out + (uint64_t)(first + r) * o.ld_out + w.col0 : nullptr;
-                });
+                stage_rows<O, NT * 32>(stage, value);
+                write_rows<O, NT * 32>(stage, out + (uint64_t)first * o.ld_out + w.col0, o.ld_out, 0, o.m - first, o.n - w.col0);
             }
         }
     });
@@ -463,48 +451,14 @@ OrthoSpace ortho_space(const ar_ortho_desc &d, uint32_t mp, uint32_t np)
         return here;
     };
     const size_t x = (size_t)mp * np * 2, sq = (size_t)mp * mp * 2;
-    s.xh = take(x), s.xl = take(x), s.xf = take(two ? 2 * x : 0);
-    s.xt_lo = s.a_lo = s.b_lo = 0;
-    s.xt[0] = take(two ? 2 * x : x), s.xt[1] = take(two ? 2 * x : x);
+    s.x[0] = take(2 * x), s.x[1] = take(2 * x), s.xf = take(two ? 2 * x : 0);
     s.a = take(two ? 2 * sq : sq), s.b = take(two ? 2 * sq : sq);
-    if (two) s.xt_lo = x, s.a_lo = s.b_lo = sq;
+    s.x_lo = x, s.a_lo = s.b_lo = sq;
     s.diag_a = take(mp * 4), s.diag_b = take(mp * 4);
     s.scales = take(sizeof(Scales) * (AR_ORTHO_MAX_STEPS + 1));
     s.norms = take(sizeof(double) * kNormParts);
     s.bytes = at;
     return s;
-}
-
-// Tiles, by planes: rows and columns, and what they cost.  `busy`: us of a
-// compute unit for k = 64 of a tile while it has several to work on; `alone`:
-// us for the same when one tile has the unit to itself (its loads' way to the
-// L2 and back is then in the open); `fit`: tiles that share a unit; `ends`: us
-// before and after the products.  Measured on products of 1024 x 1024 x 4096
-// (alone) and 8192 x 8192 x 8192 (busy).
-struct TileCost {
-    int side;
-    double busy, alone, ends;
-    int fit;
-};
-constexpr TileCost kTiles[2][4] = {
-    {{64, 0.19, 0.26, 2.5, 2}, {128, 0.5, 0.68, 4.0, 2}, {192, 1.1, 1.1, 6.0, 1}, {256, 1.67, 1.67, 9.0, 1}},
-    {{64, 0.4, 0.5, 3.0, 1}, {128, 1.2, 1.3, 6.0, 1}, {192, 2.8, 2.8, 9.0, 1}, {256, 4.6, 4.6, 14.0, 1}},
-};
-
-// The tile that finishes a product of k = 64 * steps first.
-int tile_for(int planes, size_t m, size_t n, size_t steps, size_t batch, bool lower)
-{
-    int best = 0;
-    double least = 0;
-    for (int t = 0; t < 4; ++t) {
-        const TileCost &c = kTiles[planes - 1][t];
-        const size_t a = (m + c.side - 1) / c.side, b = (n + c.side - 1) / c.side;
-        const size_t tiles = batch * (lower ? a * (a + 1) / 2 : a * b), per_unit = (tiles + 255) / 256;
-        const double busy = per_unit * c.busy, alone = (double)((per_unit + c.fit - 1) / c.fit) * c.alone;
-        const double time = steps * (busy > alone ? busy : alone) + c.ends * per_unit;
-        if (t == 0 || time < least) best = t, least = time;
-    }
-    return best;
 }
 
 // The shapes of kTiles' tiles.
@@ -530,7 +484,7 @@ template <typename S, bool SECOND> int launch_square(GemmArgs &g, const OrthoArg
 }
 template <int PLANES, bool SECOND> int square(GemmArgs &g, const OrthoArgs &o, hipStream_t st)
 {
-    switch (tile_for(PLANES, o.m, o.m, g.steps, o.batch, true)) {
+    switch (cut_for(PLANES, o.m, o.m, g.steps, o.batch, true, 0, 3, 1).tile) {
     case 0: return launch_square<typename ShapeOf<PLANES, 0>::type, SECOND>(g, o, st);
     case 1: return launch_square<typename ShapeOf<PLANES, 1>::type, SECOND>(g, o, st);
     case 2: return launch_square<typename ShapeOf<PLANES, 2>::type, SECOND>(g, o, st);
@@ -549,7 +503,7 @@ template <typename S, typename O> int launch_update(GemmArgs &g, const OrthoArgs
 }
 template <int PLANES, typename O> int update(GemmArgs &g, const OrthoArgs &o, hipStream_t st)
 {
-    switch (tile_for(PLANES, o.m, o.n, g.steps, o.batch, false)) {
+    switch (cut_for(PLANES, o.m, o.n, g.steps, o.batch, false, 0, 3, 1).tile) {
     case 0: return launch_update<typename ShapeOf<PLANES, 0>::type, O>(g, o, st);
     case 1: return launch_update<typename ShapeOf<PLANES, 1>::type, O>(g, o, st);
     case 2: return launch_update<typename ShapeOf<PLANES, 2>::type, O>(g, o, st);
@@ -557,13 +511,14 @@ template <int PLANES, typename O> int update(GemmArgs &g, const OrthoArgs &o, hi
     }
 }
 
-// A product of a's rows and b's rows in the workspace.
-void operands(GemmArgs *g, const OrthoArgs &o, size_t a, size_t a_lo, size_t b, size_t b_lo, uint32_t k, uint32_t m, uint32_t n)
+// A product in the workspace; the second planes lie a_lo and b_lo behind the first.
+void operands(GemmArgs *g, const OrthoArgs &o, size_t a, size_t a_lo, uint32_t lda, size_t b, size_t b_lo, uint32_t ldb, uint32_t k,
+              uint32_t m, uint32_t n)
 {
     *g = GemmArgs{};
     g->segments = 1, g->steps = k / kStepK;
     g->a[0] = o.ws + a, g->b[0] = o.ws + b, g->a_lo = a_lo, g->b_lo = b_lo;
-    g->lda = g->ldb = k * 2;
+    g->lda = lda * 2, g->ldb = ldb * 2;
     g->m = m, g->n = n, g->batch_a = g->batch_b = o.at.bytes, g->batch = o.batch, g->splits = 1;
 }
 
@@ -577,11 +532,12 @@ template <typename O, int PLANES> int run_ortho(OrthoArgs &o, const float *coefs
     for (o.step = 0; o.step < o.steps; ++o.step) {
         o.a = coefs[3 * o.step], o.b = coefs[3 * o.step + 1], o.c = coefs[3 * o.step + 2];
         GemmArgs g;
-        operands(&g, o, o.at.xh, o.at.xl - o.at.xh, o.at.xh, o.at.xl - o.at.xh, o.np, o.m, o.m);
+        const size_t x = o.at.x[o.step & 1u];
+        operands(&g, o, x, o.at.x_lo, o.np, x, o.at.x_lo, o.np, o.np, o.m, o.m);
         if ((rc = square<PLANES, false>(g, o, st)) != AR_OK) return rc;
-        operands(&g, o, o.at.a, o.at.a_lo, o.at.a, o.at.a_lo, o.mp, o.m, o.m);
+        operands(&g, o, o.at.a, o.at.a_lo, o.mp, o.at.a, o.at.a_lo, o.mp, o.mp, o.m, o.m);
         if ((rc = square<PLANES, true>(g, o, st)) != AR_OK) return rc;
-        operands(&g, o, o.at.b, o.at.b_lo, o.at.xt[o.step & 1u], o.at.xt_lo, o.mp, o.m, o.n);
+        operands(&g, o, o.at.b, o.at.b_lo, o.mp, x, o.at.x_lo, o.np, o.mp, o.m, o.np);
         if ((rc = update<PLANES, O>(g, o, st)) != AR_OK) return rc;
     }
     return AR_OK;

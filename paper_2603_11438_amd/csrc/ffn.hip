@@ -69,46 +69,45 @@ template <typename S, int ACT> __global__ __launch_bounds__(S::THREADS) void ffn
     });
 }
 
-// Copies a matrix into `to_rows` rows of `to_ld` elements, zeros behind its
-// rows and columns.
+// Copies a matrix into rows of `to_ld` elements, zeros behind its columns.
 struct PackArgs {
     const bf16 *from;
     bf16 *to;
-    uint64_t rows, ld, to_rows, to_ld;
+    uint64_t rows, ld, to_ld;
     uint32_t cols;
 };
 __global__ __launch_bounds__(256) void pack_kernel(const PackArgs p)
 {
-    const uint64_t per = p.to_ld / 8, n = p.to_rows * per;
+    const uint64_t per = p.to_ld / 8, n = p.rows * per;
     for (uint64_t i = (uint64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (uint64_t)gridDim.x * 256) {
         const uint64_t row = i / per;
         const uint32_t c = (uint32_t)(i % per) * 8;
         const bf16 *from = p.from + row * p.ld + c;
         float v[8];
-        if (row < p.rows && c + 8 <= p.cols) load_vec<bf16, 8>(from, v);
-        else load_part<bf16, 8>(from, row < p.rows && c < p.cols ? (int)(p.cols - c) : 0, v);
+        if (c + 8 <= p.cols) load_vec<bf16, 8>(from, v);
+        else load_part<bf16, 8>(from, (int)(p.cols - c), v);
         store_vec<bf16, 8>(p.to + row * p.to_ld + c, v);
     }
 }
 
 // dG = dh * U * act'(G) and dU = dh * act(G) from the saved projections, rounded
 // to bf16 as operands of the backward products: rows of dG, then dU, with zeros
-// behind the columns of each and behind the rows.
+// behind the columns of each.
 struct GradArgs {
     const float *saved;
     const bf16 *dh;
     bf16 *to;
-    uint64_t ld_dh, tokens, to_tokens;
+    uint64_t ld_dh, tokens;
     uint32_t hidden, to_hidden;
 };
 template <int ACT> __global__ __launch_bounds__(256) void ffn_grad_kernel(const GradArgs a)
 {
-    const uint64_t per = a.to_hidden / 8, n = a.to_tokens * per, half = a.tokens * a.hidden;
+    const uint64_t per = a.to_hidden / 8, n = a.tokens * per, half = a.tokens * a.hidden;
     for (uint64_t i = (uint64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (uint64_t)gridDim.x * 256) {
         const uint64_t t = i / per;
         const uint32_t f = (uint32_t)(i % per) * 8;
         float g[8], u[8], d[8];
-        const int have = t < a.tokens && f < a.hidden ? (int)(a.hidden - f) : 0;
+        const int have = f < a.hidden ? (int)(a.hidden - f) : 0;
         const float *from = a.saved + t * a.hidden + f;
         const bf16 *dh = a.dh + t * a.ld_dh + f;
         if (have >= 8) {
@@ -224,16 +223,12 @@ int check_ffn(const ar_ffn_desc *d)
     return AR_OK;
 }
 
-// Whether the product kernel can read a matrix where it lies, by rows or by k.
-bool direct(const Mat &m, bool by_k)
+// Whether the product kernel can read a matrix where it lies.
+bool direct(const Mat &m)
 {
-    if ((uintptr_t)m.p % 16 != 0 || m.ld % 8 != 0 || !gemm_reaches(m.ld * 2, m.cols * 2)) return false;
-    return by_k ? m.rows % kStepK == 0 && m.cols % 8 == 0 : m.cols % kStepK == 0;
+    return (uintptr_t)m.p % 16 == 0 && m.ld % 8 == 0 && m.cols % 8 == 0 && gemm_reaches(m.ld * 2, m.cols * 2);
 }
-size_t packed_bytes(size_t rows, size_t cols, bool by_k)
-{
-    return round_up((by_k ? round_up(rows, kStepK) : rows) * round_up(cols, kStepK) * 2, 256);
-}
+size_t packed_bytes(size_t rows, size_t cols) { return round_up(rows * round_up(cols, 8) * 2, 256); }
 
 // A matrix as the product kernel takes it: itself, or a copy in the workspace.
 struct Operand {
@@ -242,18 +237,18 @@ struct Operand {
     uint32_t cols;  // that can be read
 };
 
-int pack(const Mat &m, bool by_k, bool as_is, char *&ws, hipStream_t st, Operand *out)
+int pack(const Mat &m, bool as_is, char *&ws, hipStream_t st, Operand *out)
 {
     if (as_is) {
         *out = {m.p, (uint32_t)(m.ld * 2), (uint32_t)m.cols};
         return AR_OK;
     }
-    const size_t to_ld = round_up(m.cols, kStepK), to_rows = by_k ? round_up(m.rows, kStepK) : m.rows;
-    PackArgs p{(const bf16 *)m.p, (bf16 *)ws, m.rows, m.ld, to_rows, to_ld, (uint32_t)m.cols};
-    const uint64_t groups = (to_rows * (to_ld / 8) + 255) / 256;
+    const size_t to_ld = round_up(m.cols, 8);
+    PackArgs p{(const bf16 *)m.p, (bf16 *)ws, m.rows, m.ld, to_ld, (uint32_t)m.cols};
+    const uint64_t groups = (m.rows * (to_ld / 8) + 255) / 256;
     hipLaunchKernelGGL(pack_kernel, dim3((uint32_t)(groups < 8192 ? groups : 8192)), dim3(256), 0, st, p);
     *out = {ws, (uint32_t)(to_ld * 2), (uint32_t)to_ld};
-    ws += packed_bytes(m.rows, m.cols, by_k);
+    ws += packed_bytes(m.rows, m.cols);
     return launch_status();
 }
 
@@ -295,7 +290,7 @@ FfnMats ffn_mats(const ar_ffn_desc &d, const void *x, const void *wg, const void
 // before the call, so every operand counts.
 size_t ffn_workspace(const ar_ffn_desc &d)
 {
-    return packed_bytes(d.tokens, d.dim, false) + 2 * packed_bytes(d.hidden, d.dim, false);
+    return packed_bytes(d.tokens, d.dim) + 2 * packed_bytes(d.hidden, d.dim);
 }
 
 int ffn(const ar_ffn_desc *desc, const void *x, const void *wg, const void *wu, void *h, float *saved, void *ws,
@@ -313,7 +308,7 @@ int ffn(const ar_ffn_desc *desc, const void *x, const void *wg, const void *wu, 
     if (meet(m.h, sv)) return AR_ERR_ARG;
     size_t need = 0;
     for (const Mat &in : {m.x, m.wg, m.wu})
-        if (!direct(in, false)) need += packed_bytes(in.rows, in.cols, false);
+        if (!direct(in)) need += packed_bytes(in.rows, in.cols);
     if (need) {
         if (!ws || ws_bytes < need) return AR_ERR_SCRATCH;
         if ((uintptr_t)ws % 256 != 0) return AR_ERR_ARG;
@@ -324,13 +319,14 @@ int ffn(const ar_ffn_desc *desc, const void *x, const void *wg, const void *wu, 
     hipStream_t st = (hipStream_t)stream;
     char *at = (char *)ws;
     Operand px, pg, pu;
-    if ((rc = pack(m.x, false, direct(m.x, false), at, st, &px)) != AR_OK) return rc;
-    if ((rc = pack(m.wg, false, direct(m.wg, false), at, st, &pg)) != AR_OK) return rc;
-    if ((rc = pack(m.wu, false, direct(m.wu, false), at, st, &pu)) != AR_OK) return rc;
+    if ((rc = pack(m.x, direct(m.x), at, st, &px)) != AR_OK) return rc;
+    if ((rc = pack(m.wg, direct(m.wg), at, st, &pg)) != AR_OK) return rc;
+    if ((rc = pack(m.wu, direct(m.wu), at, st, &pu)) != AR_OK) return rc;
     GemmArgs g{};
     g.a[0] = px.p, g.b[0] = pg.p, g.b2 = pu.p;
     g.lda = px.ld, g.ldb = pg.ld, g.ldb2 = pu.ld;
     g.segments = 1, g.steps = (uint32_t)(round_up(d.dim, kStepK) / kStepK);
+    g.ka = g.kb = (uint32_t)round_up(d.dim, 8);
     g.m = (uint32_t)d.tokens, g.n = (uint32_t)d.hidden, g.batch = 1, g.splits = 1;
     const FfnOut o{(bf16 *)h, saved, m.h.ld};
     switch (d.act) {
@@ -380,21 +376,21 @@ template <bool ABYK> int product(GemmArgs &g, const ProductOut &o, hipStream_t s
 // Where the backward pass keeps what, in bytes from the workspace's start.
 // Copies of operands lie behind the rest, as many as there are.
 struct FfnBackwardSpace {
-    size_t tokens, hidden;  // padded
-    size_t grads, part, copies;
+    size_t hidden;  // padded: a tile's block of rows belongs to one of dG and dU
+    size_t steps;   // of tokens
+    size_t part, copies;  // dG and dU lie at the start
 };
 FfnBackwardSpace ffn_backward_space(const ar_ffn_desc &d, bool dx, bool dw)
 {
     FfnBackwardSpace s{};
-    s.tokens = round_up(d.tokens, kStepK), s.hidden = round_up(d.hidden, kStepK);
+    s.hidden = round_up(d.hidden, kStepK), s.steps = (d.tokens + kStepK - 1) / kStepK;
     size_t parts = 0;
     if (dx) parts = part_bytes(d.tokens, d.dim, 2 * s.hidden / kStepK);
     if (dw) {
-        const size_t p = part_bytes(2 * s.hidden, d.dim, s.tokens / kStepK);
+        const size_t p = part_bytes(2 * s.hidden, d.dim, s.steps);
         parts = p > parts ? p : parts;
     }
-    s.grads = 0;
-    s.part = round_up(s.tokens * 2 * s.hidden * 2, 256);
+    s.part = round_up(d.tokens * 2 * s.hidden * 2, 256);
     s.copies = s.part + parts;
     return s;
 }
@@ -433,10 +429,10 @@ int ffn_backward(const ar_ffn_desc *desc, const void *dh, const void *x, const v
     if (!dx && !dwg) return AR_OK;  // nothing wanted
     const FfnBackwardSpace s = ffn_backward_space(d, dx != nullptr, dwg != nullptr);
     // both weights are read with one row stride
-    const bool w_direct = direct(m.wg, true) && direct(m.wu, true) && m.wg.ld == m.wu.ld, x_direct = direct(m.x, true);
+    const bool w_direct = direct(m.wg) && direct(m.wu) && m.wg.ld == m.wu.ld, x_direct = direct(m.x);
     size_t need = s.copies;
-    if (dx && !w_direct) need += 2 * packed_bytes(d.hidden, d.dim, true);
-    if (dwg && !x_direct) need += packed_bytes(d.tokens, d.dim, true);
+    if (dx && !w_direct) need += 2 * packed_bytes(d.hidden, d.dim);
+    if (dwg && !x_direct) need += packed_bytes(d.tokens, d.dim);
     if (!ws || ws_bytes < need) return AR_ERR_SCRATCH;
     if ((uintptr_t)ws % 256 != 0) return AR_ERR_ARG;
     const Mat wsm{ws, 1, need, need, 1};
@@ -446,8 +442,8 @@ int ffn_backward(const ar_ffn_desc *desc, const void *dh, const void *x, const v
         if (meet(wsm, in)) return AR_ERR_ARG;
 
     char *w = (char *)ws, *copies = w + s.copies;
-    const GradArgs ga{saved, (const bf16 *)dh, (bf16 *)(w + s.grads), m.h.ld, d.tokens, s.tokens, (uint32_t)d.hidden, (uint32_t)s.hidden};
-    const uint64_t groups = (s.tokens * (s.hidden / 8) + 255) / 256;
+    const GradArgs ga{saved, (const bf16 *)dh, (bf16 *)w, m.h.ld, d.tokens, (uint32_t)d.hidden, (uint32_t)s.hidden};
+    const uint64_t groups = (d.tokens * (s.hidden / 8) + 255) / 256;
     const dim3 grid((uint32_t)(groups < 16384 ? groups : 16384));
     switch (d.act) {
     case AR_ACT_SILU: hipLaunchKernelGGL((ffn_grad_kernel<AR_ACT_SILU>), grid, dim3(256), 0, st, ga); break;
@@ -457,11 +453,12 @@ int ffn_backward(const ar_ffn_desc *desc, const void *dh, const void *x, const v
     if ((rc = launch_status()) != AR_OK) return rc;
     if (dx) {
         Operand pg, pu;
-        if ((rc = pack(m.wg, true, w_direct, copies, st, &pg)) != AR_OK) return rc;
-        if ((rc = pack(m.wu, true, w_direct, copies, st, &pu)) != AR_OK) return rc;
+        if ((rc = pack(m.wg, w_direct, copies, st, &pg)) != AR_OK) return rc;
+        if ((rc = pack(m.wu, w_direct, copies, st, &pu)) != AR_OK) return rc;
         GemmArgs g{};
         g.segments = 2, g.steps = (uint32_t)(s.hidden / kStepK);
-        g.a[0] = w + s.grads, g.a[1] = w + s.grads + s.hidden * 2;
+        g.ka = (uint32_t)s.hidden, g.kb = (uint32_t)d.hidden;
+        g.a[0] = w, g.a[1] = w + s.hidden * 2;
         g.b[0] = pg.p, g.b[1] = pu.p;
         g.lda = (uint32_t)(s.hidden * 4), g.ldb = pg.ld;
         g.m = (uint32_t)d.tokens, g.n = pg.cols;
@@ -470,10 +467,11 @@ int ffn_backward(const ar_ffn_desc *desc, const void *dh, const void *x, const v
     }
     if (dwg) {
         Operand px;
-        if ((rc = pack(m.x, true, x_direct, copies, st, &px)) != AR_OK) return rc;
+        if ((rc = pack(m.x, x_direct, copies, st, &px)) != AR_OK) return rc;
         GemmArgs g{};
-        g.segments = 1, g.steps = (uint32_t)(s.tokens / kStepK);
-        g.a[0] = w + s.grads, g.b[0] = px.p;
+        g.segments = 1, g.steps = (uint32_t)s.steps;
+        g.ka = g.kb = (uint32_t)d.tokens;
+        g.a[0] = w, g.b[0] = px.p;
         g.lda = (uint32_t)(s.hidden * 4), g.ldb = px.ld;
         g.m = (uint32_t)(2 * s.hidden), g.n = px.cols;
         const ProductOut o{{(bf16 *)dwg, (bf16 *)dwu}, (float *)(w + s.part), {og.ld, ou.ld}, (uint32_t)s.hidden, (uint32_t)d.hidden, (uint32_t)d.dim};
@@ -496,8 +494,8 @@ extern "C" size_t ar_gated_ffn_backward_workspace(const ar_ffn_desc *desc)
 {
     if (ar::check_ffn(desc) != AR_OK || !desc->tokens) return 0;
     // pointers' alignment is not known before the call, so every copy counts
-    return ar::ffn_backward_space(*desc, true, true).copies + 2 * ar::packed_bytes(desc->hidden, desc->dim, true) +
-           ar::packed_bytes(desc->tokens, desc->dim, true);
+    return ar::ffn_backward_space(*desc, true, true).copies + 2 * ar::packed_bytes(desc->hidden, desc->dim) +
+           ar::packed_bytes(desc->tokens, desc->dim);
 }
 
 extern "C" int ar_gated_ffn(const ar_ffn_desc *desc, const void *x, const void *w_gate, const void *w_up, void *h,

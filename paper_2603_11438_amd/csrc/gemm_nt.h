@@ -3,9 +3,10 @@
 //
 // Operands are 16-bit and row-major, rows 16-byte aligned.  Each lies either by
 // rows, A[m][k] or B[n][k] with k contiguous, or by k, A[k][m] or B[k][n]; then
-// fragments are transposed on their way out of LDS, four k at a time.  k is a
-// multiple of 64; callers lay out what is not so.  A product may run over
-// several (A, B) pairs ("segments") of one k length one after another, all into
+// fragments are transposed on their way out of LDS, four k at a time.  What lies
+// behind the last k of an operand is not read: those lanes' loads are out of
+// their resource's range and bring zeros.  A product may run over several (A, B)
+// pairs ("segments") of one k length one after another, all into
 // the same sums ([dG dU] times [Wg; Wu]).  Operands in two planes, hi and lo,
 // are multiplied as hi hi + hi lo + lo hi.
 //
@@ -62,7 +63,7 @@ template <> struct Frag<bf16> {
 };
 
 constexpr int kMaxSegments = 2;
-constexpr int kStepK = 64;  // k is a multiple of this
+constexpr int kStepK = 64;  // steps that k is counted in
 
 // Tiles, by planes: rows and columns, and what they cost.  `busy`: us of a
 // compute unit for k = 64 of a tile while it has several to work on; `alone`:
@@ -77,8 +78,8 @@ struct TileCost {
 };
 constexpr int kTileSizes = 4;
 constexpr TileCost kTiles[2][kTileSizes] = {
-    {{64, 0.19, 0.26, 2.5, 2}, {128, 0.5, 0.68, 4.0, 2}, {192, 1.1, 1.1, 6.0, 1}, {256, 1.67, 1.67, 9.0, 1}},
-    {{64, 0.4, 0.5, 3.0, 1}, {128, 1.2, 1.3, 6.0, 1}, {192, 2.8, 2.8, 9.0, 1}, {256, 4.6, 4.6, 14.0, 1}},
+    {{64, 0.19, 0.26, 2.5, 2}, {128, 0.5, 0.68, 5.0, 2}, {192, 1.1, 1.1, 12.0, 1}, {256, 1.67, 1.67, 20.0, 1}},
+    {{64, 0.4, 0.45, 3.0, 1}, {128, 1.2, 1.3, 8.0, 1}, {192, 2.8, 2.8, 14.0, 1}, {256, 4.6, 4.6, 24.0, 1}},
 };
 
 // The tile (an index of kTiles) and the number of runs k is split into that
@@ -117,7 +118,8 @@ struct GemmArgs {
     const void *a[kMaxSegments], *b[kMaxSegments];
     const void *b2;             // paired operands: the second of each pair of columns (one segment)
     uint64_t a_lo, b_lo;        // two planes: bytes from the hi plane to the lo plane (one segment)
-    uint32_t segments, steps;   // steps of 64 per segment
+    uint32_t segments, steps;   // steps of 64 per segment, the last one not always whole
+    uint32_t ka, kb;            // each operand's k of a segment (by rows: a multiple of 8)
     uint32_t lda, ldb, ldb2;    // bytes
     uint32_t m, n;              // of the result (paired: of each; by k: multiples of 8 that can be read)
     uint32_t tiles_m, tiles_n;
@@ -126,13 +128,16 @@ struct GemmArgs {
     uint32_t splits;            // runs of stages that k is split into (grid.y); 1: not split
 };
 
+// A load from this offset on is out of range: it touches no memory and brings zeros.
+constexpr uint32_t kOutOfRange = 0x80000000u;
+
 // a: wave-uniform
 __device__ __forceinline__ u32x4v tile_resource(uint64_t a)
 {
     u32x4v r;
     r.x = (uint32_t)a;
     r.y = (uint32_t)(a >> 32) & 0xffffu;
-    r.z = 0x80000000u;  // offsets stay below 2^31 (gemm_reaches); rows are clamped to the matrix
+    r.z = kOutOfRange;  // offsets stay below 2^31 (gemm_reaches); rows are clamped to the matrix
     r.w = 0x00020000u;
     return r;
 }
@@ -247,6 +252,17 @@ template <typename S, bool BYK, int R> struct Side {
             }
         }
     }
+
+    // Puts the lanes that would load from k = `left` of the stage on out of range.
+    __device__ __forceinline__ void stop_at(uint32_t wave, int left)
+    {
+        const uint32_t lane = threadIdx.x & 63u;
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i) {
+            const uint32_t q = (i * S::WAVES + wave) * 64 + lane, row = q / CHUNKS, k = BYK ? row : ((q % CHUNKS) ^ swizzle(row)) * 8;
+            if ((int)k >= left) off[i] = kOutOfRange;
+        }
+    }
 };
 
 __device__ __forceinline__ uint64_t uniform_address(const void *p)
@@ -286,19 +302,22 @@ __device__ __forceinline__ void gemm_tile(const GemmArgs &g, const TileAt at, ch
 
     SideA sa;
     SideB sb;
-    sa.place(wave, m0, g.m, [&](uint32_t row, uint32_t first) {
-        return ABYK ? row * g.lda : ((first + row < g.m ? first + row : g.m - 1) - first) * g.lda;
-    });
-    sb.place(wave, n0, g.n, [&](uint32_t row, uint32_t first) {
-        if (BBYK) return row * g.ldb;
-        uint32_t ld = g.ldb, r = row;
-        if (PAIRED) {
-            const uint32_t in = row % (2 * HALF);
-            ld = in < HALF ? g.ldb : g.ldb2;
-            r = row / (2 * HALF) * HALF + in % HALF;
-        }
-        return ((first + r < g.n ? first + r : g.n - 1) - first) * ld;
-    });
+    auto place = [&]() {
+        sa.place(wave, m0, g.m, [&](uint32_t row, uint32_t first) {
+            return ABYK ? row * g.lda : ((first + row < g.m ? first + row : g.m - 1) - first) * g.lda;
+        });
+        sb.place(wave, n0, g.n, [&](uint32_t row, uint32_t first) {
+            if (BBYK) return row * g.ldb;
+            uint32_t ld = g.ldb, r = row;
+            if (PAIRED) {
+                const uint32_t in = row % (2 * HALF);
+                ld = in < HALF ? g.ldb : g.ldb2;
+                r = row / (2 * HALF) * HALF + in % HALF;
+            }
+            return ((first + r < g.n ? first + r : g.n - 1) - first) * ld;
+        });
+    };
+    place();
     const uint32_t per = g.steps * (kStepK / S::BK), all = g.segments * per;
     const uint32_t begin = (uint32_t)((uint64_t)all * blockIdx.y / g.splits);
     const uint32_t total = (uint32_t)((uint64_t)all * (blockIdx.y + 1) / g.splits) - begin;
@@ -316,7 +335,12 @@ __device__ __forceinline__ void gemm_tile(const GemmArgs &g, const TileAt at, ch
                                   (BBYK ? (uint64_t)step * S::BK * g.ldb + n0 * 2 : (uint64_t)n0 * g.ldb));
         point();
     };
+    auto mask = [&]() {
+        if ((step + 1) * S::BK > g.ka) sa.stop_at(wave, (int)g.ka - (int)(step * S::BK));
+        if ((step + 1) * S::BK > g.kb) sb.stop_at(wave, (int)g.kb - (int)(step * S::BK));
+    };
     enter();
+    mask();
     if (PAIRED) rb2 = tile_resource(uniform_address((const char *)g.b2 + (uint64_t)n0 * g.ldb2));
     uint32_t put = lds0 + wave * 1024, kbyte = step * S::ROW, slot = 0;
     auto load_one = [&](int n) {
@@ -325,7 +349,9 @@ __device__ __forceinline__ void gemm_tile(const GemmArgs &g, const TileAt at, ch
             load_to_lds(put + plane * S::PLANE + i * S::WAVES * 1024, sa.off[i], plane ? ra_lo : ra, ABYK ? 0u : kbyte);
         } else {
             const int k = i - LOADS_A;
-            const bool second = PAIRED && (((k * S::WAVES + wave) * (1024 / S::ROW)) % (2 * HALF)) >= HALF;
+            // a load of the four waves covers 32 rows (or 64): all of one half
+            static_assert(!PAIRED || HALF % (S::WAVES * 1024 / S::ROW) == 0, "loads do not straddle halves");
+            const bool second = PAIRED && k * S::WAVES * (1024 / S::ROW) % (2 * HALF) >= HALF;
             load_to_lds(put + plane * S::PLANE + A_BYTES + k * S::WAVES * 1024, sb.off[k], plane ? rb_lo : second ? rb2 : rb,
                         BBYK ? 0u : kbyte);
         }
@@ -337,12 +363,15 @@ __device__ __forceinline__ void gemm_tile(const GemmArgs &g, const TileAt at, ch
         kbyte += S::ROW;
         if (++step == per) {
             step = 0, kbyte = 0;
-            if (++segment < g.segments) enter();
+            ++segment;  // never past the last: stages end there
+            enter();
+            place();
         } else if (ABYK || BBYK) {
             if (ABYK) sa.base += (uint64_t)S::BK * g.lda;
             if (BBYK) sb.base += (uint64_t)S::BK * g.ldb;
             point();
         }
+        mask();
     };
 
     // Fragments: lane l holds row (by k: column) l%32 of a block and k = 16 *
@@ -483,6 +512,43 @@ template <typename O, int COLS, typename V> __device__ __forceinline__ void stag
         }
     asm volatile("" ::: "memory");
 }
+
+// 32 rows of a padded matrix on their way to the lanes that hold their
+// elements' sums: loaded by rows, a whole row's bytes together, and later staged
+// in LDS.  Rows of at least `cols` elements (a multiple of 8); 0: no rows.
+template <typename O, int COLS> struct RowsAhead {
+    static constexpr int PER = 16 / (int)sizeof(O), LANES = COLS / PER, N = 32 * LANES / 64;
+    u32x4v v[N];
+    __device__ __forceinline__ void load(const O *from, uint64_t ld, uint32_t cols)
+    {
+        const uint32_t lane = threadIdx.x & 63u;
+#pragma unroll
+        for (int n = 0; n < N; ++n) {
+            const uint32_t r = (n * 64 + lane) / LANES, c = (n * 64 + lane) % LANES * PER;
+            if (c < cols) v[n] = *(const u32x4v *)(from + r * ld + c);
+        }
+    }
+    __device__ __forceinline__ void stage(char *lds) const
+    {
+        const uint32_t lane = threadIdx.x & 63u;
+        asm volatile("" ::: "memory");
+#pragma unroll
+        for (int n = 0; n < N; ++n) {
+            const uint32_t r = (n * 64 + lane) / LANES, c = (n * 64 + lane) % LANES * PER;
+            *(u32x4v *)(lds + r * kStagePitch<O, COLS> + c * sizeof(O)) = v[n];
+        }
+        asm volatile("" ::: "memory");
+    }
+    // the staged elements of columns j*32 + 8*q + 4*(l/32) on, row l%32
+    static __device__ __forceinline__ void take(const char *lds, int j, int q, float *out)
+    {
+        const uint32_t lane = threadIdx.x & 63u;
+        typedef O O4 __attribute__((ext_vector_type(4)));
+        const O4 x = *(const O4 *)(lds + (lane & 31u) * kStagePitch<O, COLS> + (j * 32 + q * 8 + (lane >> 5) * 4) * sizeof(O));
+#pragma unroll
+        for (int k = 0; k < 4; ++k) out[k] = (float)x[k];
+    }
+};
 
 // Writes staged rows to `out` and the rows behind it: of the 32 rows those in
 // [from, until), of the columns the first `cols`.

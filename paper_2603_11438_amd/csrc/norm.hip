@@ -36,6 +36,7 @@ struct NormBwdArgs {
     uint32_t cols;
     int flags;
     int want;            // kWant*
+    int has_ds;          // else ds is s: read, and taken as zero
     float alpha, eps;
 };
 
@@ -54,7 +55,29 @@ __device__ __forceinline__ uint32_t group_of(uint64_t rows, uint64_t t, uint32_t
 
 template <typename T> constexpr int kVec = 16 / (int)sizeof(T);
 
-// One thread's share of a row: vectors threadIdx.x + k * BS.
+// One thread's share of a row, vectors threadIdx.x + k * BS, in its own type: the
+// next row waits like this while one is worked on.
+template <typename T, int NV> struct RawRow {
+    typedef T Vec __attribute__((ext_vector_type(kVec<T>)));
+    Vec v[NV];
+    __device__ __forceinline__ float at(int k, int j) const { return (float)v[k][j]; }
+};
+template <int NV, int BS, bool TAIL, typename T>
+__device__ __forceinline__ void load_raw(const T *p, uint32_t cols, RawRow<T, NV> &out)
+{
+    constexpr int VEC = kVec<T>;
+#pragma unroll
+    for (int k = 0; k < NV; ++k) {
+        const uint32_t at = (threadIdx.x + k * BS) * VEC;
+        if (at + VEC <= cols) {
+            out.v[k] = *(const typename VecOf<T, VEC>::type *)(p + at);
+        } else {
+#pragma unroll
+            for (int j = 0; j < VEC; ++j) out.v[k][j] = TAIL && at + j < cols ? p[at + j] : (T)0.0f;
+        }
+    }
+}
+
 template <typename T, int VEC, int NV, int BS, bool TAIL>
 __device__ __forceinline__ void load_row(const T *p, uint32_t cols, float (*out)[VEC])
 {
@@ -108,9 +131,10 @@ __global__ __launch_bounds__(BS) void norm_kernel(const NormArgs a)
     uint64_t row = first_row(a.rows, blockIdx.x, gridDim.x);
     if (row >= last) return;
     const float inv = 1.0f / (float)a.cols;
-    float w1[NV][VEC], w2[NV][VEC], g[NV][VEC], y[NV][VEC], r[NV][VEC];
-    load_row<T, VEC, NV, BS, TAIL>((const T *)a.y + row * a.ld_y, a.cols, y);
-    load_row<T, VEC, NV, BS, TAIL>((const T *)a.residual + row * a.ld_r, a.cols, r);
+    float w1[NV][VEC], w2[NV][VEC], g[NV][VEC];
+    RawRow<T, NV> y, r, next_y, next_r;
+    load_raw<NV, BS, TAIL>((const T *)a.y + row * a.ld_y, a.cols, next_y);
+    load_raw<NV, BS, TAIL>((const T *)a.residual + row * a.ld_r, a.cols, next_r);
     load_param<P, VEC, NV, BS, TAIL>(post ? a.post_w : nullptr, a.cols, w1);
     load_param<P, VEC, NV, BS, TAIL>(a.pre_w, a.cols, w2);
     uint64_t gate_end = 0;  // first row that this gate row does not hold for
@@ -120,30 +144,27 @@ __global__ __launch_bounds__(BS) void norm_kernel(const NormArgs a)
             gate_end = (k + 1) * a.rows_per_gate;
             load_param<P, VEC, NV, BS, TAIL>(a.gate ? (const P *)a.gate + k * a.cols : nullptr, a.cols, g);
         }
-        float v[NV][VEC], base[NV][VEC], sum[1] = {0.0f};
-#pragma unroll
-        for (int k = 0; k < NV; ++k)
-#pragma unroll
-            for (int j = 0; j < VEC; ++j) {
-                v[k][j] = y[k][j];
-                base[k][j] = a.alpha * r[k][j];
-                sum[0] += y[k][j] * y[k][j];
-            }
+        y = next_y, r = next_r;
         if (row + 1 < last) {
-            load_row<T, VEC, NV, BS, TAIL>((const T *)a.y + (row + 1) * a.ld_y, a.cols, y);
-            load_row<T, VEC, NV, BS, TAIL>((const T *)a.residual + (row + 1) * a.ld_r, a.cols, r);
+            load_raw<NV, BS, TAIL>((const T *)a.y + (row + 1) * a.ld_y, a.cols, next_y);
+            load_raw<NV, BS, TAIL>((const T *)a.residual + (row + 1) * a.ld_r, a.cols, next_r);
         }
-        float r1 = 1.0f;
+        float sum[1] = {0.0f}, r1 = 1.0f;
         if (post) {
+#pragma unroll
+            for (int k = 0; k < NV; ++k)
+#pragma unroll
+                for (int j = 0; j < VEC; ++j) sum[0] += y.at(k, j) * y.at(k, j);
             group_sum<W, 1>(sum, slots, turn);
             r1 = 1.0f / sqrtf(sum[0] * inv + a.eps);
         }
+        float v[NV][VEC];
         sum[0] = 0.0f;
 #pragma unroll
         for (int k = 0; k < NV; ++k)
 #pragma unroll
             for (int j = 0; j < VEC; ++j) {
-                v[k][j] = base[k][j] + g[k][j] * (v[k][j] * r1 * w1[k][j]);
+                v[k][j] = a.alpha * r.at(k, j) + g[k][j] * (y.at(k, j) * r1 * w1[k][j]);
                 sum[0] += v[k][j] * v[k][j];
             }
         store_row<T, VEC, NV, BS, TAIL>((T *)a.s + row * a.ld_s, a.cols, v);
@@ -162,7 +183,29 @@ __global__ __launch_bounds__(BS) void norm_kernel(const NormArgs a)
 // Rows too long for registers: each pass reads the row again, from the caches
 // where it fits them.  A thread meets the same elements in every pass, so the
 // outputs may still be the inputs.
-constexpr int kLongThreads = 512;
+constexpr int kLongThreads = 1024;
+
+// f(first column, how many) for this thread's vectors of four columns.
+template <typename F> __device__ __forceinline__ void long_row(uint32_t cols, F f)
+{
+    for (uint32_t i = threadIdx.x * 4; i < cols; i += kLongThreads * 4) f(i, i + 4 <= cols ? 4 : (int)(cols - i));
+}
+template <typename T> __device__ __forceinline__ void load4(const T *p, uint32_t at, int have, float *out)
+{
+    if (have == 4) load_vec<T, 4>(p + at, out);
+    else load_part<T, 4>(p + at, have, out);
+}
+template <typename T> __device__ __forceinline__ void store4(T *p, uint32_t at, int have, const float *in)
+{
+    if (have == 4) store_vec<T, 4>(p + at, in);
+    else store_part<T, 4>(p + at, have, in);
+}
+// A weight or gate; absent ones are ones.
+template <typename P> __device__ __forceinline__ void param4(const P *p, uint32_t at, int have, float *out)
+{
+    if (p) load4(p, at, have, out);
+    else out[0] = out[1] = out[2] = out[3] = 1.0f;
+}
 
 template <typename T, typename P> __global__ __launch_bounds__(kLongThreads) void norm_long_kernel(const NormArgs a)
 {
@@ -177,28 +220,39 @@ template <typename T, typename P> __global__ __launch_bounds__(kLongThreads) voi
         const P *g = a.gate ? (const P *)a.gate + row / a.rows_per_gate * a.cols : nullptr;
         float sum[1] = {0.0f}, r1 = 1.0f, r2 = 1.0f;
         if (post) {
-            for (uint32_t i = threadIdx.x; i < a.cols; i += kLongThreads) sum[0] += (float)y[i] * (float)y[i];
+            long_row(a.cols, [&](uint32_t i, int have) {
+                float v[4];
+                load4(y, i, have, v);
+                for (int k = 0; k < 4; ++k) sum[0] += v[k] * v[k];
+            });
             group_sum<W, 1>(sum, slots, turn);
             r1 = 1.0f / sqrtf(sum[0] * inv + a.eps);
         }
-        auto at = [&](uint32_t i) {
-            return a.alpha * (float)r[i] + (g ? (float)g[i] : 1.0f) * ((float)y[i] * r1 * (w1 ? (float)w1[i] : 1.0f));
+        auto at = [&](uint32_t i, int have, float *v) {
+            float u[4], w[4], h[4];
+            load4(y, i, have, v), load4(r, i, have, u), param4(w1, i, have, w), param4(g, i, have, h);
+            for (int k = 0; k < 4; ++k) v[k] = a.alpha * u[k] + h[k] * (v[k] * r1 * w[k]);
         };
         if (pre) {
             sum[0] = 0.0f;
-            for (uint32_t i = threadIdx.x; i < a.cols; i += kLongThreads) {
-                const float v = at(i);
-                sum[0] += v * v;
-            }
+            long_row(a.cols, [&](uint32_t i, int have) {
+                float v[4];
+                at(i, have, v);
+                for (int k = 0; k < have; ++k) sum[0] += v[k] * v[k];
+            });
             group_sum<W, 1>(sum, slots, turn);
             r2 = 1.0f / sqrtf(sum[0] * inv + a.eps);
         }
         T *s = (T *)a.s + row * a.ld_s, *x = (T *)a.x + row * a.ld_x;
-        for (uint32_t i = threadIdx.x; i < a.cols; i += kLongThreads) {
-            const float v = at(i);
-            s[i] = (T)v;
-            if (pre) x[i] = (T)(v * r2 * (w2 ? (float)w2[i] : 1.0f));
-        }
+        long_row(a.cols, [&](uint32_t i, int have) {
+            float v[4], w[4];
+            at(i, have, v);
+            if (pre) param4(w2, i, have, w);
+            store4(s, i, have, v);
+            if (!pre) return;
+            for (int k = 0; k < 4; ++k) v[k] = v[k] * r2 * w[k];
+            store4(x, i, have, v);
+        });
     }
 }
 
@@ -235,67 +289,66 @@ __global__ __launch_bounds__(BS) void norm_bwd_kernel(const NormBwdArgs a)
     for (int k = 0; k < NV; ++k)
 #pragma unroll
         for (int j = 0; j < VEC; ++j) dw1[k][j] = dw2[k][j] = dg[k][j] = 0.0f;
+    RawRow<T, NV> y, z, ds, dx, next_y, next_z, next_ds, next_dx;
+    auto load_next = [&](uint64_t row) {
+        load_raw<NV, BS, TAIL>((const T *)a.y + row * a.ld_y, a.cols, next_y);
+        load_raw<NV, BS, TAIL>((const T *)a.s + row * a.ld_s, a.cols, next_z);
+        // absent ones are not used (dx), or read where s is and taken as zero (ds)
+        load_raw<NV, BS, TAIL>((const T *)a.ds + row * a.ld_ds, a.cols, next_ds);
+        load_raw<NV, BS, TAIL>((const T *)a.dx + row * a.ld_dx, a.cols, next_dx);
+    };
+    load_next(first);
     uint64_t gate_end = 0;
     for (uint64_t row = first; row < last; ++row) {
-        float y[NV][VEC], z[NV][VEC], dz[NV][VEC], dx[NV][VEC];
-        load_row<T, VEC, NV, BS, TAIL>((const T *)a.y + row * a.ld_y, a.cols, y);
-        load_row<T, VEC, NV, BS, TAIL>((const T *)a.s + row * a.ld_s, a.cols, z);
-        if (a.ds) {
-            load_row<T, VEC, NV, BS, TAIL>((const T *)a.ds + row * a.ld_ds, a.cols, dz);
-        } else {
-#pragma unroll
-            for (int k = 0; k < NV; ++k)
-#pragma unroll
-                for (int j = 0; j < VEC; ++j) dz[k][j] = 0.0f;
-        }
-        if (pre) load_row<T, VEC, NV, BS, TAIL>((const T *)a.dx + row * a.ld_dx, a.cols, dx);
         if (row >= gate_end) {
             const uint64_t k = row / a.rows_per_gate;
             gate_end = (k + 1) * a.rows_per_gate;
             load_param<P, VEC, NV, BS, TAIL>(a.gate ? (const P *)a.gate + k * a.cols : nullptr, a.cols, g);
         }
+        y = next_y, z = next_z, ds = next_ds, dx = next_dx;
+        if (row + 1 < last) load_next(row + 1);
         float sum[3] = {0.0f, 0.0f, 0.0f};
 #pragma unroll
         for (int k = 0; k < NV; ++k)
 #pragma unroll
             for (int j = 0; j < VEC; ++j) {
-                sum[0] += y[k][j] * y[k][j];
+                sum[0] += y.at(k, j) * y.at(k, j);
                 if (pre) {
-                    sum[1] += z[k][j] * z[k][j];
-                    sum[2] += dx[k][j] * w2[k][j] * z[k][j];
+                    sum[1] += z.at(k, j) * z.at(k, j);
+                    sum[2] += dx.at(k, j) * w2[k][j] * z.at(k, j);
                 }
             }
         if (post || pre) group_sum<W, 3>(sum, slots3, turn3);
         const float r1 = post ? 1.0f / sqrtf(sum[0] * inv + a.eps) : 1.0f;
         const float r2 = pre ? 1.0f / sqrtf(sum[1] * inv + a.eps) : 1.0f;
         const float c2 = r2 * r2 * (sum[2] * inv);
-        float svy[1] = {0.0f};
+        float svy[1] = {0.0f}, out[NV][VEC], v[NV][VEC];
 #pragma unroll
         for (int k = 0; k < NV; ++k)
 #pragma unroll
             for (int j = 0; j < VEC; ++j) {
-                float G = dz[k][j];
+                float G = a.has_ds ? ds.at(k, j) : 0.0f;
                 if (pre) {
-                    G += r2 * (dx[k][j] * w2[k][j] - z[k][j] * c2);
-                    dw2[k][j] += dx[k][j] * (z[k][j] * r2);
+                    G += r2 * (dx.at(k, j) * w2[k][j] - z.at(k, j) * c2);
+                    dw2[k][j] += dx.at(k, j) * (z.at(k, j) * r2);
                 }
-                const float unit = y[k][j] * r1, dn = G * g[k][j];
+                const float unit = y.at(k, j) * r1, dn = G * g[k][j];
                 dg[k][j] += G * (unit * w1[k][j]);
                 dw1[k][j] += dn * unit;
-                z[k][j] = a.alpha * G;
-                dz[k][j] = dn * w1[k][j];
-                svy[0] += dz[k][j] * y[k][j];
+                out[k][j] = a.alpha * G;
+                v[k][j] = dn * w1[k][j];
+                svy[0] += v[k][j] * y.at(k, j);
             }
-        store_row<T, VEC, NV, BS, TAIL>((T *)a.dr + row * a.ld_dr, a.cols, z);
+        store_row<T, VEC, NV, BS, TAIL>((T *)a.dr + row * a.ld_dr, a.cols, out);
         if (post) {
             group_sum<W, 1>(svy, slots1, turn1);
             const float c1 = r1 * r1 * (svy[0] * inv);
 #pragma unroll
             for (int k = 0; k < NV; ++k)
 #pragma unroll
-                for (int j = 0; j < VEC; ++j) dz[k][j] = r1 * (dz[k][j] - y[k][j] * c1);
+                for (int j = 0; j < VEC; ++j) v[k][j] = r1 * (v[k][j] - y.at(k, j) * c1);
         }
-        store_row<T, VEC, NV, BS, TAIL>((T *)a.dy + row * a.ld_dy, a.cols, dz);
+        store_row<T, VEC, NV, BS, TAIL>((T *)a.dy + row * a.ld_dy, a.cols, v);
         if ((a.want & kWantGate) && (row + 1 == gate_end || row + 1 == last)) {
             const GateOut<P> o = gate_out<P>(a, part, row / a.rows_per_gate, first, last);
             if (o.whole) store_row<P, VEC, NV, BS, TAIL>(o.whole, a.cols, dg);
@@ -324,32 +377,41 @@ template <typename T, typename P> __global__ __launch_bounds__(kLongThreads) voi
     const P *w1 = post ? (const P *)a.post_w : nullptr, *w2 = (const P *)a.pre_w;
     for (uint64_t row = first; row < last; ++row) {
         const T *y = (const T *)a.y + row * a.ld_y, *z = (const T *)a.s + row * a.ld_s;
-        const T *ds = a.ds ? (const T *)a.ds + row * a.ld_ds : nullptr, *dx = (const T *)a.dx + row * a.ld_dx;
+        const T *ds = (const T *)a.ds + row * a.ld_ds, *dx = (const T *)a.dx + row * a.ld_dx;
         const uint64_t gk = row / a.rows_per_gate;
         const P *g = a.gate ? (const P *)a.gate + gk * a.cols : nullptr;
         float sum[3] = {0.0f, 0.0f, 0.0f};
         if (post || pre) {
-            for (uint32_t i = threadIdx.x; i < a.cols; i += kLongThreads) {
-                sum[0] += (float)y[i] * (float)y[i];
-                if (pre) {
-                    sum[1] += (float)z[i] * (float)z[i];
-                    sum[2] += (float)dx[i] * (w2 ? (float)w2[i] : 1.0f) * (float)z[i];
+            long_row(a.cols, [&](uint32_t i, int have) {
+                float v[4], u[4], d[4], w[4];
+                load4(y, i, have, v), load4(z, i, have, u), load4(dx, i, have, d), param4(w2, i, have, w);
+                for (int k = 0; k < have; ++k) {
+                    sum[0] += v[k] * v[k];
+                    if (pre) sum[1] += u[k] * u[k], sum[2] += d[k] * w[k] * u[k];
                 }
-            }
+            });
             group_sum<W, 3>(sum, slots3, turn3);
         }
         const float r1 = post ? 1.0f / sqrtf(sum[0] * inv + a.eps) : 1.0f;
         const float r2 = pre ? 1.0f / sqrtf(sum[1] * inv + a.eps) : 1.0f;
         const float c2 = r2 * r2 * (sum[2] * inv);
-        auto total = [&](uint32_t i) {
-            float G = ds ? (float)ds[i] : 0.0f;
-            if (pre) G += r2 * ((float)dx[i] * (w2 ? (float)w2[i] : 1.0f) - (float)z[i] * c2);
-            return G;
+        // the gradient of s, and dx * s / rms(s)
+        auto total = [&](uint32_t i, int have, float *G, float *unit2) {
+            float u[4], d[4], w[4];
+            load4(ds, i, have, G), load4(z, i, have, u), load4(dx, i, have, d), param4(w2, i, have, w);
+            for (int k = 0; k < 4; ++k) {
+                if (!a.has_ds) G[k] = 0.0f;
+                if (pre) G[k] += r2 * (d[k] * w[k] - u[k] * c2);
+                unit2[k] = d[k] * (u[k] * r2);
+            }
         };
         float svy[1] = {0.0f}, c1 = 0.0f;
         if (post) {
-            for (uint32_t i = threadIdx.x; i < a.cols; i += kLongThreads)
-                svy[0] += total(i) * (g ? (float)g[i] : 1.0f) * (w1 ? (float)w1[i] : 1.0f) * (float)y[i];
+            long_row(a.cols, [&](uint32_t i, int have) {
+                float G[4], t[4], v[4], w[4], h[4];
+                total(i, have, G, t), load4(y, i, have, v), param4(w1, i, have, w), param4(g, i, have, h);
+                for (int k = 0; k < have; ++k) svy[0] += G[k] * h[k] * w[k] * v[k];
+            });
             group_sum<W, 1>(svy, slots1, turn1);
             c1 = r1 * r1 * (svy[0] * inv);
         }
@@ -358,26 +420,42 @@ template <typename T, typename P> __global__ __launch_bounds__(kLongThreads) voi
         const bool gate_ends = o.whole && (row + 1) % a.rows_per_gate == 0;
         // a gate row that ends here adds up in the tail row until then
         float *acc = o.whole ? part + (size_t)kPartGateTail * a.cols : o.part;
-        for (uint32_t i = threadIdx.x; i < a.cols; i += kLongThreads) {
-            const float G = total(i), yi = (float)y[i], unit = yi * r1, wi = w1 ? (float)w1[i] : 1.0f;
-            const float dn = G * (g ? (float)g[i] : 1.0f);
-            if (a.want & kWantPre) {
-                float *p = part + (size_t)kPartPre * a.cols + i;
-                *p = (row == first ? 0.0f : *p) + (float)dx[i] * ((float)z[i] * r2);
+        auto add = [&](float *p, uint32_t i, int have, bool fresh, float *v) {
+            float old[4];
+            if (!fresh) {
+                load4(p, i, have, old);
+                for (int k = 0; k < 4; ++k) v[k] += old[k];
             }
+        };
+        long_row(a.cols, [&](uint32_t i, int have) {
+            float G[4], t[4], v[4], w[4], h[4], dn[4], p[4];
+            total(i, have, G, t), load4(y, i, have, v), param4(w1, i, have, w), param4(g, i, have, h);
+            if (a.want & kWantPre) {
+                float *to = part + (size_t)kPartPre * a.cols;
+                add(to, i, have, row == first, t);
+                store4(to, i, have, t);
+            }
+            for (int k = 0; k < 4; ++k) dn[k] = G[k] * h[k];
             if (a.want & kWantPost) {
-                float *p = part + (size_t)kPartPost * a.cols + i;
-                *p = (row == first ? 0.0f : *p) + dn * unit;
+                float *to = part + (size_t)kPartPost * a.cols;
+                for (int k = 0; k < 4; ++k) p[k] = dn[k] * (v[k] * r1);
+                add(to, i, have, row == first, p);
+                store4(to, i, have, p);
             }
             if (a.want & kWantGate) {
-                const float v = (new_gate ? 0.0f : acc[i]) + G * (unit * wi);
-                if (gate_ends) o.whole[i] = (P)v;
-                else acc[i] = v;
+                for (int k = 0; k < 4; ++k) p[k] = G[k] * (v[k] * r1 * w[k]);
+                add(acc, i, have, new_gate, p);
+                if (gate_ends) store4(o.whole, i, have, p);
+                else store4(acc, i, have, p);
             }
-            const float v = dn * wi;
-            ((T *)a.dr)[row * a.ld_dr + i] = (T)(a.alpha * G);
-            ((T *)a.dy)[row * a.ld_dy + i] = (T)(post ? r1 * (v - yi * c1) : v);
-        }
+            for (int k = 0; k < 4; ++k) {
+                const float q = dn[k] * w[k];
+                dn[k] = post ? r1 * (q - v[k] * c1) : q;
+                G[k] = a.alpha * G[k];
+            }
+            store4((T *)a.dr + row * a.ld_dr, i, have, G);
+            store4((T *)a.dy + row * a.ld_dy, i, have, dn);
+        });
     }
 }
 
@@ -488,11 +566,14 @@ int check_outputs(const Mat *outs, int n_out, const Mat *ins, int n_in, const Ma
 
 uint64_t rows_per_gate(const ar_norm_desc &d) { return d.gate_rows ? d.rows / d.gate_rows : (d.rows ? d.rows : 1); }
 
-// Threads of a row and vectors of each, by the vectors of a row.
-struct Shape {
+// Threads of a row and vectors of each, by the vectors of a row.  Two vectors a
+// thread rather than four: 16384 x 8192 bf16 forward, 256 threads of four 216
+// us, 512 of two 190, 1024 of one 238 (its waves wait for each other longer).
+// Few rows are spread over more threads.
+struct RowShape {
     int threads, vecs;  // 0: the row does not fit
 };
-Shape forward_shape(size_t nvec, bool few)
+RowShape forward_shape(size_t nvec, bool few, int dtype)
 {
     if (few && nvec > 64) {
         if (nvec <= 256) return {256, 1};
@@ -500,13 +581,13 @@ Shape forward_shape(size_t nvec, bool few)
     }
     if (nvec <= 64) return {64, 1};
     if (nvec <= 128) return {64, 2};
-    if (nvec <= 256) return {64, 4};
     if (nvec <= 512) return {256, 2};
-    if (nvec <= 1024) return {256, 4};
+    if (nvec <= 1024) return {512, 2};
     if (nvec <= 2048) return {512, 4};
+    if (nvec <= 3072 && dtype == AR_FLOAT32) return {1024, 3};
     return {0, 0};
 }
-Shape backward_shape(size_t nvec)
+RowShape backward_shape(size_t nvec)
 {
     if (nvec <= 64) return {64, 1};
     if (nvec <= 256) return {256, 1};
@@ -515,17 +596,23 @@ Shape backward_shape(size_t nvec)
     return {0, 0};
 }
 
-// Workgroups: those that fit the device at once, each with a run of rows.
+// Workgroups of the forward: each with a run of rows, as many as the device
+// holds at once, and with many rows more of shorter runs (16384 x 8192 bf16:
+// 1024 workgroups 214 us, 8192 190).
 uint32_t forward_groups(const ar_norm_desc &d, int threads)
 {
-    const size_t fit = 256 * (size_t)(2048 / threads);
-    return (uint32_t)(d.rows < fit ? d.rows : fit);
+    const size_t fit = 256 * (size_t)(2048 / threads), half = d.rows / 2 < 8192 ? d.rows / 2 : 8192;
+    const size_t groups = half > fit ? half : fit;
+    return (uint32_t)(d.rows < groups ? d.rows : groups);
 }
-// The backward pass writes a row of partial sums for each.
+// The backward pass writes a row of partial sums for each workgroup: as few as
+// keep the device busy (8192 x 4096 bf16, of 256 threads: 512 89 us, 1024 94,
+// 256 115; 8192 x 8192, of 512 threads: 256 179 us, 512 188; 65536 x 512, of one
+// wave: 2048 85 us, 1024 126).
 uint32_t backward_groups(const ar_norm_desc &d)
 {
-    const size_t nvec = (d.cols * elem_bytes(d.dtype) + 15) / 16;
-    const size_t fit = nvec <= 256 ? 2048 : 512;
+    const RowShape sh = backward_shape((d.cols * elem_bytes(d.dtype) + 15) / 16);
+    const size_t fit = sh.threads == 64 ? 2048 : sh.threads == 256 ? 512 : 256;
     return (uint32_t)(d.rows < fit ? d.rows : fit);
 }
 
@@ -533,7 +620,7 @@ template <typename T, typename P> int launch_norm(const ar_norm_desc &d, const N
 {
     const size_t nvec = (d.cols + kVec<T> - 1) / kVec<T>;
     const bool tail = d.cols % kVec<T> != 0;
-    const Shape sh = forward_shape(nvec, d.rows <= kFewRows);
+    const RowShape sh = forward_shape(nvec, d.rows <= kFewRows, d.dtype);
     if (!sh.threads) {
         hipLaunchKernelGGL((norm_long_kernel<T, P>), dim3(forward_groups(d, kLongThreads)), dim3(kLongThreads), 0, st, a);
         return launch_status();
@@ -547,12 +634,14 @@ template <typename T, typename P> int launch_norm(const ar_norm_desc &d, const N
     }
     AR_NORM_CASE(64, 1)
     AR_NORM_CASE(64, 2)
-    AR_NORM_CASE(64, 4)
     AR_NORM_CASE(256, 1)
     AR_NORM_CASE(256, 2)
-    AR_NORM_CASE(256, 4)
+    AR_NORM_CASE(512, 2)
     AR_NORM_CASE(512, 4)
     AR_NORM_CASE(1024, 1)
+    if constexpr (sizeof(T) == 4) {
+        AR_NORM_CASE(1024, 3)
+    }
 #undef AR_NORM_CASE
     return AR_ERR_UNSUPPORTED;
 }
@@ -562,7 +651,7 @@ int launch_norm_bwd(const ar_norm_desc &d, const NormBwdArgs &a, uint32_t groups
 {
     const size_t nvec = (d.cols + kVec<T> - 1) / kVec<T>;
     const bool tail = d.cols % kVec<T> != 0;
-    const Shape sh = backward_shape(nvec);
+    const RowShape sh = backward_shape(nvec);
     const dim3 grid(groups);
     if (!sh.threads) {
         hipLaunchKernelGGL((norm_bwd_long_kernel<T, P>), grid, dim3(kLongThreads), 0, st, a);
@@ -674,11 +763,11 @@ int norm_backward(const ar_norm_desc *desc, const void *y, const void *s, const 
         for (const Mat &m : pars)
             if (meet(wsm, m)) return AR_ERR_ARG;
     }
-    a.y = y, a.s = s, a.ds = ds, a.dx = pre ? dx : s;
+    a.y = y, a.s = s, a.ds = ds ? ds : s, a.dx = pre ? dx : s, a.has_ds = ds != nullptr;
     a.post_w = post_w, a.gate = d.gate_rows ? gate : nullptr, a.pre_w = pre ? pre_w : nullptr;
     a.dy = dy, a.dr = dr, a.dgate = dgate, a.part = (float *)ws;
     a.rows = d.rows, a.rows_per_gate = rows_per_gate(d);
-    a.ld_y = ins[0].ld, a.ld_s = ins[1].ld, a.ld_ds = ins[2].ld, a.ld_dx = ins[3].ld, a.ld_dy = outs[0].ld, a.ld_dr = outs[1].ld;
+    a.ld_y = ins[0].ld, a.ld_s = ins[1].ld, a.ld_ds = ds ? ins[2].ld : ins[1].ld, a.ld_dx = pre ? ins[3].ld : ins[1].ld, a.ld_dy = outs[0].ld, a.ld_dr = outs[1].ld;
     a.cols = (uint32_t)d.cols, a.flags = d.flags, a.alpha = d.alpha, a.eps = d.eps;
     if (d.dtype == AR_FLOAT32)
         rc = d.param_dtype == AR_FLOAT32 ? launch_norm_bwd<float, float>(d, a, groups, st)

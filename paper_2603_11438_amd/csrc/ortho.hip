@@ -227,8 +227,43 @@ __device__ __forceinline__ void store_planes(char *stage, const float (&v)[S::NT
     }
 }
 
-template <typename S> constexpr int kOrthoStage = kStageColBytes<float, S::NT * 32> > kStageBytes<float, S::NT * 32>
-                                                      ? kStageColBytes<float, S::NT * 32> : kStageBytes<float, S::NT * 32>;
+// What an epilogue adds to its sums, from N planes of a padded matrix: block
+// row bi + 1 is loaded while bi is worked on.  Each plane has its own stage, the
+// first one also the epilogue's own (free again after the last take).
+template <typename S, typename X, int N> struct Ahead {
+    static constexpr int COLS = S::NT * 32;
+    const X *from;
+    size_t lo;  // bytes between planes
+    uint32_t rows, cols, row0, col0;
+    char *lds;
+    RowsAhead<X, COLS> next[N];
+    __device__ __forceinline__ void load(int bi)
+    {
+        const uint32_t first = row0 + bi * 32;
+        if (bi >= S::MT || first >= rows || col0 >= cols) return;
+#pragma unroll
+        for (int n = 0; n < N; ++n) next[n].load((const X *)((const char *)from + n * lo) + (uint64_t)first * cols + col0, cols, cols - col0);
+    }
+    __device__ __forceinline__ void stage(int bi)
+    {
+#pragma unroll
+        for (int n = 0; n < N; ++n) next[n].stage(lds + n * kStageBytes<X, COLS>);
+        load(bi + 1);
+    }
+    __device__ __forceinline__ void take(int bj, int q, float *out) const
+    {
+        RowsAhead<X, COLS>::take(lds, bj, q, out);
+        if (N == 2) {
+            float more[4];
+            RowsAhead<X, COLS>::take(lds + kStageBytes<X, COLS>, bj, q, more);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) out[k] += more[k];
+        }
+    }
+};
+
+template <typename S> constexpr int kOrthoStage = kStageColBytes<float, S::NT * 32> > 2 * kStageBytes<f16, S::NT * 32>
+                                                      ? kStageColBytes<float, S::NT * 32> : 2 * kStageBytes<f16, S::NT * 32>;
 template <typename S> constexpr int kOrthoLds = S::LDS > 4 * kOrthoStage<S> ? S::LDS : 4 * kOrthoStage<S>;
 
 // A = X X^T (SECOND false) or B = b A + c A A (true): tiles on and below the
@@ -250,30 +285,24 @@ __global__ __launch_bounds__(S::THREADS) void ortho_square_kernel(const GemmArgs
     char *stage = lds + (threadIdx.x >> 6) * kOrthoStage<S>;
     char *hi = ws + (SECOND ? o.at.b : o.at.a);
     const size_t lo = SECOND ? o.at.b_lo : o.at.a_lo;
+    Ahead<S, f16, PLANES> ahead{(const f16 *)(ws + o.at.a), o.at.a_lo, o.mp, o.mp, w.row0, w.col0, stage};
+    if (SECOND) ahead.load(0);
     static_for<S::MT>([&](auto block) {
         constexpr int bi = block.value;
         float v[NT][16];
         take(acc[bi], v);
         const uint32_t i = w.i(bi);
         const float di = SECOND && i < o.m ? diag_a[i] : 0.0f;
+        if (SECOND) ahead.stage(bi);
 #pragma unroll
         for (int bj = 0; bj < NT; ++bj)
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
                 const uint32_t j0 = w.j(bj, q * 4);
                 float off[4] = {0.0f, 0.0f, 0.0f, 0.0f}, dj[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-                if (SECOND && i < o.m && j0 < o.mp) {
-                    load_vec<float, 4>(diag_a + j0, dj);
-                    const f16 *p = (const f16 *)(ws + o.at.a) + (uint64_t)i * o.mp + j0;
-                    typedef f16 f16x4 __attribute__((ext_vector_type(4)));
-                    const f16x4 h = *(const f16x4 *)p;
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) off[k] = (float)h[k];
-                    if (PLANES == 2) {
-                        const f16x4 l = *(const f16x4 *)((const char *)p + o.at.a_lo);
-#pragma unroll
-                        for (int k = 0; k < 4; ++k) off[k] += (float)l[k];
-                    }
+                if (SECOND) {
+                    if (j0 < o.mp) load_vec<float, 4>(diag_a + j0, dj);
+                    ahead.take(bj, q, off);
                 }
 #pragma unroll
                 for (int k = 0; k < 4; ++k) {
@@ -322,8 +351,10 @@ __global__ __launch_bounds__(S::THREADS) void ortho_update_kernel(const GemmArgs
     const float to = last ? o.scale : next.x, ib = 1.0f / s.b, ix = s.tau / s.x;
     // X's planes are read by other tiles too, so they alternate; its fp32 values are not.
     char *stage = lds + (threadIdx.x >> 6) * kOrthoStage<S>;
-    const char *x_now = ws + o.at.x[o.step & 1u];
     char *x_next = ws + o.at.x[(o.step + 1) & 1u];
+    typedef typename std::conditional<PLANES == 2, float, f16>::type X;
+    Ahead<S, X, PLANES == 2 ? 1 : 2> ahead{(const X *)(ws + (PLANES == 2 ? o.at.xf : o.at.x[o.step & 1u])), o.at.x_lo, o.mp, o.np, w.row0, w.col0, stage};
+    ahead.load(0);
     O *out = (O *)o.out + at.batch * o.stride_out;
     static_for<S::MT>([&](auto block) {
         constexpr int bi = block.value;
@@ -331,23 +362,14 @@ __global__ __launch_bounds__(S::THREADS) void ortho_update_kernel(const GemmArgs
         take(acc[bi], v);
         const uint32_t i = w.i(bi);
         const float d = i < o.m ? o.a + diag_b[i] : 0.0f;
+        ahead.stage(bi);
 #pragma unroll
         for (int bj = 0; bj < NT; ++bj)
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
                 const uint32_t j0 = w.j(bj, q * 4);
-                float x[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-                if (i < o.m && j0 < o.np) {
-                    const size_t x_at = ((size_t)i * o.np + j0) * 2;
-                    if (PLANES == 2) {
-                        load_vec<float, 4>((const float *)(ws + o.at.xf + x_at * 2), x);
-                    } else {
-                        typedef f16 f16x4 __attribute__((ext_vector_type(4)));
-                        const f16x4 h = *(const f16x4 *)(x_now + x_at), l = *(const f16x4 *)(x_now + o.at.x_lo + x_at);
-#pragma unroll
-                        for (int k = 0; k < 4; ++k) x[k] = (float)h[k] + (float)l[k];
-                    }
-                }
+                float x[4];
+                ahead.take(bj, q, x);
 #pragma unroll
                 for (int k = 0; k < 4; ++k) {
                     const float y = (d * x[k] + v[bj][q * 4 + k] * ib) * ix;
@@ -516,7 +538,7 @@ void operands(GemmArgs *g, const OrthoArgs &o, size_t a, size_t a_lo, uint32_t l
               uint32_t m, uint32_t n)
 {
     *g = GemmArgs{};
-    g->segments = 1, g->steps = k / kStepK;
+    g->segments = 1, g->steps = k / kStepK, g->ka = g->kb = k;
     g->a[0] = o.ws + a, g->b[0] = o.ws + b, g->a_lo = a_lo, g->b_lo = b_lo;
     g->lda = lda * 2, g->ldb = ldb * 2;
     g->m = m, g->n = n, g->batch_a = g->batch_b = o.at.bytes, g->batch = o.batch, g->splits = 1;

@@ -36,9 +36,9 @@ def hipcc() -> str:
 
 def build(verbose: bool = False) -> str:
     """Compile every HIP/C++ source of libar into _lib/libar.so, and the native
-    part of the Python binding (always rebuilds)."""
+    parts of the Python binding (always rebuilds)."""
     os.makedirs(LIBDIR, exist_ok=True)
-    args_job = start_tensor_args()
+    extensions = {name: start_extension(name) for name in EXTENSIONS}
     tmp = LIB + ".tmp"
     with tempfile.TemporaryDirectory() as objdir:
         # One compiler per source, at the same time; then one link.
@@ -61,16 +61,21 @@ def build(verbose: bool = False) -> str:
     if verbose and lines:
         print("\n".join(lines))
     os.replace(tmp, LIB)
-    finish_tensor_args(args_job)
+    for name, job in extensions.items():
+        finish_extension(name, job)
     return LIB
 
 
-TENSOR_ARGS_SRC = os.path.join(CSRC, "tensor_args.cpp")
-TENSOR_ARGS = os.path.join(LIBDIR, "_tensor_args.so")
+# The native parts of the Python binding: module -> source.
+EXTENSIONS = {"_tensor_args": "tensor_args.cpp", "_ops_args": "ops_args.cpp"}
 
 
-def start_tensor_args() -> subprocess.Popen:
-    """Start compiling the native part of the Python binding against torch's
+def _extension(name: str) -> str:
+    return os.path.join(LIBDIR, name + ".so")
+
+
+def start_extension(name: str) -> subprocess.Popen:
+    """Start compiling a native part of the Python binding against torch's
     headers (its symbols come from the torch that the caller has imported)."""
     import sysconfig
 
@@ -79,20 +84,20 @@ def start_tensor_args() -> subprocess.Popen:
 
     cmd = ["g++", "-O2", "-std=c++17", "-fPIC", "-shared", "-w",
            f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", f'-DAR_TORCH_VERSION="{torch.__version__}"',
-           "-I", sysconfig.get_paths()["include"],
-           *[a for d in cpp_extension.include_paths() for a in ("-I", d)], TENSOR_ARGS_SRC,
+           "-I", INCLUDE, "-I", sysconfig.get_paths()["include"],
+           *[a for d in cpp_extension.include_paths() for a in ("-I", d)], os.path.join(CSRC, EXTENSIONS[name]),
            *[a for d in cpp_extension.library_paths() for a in ("-L", d)], "-ltorch_python", "-ltorch_cpu", "-lc10",
-           "-o", TENSOR_ARGS + ".tmp"]
+           "-o", _extension(name) + ".tmp"]
     os.makedirs(LIBDIR, exist_ok=True)
     return subprocess.Popen(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
 
 
-def finish_tensor_args(job: subprocess.Popen) -> str:
+def finish_extension(name: str, job: subprocess.Popen) -> str:
     out = job.communicate()[0]
     if job.returncode != 0:
-        raise RuntimeError("tensor_args build failed:\n" + (out or ""))
-    os.replace(TENSOR_ARGS + ".tmp", TENSOR_ARGS)
-    return TENSOR_ARGS
+        raise RuntimeError(f"{name} build failed:\n" + (out or ""))
+    os.replace(_extension(name) + ".tmp", _extension(name))
+    return _extension(name)
 
 
 ABI_CHECK_SRC = os.path.join(ROOT, "tests", "native", "abi_gpu_check.cpp")

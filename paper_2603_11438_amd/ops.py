@@ -11,13 +11,20 @@ itself refuses is an ARError.  Results and workspaces are allocated by torch
 on the stream of the call (``stream``, or torch's current one); a result given
 as ``out`` is written in place.  Rows must be contiguous; the stride between
 rows is free.
+
+Calls on the current stream that make their own results are checked and made in
+native code (csrc/ops_args.cpp, used with the torch it was built against); what
+is not plainly right there, and every other call, takes the checks below.
 """
 from __future__ import annotations
 
 import ctypes
+import os
 from typing import Optional
 
 import paper_2603_11438_amd as _ar
+
+OPS_ARGS_PATH = os.path.join(os.path.dirname(_ar.LIB_PATH), "_ops_args.so")
 
 AR_NORM_POST, AR_NORM_PRE = 1, 2
 AR_ACT_SILU, AR_ACT_GELU, AR_ACT_RELU = 0, 1, 2
@@ -68,6 +75,58 @@ def _lib() -> ctypes.CDLL:
             f.restype, f.argtypes = res, args
         _bound = L
     return _bound
+
+
+class _Native:
+    """The native call path and the addresses of the functions it calls."""
+
+    def __init__(self):
+        import importlib.util
+
+        import torch  # the extension's symbols come from torch's libraries
+
+        if not os.path.exists(OPS_ARGS_PATH):
+            raise ImportError(f"not built ({OPS_ARGS_PATH} missing); run __graft_entry__.build()")
+        spec = importlib.util.spec_from_file_location("_ops_args", OPS_ARGS_PATH)
+        mod = importlib.util.module_from_spec(spec)
+        spec.loader.exec_module(mod)
+        if mod.torch_version != str(torch.__version__):
+            # it reads torch's C++ objects as that version laid them out
+            raise ImportError(f"built against torch {mod.torch_version}, loaded is {torch.__version__}")
+        L = _lib()
+        address = lambda name: ctypes.cast(getattr(L, name), ctypes.c_void_p).value  # noqa: E731
+        self.norm, self.norm_backward, self.ffn, self.ffn_backward = mod.norm, mod.norm_backward, mod.ffn, mod.ffn_backward
+        self.norm_fn = address("ar_residual_norm")
+        self.norm_backward_fns = address("ar_residual_norm_backward"), address("ar_residual_norm_backward_workspace")
+        self.ffn_fns = address("ar_gated_ffn"), address("ar_gated_ffn_workspace")
+        self.ffn_backward_fns = address("ar_gated_ffn_backward"), address("ar_gated_ffn_backward_workspace")
+        self.in_use, self.device, self.stream = torch.cuda.is_initialized, torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream
+
+
+_native_path = None  # not looked for yet; False: cannot be used
+
+
+def _native() -> Optional[_Native]:
+    """The native call path, where there is a device context to call it in; None
+    (with a warning, once) where it cannot be used."""
+    global _native_path
+    if _native_path is None:
+        try:
+            _native_path = _Native()
+        except (ImportError, AttributeError) as e:  # AttributeError: a torch without devices
+            import warnings
+
+            warnings.warn(f"the native part of the operators' binding cannot be used: {e}; tensors are checked in Python, "
+                          "some 10 us per call", RuntimeWarning, stacklevel=3)
+            _native_path = False
+    return _native_path if _native_path and _native_path.in_use() else None
+
+
+def _done(got, what):
+    """The results of a native call; raises for a status."""
+    if type(got) is int:
+        _ar._check(got, what)
+    return got
 
 
 # ---- tensors ----------------------------------------------------------------
@@ -193,6 +252,12 @@ def residual_norm(y, residual, *, post_weight=None, pre_weight=None, gate=None, 
     s may be y or residual, and so may x."""
     import torch
 
+    if out is None and stream is None and (nat := _native()) is not None:
+        dev = nat.device()
+        got = nat.norm(nat.norm_fn, y, residual, post_weight, pre_weight, gate, alpha, eps,
+                       (AR_NORM_POST if post else 0) | (AR_NORM_PRE if pre else 0), dev, nat.stream(dev))
+        if got is not None:
+            return _done(got, "ar_residual_norm")
     with _On(y, stream) as on:
         d, _, (w1, g, w2) = _norm_desc(y, post_weight, pre_weight, gate, alpha, eps, post, pre)
         dev = on.index
@@ -227,6 +292,13 @@ def residual_norm_backward(y, s, ds, dx, *, post_weight=None, pre_weight=None, g
     in place of a new one (residual_norm_backward_workspace)."""
     import torch
 
+    if out is None and workspace is None and stream is None and (nat := _native()) is not None:
+        dev = nat.device()
+        got = nat.norm_backward(*nat.norm_backward_fns, y, s, ds, dx, post_weight, pre_weight, gate, alpha, eps,
+                                (AR_NORM_POST if post else 0) | (AR_NORM_PRE if pre else 0), param_grads, dev, nat.stream(dev))
+        if got is not None:
+            got = zip(("dy", "dresidual", "dpost_weight", "dpre_weight", "dgate"), _done(got, "ar_residual_norm_backward"))
+            return {k: t for k, t in got if t is not None}
     with _On(y, stream) as on:
         d, pdt, (w1, g, w2) = _norm_desc(y, post_weight, pre_weight, gate, alpha, eps, post, pre)
         dev = on.index
@@ -293,6 +365,12 @@ def gated_ffn(x, w_gate, w_up, *, act: str = "silu", save: bool = False, out=Non
     saved: (2, tokens, hidden) fp32, both projections."""
     import torch
 
+    if out is None and stream is None and act in ACTS and (nat := _native()) is not None:
+        dev = nat.device()
+        got = nat.ffn(*nat.ffn_fns, x, w_gate, w_up, ACTS[act], save, dev, nat.stream(dev))
+        if got is not None:
+            h, saved = _done(got, "ar_gated_ffn")
+            return (h, saved) if save else h
     with _On(x, stream) as on:
         d = _ffn_desc(x, w_gate, w_up, act)
         h = out
@@ -322,6 +400,11 @@ def gated_ffn_backward(dh, x, w_gate, w_up, saved, *, act: str = "silu", need_dx
     (gated_ffn_backward_workspace)."""
     import torch
 
+    if out is None and workspace is None and stream is None and act in ACTS and (nat := _native()) is not None:
+        dev = nat.device()
+        got = nat.ffn_backward(*nat.ffn_backward_fns, dh, x, w_gate, w_up, saved, ACTS[act], need_dx, need_dw, dev, nat.stream(dev))
+        if got is not None:
+            return _done(got, "ar_gated_ffn_backward")
     with _On(x, stream) as on:
         d = _ffn_desc(x, w_gate, w_up, act)
         dev = on.index

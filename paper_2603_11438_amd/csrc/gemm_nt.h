@@ -10,7 +10,7 @@
 // the same sums ([dG dU] times [Wg; Wu]).  Operands in two planes, hi and lo,
 // are multiplied as hi hi + hi lo + lo hi.
 //
-// A workgroup of four waves, one per SIMD, owns a tile; each wave holds MT x NT
+// A workgroup, mostly of four waves, one per SIMD, owns a tile; each wave holds MT x NT
 // accumulators of 32 x 32 in registers.  k advances in stages of BK through
 // BUFS LDS buffers.  Loads go from memory straight into LDS (16 bytes a lane).
 // Once every wave has read the last fragments of a buffer its next loads
@@ -212,16 +212,40 @@ constexpr int upto(int k, int steps, int things, int most)
     return n < most ? n : most;
 }
 
-// The shape of a workgroup's tile and pipeline: 2 x 2 waves of MT x NT blocks of
+// The shape of a workgroup's tile and pipeline: WM x 2 waves of MT x NT blocks of
 // 32 x 32, PLANES planes of each operand, k in stages of BK through BUFS buffers.
-template <int MT_, int NT_, int PLANES_, int BK_, int BUFS_> struct Shape {
+template <int MT_, int NT_, int PLANES_, int BK_, int BUFS_, int WM_ = 2> struct Shape {
     static constexpr int MT = MT_, NT = NT_, PLANES = PLANES_, BK = BK_, BUFS = BUFS_;
-    static constexpr int WM = 2, WN = 2, WAVES = WM * WN, THREADS = 64 * WAVES, BM = WM * MT * 32, BN = WN * NT * 32;
+    static constexpr int WM = WM_, WN = 2, WAVES = WM * WN, THREADS = 64 * WAVES, BM = WM * MT * 32, BN = WN * NT * 32;
     static constexpr int ROW = BK * 2;                        // bytes of a row in a buffer
     static constexpr int PLANE = (BM + BN) * ROW;             // A's rows, then B's
     static constexpr int BUF = PLANES * PLANE, LDS = BUFS * BUF;
     static_assert(BM * ROW % (1024 * WAVES) == 0 && BN * ROW % (1024 * WAVES) == 0, "whole loads");
 };
+
+// Makes the accumulators safe to read by take().  Nothing in the hardware holds
+// up a read of a register that a matrix instruction is still writing, and the
+// compiler, which otherwise counts the cycles in between, does not look into
+// take()'s instructions: the wait has to stand here (19 cycles at most), behind
+// every product, which the operands see to.
+template <int MT, int NT> __device__ __forceinline__ void settle(f32x16 (&acc)[MT][NT])
+{
+#pragma unroll
+    for (int i = 0; i < MT; ++i)
+#pragma unroll
+        for (int j = 0; j < NT; ++j) asm volatile("" : "+a"(acc[i][j]));
+    asm volatile("s_nop 15\n\ts_nop 7" : "+a"(acc[MT - 1][NT - 1]));
+}
+
+// A block row of the accumulators in ordinary registers.  The reads stay where
+// they are written: moved up as one, all accumulators together would not fit.
+template <int NT> __device__ __forceinline__ void take(const f32x16 (&acc)[NT], float (&v)[NT][16])
+{
+#pragma unroll
+    for (int j = 0; j < NT; ++j)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) asm volatile("v_accvgpr_read_b32 %0, %1" : "=v"(v[j][r]) : "a"(acc[j][r]));
+}
 
 // One operand of a tile: which of its bytes each lane loads, and where its
 // fragments lie in LDS.  R: rows (by rows) or columns (by k) of the tile; X:
@@ -477,16 +501,7 @@ __device__ __forceinline__ void gemm_tile(const GemmArgs &g, const TileAt at, ch
     }
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     __syncthreads();
-}
-
-// A block row of the accumulators in ordinary registers.  The reads stay where
-// they are written: moved up as one, all accumulators together would not fit.
-template <int NT> __device__ __forceinline__ void take(const f32x16 (&acc)[NT], float (&v)[NT][16])
-{
-#pragma unroll
-    for (int j = 0; j < NT; ++j)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) asm volatile("v_accvgpr_read_b32 %0, %1" : "=v"(v[j][r]) : "a"(acc[j][r]));
+    settle(acc);
 }
 
 // 32 rows of a wave's results in its own part of LDS, so that a row's bytes can

@@ -203,7 +203,7 @@ template <typename S> struct WaveAt {
     __device__ __forceinline__ WaveAt(const TileAt at)
     {
         const uint32_t lane = threadIdx.x & 63u, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-        row0 = at.m * S::BM + (wave >> 1) * S::MT * 32, col0 = at.n * S::BN + (wave & 1u) * S::NT * 32;
+        row0 = at.m * S::BM + wave / S::WN * S::MT * 32, col0 = at.n * S::BN + wave % S::WN * S::NT * 32;
         row = lane & 31u, half = (lane >> 5) * 4;
     }
     __device__ __forceinline__ uint32_t i(int bi) const { return row0 + bi * 32 + row; }
@@ -275,18 +275,19 @@ __global__ __launch_bounds__(S::THREADS) void ortho_square_kernel(const GemmArgs
     constexpr int NT = S::NT, PLANES = S::PLANES;
     extern __shared__ __attribute__((aligned(16))) char lds[];
     const TileAt at = tile_at_lower(g.tiles_m, g.batch);
-    f32x16 acc[S::MT][NT];
-    gemm_tile<f16, S, false>(g, at, lds, acc);
     const WaveAt<S> w(at);
     char *ws = o.ws + at.batch * o.at.bytes;
+    // what the epilogue begins with is on its way during the products
     const Scales s = ((const Scales *)(ws + o.at.scales))[o.step];
     float *diag_a = (float *)(ws + o.at.diag_a), *diag_b = (float *)(ws + o.at.diag_b);
-    const float sx = s.tau / s.x, ia = 1.0f / s.a, to = SECOND ? s.b : s.a;  // powers of two but for tau
     char *stage = lds + (threadIdx.x >> 6) * kOrthoStage<S>;
     char *hi = ws + (SECOND ? o.at.b : o.at.a);
     const size_t lo = SECOND ? o.at.b_lo : o.at.a_lo;
     Ahead<S, f16, PLANES> ahead{(const f16 *)(ws + o.at.a), o.at.a_lo, o.mp, o.mp, w.row0, w.col0, stage};
     if (SECOND) ahead.load(0);
+    f32x16 acc[S::MT][NT];
+    gemm_tile<f16, S, false>(g, at, lds, acc);
+    const float sx = s.tau / s.x, ia = 1.0f / s.a, to = SECOND ? s.b : s.a;  // powers of two but for tau
     static_for<S::MT>([&](auto block) {
         constexpr int bi = block.value;
         float v[NT][16];
@@ -334,27 +335,29 @@ __global__ __launch_bounds__(S::THREADS) void ortho_square_kernel(const GemmArgs
     });
 }
 
-// X = a X + B X; after the last step the result in the output's type.
+// X = a X + B X from the sums of B X (the off-diagonal B); after the last step the
+// result in the output's type.  stage: this wave's.
+// ahead: X's elements, begun before the products.
+template <typename S> using X = typename std::conditional<S::PLANES == 2, float, f16>::type;
+template <typename S> using XAhead = Ahead<S, X<S>, S::PLANES == 2 ? 1 : 2>;
+template <typename S> __device__ __forceinline__ XAhead<S> x_ahead(const TileAt at, const OrthoArgs &o, char *stage)
+{
+    const WaveAt<S> w(at);
+    const char *ws = o.ws + at.batch * o.at.bytes;
+    return XAhead<S>{(const X<S> *)(ws + (S::PLANES == 2 ? o.at.xf : o.at.x[o.step & 1u])), o.at.x_lo, o.mp, o.np, w.row0, w.col0, stage};
+}
 template <typename S, typename O>
-__global__ __launch_bounds__(S::THREADS) void ortho_update_kernel(const GemmArgs g, const OrthoArgs o)
+__device__ __forceinline__ void update(f32x16 (&acc)[S::MT][S::NT], const TileAt at, const OrthoArgs &o, const Scales s, const Scales next,
+                                       XAhead<S> &ahead, const float *diag_b)
 {
     constexpr int NT = S::NT, PLANES = S::PLANES;
-    extern __shared__ __attribute__((aligned(16))) char lds[];
-    const TileAt at = tile_at(g.tiles_m, g.tiles_n, g.batch);
-    f32x16 acc[S::MT][NT];
-    gemm_tile<f16, S, false, false, true>(g, at, lds, acc);
+    char *stage = ahead.lds;
     const WaveAt<S> w(at);
     char *ws = o.ws + at.batch * o.at.bytes;
-    const Scales s = ((const Scales *)(ws + o.at.scales))[o.step], next = ((const Scales *)(ws + o.at.scales))[o.step + 1];
-    const float *diag_b = (const float *)(ws + o.at.diag_b);
     const bool last = o.step + 1 == o.steps;
     const float to = last ? o.scale : next.x, ib = 1.0f / s.b, ix = s.tau / s.x;
     // X's planes are read by other tiles too, so they alternate; its fp32 values are not.
-    char *stage = lds + (threadIdx.x >> 6) * kOrthoStage<S>;
     char *x_next = ws + o.at.x[(o.step + 1) & 1u];
-    typedef typename std::conditional<PLANES == 2, float, f16>::type X;
-    Ahead<S, X, PLANES == 2 ? 1 : 2> ahead{(const X *)(ws + (PLANES == 2 ? o.at.xf : o.at.x[o.step & 1u])), o.at.x_lo, o.mp, o.np, w.row0, w.col0, stage};
-    ahead.load(0);
     O *out = (O *)o.out + at.batch * o.stride_out;
     static_for<S::MT>([&](auto block) {
         constexpr int bi = block.value;
@@ -395,6 +398,176 @@ __global__ __launch_bounds__(S::THREADS) void ortho_update_kernel(const GemmArgs
             }
         }
     });
+}
+
+template <typename S, typename O>
+__global__ __launch_bounds__(S::THREADS) void ortho_update_kernel(const GemmArgs g, const OrthoArgs o)
+{
+    extern __shared__ __attribute__((aligned(16))) char lds[];
+    const TileAt at = tile_at(g.tiles_m, g.tiles_n, g.batch);
+    const Scales *scales = (const Scales *)(o.ws + at.batch * o.at.bytes + o.at.scales);
+    const Scales s = scales[o.step], next = scales[o.step + 1];
+    XAhead<S> ahead = x_ahead<S>(at, o, lds + (threadIdx.x >> 6) * kOrthoStage<S>);
+    ahead.load(0);
+    f32x16 acc[S::MT][S::NT];
+    gemm_tile<f16, S, false, false, true>(g, at, lds, acc);
+    update<S, O>(acc, at, o, s, next, ahead, (const float *)(o.ws + at.batch * o.at.bytes + o.at.diag_b));
+}
+
+// A whole step of a small matrix (at most 128 rows) in one kernel: every
+// workgroup computes A and B for itself, keeps their planes in LDS, and updates
+// 64 columns of X.  Launches are what small matrices spend their time on (128 x
+// 384 fp32: a step as three kernels 20 us); the repeated products cost less.
+typedef Shape<1, 2, 2, 64, 2, 4> SmallSquare;  // eight waves: they hide each other's waits
+typedef Shape<1, 1, 2, 64, 2, 4> SmallUpdate;
+constexpr uint32_t kSmallRows = 128, kSmallBlock = kSmallRows * 128, kSmallPlane = 2 * kSmallBlock;  // k = 64 of a plane; a plane
+constexpr uint32_t kSmallX = 2 * kSmallPlane, kSmallStage = kSmallX + 2 * kSmallBlock;  // X's 64 columns; the epilogue
+constexpr uint32_t kSmallDiag = kSmallStage + 8 * kOrthoStage<SmallUpdate> > SmallSquare::LDS ? kSmallStage + 8 * kOrthoStage<SmallUpdate> : SmallSquare::LDS;
+constexpr uint32_t kSmallLds = kSmallDiag + 2 * kSmallRows * 4;
+static_assert(kSmallStage + 8 * kOrthoStage<SmallUpdate> <= kSmallLds - 2 * kSmallRows * 4, "the stages fit");
+
+template <typename O> __global__ __launch_bounds__(512) void ortho_step_kernel(const GemmArgs g, const OrthoArgs o)
+{
+    extern __shared__ __attribute__((aligned(16))) char lds[];
+    float *diag_a = (float *)(lds + kSmallDiag), *diag_b = diag_a + kSmallRows;
+    const uint32_t tiles = o.np / 64, lane = threadIdx.x & 63u, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const TileAt at{blockIdx.x / tiles, 0, blockIdx.x % tiles};
+    char *ws = o.ws + at.batch * o.at.bytes;
+    const Scales s = ((const Scales *)(ws + o.at.scales))[o.step], following = ((const Scales *)(ws + o.at.scales))[o.step + 1];
+    const WaveAt<SmallSquare> w(TileAt{at.batch, 0, 0});
+    XAhead<SmallUpdate> ahead = x_ahead<SmallUpdate>(at, o, lds + kSmallStage + wave * kOrthoStage<SmallUpdate>);
+    ahead.load(0);
+    // where the planes' element (row, column) lies: rows of 64 columns, chunks swizzled as the products read them
+    auto place = [&](uint32_t row, uint32_t col) { return col / 64 * kSmallBlock + row * 128 + ((col % 64 / 8) ^ (row >> 1 & 7u)) * 16 + col % 8 * 2; };
+    typedef f16 f16x4 __attribute__((ext_vector_type(4)));
+
+    f32x16 acc[1][2];
+    gemm_tile<f16, SmallSquare, false>(g, TileAt{at.batch, 0, 0}, lds, acc);
+
+    // X's columns on their way while A and B are made: 128 rows by k, both planes
+    {
+        const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)lds + kSmallX;
+        Side<SmallUpdate, true, 64> side;  // 64 rows a buffer: two of them
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+            side.place(wave, at.n * 64, o.np, [&](uint32_t row, uint32_t) { return row * o.np * 2; });
+            if (half * 64u >= o.mp) side.stop_at(wave, 0);
+#pragma unroll
+            for (int plane = 0; plane < 2; ++plane) {
+                const u32x4v from = tile_resource(uniform_address(ws + o.at.x[o.step & 1u] + plane * o.at.x_lo + (size_t)half * 64 * o.np * 2 + at.n * 128));
+#pragma unroll
+                for (int n = 0; n < side.LOADS; ++n)
+                    load_to_lds(lds0 + plane * kSmallBlock + half * (kSmallBlock / 2) + (n * 8 + wave) * 1024, side.off[n], from, 0);
+            }
+        }
+    }
+
+    // The sums scaled by `to` become the planes; the diagonal goes to its vector.
+    auto keep = [&](float (&v)[2][16], float *diag, float to, float of_diag) {
+        const uint32_t i = w.i(0);
+#pragma unroll
+        for (int bj = 0; bj < 2; ++bj)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const uint32_t j0 = w.j(bj, q * 4);
+                f16x4 h, l;
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    float x = i < o.m && j0 + k < o.m ? v[bj][q * 4 + k] : 0.0f;
+                    if (j0 + k == i) {
+                        diag[i] = x + of_diag;
+                        x = 0.0f;
+                    }
+                    x *= to;
+                    h[k] = (f16)x, l[k] = (f16)(x - (float)h[k]);
+                }
+                *(f16x4 *)(lds + place(i, j0)) = h;
+                *(f16x4 *)(lds + kSmallPlane + place(i, j0)) = l;
+            }
+    };
+    const float sx = s.tau / s.x, ia = 1.0f / s.a;
+    float v[2][16];
+    take(acc[0], v);
+#pragma unroll
+    for (int bj = 0; bj < 2; ++bj)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) v[bj][r] = v[bj][r] * sx * sx;
+    keep(v, diag_a, s.a, 0.0f);
+    __syncthreads();
+
+    // Fragments of the planes: row l%32 from `row0` on, k = 16 * quarter + 8 * (l/32) + 0..7.
+    const uint32_t fr = lane & 31u, fc = lane >> 5;
+    auto rows = [&](int plane, uint32_t row0, int quarter) {
+        return *(const f16x8 *)(lds + plane * kSmallPlane + quarter / 4 * kSmallBlock + (row0 + fr) * 128 +
+                                ((2 * (quarter % 4) + fc) ^ (fr >> 1 & 7u)) * 16);
+    };
+    const uint32_t wm = wave / 2, wn = wave % 2;
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) acc[0][j][r] = 0.0f;
+    static_for<8>([&](auto quarter) {
+        f16x8 a[2], b[2][2];
+#pragma unroll
+        for (int plane = 0; plane < 2; ++plane) {
+            a[plane] = rows(plane, wm * 32, quarter.value);
+#pragma unroll
+            for (int j = 0; j < 2; ++j) b[plane][j] = rows(plane, wn * 64 + j * 32, quarter.value);
+        }
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            acc[0][j] = Frag<f16>::mfma(b[0][j], a[0], acc[0][j]);
+            acc[0][j] = Frag<f16>::mfma(b[1][j], a[0], acc[0][j]);
+            acc[0][j] = Frag<f16>::mfma(b[0][j], a[1], acc[0][j]);
+        }
+    });
+    settle(acc);
+    // b A + c A A, with A's elements from the planes, before those make room
+    take(acc[0], v);
+    const float di = diag_a[w.i(0)];
+#pragma unroll
+    for (int bj = 0; bj < 2; ++bj)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            const uint32_t at_ij = place(w.i(0), w.j(bj, q * 4));
+            const f16x4 h = *(const f16x4 *)(lds + at_ij), l = *(const f16x4 *)(lds + kSmallPlane + at_ij);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const float t = ((float)h[k] + (float)l[k]) * ia;  // zero on the diagonal
+                v[bj][q * 4 + k] = o.b * t + o.c * (v[bj][q * 4 + k] * ia * ia + (di + diag_a[w.j(bj, q * 4 + k)]) * t);
+            }
+        }
+    __syncthreads();
+    keep(v, diag_b, s.b, o.b * di + o.c * di * di);
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // X's columns
+    __syncthreads();
+
+    // B X: 32 rows and 32 columns a wave
+    f32x16 sums[1][1];
+#pragma unroll
+    for (int r = 0; r < 16; ++r) sums[0][0][r] = 0.0f;
+    const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)lds;
+    typedef Side<SmallUpdate, true, 64> SideX;
+    const uint32_t tk = 8 * fc + (lane & 15u) / 4, tc = 2 * (lane >> 4 & 1u) + (lane >> 1 & 1u);
+    const uint32_t col = tk * 128 + (wn * 4 + tc + SideX::turn(tk)) % 8 * 16 + (lane & 1u) * 8;
+    static_for<8>([&](auto quarter) {
+        f16x8 a[2], b[2];
+        typedef short s16x4 __attribute__((ext_vector_type(4)));
+        typedef __attribute__((address_space(3))) s16x4 *P;
+#pragma unroll
+        for (int plane = 0; plane < 2; ++plane) {
+            a[plane] = rows(plane, wm * 32, quarter.value);
+            const uint32_t from = lds0 + kSmallX + plane * kSmallBlock + quarter.value * 16 * 128 + col;
+            const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((P)(uintptr_t)from);
+            const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((P)(uintptr_t)(from + 4 * 128));
+            b[plane] = __builtin_bit_cast(f16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+        }
+        sums[0][0] = Frag<f16>::mfma(b[0], a[0], sums[0][0]);
+        sums[0][0] = Frag<f16>::mfma(b[1], a[0], sums[0][0]);
+        sums[0][0] = Frag<f16>::mfma(b[0], a[1], sums[0][0]);
+    });
+    settle(sums);
+    update<SmallUpdate, O>(sums, at, o, s, following, ahead, diag_b);
 }
 
 }  // namespace dev
@@ -523,7 +696,7 @@ template <typename S, typename O> int launch_update(GemmArgs &g, const OrthoArgs
     hipLaunchKernelGGL((ortho_update_kernel<S, O>), dim3(g.tiles_m * g.tiles_n * o.batch), dim3(S::THREADS), kOrthoLds<S>, st, g, o);
     return launch_status();
 }
-template <int PLANES, typename O> int update(GemmArgs &g, const OrthoArgs &o, hipStream_t st)
+template <int PLANES, typename O> int update_step(GemmArgs &g, const OrthoArgs &o, hipStream_t st)
 {
     switch (cut_for(PLANES, o.m, o.n, g.steps, o.batch, false, 0, 3, 1).tile) {
     case 0: return launch_update<typename ShapeOf<PLANES, 0>::type, O>(g, o, st);
@@ -551,16 +724,28 @@ template <typename O, int PLANES> int run_ortho(OrthoArgs &o, const float *coefs
     if (rc != AR_OK) return rc;
     hipLaunchKernelGGL((ortho_enter_kernel<O, PLANES>), dim3(o.np / 64, o.mp / 64, o.batch), dim3(256), 0, st, o);
     if ((rc = launch_status()) != AR_OK) return rc;
+    // One kernel a step for short rows of few columns: beyond about 1024 the
+    // repeated A costs more than the launches.
+    const bool small = PLANES == 2 && o.mp <= kSmallRows && o.np <= 1024;
     for (o.step = 0; o.step < o.steps; ++o.step) {
         o.a = coefs[3 * o.step], o.b = coefs[3 * o.step + 1], o.c = coefs[3 * o.step + 2];
         GemmArgs g;
         const size_t x = o.at.x[o.step & 1u];
         operands(&g, o, x, o.at.x_lo, o.np, x, o.at.x_lo, o.np, o.np, o.m, o.m);
+        if constexpr (PLANES == 2) {
+            if (small) {
+                static const hipError_t set = hipFuncSetAttribute((const void *)ortho_step_kernel<O>, hipFuncAttributeMaxDynamicSharedMemorySize, kSmallLds);
+                if (set != hipSuccess) return AR_ERR_HIP;
+                hipLaunchKernelGGL((ortho_step_kernel<O>), dim3(o.np / 64 * o.batch), dim3(512), kSmallLds, st, g, o);
+                if ((rc = launch_status()) != AR_OK) return rc;
+                continue;
+            }
+        }
         if ((rc = square<PLANES, false>(g, o, st)) != AR_OK) return rc;
         operands(&g, o, o.at.a, o.at.a_lo, o.mp, o.at.a, o.at.a_lo, o.mp, o.mp, o.m, o.m);
         if ((rc = square<PLANES, true>(g, o, st)) != AR_OK) return rc;
         operands(&g, o, o.at.b, o.at.b_lo, o.mp, x, o.at.x_lo, o.np, o.mp, o.m, o.np);
-        if ((rc = update<PLANES, O>(g, o, st)) != AR_OK) return rc;
+        if ((rc = update_step<PLANES, O>(g, o, st)) != AR_OK) return rc;
     }
     return AR_OK;
 }

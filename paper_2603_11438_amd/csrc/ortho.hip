@@ -39,7 +39,7 @@ struct Scales {
 
 // One matrix' part of the workspace, in bytes.
 struct OrthoSpace {
-    size_t x[2], x_lo, xf, a, a_lo, b, b_lo, diag_a, diag_b, scales, norms, bytes;
+    size_t x[2], x_lo, xf, a, a_lo, b, b_lo, diag_a, diag_b, part, scales, norms, bytes;
 };
 
 struct OrthoArgs {
@@ -266,73 +266,136 @@ template <typename S> constexpr int kOrthoStage = kStageColBytes<float, S::NT * 
                                                       ? kStageColBytes<float, S::NT * 32> : 2 * kStageBytes<f16, S::NT * 32>;
 template <typename S> constexpr int kOrthoLds = S::LDS > 4 * kOrthoStage<S> ? S::LDS : 4 * kOrthoStage<S>;
 
+// 32 rows of A (SECOND false) or B from their sums: written to both places; the
+// diagonal goes to its fp32 vector and is zero in the planes.
+template <typename S, bool SECOND, typename A>
+__device__ __forceinline__ void square_rows(float (&v)[S::NT][16], int bi, const TileAt at, const WaveAt<S> &w, const OrthoArgs &o,
+                                            const Scales &s, A &ahead, char *stage)
+{
+    constexpr int NT = S::NT, PLANES = S::PLANES;
+    char *ws = o.ws + at.batch * o.at.bytes;
+    float *diag_a = (float *)(ws + o.at.diag_a), *diag_b = (float *)(ws + o.at.diag_b);
+    const float sx = s.tau / s.x, ia = 1.0f / s.a, to = SECOND ? s.b : s.a;  // powers of two but for tau
+    const uint32_t i = w.i(bi);
+    const float di = SECOND && i < o.m ? diag_a[i] : 0.0f;
+    if constexpr (SECOND) ahead.stage(bi);
+#pragma unroll
+    for (int bj = 0; bj < NT; ++bj)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            const uint32_t j0 = w.j(bj, q * 4);
+            float off[4] = {0.0f, 0.0f, 0.0f, 0.0f}, dj[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+            if constexpr (SECOND) {
+                if (j0 < o.mp) load_vec<float, 4>(diag_a + j0, dj);
+                ahead.take(bj, q, off);
+            }
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const uint32_t j = j0 + k;
+                float x = v[bj][q * 4 + k];
+                if (!SECOND) {
+                    x = x * sx * sx;
+                } else {
+                    const float t = off[k] * ia;
+                    x = o.b * t + o.c * (x * ia * ia + (di + dj[k]) * t);
+                }
+                v[bj][q * 4 + k] = i < o.m && j < o.m ? x * to : 0.0f;
+            }
+        }
+    if (at.m == at.n) {
+        // the diagonal goes to its vector (off and dj are zero there)
+#pragma unroll
+        for (int bj = 0; bj < NT; ++bj)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                if (w.j(bj, r) != i) continue;
+                if (i < o.m) (SECOND ? diag_b : diag_a)[i] = SECOND ? o.b * di + v[bj][r] / to + o.c * di * di : v[bj][r] / to;
+                v[bj][r] = 0.0f;
+            }
+    }
+    char *hi = ws + (SECOND ? o.at.b : o.at.a);
+    const size_t lo = SECOND ? o.at.b_lo : o.at.a_lo;
+    const uint32_t first = w.row0 + bi * 32;
+    if (at.m != at.n) store_planes<S, PLANES, true>(stage, v, first, w.col0, hi, lo, o.mp, o.mp);
+    else store_planes<S, PLANES, false>(stage, v, first, w.col0, hi, lo, o.mp, o.mp);
+}
+
+// Where a wave's sums of one run of k go: blocks in turn, each four vectors of
+// four elements a lane, as the accumulators hold them.
+template <typename S> __device__ __forceinline__ float *run_sums(const OrthoArgs &o, const TileAt at, uint32_t tiles, uint32_t split)
+{
+    const uint64_t tile = (uint64_t)split * (tiles * (tiles + 1) / 2) + at.m * (at.m + 1) / 2 + at.n;
+    return (float *)(o.ws + at.batch * o.at.bytes + o.at.part) + (tile * S::WAVES + (threadIdx.x >> 6)) * (S::MT * S::NT * 1024) +
+           (threadIdx.x & 63u) * 4;
+}
+
 // A = X X^T (SECOND false) or B = b A + c A A (true): tiles on and below the
-// diagonal, written to both places; the diagonal goes to its fp32 vector and
-// is zero in the planes.
+// diagonal.  A of short rows is split over its long k: the runs' sums go to
+// the workspace, for ortho_join_kernel.
 template <typename S, bool SECOND>
 __global__ __launch_bounds__(S::THREADS) void ortho_square_kernel(const GemmArgs g, const OrthoArgs o)
 {
     constexpr int NT = S::NT, PLANES = S::PLANES;
     extern __shared__ __attribute__((aligned(16))) char lds[];
-    const TileAt at = tile_at_lower(g.tiles_m, g.batch);
+    const TileAt at = tile_at_lower(g.tiles_m, g.batch, g.splits);
     const WaveAt<S> w(at);
-    char *ws = o.ws + at.batch * o.at.bytes;
+    const char *ws = o.ws + at.batch * o.at.bytes;
     // what the epilogue begins with is on its way during the products
     const Scales s = ((const Scales *)(ws + o.at.scales))[o.step];
-    float *diag_a = (float *)(ws + o.at.diag_a), *diag_b = (float *)(ws + o.at.diag_b);
     char *stage = lds + (threadIdx.x >> 6) * kOrthoStage<S>;
-    char *hi = ws + (SECOND ? o.at.b : o.at.a);
-    const size_t lo = SECOND ? o.at.b_lo : o.at.a_lo;
     Ahead<S, f16, PLANES> ahead{(const f16 *)(ws + o.at.a), o.at.a_lo, o.mp, o.mp, w.row0, w.col0, stage};
     if (SECOND) ahead.load(0);
     f32x16 acc[S::MT][NT];
     gemm_tile<f16, S, false>(g, at, lds, acc);
-    const float sx = s.tau / s.x, ia = 1.0f / s.a, to = SECOND ? s.b : s.a;  // powers of two but for tau
+    if (!SECOND && g.splits > 1) {
+        float *to = run_sums<S>(o, at, g.tiles_m, at.split);
+        static_for<S::MT>([&](auto block) {
+            float v[NT][16];
+            take(acc[block.value], v);
+#pragma unroll
+            for (int bj = 0; bj < NT; ++bj)
+#pragma unroll
+                for (int q = 0; q < 4; ++q) store_vec<float, 4>(to + ((block.value * NT + bj) * 4 + q) * 256, &v[bj][q * 4]);
+        });
+        return;
+    }
     static_for<S::MT>([&](auto block) {
-        constexpr int bi = block.value;
         float v[NT][16];
-        take(acc[bi], v);
-        const uint32_t i = w.i(bi);
-        const float di = SECOND && i < o.m ? diag_a[i] : 0.0f;
-        if (SECOND) ahead.stage(bi);
+        take(acc[block.value], v);
+        square_rows<S, SECOND>(v, block.value, at, w, o, s, ahead, stage);
+    });
+}
+
+// A from the runs' sums, added in their order; a workgroup has one block row of
+// each wave's.
+template <typename S> __global__ __launch_bounds__(S::THREADS) void ortho_join_kernel(const GemmArgs g, const OrthoArgs o)
+{
+    constexpr int NT = S::NT;
+    extern __shared__ __attribute__((aligned(16))) char lds[];
+    const TileAt at = tile_at_lower(g.tiles_m, g.batch, 1);
+    const WaveAt<S> w(at);
+    const Scales s = ((const Scales *)(o.ws + at.batch * o.at.bytes + o.at.scales))[o.step];
+    const float *from = run_sums<S>(o, at, g.tiles_m, 0) + blockIdx.y * NT * 1024;
+    const uint64_t run = run_sums<S>(o, at, g.tiles_m, 1) - run_sums<S>(o, at, g.tiles_m, 0);
+    float v[NT][16];
+#pragma unroll
+    for (int bj = 0; bj < NT; ++bj)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) v[bj][r] = 0.0f;
+#pragma unroll 4
+    for (uint32_t split = 0; split < g.splits; ++split) {
 #pragma unroll
         for (int bj = 0; bj < NT; ++bj)
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
-                const uint32_t j0 = w.j(bj, q * 4);
-                float off[4] = {0.0f, 0.0f, 0.0f, 0.0f}, dj[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-                if (SECOND) {
-                    if (j0 < o.mp) load_vec<float, 4>(diag_a + j0, dj);
-                    ahead.take(bj, q, off);
-                }
+                float x[4];
+                load_vec<float, 4>(from + split * run + (bj * 4 + q) * 256, x);
 #pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    const uint32_t j = j0 + k;
-                    float x = v[bj][q * 4 + k];
-                    if (!SECOND) {
-                        x = x * sx * sx;
-                    } else {
-                        const float t = off[k] * ia;
-                        x = o.b * t + o.c * (x * ia * ia + (di + dj[k]) * t);
-                    }
-                    v[bj][q * 4 + k] = i < o.m && j < o.m ? x * to : 0.0f;
-                }
+                for (int k = 0; k < 4; ++k) v[bj][q * 4 + k] += x[k];
             }
-        if (at.m == at.n) {
-            // the diagonal goes to its vector (off and dj are zero there)
-#pragma unroll
-            for (int bj = 0; bj < NT; ++bj)
-#pragma unroll
-                for (int r = 0; r < 16; ++r) {
-                    if (w.j(bj, r) != i) continue;
-                    if (i < o.m) (SECOND ? diag_b : diag_a)[i] = SECOND ? o.b * di + v[bj][r] / to + o.c * di * di : v[bj][r] / to;
-                    v[bj][r] = 0.0f;
-                }
-        }
-        const uint32_t first = w.row0 + bi * 32;
-        if (at.m != at.n) store_planes<S, PLANES, true>(stage, v, first, w.col0, hi, lo, o.mp, o.mp);
-        else store_planes<S, PLANES, false>(stage, v, first, w.col0, hi, lo, o.mp, o.mp);
-    });
+    }
+    int none = 0;
+    square_rows<S, false>(v, (int)blockIdx.y, at, w, o, s, none, lds + (threadIdx.x >> 6) * kOrthoStage<S>);
 }
 
 // X = a X + B X from the sums of B X (the off-diagonal B); after the last step the
@@ -431,10 +494,10 @@ template <typename O> __global__ __launch_bounds__(512) void ortho_step_kernel(c
     extern __shared__ __attribute__((aligned(16))) char lds[];
     float *diag_a = (float *)(lds + kSmallDiag), *diag_b = diag_a + kSmallRows;
     const uint32_t tiles = o.np / 64, lane = threadIdx.x & 63u, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const TileAt at{blockIdx.x / tiles, 0, blockIdx.x % tiles};
+    const TileAt at{blockIdx.x / tiles, 0, blockIdx.x % tiles, 0};
     char *ws = o.ws + at.batch * o.at.bytes;
     const Scales s = ((const Scales *)(ws + o.at.scales))[o.step], following = ((const Scales *)(ws + o.at.scales))[o.step + 1];
-    const WaveAt<SmallSquare> w(TileAt{at.batch, 0, 0});
+    const WaveAt<SmallSquare> w(TileAt{at.batch, 0, 0, 0});
     XAhead<SmallUpdate> ahead = x_ahead<SmallUpdate>(at, o, lds + kSmallStage + wave * kOrthoStage<SmallUpdate>);
     ahead.load(0);
     // where the planes' element (row, column) lies: rows of 64 columns, chunks swizzled as the products read them
@@ -442,7 +505,7 @@ template <typename O> __global__ __launch_bounds__(512) void ortho_step_kernel(c
     typedef f16 f16x4 __attribute__((ext_vector_type(4)));
 
     f32x16 acc[1][2];
-    gemm_tile<f16, SmallSquare, false>(g, TileAt{at.batch, 0, 0}, lds, acc);
+    gemm_tile<f16, SmallSquare, false>(g, TileAt{at.batch, 0, 0, 0}, lds, acc);
 
     // X's columns on their way while A and B are made: 128 rows by k, both planes
     {
@@ -635,10 +698,17 @@ bool two_planes(const ar_ortho_desc &d)
     return d.dtype == AR_FLOAT32 || (d.rows < d.cols ? d.rows : d.cols) <= 256;
 }
 
+// The tiles of A and the runs that its k is split into.
+constexpr uint32_t kMostRuns = 32;
+Cut cut_of_a(int planes, size_t m, size_t np, size_t batch) { return cut_for(planes, m, m, np / kStepK, batch, true, 0, 3, kMostRuns); }
+
 OrthoSpace ortho_space(const ar_ortho_desc &d, uint32_t mp, uint32_t np)
 {
     OrthoSpace s{};
     const bool two = two_planes(d);
+    const size_t m = d.rows < d.cols ? d.rows : d.cols;
+    const Cut c = cut_of_a(two ? 2 : 1, m, np, d.batch);
+    const size_t side = kTiles[0][c.tile].side, tiles = (m + side - 1) / side;
     size_t at = 0;
     auto take = [&](size_t bytes) {
         const size_t here = at;
@@ -650,6 +720,7 @@ OrthoSpace ortho_space(const ar_ortho_desc &d, uint32_t mp, uint32_t np)
     s.a = take(two ? 2 * sq : sq), s.b = take(two ? 2 * sq : sq);
     s.x_lo = x, s.a_lo = s.b_lo = sq;
     s.diag_a = take(mp * 4), s.diag_b = take(mp * 4);
+    s.part = take(c.splits > 1 ? c.splits * (tiles * (tiles + 1) / 2) * side * side * 4 : 0);
     s.scales = take(sizeof(Scales) * (AR_ORTHO_MAX_STEPS + 1));
     s.norms = take(sizeof(double) * kNormParts);
     s.bytes = at;
@@ -674,12 +745,20 @@ template <typename S, bool SECOND> int launch_square(GemmArgs &g, const OrthoArg
                                                       hipFuncAttributeMaxDynamicSharedMemorySize, kOrthoLds<S>);
     if (set != hipSuccess) return AR_ERR_HIP;
     const uint32_t tiles = g.tiles_m * (g.tiles_m + 1) / 2 * o.batch;
-    hipLaunchKernelGGL((ortho_square_kernel<S, SECOND>), dim3(tiles), dim3(S::THREADS), kOrthoLds<S>, st, g, o);
+    hipLaunchKernelGGL((ortho_square_kernel<S, SECOND>), dim3(tiles * g.splits), dim3(S::THREADS), kOrthoLds<S>, st, g, o);
+    const int rc = launch_status();
+    if (rc != AR_OK || SECOND || g.splits == 1) return rc;
+    constexpr int LDS = S::WAVES * kOrthoStage<S>;
+    static const hipError_t also = hipFuncSetAttribute((const void *)ortho_join_kernel<S>, hipFuncAttributeMaxDynamicSharedMemorySize, LDS);
+    if (also != hipSuccess) return AR_ERR_HIP;
+    hipLaunchKernelGGL((ortho_join_kernel<S>), dim3(tiles, S::MT), dim3(S::THREADS), LDS, st, g, o);
     return launch_status();
 }
 template <int PLANES, bool SECOND> int square(GemmArgs &g, const OrthoArgs &o, hipStream_t st)
 {
-    switch (cut_for(PLANES, o.m, o.m, g.steps, o.batch, true, 0, 3, 1).tile) {
+    const Cut c = SECOND ? cut_for(PLANES, o.m, o.m, g.steps, o.batch, true, 0, 3, 1) : cut_of_a(PLANES, o.m, o.np, o.batch);
+    g.splits = c.splits;
+    switch (c.tile) {
     case 0: return launch_square<typename ShapeOf<PLANES, 0>::type, SECOND>(g, o, st);
     case 1: return launch_square<typename ShapeOf<PLANES, 1>::type, SECOND>(g, o, st);
     case 2: return launch_square<typename ShapeOf<PLANES, 2>::type, SECOND>(g, o, st);

@@ -153,3 +153,15 @@ def test_same_bits_stream_and_graph():
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(got, want), k
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("m,n", [(256, 4096), (130, 1999), (300, 5001), (2500, 270), (700, 6000)])
+def test_long_k(m, n, dtype):
+    """Short rows: the first product is split over the long side and joined."""
+    say("long k", m, n, dtype)
+    x = torch.stack([make("normal", m, n, 1), make("decades", m, n, 2)]).to(TORCH[dtype]).cuda()
+    got = ar.orthogonalize(x)
+    for g, w in zip(got, x):
+        check(g, w)
+    assert torch.equal(got, ar.orthogonalize(x)), "the runs are added in one order"

@@ -256,6 +256,7 @@ typedef Shape<4, 4, 1, 64, 2> Large;
 typedef Shape<3, 3, 1, 64, 2> Middle;
 typedef Shape<2, 2, 1, 64, 2> Small;
 typedef Shape<1, 1, 1, 64, 4> Tiny;
+typedef Shape<2, 2, 1, 64, 3> Deep;  // 128 x 128 alone on its compute unit
 typedef Shape<1, 2, 1, 64, 3> Flat;  // 64 tokens, both projections of 64 columns
 
 template <typename S, int ACT> int launch_ffn(GemmArgs &g, const FfnOut &o, hipStream_t st)
@@ -341,7 +342,7 @@ int ffn(const ar_ffn_desc *desc, const void *x, const void *wg, const void *wu, 
 constexpr uint32_t kMaxSplits = 32;
 size_t part_bytes(size_t m, size_t cols, size_t steps)
 {
-    const Cut c = cut_for(1, m, cols, steps, 1, false, 0, 3, kMaxSplits);
+    const Cut c = cut_for(1, m, cols, steps, 1, false, 0, 4, kMaxSplits);
     return c.splits > 1 ? round_up(c.splits * m * cols * sizeof(float), 256) : 0;
 }
 
@@ -363,13 +364,14 @@ template <typename S, bool ABYK> int launch_product(GemmArgs &g, const ProductOu
 // B by k; A by rows (dx) or by k (the weights' gradients).
 template <bool ABYK> int product(GemmArgs &g, const ProductOut &o, hipStream_t st)
 {
-    const Cut c = cut_for(1, g.m, o.cols, (size_t)g.steps * g.segments, 1, false, 0, 3, kMaxSplits);
+    const Cut c = cut_for(1, g.m, o.cols, (size_t)g.steps * g.segments, 1, false, 0, 4, kMaxSplits);
     g.splits = c.splits, g.batch = 1;
     switch (c.tile) {
     case 0: return launch_product<Tiny, ABYK>(g, o, st);
     case 1: return launch_product<Small, ABYK>(g, o, st);
     case 2: return launch_product<Middle, ABYK>(g, o, st);
-    default: return launch_product<Large, ABYK>(g, o, st);
+    case 3: return launch_product<Large, ABYK>(g, o, st);
+    default: return launch_product<Deep, ABYK>(g, o, st);
     }
 }
 

@@ -70,15 +70,18 @@ constexpr int kStepK = 64;  // steps that k is counted in
 // us for the same when one tile has the unit to itself (its loads' way to the
 // L2 and back is then in the open); `fit`: tiles that share a unit; `ends`: us
 // before and after the products.  Measured on products of 1024 x 1024 x 4096
-// (alone) and 8192 x 8192 x 8192 (busy).
+// (alone) and 8192 x 8192 x 8192 (busy).  The last one has three buffers, for a
+// tile alone on its unit: 768 x 1024 x 5376 in four runs 19.2 us, with two
+// buffers 23.7 and in 64 x 64 tiles 31.1; with two tiles to a unit it is slower
+// (5376 x 1024 x 768: 23.0 us, with two buffers 18.2).
 struct TileCost {
     int side;
     double busy, alone, ends;
     int fit;
 };
-constexpr int kTileSizes = 4;
+constexpr int kTileSizes = 5;
 constexpr TileCost kTiles[2][kTileSizes] = {
-    {{64, 0.19, 0.26, 2.5, 2}, {128, 0.5, 0.68, 5.0, 2}, {192, 1.1, 1.1, 12.0, 1}, {256, 1.67, 1.67, 20.0, 1}},
+    {{64, 0.19, 0.32, 2.5, 2}, {128, 0.5, 0.68, 5.0, 2}, {192, 1.1, 1.1, 12.0, 1}, {256, 1.67, 1.67, 20.0, 1}, {128, 0.5, 0.5, 5.0, 1}},
     {{64, 0.4, 0.45, 3.0, 1}, {128, 1.2, 1.3, 8.0, 1}, {192, 2.8, 2.8, 14.0, 1}, {256, 4.6, 4.6, 24.0, 1}},
 };
 

@@ -118,8 +118,9 @@ typedef struct ar_ffn_desc {
 } ar_ffn_desc;
 
 /* Forward, one kernel for both products, the activation and their product
- * (operands that are not laid out for it, by alignment or a dim that is no
- * multiple of 64, are first copied into the workspace).  saved: NULL, or
+ * (operands that it cannot read where they lie, not 16-byte aligned or with a
+ * dim or row stride that is no multiple of 8, are first copied into the
+ * workspace; without such operands none is needed).  saved: NULL, or
  * 2 * tokens * hidden floats (16-byte aligned) that receive G and U for the
  * backward pass, in fp32.  Errors: AR_ERR_ARG, AR_ERR_UNSUPPORTED,
  * AR_ERR_SCRATCH, AR_ERR_HIP. */

@@ -3,7 +3,15 @@
 //
 // Compute-bound with many tokens: one product kernel (gemm_nt.h) whose waves
 // hold both projections of the same columns, so that the activation and the
-// product happen in registers and only h is written.
+// product happen in registers and only h is written.  8192 x 4096 x 11264, silu:
+// 1240 us, 1220 TFLOP/s.  Bound by the weights' bytes with few: up to 64 tokens
+// share a tile of 64 columns of both, 1 x 4096 x 11264: 41 us, 4.5 TB/s.
+//
+// Backward: dG and dU by one pass over the saved projections (4096 x 11264: 125
+// us, 5.2 TB/s), dx as one product over both pairs of operands, both weights'
+// gradients as another, operands read by rows or by k where they lie.  Forward
+// with saved projections and backward, 4096 x 4096 x 11264: 2080 us, 1090
+// TFLOP/s; of that 720 the forward, 125, 590 dx and 640 the weights.
 #include <type_traits>
 
 #include "gemm_nt.h"
@@ -85,7 +93,7 @@ __global__ __launch_bounds__(256) void pack_kernel(const PackArgs p)
         const bf16 *from = p.from + row * p.ld + c;
         float v[8];
         if (c + 8 <= p.cols) load_vec<bf16, 8>(from, v);
-        else load_part<bf16, 8>(from, (int)(p.cols - c), v);
+        else load_part<bf16, 8>(from, (int)p.cols - (int)c, v);
         store_vec<bf16, 8>(p.to + row * p.to_ld + c, v);
     }
 }
@@ -228,7 +236,11 @@ bool direct(const Mat &m)
 {
     return (uintptr_t)m.p % 16 == 0 && m.ld % 8 == 0 && m.cols % 8 == 0 && gemm_reaches(m.ld * 2, m.cols * 2);
 }
-size_t packed_bytes(size_t rows, size_t cols) { return round_up(rows * round_up(cols, 8) * 2, 256); }
+// A copy's rows begin at 128 bytes: a load of 64 elements is one line of the
+// cache then, else two (64 to 66 bytes a ns to a compute unit instead of 125;
+// 2000 x 1999 x 5001 forward 120 us, with rows of whole 16 bytes alone 137).
+constexpr size_t kLine = 64;
+size_t packed_bytes(size_t rows, size_t cols) { return rows * round_up(cols, kLine) * 2; }
 
 // A matrix as the product kernel takes it: itself, or a copy in the workspace.
 struct Operand {
@@ -243,11 +255,11 @@ int pack(const Mat &m, bool as_is, char *&ws, hipStream_t st, Operand *out)
         *out = {m.p, (uint32_t)(m.ld * 2), (uint32_t)m.cols};
         return AR_OK;
     }
-    const size_t to_ld = round_up(m.cols, 8);
+    const size_t to_ld = round_up(m.cols, kLine);
     PackArgs p{(const bf16 *)m.p, (bf16 *)ws, m.rows, m.ld, to_ld, (uint32_t)m.cols};
     const uint64_t groups = (m.rows * (to_ld / 8) + 255) / 256;
     hipLaunchKernelGGL(pack_kernel, dim3((uint32_t)(groups < 8192 ? groups : 8192)), dim3(256), 0, st, p);
-    *out = {ws, (uint32_t)(to_ld * 2), (uint32_t)to_ld};
+    *out = {ws, (uint32_t)(to_ld * 2), (uint32_t)round_up(m.cols, 8)};
     ws += packed_bytes(m.rows, m.cols);
     return launch_status();
 }

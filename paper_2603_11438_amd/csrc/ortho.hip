@@ -20,6 +20,12 @@
 //
 // A and B are symmetric: only tiles on and below the diagonal are computed and
 // written to both places.  Tall matrices are transposed on the way in and out.
+//
+// Five steps of 4096 x 4096 bf16: 1580 us, 870 TFLOP/s (a step's A 83 us, B 89, X
+// 145, of which 40 the epilogue's bytes); six of 1410 x 700 bf16: 246 us; 1024 x
+// 4096 fp32: 395 us, 530 TFLOP/s of fp16 products; 128 x 384 fp32: 97 us.  The small
+// ones are bound by the LDS (a 64 x 64 tile's fragments take twice the cycles of
+// its products) and by launches.
 #include <type_traits>
 
 #include "gemm_nt.h"
@@ -480,7 +486,8 @@ __global__ __launch_bounds__(S::THREADS) void ortho_update_kernel(const GemmArgs
 // A whole step of a small matrix (at most 128 rows) in one kernel: every
 // workgroup computes A and B for itself, keeps their planes in LDS, and updates
 // 64 columns of X.  Launches are what small matrices spend their time on (128 x
-// 384 fp32: a step as three kernels 20 us); the repeated products cost less.
+// 384 fp32: a step as three kernels 20 us, as this one 17.5); the repeated
+// products cost less.
 typedef Shape<1, 2, 2, 64, 2, 4> SmallSquare;  // eight waves: they hide each other's waits
 typedef Shape<1, 1, 2, 64, 2, 4> SmallUpdate;
 constexpr uint32_t kSmallRows = 128, kSmallBlock = kSmallRows * 128, kSmallPlane = 2 * kSmallBlock;  // k = 64 of a plane; a plane

@@ -11,7 +11,7 @@
 // us, 5.2 TB/s), dx as one product over both pairs of operands, both weights'
 // gradients as another, operands read by rows or by k where they lie.  Forward
 // with saved projections and backward, 4096 x 4096 x 11264: 2080 us, 1090
-// TFLOP/s; of that 720 the forward, 125, 590 dx and 640 the weights.
+// TFLOP/s; a third of that the forward, a third the weights' gradients, 28 % dx.
 #include <type_traits>
 
 #include "gemm_nt.h"

@@ -409,6 +409,13 @@ FfnBackwardSpace ffn_backward_space(const ar_ffn_desc &d, bool dx, bool dw)
     return s;
 }
 
+// What a caller is asked for.  Pointers' alignment is not known before the call,
+// and what is wanted neither, so everything counts.
+size_t ffn_backward_bytes(const ar_ffn_desc &d)
+{
+    return ffn_backward_space(d, true, true).copies + 2 * packed_bytes(d.hidden, d.dim) + packed_bytes(d.tokens, d.dim);
+}
+
 __global__ void zero_rows_kernel(bf16 *p, uint64_t rows, uint64_t cols, uint64_t ld)
 {
     for (uint64_t i = (uint64_t)blockIdx.x * blockDim.x + threadIdx.x; i < rows * cols; i += (uint64_t)gridDim.x * blockDim.x)
@@ -444,10 +451,10 @@ int ffn_backward(const ar_ffn_desc *desc, const void *dh, const void *x, const v
     const FfnBackwardSpace s = ffn_backward_space(d, dx != nullptr, dwg != nullptr);
     // both weights are read with one row stride
     const bool w_direct = direct(m.wg) && direct(m.wu) && m.wg.ld == m.wu.ld, x_direct = direct(m.x);
-    size_t need = s.copies;
+    size_t need = s.copies;  // of this call
     if (dx && !w_direct) need += 2 * packed_bytes(d.hidden, d.dim);
     if (dwg && !x_direct) need += packed_bytes(d.tokens, d.dim);
-    if (!ws || ws_bytes < need) return AR_ERR_SCRATCH;
+    if (!ws || ws_bytes < ffn_backward_bytes(d)) return AR_ERR_SCRATCH;
     if ((uintptr_t)ws % 256 != 0) return AR_ERR_ARG;
     const Mat wsm{ws, 1, need, need, 1};
     for (const Mat &in : {m.x, m.wg, m.wu, m.h, sv, wsm})
@@ -506,10 +513,7 @@ extern "C" int ar_gated_ffn_backward(const ar_ffn_desc *desc, const void *dh, co
 
 extern "C" size_t ar_gated_ffn_backward_workspace(const ar_ffn_desc *desc)
 {
-    if (ar::check_ffn(desc) != AR_OK || !desc->tokens) return 0;
-    // pointers' alignment is not known before the call, so every copy counts
-    return ar::ffn_backward_space(*desc, true, true).copies + 2 * ar::packed_bytes(desc->hidden, desc->dim) +
-           ar::packed_bytes(desc->tokens, desc->dim);
+    return ar::check_ffn(desc) == AR_OK && desc->tokens ? ar::ffn_backward_bytes(*desc) : 0;
 }
 
 extern "C" int ar_gated_ffn(const ar_ffn_desc *desc, const void *x, const void *w_gate, const void *w_up, void *h,

@@ -9,11 +9,14 @@
 // consecutive rows: the weights and the gate stay in its registers, the next
 // row's loads are in flight while this one is summed, and the backward's
 // parameter gradients add up in registers and leave as one row of partial
-// sums per workgroup, which a second kernel adds in a fixed order.
+// sums per workgroup, which a second kernel adds in a fixed order.  Rows too wide
+// for all of that give up the next row first, then keep those sums in LDS.
 //
 // 16384 x 8192 bf16 forward 191 us, 5.6 TB/s (a large copy 5.2); 8192 x 4096 bf16
 // backward with parameter gradients 96 us, 4.2 TB/s; 2049 x 2501 fp32, rows that
 // begin at no vector's bound, 20 us, 4.1 TB/s; one row of 8192 3 us, a launch.
+// Wide rows backward: 2048 x 8192 fp32 93 us, 4.3 TB/s; 4096 x 12288 bf16 140 us,
+// 4.3 TB/s; 2048 x 12288 fp32 130 us, 4.7 TB/s.
 #include <type_traits>
 
 #include "ops_common.h"
@@ -275,7 +278,60 @@ __device__ __forceinline__ GateOut<P> gate_out(const NormBwdArgs &a, float *part
     return {nullptr, part + (size_t)(begin < first ? kPartGateHead : kPartGateTail) * a.cols};
 }
 
-template <typename T, typename P, int NV, int BS, bool TAIL>
+// Where a workgroup of wide rows finds registers: the next row is loaded only
+// when this one is done (kNoneAhead), and the parameter gradients add up in LDS,
+// each thread's in slots of its own, without barriers (kSumsInLds).
+enum Room { kNextAhead, kNoneAhead, kSumsInLds };
+
+// A parameter gradient's share of a thread.
+template <int VEC, int NV, int BS, bool LDS> struct ParamSum {
+    float v[NV][VEC];
+    __device__ __forceinline__ ParamSum(float *) { clear(); }
+    __device__ __forceinline__ void clear()
+    {
+#pragma unroll
+        for (int k = 0; k < NV; ++k)
+#pragma unroll
+            for (int j = 0; j < VEC; ++j) v[k][j] = 0.0f;
+    }
+    __device__ __forceinline__ void add(int k, const float *x)
+    {
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) v[k][j] += x[j];
+    }
+    template <typename O, bool TAIL> __device__ __forceinline__ void store(O *p, uint32_t cols) const
+    {
+        store_row<O, VEC, NV, BS, TAIL>(p, cols, v);
+    }
+};
+template <int VEC, int NV, int BS> struct ParamSum<VEC, NV, BS, true> {
+    static constexpr int N = NV * VEC / 4;  // vectors of four, those of all threads side by side
+    typedef float f32x4 __attribute__((ext_vector_type(4)));
+    f32x4 *at;
+    __device__ __forceinline__ ParamSum(float *lds) : at((f32x4 *)lds + threadIdx.x) { clear(); }
+    __device__ __forceinline__ void clear()
+    {
+#pragma unroll
+        for (int n = 0; n < N; ++n) at[n * BS] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    }
+    __device__ __forceinline__ void add(int k, const float *x)
+    {
+#pragma unroll
+        for (int n = 0; n < VEC / 4; ++n) at[(k * (VEC / 4) + n) * BS] += f32x4{x[n * 4], x[n * 4 + 1], x[n * 4 + 2], x[n * 4 + 3]};
+    }
+    template <typename O, bool TAIL> __device__ __forceinline__ void store(O *p, uint32_t cols) const
+    {
+        float v[NV][VEC];
+#pragma unroll
+        for (int n = 0; n < N; ++n)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) v[n / (VEC / 4)][n % (VEC / 4) * 4 + j] = at[n * BS][j];
+        store_row<O, VEC, NV, BS, TAIL>(p, cols, v);
+    }
+};
+template <typename T, int NV, int BS> constexpr int kSumsBytes = 3 * NV * kVec<T> * BS * 4;
+
+template <typename T, typename P, int NV, int BS, bool TAIL, Room ROOM = kNextAhead>
 __global__ __launch_bounds__(BS) void norm_bwd_kernel(const NormBwdArgs a)
 {
     constexpr int VEC = kVec<T>, W = BS / 64;
@@ -286,13 +342,12 @@ __global__ __launch_bounds__(BS) void norm_bwd_kernel(const NormBwdArgs a)
     if (first >= last) return;
     float *part = a.part + (size_t)blockIdx.x * kParts * a.cols;
     const float inv = 1.0f / (float)a.cols;
-    float w1[NV][VEC], w2[NV][VEC], g[NV][VEC], dw1[NV][VEC], dw2[NV][VEC], dg[NV][VEC];
+    extern __shared__ __attribute__((aligned(16))) float sums[];
+    typedef ParamSum<VEC, NV, BS, ROOM == kSumsInLds> Sum;
+    Sum dw1(sums), dw2(sums + NV * VEC * BS), dg(sums + 2 * NV * VEC * BS);
+    float w1[NV][VEC], w2[NV][VEC], g[NV][VEC];
     load_param<P, VEC, NV, BS, TAIL>(post ? a.post_w : nullptr, a.cols, w1);
     load_param<P, VEC, NV, BS, TAIL>(a.pre_w, a.cols, w2);
-#pragma unroll
-    for (int k = 0; k < NV; ++k)
-#pragma unroll
-        for (int j = 0; j < VEC; ++j) dw1[k][j] = dw2[k][j] = dg[k][j] = 0.0f;
     RawRow<T, NV> y, z, ds, dx, next_y, next_z, next_ds, next_dx;
     auto load_next = [&](uint64_t row) {
         load_raw<NV, BS, TAIL>((const T *)a.y + row * a.ld_y, a.cols, next_y);
@@ -301,16 +356,19 @@ __global__ __launch_bounds__(BS) void norm_bwd_kernel(const NormBwdArgs a)
         load_raw<NV, BS, TAIL>((const T *)a.ds + row * a.ld_ds, a.cols, next_ds);
         load_raw<NV, BS, TAIL>((const T *)a.dx + row * a.ld_dx, a.cols, next_dx);
     };
-    load_next(first);
+    if constexpr (ROOM == kNextAhead) load_next(first);
     uint64_t gate_end = 0;
     for (uint64_t row = first; row < last; ++row) {
+        if constexpr (ROOM != kNextAhead) load_next(row);
         if (row >= gate_end) {
             const uint64_t k = row / a.rows_per_gate;
             gate_end = (k + 1) * a.rows_per_gate;
             load_param<P, VEC, NV, BS, TAIL>(a.gate ? (const P *)a.gate + k * a.cols : nullptr, a.cols, g);
         }
         y = next_y, z = next_z, ds = next_ds, dx = next_dx;
-        if (row + 1 < last) load_next(row + 1);
+        if constexpr (ROOM == kNextAhead) {
+            if (row + 1 < last) load_next(row + 1);
+        }
         float sum[3] = {0.0f, 0.0f, 0.0f};
 #pragma unroll
         for (int k = 0; k < NV; ++k)
@@ -328,21 +386,25 @@ __global__ __launch_bounds__(BS) void norm_bwd_kernel(const NormBwdArgs a)
         const float c2 = r2 * r2 * (sum[2] * inv);
         float svy[1] = {0.0f}, out[NV][VEC], v[NV][VEC];
 #pragma unroll
-        for (int k = 0; k < NV; ++k)
+        for (int k = 0; k < NV; ++k) {
+            float of_w1[VEC], of_w2[VEC], of_g[VEC];
 #pragma unroll
             for (int j = 0; j < VEC; ++j) {
                 float G = a.has_ds ? ds.at(k, j) : 0.0f;
+                of_w2[j] = 0.0f;
                 if (pre) {
                     G += r2 * (dx.at(k, j) * w2[k][j] - z.at(k, j) * c2);
-                    dw2[k][j] += dx.at(k, j) * (z.at(k, j) * r2);
+                    of_w2[j] = dx.at(k, j) * (z.at(k, j) * r2);
                 }
                 const float unit = y.at(k, j) * r1, dn = G * g[k][j];
-                dg[k][j] += G * (unit * w1[k][j]);
-                dw1[k][j] += dn * unit;
+                of_g[j] = G * (unit * w1[k][j]);
+                of_w1[j] = dn * unit;
                 out[k][j] = a.alpha * G;
                 v[k][j] = dn * w1[k][j];
                 svy[0] += v[k][j] * y.at(k, j);
             }
+            dw1.add(k, of_w1), dw2.add(k, of_w2), dg.add(k, of_g);
+        }
         store_row<T, VEC, NV, BS, TAIL>((T *)a.dr + row * a.ld_dr, a.cols, out);
         if (post) {
             group_sum<W, 1>(svy, slots1, turn1);
@@ -355,16 +417,13 @@ __global__ __launch_bounds__(BS) void norm_bwd_kernel(const NormBwdArgs a)
         store_row<T, VEC, NV, BS, TAIL>((T *)a.dy + row * a.ld_dy, a.cols, v);
         if ((a.want & kWantGate) && (row + 1 == gate_end || row + 1 == last)) {
             const GateOut<P> o = gate_out<P>(a, part, row / a.rows_per_gate, first, last);
-            if (o.whole) store_row<P, VEC, NV, BS, TAIL>(o.whole, a.cols, dg);
-            else store_row<float, VEC, NV, BS, TAIL>(o.part, a.cols, dg);
-#pragma unroll
-            for (int k = 0; k < NV; ++k)
-#pragma unroll
-                for (int j = 0; j < VEC; ++j) dg[k][j] = 0.0f;
+            if (o.whole) dg.template store<P, TAIL>(o.whole, a.cols);
+            else dg.template store<float, TAIL>(o.part, a.cols);
+            dg.clear();
         }
     }
-    if (a.want & kWantPost) store_row<float, VEC, NV, BS, TAIL>(part + (size_t)kPartPost * a.cols, a.cols, dw1);
-    if (a.want & kWantPre) store_row<float, VEC, NV, BS, TAIL>(part + (size_t)kPartPre * a.cols, a.cols, dw2);
+    if (a.want & kWantPost) dw1.template store<float, TAIL>(part + (size_t)kPartPost * a.cols, a.cols);
+    if (a.want & kWantPre) dw2.template store<float, TAIL>(part + (size_t)kPartPre * a.cols, a.cols);
 }
 
 // Rows too long for registers, see norm_long_kernel; the parameter gradients
@@ -591,12 +650,19 @@ RowShape forward_shape(size_t nvec, bool few, int dtype)
     if (nvec <= 3072 && dtype == AR_FLOAT32) return {1024, 3};
     return {0, 0};
 }
-RowShape backward_shape(size_t nvec)
+// The backward holds four rows, three parameters and their sums; above 1024
+// vectors see Room.  What does not fit goes several times over memory (2048 x
+// 5120 fp32: in registers 52 us, so 123; 2048 x 12288: with the sums in LDS 130
+// us, so 287; 4096 x 12288 bf16: 140 and 495).
+RowShape backward_shape(size_t nvec, int dtype)
 {
     if (nvec <= 64) return {64, 1};
     if (nvec <= 256) return {256, 1};
     if (nvec <= 512) return {256, 2};
     if (nvec <= 1024) return {512, 2};
+    if (nvec <= 1536) return {512, 3};
+    if (nvec <= 2048 && dtype == AR_FLOAT32) return {512, 4};
+    if (nvec <= 3072 && dtype == AR_FLOAT32) return {512, 6};
     return {0, 0};
 }
 
@@ -615,7 +681,7 @@ uint32_t forward_groups(const ar_norm_desc &d, int threads)
 // wave: 2048 85 us, 1024 126).
 uint32_t backward_groups(const ar_norm_desc &d)
 {
-    const RowShape sh = backward_shape((d.cols * elem_bytes(d.dtype) + 15) / 16);
+    const RowShape sh = backward_shape((d.cols * elem_bytes(d.dtype) + 15) / 16, d.dtype);
     const size_t fit = sh.threads == 64 ? 2048 : sh.threads == 256 ? 512 : 256;
     return (uint32_t)(d.rows < fit ? d.rows : fit);
 }
@@ -650,27 +716,42 @@ template <typename T, typename P> int launch_norm(const ar_norm_desc &d, const N
     return AR_ERR_UNSUPPORTED;
 }
 
+template <typename T, typename P, int NV, int BS, bool TAIL, Room ROOM>
+int launch_bwd_shape(const NormBwdArgs &a, uint32_t groups, hipStream_t st)
+{
+    constexpr int LDS = ROOM == kSumsInLds ? kSumsBytes<T, NV, BS> : 0;
+    if (LDS) {
+        static const hipError_t set = hipFuncSetAttribute((const void *)norm_bwd_kernel<T, P, NV, BS, TAIL, ROOM>,
+                                                          hipFuncAttributeMaxDynamicSharedMemorySize, LDS);
+        if (set != hipSuccess) return AR_ERR_HIP;
+    }
+    hipLaunchKernelGGL((norm_bwd_kernel<T, P, NV, BS, TAIL, ROOM>), dim3(groups), dim3(BS), LDS, st, a);
+    return launch_status();
+}
+
 template <typename T, typename P>
 int launch_norm_bwd(const ar_norm_desc &d, const NormBwdArgs &a, uint32_t groups, hipStream_t st)
 {
     const size_t nvec = (d.cols + kVec<T> - 1) / kVec<T>;
     const bool tail = d.cols % kVec<T> != 0;
-    const RowShape sh = backward_shape(nvec);
-    const dim3 grid(groups);
+    const RowShape sh = backward_shape(nvec, d.dtype);
     if (!sh.threads) {
-        hipLaunchKernelGGL((norm_bwd_long_kernel<T, P>), grid, dim3(kLongThreads), 0, st, a);
+        hipLaunchKernelGGL((norm_bwd_long_kernel<T, P>), dim3(groups), dim3(kLongThreads), 0, st, a);
         return launch_status();
     }
-#define AR_NORM_CASE(BS, NV)                                                                                   \
-    if (sh.threads == BS && sh.vecs == NV) {                                                                   \
-        if (tail) hipLaunchKernelGGL((norm_bwd_kernel<T, P, NV, BS, true>), grid, dim3(BS), 0, st, a);         \
-        else hipLaunchKernelGGL((norm_bwd_kernel<T, P, NV, BS, false>), grid, dim3(BS), 0, st, a);             \
-        return launch_status();                                                                                \
+#define AR_NORM_CASE(BS, NV, ROOM)                                                     \
+    if (sh.threads == BS && sh.vecs == NV)                                             \
+        return tail ? launch_bwd_shape<T, P, NV, BS, true, ROOM>(a, groups, st)        \
+                    : launch_bwd_shape<T, P, NV, BS, false, ROOM>(a, groups, st);
+    AR_NORM_CASE(64, 1, kNextAhead)
+    AR_NORM_CASE(256, 1, kNextAhead)
+    AR_NORM_CASE(256, 2, kNextAhead)
+    AR_NORM_CASE(512, 2, kNextAhead)
+    AR_NORM_CASE(512, 3, sizeof(T) == 4 ? kNoneAhead : kSumsInLds)
+    if constexpr (sizeof(T) == 4) {
+        AR_NORM_CASE(512, 4, kNoneAhead)
+        AR_NORM_CASE(512, 6, kSumsInLds)
     }
-    AR_NORM_CASE(64, 1)
-    AR_NORM_CASE(256, 1)
-    AR_NORM_CASE(256, 2)
-    AR_NORM_CASE(512, 2)
 #undef AR_NORM_CASE
     return AR_ERR_UNSUPPORTED;
 }

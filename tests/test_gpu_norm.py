@@ -207,3 +207,40 @@ def test_backward_against_differences():
         fd = (loss(up) - loss(down)) / (2 * h)
         an = float((got[key].double() * e.double()).sum())
         assert abs(fd - an) < 1e-3 * size, (name, fd, an, size)
+
+
+# Rows at and beside the widths where the backward pass gives up the next row,
+# keeps its parameter gradients in LDS, or leaves a row in memory.
+WIDE = [(d, dtype) for dtype, widths in (("f32", (4100, 6144, 6147, 8190, 8192, 8196, 12285, 12288, 12290)),
+                                         ("bf16", (8196, 12279, 12288, 12290))) for d in widths]
+
+
+@pytest.mark.parametrize("d,dtype", WIDE)
+def test_wide_rows_backward(d, dtype):
+    """More rows than workgroups, gate rows that end inside and between them:
+    each output against 64 bits, and the same bits in its input's place."""
+    t = 520
+    for groups, param in ((0, "f32"), (5, dtype), (260, "bf16")):
+        say(f"norm backward {t} x {d} {dtype} gate rows {groups}")
+        v = inputs(t, d, dtype, param, groups, 3 if d % 2 else 0, d + groups)
+        kw = dict(post_weight=v["w1"], pre_weight=v["w2"], gate=v["gate"], alpha=0.75, eps=EPS)
+        got = ar.residual_norm_backward(v["y"], v["residual"], v["ds"], v["dx"], **kw)
+        want = oo.residual_norm_backward(v["y"], v["residual"], v["ds"], v["dx"], v["w1"], v["w2"], v["gate"], 0.75, EPS)
+        k = 48 + d / 512
+        for name, val in got.items():
+            sums = name in ("dgate", "dpost_weight", "dpre_weight")
+            near(val, *want[name], 2 * k + (t if sums else 0), param if sums else dtype, name)
+        two = ar.residual_norm_backward(v["y"], v["residual"], v["ds"], v["dx"], out=(v["dx"], v["ds"]), **kw)
+        assert all(torch.equal(got[n], two[n]) for n in got)
+
+
+@pytest.mark.parametrize("post,pre", [(True, False), (False, True), (False, False)])
+@pytest.mark.parametrize("d", (6000, 12288))
+def test_wide_rows_norms_switched_off(post, pre, d):
+    t, v = 300, inputs(300, d, "f32", "f32", 3, 0, 23)
+    w1, w2, dx = v["w1"] if post else None, v["w2"] if pre else None, v["dx"] if pre else None
+    got = ar.residual_norm_backward(v["y"], v["residual"], None, dx, post_weight=w1, pre_weight=w2, gate=v["gate"], alpha=-1.5, eps=EPS,
+                                    post=post, pre=pre)
+    want = oo.residual_norm_backward(v["y"], v["residual"], None, dx, w1, w2, v["gate"], -1.5, EPS, post, pre)
+    for name, val in got.items():
+        near(val, *want[name], 2 * (48 + d / 512) + t, "f32", name)

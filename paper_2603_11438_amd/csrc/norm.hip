@@ -526,7 +526,7 @@ template <typename T, typename P> __global__ __launch_bounds__(kLongThreads) voi
 // order of the rows: 64 columns a workgroup, kFinishWaves runs of workgroups
 // side by side.  blockIdx.y: 0 post weight, 1 pre weight, from 2 on the gate
 // rows whose rows fell to several workgroups.
-constexpr int kFinishWaves = 8;
+constexpr int kFinishWaves = 16;
 
 struct FinishArgs {
     const float *part;
@@ -568,7 +568,7 @@ template <typename P> __global__ __launch_bounds__(64 * kFinishWaves) void norm_
                    to = w0 + (uint32_t)((uint64_t)n * (wave + 1) / kFinishWaves);
     float t = 0.0f;
     if (col < a.cols) {
-#pragma unroll 8
+#pragma unroll 16
         for (uint32_t w = from; w < to; ++w)
             t += a.part[((size_t)w * kParts + (w == w0 ? head : which)) * a.cols + col];
     }
@@ -678,12 +678,16 @@ uint32_t forward_groups(const ar_norm_desc &d, int threads)
 // The backward pass writes a row of partial sums for each workgroup: as few as
 // keep the device busy (8192 x 4096 bf16, of 256 threads: 512 89 us, 1024 94,
 // 256 115; 8192 x 8192, of 512 threads: 256 179 us, 512 188; 65536 x 512, of one
-// wave: 2048 85 us, 1024 126).
+// wave: 2048 85 us, 1024 126; 4096 no better).  Rows of one wave are short beside
+// their workgroup's partial sums: at least eight of them to a workgroup (1834 x 248
+// 16.6 us, one to a workgroup 25.8; 5445 x 176 22.6 and 27.5).  For wider rows
+// that is slower (2000 x 4096: 33 us for 30).
 uint32_t backward_groups(const ar_norm_desc &d)
 {
     const RowShape sh = backward_shape((d.cols * elem_bytes(d.dtype) + 15) / 16, d.dtype);
-    const size_t fit = sh.threads == 64 ? 2048 : sh.threads == 256 ? 512 : 256;
-    return (uint32_t)(d.rows < fit ? d.rows : fit);
+    const size_t most = sh.threads == 64 ? 2048 : sh.threads == 256 ? 512 : 256;
+    const size_t few = sh.threads == 64 && d.rows > 256 ? (d.rows / 8 > 256 ? d.rows / 8 : 256) : d.rows;
+    return (uint32_t)(few < most ? few : most);
 }
 
 template <typename T, typename P> int launch_norm(const ar_norm_desc &d, const NormArgs &a, hipStream_t st)

@@ -117,10 +117,12 @@ typedef struct ar_ffn_desc {
     size_t ld_dx, ld_dw_gate, ld_dw_up;     /* backward only */
 } ar_ffn_desc;
 
-/* Forward, one kernel for both products, the activation and their product
- * (operands that it cannot read where they lie, not 16-byte aligned or with a
+/* Forward, one kernel for both products, the activation and their product.
+ * Operands that it cannot read where they lie, not 16-byte aligned or with a
  * dim or row stride that is no multiple of 8, are first copied into the
- * workspace; without such operands none is needed).  saved: NULL, or
+ * workspace.  Where tokens x hidden is small beside a long dim, the sums over
+ * dim are taken in several runs, which a second kernel joins, from the
+ * workspace.  Calls that need neither need no workspace.  saved: NULL, or
  * 2 * tokens * hidden floats (16-byte aligned) that receive G and U for the
  * backward pass, in fp32.  Errors: AR_ERR_ARG, AR_ERR_UNSUPPORTED,
  * AR_ERR_SCRATCH, AR_ERR_HIP. */

@@ -5,7 +5,10 @@
 // hold both projections of the same columns, so that the activation and the
 // product happen in registers and only h is written.  8192 x 4096 x 11264, silu:
 // 1240 us, 1220 TFLOP/s.  Bound by the weights' bytes with few: up to 64 tokens
-// share a tile of 64 columns of both, 1 x 4096 x 11264: 41 us, 4.5 TB/s.
+// share a tile of 64 columns of both, 1 x 4096 x 11264: 41 us, 4.5 TB/s.  Bound by the
+// length of k where there are few tiles, as in a rank's share of the columns: there
+// k is split, and a second kernel joins the runs and applies the activation (1 x
+// 4096 x 1408: 13 us, in one piece 32; 256 x 4096 x 1408: 19 us, in one piece 63).
 //
 // Backward: dG and dU by one pass over the saved projections (4096 x 11264: 125
 // us, 5.2 TB/s), dx as one product over both pairs of operands, both weights'
@@ -43,6 +46,7 @@ template <int ACT> __device__ __forceinline__ float activation(float g, float *s
 struct FfnOut {
     bf16 *h;
     float *saved;  // G, then U; null: not kept
+    float *part;   // with k split: the runs' sums, [run][G, U][m][n]
     uint64_t ld_h;
 };
 
@@ -65,16 +69,49 @@ template <typename S, int ACT> __global__ __launch_bounds__(S::THREADS) void ffn
         const uint32_t first = row0 + i * 32;
         if (first >= g.m) return;
         const uint32_t rows = g.m - first;
-        if (o.saved) {
-            float *to = o.saved + (uint64_t)first * g.n + col0;
+        float *keep = g.splits > 1 ? o.part + (uint64_t)blockIdx.y * 2 * g.m * g.n : o.saved;
+        if (keep) {
+            float *to = keep + (uint64_t)first * g.n + col0;
             stage_rows<float, HALF>(stage, [&](int j, int r) { return v[j][r]; });
             write_rows<float, HALF>(stage, to, g.n, 0, rows, cols);
             stage_rows<float, HALF>(stage, [&](int j, int r) { return v[j + NT / 2][r]; });
             write_rows<float, HALF>(stage, to + (uint64_t)g.m * g.n, g.n, 0, rows, cols);
         }
+        if (g.splits > 1) return;
         stage_rows<bf16, HALF>(stage, [&](int j, int r) { return activation<ACT>(v[j][r]) * v[j + NT / 2][r]; });
         write_rows<bf16, HALF>(stage, o.h + (uint64_t)first * o.ld_h + col0, o.ld_h, 0, rows, cols);
     });
+}
+
+// The projections from the runs' sums, added in their order, and h; four columns
+// a thread.
+template <int ACT> __global__ __launch_bounds__(256) void ffn_join_kernel(const FfnOut o, uint32_t m, uint32_t n, uint32_t splits)
+{
+    const uint64_t half = (uint64_t)m * n, per = (n + 3) / 4, all = m * per;
+    for (uint64_t i = (uint64_t)blockIdx.x * 256 + threadIdx.x; i < all; i += (uint64_t)gridDim.x * 256) {
+        const uint32_t row = (uint32_t)(i / per), c = (uint32_t)(i % per) * 4;
+        const int have = n - c < 4 ? (int)(n - c) : 4;
+        const uint64_t at = (uint64_t)row * n + c;
+        float g[4] = {0.0f, 0.0f, 0.0f, 0.0f}, u[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+        auto add = [&](auto load) {
+#pragma unroll 8
+            for (uint32_t s = 0; s < splits; ++s) {
+                float a[4], b[4];
+                load(o.part + s * 2 * half + at, a), load(o.part + (s * 2 + 1) * half + at, b);
+#pragma unroll
+                for (int k = 0; k < 4; ++k) g[k] += a[k], u[k] += b[k];
+            }
+        };
+        if (have == 4) add([](const float *p, float *v) { load_vec<float, 4>(p, v); });
+        else add([&](const float *p, float *v) { load_part<float, 4>(p, have, v); });
+        if (o.saved) {
+            store_part<float, 4>(o.saved + at, have, g);
+            store_part<float, 4>(o.saved + half + at, have, u);
+        }
+#pragma unroll
+        for (int k = 0; k < 4; ++k) u[k] *= activation<ACT>(g[k]);
+        store_part<bf16, 4>(o.h + row * o.ld_h + c, have, u);
+    }
 }
 
 // Copies a matrix into rows of `to_ld` elements, zeros behind its columns.
@@ -278,16 +315,54 @@ template <typename S, int ACT> int launch_ffn(GemmArgs &g, const FfnOut &o, hipS
     static_assert(4 * kStageBytes<float, S::NT * 16> <= S::LDS, "the epilogue's staging fits");
     static const hipError_t set = hipFuncSetAttribute((const void *)ffn_kernel<S, ACT>, hipFuncAttributeMaxDynamicSharedMemorySize, S::LDS);
     if (set != hipSuccess) return AR_ERR_HIP;
-    hipLaunchKernelGGL((ffn_kernel<S, ACT>), dim3(g.tiles_m * g.tiles_n), dim3(S::THREADS), S::LDS, st, g, o);
+    hipLaunchKernelGGL((ffn_kernel<S, ACT>), dim3(g.tiles_m * g.tiles_n, g.splits), dim3(S::THREADS), S::LDS, st, g, o);
+    const int rc = launch_status();
+    if (rc != AR_OK || g.splits == 1) return rc;
+    const uint64_t groups = ((uint64_t)g.m * ((g.n + 3) / 4) + 255) / 256;
+    hipLaunchKernelGGL((ffn_join_kernel<ACT>), dim3((uint32_t)(groups < 8192 ? groups : 8192)), dim3(256), 0, st, o, g.m, g.n, g.splits);
     return launch_status();
 }
 
-template <int ACT> int launch_ffn_tiles(GemmArgs &g, const FfnOut &o, hipStream_t st)
+constexpr uint32_t kMaxSplits = 32;
+
+// The forward's tile (an index of kTiles, kFlat for up to 64 tokens) and the runs
+// of its k.  Few tiles, of a rank's share of the hidden columns say, leave units
+// idle that a split puts to work.  Flat: kFlatStep us a step of 64 for a tile (1 x
+// 4096 x 1408 in one piece 32 us), two tiles to a unit, the weights' bytes at 4.5
+// TB/s, and a join as in cut_for.  So 1 x 4096 x 5632 is split (25 us, in one piece
+// 33) and 1 x 4096 x 11264 is not.  A 128 x 128 tile alone on its unit has three
+// buffers: 1024 x 4096 x 1408 39 us, with two 62; 128 x 4096 x 11264 48 and 67.
+constexpr int kFlat = -1;
+constexpr double kFlatStep = 0.45;
+Cut ffn_cut(size_t tokens, size_t dim, size_t hidden)
 {
+    const size_t steps = (dim + kStepK - 1) / kStepK;
+    if (tokens <= 64) {
+        const size_t tiles = (hidden + 63) / 64;
+        const double bytes = 4.0 * dim * hidden / 4.5e6;
+        Cut best{kFlat, 1};
+        double time = 0;
+        for (uint32_t s = 1; s <= kMaxSplits && (s == 1 || s * 2 <= steps); ++s) {
+            double sum = (tiles * s + 511) / 512 * ((steps + s - 1) / s) * kFlatStep;
+            sum = sum > bytes ? sum : bytes;
+            if (s > 1) sum += 4.0 + 2.0 * s * tokens * 2 * hidden * 4 / 6e6;
+            if (s == 1 || sum < time) best.splits = s, time = sum;
+        }
+        return best;
+    }
     // the pairs' columns count twice
-    if (g.m <= 64) return launch_ffn<Flat, ACT>(g, o, st);
-    return cut_for(1, g.m, 2 * (size_t)g.n, g.steps, 1, false, 1, 3, 1).tile == 1 ? launch_ffn<Small, ACT>(g, o, st)
-                                                                                  : launch_ffn<Large, ACT>(g, o, st);
+    if (cut_for(1, tokens, 2 * hidden, steps, 1, false, 1, 3, 1).tile != 1) return {3, 1};
+    Cut c = cut_for(1, tokens, 2 * hidden, steps, 1, false, 1, 1, kMaxSplits);
+    if ((tokens + 127) / 128 * ((hidden + 63) / 64) * c.splits <= 256) c.tile = 4;
+    return c;
+}
+size_t ffn_part_bytes(const ar_ffn_desc &d, const Cut &c) { return c.splits > 1 ? c.splits * 2 * d.tokens * d.hidden * sizeof(float) : 0; }
+
+template <int ACT> int launch_ffn_tiles(const Cut &c, GemmArgs &g, const FfnOut &o, hipStream_t st)
+{
+    if (c.tile == kFlat) return launch_ffn<Flat, ACT>(g, o, st);
+    if (c.tile == 4) return launch_ffn<Deep, ACT>(g, o, st);
+    return c.tile == 1 ? launch_ffn<Small, ACT>(g, o, st) : launch_ffn<Large, ACT>(g, o, st);
 }
 
 struct FfnMats {
@@ -303,7 +378,7 @@ FfnMats ffn_mats(const ar_ffn_desc &d, const void *x, const void *wg, const void
 // before the call, so every operand counts.
 size_t ffn_workspace(const ar_ffn_desc &d)
 {
-    return packed_bytes(d.tokens, d.dim) + 2 * packed_bytes(d.hidden, d.dim);
+    return packed_bytes(d.tokens, d.dim) + 2 * packed_bytes(d.hidden, d.dim) + ffn_part_bytes(d, ffn_cut(d.tokens, d.dim, d.hidden));
 }
 
 int ffn(const ar_ffn_desc *desc, const void *x, const void *wg, const void *wu, void *h, float *saved, void *ws,
@@ -319,7 +394,8 @@ int ffn(const ar_ffn_desc *desc, const void *x, const void *wg, const void *wu, 
     for (const Mat &in : {m.x, m.wg, m.wu})
         if (meet(m.h, in) || meet(sv, in)) return AR_ERR_ARG;
     if (meet(m.h, sv)) return AR_ERR_ARG;
-    size_t need = 0;
+    const Cut cut = ffn_cut(d.tokens, d.dim, d.hidden);
+    size_t need = ffn_part_bytes(d, cut);
     for (const Mat &in : {m.x, m.wg, m.wu})
         if (!direct(in)) need += packed_bytes(in.rows, in.cols);
     if (need) {
@@ -340,18 +416,17 @@ int ffn(const ar_ffn_desc *desc, const void *x, const void *wg, const void *wu, 
     g.lda = px.ld, g.ldb = pg.ld, g.ldb2 = pu.ld;
     g.segments = 1, g.steps = (uint32_t)(round_up(d.dim, kStepK) / kStepK);
     g.ka = g.kb = (uint32_t)round_up(d.dim, 8);
-    g.m = (uint32_t)d.tokens, g.n = (uint32_t)d.hidden, g.batch = 1, g.splits = 1;
-    const FfnOut o{(bf16 *)h, saved, m.h.ld};
+    g.m = (uint32_t)d.tokens, g.n = (uint32_t)d.hidden, g.batch = 1, g.splits = cut.splits;
+    const FfnOut o{(bf16 *)h, saved, (float *)at, m.h.ld};  // the runs' sums behind the copies
     switch (d.act) {
-    case AR_ACT_SILU: return launch_ffn_tiles<AR_ACT_SILU>(g, o, st);
-    case AR_ACT_GELU: return launch_ffn_tiles<AR_ACT_GELU>(g, o, st);
-    default: return launch_ffn_tiles<AR_ACT_RELU>(g, o, st);
+    case AR_ACT_SILU: return launch_ffn_tiles<AR_ACT_SILU>(cut, g, o, st);
+    case AR_ACT_GELU: return launch_ffn_tiles<AR_ACT_GELU>(cut, g, o, st);
+    default: return launch_ffn_tiles<AR_ACT_RELU>(cut, g, o, st);
     }
 }
 
 // ---- backward ---------------------------------------------------------------
 
-constexpr uint32_t kMaxSplits = 32;
 size_t part_bytes(size_t m, size_t cols, size_t steps)
 {
     const Cut c = cut_for(1, m, cols, steps, 1, false, 0, 4, kMaxSplits);

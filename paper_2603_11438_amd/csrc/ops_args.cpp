@@ -218,7 +218,7 @@ PyObject *ffn(PyObject *, PyObject *const *a, Py_ssize_t n)
         Py_BEGIN_ALLOW_THREADS
         rc = ((decltype(&ar_gated_ffn))fn)(&d, x.p(), g.p(), u.p(), ptr(h), (float *)ptr(saved), nullptr, 0, stream);
         Py_END_ALLOW_THREADS
-        if (rc == AR_ERR_SCRATCH) {  // only operands that have to be laid out need a workspace
+        if (rc == AR_ERR_SCRATCH) {  // only operands that have to be laid out, and a dim in several runs, need a workspace
             bytes = ((decltype(&ar_gated_ffn_workspace))space)(&d);
             ws = workspace(bytes, x);
             Py_BEGIN_ALLOW_THREADS

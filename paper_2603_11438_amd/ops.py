@@ -382,7 +382,7 @@ def gated_ffn(x, w_gate, w_up, *, act: str = "silu", save: bool = False, out=Non
         ws = None
         rc = L.ar_gated_ffn(ctypes.byref(d), x.data_ptr(), w_gate.data_ptr(), w_up.data_ptr(), h.data_ptr(), _ptr(saved),
                             None, 0, on.ptr)
-        if rc == _ar.AR_ERR_SCRATCH:  # only operands that have to be laid out need one
+        if rc == _ar.AR_ERR_SCRATCH:  # only operands that have to be laid out, and a dim in several runs, need one
             ws = _workspace(L.ar_gated_ffn_workspace(ctypes.byref(d)), x)
             rc = L.ar_gated_ffn(ctypes.byref(d), x.data_ptr(), w_gate.data_ptr(), w_up.data_ptr(), h.data_ptr(), _ptr(saved),
                                 _ptr(ws), ws.numel(), on.ptr)

@@ -209,3 +209,43 @@ def test_backward_against_differences():
         off = abs((loss(up, True) - loss(down, True)) / (2 * step) - ref_an)
         an = float((got[name].cpu().double() * e.cpu().double()).sum())
         assert abs(fd - an) <= off + 2 * R * float((ref[name].abs() * e.cpu().double().abs()).sum()) + 1e-3, (name, fd, an, off)
+
+
+# Few tiles: k is split and its runs joined; long and short k, ragged ends, one
+# token to several tiles of them, and operands that have to be laid out.
+@pytest.mark.parametrize("t,d,f,pad", [(1, 4096, 1408, 0), (5, 4357, 157, 0), (64, 1000, 64, 0), (64, 2056, 130, 8), (65, 4096, 130, 0),
+                                       (160, 4488, 184, 0), (300, 1999, 61, 3), (747, 2048, 581, 0), (33, 128, 8, 0), (200, 192, 72, 0)])
+def test_forward_of_narrow_shares(t, d, f, pad):
+    for act in ("silu", "relu"):
+        say(f"ffn forward {t} x {d} x {f} {act} pad {pad}")
+        x, wg, wu, _ = inputs(t, d, f, pad, seed=3)
+        e, g, u = oo.gated_ffn(x, wg, wu, act)
+        X, G, W = x.cpu().double().abs(), wg.cpu().double().abs(), wu.cpu().double().abs()
+        gm, um = X @ G.T, X @ W.T
+        k = (d + 16) * U  # a split adds its runs one after another: no more terms in a row than one sum has
+        h, saved = ar.gated_ffn(x, wg, wu, act=act, save=True)
+        within(saved[0], g, k * gm, "G")
+        within(saved[1], u, k * um, "U")
+        # |act'| is below 1.13, |act(g)| at most |g|
+        tol = 1.13 * k * gm * (u.abs() + k * um) + k * um * g.abs() + (32 + g.abs()) * U * (g * u).abs() + R * e.abs() * 1.01
+        within(h, e, tol, "h")
+        assert torch.equal(ar.gated_ffn(x, wg, wu, act=act), h)
+        out = torch.full((t, f + 5), 7.0, dtype=torch.bfloat16, device="cuda")
+        ar.gated_ffn(x, wg, wu, act=act, out=out[:, :f])
+        assert torch.equal(out[:, :f], h) and bool((out[:, f:] == 7).all())
+
+
+def test_narrow_share_graph_replays():
+    x, wg, wu, _ = inputs(8, 4096, 256)
+    ar.gated_ffn(x, wg, wu)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = ar.gated_ffn(x, wg, wu)
+    for k in range(4):
+        x.copy_(inputs(8, 4096, 256, seed=50 + k)[0])
+        want = ar.gated_ffn(x, wg, wu)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(got, want), k

@@ -207,3 +207,20 @@ def test_ortho_without_matrices_is_done():
 def test_ortho_tensor_checks():
     with pytest.raises(ValueError, match="GPU"):
         ar.orthogonalize(torch.zeros(4, 8))
+
+
+def test_ffn_in_runs_needs_its_workspace():
+    """One tile and a long dim: the sums are taken in runs, which lie in the
+    workspace; a large hidden takes them in one piece."""
+    L = ops._lib()
+    d = ops.ar_ffn_desc(tokens=4, dim=4096, hidden=64, dtype=1, act=0)
+    copies = 2 * 4096 * (4 + 2 * 64)
+    assert L.ar_gated_ffn_workspace(ctypes.byref(d)) > copies
+    assert (L.ar_gated_ffn_workspace(ctypes.byref(d)) - copies) % (2 * 4 * 64 * 4) == 0
+    big = dict(x=0x100000000, wg=0x200000000, wu=0x300000000, h=0x400000000, dim=4096, hidden=64)
+    assert ffn(**big) == ar.AR_ERR_SCRATCH
+    assert ffn(ws=0x500000000, nbytes=1024, **big) == ar.AR_ERR_SCRATCH
+    assert ffn(ws=0x500000008, nbytes=1 << 30, **big) == ar.AR_ERR_ARG
+    assert ffn(ws=0x400000000, nbytes=1 << 30, **big) == ar.AR_ERR_ARG
+    d = ops.ar_ffn_desc(tokens=4, dim=4096, hidden=16384, dtype=1, act=0)
+    assert L.ar_gated_ffn_workspace(ctypes.byref(d)) == 2 * 4096 * (4 + 2 * 16384)

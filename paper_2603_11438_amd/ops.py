@@ -231,6 +231,8 @@ def _norm_desc(y, post_weight, pre_weight, gate, alpha, eps, post, pre):
     if pdt not in (torch.float32, torch.bfloat16):
         raise TypeError(f"unsupported dtype {pdt}")
     if gate is not None:
+        if gate.dim() not in (1, 2):
+            raise ValueError("gate must be a row or a matrix")
         d.gate_rows = 1 if gate.dim() == 1 else gate.shape[0]
         if d.gate_rows == 0 or rows % d.gate_rows:
             raise ValueError(f"{rows} rows cannot be shared by {d.gate_rows} rows of the gate")

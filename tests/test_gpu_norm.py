@@ -244,3 +244,12 @@ def test_wide_rows_norms_switched_off(post, pre, d):
     want = oo.residual_norm_backward(v["y"], v["residual"], None, dx, w1, w2, v["gate"], -1.5, EPS, post, pre)
     for name, val in got.items():
         near(val, *want[name], 2 * (48 + d / 512) + t, "f32", name)
+
+
+@pytest.mark.parametrize("shape", [(), (1, 2, 64)])
+def test_gate_is_a_row_or_a_matrix(shape):
+    y = torch.zeros(4, 64, device="cuda")
+    with pytest.raises(ValueError, match="gate must be"):
+        ar.residual_norm(y, y, gate=torch.ones(shape, device="cuda"))
+    with pytest.raises(ValueError, match="gate must be"):
+        ar.residual_norm_backward(y, y, None, y, gate=torch.ones(shape, device="cuda"))

@@ -45,7 +45,7 @@ struct Scales {
 
 // One matrix' part of the workspace, in bytes.
 struct OrthoSpace {
-    size_t x[2], x_lo, xf, a, a_lo, b, b_lo, diag_a, diag_b, part, scales, norms, bytes;
+    size_t x[2], x_lo, xf, a, a_lo, b, b_lo, diag_a, diag_b, squares, part, scales, norms, bytes;
 };
 
 struct OrthoArgs {
@@ -56,6 +56,7 @@ struct OrthoArgs {
     uint64_t ld_in, ld_out, stride_in, stride_out;
     uint32_t m, n, mp, np;       // rows <= columns, and both in multiples of 64
     uint32_t batch, norm_parts, step, steps;
+    uint32_t strips;             // of X's columns: one plane keeps a row's sum of squares in so many parts
     int tall;                    // the matrix is the transpose
     float a, b, c, eps, scale;
     // bound of |X| after k steps, and of its growth from |X| = tau, for
@@ -272,11 +273,44 @@ template <typename S> constexpr int kOrthoStage = kStageColBytes<float, S::NT * 
                                                       ? kStageColBytes<float, S::NT * 32> : 2 * kStageBytes<f16, S::NT * 32>;
 template <typename S> constexpr int kOrthoLds = S::LDS > 4 * kOrthoStage<S> ? S::LDS : 4 * kOrthoStage<S>;
 
+// The sums of squares of X's rows that the update left, one part for each strip of
+// columns, for the block rows of a tile on the diagonal.  Both halves of a wave
+// share out a row's parts.  The loads begin with the products (4096 x 4096 bf16:
+// behind them 7 us a step more).
+template <int N> struct RowSquares {
+    static constexpr int EARLY = 16;
+    float part[N][EARLY];
+    const float *from;
+    uint32_t strips, pitch;
+    __device__ __forceinline__ void load(const OrthoArgs &o, const char *ws, uint32_t row0)
+    {
+        from = (const float *)(ws + o.at.squares), strips = o.strips, pitch = o.mp;
+#pragma unroll
+        for (int n = 0; n < N; ++n)
+#pragma unroll
+            for (int k = 0; k < EARLY; ++k) part[n][k] = at(row0 + n * 32, k);
+    }
+    // row l%32 of the block that begins at `first`
+    __device__ __forceinline__ float at(uint32_t first, uint32_t k) const
+    {
+        const uint32_t i = first + (threadIdx.x & 31u), s = 2 * k + (threadIdx.x >> 5 & 1u);
+        return i < pitch && s < strips ? from[(uint64_t)s * pitch + i] : 0.0f;
+    }
+    __device__ __forceinline__ float sum(int n, uint32_t first) const
+    {
+        float t = 0.0f;
+#pragma unroll
+        for (int k = 0; k < EARLY; ++k) t += part[n][k];
+        for (uint32_t k = EARLY; 2 * k < strips; ++k) t += at(first, k);
+        return t + __shfl_xor(t, 32);
+    }
+};
+
 // 32 rows of A (SECOND false) or B from their sums: written to both places; the
 // diagonal goes to its fp32 vector and is zero in the planes.
-template <typename S, bool SECOND, typename A>
+template <typename S, bool SECOND, typename A, int N>
 __device__ __forceinline__ void square_rows(float (&v)[S::NT][16], int bi, const TileAt at, const WaveAt<S> &w, const OrthoArgs &o,
-                                            const Scales &s, A &ahead, char *stage)
+                                            const Scales &s, A &ahead, const RowSquares<N> &squares, char *stage)
 {
     constexpr int NT = S::NT, PLANES = S::PLANES;
     char *ws = o.ws + at.batch * o.at.bytes;
@@ -308,20 +342,25 @@ __device__ __forceinline__ void square_rows(float (&v)[S::NT][16], int bi, const
                 v[bj][q * 4 + k] = i < o.m && j < o.m ? x * to : 0.0f;
             }
         }
+    const uint32_t first = w.row0 + bi * 32;
     if (at.m == at.n) {
+        // One plane: A's diagonal is the rows' sums of squares, of which the products
+        // hold those of X rounded to a plane (the input's plane is exact).
+        const bool exact = !SECOND && PLANES == 1 && o.step > 0;
+        const float square = exact ? squares.sum(N == 1 ? 0 : bi, first) * sx * sx : 0.0f;
         // the diagonal goes to its vector (off and dj are zero there)
 #pragma unroll
         for (int bj = 0; bj < NT; ++bj)
 #pragma unroll
             for (int r = 0; r < 16; ++r) {
                 if (w.j(bj, r) != i) continue;
-                if (i < o.m) (SECOND ? diag_b : diag_a)[i] = SECOND ? o.b * di + v[bj][r] / to + o.c * di * di : v[bj][r] / to;
+                const float found = exact ? square : v[bj][r] / to;
+                if (i < o.m) (SECOND ? diag_b : diag_a)[i] = SECOND ? o.b * di + found + o.c * di * di : found;
                 v[bj][r] = 0.0f;
             }
     }
     char *hi = ws + (SECOND ? o.at.b : o.at.a);
     const size_t lo = SECOND ? o.at.b_lo : o.at.a_lo;
-    const uint32_t first = w.row0 + bi * 32;
     if (at.m != at.n) store_planes<S, PLANES, true>(stage, v, first, w.col0, hi, lo, o.mp, o.mp);
     else store_planes<S, PLANES, false>(stage, v, first, w.col0, hi, lo, o.mp, o.mp);
 }
@@ -351,6 +390,8 @@ __global__ __launch_bounds__(S::THREADS) void ortho_square_kernel(const GemmArgs
     char *stage = lds + (threadIdx.x >> 6) * kOrthoStage<S>;
     Ahead<S, f16, PLANES> ahead{(const f16 *)(ws + o.at.a), o.at.a_lo, o.mp, o.mp, w.row0, w.col0, stage};
     if (SECOND) ahead.load(0);
+    RowSquares<S::MT> squares;
+    if (!SECOND && PLANES == 1 && o.step > 0 && at.m == at.n) squares.load(o, ws, w.row0);
     f32x16 acc[S::MT][NT];
     gemm_tile<f16, S, false>(g, at, lds, acc);
     if (!SECOND && g.splits > 1) {
@@ -368,7 +409,7 @@ __global__ __launch_bounds__(S::THREADS) void ortho_square_kernel(const GemmArgs
     static_for<S::MT>([&](auto block) {
         float v[NT][16];
         take(acc[block.value], v);
-        square_rows<S, SECOND>(v, block.value, at, w, o, s, ahead, stage);
+        square_rows<S, SECOND>(v, block.value, at, w, o, s, ahead, squares, stage);
     });
 }
 
@@ -383,6 +424,8 @@ template <typename S> __global__ __launch_bounds__(S::THREADS) void ortho_join_k
     const Scales s = ((const Scales *)(o.ws + at.batch * o.at.bytes + o.at.scales))[o.step];
     const float *from = run_sums<S>(o, at, g.tiles_m, 0) + blockIdx.y * NT * 1024;
     const uint64_t run = run_sums<S>(o, at, g.tiles_m, 1) - run_sums<S>(o, at, g.tiles_m, 0);
+    RowSquares<1> squares;
+    if (S::PLANES == 1 && o.step > 0 && at.m == at.n) squares.load(o, o.ws + at.batch * o.at.bytes, w.row0 + blockIdx.y * 32);
     float v[NT][16];
 #pragma unroll
     for (int bj = 0; bj < NT; ++bj)
@@ -401,7 +444,7 @@ template <typename S> __global__ __launch_bounds__(S::THREADS) void ortho_join_k
             }
     }
     int none = 0;
-    square_rows<S, false>(v, (int)blockIdx.y, at, w, o, s, none, lds + (threadIdx.x >> 6) * kOrthoStage<S>);
+    square_rows<S, false>(v, (int)blockIdx.y, at, w, o, s, none, squares, lds + (threadIdx.x >> 6) * kOrthoStage<S>);
 }
 
 // X = a X + B X from the sums of B X (the off-diagonal B); after the last step the
@@ -451,6 +494,15 @@ __device__ __forceinline__ void update(f32x16 (&acc)[S::MT][S::NT], const TileAt
         const uint32_t first = w.row0 + bi * 32;
         auto value = [&](int j, int r) { return v[j][r]; };
         if (!last) {
+            if (PLANES == 1 && w.col0 < o.np) {
+                float square = 0.0f;
+#pragma unroll
+                for (int bj = 0; bj < NT; ++bj)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) square += v[bj][r] * v[bj][r];
+                square += __shfl_xor(square, 32);
+                if (w.half == 0 && i < o.mp) ((float *)(ws + o.at.squares))[(uint64_t)(w.col0 / (NT * 32)) * o.mp + i] = square;
+            }
             store_planes<S, 2, false>(stage, v, first, w.col0, x_next, o.at.x_lo, o.mp, o.np);
             if (PLANES == 2 && first < o.m && w.col0 < o.np) {
                 stage_rows<float, NT * 32>(stage, value);
@@ -727,6 +779,7 @@ OrthoSpace ortho_space(const ar_ortho_desc &d, uint32_t mp, uint32_t np)
     s.a = take(two ? 2 * sq : sq), s.b = take(two ? 2 * sq : sq);
     s.x_lo = x, s.a_lo = s.b_lo = sq;
     s.diag_a = take(mp * 4), s.diag_b = take(mp * 4);
+    s.squares = take(two ? 0 : (size_t)np / 32 * mp * 4);  // strips of 32 columns at least
     s.part = take(c.splits > 1 ? c.splits * (tiles * (tiles + 1) / 2) * side * side * 4 : 0);
     s.scales = take(sizeof(Scales) * (AR_ORTHO_MAX_STEPS + 1));
     s.norms = take(sizeof(double) * kNormParts);
@@ -773,8 +826,9 @@ template <int PLANES, bool SECOND> int square(GemmArgs &g, const OrthoArgs &o, h
     }
 }
 
-template <typename S, typename O> int launch_update(GemmArgs &g, const OrthoArgs &o, hipStream_t st)
+template <typename S, typename O> int launch_update(GemmArgs &g, OrthoArgs &o, hipStream_t st)
 {
+    o.strips = (o.np + S::NT * 32 - 1) / (S::NT * 32);
     g.tiles_m = (o.m + S::BM - 1) / S::BM, g.tiles_n = (o.n + S::BN - 1) / S::BN;
     static const hipError_t set = hipFuncSetAttribute((const void *)ortho_update_kernel<S, O>,
                                                       hipFuncAttributeMaxDynamicSharedMemorySize, kOrthoLds<S>);
@@ -782,7 +836,7 @@ template <typename S, typename O> int launch_update(GemmArgs &g, const OrthoArgs
     hipLaunchKernelGGL((ortho_update_kernel<S, O>), dim3(g.tiles_m * g.tiles_n * o.batch), dim3(S::THREADS), kOrthoLds<S>, st, g, o);
     return launch_status();
 }
-template <int PLANES, typename O> int update_step(GemmArgs &g, const OrthoArgs &o, hipStream_t st)
+template <int PLANES, typename O> int update_step(GemmArgs &g, OrthoArgs &o, hipStream_t st)
 {
     switch (cut_for(PLANES, o.m, o.n, g.steps, o.batch, false, 0, 3, 1).tile) {
     case 0: return launch_update<typename ShapeOf<PLANES, 0>::type, O>(g, o, st);

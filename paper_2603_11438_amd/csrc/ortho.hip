@@ -7,14 +7,18 @@
 //   fp32 matrices: products of hi and lo, hi hi + hi lo + lo hi, and X also in
 //   fp32 for the a X term.
 //   bf16 matrices: products of hi alone, one third of the work.  What a single
-//   plane would lose is kept out of the products: X itself has both planes for
-//   the a X term (a strong direction's rounding error would otherwise swamp
-//   weak directions, which the steps amplify up to a^steps = 485 times), and
-//   the diagonals of A and B, on which most of their norm sits, stay in fp32:
-//   with A = D + O, D diagonal,
-//     A A = D D + D O + O D + O O,   a X + B X = (a + diag B) X + (B - diag B) X.
-//   The result's error before its rounding to bf16 is 0.5e-3 to 0.9e-3 of its
-//   norm (bf16's own rounding 1.7e-3); without the two measures up to 1.8e-2.
+//   plane would lose is kept out of the products, or kept from adding up: X itself
+//   has both planes for the a X term (a strong direction's rounding error would
+//   otherwise swamp weak directions, which the steps amplify up to a^steps = 485
+//   times); the diagonals of A and B, on which most of their norm sits, stay in
+//   fp32, A's from the rows of both planes: with A = D + O, D diagonal,
+//     A A = D D + D O + O D + O O,   a X + B X = (a + diag B) X + (B - diag B) X;
+//   and values among equals are rounded at random (round_alike).
+//   The result's error before its rounding to bf16 (1.7e-3 of its norm, up to
+//   3.9e-3), with every rounding modelled in 64 bits: 0.2e-3 to 0.9e-3 of its norm
+//   for matrices of full rank, up to 1.8e-3 for those of low rank, up to 2.8e-3 where
+//   rows hold few magnitudes or few elements (identity, constant, signs, blocks of
+//   ones, repeated columns: 50 kinds in all).  Without these measures up to 1.8e-2.
 //   Small matrices, whose few singular values do not average such errors, take
 //   two planes in bf16 too.
 //
@@ -217,10 +221,57 @@ template <typename S> struct WaveAt {
     __device__ __forceinline__ uint32_t j(int bj, int r) const { return col0 + bj * 32 + r / 4 * 8 + half + r % 4; }
 };
 
+// Whether among four neighbouring elements of a row two have the same magnitude, to
+// 18 bits, and it is not zero.
+__device__ __forceinline__ bool two_alike(const float *v)
+{
+    uint32_t m[4];
+    bool same = false;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        const uint32_t found = (__builtin_bit_cast(uint32_t, v[k]) + 32) >> 6 & 0x1ffffffu;
+        m[k] = found > (uint32_t)k ? found : (uint32_t)k;  // zeros differ from each other
+#pragma unroll
+        for (int h = 0; h < k; ++h) same |= m[h] == m[k];
+    }
+    return same;
+}
+
+// 32 rows of a wave's block on their way into a product's only plane.  The plane's 11
+// bits are the nearest, left to the caller's conversion, but where many neighbours
+// are alike: there a value goes up or down at random, in proportion.  Equal values'
+// rounding errors are equal: in a matrix of few magnitudes they add up over its rows
+// and columns instead of averaging, and the steps amplify them (a constant 572 x
+// 2158: off by 9.7e-3 of its norm, so by 4e-4).  Elsewhere the nearest value errs less.
+// Each block of 32 x 32 is judged by its first eight columns, which costs next to
+// nothing (a hash and comparisons for every four elements: 3 to 6 % of a call).  The
+// random bits come from an element's place and `salt` alone.  w.j: column.
+template <int NT, typename W> __device__ __forceinline__ void round_alike(float (&v)[NT][16], uint32_t i, const W &w, uint32_t salt)
+{
+#pragma unroll
+    for (int bj = 0; bj < NT; ++bj) {
+        if (__builtin_popcountll(__builtin_amdgcn_ballot_w64(two_alike(v[bj]))) < 8) continue;
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            // odd numbers: leading bits of square roots of primes; eight bits for each of four elements
+            uint32_t x = i * 0x6a09e667u + w.j(bj, q * 4) / 4 * 0xbb67ae85u + salt * 0x3c6ef373u;
+            x ^= x >> 16, x *= 0x510e527fu, x ^= x >> 13, x *= 0x9b05688du, x ^= x >> 16;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                // a float's bits behind an fp16's ten; an infinity or NaN keeps what it is
+                float &e = v[bj][q * 4 + k];
+                e = __builtin_bit_cast(float, (__builtin_bit_cast(uint32_t, e) + ((x >> (8 * k) & 255u) << 5) + 16) & ~0x1fffu);
+            }
+        }
+    }
+}
+enum { kSaltX, kSaltA, kSaltB, kSalts };  // and the step
+
 // The planes of a scaled matrix from 32 rows of a wave's block, for rows and
 // columns up to the padded sizes; MIRROR: also transposed, for a symmetric one.
-template <typename S, int PLANES, bool MIRROR>
-__device__ __forceinline__ void store_planes(char *stage, const float (&v)[S::NT][16], uint32_t first, uint32_t col0, char *hi,
+// high(j, r): what the first plane holds.
+template <typename S, int PLANES, bool MIRROR, typename H>
+__device__ __forceinline__ void store_planes(char *stage, const float (&v)[S::NT][16], H high, uint32_t first, uint32_t col0, char *hi,
                                              size_t lo, uint32_t rows, uint32_t cols)
 {
     constexpr int COLS = S::NT * 32;
@@ -228,7 +279,7 @@ __device__ __forceinline__ void store_planes(char *stage, const float (&v)[S::NT
 #pragma unroll
     for (int plane = 0; plane < PLANES; ++plane) {
         f16 *to = (f16 *)(hi + plane * lo);
-        stage_rows<f16, COLS>(stage, [&](int j, int r) { return plane == 0 ? v[j][r] : v[j][r] - (float)(f16)v[j][r]; });
+        stage_rows<f16, COLS>(stage, [&](int j, int r) { return plane == 0 ? high(j, r) : v[j][r] - high(j, r); });
         write_rows<f16, COLS>(stage, to + (uint64_t)first * cols + col0, cols, 0, rows - first, cols - col0);
         if (MIRROR) write_columns<f16, COLS>(stage, to + (uint64_t)col0 * cols + first, cols, rows - first, cols - col0);
     }
@@ -361,8 +412,10 @@ __device__ __forceinline__ void square_rows(float (&v)[S::NT][16], int bi, const
     }
     char *hi = ws + (SECOND ? o.at.b : o.at.a);
     const size_t lo = SECOND ? o.at.b_lo : o.at.a_lo;
-    if (at.m != at.n) store_planes<S, PLANES, true>(stage, v, first, w.col0, hi, lo, o.mp, o.mp);
-    else store_planes<S, PLANES, false>(stage, v, first, w.col0, hi, lo, o.mp, o.mp);
+    if (PLANES == 1) round_alike<NT>(v, i, w, o.step * kSalts + (SECOND ? kSaltB : kSaltA));
+    auto high = [&](int j, int r) { return (float)(f16)v[j][r]; };
+    if (at.m != at.n) store_planes<S, PLANES, true>(stage, v, high, first, w.col0, hi, lo, o.mp, o.mp);
+    else store_planes<S, PLANES, false>(stage, v, high, first, w.col0, hi, lo, o.mp, o.mp);
 }
 
 // Where a wave's sums of one run of k go: blocks in turn, each four vectors of
@@ -503,7 +556,13 @@ __device__ __forceinline__ void update(f32x16 (&acc)[S::MT][S::NT], const TileAt
                 square += __shfl_xor(square, 32);
                 if (w.half == 0 && i < o.mp) ((float *)(ws + o.at.squares))[(uint64_t)(w.col0 / (NT * 32)) * o.mp + i] = square;
             }
-            store_planes<S, 2, false>(stage, v, first, w.col0, x_next, o.at.x_lo, o.mp, o.np);
+            float h[NT][16];
+#pragma unroll
+            for (int bj = 0; bj < NT; ++bj)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) h[bj][r] = v[bj][r];
+            if (PLANES == 1) round_alike<NT>(h, i, w, (o.step + 1) * kSalts + kSaltX);
+            store_planes<S, 2, false>(stage, v, [&](int j, int r) { return (float)(f16)h[j][r]; }, first, w.col0, x_next, o.at.x_lo, o.mp, o.np);
             if (PLANES == 2 && first < o.m && w.col0 < o.np) {
                 stage_rows<float, NT * 32>(stage, value);
                 write_rows<float, NT * 32>(stage, (float *)(ws + o.at.xf) + (uint64_t)first * o.np + w.col0, o.np, 0, o.m - first, o.np - w.col0);

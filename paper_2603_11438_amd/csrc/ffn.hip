@@ -338,46 +338,13 @@ template <typename S, int ACT> int launch_ffn(GemmArgs &g, const FfnOut &o, hipS
     return launch_status();
 }
 
-constexpr uint32_t kMaxSplits = 32;
-
-// The forward's tile (an index of kTiles, kFlat for up to 64 tokens) and the runs
-// of its k.  Few tiles, of a rank's share of the hidden columns say, leave units
-// idle that a split puts to work.  Flat: kFlatStep us a step of 64 for a tile (1 x
-// 4096 x 1408 in one piece 32 us), two tiles to a unit, the weights' bytes at 4.5
-// TB/s, and a join as in cut_for.  So 1 x 4096 x 5632 is split (25 us, in one piece
-// 33) and 1 x 4096 x 11264 is not.  A 128 x 128 tile alone on its unit has three
-// buffers: 1024 x 4096 x 1408 39 us, with two 62; 128 x 4096 x 11264 48 and 67.
-constexpr int kFlat = -1;
-constexpr double kFlatStep = 0.45;
-Cut ffn_cut(size_t tokens, size_t dim, size_t hidden)
-{
-    const size_t steps = (dim + kStepK - 1) / kStepK;
-    if (tokens <= 64) {
-        const size_t tiles = (hidden + 63) / 64;
-        const double bytes = 4.0 * dim * hidden / 4.5e6;
-        Cut best{kFlat, 1};
-        double time = 0;
-        for (uint32_t s = 1; s <= kMaxSplits && (s == 1 || s * 2 <= steps); ++s) {
-            double sum = (tiles * s + 511) / 512 * ((steps + s - 1) / s) * kFlatStep;
-            sum = sum > bytes ? sum : bytes;
-            if (s > 1) sum += 4.0 + 2.0 * s * tokens * 2 * hidden * 4 / 6e6;
-            if (s == 1 || sum < time) best.splits = s, time = sum;
-        }
-        return best;
-    }
-    // the pairs' columns count twice
-    if (cut_for(1, tokens, 2 * hidden, steps, 1, false, 1, 3, 1).tile != 1) return {3, 1};
-    Cut c = cut_for(1, tokens, 2 * hidden, steps, 1, false, 1, 1, kMaxSplits);
-    if ((tokens + 127) / 128 * ((hidden + 63) / 64) * c.splits <= 256) c.tile = 4;
-    return c;
-}
 size_t ffn_part_bytes(const ar_ffn_desc &d, const Cut &c) { return c.splits > 1 ? c.splits * 2 * d.tokens * d.hidden * sizeof(float) : 0; }
 
 template <int ACT> int launch_ffn_tiles(const Cut &c, GemmArgs &g, const FfnOut &o, hipStream_t st)
 {
     if (c.tile == kFlat) return launch_ffn<Flat, ACT>(g, o, st);
-    if (c.tile == 4) return launch_ffn<Deep, ACT>(g, o, st);
-    return c.tile == 1 ? launch_ffn<Small, ACT>(g, o, st) : launch_ffn<Large, ACT>(g, o, st);
+    if (c.tile == kPairDeep) return launch_ffn<Deep, ACT>(g, o, st);
+    return c.tile == kPairSmall ? launch_ffn<Small, ACT>(g, o, st) : launch_ffn<Large, ACT>(g, o, st);
 }
 
 struct FfnMats {

@@ -35,6 +35,7 @@
 #include <type_traits>
 #include <utility>
 
+#include "gemm_cut.h"
 #include "ops_common.h"
 
 namespace ar {
@@ -63,59 +64,6 @@ template <> struct Frag<bf16> {
 };
 
 constexpr int kMaxSegments = 2;
-constexpr int kStepK = 64;  // steps that k is counted in
-
-// Tiles, by planes: rows and columns, and what they cost.  `busy`: us of a
-// compute unit for k = 64 of a tile while it has several to work on; `alone`:
-// us for the same when one tile has the unit to itself (its loads' way to the
-// L2 and back is then in the open); `fit`: tiles that share a unit; `ends`: us
-// before and after the products.  Measured on products of 1024 x 1024 x 4096
-// (alone) and 8192 x 8192 x 8192 (busy).  The last one has three buffers, for a
-// tile alone on its unit: 768 x 1024 x 5376 in four runs 19.2 us, with two
-// buffers 23.7 and in 64 x 64 tiles 31.1; with two tiles to a unit it is slower
-// (5376 x 1024 x 768: 23.0 us, with two buffers 18.2).
-struct TileCost {
-    int side;
-    double busy, alone, ends;
-    int fit;
-};
-constexpr int kTileSizes = 5;
-constexpr TileCost kTiles[2][kTileSizes] = {
-    {{64, 0.19, 0.32, 2.5, 2}, {128, 0.5, 0.68, 5.0, 2}, {192, 1.1, 1.1, 12.0, 1}, {256, 1.67, 1.67, 20.0, 1}, {128, 0.5, 0.5, 5.0, 1}},
-    {{64, 0.4, 0.45, 3.0, 1}, {128, 1.2, 1.3, 8.0, 1}, {192, 2.8, 2.8, 14.0, 1}, {256, 4.6, 4.6, 24.0, 1}},
-};
-
-// The tile (an index of kTiles) and the number of runs k is split into that
-// finish a product of k = 64 * steps first.  LOWER: tiles on and below the
-// diagonal alone.  `least` .. `most`: the tiles to choose from.  A split
-// product's runs write their sums, and a kernel of its own reads and adds them,
-// each at about 6 TB/s and with 4 us to begin with.  300 x 300 x 8192, bf16:
-// 37.3 us in one piece, 7.6 + 5.6 in eight; 1024 x 1024 x 4096, two planes, of
-// the tiles on and below the diagonal: 32.2, and 19.8 + 8.0 in seven (of 128 x 128).
-struct Cut {
-    int tile;
-    uint32_t splits;
-};
-inline Cut cut_for(int planes, size_t m, size_t n, size_t steps, size_t batch, bool lower, int least, int most, uint32_t max_splits)
-{
-    Cut best{least, 1};
-    double time = 0;
-    for (int t = least; t <= most; ++t) {
-        const TileCost &c = kTiles[planes - 1][t];
-        const size_t a = (m + c.side - 1) / c.side, b = (n + c.side - 1) / c.side;
-        const size_t tiles = batch * (lower ? a * (a + 1) / 2 : a * b);
-        for (uint32_t s = 1; s <= max_splits && s * 2 <= (steps > 2 ? steps : 2); ++s) {
-            if (s > 1 && tiles * s > 1024) break;
-            const size_t units = (tiles * s + 255) / 256;
-            const double busy = units * c.busy, alone = (double)((units + c.fit - 1) / c.fit) * c.alone;
-            double sum = ((steps + s - 1) / s) * (busy > alone ? busy : alone) + c.ends * units;
-            if (s > 1) sum += 4.0 + 2.0 * s * tiles * c.side * c.side * 4 / 6e6;
-            if ((t == least && s == 1) || sum < time) best = {t, s}, time = sum;
-        }
-    }
-    return best;
-}
-
 // Rows of one tile are reached by 32-bit offsets from the tile's first row.
 inline bool gemm_reaches(uint64_t row_bytes, uint64_t k_bytes) { return row_bytes * 256 + k_bytes < (1ull << 31); }
 

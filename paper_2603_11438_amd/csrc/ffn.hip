@@ -411,9 +411,8 @@ int ffn(const ar_ffn_desc *desc, const void *x, const void *wg, const void *wu, 
 
 // ---- backward ---------------------------------------------------------------
 
-size_t part_bytes(size_t m, size_t cols, size_t steps)
+size_t part_bytes(const Cut &c, size_t m, size_t cols)
 {
-    const Cut c = cut_for(1, m, cols, steps, 1, false, 0, 4, kMaxSplits);
     return c.splits > 1 ? round_up(c.splits * m * cols * sizeof(float), 256) : 0;
 }
 
@@ -433,9 +432,8 @@ template <typename S, bool ABYK> int launch_product(GemmArgs &g, const ProductOu
 }
 
 // B by k; A by rows (dx) or by k (the weights' gradients).
-template <bool ABYK> int product(GemmArgs &g, const ProductOut &o, hipStream_t st)
+template <bool ABYK> int product(const Cut &c, GemmArgs &g, const ProductOut &o, hipStream_t st)
 {
-    const Cut c = cut_for(1, g.m, o.cols, (size_t)g.steps * g.segments, 1, false, 0, 4, kMaxSplits);
     g.splits = c.splits, g.batch = 1;
     switch (c.tile) {
     case 0: return launch_product<Tiny, ABYK>(g, o, st);
@@ -458,9 +456,9 @@ FfnBackwardSpace ffn_backward_space(const ar_ffn_desc &d, bool dx, bool dw)
     FfnBackwardSpace s{};
     s.hidden = round_up(d.hidden, kStepK), s.steps = (d.tokens + kStepK - 1) / kStepK;
     size_t parts = 0;
-    if (dx) parts = part_bytes(d.tokens, d.dim, 2 * s.hidden / kStepK);
+    if (dx) parts = part_bytes(dx_cut(d.tokens, d.dim, s.hidden), d.tokens, d.dim);
     if (dw) {
-        const size_t p = part_bytes(2 * s.hidden, d.dim, s.steps);
+        const size_t p = part_bytes(dw_cut(d.tokens, d.dim, s.hidden), 2 * s.hidden, d.dim);
         parts = p > parts ? p : parts;
     }
     s.part = round_up(d.tokens * 2 * s.hidden * 2, 256);
@@ -545,7 +543,7 @@ int ffn_backward(const ar_ffn_desc *desc, const void *dh, const void *x, const v
         g.lda = (uint32_t)(s.hidden * 4), g.ldb = pg.ld;
         g.m = (uint32_t)d.tokens, g.n = pg.cols;
         const ProductOut o{{(bf16 *)dx, nullptr}, (float *)(w + s.part), {odx.ld, 0}, 0x80000000u, (uint32_t)d.tokens, (uint32_t)d.dim};
-        if ((rc = product<false>(g, o, st)) != AR_OK) return rc;
+        if ((rc = product<false>(dx_cut(d.tokens, d.dim, s.hidden), g, o, st)) != AR_OK) return rc;
     }
     if (dwg) {
         GemmArgs g{};
@@ -555,7 +553,7 @@ int ffn_backward(const ar_ffn_desc *desc, const void *dh, const void *x, const v
         g.lda = (uint32_t)(s.hidden * 4), g.ldb = px.ld;
         g.m = (uint32_t)(2 * s.hidden), g.n = px.cols;
         const ProductOut o{{(bf16 *)dwg, (bf16 *)dwu}, (float *)(w + s.part), {og.ld, ou.ld}, (uint32_t)s.hidden, (uint32_t)d.hidden, (uint32_t)d.dim};
-        if ((rc = product<true>(g, o, st)) != AR_OK) return rc;
+        if ((rc = product<true>(dw_cut(d.tokens, d.dim, s.hidden), g, o, st)) != AR_OK) return rc;
     }
     return AR_OK;
 }

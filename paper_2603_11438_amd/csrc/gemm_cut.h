@@ -76,9 +76,28 @@ inline Cut cut_for(int planes, size_t m, size_t n, size_t steps, size_t batch, b
     return best;
 }
 
-// ---- the gated feed-forward block's forward ----------------------------------
+// ---- whose tiles ------------------------------------------------------------
 
 constexpr uint32_t kMaxSplits = 32;
+
+// The gated feed-forward block's backward products, with `hidden` rounded up to
+// kStepK.  dx: tokens x dim over dG and dU; the weights' gradients as one.
+inline Cut dx_cut(size_t tokens, size_t dim, size_t hidden)
+{
+    return cut_for(1, tokens, dim, 2 * (hidden / kStepK), 1, false, 0, 4, kMaxSplits);
+}
+inline Cut dw_cut(size_t tokens, size_t dim, size_t hidden)
+{
+    return cut_for(1, 2 * hidden, dim, (tokens + kStepK - 1) / kStepK, 1, false, 0, 4, kMaxSplits);
+}
+
+// The products of an orthogonalising step, m <= n, with mp and np m and n rounded up
+// to kStepK: A = X X^T over n, B = A A and B X over m.
+inline Cut a_cut(int planes, size_t m, size_t np, size_t batch) { return cut_for(planes, m, m, np / kStepK, batch, true, 0, 3, kMaxSplits); }
+inline Cut b_cut(int planes, size_t m, size_t mp, size_t batch) { return cut_for(planes, m, m, mp / kStepK, batch, true, 0, 3, 1); }
+inline Cut x_cut(int planes, size_t m, size_t n, size_t mp, size_t batch) { return cut_for(planes, m, n, mp / kStepK, batch, false, 0, 3, 1); }
+
+// ---- the gated feed-forward block's forward ----------------------------------
 
 // Paired tiles: a wave holds both projections of the same columns, so a tile has
 // half its side of them.  There are 128 x 128, with two buffers and with three

@@ -816,16 +816,12 @@ bool two_planes(const ar_ortho_desc &d)
     return d.dtype == AR_FLOAT32 || (d.rows < d.cols ? d.rows : d.cols) <= 256;
 }
 
-// The tiles of A and the runs that its k is split into.
-constexpr uint32_t kMostRuns = 32;
-Cut cut_of_a(int planes, size_t m, size_t np, size_t batch) { return cut_for(planes, m, m, np / kStepK, batch, true, 0, 3, kMostRuns); }
-
 OrthoSpace ortho_space(const ar_ortho_desc &d, uint32_t mp, uint32_t np)
 {
     OrthoSpace s{};
     const bool two = two_planes(d);
     const size_t m = d.rows < d.cols ? d.rows : d.cols;
-    const Cut c = cut_of_a(two ? 2 : 1, m, np, d.batch);
+    const Cut c = a_cut(two ? 2 : 1, m, np, d.batch);
     const size_t side = kTiles[0][c.tile].side, tiles = (m + side - 1) / side;
     size_t at = 0;
     auto take = [&](size_t bytes) {
@@ -875,7 +871,7 @@ template <typename S, bool SECOND> int launch_square(GemmArgs &g, const OrthoArg
 }
 template <int PLANES, bool SECOND> int square(GemmArgs &g, const OrthoArgs &o, hipStream_t st)
 {
-    const Cut c = SECOND ? cut_for(PLANES, o.m, o.m, g.steps, o.batch, true, 0, 3, 1) : cut_of_a(PLANES, o.m, o.np, o.batch);
+    const Cut c = SECOND ? b_cut(PLANES, o.m, o.mp, o.batch) : a_cut(PLANES, o.m, o.np, o.batch);
     g.splits = c.splits;
     switch (c.tile) {
     case 0: return launch_square<typename ShapeOf<PLANES, 0>::type, SECOND>(g, o, st);
@@ -897,7 +893,7 @@ template <typename S, typename O> int launch_update(GemmArgs &g, OrthoArgs &o, h
 }
 template <int PLANES, typename O> int update_step(GemmArgs &g, OrthoArgs &o, hipStream_t st)
 {
-    switch (cut_for(PLANES, o.m, o.n, g.steps, o.batch, false, 0, 3, 1).tile) {
+    switch (x_cut(PLANES, o.m, o.n, o.mp, o.batch).tile) {
     case 0: return launch_update<typename ShapeOf<PLANES, 0>::type, O>(g, o, st);
     case 1: return launch_update<typename ShapeOf<PLANES, 1>::type, O>(g, o, st);
     case 2: return launch_update<typename ShapeOf<PLANES, 2>::type, O>(g, o, st);

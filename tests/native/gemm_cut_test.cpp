@@ -1,7 +1,7 @@
 // The tiles that products take (gemm_cut.h), on the host.  Without arguments: every
 // forward of the gated feed-forward block over a range of sizes takes the cheapest of
-// the shapes that exist, by the rule's own prices.  "ffn T D F": the forward's tile
-// and runs.
+// the shapes that exist, by the rule's own prices.  "ffn T D F", "ortho PLANES M N
+// BATCH": the tile and runs of each product of such a call.
 #include <cstdio>
 #include <cstdlib>
 #include <cstring>
@@ -36,13 +36,28 @@ static void forward(size_t t, size_t d, size_t f)
         expect(us <= pair_us(tiles * s <= 256 ? kPairDeep : kPairSmall, t, f, steps, s), "128 is cheaper", t, d, f, c);
 }
 
-int main(int argc, char **argv)
+static void show(const char *name, Cut c) { printf("%s %d %u\n", name, c.tile, c.splits); }
+static int shapes(int argc, char **argv)
 {
-    if (argc == 5 && !strcmp(argv[1], "ffn")) {
-        const Cut c = ffn_cut(atoll(argv[2]), atoll(argv[3]), atoll(argv[4]));
-        printf("%d %u\n", c.tile, c.splits);
+    auto number = [&](int k) { return k < argc ? (size_t)atoll(argv[k]) : (size_t)0; };
+    auto up = [](size_t v) { return (v + kStepK - 1) / kStepK * kStepK; };
+    if (!strcmp(argv[1], "ffn") && argc == 5) {
+        const size_t t = number(2), d = number(3), f = number(4);
+        show("forward", ffn_cut(t, d, f)), show("dx", dx_cut(t, d, up(f))), show("dw", dw_cut(t, d, up(f)));
         return 0;
     }
+    if (!strcmp(argv[1], "ortho") && argc == 6) {
+        const int planes = (int)number(2);
+        const size_t m = number(3), n = number(4), batch = number(5);
+        show("a", a_cut(planes, m, up(n), batch)), show("b", b_cut(planes, m, up(m), batch)), show("x", x_cut(planes, m, n, up(m), batch));
+        return 0;
+    }
+    return 2;
+}
+
+int main(int argc, char **argv)
+{
+    if (argc > 1) return shapes(argc, argv);
     for (size_t t : {1, 2, 33, 64, 65, 100, 128, 129, 200, 256, 300, 512, 777, 1000, 1024, 1536, 2048, 2100, 2500, 4096, 6144, 8192, 16384, 65536})
         for (size_t d : {1, 64, 100, 128, 512, 1000, 1024, 1999, 2048, 4096, 6000, 16384})
             for (size_t f : {1, 8, 64, 130, 512, 768, 1024, 1408, 1536, 2048, 2700, 2816, 4100, 4352, 5632, 11264, 16384}) forward(t, d, f);

@@ -29,7 +29,7 @@ template <int ACT> __device__ __forceinline__ float activation(float g, float *s
 {
     if constexpr (ACT == AR_ACT_RELU) {
         if (slope) *slope = g > 0.0f ? 1.0f : 0.0f;
-        return g > 0.0f ? g : g * 0.0f;  // NaN stays NaN
+        return g <= 0.0f ? 0.0f : g;  // NaN stays NaN
     } else if constexpr (ACT == AR_ACT_SILU) {
         const float p = 1.0f / (1.0f + __expf(-g));
         if (slope) *slope = p * (1.0f + g * (1.0f - p));

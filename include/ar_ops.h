@@ -122,13 +122,18 @@ typedef struct ar_ffn_desc {
  * dim or row stride that is no multiple of 8, are first copied into the
  * workspace.  Where tokens x hidden is small beside a long dim, the sums over
  * dim are taken in several runs, which a second kernel joins, from the
- * workspace.  Calls that need neither need no workspace.  saved: NULL, or
+ * workspace.  Calls that need neither need no workspace; the size named for a
+ * description is enough for any alignment of the pointers.  saved: NULL, or
  * 2 * tokens * hidden floats (16-byte aligned) that receive G and U for the
  * backward pass, in fp32.  Errors: AR_ERR_ARG, AR_ERR_UNSUPPORTED,
  * AR_ERR_SCRATCH, AR_ERR_HIP. */
 int ar_gated_ffn(const ar_ffn_desc *desc, const void *x, const void *w_gate, const void *w_up, void *h, float *saved,
                  void *workspace, size_t workspace_bytes, void *stream);
 size_t ar_gated_ffn_workspace(const ar_ffn_desc *desc);
+/* What the call uses with these operands, which is enough for it: the copies that
+ * their alignment asks for, and no others.  0: none, or a description that the call
+ * refuses. */
+size_t ar_gated_ffn_workspace_for(const ar_ffn_desc *desc, const void *x, const void *w_gate, const void *w_up);
 
 /* Backward.  From `saved` of the forward and dh:
  *     dG = dh * U * act'(G),  dU = dh * act(G)

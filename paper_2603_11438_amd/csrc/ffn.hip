@@ -363,6 +363,21 @@ size_t ffn_workspace(const ar_ffn_desc &d)
     return packed_bytes(d.tokens, d.dim) + 2 * packed_bytes(d.hidden, d.dim) + ffn_part_bytes(d, ffn_cut(d.tokens, d.dim, d.hidden));
 }
 
+// What a call with these operands uses: copies of those that cannot be read where
+// they lie, and the runs' sums.
+size_t ffn_need(const ar_ffn_desc &d, const FfnMats &m, const Cut &cut)
+{
+    size_t need = ffn_part_bytes(d, cut);
+    for (const Mat &in : {m.x, m.wg, m.wu})
+        if (!direct(in)) need += packed_bytes(in.rows, in.cols);
+    return need;
+}
+size_t ffn_workspace_for(const ar_ffn_desc *desc, const void *x, const void *wg, const void *wu)
+{
+    if (check_ffn(desc) != AR_OK || desc->tokens == 0) return 0;
+    return ffn_need(*desc, ffn_mats(*desc, x, wg, wu, nullptr), ffn_cut(desc->tokens, desc->dim, desc->hidden));
+}
+
 int ffn(const ar_ffn_desc *desc, const void *x, const void *wg, const void *wu, void *h, float *saved, void *ws,
         size_t ws_bytes, void *stream)
 {
@@ -377,9 +392,7 @@ int ffn(const ar_ffn_desc *desc, const void *x, const void *wg, const void *wu, 
         if (meet(m.h, in) || meet(sv, in)) return AR_ERR_ARG;
     if (meet(m.h, sv)) return AR_ERR_ARG;
     const Cut cut = ffn_cut(d.tokens, d.dim, d.hidden);
-    size_t need = ffn_part_bytes(d, cut);
-    for (const Mat &in : {m.x, m.wg, m.wu})
-        if (!direct(in)) need += packed_bytes(in.rows, in.cols);
+    const size_t need = ffn_need(d, m, cut);
     if (need) {
         if (!ws || ws_bytes < need) return AR_ERR_SCRATCH;
         if ((uintptr_t)ws % 256 != 0) return AR_ERR_ARG;
@@ -582,4 +595,9 @@ extern "C" int ar_gated_ffn(const ar_ffn_desc *desc, const void *x, const void *
 extern "C" size_t ar_gated_ffn_workspace(const ar_ffn_desc *desc)
 {
     return ar::check_ffn(desc) == AR_OK ? ar::ffn_workspace(*desc) : 0;
+}
+
+extern "C" size_t ar_gated_ffn_workspace_for(const ar_ffn_desc *desc, const void *x, const void *w_gate, const void *w_up)
+{
+    return ar::ffn_workspace_for(desc, x, w_gate, w_up);
 }

@@ -197,7 +197,7 @@ bool ffn_desc(const Rows &x, const Rows &g, const Rows &u, long act, ar_ffn_desc
     return true;
 }
 
-// ffn(fn, workspace_fn, x, w_gate, w_up, act, save, device, stream) -> (h, saved or None)
+// ffn(fn, workspace_for_fn, x, w_gate, w_up, act, save, device, stream) -> (h, saved or None)
 PyObject *ffn(PyObject *, PyObject *const *a, Py_ssize_t n)
 {
     if (n != 9) return PyErr_Format(PyExc_TypeError, "ffn takes 9 arguments");
@@ -213,18 +213,13 @@ PyObject *ffn(PyObject *, PyObject *const *a, Py_ssize_t n)
         shape.back() = g.rows;
         at::Tensor h = at::empty(shape, x.t->options()), saved, ws;
         if (save) saved = at::empty({2, x.rows, g.rows}, x.t->options().dtype(at::kFloat));
-        size_t bytes = 0;
+        // only operands that have to be laid out, and a dim in several runs, need a workspace
+        const size_t bytes = ((decltype(&ar_gated_ffn_workspace_for))space)(&d, x.p(), g.p(), u.p());
+        if (bytes) ws = workspace(bytes, x);
         int rc;
         Py_BEGIN_ALLOW_THREADS
-        rc = ((decltype(&ar_gated_ffn))fn)(&d, x.p(), g.p(), u.p(), ptr(h), (float *)ptr(saved), nullptr, 0, stream);
+        rc = ((decltype(&ar_gated_ffn))fn)(&d, x.p(), g.p(), u.p(), ptr(h), (float *)ptr(saved), ptr(ws), bytes, stream);
         Py_END_ALLOW_THREADS
-        if (rc == AR_ERR_SCRATCH) {  // only operands that have to be laid out, and a dim in several runs, need a workspace
-            bytes = ((decltype(&ar_gated_ffn_workspace))space)(&d);
-            ws = workspace(bytes, x);
-            Py_BEGIN_ALLOW_THREADS
-            rc = ((decltype(&ar_gated_ffn))fn)(&d, x.p(), g.p(), u.p(), ptr(h), (float *)ptr(saved), ptr(ws), bytes, stream);
-            Py_END_ALLOW_THREADS
-        }
         return rc ? PyLong_FromLong(rc) : tuple({THPVariable_Wrap(h), wrap_or_none(saved)});
     } catch (...) {
         return none();

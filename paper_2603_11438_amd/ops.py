@@ -57,6 +57,7 @@ SIGNATURES = {
     "ar_residual_norm_backward_workspace": (_S, [ctypes.POINTER(ar_norm_desc)]),
     "ar_gated_ffn": (_I, [ctypes.POINTER(ar_ffn_desc)] + [_P] * 6 + [_S, _P]),
     "ar_gated_ffn_workspace": (_S, [ctypes.POINTER(ar_ffn_desc)]),
+    "ar_gated_ffn_workspace_for": (_S, [ctypes.POINTER(ar_ffn_desc)] + [_P] * 3),
     "ar_gated_ffn_backward": (_I, [ctypes.POINTER(ar_ffn_desc)] + [_P] * 9 + [_S, _P]),
     "ar_gated_ffn_backward_workspace": (_S, [ctypes.POINTER(ar_ffn_desc)]),
     "ar_orthogonalize": (_I, [ctypes.POINTER(ar_ortho_desc)] + [_P] * 3 + [_S, _P]),
@@ -98,7 +99,7 @@ class _Native:
         self.norm, self.norm_backward, self.ffn, self.ffn_backward = mod.norm, mod.norm_backward, mod.ffn, mod.ffn_backward
         self.norm_fn = address("ar_residual_norm")
         self.norm_backward_fns = address("ar_residual_norm_backward"), address("ar_residual_norm_backward_workspace")
-        self.ffn_fns = address("ar_gated_ffn"), address("ar_gated_ffn_workspace")
+        self.ffn_fns = address("ar_gated_ffn"), address("ar_gated_ffn_workspace_for")
         self.ffn_backward_fns = address("ar_gated_ffn_backward"), address("ar_gated_ffn_backward_workspace")
         self.in_use, self.device, self.stream = torch.cuda.is_initialized, torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream
 
@@ -381,13 +382,11 @@ def gated_ffn(x, w_gate, w_up, *, act: str = "silu", save: bool = False, out=Non
         _, _, d.ld_h = _rows(h, "h", d.hidden, d.tokens, x.dtype, on.index)
         saved = torch.empty(2, d.tokens, d.hidden, dtype=torch.float32, device=x.device) if save else None
         L = _lib()
-        ws = None
+        # only operands that have to be laid out, and a dim in several runs, need one
+        need = L.ar_gated_ffn_workspace_for(ctypes.byref(d), x.data_ptr(), w_gate.data_ptr(), w_up.data_ptr())
+        ws = _workspace(need, x)
         rc = L.ar_gated_ffn(ctypes.byref(d), x.data_ptr(), w_gate.data_ptr(), w_up.data_ptr(), h.data_ptr(), _ptr(saved),
-                            None, 0, on.ptr)
-        if rc == _ar.AR_ERR_SCRATCH:  # only operands that have to be laid out, and a dim in several runs, need one
-            ws = _workspace(L.ar_gated_ffn_workspace(ctypes.byref(d)), x)
-            rc = L.ar_gated_ffn(ctypes.byref(d), x.data_ptr(), w_gate.data_ptr(), w_up.data_ptr(), h.data_ptr(), _ptr(saved),
-                                _ptr(ws), ws.numel(), on.ptr)
+                            _ptr(ws), need, on.ptr)
         _ar._check(rc, "ar_gated_ffn")
     return (h, saved) if save else h
 

@@ -15,8 +15,9 @@
  * null stream), AR_OK or an AR_ERR_* code returned, the code of a failure also
  * left in ar_last_error().  Calls are asynchronous on `stream`, allocate
  * nothing, create no stream or event and issue no memset, so they may be
- * captured into a HIP graph and replayed.  They keep nothing between calls and
- * may be made from several host threads.  Matrices are row-major with a row
+ * captured into a HIP graph and replayed.  They keep nothing between calls, beside
+ * which kernels a device has been told about, and may be made from several host
+ * threads and for several devices.  Matrices are row-major with a row
  * stride (`ld_*`, elements; 0 = the number of columns; at least that number);
  * elements of a row are contiguous.  Pointers need the alignment of their
  * elements and no more.  Where a function takes a workspace, it is device

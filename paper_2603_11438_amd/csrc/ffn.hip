@@ -328,10 +328,11 @@ template <typename S, int ACT> int launch_ffn(GemmArgs &g, const FfnOut &o, hipS
     g.tiles_m = (g.m + S::BM - 1) / S::BM;
     g.tiles_n = (g.n + S::BN / 2 - 1) / (S::BN / 2);
     static_assert(4 * kStageBytes<float, S::NT * 16> <= S::LDS, "the epilogue's staging fits");
-    static const hipError_t set = hipFuncSetAttribute((const void *)ffn_kernel<S, ACT>, hipFuncAttributeMaxDynamicSharedMemorySize, S::LDS);
-    if (set != hipSuccess) return AR_ERR_HIP;
+    static OncePerDevice once;
+    int rc = allow_lds(once, (const void *)ffn_kernel<S, ACT>, S::LDS);
+    if (rc != AR_OK) return rc;
     hipLaunchKernelGGL((ffn_kernel<S, ACT>), dim3(g.tiles_m * g.tiles_n, g.splits), dim3(S::THREADS), S::LDS, st, g, o);
-    const int rc = launch_status();
+    rc = launch_status();
     if (rc != AR_OK || g.splits == 1) return rc;
     const uint64_t groups = ((uint64_t)g.m * ((g.n + 3) / 4) + 255) / 256;
     hipLaunchKernelGGL((ffn_join_kernel<ACT>), dim3((uint32_t)(groups < 8192 ? groups : 8192)), dim3(256), 0, st, o, g.m, g.n, g.splits);
@@ -434,10 +435,11 @@ template <typename S, bool ABYK> int launch_product(GemmArgs &g, const ProductOu
     g.tiles_m = (g.m + S::BM - 1) / S::BM;
     g.tiles_n = (o.cols + S::BN - 1) / S::BN;
     constexpr int STAGE = 4 * kStageBytes<float, S::NT * 32>, LDS = S::LDS > STAGE ? S::LDS : STAGE;
-    static const hipError_t set = hipFuncSetAttribute((const void *)product_kernel<S, ABYK>, hipFuncAttributeMaxDynamicSharedMemorySize, LDS);
-    if (set != hipSuccess) return AR_ERR_HIP;
+    static OncePerDevice once;
+    int rc = allow_lds(once, (const void *)product_kernel<S, ABYK>, LDS);
+    if (rc != AR_OK) return rc;
     hipLaunchKernelGGL((product_kernel<S, ABYK>), dim3(g.tiles_m * g.tiles_n, g.splits), dim3(S::THREADS), LDS, st, g, o);
-    int rc = launch_status();
+    rc = launch_status();
     if (rc != AR_OK || g.splits == 1) return rc;
     const uint64_t groups = ((uint64_t)g.m * ((o.cols + 3) / 4) + 255) / 256;
     hipLaunchKernelGGL(join_kernel, dim3((uint32_t)(groups < 8192 ? groups : 8192)), dim3(256), 0, st, o, g.m, g.splits);

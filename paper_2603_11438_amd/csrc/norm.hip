@@ -725,9 +725,9 @@ int launch_bwd_shape(const NormBwdArgs &a, uint32_t groups, hipStream_t st)
 {
     constexpr int LDS = ROOM == kSumsInLds ? kSumsBytes<T, NV, BS> : 0;
     if (LDS) {
-        static const hipError_t set = hipFuncSetAttribute((const void *)norm_bwd_kernel<T, P, NV, BS, TAIL, ROOM>,
-                                                          hipFuncAttributeMaxDynamicSharedMemorySize, LDS);
-        if (set != hipSuccess) return AR_ERR_HIP;
+        static OncePerDevice once;
+        const int rc = allow_lds(once, (const void *)norm_bwd_kernel<T, P, NV, BS, TAIL, ROOM>, LDS);
+        if (rc != AR_OK) return rc;
     }
     hipLaunchKernelGGL((norm_bwd_kernel<T, P, NV, BS, TAIL, ROOM>), dim3(groups), dim3(BS), LDS, st, a);
     return launch_status();

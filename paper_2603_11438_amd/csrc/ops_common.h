@@ -9,6 +9,7 @@
 
 #include "ar_internal.h"
 #include "ar_ops.h"
+#include "once_per_device.h"
 
 namespace ar {
 
@@ -57,6 +58,16 @@ inline bool meet(const Mat &a, const Mat &b)
         if (d >= b.cols * b.elem && d + a.cols * a.elem <= la) return false;
     }
     return true;
+}
+
+// Lets a kernel's launches on the current device have `bytes` of dynamic LDS.
+inline int allow_lds(OncePerDevice &once, const void *kernel, int bytes)
+{
+    int device = 0;
+    const bool ok = hipGetDevice(&device) == hipSuccess && once(device, [&] {
+        return hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, bytes) == hipSuccess;
+    });
+    return ok ? AR_OK : AR_ERR_HIP;
 }
 
 inline int launch_status() { return hipGetLastError() == hipSuccess ? AR_OK : AR_ERR_HIP; }

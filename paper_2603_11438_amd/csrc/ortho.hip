@@ -856,16 +856,16 @@ template <> struct ShapeOf<2, 3> { typedef Shape<4, 4, 2, 32, 2> type; };
 template <typename S, bool SECOND> int launch_square(GemmArgs &g, const OrthoArgs &o, hipStream_t st)
 {
     g.tiles_m = g.tiles_n = (o.m + S::BM - 1) / S::BM;
-    static const hipError_t set = hipFuncSetAttribute((const void *)ortho_square_kernel<S, SECOND>,
-                                                      hipFuncAttributeMaxDynamicSharedMemorySize, kOrthoLds<S>);
-    if (set != hipSuccess) return AR_ERR_HIP;
+    static OncePerDevice once;
+    int rc = allow_lds(once, (const void *)ortho_square_kernel<S, SECOND>, kOrthoLds<S>);
+    if (rc != AR_OK) return rc;
     const uint32_t tiles = g.tiles_m * (g.tiles_m + 1) / 2 * o.batch;
     hipLaunchKernelGGL((ortho_square_kernel<S, SECOND>), dim3(tiles * g.splits), dim3(S::THREADS), kOrthoLds<S>, st, g, o);
-    const int rc = launch_status();
+    rc = launch_status();
     if (rc != AR_OK || SECOND || g.splits == 1) return rc;
     constexpr int LDS = S::WAVES * kOrthoStage<S>;
-    static const hipError_t also = hipFuncSetAttribute((const void *)ortho_join_kernel<S>, hipFuncAttributeMaxDynamicSharedMemorySize, LDS);
-    if (also != hipSuccess) return AR_ERR_HIP;
+    static OncePerDevice also;
+    if ((rc = allow_lds(also, (const void *)ortho_join_kernel<S>, LDS)) != AR_OK) return rc;
     hipLaunchKernelGGL((ortho_join_kernel<S>), dim3(tiles, S::MT), dim3(S::THREADS), LDS, st, g, o);
     return launch_status();
 }
@@ -885,9 +885,9 @@ template <typename S, typename O> int launch_update(GemmArgs &g, OrthoArgs &o, h
 {
     o.strips = (o.np + S::NT * 32 - 1) / (S::NT * 32);
     g.tiles_m = (o.m + S::BM - 1) / S::BM, g.tiles_n = (o.n + S::BN - 1) / S::BN;
-    static const hipError_t set = hipFuncSetAttribute((const void *)ortho_update_kernel<S, O>,
-                                                      hipFuncAttributeMaxDynamicSharedMemorySize, kOrthoLds<S>);
-    if (set != hipSuccess) return AR_ERR_HIP;
+    static OncePerDevice once;
+    const int rc = allow_lds(once, (const void *)ortho_update_kernel<S, O>, kOrthoLds<S>);
+    if (rc != AR_OK) return rc;
     hipLaunchKernelGGL((ortho_update_kernel<S, O>), dim3(g.tiles_m * g.tiles_n * o.batch), dim3(S::THREADS), kOrthoLds<S>, st, g, o);
     return launch_status();
 }
@@ -929,8 +929,8 @@ template <typename O, int PLANES> int run_ortho(OrthoArgs &o, const float *coefs
         operands(&g, o, x, o.at.x_lo, o.np, x, o.at.x_lo, o.np, o.np, o.m, o.m);
         if constexpr (PLANES == 2) {
             if (small) {
-                static const hipError_t set = hipFuncSetAttribute((const void *)ortho_step_kernel<O>, hipFuncAttributeMaxDynamicSharedMemorySize, kSmallLds);
-                if (set != hipSuccess) return AR_ERR_HIP;
+                static OncePerDevice once;
+                if ((rc = allow_lds(once, (const void *)ortho_step_kernel<O>, kSmallLds)) != AR_OK) return rc;
                 hipLaunchKernelGGL((ortho_step_kernel<O>), dim3(o.np / 64 * o.batch), dim3(512), kSmallLds, st, g, o);
                 if ((rc = launch_status()) != AR_OK) return rc;
                 continue;

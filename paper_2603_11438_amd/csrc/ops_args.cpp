@@ -11,6 +11,7 @@
 #include <Python.h>
 
 #include <ATen/ATen.h>
+#include <c10/core/GradMode.h>
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <stdint.h>
@@ -19,6 +20,10 @@
 
 namespace {
 
+// Set once the caller has been told that results have no autograd graph; until
+// then a tensor that would need one is left to the checks in Python, which tell.
+bool graphs_told = false;
+
 // A tensor argument that is plainly right so far, or null.
 const at::Tensor *plain(PyObject *o, long device)
 {
@@ -26,6 +31,7 @@ const at::Tensor *plain(PyObject *o, long device)
     if (!THPVariable_CheckExact(o) && (PyObject *)Py_TYPE(o) != ParameterClass) return nullptr;
     const at::Tensor &t = THPVariable_Unpack(o);
     if (!t.defined() || !t.is_cuda() || t.layout() != at::kStrided || !t.has_storage() || t.device().index() != device) return nullptr;
+    if (!graphs_told && t.requires_grad() && c10::GradMode::is_enabled()) return nullptr;
     return &t;
 }
 
@@ -261,11 +267,20 @@ PyObject *ffn_backward(PyObject *, PyObject *const *a, Py_ssize_t n)
     }
 }
 
+PyObject *tell_graphs(PyObject *, PyObject *told)
+{
+    const int is = PyObject_IsTrue(told);
+    if (is < 0) return nullptr;
+    graphs_told = is != 0;
+    return none();
+}
+
 PyMethodDef methods[] = {
     {"norm", (PyCFunction)(void (*)(void))norm, METH_FASTCALL, "ar_residual_norm on tensors."},
     {"norm_backward", (PyCFunction)(void (*)(void))norm_backward, METH_FASTCALL, "ar_residual_norm_backward on tensors."},
     {"ffn", (PyCFunction)(void (*)(void))ffn, METH_FASTCALL, "ar_gated_ffn on tensors."},
     {"ffn_backward", (PyCFunction)(void (*)(void))ffn_backward, METH_FASTCALL, "ar_gated_ffn_backward on tensors."},
+    {"tell_graphs", tell_graphs, METH_O, "Whether the caller knows that results have no autograd graph."},
     {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_ops_args", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};

@@ -12,6 +12,10 @@ on the stream of the call (``stream``, or torch's current one); a result given
 as ``out`` is written in place.  Rows must be contiguous; the stride between
 rows is free.
 
+Results have no autograd graph, whatever the arguments require: gradients come
+from the *_backward functions.  The first call with a tensor that requires one,
+outside of torch.no_grad(), warns (RuntimeWarning).
+
 Calls on the current stream that make their own results are checked and made in
 native code (csrc/ops_args.cpp, used with the torch it was built against); what
 is not plainly right there, and every other call, takes the checks below.
@@ -96,6 +100,8 @@ class _Native:
             raise ImportError(f"built against torch {mod.torch_version}, loaded is {torch.__version__}")
         L = _lib()
         address = lambda name: ctypes.cast(getattr(L, name), ctypes.c_void_p).value  # noqa: E731
+        self.tell_graphs = mod.tell_graphs
+        self.tell_graphs(_graphs_told)
         self.norm, self.norm_backward, self.ffn, self.ffn_backward = mod.norm, mod.norm_backward, mod.ffn, mod.ffn_backward
         self.norm_fn = address("ar_residual_norm")
         self.norm_backward_fns = address("ar_residual_norm_backward"), address("ar_residual_norm_backward_workspace")
@@ -121,6 +127,26 @@ def _native() -> Optional[_Native]:
                           "some 10 us per call", RuntimeWarning, stacklevel=3)
             _native_path = False
     return _native_path if _native_path and _native_path.in_use() else None
+
+
+_graphs_told = False
+
+
+def _tell_of_graphs(*tensors):
+    """Warns, once, where autograd would expect a graph that results do not have."""
+    global _graphs_told
+    if _graphs_told:
+        return
+    import torch
+
+    if torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in tensors):
+        import warnings
+
+        _graphs_told = True
+        if (nat := _native()) is not None:
+            nat.tell_graphs(True)
+        warnings.warn("the results of this package's operators have no autograd graph: gradients come from the *_backward functions "
+                      "(torch.no_grad() or detached tensors say that this is known)", RuntimeWarning, stacklevel=3)
 
 
 def _done(got, what):
@@ -261,6 +287,7 @@ def residual_norm(y, residual, *, post_weight=None, pre_weight=None, gate=None, 
                        (AR_NORM_POST if post else 0) | (AR_NORM_PRE if pre else 0), dev, nat.stream(dev))
         if got is not None:
             return _done(got, "ar_residual_norm")
+    _tell_of_graphs(y, residual, post_weight, pre_weight, gate)
     with _On(y, stream) as on:
         d, _, (w1, g, w2) = _norm_desc(y, post_weight, pre_weight, gate, alpha, eps, post, pre)
         dev = on.index
@@ -302,6 +329,7 @@ def residual_norm_backward(y, s, ds, dx, *, post_weight=None, pre_weight=None, g
         if got is not None:
             got = zip(("dy", "dresidual", "dpost_weight", "dpre_weight", "dgate"), _done(got, "ar_residual_norm_backward"))
             return {k: t for k, t in got if t is not None}
+    _tell_of_graphs(y, s, ds, dx, post_weight, pre_weight, gate)
     with _On(y, stream) as on:
         d, pdt, (w1, g, w2) = _norm_desc(y, post_weight, pre_weight, gate, alpha, eps, post, pre)
         dev = on.index
@@ -374,6 +402,7 @@ def gated_ffn(x, w_gate, w_up, *, act: str = "silu", save: bool = False, out=Non
         if got is not None:
             h, saved = _done(got, "ar_gated_ffn")
             return (h, saved) if save else h
+    _tell_of_graphs(x, w_gate, w_up)
     with _On(x, stream) as on:
         d = _ffn_desc(x, w_gate, w_up, act)
         h = out
@@ -406,6 +435,7 @@ def gated_ffn_backward(dh, x, w_gate, w_up, saved, *, act: str = "silu", need_dx
         got = nat.ffn_backward(*nat.ffn_backward_fns, dh, x, w_gate, w_up, saved, ACTS[act], need_dx, need_dw, dev, nat.stream(dev))
         if got is not None:
             return _done(got, "ar_gated_ffn_backward")
+    _tell_of_graphs(dh, x, w_gate, w_up)
     with _On(x, stream) as on:
         d = _ffn_desc(x, w_gate, w_up, act)
         dev = on.index
@@ -477,6 +507,7 @@ def orthogonalize(g, *, steps: int = 5, coefs=ORTHO_COEFS, eps: float = 1e-7, sc
     (orthogonalize_workspace)."""
     import torch
 
+    _tell_of_graphs(g)
     with _On(g, stream) as on:
         dt = _ar._dtype_of(g)
         b, m, n, ld, stride = _matrices(g, "g")

@@ -60,6 +60,45 @@ inline bool meet(const Mat &a, const Mat &b)
     return true;
 }
 
+// A batch of equal matrices, `stride` elements from each to the next.
+struct Batch {
+    Mat first;
+    size_t count, stride;
+    size_t bytes() const { return count ? (count - 1) * stride * first.elem + first.bytes() : 0; }
+    Mat at(size_t k) const
+    {
+        Mat m = first;
+        m.p = (const char *)m.p + k * stride * m.elem;
+        return m;
+    }
+};
+
+// Whether matrices of two batches, of one count, may share an element: as `meet` for
+// each pair whose address ranges meet.
+inline bool meet(const Batch &a, const Batch &b)
+{
+    if (!a.first.p || !b.first.p || !a.bytes() || !b.bytes()) return false;
+    const uintptr_t pa = (uintptr_t)a.first.p, pb = (uintptr_t)b.first.p;
+    if (pa >= pb + b.bytes() || pb >= pa + a.bytes()) return false;
+    if (a.stride == b.stride) {
+        // a pair's places beside each other depend on the difference of its indexes alone
+        for (size_t k = 0; k < a.count; ++k)
+            if (meet(a.at(k), b.first) || meet(a.first, b.at(k))) return true;
+        return false;
+    }
+    size_t pairs = 0;
+    const size_t step = b.stride * b.first.elem, span = b.first.bytes();
+    for (size_t i = 0; i < a.count; ++i) {
+        const Mat m = a.at(i);
+        const uintptr_t p = (uintptr_t)m.p;
+        // the matrices of b that end behind m's begin and begin before its end
+        const size_t from = p >= pb + span ? (p - pb - span) / step + 1 : 0;
+        for (size_t k = from; k < b.count && pb + k * step < p + m.bytes(); ++k)
+            if (++pairs > (1u << 20) || meet(m, b.at(k))) return true;  // past a million pairs: the ranges decide
+    }
+    return false;
+}
+
 // Lets a kernel's launches on the current device have `bytes` of dynamic LDS.
 inline int allow_lds(OncePerDevice &once, const void *kernel, int bytes)
 {

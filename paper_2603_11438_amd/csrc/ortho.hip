@@ -961,15 +961,13 @@ int ortho(const ar_ortho_desc *desc, const void *in, void *out, void *ws, size_t
     };
     if (!apart(si, ld_in) || !apart(so, ld_out)) return AR_ERR_ARG;
     if (!in || !out || (uintptr_t)in % e || (uintptr_t)out % e) return AR_ERR_ARG;
-    // the whole batch as one range
-    const Mat mi{in, 1, (d.batch - 1) * si + (d.rows - 1) * ld_in + d.cols, kOpsMaxSize, e};
-    const Mat mo{out, 1, (d.batch - 1) * so + (d.rows - 1) * ld_out + d.cols, kOpsMaxSize, e};
-    if (meet(mi, mo) && !(in == out && ld_in == ld_out && si == so)) return AR_ERR_ARG;
+    const Batch bi{mat(in, d.rows, d.cols, ld_in, d.dtype), d.batch, si}, bo{mat(out, d.rows, d.cols, ld_out, d.dtype), d.batch, so};
+    if (!(bi.first.same(bo.first) && (d.batch == 1 || si == so)) && meet(bi, bo)) return AR_ERR_ARG;
     const size_t need = ar_orthogonalize_workspace(desc);
     if (!ws || ws_bytes < need) return AR_ERR_SCRATCH;
     if ((uintptr_t)ws % 256 != 0) return AR_ERR_ARG;
-    const Mat wsm{ws, 1, need, kOpsMaxSize, 1};
-    if (meet(wsm, mi) || meet(wsm, mo)) return AR_ERR_ARG;
+    const Batch bw{Mat{ws, 1, need, need, 1}, 1, need};
+    if (meet(bw, bi) || meet(bw, bo)) return AR_ERR_ARG;
 
     o.tall = d.rows > d.cols;
     o.m = (uint32_t)(o.tall ? d.cols : d.rows), o.n = (uint32_t)(o.tall ? d.rows : d.cols);

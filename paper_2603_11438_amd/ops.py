@@ -511,10 +511,14 @@ def orthogonalize(g, *, steps: int = 5, coefs=ORTHO_COEFS, eps: float = 1e-7, sc
     with _On(g, stream) as on:
         dt = _ar._dtype_of(g)
         b, m, n, ld, stride = _matrices(g, "g")
-        flat = [float(v) for c in coefs for v in (c if hasattr(c, "__len__") else (c,))]
+        flat, whole = [], True
+        for c in coefs:
+            one = [float(v) for v in c] if hasattr(c, "__len__") else [float(c)]
+            whole = whole and len(one) == (3 if hasattr(c, "__len__") else 1)
+            flat += one
         if len(flat) == 3:
             flat = flat * steps
-        if not 1 <= steps <= AR_ORTHO_MAX_STEPS or len(flat) != 3 * steps:
+        if not 1 <= steps <= AR_ORTHO_MAX_STEPS or len(flat) != 3 * steps or not whole:
             raise ValueError(f"steps is 1 .. {AR_ORTHO_MAX_STEPS}, with one (a, b, c) for all or one for each")
         o = torch.empty(g.shape, dtype=g.dtype, device=g.device) if out is None else out
         if o.shape != g.shape or o.dtype != g.dtype or not o.is_cuda or o.device.index != on.index:

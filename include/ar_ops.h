@@ -108,7 +108,8 @@ size_t ar_residual_norm_backward_workspace(const ar_norm_desc *desc);
 enum { AR_ACT_SILU = 0, AR_ACT_GELU = 1, AR_ACT_RELU = 2 };
 
 /* With G = x Wg^T and U = x Wu^T (x: tokens x dim; weights: hidden x dim):
- *     h = act(G) * U */
+ *     h = act(G) * U
+ * The block's way back from hidden to dim is a plain product and no part of it. */
 typedef struct ar_ffn_desc {
     size_t tokens;         /* 0 is a valid no-op (backward: zero weight gradients) */
     size_t dim, hidden;    /* 1 .. 2^20 */

@@ -111,7 +111,7 @@ inline size_t pair_tiles(int tile, size_t tokens, size_t hidden) { return tiles_
 inline int pair_small(size_t runs) { return runs <= 256 ? kPairDeep : kPairSmall; }
 
 // us of a forward, a fit to 432 measured ones (128 to 6144 tokens, dim 1024 to 4096,
-// hidden 512 to 5632; the tile so chosen takes 0.5 % more than the best of them in the
+// hidden 512 to 5632, operands in the caches; the tile so chosen takes 0.5 % more than the best of them in the
 // mean, 15 % at most).  A step of a tile, several on a unit one after another: 256 x
 // 256 1.45, alone 1.15 (the clock is higher then); two of 128 x 128 side by side
 // 0.9, one 0.73, with three buffers 0.41; their ends 11, 2.5 and 4.5.  A join: 3 and

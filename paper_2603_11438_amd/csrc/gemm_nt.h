@@ -22,9 +22,10 @@
 // A row's 16-byte chunks are stored in the order chunk ^ (row >> 1 & 7) (rows of
 // 64 bytes: row >> 2 & 3), by permuting which chunk a lane loads: the sixteen
 // rows' equal chunks that a read touches together then lie in sixteen different
-// groups of four banks (SQ_LDS_BANK_CONFLICT: 0; with row & 7 a read took
-// twice as long).  By k, row k's chunks are rotated by 4 (k & 3) (64 columns: by
-// 4 (k >> 1 & 1)): a transposing read takes 64 bytes of each of four rows.
+// groups of four banks (SQ_LDS_BANK_CONFLICT: 0 where no epilogue is staged, else
+// up to 2 % of the cycles; with row & 7 a read took twice as long).  By k, row k's
+// chunks are rotated by 4 (k & 3) (64 columns: by 4 (k >> 1 & 1)): a transposing
+// read takes 64 bytes of each of four rows.
 //
 // Rate, bf16, 8192 x 8192 x 8192: 856 us, 1284 TFLOP/s with the 256 x 256 tile,
 // at 1.75 GHz: the board's power limit has the clock.  With every load an L2 hit

@@ -13,8 +13,8 @@
 // for all of that give up the next row first, then keep those sums in LDS.
 //
 // 16384 x 8192 bf16 forward 191 us, 5.6 TB/s (a large copy 5.2); 8192 x 4096 bf16
-// backward with parameter gradients 96 us, 4.2 TB/s; 2049 x 2501 fp32, rows that
-// begin at no vector's bound, 20 us, 4.1 TB/s; one row of 8192 3 us, a launch.
+// backward with parameter gradients 98 us, 4.1 TB/s; 2049 x 2501 fp32, rows that
+// begin at no vector's bound, 20 us, 4.1 TB/s; one row of 4096 3 us, a launch.
 // Wide rows backward: 2048 x 8192 fp32 93 us, 4.3 TB/s; 4096 x 12288 bf16 140 us,
 // 4.3 TB/s; 2048 x 12288 fp32 130 us, 4.7 TB/s.
 #include <type_traits>

@@ -25,11 +25,12 @@
 // A and B are symmetric: only tiles on and below the diagonal are computed and
 // written to both places.  Tall matrices are transposed on the way in and out.
 //
-// Five steps of 4096 x 4096 bf16: 1580 us, 870 TFLOP/s (a step's A 83 us, B 89, X
-// 145, of which 40 the epilogue's bytes); six of 1410 x 700 bf16: 246 us; 1024 x
+// Five steps of 4096 x 4096 bf16: 1600 us, 860 TFLOP/s (a step's A 84 us, B 88, X
+// 150, of which 40 the epilogue's bytes); six of 1410 x 700 bf16: 250 us; 1024 x
 // 4096 fp32: 395 us, 530 TFLOP/s of fp16 products; 128 x 384 fp32: 97 us.  The small
-// ones are bound by the LDS (a 64 x 64 tile's fragments take twice the cycles of
-// its products) and by launches.
+// ones are bound by no unit (matrix units busy 11 to 45 % of the cycles, the LDS 30 to
+// 45 %) but by what one or two rounds of tiles leave in the open: first loads,
+// epilogues, launches.
 #include <type_traits>
 
 #include "gemm_nt.h"

@@ -445,7 +445,7 @@ __global__ __launch_bounds__(S::THREADS) void ortho_square_kernel(const GemmArgs
     Ahead<S, f16, PLANES> ahead{(const f16 *)(ws + o.at.a), o.at.a_lo, o.mp, o.mp, w.row0, w.col0, stage};
     if (SECOND) ahead.load(0);
     RowSquares<S::MT> squares;
-    if (!SECOND && PLANES == 1 && o.step > 0 && at.m == at.n) squares.load(o, ws, w.row0);
+    if (!SECOND && PLANES == 1 && o.step > 0 && at.m == at.n && g.splits == 1) squares.load(o, ws, w.row0);
     f32x16 acc[S::MT][NT];
     gemm_tile<f16, S, false>(g, at, lds, acc);
     if (!SECOND && g.splits > 1) {

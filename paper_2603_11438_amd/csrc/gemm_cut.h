@@ -110,20 +110,23 @@ inline size_t pair_tiles(int tile, size_t tokens, size_t hidden) { return tiles_
 // a unit: 1024 x 4096 x 1408 39 us, with two buffers 62; 128 x 4096 x 11264 48 and 67.
 inline int pair_small(size_t runs) { return runs <= 256 ? kPairDeep : kPairSmall; }
 
-// us of a forward, a fit to 432 measured ones (128 to 6144 tokens, dim 1024 to 4096,
-// hidden 512 to 5632, operands in the caches; the tile so chosen takes 0.5 % more than the best of them in the
-// mean, 15 % at most).  A step of a tile, several on a unit one after another: 256 x
-// 256 1.45, alone 1.15 (the clock is higher then); two of 128 x 128 side by side
-// 0.9, one 0.73, with three buffers 0.41; their ends 11, 2.5 and 4.5.  A join: 3 and
-// its bytes at 5 TB/s.  The 256 tile first, then the cheaper 128: 2048 x 1024 x 4352
-// 65 us, 54; 1536 x 1024 x 5632 66, 54; but 1536 x 4096 x 2816 92, 112.
-inline double pair_us(int tile, size_t tokens, size_t hidden, size_t steps, uint32_t splits)
+// us of a forward, a fit to 932 sizes in every shape (65 to 16384 tokens, dim 128 to
+// 6144, hidden 125 to 6144, half of them also with the projections saved; operands in
+// the caches): the tile so chosen takes 0.6 % more than the best of them in the mean.
+// A step of a tile, several on a unit one after another: 256 x 256 1.45, alone 1.15
+// (the clock is higher then); two of 128 x 128 side by side 0.9, one 0.73, a fifth
+// more where rows begin between cache lines; with three buffers 0.41.  Their ends 16,
+// 3 and 6, between those of calls that save the projections and of those that do not.
+// A join: 3 and its bytes at 5 TB/s.  The 256 tile first, then the cheaper 128: 2048 x
+// 1024 x 4352 65 us, 54; 1536 x 1024 x 5632 66, 54; but 1536 x 4096 x 2816 92, 112.
+inline double pair_us(int tile, size_t tokens, size_t dim, size_t hidden, uint32_t splits)
 {
-    const size_t units = (pair_tiles(tile, tokens, hidden) * splits + 255) / 256;
+    const size_t units = (pair_tiles(tile, tokens, hidden) * splits + 255) / 256, steps = (dim + kStepK - 1) / kStepK;
     const double per = (double)((steps + splits - 1) / splits);
-    double us = tile == kPairLarge ? per * (units == 1 ? 1.15 : 1.45 * units) + 11.0 * units
-                : tile == kPairDeep ? per * (units == 1 ? 0.41 : 0.5 * units) + 4.5 * units
-                                    : per * (units / 2 * 0.9 + units % 2 * 0.73) + 2.5 * units;
+    const bool between = dim % 8 == 0 && dim % 64 != 0;  // other rows are copied to whole lines
+    double us = tile == kPairLarge ? per * (units == 1 ? 1.15 : 1.45 * units) + 16.0 * units
+                : tile == kPairDeep ? per * (units == 1 ? 0.41 : 0.5 * units) + 6.0 * units
+                                    : per * (between ? 1.2 : 1.0) * (units / 2 * 0.9 + units % 2 * 0.73) + 3.0 * units;
     if (splits > 1) us += 3.0 + 2.0 * splits * 2 * tokens * hidden * 4 / 5e6;
     return us;
 }
@@ -150,11 +153,11 @@ inline Cut ffn_cut(size_t tokens, size_t dim, size_t hidden)
         return best;
     }
     Cut best{kPairLarge, 1};
-    double time = pair_us(kPairLarge, tokens, hidden, steps, 1);
+    double time = pair_us(kPairLarge, tokens, dim, hidden, 1);
     const size_t tiles = pair_tiles(kPairSmall, tokens, hidden);
     for (uint32_t s = 1; s <= kMaxSplits && may_split(tiles, steps, s); ++s) {
         const int tile = pair_small(tiles * s);
-        const double us = pair_us(tile, tokens, hidden, steps, s);
+        const double us = pair_us(tile, tokens, dim, hidden, s);
         if (us < time) best = {tile, s}, time = us;
     }
     return best;

@@ -29,11 +29,11 @@ static void forward(size_t t, size_t d, size_t f)
     // the shapes that ffn.hip has for more than 64 tokens
     expect(c.tile == kPairSmall || c.tile == kPairLarge || c.tile == kPairDeep, "exists", t, d, f, c);
     expect(c.tile != kPairLarge || c.splits == 1, "256 in one piece", t, d, f, c);
-    const double us = pair_us(c.tile, t, f, steps, c.splits);
-    expect(us <= pair_us(kPairLarge, t, f, steps, 1), "256 is cheaper", t, d, f, c);
+    const double us = pair_us(c.tile, t, d, f, c.splits);
+    expect(us <= pair_us(kPairLarge, t, d, f, 1), "256 is cheaper", t, d, f, c);
     const size_t tiles = pair_tiles(kPairSmall, t, f);
     for (uint32_t s = 1; s <= kMaxSplits && may_split(tiles, steps, s); ++s)
-        expect(us <= pair_us(tiles * s <= 256 ? kPairDeep : kPairSmall, t, f, steps, s), "128 is cheaper", t, d, f, c);
+        expect(us <= pair_us(tiles * s <= 256 ? kPairDeep : kPairSmall, t, d, f, s), "128 is cheaper", t, d, f, c);
 }
 
 static void show(const char *name, Cut c) { printf("%s %d %u\n", name, c.tile, c.splits); }

@@ -189,6 +189,61 @@ int ar_orthogonalize(const ar_ortho_desc *desc, const void *in, void *out, void 
                      void *stream);
 size_t ar_orthogonalize_workspace(const ar_ortho_desc *desc);
 
+/* ---- attention ------------------------------------------------------------ */
+
+/* Sequences lie one after another in the tokens: sequence i has the queries
+ * starts_q[i] .. starts_q[i+1] - 1 and the keys starts_k[i] .. starts_k[i+1] - 1 (device
+ * memory, sequences + 1 values each, not decreasing; both NULL for one sequence of all
+ * tokens).  Its query i (of lq) sees its key j (of lk) where AR_ATTN_CAUSAL is not set or
+ * j <= i + lk - lq: the last query sees every key.  Head h reads key head
+ * h / (heads / kv_heads).  With z_ij = scale * q_i . k_j over the keys that i sees:
+ *     lse_i = log sum_j e^z_ij,  o_i = sum_j e^(z_ij - lse_i) v_j
+ * A query that sees no key has o = 0 and lse = minus infinity.  Tokens of no sequence
+ * (before the first start, from the last one on) keep their o and lse, or get zeros
+ * with AR_ATTN_CLEAR.  Values of `starts` outside the tokens are taken as the nearest
+ * end of them; where they decrease, no output is defined, but nothing else is touched.
+ * A key that a query does not see has no part in it but for one thing: in a value (v)
+ * or, backward, a k, q or dout that is infinite or NaN, 0 times it is NaN, which can
+ * reach rows of the same sequence within 256 tokens. */
+enum { AR_ATTN_CAUSAL = 1, AR_ATTN_CLEAR = 2 };
+
+/* Element d of head h of token t lies at t * ld + h * hs + d: ld_* strides between
+ * tokens (0 = heads * hs), hs_* between heads (0 = dim).  Either a token's heads lie
+ * within ld, or a head's tokens within hs; nothing overlaps. */
+typedef struct ar_attention_desc {
+    size_t sequences;             /* 0, or no tokens: a valid no-op */
+    size_t tokens_q, tokens_k;    /* times the heads: below 2^31 */
+    size_t heads, kv_heads, dim;  /* heads a multiple of kv_heads; dim 1 .. 128 (AR_ERR_UNSUPPORTED above) */
+    int dtype;                    /* AR_BFLOAT16 */
+    int flags;                    /* AR_ATTN_* */
+    float scale;                  /* > 0 and finite; 1 / sqrt(dim) as a rule */
+    size_t ld_q, hs_q, ld_k, hs_k, ld_v, hs_v, ld_o, hs_o;
+    size_t ld_dout, hs_dout, ld_dq, hs_dq, ld_dk, hs_dk, ld_dv, hs_dv;  /* backward only */
+} ar_attention_desc;
+
+/* Forward.  lse: NULL, or tokens_q * heads floats, by tokens, that the backward pass
+ * needs.  e^(z - m) is rounded to bf16 as an operand of the product with v (m: within
+ * e^5.6 of the row's maximum); its sum is not.  Tensors that cannot be read where
+ * they lie, not 16-byte aligned or with a dim or stride that is no multiple of 8, are
+ * first copied into the workspace.  Where there are few rows the keys are taken in
+ * several runs, which a second kernel joins, from the workspace.  Errors: AR_ERR_ARG,
+ * AR_ERR_UNSUPPORTED, AR_ERR_SCRATCH, AR_ERR_HIP. */
+int ar_attention(const ar_attention_desc *desc, const void *q, const void *k, const void *v, const int32_t *starts_q,
+                 const int32_t *starts_k, void *o, float *lse, void *workspace, size_t workspace_bytes, void *stream);
+size_t ar_attention_workspace(const ar_attention_desc *desc);
+/* What the call uses with these tensors, which is enough for it (0: none, or refused). */
+size_t ar_attention_workspace_for(const ar_attention_desc *desc, const void *q, const void *k, const void *v);
+
+/* Backward.  From dout, o and lse of the forward, with p_ij = e^(z_ij - lse_i):
+ *     delta_i = dout_i . o_i,  dz_ij = p_ij (dout_i . v_j - delta_i)
+ *     dq_i = scale sum_j dz_ij k_j,  dk_j = scale sum_i dz_ij q_i,  dv_j = sum_i p_ij dout_i
+ * dk and dv are summed over the heads that share them.  p and dz are rounded to bf16 as
+ * operands of these products.  dq, or both dk and dv, may be NULL (not wanted). */
+int ar_attention_backward(const ar_attention_desc *desc, const void *dout, const void *q, const void *k, const void *v,
+                          const void *o, const float *lse, const int32_t *starts_q, const int32_t *starts_k, void *dq, void *dk,
+                          void *dv, void *workspace, size_t workspace_bytes, void *stream);
+size_t ar_attention_backward_workspace(const ar_attention_desc *desc);
+
 #ifdef __cplusplus
 }
 #endif

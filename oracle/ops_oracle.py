@@ -110,3 +110,67 @@ def orthogonalize(m, coefs, eps=1e-7, scale=1.0):
         x = a * x + (b * p + c * (p @ p)) @ x
     x = scale * x
     return x.T if m.shape[0] > m.shape[1] else x
+
+
+# bf16's and fp32's largest relative rounding error, and the room left for what fp32
+# sums and exponentials are off by.
+U, U32 = 2.0 ** -8, 2.0 ** -24
+ROOM = 2.0 ** -14
+# What fp32 and bf16 leave out at their lower end: a p below 2^-126 is 0 there.  Fewer than
+# 2^26 such terms, each times factors whose product is below 1, or fewer by as much, are
+# off by less than this.
+UNDER = 2.0 ** -100
+
+
+def attention(q, k, v, starts_q, starts_k, causal=True, scale=None, do=None):
+    """Attention over packed sequences, and with `do` its gradients: {name: (value,
+    bound)}, with bounds of what an implementation may be off by that rounds p and dz to
+    bf16 as operands, sums in fp32 and rounds results to bf16.
+
+    o: rounding p moves o by U M at most, M = sum p |v|; rounding o by U |o|.
+    dv: likewise with M = sum_i p |do|.
+    dq, dk: rounding dz: U sum |dz| |k|; the result: U |dq|; delta is taken from the
+    rounded o: off by |do| . E, with E the bound of o, through p."""
+    q, k, v, do = (_d(t) for t in (q, k, v, do))
+    h, group, dim = q.shape[1], q.shape[1] // k.shape[1], q.shape[2]
+    scale = dim ** -0.5 if scale is None else scale
+    out = {n: (torch.zeros_like(t), torch.zeros_like(t)) for n, t in (("o", q), ("dq", q), ("dk", k), ("dv", v))}
+    lse = torch.full(q.shape[:2], -math.inf, dtype=torch.float64), torch.zeros(q.shape[:2], dtype=torch.float64)
+    for a, b, c, d in zip(starts_q, starts_q[1:], starts_k, starts_k[1:]):
+        lq, lk = b - a, d - c
+        if lq == 0 or lk == 0:
+            continue
+        sees = torch.ones(lq, lk, dtype=torch.bool)
+        if causal:
+            sees = torch.arange(lk)[None] <= torch.arange(lq)[:, None] + lk - lq
+        for n in range(h):
+            qi, kj, vj = q[a:b, n], k[c:d, n // group], v[c:d, n // group]
+            z = torch.where(sees, scale * (qi @ kj.T), -math.inf)
+            most = z.amax(1, keepdim=True)
+            e = torch.exp(z - torch.where(most == -math.inf, 0.0, most))
+            total = e.sum(1, keepdim=True)
+            p = e / torch.where(total == 0, 1.0, total)
+            lse[0][a:b, n] = torch.where(total == 0, -math.inf, most + torch.log(total))[:, 0]
+            lse[1][a:b, n] = (dim + 16) * U32 * scale * torch.where(sees, qi.abs() @ kj.abs().T, 0.0).amax(1) + 2.0 ** -19
+            # what z is off by in fp32 is p's relative error
+            room = ROOM + 4 * lse[1][a:b, n, None]
+            o, mag = p @ vj, p @ vj.abs()
+            off = (U * 1.01 + room) * mag + U * o.abs()
+            out["o"][0][a:b, n], out["o"][1][a:b, n] = o, off
+            if do is None:
+                continue
+            g = do[a:b, n]
+            dp, dp_mag = g @ vj.T, g.abs() @ vj.abs().T
+            dz = p * (dp - (g * o).sum(1, keepdim=True))
+            dz_off = (U * 1.01 + room) * dz.abs() + room * p * (dp_mag + (g * o).abs().sum(1, keepdim=True)) + \
+                p * (g.abs() * off).sum(1, keepdim=True)
+            for name, where, value, bound in (
+                    ("dq", (slice(a, b), n), scale * dz @ kj, scale * dz_off @ kj.abs()),
+                    ("dk", (slice(c, d), n // group), scale * dz.T @ qi, scale * dz_off.T @ qi.abs()),
+                    ("dv", (slice(c, d), n // group), p.T @ g, ((U * 1.01 + room) * p).T @ g.abs())):
+                out[name][0][where] += value
+                out[name][1][where] += bound
+    out["o"] = out["o"][0], out["o"][1] + UNDER
+    for name in ("dq", "dk", "dv"):  # a result's own rounding
+        out[name] = out[name][0], out[name][1] * (1 + U) + U * out[name][0].abs() + UNDER
+    return {**out, "lse": lse}

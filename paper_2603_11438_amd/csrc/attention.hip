@@ -1,0 +1,1034 @@
+// Attention over packed sequences (gfx950), forward and backward (formulas and
+// layouts in ar_ops.h).
+//
+// The queries of one key head and its group of heads are the rows of a tile: row
+// r is query r / group of the sequence, head r % group of the group.  Single
+// queries of many heads then share a read of the keys, and a prompt's tile has
+// the rows of few positions, so little of it is masked.
+//
+// Everything is computed transposed, S^T = K Q^T and O^T = V^T P^T, so that a lane
+// holds one query: the row's maximum and sum are sums in the lane and one exchange
+// with lane ^ 32.  The instruction's sums lie so that eight neighbouring ones are,
+// rounded, a fragment of P^T for the next product, if V's keys are taken in the same
+// order (4 h + 0..3, 8 + 4 h + 0..3 for lane half h): P never leaves its lane.
+#include <type_traits>
+
+#include "gemm_nt.h"
+
+#pragma clang fp contract(fast)
+
+namespace ar {
+namespace dev {
+
+constexpr int kKeys = 64;   // keys, or queries, of a stage
+constexpr int kRows = 128;  // rows of a workgroup's tile: 32 for each of four waves
+constexpr float kLog2e = 1.4426950408889634f;
+
+// One of q, k, v, o and their gradients: element d of head h of token t lies at
+// t * ld + h * hs + d.
+template <typename T> struct Heads {
+    T *p;
+    uint64_t ld, hs;
+    __device__ __forceinline__ T *at(uint64_t token, uint64_t head) const { return p + token * ld + head * hs; }
+};
+
+struct AttnArgs {
+    Heads<const bf16> q, k, v, dout;
+    Heads<bf16> o, dq, dk, dv;
+    const int32_t *starts_q, *starts_k;  // null: one sequence
+    float *lse;                          // [token][head]; null: not kept
+    const float *delta;                  // [token][head]
+    float *part, *part_lse;              // with keys split: [split][token][head][dim], [split][token][head]
+    uint32_t sequences, tokens_q, tokens_k, heads, kv_heads, group;
+    uint32_t dim, dim_in;  // dim_in: a multiple of eight, up to which the inputs can be read
+    uint32_t slots, splits;
+    uint32_t causal, rest;  // rest: rows of no sequence are set to zero
+    float scale;
+};
+
+__device__ __forceinline__ uint32_t uniform(uint32_t v) { return (uint32_t)__builtin_amdgcn_readfirstlane((int)v); }
+
+// Where sequence i begins, kept inside the tokens whatever the array holds.
+__device__ __forceinline__ uint32_t start_of(const int32_t *starts, uint32_t i, uint32_t tokens)
+{
+    if (!starts) return i ? tokens : 0u;
+    const int32_t s = starts[i];
+    return s < 0 ? 0u : (uint32_t)s < tokens ? (uint32_t)s : tokens;
+}
+
+// A sequence's part of the tokens, and which of its tiles a slot stands for.
+// Tiles are not counted on the host, which does not know the lengths: sequence i
+// has the slots from floor(start_i * per / rows) + i on, which are enough for its
+// tiles (of `rows` rows, `per` for each token) and do not meet the next one's.
+struct Place {
+    uint32_t q0, lq, k0, lk, tile;
+    bool some;
+};
+__device__ __forceinline__ Place find_place(const AttnArgs &a, uint32_t slot, bool by_keys, uint32_t per, uint32_t rows)
+{
+    const uint32_t lane = threadIdx.x & 63u;
+    const int32_t *starts = by_keys ? a.starts_k : a.starts_q;
+    const uint32_t tokens = by_keys ? a.tokens_k : a.tokens_q;
+    auto first_slot = [&](uint32_t i) { return (uint64_t)start_of(starts, i, tokens) * per / rows + i; };
+    uint32_t lo = 0, hi = a.sequences;  // the last sequence whose slots begin at `slot` or before
+    Place p{};
+    do {
+        const uint32_t step = (hi - lo + 63) / 64, i = lo + lane * step;
+        const uint32_t below = (uint32_t)__popcll(__ballot(i < hi && first_slot(i) <= slot));
+        if (below == 0) return p;
+        lo += (below - 1) * step;
+        hi = lo + step < hi ? lo + step : hi;
+    } while (hi - lo > 1);
+    lo = uniform(lo);
+    const uint64_t before = first_slot(lo);
+    const uint32_t qa = start_of(a.starts_q, lo, a.tokens_q), qb = start_of(a.starts_q, lo + 1, a.tokens_q);
+    const uint32_t ka = start_of(a.starts_k, lo, a.tokens_k), kb = start_of(a.starts_k, lo + 1, a.tokens_k);
+    p.q0 = uniform(qa), p.lq = uniform(qb > qa ? qb - qa : 0), p.k0 = uniform(ka), p.lk = uniform(kb > ka ? kb - ka : 0);
+    if (before > slot) return p;
+    p.tile = uniform(slot - (uint32_t)before);
+    p.some = (uint64_t)p.tile * rows < (uint64_t)(by_keys ? p.lk : p.lq) * per;
+    return p;
+}
+
+// Zeros in the rows of no sequence, by the workgroups behind the tiles'.
+constexpr uint32_t kRestGroups = 32;
+template <typename T> __device__ void clear_rest(const Heads<T> &x, const int32_t *starts, uint32_t sequences, uint32_t tokens,
+                                                uint32_t heads, uint32_t dim, uint32_t group)
+{
+    const uint32_t a = start_of(starts, 0, tokens), b = start_of(starts, starts ? sequences : 1, tokens), rest = a + (tokens - b);
+    if (b < a) return;
+    const uint64_t n = (uint64_t)rest * heads * dim;
+    for (uint64_t i = (uint64_t)group * blockDim.x + threadIdx.x; i < n; i += (uint64_t)kRestGroups * blockDim.x) {
+        const uint32_t t = (uint32_t)(i / ((uint64_t)heads * dim)), c = (uint32_t)(i % ((uint64_t)heads * dim));
+        x.at(t < a ? t : b + (t - a), c / dim)[c % dim] = (T)0.0f;
+    }
+}
+
+// A stage's rows, 64 of DP elements, in LDS: read by rows and transposed.  Row r's
+// 16-byte chunks lie in the order chunk ^ turn(r): sixteen rows' equal chunks are in
+// sixteen groups of four banks, and so are the four chunks of four rows that a
+// transposing read touches together.
+template <int DP> struct Stage {
+    static constexpr int CHUNKS = DP / 8, ROW = DP * 2, BYTES = kKeys * ROW, LOADS = BYTES / 4096;
+    static __device__ __forceinline__ uint32_t turn(uint32_t r)
+    {
+        return DP == 128 ? (r & 3u) << 2 | (r >> 2 & 3u) : (r >> 1 & 1u) << 2 | (r >> 2 & 3u);
+    }
+    uint32_t off[LOADS];
+    __device__ __forceinline__ void place(uint32_t wave, uint64_t ld, uint32_t dim)
+    {
+        const uint32_t lane = threadIdx.x & 63u;
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i) {
+            const uint32_t n = (i * 4 + wave) * 64 + lane, r = n / CHUNKS, c = (n % CHUNKS) ^ turn(r);
+            off[i] = c * 8 < dim ? r * (uint32_t)ld * 2 + c * 16 : kOutOfRange;
+        }
+    }
+    // rows from `left` on are zeros
+    __device__ __forceinline__ void load(uint32_t lds, uint32_t wave, const void *first, uint32_t left) const
+    {
+        const uint32_t lane = threadIdx.x & 63u;
+        const u32x4v from = tile_resource(uniform_address(first));
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i) {
+            const uint32_t r = ((i * 4 + wave) * 64 + lane) / CHUNKS;
+            load_to_lds(lds + (i * 4 + wave) * 1024, r < left ? off[i] : kOutOfRange, from, 0u);
+        }
+    }
+};
+
+// Addresses of a lane's fragments in a stage.  By rows: lane l has row l % 32 of a
+// block of 32 and elements 16 c + 8 (l / 32) + 0..7.  Transposed: element l % 32 of a
+// block of 32 and rows 16 c + 4 (l / 32) + 0..3 and 8 + 4 (l / 32) + 0..3.
+template <int DP> struct Reads {
+    uint32_t by_row[DP / 16], across[DP / 32][2];
+    __device__ __forceinline__ void place(uint32_t lds)
+    {
+        const uint32_t lane = threadIdx.x & 63u, h = lane >> 5, r = lane & 31u;
+#pragma unroll
+        for (int c = 0; c < DP / 16; ++c) by_row[c] = lds + r * Stage<DP>::ROW + ((2 * c + h) ^ Stage<DP>::turn(r)) * 16;
+#pragma unroll
+        for (int b = 0; b < DP / 32; ++b)
+#pragma unroll
+            for (int s = 0; s < 2; ++s) {
+                const uint32_t k = 8 * s + 4 * h + (lane & 15u) / 4, c = 4 * b + 2 * (lane >> 4 & 1u) + (lane >> 1 & 1u);
+                across[b][s] = lds + k * Stage<DP>::ROW + (c ^ Stage<DP>::turn(k)) * 16 + (lane & 1u) * 8;
+            }
+    }
+    // block: of 32 rows; c: of 16 elements; at: bytes from the stage that `place` was told
+    __device__ __forceinline__ bf16x8 rows(int block, int c, int at) const
+    {
+        return *(__attribute__((address_space(3))) const bf16x8 *)(uintptr_t)(by_row[c] + block * 32 * Stage<DP>::ROW + at);
+    }
+    // block: of 32 elements; c: of 16 rows
+    __device__ __forceinline__ bf16x8 columns(int block, int c, int at) const
+    {
+        typedef short s16x4 __attribute__((ext_vector_type(4)));
+        typedef __attribute__((address_space(3))) s16x4 *P;
+        const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((P)(uintptr_t)(across[block][0] + c * 16 * Stage<DP>::ROW + at));
+        const s16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((P)(uintptr_t)(across[block][1] + c * 16 * Stage<DP>::ROW + at));
+        return __builtin_bit_cast(bf16x8, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
+    }
+};
+
+// The fragment of a lane's row, elements 16 c + 8 (l / 32) + 0..7.
+template <int DP> __device__ __forceinline__ void load_row(const bf16 *row, uint32_t dim, bf16x8 (&f)[DP / 16])
+{
+    const uint32_t h = threadIdx.x >> 5 & 1u;
+#pragma unroll
+    for (int c = 0; c < DP / 16; ++c) {
+        const uint32_t d = c * 16 + h * 8;
+        f[c] = bf16x8{};
+        if (d < dim) f[c] = *(const bf16x8 *)(row + d);
+    }
+}
+
+// Eight neighbouring sums of a lane, rounded: a fragment of the next product.
+__device__ __forceinline__ bf16x8 rounded(const f32x16 &v, int from)
+{
+    bf16x8 f;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) f[k] = (bf16)v[from + k];
+    return f;
+}
+
+__device__ __forceinline__ float other_half(float v) { return __shfl_xor(v, 32); }
+
+// A lane's row of O^T (or of a gradient), times `by`: elements 32 b + 8 q + 4 (l / 32)
+// + 0..3 of row l % 32.
+template <int DP, typename O> __device__ __forceinline__ void store_row(O *row, uint32_t dim, const f32x16 (&acc)[DP / 32], float by)
+{
+    typedef O O4 __attribute__((ext_vector_type(4)));
+    typedef O4 Out __attribute__((aligned(sizeof(O))));
+    const uint32_t h = threadIdx.x >> 5 & 1u;
+#pragma unroll
+    for (int b = 0; b < DP / 32; ++b)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            const uint32_t d = b * 32 + q * 8 + h * 4;
+            O4 v;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) v[k] = (O)(acc[b][q * 4 + k] * by);
+            if (d + 4 <= dim) {
+                *(Out *)(row + d) = v;
+            } else {
+#pragma unroll
+                for (int k = 0; k < 4; ++k)
+                    if (d + k < dim) row[d + k] = v[k];
+            }
+        }
+}
+
+// What the rows of a wave's tile may see.
+struct Rows {
+    uint32_t row, query, head;  // of the lane; rows past the last one repeat it
+    uint32_t limit;             // keys that the lane's row sees
+    uint32_t least, most;       // of the wave's rows
+    bool real;                  // there is such a row
+};
+__device__ __forceinline__ Rows rows_of(const AttnArgs &a, const Place &p, uint32_t first, uint32_t kv_head)
+{
+    const uint32_t lane = threadIdx.x & 63u, count = p.lq * a.group;
+    auto limit = [&](uint32_t query) {
+        const int64_t n = a.causal ? (int64_t)query + 1 + p.lk - p.lq : (int64_t)p.lk;
+        return n > 0 ? (uint32_t)n : 0u;
+    };
+    Rows r;
+    r.row = first + (lane & 31u);
+    r.real = r.row < count;
+    r.row = r.real ? r.row : count - 1;
+    r.query = r.row / a.group;
+    r.head = kv_head * a.group + (r.row - r.query * a.group);
+    r.limit = limit(r.query);
+    r.least = uniform(limit((first < count ? first : count - 1) / a.group));
+    r.most = uniform(limit((first + 31 < count ? first + 31 : count - 1) / a.group));
+    if (first >= count) r.most = 0;  // nothing to do for this wave
+    return r;
+}
+
+// Sums that are more than this far (powers of two) below the running maximum's new
+// value are what makes the kept sums be scaled down: up to there P grows to 2^8,
+// which costs none of its bits.
+constexpr float kSlack = 8.0f;
+
+template <int DP> __global__ __launch_bounds__(256, 2) void attention_kernel(const AttnArgs a)
+{
+    typedef Stage<DP> S;
+    extern __shared__ __attribute__((aligned(16))) char lds[];
+    const uint32_t wave = uniform(threadIdx.x >> 6);
+    const uint32_t tiles = a.slots * a.kv_heads * a.splits;
+    if (blockIdx.x >= tiles) {
+        clear_rest(a.o, a.starts_q, a.sequences, a.tokens_q, a.heads, a.dim, blockIdx.x - tiles);
+        if (a.lse) clear_rest(Heads<float>{a.lse, a.heads, 1}, a.starts_q, a.sequences, a.tokens_q, a.heads, 1, blockIdx.x - tiles);
+        return;
+    }
+    // a key head's workgroups on one XCD where the heads come to eight; the last
+    // tiles of a sequence, which see the most keys, first
+    const uint32_t kv_head = blockIdx.x % a.kv_heads, rest = blockIdx.x / a.kv_heads, split = rest % a.splits;
+    const Place p = find_place(a, a.slots - 1 - rest / a.splits, false, a.group, kRows);
+    if (!p.some) return;
+    const Rows r = rows_of(a, p, p.tile * kRows + wave * 32, kv_head);
+    const uint32_t last = (p.tile + 1) * kRows < p.lq * a.group ? (p.tile + 1) * kRows - 1 : p.lq * a.group - 1;
+    const int64_t sees = a.causal ? (int64_t)(last / a.group) + 1 + p.lk - p.lq : (int64_t)p.lk;
+    const uint32_t stages = sees > 0 ? ((uint32_t)sees + kKeys - 1) / kKeys : 0;
+    const uint32_t begin = (uint32_t)((uint64_t)stages * split / a.splits), end = (uint32_t)((uint64_t)stages * (split + 1) / a.splits);
+
+    const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)lds;
+    S ks, vs;
+    ks.place(wave, a.k.ld, a.dim_in), vs.place(wave, a.v.ld, a.dim_in);
+    Reads<DP> at;
+    at.place(lds0);
+    auto load = [&](uint32_t t, uint32_t buf) {
+        const uint32_t key = t * kKeys;
+        ks.load(lds0 + buf * 2 * S::BYTES, wave, a.k.at(p.k0 + key, kv_head), p.lk - key);
+        vs.load(lds0 + buf * 2 * S::BYTES + S::BYTES, wave, a.v.at(p.k0 + key, kv_head), p.lk - key);
+    };
+    bf16x8 q[DP / 16];
+    load_row<DP>(a.q.at(p.q0 + r.query, r.head), a.dim_in, q);
+    f32x16 o[DP / 32];
+#pragma unroll
+    for (int b = 0; b < DP / 32; ++b) o[b] = f32x16{};
+    const float c = a.scale * kLog2e;
+    float top = -INFINITY, sum = 0.0f;  // top: in units of S, times c once used
+    const uint32_t h = threadIdx.x >> 5 & 1u;
+
+    auto stage = [&](uint32_t t, auto buffer) {
+        constexpr int K = buffer.value * 2 * S::BYTES, V = K + S::BYTES;
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+        if (t + 1 < end) load(t + 1, 1 - buffer.value);
+        if (t * kKeys >= r.most) return;
+        f32x16 s[2];
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+            s[b] = f32x16{};
+#pragma unroll
+            for (int d = 0; d < DP / 16; ++d) s[b] = Frag<bf16>::mfma(at.rows(b, d, K), q[d], s[b]);
+        }
+        if (t * kKeys + kKeys > r.least) {
+            const uint32_t from = t * kKeys + 4 * h;
+#pragma unroll
+            for (int b = 0; b < 2; ++b)
+#pragma unroll
+                for (int k = 0; k < 16; ++k)
+                    if (from + b * 32 + 8 * (k / 4) + k % 4 >= r.limit) s[b][k] = -INFINITY;
+        }
+        float m = s[0][0];
+#pragma unroll
+        for (int k = 1; k < 16; ++k) m = fmaxf(m, s[0][k]);
+#pragma unroll
+        for (int k = 0; k < 16; ++k) m = fmaxf(m, s[1][k]);
+        m = fmaxf(m, other_half(m));
+        const bool rises = m * c > top * c + kSlack;
+        if (__any(rises)) {
+            // a row's bits do not depend on the others: a lane whose maximum stays goes on as it was
+            const float next = rises ? m : top, to = next == -INFINITY ? 0.0f : next;
+            const float by = __builtin_amdgcn_exp2f((top - to) * c);
+            top = next;
+            sum *= by;
+#pragma unroll
+            for (int b = 0; b < DP / 32; ++b)
+#pragma unroll
+                for (int k = 0; k < 16; ++k) o[b][k] *= by;
+        }
+        const float base = top == -INFINITY ? 0.0f : top * c;
+        float part[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+#pragma unroll
+            for (int k = 0; k < 16; ++k) {
+                s[b][k] = __builtin_amdgcn_exp2f(s[b][k] * c - base);
+                part[k & 3] += s[b][k];
+            }
+        sum += (part[0] + part[1]) + (part[2] + part[3]);
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                const bf16x8 w = rounded(s[b], k * 8);
+#pragma unroll
+                for (int d = 0; d < DP / 32; ++d) o[d] = Frag<bf16>::mfma(at.columns(d, b * 2 + k, V), w, o[d]);
+            }
+    };
+    if (begin < end) load(begin, 0);
+    for (uint32_t t = begin; t < end; t += 2) {
+        stage(t, std::integral_constant<int, 0>{});
+        if (t + 1 < end) stage(t + 1, std::integral_constant<int, 1>{});
+    }
+    sum += other_half(sum);
+    if (!r.real) return;
+    const float by = sum == 0.0f ? 0.0f : 1.0f / sum;
+    const float lse = sum == 0.0f ? -INFINITY : top * a.scale + __logf(sum);
+    const uint64_t token = p.q0 + r.query;
+    if (a.splits > 1) {
+        const uint64_t at_row = ((uint64_t)split * a.tokens_q + token) * a.heads + r.head;
+        store_row<DP>(a.part + at_row * a.dim, a.dim, o, by);
+        if (h == 0) a.part_lse[at_row] = lse;
+    } else {
+        store_row<DP>(a.o.at(token, r.head), a.dim, o, by);
+        if (a.lse && h == 0) a.lse[token * a.heads + r.head] = lse;
+    }
+}
+
+// Joins the runs of keys of a split call: one wave for each row.
+__global__ __launch_bounds__(256) void attention_join_kernel(const AttnArgs a)
+{
+    const uint32_t lane = threadIdx.x & 63u;
+    const uint64_t rows = (uint64_t)a.tokens_q * a.heads;
+    const uint32_t from = start_of(a.starts_q, 0, a.tokens_q), until = start_of(a.starts_q, a.starts_q ? a.sequences : 1, a.tokens_q);
+    for (uint64_t i = (uint64_t)blockIdx.x * 4 + (threadIdx.x >> 6); i < rows; i += (uint64_t)gridDim.x * 4) {
+        const uint32_t token = (uint32_t)(i / a.heads), head = (uint32_t)(i % a.heads);
+        if (token < from || token >= until) continue;
+        float top = -INFINITY;
+        for (uint32_t s = 0; s < a.splits; ++s) {
+            const float l = a.part_lse[s * rows + i];
+            top = l > top || l != l ? l : top;  // NaN stays
+        }
+        const float base = top == -INFINITY ? 0.0f : top;
+        float sum = 0.0f, v[2] = {0.0f, 0.0f};
+        for (uint32_t s = 0; s < a.splits; ++s) {
+            const float w = __expf(a.part_lse[s * rows + i] - base);
+            sum += w;
+            const float *o = a.part + (s * rows + i) * a.dim;
+#pragma unroll
+            for (int k = 0; k < 2; ++k)
+                if (lane + 64 * k < a.dim) v[k] += w * o[lane + 64 * k];
+        }
+        const float by = sum == 0.0f ? 0.0f : 1.0f / sum;
+#pragma unroll
+        for (int k = 0; k < 2; ++k)
+            if (lane + 64 * k < a.dim) a.o.at(token, head)[lane + 64 * k] = (bf16)(v[k] * by);
+        if (a.lse && lane == 0) a.lse[i] = sum == 0.0f ? -INFINITY : base + __logf(sum);
+    }
+}
+
+// ---- backward -----------------------------------------------------------------
+
+// delta = the sum over a row of dout * o: sixteen lanes a row.
+__global__ __launch_bounds__(256) void attention_delta_kernel(const Heads<const bf16> dout, const Heads<const bf16> o, float *delta,
+                                                              uint64_t rows, uint32_t heads, uint32_t dim)
+{
+    const uint32_t d = (threadIdx.x & 15u) * 8;
+    for (uint64_t i0 = (uint64_t)blockIdx.x * 16; i0 < rows; i0 += (uint64_t)gridDim.x * 16) {
+        const uint64_t i = i0 + (threadIdx.x >> 4);
+        float sum = 0.0f;
+        if (i < rows && d < dim) {
+            const bf16 *a = dout.at(i / heads, i % heads) + d, *b = o.at(i / heads, i % heads) + d;
+            float x[8], y[8];
+            if (d + 8 <= dim) load_vec<bf16, 8>(a, x), load_vec<bf16, 8>(b, y);
+            else load_part<bf16, 8>(a, (int)(dim - d), x), load_part<bf16, 8>(b, (int)(dim - d), y);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) sum += x[k] * y[k];
+        }
+#pragma unroll
+        for (int m = 8; m; m >>= 1) sum += __shfl_xor(sum, m);
+        if (i < rows && d == 0) delta[i] = sum;
+    }
+}
+
+// dQ of a tile of rows, over the keys they see: dS^T = P^T * (V dO^T - delta) and
+// dQ^T += K^T dS^T, S^T as in the forward pass.
+template <int DP> __global__ __launch_bounds__(256, 2) void attention_dq_kernel(const AttnArgs a)
+{
+    typedef Stage<DP> S;
+    extern __shared__ __attribute__((aligned(16))) char lds[];
+    const uint32_t wave = uniform(threadIdx.x >> 6);
+    const uint32_t tiles = a.slots * a.kv_heads * a.splits;
+    if (blockIdx.x >= tiles) {
+        clear_rest(a.dq, a.starts_q, a.sequences, a.tokens_q, a.heads, a.dim, blockIdx.x - tiles);
+        return;
+    }
+    const uint32_t kv_head = blockIdx.x % a.kv_heads, rest = blockIdx.x / a.kv_heads, split = rest % a.splits;
+    const Place p = find_place(a, a.slots - 1 - rest / a.splits, false, a.group, kRows);
+    if (!p.some) return;
+    const Rows r = rows_of(a, p, p.tile * kRows + wave * 32, kv_head);
+    const uint32_t last = (p.tile + 1) * kRows < p.lq * a.group ? (p.tile + 1) * kRows - 1 : p.lq * a.group - 1;
+    const int64_t sees = a.causal ? (int64_t)(last / a.group) + 1 + p.lk - p.lq : (int64_t)p.lk;
+    const uint32_t stages = sees > 0 ? ((uint32_t)sees + kKeys - 1) / kKeys : 0;
+    const uint32_t begin = (uint32_t)((uint64_t)stages * split / a.splits), end = (uint32_t)((uint64_t)stages * (split + 1) / a.splits);
+
+    const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)lds;
+    S ks, vs;
+    ks.place(wave, a.k.ld, a.dim_in), vs.place(wave, a.v.ld, a.dim_in);
+    Reads<DP> at;
+    at.place(lds0);
+    auto load = [&](uint32_t t, uint32_t buf) {
+        const uint32_t key = t * kKeys;
+        ks.load(lds0 + buf * 2 * S::BYTES, wave, a.k.at(p.k0 + key, kv_head), p.lk - key);
+        vs.load(lds0 + buf * 2 * S::BYTES + S::BYTES, wave, a.v.at(p.k0 + key, kv_head), p.lk - key);
+    };
+    bf16x8 q[DP / 16], g[DP / 16];
+    load_row<DP>(a.q.at(p.q0 + r.query, r.head), a.dim_in, q);
+    load_row<DP>(a.dout.at(p.q0 + r.query, r.head), a.dim_in, g);
+    const uint64_t token = p.q0 + r.query;
+    const float lse = a.lse[token * a.heads + r.head] * kLog2e, delta = a.delta[token * a.heads + r.head], c = a.scale * kLog2e;
+    f32x16 dq[DP / 32];
+#pragma unroll
+    for (int b = 0; b < DP / 32; ++b) dq[b] = f32x16{};
+    const uint32_t h = threadIdx.x >> 5 & 1u;
+
+    auto stage = [&](uint32_t t, auto buffer) {
+        constexpr int K = buffer.value * 2 * S::BYTES, V = K + S::BYTES;
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+        if (t + 1 < end) load(t + 1, 1 - buffer.value);
+        if (t * kKeys >= r.most) return;
+        const bool masked = t * kKeys + kKeys > r.least;
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+            f32x16 s{}, dp{};
+#pragma unroll
+            for (int d = 0; d < DP / 16; ++d) s = Frag<bf16>::mfma(at.rows(b, d, K), q[d], s);
+#pragma unroll
+            for (int d = 0; d < DP / 16; ++d) dp = Frag<bf16>::mfma(at.rows(b, d, V), g[d], dp);
+#pragma unroll
+            for (int k = 0; k < 16; ++k) s[k] = __builtin_amdgcn_exp2f(s[k] * c - lse) * (dp[k] - delta);
+            if (masked) {
+                const uint32_t from = t * kKeys + b * 32 + 4 * h;
+#pragma unroll
+                for (int k = 0; k < 16; ++k)
+                    if (from + 8 * (k / 4) + k % 4 >= r.limit) s[k] = 0.0f;
+            }
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                const bf16x8 w = rounded(s, k * 8);
+#pragma unroll
+                for (int d = 0; d < DP / 32; ++d) dq[d] = Frag<bf16>::mfma(at.columns(d, b * 2 + k, K), w, dq[d]);
+            }
+        }
+    };
+    if (begin < end) load(begin, 0);
+    for (uint32_t t = begin; t < end; t += 2) {
+        stage(t, std::integral_constant<int, 0>{});
+        if (t + 1 < end) stage(t + 1, std::integral_constant<int, 1>{});
+    }
+    if (!r.real) return;
+    if (a.splits > 1)
+        store_row<DP>(a.part + (((uint64_t)split * a.tokens_q + token) * a.heads + r.head) * a.dim, a.dim, dq, a.scale);
+    else
+        store_row<DP>(a.dq.at(token, r.head), a.dim, dq, a.scale);
+}
+
+// dK and dV of 128 keys of a key head, 32 for each wave, over the queries that see
+// them, of every head of the group in turn: a lane holds one key.  dV^T += dO^T P and
+// dK^T += Q^T dS with P = e^(Q K^T - lse), dS = P * (dO V^T - delta).
+template <int DP> __global__ __launch_bounds__(256, 1) void attention_dkv_kernel(const AttnArgs a)
+{
+    typedef Stage<DP> S;
+    extern __shared__ __attribute__((aligned(16))) char lds[];
+    const uint32_t wave = uniform(threadIdx.x >> 6), lane = threadIdx.x & 63u, h = lane >> 5;
+    const uint32_t tiles = a.slots * a.kv_heads * a.splits;
+    if (blockIdx.x >= tiles) {
+        clear_rest(a.dk, a.starts_k, a.sequences, a.tokens_k, a.kv_heads, a.dim, blockIdx.x - tiles);
+        clear_rest(a.dv, a.starts_k, a.sequences, a.tokens_k, a.kv_heads, a.dim, blockIdx.x - tiles);
+        return;
+    }
+    const uint32_t kv_head = blockIdx.x % a.kv_heads, rest = blockIdx.x / a.kv_heads, split = rest % a.splits;
+    // the first tiles, which the most queries see, first
+    const Place p = find_place(a, rest / a.splits, true, 1, kRows);
+    if (!p.some) return;
+    const uint32_t key0 = p.tile * kRows, mine = key0 + wave * 32 + (lane & 31u);
+    // query i sees key j where i >= j + lq - lk
+    const int32_t shift = a.causal ? (int32_t)p.lq - (int32_t)p.lk : INT32_MIN / 2;
+    const int32_t need = (int32_t)mine + shift, wave_needs = (int32_t)(key0 + wave * 32 + 31) + shift;
+    const int32_t wave_from = (int32_t)(key0 + wave * 32) + shift;
+    const uint32_t first = (int32_t)key0 + shift > 0 ? (uint32_t)((int32_t)key0 + shift) / kKeys * kKeys : 0;
+    const uint32_t per = first < p.lq ? (p.lq - first + kKeys - 1) / kKeys : 0;  // stages of a head
+    const uint64_t all = (uint64_t)per * a.group;
+    const uint32_t begin = (uint32_t)(all * split / a.splits), end = (uint32_t)(all * (split + 1) / a.splits);
+
+    const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)lds;
+    float *stats = (float *)(lds + 4 * S::BYTES);  // of a buffer's queries: lse, delta
+    S qs, gs;
+    qs.place(wave, a.q.ld, a.dim_in), gs.place(wave, a.dout.ld, a.dim_in);
+    Reads<DP> at;
+    at.place(lds0);
+    uint32_t next_head = per ? begin / per : 0, next_query = per ? first + begin % per * kKeys : 0;  // of the next load
+    float ahead = 0.0f;
+    auto load = [&](uint32_t buf) {
+        const uint64_t token = p.q0 + next_query;
+        const uint32_t head = kv_head * a.group + next_head, left = p.lq - next_query;
+        // what a row without keys kept is minus infinity; its P is 0, as it is behind the last row
+        if (threadIdx.x < 2 * kKeys) {
+            const uint32_t i = threadIdx.x & (kKeys - 1);
+            const bool is_delta = threadIdx.x >= kKeys;
+            ahead = is_delta ? 0.0f : INFINITY;
+            if (i < left) {
+                ahead = (is_delta ? a.delta : a.lse)[(token + i) * a.heads + head];
+                if (!is_delta) ahead = ahead == -INFINITY ? INFINITY : ahead * kLog2e;
+            }
+        }
+        qs.load(lds0 + buf * 2 * S::BYTES, wave, a.q.at(token, head), left);
+        gs.load(lds0 + buf * 2 * S::BYTES + S::BYTES, wave, a.dout.at(token, head), left);
+        next_query += kKeys;
+        if (next_query >= p.lq) next_query = first, ++next_head;
+    };
+    auto keep = [&](uint32_t buf) {
+        if (threadIdx.x < 2 * kKeys) stats[buf * 2 * kKeys + threadIdx.x] = ahead;
+    };
+    bf16x8 kf[DP / 16], vf[DP / 16];
+    const uint32_t key = mine < p.lk ? mine : p.lk - 1;
+    load_row<DP>(a.k.at(p.k0 + key, kv_head), a.dim_in, kf);
+    load_row<DP>(a.v.at(p.k0 + key, kv_head), a.dim_in, vf);
+    f32x16 dk[DP / 32], dv[DP / 32];
+#pragma unroll
+    for (int b = 0; b < DP / 32; ++b) dk[b] = f32x16{}, dv[b] = f32x16{};
+    const float c = a.scale * kLog2e;
+    uint32_t query = next_query;  // of this stage
+
+    auto stage = [&](uint32_t t, auto buffer) {
+        constexpr int Q = buffer.value * 2 * S::BYTES, G = Q + S::BYTES;
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+        const int32_t here = (int32_t)query;
+        query += kKeys;
+        if (query >= p.lq) query = first;
+        const bool more = t + 1 < end;
+        if (more) load(1 - buffer.value);
+        if (here + kKeys > wave_from) {
+            const float *st = stats + buffer.value * 2 * kKeys;
+            const bool masked = here < wave_needs;
+#pragma unroll
+            for (int b = 0; b < 2; ++b) {
+                f32x16 s{}, dp{};
+#pragma unroll
+                for (int d = 0; d < DP / 16; ++d) s = Frag<bf16>::mfma(at.rows(b, d, Q), kf[d], s);
+#pragma unroll
+                for (int d = 0; d < DP / 16; ++d) dp = Frag<bf16>::mfma(at.rows(b, d, G), vf[d], dp);
+#pragma unroll
+                for (int k4 = 0; k4 < 4; ++k4) {
+                    typedef float f32x4 __attribute__((ext_vector_type(4)));
+                    const f32x4 lse = *(const f32x4 *)(st + b * 32 + 8 * k4 + 4 * h), delta = *(const f32x4 *)(st + kKeys + b * 32 + 8 * k4 + 4 * h);
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        const int n = k4 * 4 + k;
+                        s[n] = __builtin_amdgcn_exp2f(s[n] * c - lse[k]);
+                        dp[n] = s[n] * (dp[n] - delta[k]);
+                        if (masked && here + (int32_t)(b * 32 + 8 * k4 + 4 * h + k) < need) s[n] = 0.0f, dp[n] = 0.0f;
+                    }
+                }
+#pragma unroll
+                for (int k = 0; k < 2; ++k) {
+                    const bf16x8 w = rounded(s, k * 8), u = rounded(dp, k * 8);
+#pragma unroll
+                    for (int d = 0; d < DP / 32; ++d) {
+                        dv[d] = Frag<bf16>::mfma(at.columns(d, b * 2 + k, G), w, dv[d]);
+                        dk[d] = Frag<bf16>::mfma(at.columns(d, b * 2 + k, Q), u, dk[d]);
+                    }
+                }
+            }
+        }
+        if (more) keep(1 - buffer.value);
+    };
+    if (begin < end) load(0), keep(0);
+    for (uint32_t t = begin; t < end; t += 2) {
+        stage(t, std::integral_constant<int, 0>{});
+        if (t + 1 < end) stage(t + 1, std::integral_constant<int, 1>{});
+    }
+    if (mine >= p.lk) return;
+    if (a.splits > 1) {
+        const uint64_t all_rows = (uint64_t)a.tokens_k * a.kv_heads, row = (uint64_t)(p.k0 + mine) * a.kv_heads + kv_head;
+        store_row<DP>(a.part + (split * all_rows + row) * a.dim, a.dim, dk, a.scale);
+        store_row<DP>(a.part + ((a.splits + split) * all_rows + row) * a.dim, a.dim, dv, 1.0f);
+    } else {
+        store_row<DP>(a.dk.at(p.k0 + mine, kv_head), a.dim, dk, a.scale);
+        store_row<DP>(a.dv.at(p.k0 + mine, kv_head), a.dim, dv, 1.0f);
+    }
+}
+
+// Adds the runs of a split gradient, in their order: [split][token][head][dim].
+__global__ __launch_bounds__(256) void attention_sum_kernel(const float *part, const Heads<bf16> out, const int32_t *starts,
+                                                            uint32_t sequences, uint32_t tokens, uint32_t heads, uint32_t dim, uint32_t splits)
+{
+    const uint32_t from = start_of(starts, 0, tokens), until = start_of(starts, starts ? sequences : 1, tokens);
+    const uint64_t rows = (uint64_t)tokens * heads, n = rows * dim;
+    for (uint64_t i = (uint64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (uint64_t)gridDim.x * 256) {
+        const uint64_t row = i / dim;
+        const uint32_t token = (uint32_t)(row / heads), d = (uint32_t)(i % dim);
+        if (token < from || token >= until) continue;
+        float v = part[i];
+#pragma unroll 4
+        for (uint32_t s = 1; s < splits; ++s) v += part[s * n + i];
+        out.at(token, row % heads)[d] = (bf16)v;
+    }
+}
+
+// Copies rows that the kernels cannot read where they lie, with zeros up to a
+// multiple of eight elements.
+struct HeadsCopy {
+    Heads<const bf16> from;
+    bf16 *to;
+    uint64_t rows;
+    uint32_t heads;
+};
+struct HeadsCopies {
+    HeadsCopy c[4];
+    uint32_t n, dim;
+};
+__global__ __launch_bounds__(256) void attention_pack_kernel(const HeadsCopies list)
+{
+    const HeadsCopy c = list.c[blockIdx.y];
+    const uint32_t per = (list.dim + 7) / 8;
+    const uint64_t n = c.rows * per;
+    for (uint64_t i = (uint64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (uint64_t)gridDim.x * 256) {
+        const uint64_t row = i / per;
+        const uint32_t d = (uint32_t)(i % per) * 8;
+        const bf16 *from = c.from.at(row / c.heads, row % c.heads) + d;
+        float v[8];
+        if (d + 8 <= list.dim) load_vec<bf16, 8>(from, v);
+        else load_part<bf16, 8>(from, (int)(list.dim - d), v);
+        store_vec<bf16, 8>(c.to + row * per * 8 + d, v);
+    }
+}
+
+}  // namespace dev
+
+namespace {
+
+using namespace dev;
+
+// One of the tensors of a call, as the checks see it: a matrix of the tokens' rows
+// where a token's heads lie within the stride between tokens, else one of the heads'.
+struct Tensor {
+    const void *p;
+    size_t tokens, heads, dim, ld, hs;
+    bool by_token() const { return heads == 1 || ld >= (heads - 1) * hs + dim; }
+    Mat mat() const
+    {
+        if (!tokens || !heads) return Mat{p, 0, 0, 0, 2};
+        return by_token() ? Mat{p, tokens, (heads - 1) * hs + dim, ld, 2} : Mat{p, heads, (tokens - 1) * ld + dim, hs, 2};
+    }
+    // elements of a tensor do not overlap, and are counted in 64 bits
+    bool ok() const
+    {
+        if ((uintptr_t)p % 2 != 0) return false;
+        if (!tokens || !heads) return true;
+        if (!p || ld < dim || hs < dim || ld > kOpsMaxSize / tokens || hs > kOpsMaxSize / heads) return false;
+        return by_token() || tokens == 1 || hs >= (tokens - 1) * ld + dim;
+    }
+    bool direct() const
+    {
+        return (uintptr_t)p % 16 == 0 && ld % 8 == 0 && hs % 8 == 0 && dim % 8 == 0 && gemm_reaches(ld * 2, dim * 2);
+    }
+    size_t copy_bytes() const { return round_up(tokens * heads * round_up(dim, 8) * 2, 256); }
+};
+template <typename T> Heads<T> heads_of(const Tensor &t) { return {(T *)t.p, t.ld, t.hs}; }
+
+// `heads` 0: a stride that is not given
+Tensor tensor(const void *p, size_t tokens, size_t heads, size_t dim, size_t ld, size_t hs)
+{
+    hs = hs ? hs : dim;
+    return {p, tokens, heads, dim, ld ? ld : heads * hs, hs};
+}
+
+int check_attention(const ar_attention_desc *d)
+{
+    if (!d) return AR_ERR_ARG;
+    if (d->dtype != AR_BFLOAT16) return AR_ERR_UNSUPPORTED;
+    if (d->flags & ~(AR_ATTN_CAUSAL | AR_ATTN_CLEAR)) return AR_ERR_ARG;
+    if (!(d->scale > 0.0f) || !isfinite(d->scale)) return AR_ERR_ARG;
+    if (d->heads < 1 || d->kv_heads < 1 || d->heads > (1u << 16) || d->heads % d->kv_heads || d->dim < 1) return AR_ERR_ARG;
+    if (d->dim > 128) return AR_ERR_UNSUPPORTED;
+    // rows are counted in 32 bits on the device
+    if (d->sequences > (1u << 24) || d->tokens_q > (1u << 30) || d->tokens_k > (1u << 30)) return AR_ERR_ARG;
+    if (d->tokens_q * d->heads >= (1ull << 31) || d->tokens_k * d->kv_heads >= (1ull << 31)) return AR_ERR_ARG;
+    if (d->sequences * d->heads >= (1ull << 28)) return AR_ERR_ARG;
+    const size_t strides[] = {d->ld_q, d->hs_q, d->ld_k, d->hs_k, d->ld_v, d->hs_v, d->ld_o, d->hs_o, d->ld_dout, d->hs_dout,
+                              d->ld_dq, d->hs_dq, d->ld_dk, d->hs_dk, d->ld_dv, d->hs_dv};
+    for (size_t s : strides)
+        if (s > kOpsMaxSize) return AR_ERR_ARG;
+    return AR_OK;
+}
+
+struct AttnTensors {
+    Tensor q, k, v, o;
+};
+AttnTensors attn_tensors(const ar_attention_desc &d, const void *q, const void *k, const void *v, const void *o)
+{
+    return {tensor(q, d.tokens_q, d.heads, d.dim, d.ld_q, d.hs_q), tensor(k, d.tokens_k, d.kv_heads, d.dim, d.ld_k, d.hs_k),
+            tensor(v, d.tokens_k, d.kv_heads, d.dim, d.ld_v, d.hs_v), tensor(o, d.tokens_q, d.heads, d.dim, d.ld_o, d.hs_o)};
+}
+
+// Tiles that the grid has room for: of queries' rows, and of keys.
+size_t row_slots(const ar_attention_desc &d) { return d.tokens_q * (d.heads / d.kv_heads) / kRows + d.sequences; }
+size_t key_slots(const ar_attention_desc &d) { return d.tokens_k / kRows + d.sequences; }
+
+// Runs that each tile's `stages` are split into so that `units` workgroups have work:
+// none shorter than `least` in the mean.
+uint32_t splits_for(size_t tiles, size_t stages, size_t units, size_t least)
+{
+    if (tiles >= units || !tiles) return 1;
+    size_t s = (units + tiles - 1) / tiles, most = stages / least;
+    s = s < most ? s : most;
+    return (uint32_t)(s < 1 ? 1 : s < 64 ? s : 64);
+}
+size_t mean(size_t tokens, const ar_attention_desc &d) { return (tokens + d.sequences - 1) / d.sequences; }
+uint32_t forward_splits(const ar_attention_desc &d)
+{
+    return splits_for(row_slots(d) * d.kv_heads, (mean(d.tokens_k, d) + kKeys - 1) / kKeys, 1024, 2);
+}
+uint32_t dq_splits(const ar_attention_desc &d)
+{
+    return splits_for(row_slots(d) * d.kv_heads, (mean(d.tokens_k, d) + kKeys - 1) / kKeys, 512, 4);
+}
+uint32_t dkv_splits(const ar_attention_desc &d)
+{
+    return splits_for(key_slots(d) * d.kv_heads, (mean(d.tokens_q, d) + kKeys - 1) / kKeys * (d.heads / d.kv_heads), 256, 4);
+}
+
+size_t part_bytes(uint32_t splits, size_t rows, size_t each) { return splits > 1 ? round_up(splits * rows * each * sizeof(float), 256) : 0; }
+size_t forward_part(const ar_attention_desc &d) { return part_bytes(forward_splits(d), d.tokens_q * d.heads, d.dim + 1); }
+
+bool nothing(const ar_attention_desc &d) { return d.sequences == 0 || (d.tokens_q == 0 && d.tokens_k == 0); }
+
+size_t attention_workspace(const ar_attention_desc &d)
+{
+    if (nothing(d)) return 0;
+    const AttnTensors t = attn_tensors(d, nullptr, nullptr, nullptr, nullptr);
+    return t.q.copy_bytes() + t.k.copy_bytes() + t.v.copy_bytes() + forward_part(d);
+}
+size_t attention_need(const ar_attention_desc &d, const AttnTensors &t)
+{
+    size_t need = forward_part(d);
+    for (const Tensor &in : {t.q, t.k, t.v})
+        if (!in.direct()) need += in.copy_bytes();
+    return need;
+}
+size_t attention_workspace_for(const ar_attention_desc *desc, const void *q, const void *k, const void *v)
+{
+    if (check_attention(desc) != AR_OK || nothing(*desc)) return 0;
+    return attention_need(*desc, attn_tensors(*desc, q, k, v, nullptr));
+}
+
+// A tensor as the kernels read it: itself, or a copy.
+Heads<const bf16> readable(const Tensor &t, char *&ws, HeadsCopies *list)
+{
+    if (t.direct()) return heads_of<const bf16>(t);
+    const uint64_t dim = round_up(t.dim, 8);
+    list->c[list->n++] = {heads_of<const bf16>(t), (bf16 *)ws, t.tokens * t.heads, (uint32_t)t.heads};
+    const Heads<const bf16> to{(const bf16 *)ws, t.heads * dim, dim};
+    ws += t.copy_bytes();
+    return to;
+}
+uint32_t groups_for(uint64_t threads)
+{
+    const uint64_t n = (threads + 255) / 256;
+    return (uint32_t)(n < 1 ? 1 : n < 8192 ? n : 8192);
+}
+int run_copies(const HeadsCopies &list, hipStream_t st)
+{
+    if (!list.n) return AR_OK;
+    uint64_t most = 0;
+    for (uint32_t k = 0; k < list.n; ++k) most = list.c[k].rows > most ? list.c[k].rows : most;
+    hipLaunchKernelGGL(attention_pack_kernel, dim3(groups_for(most * ((list.dim + 7) / 8)), list.n), dim3(256), 0, st, list);
+    return launch_status();
+}
+
+AttnArgs attn_args(const ar_attention_desc &d, const int32_t *starts_q, const int32_t *starts_k)
+{
+    AttnArgs a{};
+    a.starts_q = starts_q, a.starts_k = starts_k;
+    a.sequences = (uint32_t)d.sequences, a.tokens_q = (uint32_t)d.tokens_q, a.tokens_k = (uint32_t)d.tokens_k;
+    a.heads = (uint32_t)d.heads, a.kv_heads = (uint32_t)d.kv_heads, a.group = (uint32_t)(d.heads / d.kv_heads);
+    a.dim = (uint32_t)d.dim, a.dim_in = (uint32_t)round_up(d.dim, 8);
+    a.causal = d.flags & AR_ATTN_CAUSAL ? 1 : 0, a.rest = d.flags & AR_ATTN_CLEAR ? 1 : 0, a.scale = d.scale;
+    return a;
+}
+
+template <typename K> int launch_tiles(OncePerDevice &once, K kernel, int lds, const AttnArgs &a, hipStream_t st)
+{
+    const int rc = allow_lds(once, (const void *)kernel, lds);
+    if (rc != AR_OK) return rc;
+    const uint32_t groups = a.slots * a.kv_heads * a.splits + (a.rest ? kRestGroups : 0);
+    hipLaunchKernelGGL(kernel, dim3(groups), dim3(256), lds, st, a);
+    return launch_status();
+}
+template <int DP> int launch_forward(const AttnArgs &a, hipStream_t st)
+{
+    static OncePerDevice once;
+    return launch_tiles(once, attention_kernel<DP>, 4 * Stage<DP>::BYTES, a, st);
+}
+template <int DP> int launch_dq(const AttnArgs &a, hipStream_t st)
+{
+    static OncePerDevice once;
+    return launch_tiles(once, attention_dq_kernel<DP>, 4 * Stage<DP>::BYTES, a, st);
+}
+template <int DP> int launch_dkv(const AttnArgs &a, hipStream_t st)
+{
+    static OncePerDevice once;
+    return launch_tiles(once, attention_dkv_kernel<DP>, 4 * Stage<DP>::BYTES + 4 * kKeys * (int)sizeof(float), a, st);
+}
+
+// What both passes refuse of the inputs.
+bool inputs_ok(const ar_attention_desc &d, const AttnTensors &t, const int32_t *starts_q, const int32_t *starts_k)
+{
+    if ((uintptr_t)starts_q % 4 != 0 || (uintptr_t)starts_k % 4 != 0 || !starts_q != !starts_k) return false;
+    if (!starts_q && d.sequences != 1) return false;
+    return t.q.ok() && t.k.ok() && t.v.ok() && t.o.ok();
+}
+Mat starts_mat(const int32_t *s, size_t sequences) { return Mat{s, 1, sequences + 1, sequences + 1, 4}; }
+
+int attention(const ar_attention_desc *desc, const void *q, const void *k, const void *v, const int32_t *starts_q,
+              const int32_t *starts_k, void *o, float *lse, void *ws, size_t ws_bytes, void *stream)
+{
+    int rc = check_attention(desc);
+    if (rc != AR_OK) return rc;
+    const ar_attention_desc &d = *desc;
+    if (nothing(d) || d.tokens_q == 0) return AR_OK;
+    const AttnTensors t = attn_tensors(d, q, k, v, o);
+    if (!inputs_ok(d, t, starts_q, starts_k) || (uintptr_t)lse % 4 != 0) return AR_ERR_ARG;
+    const Mat om = t.o.mat(), lm = mat(lse, d.tokens_q, d.heads, 0, AR_FLOAT32);
+    for (const Mat &in : {t.q.mat(), t.k.mat(), t.v.mat(), starts_mat(starts_q, d.sequences), starts_mat(starts_k, d.sequences)})
+        if (meet(om, in) || meet(lm, in)) return AR_ERR_ARG;
+    if (meet(om, lm)) return AR_ERR_ARG;
+    const size_t need = attention_need(d, t);
+    if (need) {
+        if (!ws || ws_bytes < need) return AR_ERR_SCRATCH;
+        if ((uintptr_t)ws % 256 != 0) return AR_ERR_ARG;
+        const Mat wm{ws, 1, need, need, 1};
+        for (const Mat &x : {t.q.mat(), t.k.mat(), t.v.mat(), om, lm, starts_mat(starts_q, d.sequences), starts_mat(starts_k, d.sequences)})
+            if (meet(wm, x)) return AR_ERR_ARG;
+    }
+    hipStream_t st = (hipStream_t)stream;
+    char *at = (char *)ws;
+    AttnArgs a = attn_args(d, starts_q, starts_k);
+    HeadsCopies copies{};
+    copies.dim = a.dim;
+    a.q = readable(t.q, at, &copies), a.k = readable(t.k, at, &copies), a.v = readable(t.v, at, &copies);
+    if ((rc = run_copies(copies, st)) != AR_OK) return rc;
+    a.o = heads_of<bf16>(t.o), a.lse = lse;
+    a.slots = (uint32_t)row_slots(d), a.splits = forward_splits(d);
+    a.part = (float *)at, a.part_lse = a.part + a.splits * d.tokens_q * d.heads * d.dim;
+    if ((rc = d.dim <= 64 ? launch_forward<64>(a, st) : launch_forward<128>(a, st)) != AR_OK || a.splits == 1) return rc;
+    hipLaunchKernelGGL(attention_join_kernel, dim3(groups_for(d.tokens_q * d.heads * 64)), dim3(256), 0, st, a);
+    return launch_status();
+}
+
+// ---- backward -------------------------------------------------------------------
+
+// Where the backward pass keeps what; copies lie behind the rest.
+struct BackwardSpace {
+    size_t part, copies;  // delta lies at the start
+};
+BackwardSpace backward_space(const ar_attention_desc &d, bool dq, bool dkv)
+{
+    BackwardSpace s{};
+    s.part = round_up(d.tokens_q * d.heads * sizeof(float), 256);
+    const size_t a = dq ? part_bytes(dq_splits(d), d.tokens_q * d.heads, d.dim) : 0;
+    const size_t b = dkv ? part_bytes(dkv_splits(d), 2 * d.tokens_k * d.kv_heads, d.dim) : 0;
+    s.copies = s.part + (a > b ? a : b);
+    return s;
+}
+size_t backward_bytes(const ar_attention_desc &d)
+{
+    if (nothing(d)) return 0;
+    const AttnTensors t = attn_tensors(d, nullptr, nullptr, nullptr, nullptr);
+    return backward_space(d, true, true).copies + 2 * t.q.copy_bytes() + t.k.copy_bytes() + t.v.copy_bytes();
+}
+
+int sum_runs(const float *part, const Heads<bf16> &out, const int32_t *starts, const AttnArgs &a, uint32_t tokens, uint32_t heads, hipStream_t st)
+{
+    hipLaunchKernelGGL(attention_sum_kernel, dim3(groups_for((uint64_t)tokens * heads * a.dim)), dim3(256), 0, st, part, out, starts,
+                       a.sequences, tokens, heads, a.dim, a.splits);
+    return launch_status();
+}
+
+int attention_backward(const ar_attention_desc *desc, const void *dout, const void *q, const void *k, const void *v, const void *o,
+                       const float *lse, const int32_t *starts_q, const int32_t *starts_k, void *dq, void *dk, void *dv, void *ws,
+                       size_t ws_bytes, void *stream)
+{
+    int rc = check_attention(desc);
+    if (rc != AR_OK) return rc;
+    const ar_attention_desc &d = *desc;
+    if (!dk != !dv) return AR_ERR_ARG;
+    if (nothing(d) || (!dq && !dk)) return AR_OK;
+    const AttnTensors t = attn_tensors(d, q, k, v, o);
+    const Tensor g = tensor(dout, d.tokens_q, d.heads, d.dim, d.ld_dout, d.hs_dout);
+    if (!inputs_ok(d, t, starts_q, starts_k) || !g.ok() || (uintptr_t)lse % 4 != 0 || (!lse && d.tokens_q)) return AR_ERR_ARG;
+    const Tensor out[3] = {tensor(dq, d.tokens_q, d.heads, d.dim, d.ld_dq, d.hs_dq),
+                           tensor(dk, d.tokens_k, d.kv_heads, d.dim, d.ld_dk, d.hs_dk),
+                           tensor(dv, d.tokens_k, d.kv_heads, d.dim, d.ld_dv, d.hs_dv)};
+    const Mat lm = mat(lse, d.tokens_q, d.heads, 0, AR_FLOAT32);
+    const size_t need = backward_bytes(d);
+    if (!ws || ws_bytes < need) return AR_ERR_SCRATCH;
+    if ((uintptr_t)ws % 256 != 0) return AR_ERR_ARG;
+    const Mat wm{ws, 1, need, need, 1};
+    const Mat ins[] = {t.q.mat(), t.k.mat(), t.v.mat(), t.o.mat(), g.mat(), lm, starts_mat(starts_q, d.sequences), starts_mat(starts_k, d.sequences)};
+    for (const Mat &in : ins)
+        if (meet(wm, in)) return AR_ERR_ARG;
+    for (int i = 0; i < 3; ++i) {
+        if (!out[i].p) continue;
+        if (!out[i].ok() || meet(out[i].mat(), wm)) return AR_ERR_ARG;
+        for (const Mat &in : ins)
+            if (meet(out[i].mat(), in)) return AR_ERR_ARG;
+        for (int j = 0; j < i; ++j)
+            if (out[j].p && meet(out[i].mat(), out[j].mat())) return AR_ERR_ARG;
+    }
+
+    hipStream_t st = (hipStream_t)stream;
+    const BackwardSpace s = backward_space(d, dq != nullptr, dk != nullptr);
+    char *at = (char *)ws + s.copies;
+    AttnArgs a = attn_args(d, starts_q, starts_k);
+    HeadsCopies copies{};
+    copies.dim = a.dim;
+    a.q = readable(t.q, at, &copies), a.k = readable(t.k, at, &copies), a.v = readable(t.v, at, &copies), a.dout = readable(g, at, &copies);
+    if ((rc = run_copies(copies, st)) != AR_OK) return rc;
+    a.lse = (float *)lse, a.delta = (float *)ws, a.part = (float *)((char *)ws + s.part);
+    if (d.tokens_q) {
+        const uint64_t rows = (uint64_t)d.tokens_q * d.heads;
+        hipLaunchKernelGGL(attention_delta_kernel, dim3(groups_for(rows * 16)), dim3(256), 0, st, heads_of<const bf16>(g),
+                           heads_of<const bf16>(t.o), (float *)ws, rows, a.heads, a.dim);
+        if ((rc = launch_status()) != AR_OK) return rc;
+    }
+    if (dk && d.tokens_k) {
+        a.dk = heads_of<bf16>(out[1]), a.dv = heads_of<bf16>(out[2]);
+        a.slots = (uint32_t)key_slots(d), a.splits = dkv_splits(d);
+        if ((rc = d.dim <= 64 ? launch_dkv<64>(a, st) : launch_dkv<128>(a, st)) != AR_OK) return rc;
+        if (a.splits > 1) {
+            if ((rc = sum_runs(a.part, a.dk, starts_k, a, a.tokens_k, a.kv_heads, st)) != AR_OK) return rc;
+            const uint64_t half = (uint64_t)a.splits * d.tokens_k * d.kv_heads * d.dim;
+            if ((rc = sum_runs(a.part + half, a.dv, starts_k, a, a.tokens_k, a.kv_heads, st)) != AR_OK) return rc;
+        }
+    }
+    if (dq && d.tokens_q) {
+        a.dq = heads_of<bf16>(out[0]);
+        a.slots = (uint32_t)row_slots(d), a.splits = dq_splits(d);
+        if ((rc = d.dim <= 64 ? launch_dq<64>(a, st) : launch_dq<128>(a, st)) != AR_OK) return rc;
+        if (a.splits > 1 && (rc = sum_runs(a.part, a.dq, starts_q, a, a.tokens_q, a.heads, st)) != AR_OK) return rc;
+    }
+    return AR_OK;
+}
+
+}  // namespace
+}  // namespace ar
+
+extern "C" int ar_attention(const ar_attention_desc *desc, const void *q, const void *k, const void *v, const int32_t *starts_q,
+                            const int32_t *starts_k, void *o, float *lse, void *workspace, size_t workspace_bytes, void *stream)
+{
+    return ar::ops_ret(ar::attention(desc, q, k, v, starts_q, starts_k, o, lse, workspace, workspace_bytes, stream));
+}
+
+extern "C" size_t ar_attention_workspace(const ar_attention_desc *desc)
+{
+    return ar::check_attention(desc) == AR_OK ? ar::attention_workspace(*desc) : 0;
+}
+
+extern "C" size_t ar_attention_workspace_for(const ar_attention_desc *desc, const void *q, const void *k, const void *v)
+{
+    return ar::attention_workspace_for(desc, q, k, v);
+}
+
+extern "C" int ar_attention_backward(const ar_attention_desc *desc, const void *dout, const void *q, const void *k, const void *v,
+                                     const void *o, const float *lse, const int32_t *starts_q, const int32_t *starts_k, void *dq,
+                                     void *dk, void *dv, void *workspace, size_t workspace_bytes, void *stream)
+{
+    return ar::ops_ret(ar::attention_backward(desc, dout, q, k, v, o, lse, starts_q, starts_k, dq, dk, dv, workspace, workspace_bytes, stream));
+}
+
+extern "C" size_t ar_attention_backward_workspace(const ar_attention_desc *desc)
+{
+    return ar::check_attention(desc) == AR_OK ? ar::backward_bytes(*desc) : 0;
+}

@@ -4,6 +4,8 @@ layer over the C ABI in include/ar_ops.h (formulas and roundings there).
     gated_ffn, gated_ffn_backward           act(x Wg^T) * (x Wu^T)
     residual_norm, residual_norm_backward   norm, gate, scaled residual, norm
     orthogonalize                           Newton-Schulz steps on an update
+    packed_attention, packed_attention_backward
+                                            attention over packed sequences
 
 Every step runs in the HIP library; torch provides device memory and streams.
 Tensors are checked on every call (ValueError, TypeError); what the library
@@ -33,6 +35,7 @@ OPS_ARGS_PATH = os.path.join(os.path.dirname(_ar.LIB_PATH), "_ops_args.so")
 AR_NORM_POST, AR_NORM_PRE = 1, 2
 AR_ACT_SILU, AR_ACT_GELU, AR_ACT_RELU = 0, 1, 2
 AR_ORTHO_MAX_STEPS = 16
+AR_ATTN_CAUSAL, AR_ATTN_CLEAR = 1, 2
 ACTS = {"silu": AR_ACT_SILU, "gelu": AR_ACT_GELU, "relu": AR_ACT_RELU}
 
 _P, _S, _I, _F = ctypes.c_void_p, ctypes.c_size_t, ctypes.c_int, ctypes.c_float
@@ -54,6 +57,12 @@ class ar_ortho_desc(ctypes.Structure):
                 ("eps", _F), ("scale", _F), ("ld_in", _S), ("ld_out", _S), ("stride_in", _S), ("stride_out", _S)]
 
 
+class ar_attention_desc(ctypes.Structure):
+    _fields_ = [("sequences", _S), ("tokens_q", _S), ("tokens_k", _S), ("heads", _S), ("kv_heads", _S), ("dim", _S), ("dtype", _I),
+                ("flags", _I), ("scale", _F)] + [(kind + name, _S) for name in ("q", "k", "v", "o", "dout", "dq", "dk", "dv")
+                                                 for kind in ("ld_", "hs_")]
+
+
 # Every symbol include/ar_ops.h declares, with (restype, argtypes).
 SIGNATURES = {
     "ar_residual_norm": (_I, [ctypes.POINTER(ar_norm_desc)] + [_P] * 8),
@@ -66,6 +75,11 @@ SIGNATURES = {
     "ar_gated_ffn_backward_workspace": (_S, [ctypes.POINTER(ar_ffn_desc)]),
     "ar_orthogonalize": (_I, [ctypes.POINTER(ar_ortho_desc)] + [_P] * 3 + [_S, _P]),
     "ar_orthogonalize_workspace": (_S, [ctypes.POINTER(ar_ortho_desc)]),
+    "ar_attention": (_I, [ctypes.POINTER(ar_attention_desc)] + [_P] * 8 + [_S, _P]),
+    "ar_attention_workspace": (_S, [ctypes.POINTER(ar_attention_desc)]),
+    "ar_attention_workspace_for": (_S, [ctypes.POINTER(ar_attention_desc)] + [_P] * 3),
+    "ar_attention_backward": (_I, [ctypes.POINTER(ar_attention_desc)] + [_P] * 12 + [_S, _P]),
+    "ar_attention_backward_workspace": (_S, [ctypes.POINTER(ar_attention_desc)]),
 }
 
 _bound = None
@@ -541,3 +555,145 @@ def orthogonalize_workspace(batch: int, rows: int, cols: int, dtype="f32") -> in
     """Bytes of orthogonalize's workspace."""
     d = ar_ortho_desc(batch=batch, rows=rows, cols=cols, dtype=_ar.DTYPES[dtype], steps=1, eps=0.0, scale=1.0)
     return _lib().ar_orthogonalize_workspace(ctypes.byref(d))
+
+
+# ---- attention ------------------------------------------------------------------
+
+def _heads(t, name, device, shape=None, dtype=None):
+    """(tokens, heads, dim, token stride, head stride)."""
+    if not t.is_cuda or t.device.index != device:
+        raise ValueError(f"{name} must be on the GPU of the call")
+    if dtype is not None and t.dtype != dtype:
+        raise TypeError(f"{name} is {t.dtype}, expected {dtype}")
+    if t.dim() != 3 or (shape is not None and tuple(t.shape) != shape):
+        raise ValueError(f"{name} is {tuple(t.shape)}, expected {'(tokens, heads, dim)' if shape is None else shape}")
+    (n, h, d), (ld, hs, one) = t.shape, t.stride()
+    if h == 0 or d == 0:
+        raise ValueError(f"{name} must have heads and elements")
+    if d > 1 and one != 1:
+        raise ValueError(f"the elements of a head of {name} must be contiguous")
+    if h == 1:
+        hs = d
+    if n <= 1:
+        ld = (h - 1) * hs + d
+    if ld < d or hs < d or not (ld >= (h - 1) * hs + d or hs >= (n - 1) * ld + d):
+        raise ValueError(f"the heads of {name} must not overlap")
+    return n, h, d, ld, hs
+
+
+def _starts(starts_q, starts_k, device):
+    """(sequences, address, address)."""
+    import torch
+
+    if starts_k is None:
+        starts_k = starts_q
+    if starts_q is None:
+        if starts_k is not None:
+            raise ValueError("starts_k is given without starts_q")
+        return 1, None, None
+    for t, name in ((starts_q, "starts_q"), (starts_k, "starts_k")):
+        if not t.is_cuda or t.device.index != device or t.dim() != 1 or not t.is_contiguous() or t.numel() < 1:
+            raise ValueError(f"{name} must be a contiguous row of sequences + 1 values on the GPU of the call")
+        if t.dtype != torch.int32:
+            raise TypeError(f"{name} is {t.dtype}, expected torch.int32")
+    if starts_q.numel() != starts_k.numel():
+        raise ValueError("starts_q and starts_k must have as many sequences")
+    return starts_q.numel() - 1, starts_q.data_ptr(), starts_k.data_ptr()
+
+
+def _attention_desc(q, k, v, starts_q, starts_k, causal, scale, device, clear):
+    n, h, dim, ld_q, hs_q = _heads(q, "q", device)
+    m, hk, _, ld_k, hs_k = _heads(k, "k", device, (k.shape[0], k.shape[1], dim) if k.dim() == 3 else (0, 0, dim), q.dtype)
+    _, _, _, ld_v, hs_v = _heads(v, "v", device, (m, hk, dim), q.dtype)
+    if h % hk:
+        raise ValueError(f"{h} heads cannot share {hk} key heads evenly")
+    sequences, sq, sk = _starts(starts_q, starts_k, device)
+    flags = (AR_ATTN_CAUSAL if causal else 0) | (AR_ATTN_CLEAR if clear else 0)
+    d = ar_attention_desc(sequences=sequences, tokens_q=n, tokens_k=m, heads=h, kv_heads=hk, dim=dim, dtype=_ar._dtype_of(q), flags=flags,
+                          scale=dim ** -0.5 if scale is None else scale, ld_q=ld_q, hs_q=hs_q, ld_k=ld_k, hs_k=hs_k, ld_v=ld_v, hs_v=hs_v)
+    return d, sq, sk
+
+
+def packed_attention(q, k, v, *, starts_q=None, starts_k=None, causal: bool = True, scale: Optional[float] = None, save: bool = False,
+                     out=None, stream=None):
+    """softmax(scale q k^T) v over packed sequences, bf16; with save also what
+    packed_attention_backward needs: (o, lse).
+
+    q: (queries, heads, dim), k and v: (keys, kv_heads, dim), dim up to 128, heads a
+    multiple of kv_heads; strides are free as long as the elements of a head are
+    contiguous, so all three may be parts of one tensor.  starts_q, starts_k: int32, on
+    the GPU, sequences + 1 values that do not decrease: sequence i has the tokens
+    starts[i] .. starts[i + 1] - 1; starts_k left out is starts_q, both left out one
+    sequence.  causal: a sequence's last query sees all its keys, each one before it one
+    less; a query that sees none has o = 0.  scale: 1 / sqrt(dim) unless given; above 0.
+    out: o to write to; tokens of no sequence are then left as they were, and are zeros
+    otherwise.  lse: (queries, heads) fp32."""
+    import torch
+
+    _tell_of_graphs(q, k, v)
+    with _On(q, stream) as on:
+        d, sq, sk = _attention_desc(q, k, v, starts_q, starts_k, causal, scale, on.index, out is None)
+        o = torch.empty(q.shape, dtype=q.dtype, device=q.device) if out is None else out
+        _, _, _, d.ld_o, d.hs_o = _heads(o, "out", on.index, tuple(q.shape), q.dtype)
+        lse = torch.empty(q.shape[:2], dtype=torch.float32, device=q.device) if save else None
+        L = _lib()
+        need = L.ar_attention_workspace_for(ctypes.byref(d), q.data_ptr(), k.data_ptr(), v.data_ptr())
+        ws = _workspace(need, q)
+        rc = L.ar_attention(ctypes.byref(d), q.data_ptr(), k.data_ptr(), v.data_ptr(), sq, sk, o.data_ptr(), _ptr(lse), _ptr(ws), need,
+                            on.ptr)
+        _ar._check(rc, "ar_attention")
+        if d.sequences == 0 and out is None:
+            o.zero_()
+    return (o, lse) if save else o
+
+
+def packed_attention_backward(do, q, k, v, o, lse, *, starts_q=None, starts_k=None, causal: bool = True, scale: Optional[float] = None,
+                              need_dq: bool = True, need_dkv: bool = True, out=None, workspace=None, stream=None):
+    """Gradients of packed_attention with regard to q, k and v: (dq, dk, dv); None
+    for those not needed (need_dq, need_dkv).
+
+    o, lse: from packed_attention(save=True) on the same arguments.  out: the three
+    results to write to, which may be parts of one tensor; tokens of no sequence are
+    then left as they were, and are zeros otherwise.  workspace: a uint8 tensor to use in
+    place of a new one (packed_attention_backward_workspace)."""
+    import torch
+
+    _tell_of_graphs(do, q, k, v)
+    with _On(q, stream) as on:
+        dev = on.index
+        d, sq, sk = _attention_desc(q, k, v, starts_q, starts_k, causal, scale, dev, out is None)
+        _, _, _, d.ld_dout, d.hs_dout = _heads(do, "do", dev, tuple(q.shape), q.dtype)
+        _, _, _, d.ld_o, d.hs_o = _heads(o, "o", dev, tuple(q.shape), q.dtype)
+        if not lse.is_cuda or lse.device.index != dev or lse.dtype != torch.float32 or not lse.is_contiguous() or lse.shape != q.shape[:2]:
+            raise ValueError("lse must be what packed_attention(save=True) returned for these tensors")
+        dq, dk, dv = (None, None, None) if out is None else out
+        new = lambda like: torch.empty(like.shape, dtype=like.dtype, device=like.device)  # noqa: E731
+        if need_dq:
+            dq = new(q) if dq is None else dq
+            _, _, _, d.ld_dq, d.hs_dq = _heads(dq, "dq", dev, tuple(q.shape), q.dtype)
+        if need_dkv:
+            dk, dv = new(k) if dk is None else dk, new(v) if dv is None else dv
+            _, _, _, d.ld_dk, d.hs_dk = _heads(dk, "dk", dev, tuple(k.shape), q.dtype)
+            _, _, _, d.ld_dv, d.hs_dv = _heads(dv, "dv", dev, tuple(v.shape), q.dtype)
+        L, ws = _lib(), workspace
+        if ws is None:
+            ws = _workspace(L.ar_attention_backward_workspace(ctypes.byref(d)), q)
+        elif not ws.is_cuda or ws.device.index != dev or not ws.is_contiguous():
+            raise ValueError("workspace must be a contiguous tensor on the GPU of the call")
+        rc = L.ar_attention_backward(
+            ctypes.byref(d), do.data_ptr(), q.data_ptr(), k.data_ptr(), v.data_ptr(), o.data_ptr(), lse.data_ptr(), sq, sk,
+            _ptr(dq) if need_dq else None, _ptr(dk) if need_dkv else None, _ptr(dv) if need_dkv else None, _ptr(ws),
+            0 if ws is None else ws.numel() * ws.element_size(), on.ptr)
+        _ar._check(rc, "ar_attention_backward")
+        if d.sequences == 0 and out is None:
+            for t in (dq, dk, dv):
+                if t is not None:
+                    t.zero_()
+    return dq if need_dq else None, dk if need_dkv else None, dv if need_dkv else None
+
+
+def packed_attention_backward_workspace(queries: int, keys: int, heads: int, kv_heads: int, dim: int, sequences: int = 1) -> int:
+    """Bytes of packed_attention_backward's workspace."""
+    d = ar_attention_desc(sequences=sequences, tokens_q=queries, tokens_k=keys, heads=heads, kv_heads=kv_heads, dim=dim,
+                          dtype=_ar.AR_BFLOAT16, scale=1.0)
+    return _lib().ar_attention_backward_workspace(ctypes.byref(d))

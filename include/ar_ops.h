@@ -9,6 +9,10 @@
  *   ar_residual_norm   norm of a block's output, gate, scaled residual, norm
  *                      before the next block, and its backward pass
  *   ar_orthogonalize   Newton-Schulz products that orthogonalise an update
+ *   ar_attention       attention of a rank's heads over packed sequences, and
+ *                      its backward pass
+ *   ar_vocab_loss      cross entropy over a vocabulary or a rank's rows of it,
+ *                      and its backward pass
  *
  * Conventions.  As in ar.h: device pointers on the current device, sizes in
  * elements unless named *_bytes, `stream` a hipStream_t as void* (NULL = the
@@ -243,6 +247,54 @@ int ar_attention_backward(const ar_attention_desc *desc, const void *dout, const
                           const void *o, const float *lse, const int32_t *starts_q, const int32_t *starts_k, void *dq, void *dk,
                           void *dv, void *workspace, size_t workspace_bytes, void *stream);
 size_t ar_attention_backward_workspace(const ar_attention_desc *desc);
+
+/* ---- loss over a vocabulary ----------------------------------------------- */
+
+/* Softmax cross entropy of z = x W^T, one row of W for each class, of each token t:
+ *     lse_t = log sum_j e^z_tj,  loss_t = lse_t - z_t,target(t)
+ * W is the whole vocabulary, or a rank's rows of it: the classes first .. first + rows - 1
+ * of `classes`.  A token whose target is not one of 0 .. classes - 1, a negative one say,
+ * has no loss (0) and no gradient; its row of x has to be finite all the same where dW
+ * is wanted (0 times it is added there).  The logits are never in memory. */
+typedef struct ar_vocab_desc {
+    size_t tokens;         /* 0 is a valid no-op (backward: zero weight gradient) */
+    size_t dim;            /* 1 .. 2^20 */
+    size_t rows;           /* of W: 1 .. 2^28 */
+    size_t first, classes; /* first + rows <= classes <= 2^40 */
+    int dtype;             /* AR_BFLOAT16: x, W and their gradients */
+    int target_bytes;      /* 4 or 8: signed whole numbers */
+    size_t ld_x, ld_w, ld_dx, ld_dw;  /* row strides */
+} ar_vocab_desc;
+
+/* Forward, of the whole vocabulary (first 0, rows = classes): loss and lse, tokens
+ * floats each.  x and W are copied into the workspace where they cannot be read where
+ * they lie (not 16-byte aligned, dim or row stride no multiple of 8); the size named is
+ * for these pointers.  Errors: AR_ERR_ARG, AR_ERR_UNSUPPORTED, AR_ERR_SCRATCH, AR_ERR_HIP. */
+int ar_vocab_loss(const ar_vocab_desc *desc, const void *x, const void *w, const void *target, float *loss, float *lse,
+                  void *workspace, size_t workspace_bytes, void *stream);
+size_t ar_vocab_loss_workspace(const ar_vocab_desc *desc, const void *x, const void *w);
+
+/* Forward of a rank's rows: part[0 .. tokens - 1] = log sum e^z over them, part[tokens ..]
+ * the target's logit, 0 where the target is none of them.  Workspace as above. */
+int ar_vocab_loss_part(const ar_vocab_desc *desc, const void *x, const void *w, const void *target, float *part,
+                       void *workspace, size_t workspace_bytes, void *stream);
+/* Joins the parts of `ranks` ranks (1 .. 65536), one after another, whose rows make up the
+ * vocabulary.  Of the description tokens, classes and target_bytes count. */
+int ar_vocab_loss_join(const ar_vocab_desc *desc, size_t ranks, const float *parts, const void *target, float *loss, float *lse,
+                       void *stream);
+
+/* Backward.  From dloss (of token t at dloss[t * dloss_stride]; stride 0: one for all) and
+ * lse of the whole vocabulary:
+ *     dz_tj = (e^(z_tj - lse_t) - [j = target(t)]) dloss_t
+ *     dx = dz W  (of a rank's rows: its part of the sum over the ranks),  dW = dz^T x
+ * The logits are computed again.  dz is rounded to bf16 as an operand of these products
+ * and kept for a piece of the rows at a time, at most 512 MiB or 1024 rows.  dx or dw may
+ * be NULL (not wanted). */
+int ar_vocab_loss_backward(const ar_vocab_desc *desc, const float *dloss, size_t dloss_stride, const void *x, const void *w,
+                           const void *target, const float *lse, void *dx, void *dw, void *workspace,
+                           size_t workspace_bytes, void *stream);
+/* For a call with these pointers; dx, dw: whether the gradient is wanted. */
+size_t ar_vocab_loss_backward_workspace(const ar_vocab_desc *desc, const void *x, const void *w, int dx, int dw);
 
 #ifdef __cplusplus
 }

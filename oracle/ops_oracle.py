@@ -174,3 +174,46 @@ def attention(q, k, v, starts_q, starts_k, causal=True, scale=None, do=None):
     for name in ("dq", "dk", "dv"):  # a result's own rounding
         out[name] = out[name][0], out[name][1] * (1 + U) + U * out[name][0].abs() + UNDER
     return {**out, "lse": lse}
+
+
+def vocab_loss(x, w, target, dloss=None, device="cpu", chunk=1 << 26):
+    """Cross entropy over a vocabulary, and with `dloss` its gradients: {name: (value,
+    bound)}, with bounds of what an implementation may be off by that sums in fp32, rounds
+    dz to bf16 as an operand and the gradients once.
+
+    z: (dim + 16) U32 sum |x| |w|, a sum's bound; lse and loss: that, and a few roundings of
+    theirs; p: relative to itself what z and lse are off by; dz: U of itself and p's; sums of
+    dz: n U32 of their magnitudes, and U of the result."""
+    x, w, target = x.detach().to(device).double(), w.detach().to(device).double(), target.detach().to(device).long()
+    (t, dim), v = x.shape, w.shape[0]
+    new = lambda *s: torch.zeros(*s, dtype=torch.float64, device=device)  # noqa: E731
+    out = {"loss": (new(t), new(t)), "lse": (new(t), new(t))}
+    if dloss is not None:
+        dloss = dloss.detach().to(device).double().expand(t)
+        out |= {"dx": (new(t, dim), new(t, dim)), "dw": (new(v, dim), new(v, dim))}
+    for a in range(0, t, max(1, chunk // v)):
+        rows = slice(a, min(t, a + max(1, chunk // v)))
+        z, mag = x[rows] @ w.T, x[rows].abs() @ w.T.abs()
+        counts = (target[rows] >= 0) & (target[rows] < v)
+        at = torch.where(counts, target[rows], 0)[:, None]
+        top = z.amax(1, keepdim=True)
+        lse = top + torch.log(torch.exp(z - top).sum(1, keepdim=True))
+        z_off = (dim + 16) * U32 * mag.amax(1, keepdim=True)
+        lse_off = z_off + 2.0 ** -20 + 4 * U32 * (lse.abs() + top.abs())
+        picked = z.gather(1, at)
+        out["lse"][0][rows], out["lse"][1][rows] = lse[:, 0], lse_off[:, 0]
+        out["loss"][0][rows] = torch.where(counts, (lse - picked)[:, 0], 0.0)
+        out["loss"][1][rows] = torch.where(counts, (lse_off + z_off + 4 * U32 * picked.abs())[:, 0], 0.0)
+        if dloss is None:
+            continue
+        g = torch.where(counts, dloss[rows], 0.0)[:, None]
+        p = torch.exp(z - lse)
+        room = (ROOM + 2 * (z_off + lse_off)) * p
+        dz = p.scatter_add(1, at, torch.full_like(picked, -1.0)) * g
+        off = (U * 1.01 + max(v, t) * U32) * dz.abs() + room * g.abs()
+        out["dx"][0][rows], out["dx"][1][rows] = dz @ w, off @ w.abs()
+        out["dw"][0].add_(dz.T @ x[rows]), out["dw"][1].add_(off.T @ x[rows].abs())
+    for name in ("dx", "dw"):
+        if name in out:
+            out[name] = out[name][0], out[name][1] * (1 + U) + U * out[name][0].abs() + UNDER
+    return out

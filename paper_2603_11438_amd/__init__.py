@@ -702,4 +702,5 @@ def compulsory_bytes(msg_bytes: int, nranks: int) -> float:
 # The operators around the collectives (include/ar_ops.h).
 from .ops import (gated_ffn, gated_ffn_backward, gated_ffn_backward_workspace, orthogonalize,  # noqa: E402,F401
                   orthogonalize_workspace, packed_attention, packed_attention_backward, packed_attention_backward_workspace,
-                  residual_norm, residual_norm_backward, residual_norm_backward_workspace)
+                  residual_norm, residual_norm_backward, residual_norm_backward_workspace, vocab_loss, vocab_loss_backward,
+                  vocab_loss_backward_workspace, vocab_loss_join, vocab_loss_part)

@@ -6,6 +6,8 @@ layer over the C ABI in include/ar_ops.h (formulas and roundings there).
     orthogonalize                           Newton-Schulz steps on an update
     packed_attention, packed_attention_backward
                                             attention over packed sequences
+    vocab_loss, vocab_loss_part, vocab_loss_join, vocab_loss_backward
+                                            cross entropy over a vocabulary
 
 Every step runs in the HIP library; torch provides device memory and streams.
 Tensors are checked on every call (ValueError, TypeError); what the library
@@ -63,6 +65,11 @@ class ar_attention_desc(ctypes.Structure):
                                                  for kind in ("ld_", "hs_")]
 
 
+class ar_vocab_desc(ctypes.Structure):
+    _fields_ = [("tokens", _S), ("dim", _S), ("rows", _S), ("first", _S), ("classes", _S), ("dtype", _I), ("target_bytes", _I),
+                ("ld_x", _S), ("ld_w", _S), ("ld_dx", _S), ("ld_dw", _S)]
+
+
 # Every symbol include/ar_ops.h declares, with (restype, argtypes).
 SIGNATURES = {
     "ar_residual_norm": (_I, [ctypes.POINTER(ar_norm_desc)] + [_P] * 8),
@@ -80,6 +87,12 @@ SIGNATURES = {
     "ar_attention_workspace_for": (_S, [ctypes.POINTER(ar_attention_desc)] + [_P] * 3),
     "ar_attention_backward": (_I, [ctypes.POINTER(ar_attention_desc)] + [_P] * 12 + [_S, _P]),
     "ar_attention_backward_workspace": (_S, [ctypes.POINTER(ar_attention_desc)]),
+    "ar_vocab_loss": (_I, [ctypes.POINTER(ar_vocab_desc)] + [_P] * 6 + [_S, _P]),
+    "ar_vocab_loss_workspace": (_S, [ctypes.POINTER(ar_vocab_desc), _P, _P]),
+    "ar_vocab_loss_part": (_I, [ctypes.POINTER(ar_vocab_desc)] + [_P] * 5 + [_S, _P]),
+    "ar_vocab_loss_join": (_I, [ctypes.POINTER(ar_vocab_desc), _S] + [_P] * 5),
+    "ar_vocab_loss_backward": (_I, [ctypes.POINTER(ar_vocab_desc), _P, _S] + [_P] * 7 + [_S, _P]),
+    "ar_vocab_loss_backward_workspace": (_S, [ctypes.POINTER(ar_vocab_desc), _P, _P, _I, _I]),
 }
 
 _bound = None
@@ -697,3 +710,162 @@ def packed_attention_backward_workspace(queries: int, keys: int, heads: int, kv_
     d = ar_attention_desc(sequences=sequences, tokens_q=queries, tokens_k=keys, heads=heads, kv_heads=kv_heads, dim=dim,
                           dtype=_ar.AR_BFLOAT16, scale=1.0)
     return _lib().ar_attention_backward_workspace(ctypes.byref(d))
+
+
+# ---- loss over a vocabulary -------------------------------------------------------
+
+def _target(target, tokens, device):
+    """Bytes of a target."""
+    import torch
+
+    if not target.is_cuda or target.device.index != device or not target.is_contiguous() or target.numel() != tokens:
+        raise ValueError(f"target must hold {tokens} contiguous values on the GPU of the call")
+    if target.dtype not in (torch.int64, torch.int32):
+        raise TypeError(f"target is {target.dtype}, expected torch.int64 or torch.int32")
+    return target.element_size()
+
+
+def _vocab_desc(x, weight, target, first, classes, device):
+    tokens, dim, ld_x = _rows(x, "x")
+    if weight.dim() != 2:
+        raise ValueError("weight must be a matrix")
+    rows, _, ld_w = _rows(weight, "weight", dim, None, x.dtype, device)
+    if rows == 0 or dim == 0:
+        raise ValueError("weight must have rows and columns")
+    classes = first + rows if classes is None else classes
+    if first < 0 or first + rows > classes:
+        raise ValueError(f"rows {first} .. {first + rows - 1} are not among {classes} classes")
+    return ar_vocab_desc(tokens=tokens, dim=dim, rows=rows, first=first, classes=classes, dtype=_ar._dtype_of(x),
+                         target_bytes=_target(target, tokens, device), ld_x=ld_x, ld_w=ld_w)
+
+
+def _floats(t, name, shape, device):
+    import torch
+
+    if not t.is_cuda or t.device.index != device or not t.is_contiguous() or tuple(t.shape) != shape:
+        raise ValueError(f"{name} must be a contiguous tensor of shape {shape} on the GPU of the call")
+    if t.dtype != torch.float32:
+        raise TypeError(f"{name} is {t.dtype}, expected torch.float32")
+    return t
+
+
+def vocab_loss(x, weight, target, *, stream=None):
+    """Softmax cross entropy of each token over the classes x weight^T, without the
+    logits in memory: (loss, lse), both fp32 and shaped as target; lse, the logarithm of
+    the sum of the logits' exponentials, is what vocab_loss_backward needs.
+
+    x: (..., dim), bf16; weight: (classes, dim); target: int64 or int32, one for each
+    token; a target that is no class (a negative one, say) gives no loss and no gradient."""
+    import torch
+
+    _tell_of_graphs(x, weight)
+    with _On(x, stream) as on:
+        d = _vocab_desc(x, weight, target, 0, None, on.index)
+        loss, lse = (torch.empty(target.shape, dtype=torch.float32, device=x.device) for _ in range(2))
+        L = _lib()
+        need = L.ar_vocab_loss_workspace(ctypes.byref(d), x.data_ptr(), weight.data_ptr())
+        ws = _workspace(need, x)
+        if d.tokens:
+            rc = L.ar_vocab_loss(ctypes.byref(d), x.data_ptr(), weight.data_ptr(), target.data_ptr(), loss.data_ptr(), lse.data_ptr(), _ptr(ws),
+                                 need, on.ptr)
+            _ar._check(rc, "ar_vocab_loss")
+    return loss, lse
+
+
+def vocab_loss_part(x, weight, target, *, first: int, out=None, stream=None):
+    """A rank's part of vocab_loss, of the classes first .. first + rows - 1 that `weight`
+    has: (2, tokens) fp32, for vocab_loss_join.  out: the part to write to."""
+    import torch
+
+    _tell_of_graphs(x, weight)
+    with _On(x, stream) as on:
+        d = _vocab_desc(x, weight, target, first, None, on.index)  # targets behind these rows are another rank's
+        part = torch.empty(2, d.tokens, dtype=torch.float32, device=x.device) if out is None else _floats(out, "out", (2, d.tokens), on.index)
+        L = _lib()
+        need = L.ar_vocab_loss_workspace(ctypes.byref(d), x.data_ptr(), weight.data_ptr())
+        ws = _workspace(need, x)
+        rc = L.ar_vocab_loss_part(ctypes.byref(d), x.data_ptr(), weight.data_ptr(), target.data_ptr(), part.data_ptr(), _ptr(ws), need, on.ptr)
+        _ar._check(rc, "ar_vocab_loss_part")
+    return part
+
+
+def vocab_loss_join(parts, target, *, classes: int, stream=None):
+    """(loss, lse) from the parts of all ranks, (ranks, 2, tokens), gathered by an
+    AllReduce, say, of buffers in which each rank has filled its own."""
+    import torch
+
+    with _On(parts, stream) as on:
+        if parts.dim() != 3 or parts.shape[0] < 1 or parts.shape[1] != 2:
+            raise ValueError("parts must be (ranks, 2, tokens)")
+        tokens = parts.shape[2]
+        _floats(parts, "parts", tuple(parts.shape), on.index)
+        if classes < 1:
+            raise ValueError("classes must be 1 or more")
+        d = ar_vocab_desc(tokens=tokens, dim=1, rows=1, first=0, classes=classes, dtype=_ar.AR_BFLOAT16,
+                          target_bytes=_target(target, tokens, on.index))
+        loss, lse = (torch.empty(target.shape, dtype=torch.float32, device=parts.device) for _ in range(2))
+        rc = _lib().ar_vocab_loss_join(ctypes.byref(d), parts.shape[0], parts.data_ptr(), target.data_ptr(), loss.data_ptr(), lse.data_ptr(),
+                                       on.ptr)
+        _ar._check(rc, "ar_vocab_loss_join")
+    return loss, lse
+
+
+def vocab_loss_backward(dloss, x, weight, target, lse, *, first: Optional[int] = None, classes: Optional[int] = None, need_dx: bool = True,
+                        need_dw: bool = True, out=None, workspace=None, stream=None):
+    """Gradients of vocab_loss with regard to x and weight: (dx, dweight); None for
+    those not needed (need_dx, need_dw).
+
+    dloss: the gradient of each token's loss, fp32 and shaped as target, which may be
+    expanded from one value; lse: from vocab_loss or vocab_loss_join.  first, classes: where
+    `weight` is a rank's rows, as for vocab_loss_part and vocab_loss_join; dx is then that
+    rank's part of the sum over the ranks.  out: the two results to write to.  workspace: a uint8 tensor to
+    use in place of a new one (vocab_loss_backward_workspace)."""
+    import torch
+
+    _tell_of_graphs(dloss, x, weight)
+    with _On(x, stream) as on:
+        dev = on.index
+        if (first is None) != (classes is None):
+            raise ValueError("a rank's rows need both first and classes: targets of the other ranks' rows are told from no class by them")
+        d = _vocab_desc(x, weight, target, first or 0, classes, dev)
+        if not dloss.is_cuda or dloss.device.index != dev or dloss.numel() != d.tokens and dloss.numel() != 1:
+            raise ValueError(f"dloss must hold {d.tokens} values, or one, on the GPU of the call")
+        if dloss.dtype != torch.float32:
+            raise TypeError(f"dloss is {dloss.dtype}, expected torch.float32")
+        if dloss.numel() == 1 or all(s == 0 or n == 1 for n, s in zip(dloss.shape, dloss.stride())):
+            stride = 0
+        elif dloss.is_contiguous():
+            stride = 1
+        elif dloss.dim() == 1 and dloss.stride(0) > 0:
+            stride = dloss.stride(0)
+        else:
+            raise ValueError("dloss must be a row, contiguous, or expanded from one value")
+        if lse.numel() != d.tokens:
+            raise ValueError(f"lse must hold {d.tokens} values")
+        _floats(lse, "lse", tuple(lse.shape), dev)
+        dx, dw = (None, None) if out is None else out
+        if need_dx:
+            dx = torch.empty_like(x, memory_format=torch.contiguous_format) if dx is None else dx
+            _, _, d.ld_dx = _rows(dx, "dx", d.dim, d.tokens, x.dtype, dev)
+        if need_dw:
+            dw = torch.empty(d.rows, d.dim, dtype=x.dtype, device=x.device) if dw is None else dw
+            _, _, d.ld_dw = _rows(dw, "dweight", d.dim, d.rows, x.dtype, dev)
+        L, ws = _lib(), workspace
+        if ws is None:
+            ws = _workspace(L.ar_vocab_loss_backward_workspace(ctypes.byref(d), x.data_ptr(), weight.data_ptr(), need_dx, need_dw), x)
+        elif not ws.is_cuda or ws.device.index != dev or not ws.is_contiguous():
+            raise ValueError("workspace must be a contiguous tensor on the GPU of the call")
+        rc = L.ar_vocab_loss_backward(
+            ctypes.byref(d), dloss.data_ptr(), stride, x.data_ptr(), weight.data_ptr(), target.data_ptr(), lse.data_ptr(),
+            _ptr(dx) if need_dx else None, _ptr(dw) if need_dw else None, _ptr(ws), 0 if ws is None else ws.numel() * ws.element_size(),
+            on.ptr)
+        _ar._check(rc, "ar_vocab_loss_backward")
+    return dx if need_dx else None, dw if need_dw else None
+
+
+def vocab_loss_backward_workspace(x, weight, *, need_dx: bool = True, need_dw: bool = True) -> int:
+    """Bytes of vocab_loss_backward's workspace for these tensors."""
+    tokens, dim, ld_x = _rows(x, "x")
+    rows, _, ld_w = _rows(weight, "weight", dim, None, x.dtype)
+    d = ar_vocab_desc(tokens=tokens, dim=dim, rows=rows, first=0, classes=rows, dtype=_ar._dtype_of(x), target_bytes=8, ld_x=ld_x, ld_w=ld_w)
+    return _lib().ar_vocab_loss_backward_workspace(ctypes.byref(d), x.data_ptr(), weight.data_ptr(), need_dx, need_dw)

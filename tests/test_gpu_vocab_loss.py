@@ -1,0 +1,256 @@
+"""Cross entropy over a vocabulary on the GPU, against its definition in 64 bits, with
+the bounds that the oracle derives for each element."""
+from __future__ import annotations
+
+import math
+
+import pytest
+import torch
+
+import paper_2603_11438_amd as ar
+from gpu_helpers import say
+from oracle import ops_oracle as oo
+
+pytestmark = pytest.mark.gpu
+
+
+def draw(shape, seed, spread=1.0):
+    return (spread * torch.randn(*shape, generator=torch.Generator().manual_seed(seed))).bfloat16().cuda()
+
+
+def inputs(tokens, dim, classes, seed=0, spread=2.0, kind=torch.int64):
+    g = torch.Generator().manual_seed(seed + 5)
+    target = torch.randint(0, classes, (tokens,), generator=g, dtype=kind)
+    target[torch.rand(tokens, generator=g) < 0.1] = -100
+    dloss = torch.randn(tokens, generator=g) / tokens
+    return draw((tokens, dim), seed), draw((classes, dim), seed + 1, spread / math.sqrt(dim)), target.cuda(), dloss.cuda()
+
+
+def check(got, want, name):
+    value, bound = (t.to(got.device) for t in want)
+    off = (got.double() - value).abs()
+    assert bool((off <= bound).all()), f"{name}: {float((off / (bound + 1e-300)).max()):.3g} times its bound"
+
+
+def check_all(x, w, target, dloss, device="cpu"):
+    want = oo.vocab_loss(x, w, target, dloss, device)
+    loss, lse = ar.vocab_loss(x, w, target)
+    check(loss, want["loss"], "loss")
+    check(lse, want["lse"], "lse")
+    dx, dw = ar.vocab_loss_backward(dloss, x, w, target, lse)
+    check(dx, want["dx"], "dx")
+    check(dw, want["dw"], "dw")
+    return loss, lse, dx, dw
+
+
+SIZES = [(1, 64, 1), (1, 1, 2), (1, 7, 3), (2, 100, 97), (3, 63, 1000), (33, 512, 257), (64, 128, 5001), (65, 72, 128), (128, 512, 1000),
+         (130, 1000, 333), (200, 40, 31), (256, 256, 4096), (777, 100, 1201), (1030, 264, 2049), (1, 2000, 30001), (2100, 64, 8200)]
+
+
+@pytest.mark.parametrize("size", SIZES, ids=str)
+@pytest.mark.parametrize("kind", [torch.int64, torch.int32])
+def test_against_the_definition(size, kind):
+    say("loss", size, kind)
+    check_all(*inputs(*size, kind=kind), device="cuda" if size[0] * size[2] > 1 << 21 else "cpu")
+
+
+@pytest.mark.parametrize("size", [(2048, 64, 140001), (280001, 16, 1100)], ids=str)
+def test_pieces(size):
+    """dz of all rows would be larger than a piece may be: with runs of k in each piece, and
+    with a last piece that is short."""
+    say("pieces", size)
+    assert size[0] * size[2] * 2 > 1 << 29
+    check_all(*inputs(*size), device="cuda")
+
+
+@pytest.mark.parametrize("spread", [1e-3, 40.0])
+def test_even_and_certain(spread):
+    """From a loss of log(classes) to targets that have all the weight or none."""
+    say("spread", spread)
+    x, w, target, dloss = inputs(90, 128, 700, 3, spread)
+    target[::2] = (x.float() @ w.float().t()).argmax(1)[::2]
+    check_all(x, w, target, dloss)
+
+
+def test_targets_that_are_no_class():
+    x, w, target, dloss = inputs(70, 96, 500, 7)
+    for value in (-1, -100, 500, 1 << 40):
+        target[:40] = value
+        loss, lse, dx, dw = check_all(x, w, target, dloss)
+        assert not loss[:40].any() and not dx[:40].any() and bool(torch.isfinite(lse).all())
+    _, _, _, dw2 = check_all(x[40:], w, target[40:], dloss[40:])
+    target[:] = -100
+    loss, lse, dx, dw = check_all(x, w, target, dloss)
+    assert not loss.any() and not dx.any() and not dw.any()
+
+
+def test_ignored_tokens_may_hold_anything():
+    """NaN and infinities in padding give no loss and do not reach the others' gradients of x."""
+    x, w, target, dloss = inputs(150, 64, 300, 8)
+    target[50:90] = -100
+    clean = ar.vocab_loss(x, w, target)
+    dx = ar.vocab_loss_backward(dloss, x, w, target, clean[1])[0]
+    x[50:60], x[60:70] = math.nan, math.inf
+    loss, lse = ar.vocab_loss(x, w, target)
+    dx2 = ar.vocab_loss_backward(dloss, x, w, target, lse)[0]
+    assert torch.equal(loss, clean[0]) and torch.equal(dx, dx2)
+
+
+def layouts(t, name):
+    n, d = t.shape
+    if name == "unaligned":
+        at = torch.empty(n * d + 1, dtype=t.dtype, device=t.device)[1:].view(n, d)
+    elif name == "apart":
+        at = torch.full((n, d + 24), math.nan, dtype=t.dtype, device=t.device)[:, 8:d + 8]
+    else:
+        at = torch.full((n, d + 5), math.nan, dtype=t.dtype, device=t.device)[:, 3:d + 3]
+    return at.copy_(t)
+
+
+@pytest.mark.parametrize("name", ["unaligned", "apart", "odd apart"])
+@pytest.mark.parametrize("size", [(5, 64, 130), (140, 100, 515)], ids=str)
+def test_layouts(name, size):
+    say("layout", name, size)
+    x, w, target, dloss = inputs(*size, 11)
+    loss, lse = ar.vocab_loss(x, w, target)
+    dx, dw = ar.vocab_loss_backward(dloss, x, w, target, lse)
+    x2, w2 = layouts(x, name), layouts(w, name)
+    got = ar.vocab_loss(x2, w2, target)
+    assert torch.equal(got[0], loss) and torch.equal(got[1], lse)
+    out = layouts(torch.zeros_like(x), name), layouts(torch.zeros_like(w), name)
+    for a, b in (ar.vocab_loss_backward(dloss, x2, w2, target, lse), ar.vocab_loss_backward(dloss, x2, w2, target, lse, out=out)):
+        assert torch.equal(a, dx) and torch.equal(b, dw)
+
+
+def test_shapes_and_what_is_not_needed():
+    x, w, target, dloss = inputs(60, 64, 200, 13)
+    loss, lse = ar.vocab_loss(x, w, target)
+    dx, dw = ar.vocab_loss_backward(dloss, x, w, target, lse)
+    x3, t3 = x.view(4, 15, 64), target.view(4, 15)
+    loss3, lse3 = ar.vocab_loss(x3, w, t3)
+    assert loss3.shape == (4, 15) and torch.equal(loss3.view(-1), loss)
+    dx3, dw3 = ar.vocab_loss_backward(dloss.view(4, 15), x3, w, t3, lse3)
+    assert dx3.shape == x3.shape and torch.equal(dx3.view(60, 64), dx) and torch.equal(dw3, dw)
+    a, none = ar.vocab_loss_backward(dloss, x, w, target, lse, need_dw=False)
+    none2, b = ar.vocab_loss_backward(dloss, x, w, target, lse, need_dx=False)
+    assert none is None and none2 is None and torch.equal(a, dx) and torch.equal(b, dw)
+    ws = torch.empty(ar.vocab_loss_backward_workspace(x, w), dtype=torch.uint8, device="cuda")
+    for p, q in zip(ar.vocab_loss_backward(dloss, x, w, target, lse, workspace=ws), (dx, dw)):
+        assert torch.equal(p, q)
+
+
+def test_one_gradient_for_all_tokens():
+    x, w, target, _ = inputs(70, 64, 200, 14)
+    _, lse = ar.vocab_loss(x, w, target)
+    full = torch.full((70,), 1 / 64, device="cuda")
+    want = ar.vocab_loss_backward(full, x, w, target, lse)
+    apart = torch.zeros(70, 3, device="cuda")
+    apart[:, 1] = full
+    for dloss in (full[0], full[:1].expand(70), full[0].expand(7, 10), apart[:, 1]):
+        for a, b in zip(ar.vocab_loss_backward(dloss, x, w, target, lse), want):
+            assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("cuts", [[0, 500], [0, 100, 101, 500], [0, 125, 250, 375, 500]], ids=str)
+@pytest.mark.parametrize("tokens", [1, 75])
+def test_ranks(cuts, tokens):
+    """Rows split over ranks: the parts joined by the AllReduce, each rank's gradients."""
+    say("ranks", cuts, tokens)
+    x, w, target, dloss = inputs(tokens, 72, 500, 15)
+    want = oo.vocab_loss(x, w, target, dloss)
+    n = len(cuts) - 1
+    parts = [torch.zeros(n, 2, tokens, device="cuda") for _ in range(n)]
+    for r, (a, b) in enumerate(zip(cuts, cuts[1:])):
+        assert ar.vocab_loss_part(x, w[a:b], target, first=a, out=parts[r][r]) is not None
+        assert torch.equal(ar.vocab_loss_part(x, w[a:b], target, first=a), parts[r][r])
+    flat = [p.view(-1) for p in parts]
+    ar.allreduce(flat)
+    dx = []
+    for r, (a, b) in enumerate(zip(cuts, cuts[1:])):
+        loss, lse = ar.vocab_loss_join(flat[r].view(n, 2, tokens), target, classes=500)
+        check(loss, want["loss"], "loss")
+        check(lse, want["lse"], "lse")
+        part, dw = ar.vocab_loss_backward(dloss, x, w[a:b], target, lse, first=a, classes=500)
+        check(dw, (want["dw"][0][a:b], want["dw"][1][a:b]), "dw")
+        dx.append(part.double())
+    value, bound = want["dx"]
+    # each rank rounds its part; parts may cancel
+    mags = sum(p.abs() for p in dx).cpu() * oo.U
+    check(sum(dx), (value, bound + mags * (1 + oo.U)), "dx")
+
+
+def test_no_tokens():
+    x, w, target, _ = inputs(4, 64, 30, 16)
+    loss, lse = ar.vocab_loss(x[:0], w, target[:0])
+    assert loss.shape == (0,)
+    dx, dw = ar.vocab_loss_backward(loss, x[:0], w, target[:0], lse)
+    assert dx.shape == (0, 64) and dw.shape == w.shape and not dw.any()
+
+
+def test_another_stream_and_repeats():
+    x, w, target, dloss = inputs(300, 200, 3001, 17)
+    loss, lse = ar.vocab_loss(x, w, target)
+    grads = ar.vocab_loss_backward(dloss, x, w, target, lse)
+    other = torch.cuda.Stream()
+    other.wait_stream(torch.cuda.current_stream())
+    for _ in range(3):
+        got = ar.vocab_loss(x, w, target, stream=other)
+        got2 = ar.vocab_loss_backward(dloss, x, w, target, got[1], stream=other)
+        other.synchronize()
+        for a, b in zip((loss, lse, *grads), (*got, *got2)):
+            assert torch.equal(a, b)
+
+
+def test_graphs():
+    """Two captured steps, replayed between eager work with other values in the same memory."""
+    say("graphs")
+    x, w, target, dloss = inputs(200, 128, 1500, 18)
+
+    def step(n):
+        loss, lse = ar.vocab_loss(x[:n], w, target[:n])
+        return (loss, lse, *ar.vocab_loss_backward(dloss[:n], x[:n], w, target[:n], lse))
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step(200)
+    torch.cuda.current_stream().wait_stream(side)
+    graphs = []
+    for n in (200, 40):
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            got = step(n)
+        graphs.append((g, n, got))
+    for turn in range(4):
+        x.copy_(draw(x.shape, 300 + turn))
+        target.copy_(torch.randint(-20, 1500, (200,), generator=torch.Generator().manual_seed(turn)))
+        for g, n, got in graphs:
+            g.replay()
+            torch.cuda.synchronize()
+            for a, b in zip(got, step(n)):
+                assert torch.equal(a, b)
+
+
+def test_refusals():
+    x, w, target, dloss = inputs(8, 64, 40, 19)
+    loss, lse = ar.vocab_loss(x, w, target)
+    bad = [
+        (ValueError, lambda: ar.vocab_loss(x, w[:, :32], target)), (ValueError, lambda: ar.vocab_loss(x, w, target[:4])),
+        (TypeError, lambda: ar.vocab_loss(x, w.float(), target)), (TypeError, lambda: ar.vocab_loss(x, w, target.float())),
+        (ar.ARError, lambda: ar.vocab_loss(x.float(), w.float(), target)), (ValueError, lambda: ar.vocab_loss(x, w, target.cpu())),
+        (ValueError, lambda: ar.vocab_loss(x.cpu(), w, target)), (ValueError, lambda: ar.vocab_loss(x, w[:0], target)),
+        (ValueError, lambda: ar.vocab_loss(x.t(), w, target)), (ValueError, lambda: ar.vocab_loss(x, w[0], target)),
+        (ValueError, lambda: ar.vocab_loss_part(x, w, target, first=-1)), (ValueError, lambda: ar.vocab_loss_part(x, w, target, first=0, out=lse)),
+        (ValueError, lambda: ar.vocab_loss_join(lse, target, classes=40)), (ValueError, lambda: ar.vocab_loss_join(lse.new_zeros(2, 2, 8), target, classes=0)),
+        (ValueError, lambda: ar.vocab_loss_join(lse.new_zeros(2, 2, 7), target, classes=40)),
+        (ValueError, lambda: ar.vocab_loss_backward(dloss[:4], x, w, target, lse)), (TypeError, lambda: ar.vocab_loss_backward(dloss.double(), x, w, target, lse)),
+        (ValueError, lambda: ar.vocab_loss_backward(dloss, x, w, target, lse[:4])), (ValueError, lambda: ar.vocab_loss_backward(dloss, x, w, target, lse, first=0)),
+        (ValueError, lambda: ar.vocab_loss_backward(dloss, x, w, target, lse, classes=80)),
+        (ValueError, lambda: ar.vocab_loss_backward(dloss, x, w, target, lse, first=50, classes=80)),
+        (ar.ARError, lambda: ar.vocab_loss_backward(dloss, x, w, target, lse, out=(x, torch.empty_like(w)))),
+        (ar.ARError, lambda: ar.vocab_loss_backward(dloss, x, w, target, lse, workspace=torch.empty(16, dtype=torch.uint8, device="cuda"))),
+    ]
+    for n, (kind, call) in enumerate(bad):
+        with pytest.raises(kind):
+            call()
+            say("not refused:", n)

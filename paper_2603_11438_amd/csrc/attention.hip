@@ -145,28 +145,35 @@ template <int DP> struct Reads {
     __device__ __forceinline__ void place(uint32_t lds)
     {
         const uint32_t lane = threadIdx.x & 63u, h = lane >> 5, r = lane & 31u;
+        // The compiler would take an address apart again, for parts that several share, and
+        // add them up for every read; as they are, a read's constant goes into the instruction.
 #pragma unroll
-        for (int c = 0; c < DP / 16; ++c) by_row[c] = lds + r * Stage<DP>::ROW + ((2 * c + h) ^ Stage<DP>::turn(r)) * 16;
+        for (int c = 0; c < DP / 16; ++c) {
+            by_row[c] = lds + r * Stage<DP>::ROW + ((2 * c + h) ^ Stage<DP>::turn(r)) * 16;
+            asm("" : "+v"(by_row[c]));
+        }
 #pragma unroll
         for (int b = 0; b < DP / 32; ++b)
 #pragma unroll
             for (int s = 0; s < 2; ++s) {
                 const uint32_t k = 8 * s + 4 * h + (lane & 15u) / 4, c = 4 * b + 2 * (lane >> 4 & 1u) + (lane >> 1 & 1u);
                 across[b][s] = lds + k * Stage<DP>::ROW + (c ^ Stage<DP>::turn(k)) * 16 + (lane & 1u) * 8;
+                asm("" : "+v"(across[b][s]));
             }
     }
+    typedef __attribute__((address_space(3))) const char *P;
     // block: of 32 rows; c: of 16 elements; at: bytes from the stage that `place` was told
     __device__ __forceinline__ bf16x8 rows(int block, int c, int at) const
     {
-        return *(__attribute__((address_space(3))) const bf16x8 *)(uintptr_t)(by_row[c] + block * 32 * Stage<DP>::ROW + at);
+        return *(__attribute__((address_space(3))) const bf16x8 *)((P)(uintptr_t)by_row[c] + (block * 32 * Stage<DP>::ROW + at));
     }
     // block: of 32 elements; c: of 16 rows
     __device__ __forceinline__ bf16x8 columns(int block, int c, int at) const
     {
         typedef short s16x4 __attribute__((ext_vector_type(4)));
-        typedef __attribute__((address_space(3))) s16x4 *P;
-        const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((P)(uintptr_t)(across[block][0] + c * 16 * Stage<DP>::ROW + at));
-        const s16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((P)(uintptr_t)(across[block][1] + c * 16 * Stage<DP>::ROW + at));
+        typedef __attribute__((address_space(3))) s16x4 *V;
+        const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((V)((P)(uintptr_t)across[block][0] + (c * 16 * Stage<DP>::ROW + at)));
+        const s16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((V)((P)(uintptr_t)across[block][1] + (c * 16 * Stage<DP>::ROW + at)));
         return __builtin_bit_cast(bf16x8, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
     }
 };
@@ -192,7 +199,29 @@ __device__ __forceinline__ bf16x8 rounded(const f32x16 &v, int from)
     return f;
 }
 
-__device__ __forceinline__ float other_half(float v) { return __shfl_xor(v, 32); }
+// A lane's value and that of lane ^ 32.
+struct Halves {
+    float a, b;
+};
+__device__ __forceinline__ Halves halves(float v)
+{
+    const uint32_t u = __builtin_bit_cast(uint32_t, v);
+    const auto r = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+    return {__builtin_bit_cast(float, (uint32_t)r[0]), __builtin_bit_cast(float, (uint32_t)r[1])};
+}
+
+// One product, then so many reads of LDS for a later one and vector and transcendental
+// operations of what is independent of it, N times over: the matrix unit takes 32 cycles
+// for a product.
+template <int N, int READS, int VECTOR, int TRANS> __device__ __forceinline__ void interleave()
+{
+    static_for<N>([](auto) {
+        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+        if constexpr (READS) __builtin_amdgcn_sched_group_barrier(0x100, READS, 0);
+        if constexpr (VECTOR) __builtin_amdgcn_sched_group_barrier(0x002, VECTOR, 0);
+        if constexpr (TRANS) __builtin_amdgcn_sched_group_barrier(0x400, TRANS, 0);
+    });
+}
 
 // A lane's row of O^T (or of a gradient), times `by`: elements 32 b + 8 q + 4 (l / 32)
 // + 0..3 of row l % 32.
@@ -255,7 +284,7 @@ template <int DP> __global__ __launch_bounds__(256, 2) void attention_kernel(con
 {
     typedef Stage<DP> S;
     extern __shared__ __attribute__((aligned(16))) char lds[];
-    const uint32_t wave = uniform(threadIdx.x >> 6);
+    const uint32_t wave = uniform(threadIdx.x >> 6), h = threadIdx.x >> 5 & 1u;
     const uint32_t tiles = a.slots * a.kv_heads * a.splits;
     if (blockIdx.x >= tiles) {
         clear_rest(a.o, a.starts_q, a.sequences, a.tokens_q, a.heads, a.dim, blockIdx.x - tiles);
@@ -268,6 +297,7 @@ template <int DP> __global__ __launch_bounds__(256, 2) void attention_kernel(con
     const Place p = find_place(a, a.slots - 1 - rest / a.splits, false, a.group, kRows);
     if (!p.some) return;
     const Rows r = rows_of(a, p, p.tile * kRows + wave * 32, kv_head);
+    const bool idle = r.most == 0;
     const uint32_t last = (p.tile + 1) * kRows < p.lq * a.group ? (p.tile + 1) * kRows - 1 : p.lq * a.group - 1;
     const int64_t sees = a.causal ? (int64_t)(last / a.group) + 1 + p.lk - p.lq : (int64_t)p.lk;
     const uint32_t stages = sees > 0 ? ((uint32_t)sees + kKeys - 1) / kKeys : 0;
@@ -278,85 +308,114 @@ template <int DP> __global__ __launch_bounds__(256, 2) void attention_kernel(con
     ks.place(wave, a.k.ld, a.dim_in), vs.place(wave, a.v.ld, a.dim_in);
     Reads<DP> at;
     at.place(lds0);
-    auto load = [&](uint32_t t, uint32_t buf) {
-        const uint32_t key = t * kKeys;
-        ks.load(lds0 + buf * 2 * S::BYTES, wave, a.k.at(p.k0 + key, kv_head), p.lk - key);
-        vs.load(lds0 + buf * 2 * S::BYTES + S::BYTES, wave, a.v.at(p.k0 + key, kv_head), p.lk - key);
+    auto load_k = [&](uint32_t t, uint32_t buf) {
+        ks.load(lds0 + buf * 2 * S::BYTES, wave, a.k.at(p.k0 + t * kKeys, kv_head), p.lk - t * kKeys);
+    };
+    auto load_v = [&](uint32_t t, uint32_t buf) {
+        vs.load(lds0 + buf * 2 * S::BYTES + S::BYTES, wave, a.v.at(p.k0 + t * kKeys, kv_head), p.lk - t * kKeys);
     };
     bf16x8 q[DP / 16];
     load_row<DP>(a.q.at(p.q0 + r.query, r.head), a.dim_in, q);
-    f32x16 o[DP / 32];
+    f32x16 o[DP / 32], x{}, y;
 #pragma unroll
     for (int b = 0; b < DP / 32; ++b) o[b] = f32x16{};
+    float top = -INFINITY, part[4] = {0.0f, 0.0f, 0.0f, 0.0f};  // top: in units of S, times c once used
     const float c = a.scale * kLog2e;
-    float top = -INFINITY, sum = 0.0f;  // top: in units of S, times c once used
-    const uint32_t h = threadIdx.x >> 5 & 1u;
 
-    auto stage = [&](uint32_t t, auto buffer) {
-        constexpr int K = buffer.value * 2 * S::BYTES, V = K + S::BYTES;
-        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
-        __builtin_amdgcn_s_barrier();
-        asm volatile("" ::: "memory");
-        if (t + 1 < end) load(t + 1, 1 - buffer.value);
-        if (t * kKeys >= r.most) return;
-        f32x16 s[2];
+    // Blocks of 32 keys, in a pipeline: while the softmax of block n is computed, the
+    // matrix unit has P V of block n - 1 and Q K^T of block n + 1.  x: P of block n - 1,
+    // then S of block n + 1; y: S of block n, then P.  Half 0 and 1 of a stage: block n is
+    // the stage's first or second.
+    auto products_o = [&](const f32x16 &x, int V, int block) {
 #pragma unroll
-        for (int b = 0; b < 2; ++b) {
-            s[b] = f32x16{};
+        for (int k = 0; k < 2; ++k) {
+            const bf16x8 w = rounded(x, k * 8);
 #pragma unroll
-            for (int d = 0; d < DP / 16; ++d) s[b] = Frag<bf16>::mfma(at.rows(b, d, K), q[d], s[b]);
+            for (int d = 0; d < DP / 32; ++d) o[d] = Frag<bf16>::mfma(at.columns(d, block * 2 + k, V), w, o[d]);
         }
-        if (t * kKeys + kKeys > r.least) {
-            const uint32_t from = t * kKeys + 4 * h;
 #pragma unroll
-            for (int b = 0; b < 2; ++b)
+        for (int k = 0; k < 16; ++k) part[k & 3] += x[k];
+    };
+    auto products_s = [&](f32x16 &x, int K, int block) {
+        x = f32x16{};
 #pragma unroll
-                for (int k = 0; k < 16; ++k)
-                    if (from + b * 32 + 8 * (k / 4) + k % 4 >= r.limit) s[b][k] = -INFINITY;
+        for (int d = 0; d < DP / 16; ++d) x = Frag<bf16>::mfma(at.rows(block, d, K), q[d], x);
+    };
+    auto step = [&](uint32_t n, f32x16 &x, f32x16 &y, auto buffer, auto half) {
+        constexpr int HERE = buffer.value * 2 * S::BYTES, THERE = (1 - buffer.value) * 2 * S::BYTES;
+        constexpr int V = (half.value ? HERE : THERE) + S::BYTES, K = half.value ? THERE : HERE, B = 1 - half.value;
+        if (idle) return;
+        if (n * 32 + 32 > r.least) {
+            const int32_t left = (int32_t)(r.limit - n * 32 - 4 * h);
+#pragma unroll
+            for (int k = 0; k < 16; ++k) y[k] = 8 * (k / 4) + k % 4 < left ? y[k] : -INFINITY;
         }
-        float m = s[0][0];
+        __builtin_amdgcn_sched_barrier(0);
+        products_o(x, V, B);
+        float m = y[0];
 #pragma unroll
-        for (int k = 1; k < 16; ++k) m = fmaxf(m, s[0][k]);
-#pragma unroll
-        for (int k = 0; k < 16; ++k) m = fmaxf(m, s[1][k]);
-        m = fmaxf(m, other_half(m));
+        for (int k = 1; k < 16; ++k) m = __builtin_elementwise_maximum(m, y[k]);
+        const Halves both = halves(m);
+        m = __builtin_elementwise_maximum(both.a, both.b);
+        __builtin_amdgcn_sched_group_barrier(0x100, 8, 0);
+        interleave<DP / 16, 2, 5, 0>();
+        __builtin_amdgcn_sched_barrier(0);
         const bool rises = m * c > top * c + kSlack;
         if (__any(rises)) {
             // a row's bits do not depend on the others: a lane whose maximum stays goes on as it was
             const float next = rises ? m : top, to = next == -INFINITY ? 0.0f : next;
             const float by = __builtin_amdgcn_exp2f((top - to) * c);
             top = next;
-            sum *= by;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) part[k] *= by;
 #pragma unroll
             for (int b = 0; b < DP / 32; ++b)
 #pragma unroll
                 for (int k = 0; k < 16; ++k) o[b][k] *= by;
         }
         const float base = top == -INFINITY ? 0.0f : top * c;
-        float part[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+        __builtin_amdgcn_sched_barrier(0);
+        products_s(x, K, B);
 #pragma unroll
-        for (int b = 0; b < 2; ++b)
-#pragma unroll
-            for (int k = 0; k < 16; ++k) {
-                s[b][k] = __builtin_amdgcn_exp2f(s[b][k] * c - base);
-                part[k & 3] += s[b][k];
-            }
-        sum += (part[0] + part[1]) + (part[2] + part[3]);
-#pragma unroll
-        for (int b = 0; b < 2; ++b)
-#pragma unroll
-            for (int k = 0; k < 2; ++k) {
-                const bf16x8 w = rounded(s[b], k * 8);
-#pragma unroll
-                for (int d = 0; d < DP / 32; ++d) o[d] = Frag<bf16>::mfma(at.columns(d, b * 2 + k, V), w, o[d]);
-            }
+        for (int k = 0; k < 16; ++k) y[k] = __builtin_amdgcn_exp2f(y[k] * c - base);
+        __builtin_amdgcn_sched_group_barrier(0x100, 4, 0);
+        interleave<DP / 16, 1, 16 / (DP / 16), 16 / (DP / 16)>();
+        __builtin_amdgcn_sched_barrier(0);
     };
-    if (begin < end) load(begin, 0);
+    auto settled = [&]() {
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+    };
+    if (begin < end) {
+        // P of no block, times zeros
+        typedef float f32x4 __attribute__((ext_vector_type(4)));
+#pragma unroll
+        for (int i = 0; i < S::BYTES / 2 / 4096; ++i) *(f32x4 *)(lds + 3 * S::BYTES + S::BYTES / 2 + (i * 256 + threadIdx.x) * 16) = f32x4{};
+        load_k(begin, 0), load_v(begin, 0);
+        if (begin + 1 < end) load_k(begin + 1, 1);
+        settled();
+        products_s(y, 0, 0);
+    }
+    auto stage = [&](uint32_t t, auto buffer) {
+        constexpr int B = buffer.value;
+        step(2 * t, x, y, buffer, std::integral_constant<int, 0>{});
+        settled();
+        if (t + 2 < end) load_k(t + 2, B);
+        if (t + 1 < end) load_v(t + 1, 1 - B);
+        step(2 * t + 1, y, x, buffer, std::integral_constant<int, 1>{});
+    };
     for (uint32_t t = begin; t < end; t += 2) {
         stage(t, std::integral_constant<int, 0>{});
         if (t + 1 < end) stage(t + 1, std::integral_constant<int, 1>{});
     }
-    sum += other_half(sum);
+    if (begin < end && !idle) {
+        // the last block of the last stage
+        if ((end - begin) & 1u) products_o(x, S::BYTES, 1);
+        else products_o(x, 3 * S::BYTES, 1);
+    }
+    const Halves both = halves((part[0] + part[1]) + (part[2] + part[3]));
+    const float sum = both.a + both.b;
     if (!r.real) return;
     const float by = sum == 0.0f ? 0.0f : 1.0f / sum;
     const float lse = sum == 0.0f ? -INFINITY : top * a.scale + __logf(sum);

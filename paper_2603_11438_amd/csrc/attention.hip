@@ -649,35 +649,57 @@ template <int DP> __global__ __launch_bounds__(256, 1) void attention_dkv_kernel
         if (more) load(1 - buffer.value);
         if (here + kKeys > wave_from) {
             const float *st = stats + buffer.value * 2 * kKeys;
-            const bool masked = here < wave_needs;
+            // Each block of 32 queries in four parts, whose products have the matrix unit while
+            // the part's vector operations go on: S; dO V^T and P; dV and dS; dK.
 #pragma unroll
             for (int b = 0; b < 2; ++b) {
+                typedef float f32x4 __attribute__((ext_vector_type(4)));
                 f32x16 s{}, dp{};
+                __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
                 for (int d = 0; d < DP / 16; ++d) s = Frag<bf16>::mfma(at.rows(b, d, Q), kf[d], s);
+                f32x4 lse[4], delta[4];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    lse[k] = *(const f32x4 *)(st + b * 32 + 8 * k + 4 * h);
+                    delta[k] = *(const f32x4 *)(st + kKeys + b * 32 + 8 * k + 4 * h);
+                }
+                __builtin_amdgcn_sched_group_barrier(0x100, 4, 0);
+                interleave<DP / 16, 2, 0, 0>();
+                __builtin_amdgcn_sched_barrier(0);
+                if (here + b * 32 < wave_needs) {
+                    const int32_t hidden = need - (here + b * 32 + 4 * (int32_t)h);
+#pragma unroll
+                    for (int k = 0; k < 16; ++k) s[k] = 8 * (k / 4) + k % 4 >= hidden ? s[k] : -INFINITY;
+                }
+                __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
                 for (int d = 0; d < DP / 16; ++d) dp = Frag<bf16>::mfma(at.rows(b, d, G), vf[d], dp);
 #pragma unroll
-                for (int k4 = 0; k4 < 4; ++k4) {
-                    typedef float f32x4 __attribute__((ext_vector_type(4)));
-                    const f32x4 lse = *(const f32x4 *)(st + b * 32 + 8 * k4 + 4 * h), delta = *(const f32x4 *)(st + kKeys + b * 32 + 8 * k4 + 4 * h);
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) {
-                        const int n = k4 * 4 + k;
-                        s[n] = __builtin_amdgcn_exp2f(s[n] * c - lse[k]);
-                        dp[n] = s[n] * (dp[n] - delta[k]);
-                        if (masked && here + (int32_t)(b * 32 + 8 * k4 + 4 * h + k) < need) s[n] = 0.0f, dp[n] = 0.0f;
-                    }
-                }
+                for (int k = 0; k < 16; ++k) s[k] = __builtin_amdgcn_exp2f(s[k] * c - lse[k / 4][k % 4]);
+                __builtin_amdgcn_sched_group_barrier(0x100, 4, 0);
+                interleave<DP / 16, 1, 16 / (DP / 16), 16 / (DP / 16)>();
+                __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
                 for (int k = 0; k < 2; ++k) {
-                    const bf16x8 w = rounded(s, k * 8), u = rounded(dp, k * 8);
+                    const bf16x8 w = rounded(s, k * 8);
 #pragma unroll
-                    for (int d = 0; d < DP / 32; ++d) {
-                        dv[d] = Frag<bf16>::mfma(at.columns(d, b * 2 + k, G), w, dv[d]);
-                        dk[d] = Frag<bf16>::mfma(at.columns(d, b * 2 + k, Q), u, dk[d]);
-                    }
+                    for (int d = 0; d < DP / 32; ++d) dv[d] = Frag<bf16>::mfma(at.columns(d, b * 2 + k, G), w, dv[d]);
                 }
+#pragma unroll
+                for (int k = 0; k < 16; ++k) dp[k] = s[k] * (dp[k] - delta[k / 4][k % 4]);
+                const bf16x8 u[2] = {rounded(dp, 0), rounded(dp, 8)};
+                __builtin_amdgcn_sched_group_barrier(0x002, 4, 0);
+                __builtin_amdgcn_sched_group_barrier(0x100, 8, 0);
+                interleave<DP / 16, 2, DP == 128 ? 6 : 12, 0>();
+                __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                for (int k = 0; k < 2; ++k)
+#pragma unroll
+                    for (int d = 0; d < DP / 32; ++d) dk[d] = Frag<bf16>::mfma(at.columns(d, b * 2 + k, Q), u[k], dk[d]);
+                __builtin_amdgcn_sched_group_barrier(0x100, 8, 0);
+                interleave<DP / 16, 2, 0, 0>();
+                __builtin_amdgcn_sched_barrier(0);
             }
         }
         if (more) keep(1 - buffer.value);

@@ -115,9 +115,11 @@ template <int DP> struct Stage {
         return DP == 128 ? (r & 3u) << 2 | (r >> 2 & 3u) : (r >> 1 & 1u) << 2 | (r >> 2 & 3u);
     }
     uint32_t off[LOADS];
-    __device__ __forceinline__ void place(uint32_t wave, uint64_t ld, uint32_t dim)
+    uint64_t next, step;  // the next stage's first row; bytes from a stage to the one behind it
+    __device__ __forceinline__ void place(uint32_t wave, const void *first, uint64_t ld, uint32_t dim)
     {
         const uint32_t lane = threadIdx.x & 63u;
+        next = uniform_address(first), step = kKeys * ld * 2;
 #pragma unroll
         for (int i = 0; i < LOADS; ++i) {
             const uint32_t n = (i * 4 + wave) * 64 + lane, r = n / CHUNKS, c = (n % CHUNKS) ^ turn(r);
@@ -125,14 +127,20 @@ template <int DP> struct Stage {
         }
     }
     // rows from `left` on are zeros
-    __device__ __forceinline__ void load(uint32_t lds, uint32_t wave, const void *first, uint32_t left) const
+    __device__ __forceinline__ void load(uint32_t lds, uint32_t wave, uint32_t left)
     {
-        const uint32_t lane = threadIdx.x & 63u;
-        const u32x4v from = tile_resource(uniform_address(first));
+        const u32x4v from = tile_resource(next);
+        next += step;
+        if (left >= kKeys) {
 #pragma unroll
-        for (int i = 0; i < LOADS; ++i) {
-            const uint32_t r = ((i * 4 + wave) * 64 + lane) / CHUNKS;
-            load_to_lds(lds + (i * 4 + wave) * 1024, r < left ? off[i] : kOutOfRange, from, 0u);
+            for (int i = 0; i < LOADS; ++i) load_to_lds(lds + (i * 4 + wave) * 1024, off[i], from, 0u);
+        } else {
+            const uint32_t lane = threadIdx.x & 63u;
+#pragma unroll
+            for (int i = 0; i < LOADS; ++i) {
+                const uint32_t r = ((i * 4 + wave) * 64 + lane) / CHUNKS;
+                load_to_lds(lds + (i * 4 + wave) * 1024, r < left ? off[i] : kOutOfRange, from, 0u);
+            }
         }
     }
 };
@@ -305,15 +313,13 @@ template <int DP> __global__ __launch_bounds__(256, 2) void attention_kernel(con
 
     const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)lds;
     S ks, vs;
-    ks.place(wave, a.k.ld, a.dim_in), vs.place(wave, a.v.ld, a.dim_in);
+    ks.place(wave, a.k.at(p.k0 + begin * kKeys, kv_head), a.k.ld, a.dim_in);
+    vs.place(wave, a.v.at(p.k0 + begin * kKeys, kv_head), a.v.ld, a.dim_in);
     Reads<DP> at;
     at.place(lds0);
-    auto load_k = [&](uint32_t t, uint32_t buf) {
-        ks.load(lds0 + buf * 2 * S::BYTES, wave, a.k.at(p.k0 + t * kKeys, kv_head), p.lk - t * kKeys);
-    };
-    auto load_v = [&](uint32_t t, uint32_t buf) {
-        vs.load(lds0 + buf * 2 * S::BYTES + S::BYTES, wave, a.v.at(p.k0 + t * kKeys, kv_head), p.lk - t * kKeys);
-    };
+    // the stages of keys in turn
+    auto load_k = [&](uint32_t t, uint32_t buf) { ks.load(lds0 + buf * 2 * S::BYTES, wave, p.lk - t * kKeys); };
+    auto load_v = [&](uint32_t t, uint32_t buf) { vs.load(lds0 + buf * 2 * S::BYTES + S::BYTES, wave, p.lk - t * kKeys); };
     bf16x8 q[DP / 16];
     load_row<DP>(a.q.at(p.q0 + r.query, r.head), a.dim_in, q);
     f32x16 o[DP / 32], x{}, y;
@@ -509,13 +515,13 @@ template <int DP> __global__ __launch_bounds__(256, 2) void attention_dq_kernel(
 
     const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)lds;
     S ks, vs;
-    ks.place(wave, a.k.ld, a.dim_in), vs.place(wave, a.v.ld, a.dim_in);
+    ks.place(wave, a.k.at(p.k0 + begin * kKeys, kv_head), a.k.ld, a.dim_in);
+    vs.place(wave, a.v.at(p.k0 + begin * kKeys, kv_head), a.v.ld, a.dim_in);
     Reads<DP> at;
     at.place(lds0);
     auto load = [&](uint32_t t, uint32_t buf) {
-        const uint32_t key = t * kKeys;
-        ks.load(lds0 + buf * 2 * S::BYTES, wave, a.k.at(p.k0 + key, kv_head), p.lk - key);
-        vs.load(lds0 + buf * 2 * S::BYTES + S::BYTES, wave, a.v.at(p.k0 + key, kv_head), p.lk - key);
+        ks.load(lds0 + buf * 2 * S::BYTES, wave, p.lk - t * kKeys);
+        vs.load(lds0 + buf * 2 * S::BYTES + S::BYTES, wave, p.lk - t * kKeys);
     };
     bf16x8 q[DP / 16], g[DP / 16];
     load_row<DP>(a.q.at(p.q0 + r.query, r.head), a.dim_in, q);
@@ -601,31 +607,39 @@ template <int DP> __global__ __launch_bounds__(256, 1) void attention_dkv_kernel
     const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)lds;
     float *stats = (float *)(lds + 4 * S::BYTES);  // of a buffer's queries: lse, delta
     S qs, gs;
-    qs.place(wave, a.q.ld, a.dim_in), gs.place(wave, a.dout.ld, a.dim_in);
     Reads<DP> at;
     at.place(lds0);
     uint32_t next_head = per ? begin / per : 0, next_query = per ? first + begin % per * kKeys : 0;  // of the next load
+    // the statistics of a stage's queries: one value for each of the first threads
+    const bool is_delta = threadIdx.x >= kKeys;
+    const uint32_t mine_of = threadIdx.x & (kKeys - 1);
+    const float *stat = nullptr;
+    const uint64_t stat_step = (uint64_t)kKeys * a.heads;
+    auto enter = [&]() {
+        const uint64_t token = p.q0 + next_query;
+        const uint32_t head = kv_head * a.group + next_head;
+        qs.place(wave, a.q.at(token, head), a.q.ld, a.dim_in), gs.place(wave, a.dout.at(token, head), a.dout.ld, a.dim_in);
+        stat = (is_delta ? a.delta : a.lse) + (token + mine_of) * a.heads + head;
+    };
     float ahead = 0.0f;
     auto load = [&](uint32_t buf) {
-        const uint64_t token = p.q0 + next_query;
-        const uint32_t head = kv_head * a.group + next_head, left = p.lq - next_query;
+        const uint32_t left = p.lq - next_query;
         // what a row without keys kept is minus infinity; its P is 0, as it is behind the last row
         if (threadIdx.x < 2 * kKeys) {
-            const uint32_t i = threadIdx.x & (kKeys - 1);
-            const bool is_delta = threadIdx.x >= kKeys;
-            ahead = is_delta ? 0.0f : INFINITY;
-            if (i < left) {
-                ahead = (is_delta ? a.delta : a.lse)[(token + i) * a.heads + head];
-                if (!is_delta) ahead = ahead == -INFINITY ? INFINITY : ahead * kLog2e;
-            }
+            ahead = is_delta ? 0.0f : -INFINITY;
+            if (mine_of < left) ahead = *stat;
         }
-        qs.load(lds0 + buf * 2 * S::BYTES, wave, a.q.at(token, head), left);
-        gs.load(lds0 + buf * 2 * S::BYTES + S::BYTES, wave, a.dout.at(token, head), left);
-        next_query += kKeys;
-        if (next_query >= p.lq) next_query = first, ++next_head;
+        qs.load(lds0 + buf * 2 * S::BYTES, wave, left);
+        gs.load(lds0 + buf * 2 * S::BYTES + S::BYTES, wave, left);
+        stat += stat_step, next_query += kKeys;
+        if (next_query >= p.lq) {
+            next_query = first, ++next_head;
+            if (next_head < a.group) enter();
+        }
     };
     auto keep = [&](uint32_t buf) {
-        if (threadIdx.x < 2 * kKeys) stats[buf * 2 * kKeys + threadIdx.x] = ahead;
+        const float kept = is_delta ? ahead : ahead == -INFINITY ? INFINITY : ahead * kLog2e;
+        if (threadIdx.x < 2 * kKeys) stats[buf * 2 * kKeys + threadIdx.x] = kept;
     };
     bf16x8 kf[DP / 16], vf[DP / 16];
     const uint32_t key = mine < p.lk ? mine : p.lk - 1;
@@ -636,6 +650,7 @@ template <int DP> __global__ __launch_bounds__(256, 1) void attention_dkv_kernel
     for (int b = 0; b < DP / 32; ++b) dk[b] = f32x16{}, dv[b] = f32x16{};
     const float c = a.scale * kLog2e;
     uint32_t query = next_query;  // of this stage
+    if (begin < end) enter();
 
     auto stage = [&](uint32_t t, auto buffer) {
         constexpr int Q = buffer.value * 2 * S::BYTES, G = Q + S::BYTES;

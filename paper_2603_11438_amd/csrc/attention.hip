@@ -436,34 +436,35 @@ template <int DP> __global__ __launch_bounds__(256, 2) void attention_kernel(con
     }
 }
 
-// Joins the runs of keys of a split call: one wave for each row.
+// Joins the runs of keys of a split call: one wave for each row, lane s with the
+// statistics of run s, so that no load waits for another.
+constexpr uint32_t kMaxRuns = 64;
 __global__ __launch_bounds__(256) void attention_join_kernel(const AttnArgs a)
 {
-    const uint32_t lane = threadIdx.x & 63u;
+    const uint32_t lane = threadIdx.x & 63u, d = lane * 2;
     const uint64_t rows = (uint64_t)a.tokens_q * a.heads;
     const uint32_t from = start_of(a.starts_q, 0, a.tokens_q), until = start_of(a.starts_q, a.starts_q ? a.sequences : 1, a.tokens_q);
-    for (uint64_t i = (uint64_t)blockIdx.x * 4 + (threadIdx.x >> 6); i < rows; i += (uint64_t)gridDim.x * 4) {
+    for (uint64_t i = (uint64_t)blockIdx.x * 4 + uniform(threadIdx.x >> 6); i < rows; i += (uint64_t)gridDim.x * 4) {
         const uint32_t token = (uint32_t)(i / a.heads), head = (uint32_t)(i % a.heads);
         if (token < from || token >= until) continue;
-        float top = -INFINITY;
-        for (uint32_t s = 0; s < a.splits; ++s) {
-            const float l = a.part_lse[s * rows + i];
-            top = l > top || l != l ? l : top;  // NaN stays
-        }
-        const float base = top == -INFINITY ? 0.0f : top;
-        float sum = 0.0f, v[2] = {0.0f, 0.0f};
-        for (uint32_t s = 0; s < a.splits; ++s) {
-            const float w = __expf(a.part_lse[s * rows + i] - base);
-            sum += w;
-            const float *o = a.part + (s * rows + i) * a.dim;
+        const float lse = lane < a.splits ? a.part_lse[lane * rows + i] : -INFINITY;
+        float top = lse;
 #pragma unroll
-            for (int k = 0; k < 2; ++k)
-                if (lane + 64 * k < a.dim) v[k] += w * o[lane + 64 * k];
+        for (int m = 32; m; m >>= 1) top = __builtin_elementwise_maximum(top, __shfl_xor(top, m));  // NaN stays
+        const float base = top == -INFINITY ? 0.0f : top, w = __expf(lse - base), sum = wave_sum(w);
+        float v[2] = {0.0f, 0.0f};
+        const float *o = a.part + i * a.dim + d;
+#pragma unroll 8
+        for (uint32_t s = 0; s < a.splits; ++s) {
+            const float by = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, w), (int)s));
+            const float *from_run = o + s * rows * a.dim;
+            if (d < a.dim) v[0] += by * from_run[0];
+            if (d + 1 < a.dim) v[1] += by * from_run[1];
         }
         const float by = sum == 0.0f ? 0.0f : 1.0f / sum;
-#pragma unroll
-        for (int k = 0; k < 2; ++k)
-            if (lane + 64 * k < a.dim) a.o.at(token, head)[lane + 64 * k] = (bf16)(v[k] * by);
+        bf16 *to = a.o.at(token, head) + d;
+        if (d < a.dim) to[0] = (bf16)(v[0] * by);
+        if (d + 1 < a.dim) to[1] = (bf16)(v[1] * by);
         if (a.lse && lane == 0) a.lse[i] = sum == 0.0f ? -INFINITY : base + __logf(sum);
     }
 }
@@ -735,20 +736,41 @@ template <int DP> __global__ __launch_bounds__(256, 1) void attention_dkv_kernel
     }
 }
 
-// Adds the runs of a split gradient, in their order: [split][token][head][dim].
-__global__ __launch_bounds__(256) void attention_sum_kernel(const float *part, const Heads<bf16> out, const int32_t *starts,
-                                                            uint32_t sequences, uint32_t tokens, uint32_t heads, uint32_t dim, uint32_t splits)
+// Adds the runs of split gradients, in their order: [split][token][head][dim] of one,
+// then of the other.
+struct RunsOut {
+    Heads<bf16> to[2];
+    const float *part;
+    const int32_t *starts;
+    uint32_t sequences, tokens, heads, dim, splits;
+};
+__global__ __launch_bounds__(256) void attention_sum_kernel(const RunsOut o)
 {
-    const uint32_t from = start_of(starts, 0, tokens), until = start_of(starts, starts ? sequences : 1, tokens);
-    const uint64_t rows = (uint64_t)tokens * heads, n = rows * dim;
-    for (uint64_t i = (uint64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (uint64_t)gridDim.x * 256) {
-        const uint64_t row = i / dim;
-        const uint32_t token = (uint32_t)(row / heads), d = (uint32_t)(i % dim);
+    const uint32_t from = start_of(o.starts, 0, o.tokens), until = start_of(o.starts, o.starts ? o.sequences : 1, o.tokens);
+    const uint32_t per = (o.dim + 3) / 4;
+    const uint64_t rows = (uint64_t)o.tokens * o.heads, n = rows * o.dim;
+    const float *part = o.part + blockIdx.y * o.splits * n;
+    for (uint64_t i = (uint64_t)blockIdx.x * 256 + threadIdx.x; i < rows * per; i += (uint64_t)gridDim.x * 256) {
+        const uint64_t row = i / per;
+        const uint32_t token = (uint32_t)(row / o.heads), d = (uint32_t)(i % per) * 4;
         if (token < from || token >= until) continue;
-        float v = part[i];
-#pragma unroll 4
-        for (uint32_t s = 1; s < splits; ++s) v += part[s * n + i];
-        out.at(token, row % heads)[d] = (bf16)v;
+        bf16 *to = o.to[blockIdx.y].at(token, row % o.heads) + d;
+        const float *at = part + row * o.dim + d;
+        float v[4] = {0.0f, 0.0f, 0.0f, 0.0f}, w[4];
+        if (d + 4 <= o.dim) {
+#pragma unroll 8
+            for (uint32_t s = 0; s < o.splits; ++s) {
+                load_vec<float, 4>(at + s * n, w);
+#pragma unroll
+                for (int k = 0; k < 4; ++k) v[k] += w[k];
+            }
+            store_vec<bf16, 4>(to, v);
+        } else {
+            for (uint32_t k = 0; k < o.dim - d; ++k) {
+                for (uint32_t s = 0; s < o.splits; ++s) v[0] += at[s * n + k];
+                to[k] = (bf16)v[0], v[0] = 0.0f;
+            }
+        }
     }
 }
 
@@ -852,27 +874,40 @@ AttnTensors attn_tensors(const ar_attention_desc &d, const void *q, const void *
 size_t row_slots(const ar_attention_desc &d) { return d.tokens_q * (d.heads / d.kv_heads) / kRows + d.sequences; }
 size_t key_slots(const ar_attention_desc &d) { return d.tokens_k / kRows + d.sequences; }
 
-// Runs that each tile's `stages` are split into so that `units` workgroups have work:
-// none shorter than `least` in the mean.
-uint32_t splits_for(size_t tiles, size_t stages, size_t units, size_t least)
+// How many runs the stages of each tile are split into: what makes the time of the
+// longest tile, whose stages follow one another, and of the join least.  `stages`: of a
+// tile, in the mean, half as many again where there are several sequences, some of them
+// longer; us: of a stage, alone; bytes: of a run's sums.  A join takes 5 us, 0.2 for each
+// run and the sums' way to memory and back at 3.4 TB/s.  No more than `most` workgroups in
+// all: from there on the device is full and the sums are for nothing.  By sweeps of 1 to
+// 64 runs over fourteen sizes, each in one piece, with the best, as chosen: forward, 32
+// heads over 8 of 128, 1 query of 16000 keys 300, 34, 36 us, 32 of 7600 408, 203, 206;
+// dk and dv of 2048 queries, 16 heads over 2, 485, 74, 76 us.
+uint32_t runs_for(size_t tiles, double stages, double us, double bytes, size_t most, const ar_attention_desc &d)
 {
-    if (tiles >= units || !tiles) return 1;
-    size_t s = (units + tiles - 1) / tiles, most = stages / least;
-    s = s < most ? s : most;
-    return (uint32_t)(s < 1 ? 1 : s < 64 ? s : 64);
+    if (d.sequences > 1) stages *= 1.5;
+    uint32_t best = 1;
+    double time = stages * us;
+    for (uint32_t s = 2; s <= kMaxRuns && s <= stages && s * tiles <= most; ++s) {
+        const double t = stages / s * us + 5.0 + s * (0.2 + 2.0 * bytes / 3.4e6);
+        if (t < time) best = s, time = t;
+    }
+    return best;
 }
-size_t mean(size_t tokens, const ar_attention_desc &d) { return (tokens + d.sequences - 1) / d.sequences; }
+double mean_stages(size_t tokens, const ar_attention_desc &d) { return ceil((double)tokens / d.sequences / kKeys); }
+double sums_bytes(size_t rows, const ar_attention_desc &d) { return 4.0 * rows * d.dim; }
 uint32_t forward_splits(const ar_attention_desc &d)
 {
-    return splits_for(row_slots(d) * d.kv_heads, (mean(d.tokens_k, d) + kKeys - 1) / kKeys, 1024, 2);
+    return runs_for(row_slots(d) * d.kv_heads, mean_stages(d.tokens_k, d), d.dim <= 64 ? 0.9 : 1.2, sums_bytes(d.tokens_q * d.heads, d), 2048, d);
 }
 uint32_t dq_splits(const ar_attention_desc &d)
 {
-    return splits_for(row_slots(d) * d.kv_heads, (mean(d.tokens_k, d) + kKeys - 1) / kKeys, 512, 4);
+    return runs_for(row_slots(d) * d.kv_heads, mean_stages(d.tokens_k, d), d.dim <= 64 ? 1.3 : 1.8, sums_bytes(d.tokens_q * d.heads, d), 1024, d);
 }
 uint32_t dkv_splits(const ar_attention_desc &d)
 {
-    return splits_for(key_slots(d) * d.kv_heads, (mean(d.tokens_q, d) + kKeys - 1) / kKeys * (d.heads / d.kv_heads), 256, 4);
+    return runs_for(key_slots(d) * d.kv_heads, mean_stages(d.tokens_q, d) * (d.heads / d.kv_heads), d.dim <= 64 ? 1.2 : 1.9,
+                    2 * sums_bytes(d.tokens_k * d.kv_heads, d), 512, d);
 }
 
 size_t part_bytes(uint32_t splits, size_t rows, size_t each) { return splits > 1 ? round_up(splits * rows * each * sizeof(float), 256) : 0; }
@@ -1025,10 +1060,9 @@ size_t backward_bytes(const ar_attention_desc &d)
     return backward_space(d, true, true).copies + 2 * t.q.copy_bytes() + t.k.copy_bytes() + t.v.copy_bytes();
 }
 
-int sum_runs(const float *part, const Heads<bf16> &out, const int32_t *starts, const AttnArgs &a, uint32_t tokens, uint32_t heads, hipStream_t st)
+int sum_runs(const RunsOut &o, uint32_t results, hipStream_t st)
 {
-    hipLaunchKernelGGL(attention_sum_kernel, dim3(groups_for((uint64_t)tokens * heads * a.dim)), dim3(256), 0, st, part, out, starts,
-                       a.sequences, tokens, heads, a.dim, a.splits);
+    hipLaunchKernelGGL(attention_sum_kernel, dim3(groups_for((uint64_t)o.tokens * o.heads * ((o.dim + 3) / 4)), results), dim3(256), 0, st, o);
     return launch_status();
 }
 
@@ -1084,16 +1118,16 @@ int attention_backward(const ar_attention_desc *desc, const void *dout, const vo
         a.slots = (uint32_t)key_slots(d), a.splits = dkv_splits(d);
         if ((rc = d.dim <= 64 ? launch_dkv<64>(a, st) : launch_dkv<128>(a, st)) != AR_OK) return rc;
         if (a.splits > 1) {
-            if ((rc = sum_runs(a.part, a.dk, starts_k, a, a.tokens_k, a.kv_heads, st)) != AR_OK) return rc;
-            const uint64_t half = (uint64_t)a.splits * d.tokens_k * d.kv_heads * d.dim;
-            if ((rc = sum_runs(a.part + half, a.dv, starts_k, a, a.tokens_k, a.kv_heads, st)) != AR_OK) return rc;
+            const RunsOut o{{a.dk, a.dv}, a.part, starts_k, a.sequences, a.tokens_k, a.kv_heads, a.dim, a.splits};
+            if ((rc = sum_runs(o, 2, st)) != AR_OK) return rc;
         }
     }
     if (dq && d.tokens_q) {
         a.dq = heads_of<bf16>(out[0]);
         a.slots = (uint32_t)row_slots(d), a.splits = dq_splits(d);
         if ((rc = d.dim <= 64 ? launch_dq<64>(a, st) : launch_dq<128>(a, st)) != AR_OK) return rc;
-        if (a.splits > 1 && (rc = sum_runs(a.part, a.dq, starts_q, a, a.tokens_q, a.heads, st)) != AR_OK) return rc;
+        const RunsOut o{{a.dq, a.dq}, a.part, starts_q, a.sequences, a.tokens_q, a.heads, a.dim, a.splits};
+        if (a.splits > 1 && (rc = sum_runs(o, 1, st)) != AR_OK) return rc;
     }
     return AR_OK;
 }

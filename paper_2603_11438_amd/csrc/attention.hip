@@ -666,22 +666,41 @@ template <int DP> __global__ __launch_bounds__(256, 1) void attention_dkv_kernel
         if (here + kKeys > wave_from) {
             const float *st = stats + buffer.value * 2 * kKeys;
             // Each block of 32 queries in four parts, whose products have the matrix unit while
-            // the part's vector operations go on: S; dO V^T and P; dV and dS; dK.
+            // the part's vector operations go on: S; dO V^T and P; dV and dS; dK.  The first
+            // fragments of each part are read in the one before.
+            constexpr int N = DP / 16;  // products of a part
+            bf16x8 first_rows[4], first_columns[4];
+            auto row_of = [&](int b, int d, int at_stage) { return d < 4 ? first_rows[d] : at.rows(b, d, at_stage); };
+            auto columns_of = [&](int b, int n, int at_stage) {
+                return n < 4 ? first_columns[n] : at.columns(n % (DP / 32), b * 2 + n / (DP / 32), at_stage);
+            };
+            auto read_rows = [&](int b, int at_stage) {
+#pragma unroll
+                for (int d = 0; d < 4; ++d) first_rows[d] = at.rows(b, d, at_stage);
+            };
+            auto read_columns = [&](int b, int at_stage) {
+#pragma unroll
+                for (int n = 0; n < 4; ++n) first_columns[n] = at.columns(n % (DP / 32), b * 2 + n / (DP / 32), at_stage);
+            };
+            read_rows(0, Q);
 #pragma unroll
             for (int b = 0; b < 2; ++b) {
                 typedef float f32x4 __attribute__((ext_vector_type(4)));
                 f32x16 s{}, dp{};
+                bf16x8 f[N];
                 __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-                for (int d = 0; d < DP / 16; ++d) s = Frag<bf16>::mfma(at.rows(b, d, Q), kf[d], s);
+                for (int d = 0; d < N; ++d) f[d] = row_of(b, d, Q);
+                read_rows(b, G);
+#pragma unroll
+                for (int d = 0; d < N; ++d) s = Frag<bf16>::mfma(f[d], kf[d], s);
                 f32x4 lse[4], delta[4];
 #pragma unroll
                 for (int k = 0; k < 4; ++k) {
                     lse[k] = *(const f32x4 *)(st + b * 32 + 8 * k + 4 * h);
                     delta[k] = *(const f32x4 *)(st + kKeys + b * 32 + 8 * k + 4 * h);
                 }
-                __builtin_amdgcn_sched_group_barrier(0x100, 4, 0);
-                interleave<DP / 16, 2, 0, 0>();
+                interleave<N, 2, 0, 0>();
                 __builtin_amdgcn_sched_barrier(0);
                 if (here + b * 32 < wave_needs) {
                     const int32_t hidden = need - (here + b * 32 + 4 * (int32_t)h);
@@ -690,31 +709,32 @@ template <int DP> __global__ __launch_bounds__(256, 1) void attention_dkv_kernel
                 }
                 __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-                for (int d = 0; d < DP / 16; ++d) dp = Frag<bf16>::mfma(at.rows(b, d, G), vf[d], dp);
+                for (int d = 0; d < N; ++d) f[d] = row_of(b, d, G);
+                read_columns(b, G);
+#pragma unroll
+                for (int d = 0; d < N; ++d) dp = Frag<bf16>::mfma(f[d], vf[d], dp);
 #pragma unroll
                 for (int k = 0; k < 16; ++k) s[k] = __builtin_amdgcn_exp2f(s[k] * c - lse[k / 4][k % 4]);
-                __builtin_amdgcn_sched_group_barrier(0x100, 4, 0);
-                interleave<DP / 16, 1, 16 / (DP / 16), 16 / (DP / 16)>();
+                interleave<N, 2, 16 / N, 16 / N>();
                 __builtin_amdgcn_sched_barrier(0);
+                const bf16x8 w[2] = {rounded(s, 0), rounded(s, 8)};
 #pragma unroll
-                for (int k = 0; k < 2; ++k) {
-                    const bf16x8 w = rounded(s, k * 8);
+                for (int n = 0; n < N; ++n) f[n] = columns_of(b, n, G);
+                read_columns(b, Q);
 #pragma unroll
-                    for (int d = 0; d < DP / 32; ++d) dv[d] = Frag<bf16>::mfma(at.columns(d, b * 2 + k, G), w, dv[d]);
-                }
+                for (int n = 0; n < N; ++n) dv[n % (DP / 32)] = Frag<bf16>::mfma(f[n], w[n / (DP / 32)], dv[n % (DP / 32)]);
 #pragma unroll
                 for (int k = 0; k < 16; ++k) dp[k] = s[k] * (dp[k] - delta[k / 4][k % 4]);
                 const bf16x8 u[2] = {rounded(dp, 0), rounded(dp, 8)};
                 __builtin_amdgcn_sched_group_barrier(0x002, 4, 0);
-                __builtin_amdgcn_sched_group_barrier(0x100, 8, 0);
-                interleave<DP / 16, 2, DP == 128 ? 6 : 12, 0>();
+                interleave<N, 2, DP == 128 ? 6 : 12, 0>();
                 __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-                for (int k = 0; k < 2; ++k)
+                for (int n = 0; n < N; ++n) f[n] = columns_of(b, n, Q);
+                if (b == 0) read_rows(1, Q);
 #pragma unroll
-                    for (int d = 0; d < DP / 32; ++d) dk[d] = Frag<bf16>::mfma(at.columns(d, b * 2 + k, Q), u[k], dk[d]);
-                __builtin_amdgcn_sched_group_barrier(0x100, 8, 0);
-                interleave<DP / 16, 2, 0, 0>();
+                for (int n = 0; n < N; ++n) dk[n % (DP / 32)] = Frag<bf16>::mfma(f[n], u[n / (DP / 32)], dk[n % (DP / 32)]);
+                interleave<N, 2, 0, 0>();
                 __builtin_amdgcn_sched_barrier(0);
             }
         }

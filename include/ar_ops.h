@@ -225,8 +225,8 @@ typedef struct ar_attention_desc {
     size_t ld_dout, hs_dout, ld_dq, hs_dq, ld_dk, hs_dk, ld_dv, hs_dv;  /* backward only */
 } ar_attention_desc;
 
-/* Forward.  lse: NULL, or tokens_q * heads floats, by tokens, that the backward pass
- * needs.  e^(z - m) is rounded to bf16 as an operand of the product with v (m: within
+/* Forward.  lse: NULL, or heads * tokens_q floats, a head's tokens after one another,
+ * that the backward pass needs.  e^(z - m) is rounded to bf16 as an operand of the product with v (m: within
  * e^5.6 of the row's maximum); its sum is not.  Tensors that cannot be read where
  * they lie, not 16-byte aligned or with a dim or stride that is no multiple of 8, are
  * first copied into the workspace.  Where there are few rows the keys are taken in

@@ -26,6 +26,11 @@ HIPCC_FLAGS = [
     "-Wno-unused-but-set-variable",
 ]
 
+# attention.hip: results of matrix instructions that vector instructions read stay in
+# vector registers; by itself the compiler has all of a kernel that needs more than 256
+# registers in accumulation registers, and copies.
+SOURCE_FLAGS = {"attention.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"]}
+
 
 def hipcc() -> str:
     for cand in (os.environ.get("HIPCC"), "/opt/rocm/bin/hipcc", shutil.which("hipcc")):
@@ -45,7 +50,7 @@ def build(verbose: bool = False) -> str:
         jobs = []
         for s in SOURCES:
             obj = os.path.join(objdir, s + ".o")
-            cmd = [hipcc(), *HIPCC_FLAGS, "-c", "-I", INCLUDE, "-I", CSRC, os.path.join(CSRC, s), "-o", obj]
+            cmd = [hipcc(), *HIPCC_FLAGS, *SOURCE_FLAGS.get(s, []), "-c", "-I", INCLUDE, "-I", CSRC, os.path.join(CSRC, s), "-o", obj]
             jobs.append((obj, subprocess.Popen(cmd, cwd=PKG, stdout=subprocess.PIPE, stderr=subprocess.STDOUT,
                                                text=True)))
         done = [(obj, job.communicate()[0], job.returncode) for obj, job in jobs]

@@ -36,8 +36,8 @@ struct AttnArgs {
     Heads<const bf16> q, k, v, dout;
     Heads<bf16> o, dq, dk, dv;
     const int32_t *starts_q, *starts_k;  // null: one sequence
-    float *lse;                          // [token][head]; null: not kept
-    const float *delta;                  // [token][head]
+    float *lse;                          // [head][token]; null: not kept
+    const float *delta;                  // [head][token]
     float *part, *part_lse;              // with keys split: [split][token][head][dim], [split][token][head]
     uint32_t sequences, tokens_q, tokens_k, heads, kv_heads, group;
     uint32_t dim, dim_in;  // dim_in: a multiple of eight, up to which the inputs can be read
@@ -218,6 +218,10 @@ __device__ __forceinline__ Halves halves(float v)
     return {__builtin_bit_cast(float, (uint32_t)r[0]), __builtin_bit_cast(float, (uint32_t)r[1])};
 }
 
+// Keeps the operations that make a value before the ones written behind this: the
+// compiler's barriers hold no operations that touch no memory.
+template <typename T> __device__ __forceinline__ void here_now(T &v) { asm volatile("" : "+v"(v)); }
+
 // One product, then so many reads of LDS for a later one and vector and transcendental
 // operations of what is independent of it, N times over: the matrix unit takes 32 cycles
 // for a product.
@@ -296,7 +300,7 @@ template <int DP> __global__ __launch_bounds__(256, 2) void attention_kernel(con
     const uint32_t tiles = a.slots * a.kv_heads * a.splits;
     if (blockIdx.x >= tiles) {
         clear_rest(a.o, a.starts_q, a.sequences, a.tokens_q, a.heads, a.dim, blockIdx.x - tiles);
-        if (a.lse) clear_rest(Heads<float>{a.lse, a.heads, 1}, a.starts_q, a.sequences, a.tokens_q, a.heads, 1, blockIdx.x - tiles);
+        if (a.lse) clear_rest(Heads<float>{a.lse, 1, a.tokens_q}, a.starts_q, a.sequences, a.tokens_q, a.heads, 1, blockIdx.x - tiles);
         return;
     }
     // a key head's workgroups on one XCD where the heads come to eight; the last
@@ -432,7 +436,7 @@ template <int DP> __global__ __launch_bounds__(256, 2) void attention_kernel(con
         if (h == 0) a.part_lse[at_row] = lse;
     } else {
         store_row<DP>(a.o.at(token, r.head), a.dim, o, by);
-        if (a.lse && h == 0) a.lse[token * a.heads + r.head] = lse;
+        if (a.lse && h == 0) a.lse[(uint64_t)r.head * a.tokens_q + token] = lse;
     }
 }
 
@@ -465,22 +469,22 @@ __global__ __launch_bounds__(256) void attention_join_kernel(const AttnArgs a)
         bf16 *to = a.o.at(token, head) + d;
         if (d < a.dim) to[0] = (bf16)(v[0] * by);
         if (d + 1 < a.dim) to[1] = (bf16)(v[1] * by);
-        if (a.lse && lane == 0) a.lse[i] = sum == 0.0f ? -INFINITY : base + __logf(sum);
+        if (a.lse && lane == 0) a.lse[(uint64_t)head * a.tokens_q + token] = sum == 0.0f ? -INFINITY : base + __logf(sum);
     }
 }
 
 // ---- backward -----------------------------------------------------------------
 
-// delta = the sum over a row of dout * o: sixteen lanes a row.
+// delta = the sum over a row of dout * o: sixteen lanes a row, a head's rows in turn.
 __global__ __launch_bounds__(256) void attention_delta_kernel(const Heads<const bf16> dout, const Heads<const bf16> o, float *delta,
-                                                              uint64_t rows, uint32_t heads, uint32_t dim)
+                                                              uint64_t rows, uint32_t tokens, uint32_t dim)
 {
     const uint32_t d = (threadIdx.x & 15u) * 8;
     for (uint64_t i0 = (uint64_t)blockIdx.x * 16; i0 < rows; i0 += (uint64_t)gridDim.x * 16) {
         const uint64_t i = i0 + (threadIdx.x >> 4);
         float sum = 0.0f;
         if (i < rows && d < dim) {
-            const bf16 *a = dout.at(i / heads, i % heads) + d, *b = o.at(i / heads, i % heads) + d;
+            const bf16 *a = dout.at(i % tokens, i / tokens) + d, *b = o.at(i % tokens, i / tokens) + d;
             float x[8], y[8];
             if (d + 8 <= dim) load_vec<bf16, 8>(a, x), load_vec<bf16, 8>(b, y);
             else load_part<bf16, 8>(a, (int)(dim - d), x), load_part<bf16, 8>(b, (int)(dim - d), y);
@@ -528,7 +532,8 @@ template <int DP> __global__ __launch_bounds__(256, 2) void attention_dq_kernel(
     load_row<DP>(a.q.at(p.q0 + r.query, r.head), a.dim_in, q);
     load_row<DP>(a.dout.at(p.q0 + r.query, r.head), a.dim_in, g);
     const uint64_t token = p.q0 + r.query;
-    const float lse = a.lse[token * a.heads + r.head] * kLog2e, delta = a.delta[token * a.heads + r.head], c = a.scale * kLog2e;
+    const uint64_t stat = (uint64_t)r.head * a.tokens_q + token;
+    const float lse = a.lse[stat] * kLog2e, delta = a.delta[stat], c = a.scale * kLog2e;
     f32x16 dq[DP / 32];
 #pragma unroll
     for (int b = 0; b < DP / 32; ++b) dq[b] = f32x16{};
@@ -615,12 +620,11 @@ template <int DP> __global__ __launch_bounds__(256, 1) void attention_dkv_kernel
     const bool is_delta = threadIdx.x >= kKeys;
     const uint32_t mine_of = threadIdx.x & (kKeys - 1);
     const float *stat = nullptr;
-    const uint64_t stat_step = (uint64_t)kKeys * a.heads;
     auto enter = [&]() {
         const uint64_t token = p.q0 + next_query;
         const uint32_t head = kv_head * a.group + next_head;
         qs.place(wave, a.q.at(token, head), a.q.ld, a.dim_in), gs.place(wave, a.dout.at(token, head), a.dout.ld, a.dim_in);
-        stat = (is_delta ? a.delta : a.lse) + (token + mine_of) * a.heads + head;
+        stat = (is_delta ? a.delta : a.lse) + (uint64_t)head * a.tokens_q + token + mine_of;
     };
     float ahead = 0.0f;
     auto load = [&](uint32_t buf) {
@@ -632,7 +636,7 @@ template <int DP> __global__ __launch_bounds__(256, 1) void attention_dkv_kernel
         }
         qs.load(lds0 + buf * 2 * S::BYTES, wave, left);
         gs.load(lds0 + buf * 2 * S::BYTES + S::BYTES, wave, left);
-        stat += stat_step, next_query += kKeys;
+        stat += kKeys, next_query += kKeys;
         if (next_query >= p.lq) {
             next_query = first, ++next_head;
             if (next_head < a.group) enter();
@@ -701,6 +705,7 @@ template <int DP> __global__ __launch_bounds__(256, 1) void attention_dkv_kernel
                     delta[k] = *(const f32x4 *)(st + kKeys + b * 32 + 8 * k + 4 * h);
                 }
                 interleave<N, 2, 0, 0>();
+                here_now(s);
                 __builtin_amdgcn_sched_barrier(0);
                 if (here + b * 32 < wave_needs) {
                     const int32_t hidden = need - (here + b * 32 + 4 * (int32_t)h);
@@ -711,23 +716,32 @@ template <int DP> __global__ __launch_bounds__(256, 1) void attention_dkv_kernel
 #pragma unroll
                 for (int d = 0; d < N; ++d) f[d] = row_of(b, d, G);
                 read_columns(b, G);
+                here_now(s);
 #pragma unroll
-                for (int d = 0; d < N; ++d) dp = Frag<bf16>::mfma(f[d], vf[d], dp);
+                for (int d = 0; d < N; ++d) {
+                    dp = Frag<bf16>::mfma(f[d], vf[d], dp);
+                    here_now(dp);
 #pragma unroll
-                for (int k = 0; k < 16; ++k) s[k] = __builtin_amdgcn_exp2f(s[k] * c - lse[k / 4][k % 4]);
-                interleave<N, 2, 16 / N, 16 / N>();
+                    for (int k = 0; k < 16 / N; ++k) {
+                        const int n = d * (16 / N) + k;
+                        s[n] = __builtin_amdgcn_exp2f(s[n] * c - lse[n / 4][n % 4]);
+                    }
+                    here_now(s);
+                }
                 __builtin_amdgcn_sched_barrier(0);
                 const bf16x8 w[2] = {rounded(s, 0), rounded(s, 8)};
 #pragma unroll
                 for (int n = 0; n < N; ++n) f[n] = columns_of(b, n, G);
                 read_columns(b, Q);
 #pragma unroll
-                for (int n = 0; n < N; ++n) dv[n % (DP / 32)] = Frag<bf16>::mfma(f[n], w[n / (DP / 32)], dv[n % (DP / 32)]);
+                for (int n = 0; n < N; ++n) {
+                    dv[n % (DP / 32)] = Frag<bf16>::mfma(f[n], w[n / (DP / 32)], dv[n % (DP / 32)]);
+                    here_now(dv[n % (DP / 32)]);
 #pragma unroll
-                for (int k = 0; k < 16; ++k) dp[k] = s[k] * (dp[k] - delta[k / 4][k % 4]);
+                    for (int k = n * (16 / N); k < (n + 1) * (16 / N); ++k) dp[k] = s[k] * (dp[k] - delta[k / 4][k % 4]);
+                    here_now(dp);
+                }
                 const bf16x8 u[2] = {rounded(dp, 0), rounded(dp, 8)};
-                __builtin_amdgcn_sched_group_barrier(0x002, 4, 0);
-                interleave<N, 2, DP == 128 ? 6 : 12, 0>();
                 __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
                 for (int n = 0; n < N; ++n) f[n] = columns_of(b, n, Q);
@@ -1130,7 +1144,7 @@ int attention_backward(const ar_attention_desc *desc, const void *dout, const vo
     if (d.tokens_q) {
         const uint64_t rows = (uint64_t)d.tokens_q * d.heads;
         hipLaunchKernelGGL(attention_delta_kernel, dim3(groups_for(rows * 16)), dim3(256), 0, st, heads_of<const bf16>(g),
-                           heads_of<const bf16>(t.o), (float *)ws, rows, a.heads, a.dim);
+                           heads_of<const bf16>(t.o), (float *)ws, rows, a.tokens_q, a.dim);
         if ((rc = launch_status()) != AR_OK) return rc;
     }
     if (dk && d.tokens_k) {

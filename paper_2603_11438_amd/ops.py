@@ -640,7 +640,7 @@ def packed_attention(q, k, v, *, starts_q=None, starts_k=None, causal: bool = Tr
     sequence.  causal: a sequence's last query sees all its keys, each one before it one
     less; a query that sees none has o = 0.  scale: 1 / sqrt(dim) unless given; above 0.
     out: o to write to; tokens of no sequence are then left as they were, and are zeros
-    otherwise.  lse: (queries, heads) fp32."""
+    otherwise.  lse: (heads, queries) fp32."""
     import torch
 
     _tell_of_graphs(q, k, v)
@@ -648,7 +648,7 @@ def packed_attention(q, k, v, *, starts_q=None, starts_k=None, causal: bool = Tr
         d, sq, sk = _attention_desc(q, k, v, starts_q, starts_k, causal, scale, on.index, out is None)
         o = torch.empty(q.shape, dtype=q.dtype, device=q.device) if out is None else out
         _, _, _, d.ld_o, d.hs_o = _heads(o, "out", on.index, tuple(q.shape), q.dtype)
-        lse = torch.empty(q.shape[:2], dtype=torch.float32, device=q.device) if save else None
+        lse = torch.empty(q.shape[1], q.shape[0], dtype=torch.float32, device=q.device) if save else None
         L = _lib()
         need = L.ar_attention_workspace_for(ctypes.byref(d), q.data_ptr(), k.data_ptr(), v.data_ptr())
         ws = _workspace(need, q)
@@ -677,7 +677,7 @@ def packed_attention_backward(do, q, k, v, o, lse, *, starts_q=None, starts_k=No
         d, sq, sk = _attention_desc(q, k, v, starts_q, starts_k, causal, scale, dev, out is None)
         _, _, _, d.ld_dout, d.hs_dout = _heads(do, "do", dev, tuple(q.shape), q.dtype)
         _, _, _, d.ld_o, d.hs_o = _heads(o, "o", dev, tuple(q.shape), q.dtype)
-        if not lse.is_cuda or lse.device.index != dev or lse.dtype != torch.float32 or not lse.is_contiguous() or lse.shape != q.shape[:2]:
+        if not lse.is_cuda or lse.device.index != dev or lse.dtype != torch.float32 or not lse.is_contiguous() or tuple(lse.shape) != (d.heads, d.tokens_q):
             raise ValueError("lse must be what packed_attention(save=True) returned for these tensors")
         dq, dk, dv = (None, None, None) if out is None else out
         new = lambda like: torch.empty(like.shape, dtype=like.dtype, device=like.device)  # noqa: E731

@@ -41,7 +41,7 @@ def check_all(q, k, v, do, sq, sk, causal=True, scale=None):
     kw = dict(starts_q=on_gpu(sq), starts_k=on_gpu(sk), causal=causal, scale=scale)
     o, lse = ar.packed_attention(q, k, v, save=True, **kw)
     check(o, *want["o"], "o")
-    check(lse, *want["lse"], "lse")
+    check(lse.t(), *want["lse"], "lse")
     for name, g in zip(("dq", "dk", "dv"), ar.packed_attention_backward(do, q, k, v, o, lse, **kw)):
         check(g, *want[name], name)
 
@@ -162,8 +162,8 @@ def test_tokens_of_no_sequence(lens):
     grads = ar.packed_attention_backward(do, q, k, v, o, lse, **kw)
     want = oo.attention(q[inside], k[inside], v[inside], starts(lens), starts(lens), do=do[inside])
     check(o[inside], *want["o"], "o")
-    check(lse[inside], *want["lse"], "lse")
-    assert not lse[:before].any() and not lse[sq[-1]:].any()
+    check(lse[:, inside].t(), *want["lse"], "lse")
+    assert not lse[:, :before].any() and not lse[:, sq[-1]:].any()
     for t, name in zip((o, *grads), ("o", "dq", "dk", "dv")):
         check(t[inside], *want[name], name)
         assert not t[:before].any() and not t[sq[-1]:].any(), name
@@ -188,7 +188,7 @@ def test_keys_behind_a_sequences_end_do_not_reach_it():
         t[60:70] = math.inf
     o2, lse2 = ar.packed_attention(q, k, v, save=True, **kw)
     grads2 = ar.packed_attention_backward(do, q, k, v, o2, lse2, **kw)
-    for a, b in zip((o, lse, *grads), (o2, lse2, *grads2)):
+    for a, b in zip((o, lse.t(), *grads), (o2, lse2.t(), *grads2)):
         assert torch.equal(a[:50], b[:50]) and torch.equal(a[110:], b[110:])
 
 
@@ -320,7 +320,7 @@ def test_refusals():
         (ar.ARError, lambda: ar.packed_attention(q, k, v, scale=0.0)), (ar.ARError, lambda: ar.packed_attention(q, k, v, scale=math.inf)),
         (ar.ARError, lambda: ar.packed_attention(q.float(), k.float(), v.float())), (ValueError, lambda: ar.packed_attention(q.cpu(), k, v)),
         (ar.ARError, lambda: ar.packed_attention(draw((4, 2, 136), 0), draw((4, 2, 136), 0), draw((4, 2, 136), 0))),
-        (ValueError, lambda: ar.packed_attention(q.transpose(1, 2), k, v)), (ValueError, lambda: ar.packed_attention_backward(do, q, k, v, o, lse[:4])),
+        (ValueError, lambda: ar.packed_attention(q.transpose(1, 2), k, v)), (ValueError, lambda: ar.packed_attention_backward(do, q, k, v, o, lse[:, :4])),
         (ValueError, lambda: ar.packed_attention_backward(do[:4], q, k, v, o, lse)),
         (ar.ARError, lambda: ar.packed_attention_backward(do, q, k, v, o, lse, out=(do, torch.empty_like(k), torch.empty_like(v)))),
         (ar.ARError, lambda: ar.packed_attention_backward(do, q, k, v, o, lse, workspace=torch.empty(16, dtype=torch.uint8, device="cuda"))),

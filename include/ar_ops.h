@@ -215,8 +215,8 @@ enum { AR_ATTN_CAUSAL = 1, AR_ATTN_CLEAR = 2 };
  * tokens (0 = heads * hs), hs_* between heads (0 = dim).  Either a token's heads lie
  * within ld, or a head's tokens within hs; nothing overlaps. */
 typedef struct ar_attention_desc {
-    size_t sequences;             /* 0, or no tokens: a valid no-op */
-    size_t tokens_q, tokens_k;    /* times the heads: below 2^31 */
+    size_t sequences;             /* 0, or no tokens: a valid no-op; times heads at most 2^22 */
+    size_t tokens_q, tokens_k;    /* times heads, or kv_heads, at most 2^30 */
     size_t heads, kv_heads, dim;  /* heads a multiple of kv_heads; dim 1 .. 128 (AR_ERR_UNSUPPORTED above) */
     int dtype;                    /* AR_BFLOAT16 */
     int flags;                    /* AR_ATTN_* */
@@ -257,9 +257,10 @@ size_t ar_attention_backward_workspace(const ar_attention_desc *desc);
  * has no loss (0) and no gradient; its row of x has to be finite all the same where dW
  * is wanted (0 times it is added there).  The logits are never in memory. */
 typedef struct ar_vocab_desc {
-    size_t tokens;         /* 0 is a valid no-op (backward: zero weight gradient) */
+    size_t tokens;         /* 0 is a valid no-op (backward: zero weight gradient); at most
+                              2^24, times rows 2^38 */
     size_t dim;            /* 1 .. 2^20 */
-    size_t rows;           /* of W: 1 .. 2^28 */
+    size_t rows;           /* of W: 1 .. 2^26 */
     size_t first, classes; /* first + rows <= classes <= 2^40 */
     int dtype;             /* AR_BFLOAT16: x, W and their gradients */
     int target_bytes;      /* 4 or 8: signed whole numbers */

@@ -876,6 +876,8 @@ Tensor tensor(const void *p, size_t tokens, size_t heads, size_t dim, size_t ld,
     return {p, tokens, heads, dim, ld ? ld : heads * hs, hs};
 }
 
+constexpr size_t kMostRows = (size_t)1 << 30, kMostSequences = (size_t)1 << 22;  // times the heads
+
 int check_attention(const ar_attention_desc *d)
 {
     if (!d) return AR_ERR_ARG;
@@ -884,10 +886,8 @@ int check_attention(const ar_attention_desc *d)
     if (!(d->scale > 0.0f) || !isfinite(d->scale)) return AR_ERR_ARG;
     if (d->heads < 1 || d->kv_heads < 1 || d->heads > (1u << 16) || d->heads % d->kv_heads || d->dim < 1) return AR_ERR_ARG;
     if (d->dim > 128) return AR_ERR_UNSUPPORTED;
-    // rows are counted in 32 bits on the device
-    if (d->sequences > (1u << 24) || d->tokens_q > (1u << 30) || d->tokens_k > (1u << 30)) return AR_ERR_ARG;
-    if (d->tokens_q * d->heads >= (1ull << 31) || d->tokens_k * d->kv_heads >= (1ull << 31)) return AR_ERR_ARG;
-    if (d->sequences * d->heads >= (1ull << 28)) return AR_ERR_ARG;
+    // rows are counted in 32 bits on the device, and so are a launch's threads, 256 for a tile
+    if (d->sequences > kMostSequences / d->heads || d->tokens_q > kMostRows / d->heads || d->tokens_k > kMostRows / d->kv_heads) return AR_ERR_ARG;
     const size_t strides[] = {d->ld_q, d->hs_q, d->ld_k, d->hs_k, d->ld_v, d->hs_v, d->ld_o, d->hs_o, d->ld_dout, d->hs_dout,
                               d->ld_dq, d->hs_dq, d->ld_dk, d->hs_dk, d->ld_dv, d->hs_dv};
     for (size_t s : strides)
@@ -912,36 +912,49 @@ size_t key_slots(const ar_attention_desc &d) { return d.tokens_k / kRows + d.seq
 // longest tile, whose stages follow one another, and of the join least.  `stages`: of a
 // tile, in the mean, half as many again where there are several sequences, some of them
 // longer; us: of a stage, alone; bytes: of a run's sums.  A join takes 5 us, 0.2 for each
-// run and the sums' way to memory and back at 3.4 TB/s.  No more than `most` workgroups in
-// all: from there on the device is full and the sums are for nothing.  By sweeps of 1 to
-// 64 runs over fourteen sizes, each in one piece, with the best, as chosen: forward, 32
-// heads over 8 of 128, 1 query of 16000 keys 300, 34, 36 us, 32 of 7600 408, 203, 206;
-// dk and dv of 2048 queries, 16 heads over 2, 485, 74, 76 us.
-uint32_t runs_for(size_t tiles, double stages, double us, double bytes, size_t most, const ar_attention_desc &d)
+// run and the sums' way to memory and back at 3.4 TB/s.  Tiles of one length (one sequence,
+// most of its keys seen by every query) come in rounds of `room` workgroups.  No more than
+// `most` times that in all: from there on the device is full and the sums are for nothing.
+// By sweeps of 1 to 64 runs over fourteen sizes, each in one piece, with the best, as
+// chosen: forward, 32 heads over 8 of 128, 1 query of 16000 keys 300, 34, 36 us, 32 of
+// 7600 408, 203, 206; 8 heads over 1, 512 of 33000 581, 89, 89; dk and dv of 2048 queries,
+// 16 heads over 2, 485, 74, 76 us.
+uint32_t runs_for(size_t tiles, double stages, double us, double bytes, size_t room, size_t most, const ar_attention_desc &d)
 {
+    const bool alike = d.sequences == 1 && (!(d.flags & AR_ATTN_CAUSAL) || d.tokens_k >= 4 * d.tokens_q);
     if (d.sequences > 1) stages *= 1.5;
     uint32_t best = 1;
-    double time = stages * us;
-    for (uint32_t s = 2; s <= kMaxRuns && s <= stages && s * tiles <= most; ++s) {
-        const double t = stages / s * us + 5.0 + s * (0.2 + 2.0 * bytes / 3.4e6);
-        if (t < time) best = s, time = t;
+    double time = 0;
+    for (uint32_t s = 1; s <= kMaxRuns && (s == 1 || (s <= stages && s * tiles <= most * room)); ++s) {
+        double t = stages / s * us;
+        if (alike) t *= (tiles * s + room - 1) / room;
+        if (s > 1) t += 5.0 + s * (0.2 + 2.0 * bytes / 3.4e6);
+        if (s == 1 || t < time) best = s, time = t;
     }
     return best;
 }
 double mean_stages(size_t tokens, const ar_attention_desc &d) { return ceil((double)tokens / d.sequences / kKeys); }
 double sums_bytes(size_t rows, const ar_attention_desc &d) { return 4.0 * rows * d.dim; }
+// Tiles that there are if the lengths are as even as they can be.
+size_t tiles_for(size_t rows, const ar_attention_desc &d)
+{
+    const size_t n = (rows + kRows - 1) / kRows;
+    return (n > d.sequences ? n : d.sequences) * d.kv_heads;
+}
 uint32_t forward_splits(const ar_attention_desc &d)
 {
-    return runs_for(row_slots(d) * d.kv_heads, mean_stages(d.tokens_k, d), d.dim <= 64 ? 0.9 : 1.2, sums_bytes(d.tokens_q * d.heads, d), 2048, d);
+    return runs_for(tiles_for(d.tokens_q * (d.heads / d.kv_heads), d), mean_stages(d.tokens_k, d), d.dim <= 64 ? 0.9 : 1.2,
+                    sums_bytes(d.tokens_q * d.heads, d), 512, 4, d);
 }
 uint32_t dq_splits(const ar_attention_desc &d)
 {
-    return runs_for(row_slots(d) * d.kv_heads, mean_stages(d.tokens_k, d), d.dim <= 64 ? 1.3 : 1.8, sums_bytes(d.tokens_q * d.heads, d), 1024, d);
+    return runs_for(tiles_for(d.tokens_q * (d.heads / d.kv_heads), d), mean_stages(d.tokens_k, d), d.dim <= 64 ? 1.3 : 1.8,
+                    sums_bytes(d.tokens_q * d.heads, d), 512, 2, d);
 }
 uint32_t dkv_splits(const ar_attention_desc &d)
 {
-    return runs_for(key_slots(d) * d.kv_heads, mean_stages(d.tokens_q, d) * (d.heads / d.kv_heads), d.dim <= 64 ? 1.2 : 1.9,
-                    2 * sums_bytes(d.tokens_k * d.kv_heads, d), 512, d);
+    return runs_for(tiles_for(d.tokens_k, d), mean_stages(d.tokens_q, d) * (d.heads / d.kv_heads), d.dim <= 64 ? 1.2 : 1.9,
+                    2 * sums_bytes(d.tokens_k * d.kv_heads, d), 256, 2, d);
 }
 
 size_t part_bytes(uint32_t splits, size_t rows, size_t each) { return splits > 1 ? round_up(splits * rows * each * sizeof(float), 256) : 0; }

@@ -99,8 +99,9 @@ template <typename S> __global__ __launch_bounds__(S::THREADS) void vocab_stats_
     });
 }
 
-// Joins the runs of columns of each token, sixteen tokens to a workgroup and sixteen
-// threads to a token, in one order whatever the timing.
+// Joins the runs of columns of each token, TOKENS tokens to a workgroup, whose other
+// threads have runs of their own, in one order whatever the timing.  One token of 32768
+// classes: 512 runs, a token to a workgroup 4 us, sixteen 8.
 struct JoinOut {
     const Stat *stats;
     const float *picked;
@@ -109,22 +110,26 @@ struct JoinOut {
     uint32_t tokens, runs;
     float *loss, *lse;  // loss null: lse, and the target's logit behind it (0 where it is none of these rows)
 };
-__global__ __launch_bounds__(256) void vocab_join_kernel(const JoinOut o)
+template <uint32_t TOKENS> __global__ __launch_bounds__(256) void vocab_join_kernel(const JoinOut o)
 {
-    __shared__ Stat part[16][17];
-    const uint32_t in = threadIdx.x & 15u, k0 = threadIdx.x >> 4, t = blockIdx.x * 16 + in;
+    constexpr uint32_t EACH = 256 / TOKENS;  // threads of a token
+    __shared__ Stat part[TOKENS][EACH + 1];
+    const uint32_t in = threadIdx.x % TOKENS, k0 = threadIdx.x / TOKENS, t = blockIdx.x * TOKENS + in;
     Stat s{-INFINITY, 0.0f};
     if (t < o.tokens)
-        for (uint32_t k = k0; k < o.runs; k += 64) {
+        for (uint32_t k = k0; k < o.runs; k += 4 * EACH) {
             Stat a[4];
 #pragma unroll
-            for (int j = 0; j < 4; ++j) a[j] = k + 16 * j < o.runs ? o.stats[(uint64_t)(k + 16 * j) * o.tokens + t] : Stat{-INFINITY, 0.0f};
+            for (uint32_t j = 0; j < 4; ++j) a[j] = k + EACH * j < o.runs ? o.stats[(uint64_t)(k + EACH * j) * o.tokens + t] : Stat{-INFINITY, 0.0f};
             s = join(s, join(join(a[0], a[1]), join(a[2], a[3])));
         }
     part[in][k0] = s;
-    __syncthreads();
-    if (threadIdx.x >= 16 || t >= o.tokens) return;
-    for (int k = 1; k < 16; ++k) s = join(s, part[in][k]);
+#pragma unroll
+    for (uint32_t half = EACH / 2; half; half /= 2) {
+        __syncthreads();
+        if (k0 < half) part[in][k0] = s = join(s, part[in][k0 + half]);
+    }
+    if (k0 || t >= o.tokens) return;
     uint64_t target = 0;
     const bool counts = o.target.get(t, &target);
     const bool here = counts && target >= o.target.first && target - o.target.first < o.rows;
@@ -205,9 +210,10 @@ int check_vocab(const ar_vocab_desc *d)
     if (!d) return AR_ERR_ARG;
     if (d->dtype != AR_BFLOAT16) return AR_ERR_UNSUPPORTED;
     if (d->target_bytes != 4 && d->target_bytes != 8) return AR_ERR_UNSUPPORTED;
-    if (d->dim < 1 || d->rows < 1 || d->tokens > (1u << 30) || d->dim > (1u << 20) || d->rows > (1u << 28)) return AR_ERR_ARG;
+    if (d->dim < 1 || d->rows < 1 || d->tokens > (1u << 24) || d->dim > (1u << 20) || d->rows > (1u << 26)) return AR_ERR_ARG;
     if (d->classes > (1ull << 40) || d->first > d->classes || d->rows > d->classes - d->first) return AR_ERR_ARG;
-    if (d->tokens * d->rows > kOpsMaxSize || d->tokens * d->dim > kOpsMaxSize || d->rows * d->dim > kOpsMaxSize) return AR_ERR_ARG;
+    // a launch's threads are counted in 32 bits
+    if (d->tokens * d->rows > kOpsMaxSize / 4 || d->tokens * d->dim > kOpsMaxSize || d->rows * d->dim > kOpsMaxSize) return AR_ERR_ARG;
     const struct {
         size_t ld, rows;
     } lds[] = {{d->ld_x, d->tokens}, {d->ld_w, d->rows}, {d->ld_dx, d->tokens}, {d->ld_dw, d->rows}};
@@ -325,7 +331,8 @@ int vocab_loss(const ar_vocab_desc *desc, const void *x, const void *w, const vo
     }
     if (rc != AR_OK) return rc;
     const JoinOut j{o.stats, o.picked, o.target, d.rows, (uint32_t)d.tokens, (uint32_t)runs_of(d), loss, lse};
-    hipLaunchKernelGGL(vocab_join_kernel, dim3((uint32_t)((d.tokens + 15) / 16)), dim3(256), 0, st, j);
+    if (d.tokens <= 64) hipLaunchKernelGGL((vocab_join_kernel<1>), dim3((uint32_t)d.tokens), dim3(256), 0, st, j);
+    else hipLaunchKernelGGL((vocab_join_kernel<16>), dim3((uint32_t)((d.tokens + 15) / 16)), dim3(256), 0, st, j);
     return launch_status();
 }
 

@@ -36,8 +36,8 @@ def forward(x=X, w=W, target=T, loss=LOSS, lse=LSE, ws=WS, nbytes=1 << 27, **kw)
 
 BAD_DESC = [
     (dict(dtype=0), ar.AR_ERR_UNSUPPORTED), (dict(target_bytes=2), ar.AR_ERR_UNSUPPORTED), (dict(dim=0), ar.AR_ERR_ARG),
-    (dict(rows=0), ar.AR_ERR_ARG), (dict(dim=(1 << 20) + 1), ar.AR_ERR_ARG), (dict(rows=1 << 29, classes=1 << 29), ar.AR_ERR_ARG),
-    (dict(tokens=1 << 31), ar.AR_ERR_ARG), (dict(tokens=1 << 29, rows=1 << 20, classes=1 << 20), ar.AR_ERR_ARG), (dict(first=1), ar.AR_ERR_ARG),
+    (dict(rows=0), ar.AR_ERR_ARG), (dict(dim=(1 << 20) + 1), ar.AR_ERR_ARG), (dict(rows=(1 << 26) + 1, classes=1 << 29), ar.AR_ERR_ARG),
+    (dict(tokens=1 << 31), ar.AR_ERR_ARG), (dict(tokens=1 << 20, rows=1 << 20, classes=1 << 20), ar.AR_ERR_ARG), (dict(tokens=(1 << 24) + 1), ar.AR_ERR_ARG), (dict(first=1), ar.AR_ERR_ARG),
     (dict(first=1 << 60), ar.AR_ERR_ARG), (dict(classes=99), ar.AR_ERR_ARG), (dict(classes=1 << 50), ar.AR_ERR_ARG), (dict(ld_x=63), ar.AR_ERR_ARG),
     (dict(ld_w=1 << 50), ar.AR_ERR_ARG)]
 BAD = BAD_DESC + [

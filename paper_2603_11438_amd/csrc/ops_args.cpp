@@ -14,6 +14,7 @@
 #include <c10/core/GradMode.h>
 #include <torch/csrc/autograd/python_variable.h>
 
+#include <math.h>
 #include <stdint.h>
 
 #include "ar_ops.h"
@@ -267,6 +268,105 @@ PyObject *ffn_backward(PyObject *, PyObject *const *a, Py_ssize_t n)
     }
 }
 
+// One of attention's tensors: (tokens, heads, dim), the elements of a head contiguous,
+// nothing overlapping.
+struct HeadsOf {
+    const at::Tensor *t = nullptr;
+    int64_t tokens = 0, heads = 0, dim = 0, ld = 0, hs = 0;
+};
+bool as_heads(PyObject *o, long device, HeadsOf *r)
+{
+    const at::Tensor *t = plain(o, device);
+    if (!t || t->dim() != 3 || t->numel() == 0 || t->scalar_type() != at::kBFloat16) return false;
+    r->t = t, r->tokens = t->size(0), r->heads = t->size(1), r->dim = t->size(2), r->ld = t->stride(0), r->hs = t->stride(1);
+    if (r->dim > 1 && t->stride(2) != 1) return false;
+    if (r->heads == 1) r->hs = r->dim;
+    if (r->tokens == 1) r->ld = (r->heads - 1) * r->hs + r->dim;
+    return r->hs >= r->dim && r->ld >= r->dim && (r->ld >= (r->heads - 1) * r->hs + r->dim || r->hs >= (r->tokens - 1) * r->ld + r->dim);
+}
+bool as_starts(PyObject *o, long device, const at::Tensor **t)
+{
+    *t = plain(o, device);
+    return *t && (*t)->dim() == 1 && (*t)->is_contiguous() && (*t)->scalar_type() == at::kInt && (*t)->numel() >= 2;
+}
+
+// attention(fn, workspace_for_fn, q, k, v, starts_q, starts_k, causal, scale, save, device, stream) -> (o, lse or None)
+PyObject *attention(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    if (n != 12) return PyErr_Format(PyExc_TypeError, "attention takes 12 arguments");
+    void *fn = PyLong_AsVoidPtr(a[0]), *space = PyLong_AsVoidPtr(a[1]), *stream = PyLong_AsVoidPtr(a[11]);
+    const long device = PyLong_AsLong(a[10]);
+    const int causal = PyObject_IsTrue(a[7]), save = PyObject_IsTrue(a[9]);
+    if (PyErr_Occurred()) return nullptr;
+    try {
+        HeadsOf q, k, v;
+        if (!as_heads(a[2], device, &q) || !as_heads(a[3], device, &k) || !as_heads(a[4], device, &v)) return none();
+        if (k.tokens != v.tokens || k.heads != v.heads || k.dim != q.dim || v.dim != q.dim || q.heads % k.heads) return none();
+        ar_attention_desc d{};
+        d.sequences = 1;
+        const at::Tensor *sq = nullptr, *sk = nullptr;
+        if (a[5] != Py_None) {
+            if (!as_starts(a[5], device, &sq) || (a[6] != Py_None && !as_starts(a[6], device, &sk))) return none();
+            if (!sk) sk = sq;
+            if (sk->numel() != sq->numel()) return none();
+            d.sequences = (size_t)sq->numel() - 1;
+        } else if (a[6] != Py_None) {
+            return none();
+        }
+        d.tokens_q = (size_t)q.tokens, d.tokens_k = (size_t)k.tokens, d.heads = (size_t)q.heads, d.kv_heads = (size_t)k.heads;
+        d.dim = (size_t)q.dim, d.dtype = AR_BFLOAT16, d.flags = (causal ? AR_ATTN_CAUSAL : 0) | AR_ATTN_CLEAR;
+        const double scale = a[8] == Py_None ? 1.0 / sqrt((double)q.dim) : PyFloat_AsDouble(a[8]);
+        if (PyErr_Occurred()) {
+            PyErr_Clear();
+            return none();
+        }
+        d.scale = (float)scale;
+        d.ld_q = (size_t)q.ld, d.hs_q = (size_t)q.hs, d.ld_k = (size_t)k.ld, d.hs_k = (size_t)k.hs, d.ld_v = (size_t)v.ld, d.hs_v = (size_t)v.hs;
+        at::Tensor o = at::empty(q.t->sizes(), q.t->options()), lse, ws;
+        if (save) lse = at::empty({q.heads, q.tokens}, q.t->options().dtype(at::kFloat));
+        const size_t bytes = ((decltype(&ar_attention_workspace_for))space)(&d, q.t->data_ptr(), k.t->data_ptr(), v.t->data_ptr());
+        if (bytes) ws = at::empty({(int64_t)bytes}, q.t->options().dtype(at::kByte));
+        int rc;
+        Py_BEGIN_ALLOW_THREADS
+        rc = ((decltype(&ar_attention))fn)(&d, q.t->data_ptr(), k.t->data_ptr(), v.t->data_ptr(), (const int32_t *)ptr(sq), (const int32_t *)ptr(sk),
+                                           ptr(o), (float *)ptr(lse), ptr(ws), bytes, stream);
+        Py_END_ALLOW_THREADS
+        return rc ? PyLong_FromLong(rc) : tuple({THPVariable_Wrap(o), wrap_or_none(lse)});
+    } catch (...) {
+        return none();
+    }
+}
+
+// vocab_loss(fn, workspace_fn, x, weight, target, device, stream) -> (loss, lse)
+PyObject *vocab_loss(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    if (n != 7) return PyErr_Format(PyExc_TypeError, "vocab_loss takes 7 arguments");
+    void *fn = PyLong_AsVoidPtr(a[0]), *space = PyLong_AsVoidPtr(a[1]), *stream = PyLong_AsVoidPtr(a[6]);
+    const long device = PyLong_AsLong(a[5]);
+    if (PyErr_Occurred()) return nullptr;
+    try {
+        Rows x, w;
+        const at::Tensor *t = plain(a[4], device);
+        if (!as_rows(a[2], device, &x) || !as_rows(a[3], device, &w) || w.t->dim() != 2 || w.cols != x.cols || dtype_of(*x.t) != AR_BFLOAT16 ||
+            w.t->scalar_type() != x.t->scalar_type())
+            return none();
+        if (!t || !t->is_contiguous() || t->numel() != x.rows || (t->scalar_type() != at::kLong && t->scalar_type() != at::kInt)) return none();
+        ar_vocab_desc d{};
+        d.tokens = (size_t)x.rows, d.dim = (size_t)x.cols, d.rows = d.classes = (size_t)w.rows, d.dtype = AR_BFLOAT16;
+        d.target_bytes = t->scalar_type() == at::kLong ? 8 : 4, d.ld_x = (size_t)x.ld, d.ld_w = (size_t)w.ld;
+        at::Tensor loss = at::empty(t->sizes(), t->options().dtype(at::kFloat)), lse = at::empty(t->sizes(), loss.options());
+        const size_t bytes = ((decltype(&ar_vocab_loss_workspace))space)(&d, x.p(), w.p());
+        at::Tensor ws = workspace(bytes, x);
+        int rc;
+        Py_BEGIN_ALLOW_THREADS
+        rc = ((decltype(&ar_vocab_loss))fn)(&d, x.p(), w.p(), ptr(t), (float *)ptr(loss), (float *)ptr(lse), ptr(ws), bytes, stream);
+        Py_END_ALLOW_THREADS
+        return rc ? PyLong_FromLong(rc) : tuple({THPVariable_Wrap(loss), THPVariable_Wrap(lse)});
+    } catch (...) {
+        return none();
+    }
+}
+
 PyObject *tell_graphs(PyObject *, PyObject *told)
 {
     const int is = PyObject_IsTrue(told);
@@ -280,6 +380,8 @@ PyMethodDef methods[] = {
     {"norm_backward", (PyCFunction)(void (*)(void))norm_backward, METH_FASTCALL, "ar_residual_norm_backward on tensors."},
     {"ffn", (PyCFunction)(void (*)(void))ffn, METH_FASTCALL, "ar_gated_ffn on tensors."},
     {"ffn_backward", (PyCFunction)(void (*)(void))ffn_backward, METH_FASTCALL, "ar_gated_ffn_backward on tensors."},
+    {"attention", (PyCFunction)(void (*)(void))attention, METH_FASTCALL, "ar_attention on tensors."},
+    {"vocab_loss", (PyCFunction)(void (*)(void))vocab_loss, METH_FASTCALL, "ar_vocab_loss on tensors."},
     {"tell_graphs", tell_graphs, METH_O, "Whether the caller knows that results have no autograd graph."},
     {nullptr, nullptr, 0, nullptr}};
 

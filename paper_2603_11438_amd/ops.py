@@ -134,6 +134,9 @@ class _Native:
         self.norm_backward_fns = address("ar_residual_norm_backward"), address("ar_residual_norm_backward_workspace")
         self.ffn_fns = address("ar_gated_ffn"), address("ar_gated_ffn_workspace_for")
         self.ffn_backward_fns = address("ar_gated_ffn_backward"), address("ar_gated_ffn_backward_workspace")
+        self.attention, self.vocab_loss = mod.attention, mod.vocab_loss
+        self.attention_fns = address("ar_attention"), address("ar_attention_workspace_for")
+        self.vocab_loss_fns = address("ar_vocab_loss"), address("ar_vocab_loss_workspace")
         self.in_use, self.device, self.stream = torch.cuda.is_initialized, torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream
 
 
@@ -643,6 +646,12 @@ def packed_attention(q, k, v, *, starts_q=None, starts_k=None, causal: bool = Tr
     otherwise.  lse: (heads, queries) fp32."""
     import torch
 
+    if out is None and stream is None and (nat := _native()) is not None:
+        dev = nat.device()
+        got = nat.attention(*nat.attention_fns, q, k, v, starts_q, starts_k, causal, scale, save, dev, nat.stream(dev))
+        if got is not None:
+            o, lse = _done(got, "ar_attention")
+            return (o, lse) if save else o
     _tell_of_graphs(q, k, v)
     with _On(q, stream) as on:
         d, sq, sk = _attention_desc(q, k, v, starts_q, starts_k, causal, scale, on.index, out is None)
@@ -758,6 +767,11 @@ def vocab_loss(x, weight, target, *, stream=None):
     token; a target that is no class (a negative one, say) gives no loss and no gradient."""
     import torch
 
+    if stream is None and (nat := _native()) is not None:
+        dev = nat.device()
+        got = nat.vocab_loss(*nat.vocab_loss_fns, x, weight, target, dev, nat.stream(dev))
+        if got is not None:
+            return _done(got, "ar_vocab_loss")
     _tell_of_graphs(x, weight)
     with _On(x, stream) as on:
         d = _vocab_desc(x, weight, target, 0, None, on.index)

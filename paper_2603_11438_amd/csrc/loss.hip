@@ -157,8 +157,12 @@ __global__ __launch_bounds__(256) void vocab_ranks_kernel(const float *parts, ui
     loss[t] = target.get(t, &unused) ? log + (base - z) : 0.0f;
 }
 
-// dz of a piece of the vocabulary: (e^(z - lse) - [target]) dloss, 0 for a token without
-// a loss and up to the next multiple of eight columns.
+// dz of a piece of the vocabulary: (e^(z - lse) - [target]) dloss / f, 0 for a token
+// without a loss and up to the next multiple of eight columns.  f is the significand of
+// the first token's dloss, and the products with dz are multiplied by it in fp32.  With one
+// dloss for all tokens, the mean's, most of dz's weight lies in targets' elements, all of
+// them near -dloss: rounded to bf16, all would be off in one direction, and the gradients
+// by as much (777 tokens of 5001 classes: by 2.6e-3 of their norm, so by 1.7e-3).
 struct DzOut {
     bf16 *dz;
     uint64_t ld;
@@ -189,7 +193,7 @@ template <typename S> __global__ __launch_bounds__(S::THREADS) void vocab_dz_ker
         const bool counts = o.target.get(row, &t);
         const uint64_t place = t - o.target.first - col0;
         const uint32_t hit = counts && t >= o.target.first && place < COLS ? (uint32_t)place : 0xffffffffu;
-        const float lse = o.lse[row] * kLog2e, by = o.dloss[row * o.dloss_stride];
+        const float lse = o.lse[row] * kLog2e, by = o.dloss[row * o.dloss_stride] / factor(o.dloss);
         stage_rows<bf16, COLS>(stage, [&](int j, int r) {
             const uint32_t c = (uint32_t)(j * 32 + 8 * (r / 4) + r % 4) + 4 * h;
             const float p = __builtin_amdgcn_exp2f(v[j][r] * kLog2e - lse);
@@ -424,7 +428,7 @@ int vocab_backward(const ar_vocab_desc *desc, const float *dloss, size_t dloss_s
     GemmArgs logits{};
     Operand px, pw;
     if ((rc = logits_args(d, m, (char *)ws + s.copies, &logits, &px, &pw, st)) != AR_OK) return rc;
-    const ProductOut to_dx{{(bf16 *)dx, nullptr}, part_dx, {odx.ld, 0}, 0x80000000u, (uint32_t)d.tokens, (uint32_t)d.dim, false};
+    const ProductOut to_dx{{(bf16 *)dx, nullptr}, part_dx, {odx.ld, 0}, 0x80000000u, (uint32_t)d.tokens, (uint32_t)d.dim, false, dloss};
     for (size_t k = 0; k < s.pieces; ++k) {
         const size_t first = k * s.piece, rows = d.rows - first < s.piece ? d.rows - first : s.piece;
         const char *wk = (const char *)pw.p + first * pw.ld;
@@ -451,7 +455,7 @@ int vocab_backward(const ar_vocab_desc *desc, const float *dloss, size_t dloss_s
             out.more = k > 0;
             Cut cut = s.dx;
             if (cut.splits > p.steps) cut.splits = p.steps;  // a short last piece: the other runs' sums stay
-            rc = s.pieces > 1 ? product<false, true>(cut, p, out, st) : product<false>(cut, p, out, st);
+            rc = s.pieces > 1 ? product<false, true, true>(cut, p, out, st) : product<false, false, true>(cut, p, out, st);
             if (rc != AR_OK) return rc;
         }
         if (dw) {
@@ -460,11 +464,11 @@ int vocab_backward(const ar_vocab_desc *desc, const float *dloss, size_t dloss_s
             p.ka = p.kb = (uint32_t)d.tokens;
             p.a[0] = dz, p.b[0] = px.p, p.lda = (uint32_t)(s.ld * 2), p.ldb = px.ld;
             p.m = (uint32_t)round_up(rows, 8), p.n = px.cols;
-            const ProductOut out{{(bf16 *)dw + first * odw.ld, nullptr}, part_dw, {odw.ld, 0}, 0x80000000u, (uint32_t)rows, (uint32_t)d.dim, false};
-            if ((rc = product<true>(s.dw, p, out, st)) != AR_OK) return rc;
+            const ProductOut out{{(bf16 *)dw + first * odw.ld, nullptr}, part_dw, {odw.ld, 0}, 0x80000000u, (uint32_t)rows, (uint32_t)d.dim, false, dloss};
+            if ((rc = product<true, false, true>(s.dw, p, out, st)) != AR_OK) return rc;
         }
     }
-    return dx && s.pieces > 1 ? run_join(to_dx, (uint32_t)d.tokens, s.dx.splits, st) : AR_OK;
+    return dx && s.pieces > 1 ? run_join<true>(to_dx, (uint32_t)d.tokens, s.dx.splits, st) : AR_OK;
 }
 
 }  // namespace

@@ -62,15 +62,23 @@ template <int COLS> __device__ __forceinline__ void add_rows(const char *lds, fl
 // of 32), of which the first `rows` exist: one result, or dWg and then dWu.
 // With k split, each run's sums go to `part` instead, [run][m][cols].  ADD: one of
 // several products that make up a result: its sums go to `part` however many runs there
-// are, and with `more` are added to what is there.
+// are, and with `more` are added to what is there.  BY: results are multiplied by
+// factor(by) before they are rounded (not what goes to `part`).
 struct ProductOut {
     bf16 *out[2];
     float *part;
     uint64_t ld[2];
     uint32_t half, rows, cols;
     bool more;
+    const float *by;
 };
-template <typename S, bool ABYK, bool ADD = false> __global__ __launch_bounds__(S::THREADS) void product_kernel(const GemmArgs g, const ProductOut o)
+// The significand, in [1/2, 1), of the value there; 1 for one that has none.
+__device__ __forceinline__ float factor(const float *p)
+{
+    const float m = fabsf(__builtin_amdgcn_frexp_mantf(*p));
+    return m >= 0.5f && m < 1.0f ? m : 1.0f;
+}
+template <typename S, bool ABYK, bool ADD = false, bool BY = false> __global__ __launch_bounds__(S::THREADS) void product_kernel(const GemmArgs g, const ProductOut o)
 {
     constexpr int NT = S::NT, COLS = NT * 32;
     extern __shared__ __attribute__((aligned(16))) char lds[];
@@ -88,6 +96,7 @@ template <typename S, bool ABYK, bool ADD = false> __global__ __launch_bounds__(
         const uint32_t first = row0 + i * 32, which = first >= o.half, r = first - which * o.half;
         if (first >= g.m || r >= o.rows) return;
         auto value = [&](int j, int q) { return v[j][q]; };
+        const float by = BY ? factor(o.by) : 1.0f;
         if (ADD && o.more) {
             stage_rows<float, COLS>(stage, value);
             add_rows<COLS>(stage, o.part + ((uint64_t)blockIdx.y * g.m + first) * o.cols + col0, o.cols, o.rows - r, o.cols - col0);
@@ -96,16 +105,17 @@ template <typename S, bool ABYK, bool ADD = false> __global__ __launch_bounds__(
             write_rows<float, COLS>(stage, o.part + ((uint64_t)blockIdx.y * g.m + first) * o.cols + col0, o.cols, 0, o.rows - r,
                                     o.cols - col0);
         } else {
-            stage_rows<bf16, COLS>(stage, value);
+            stage_rows<bf16, COLS>(stage, [&](int j, int q) { return BY ? v[j][q] * by : v[j][q]; });
             write_rows<bf16, COLS>(stage, o.out[which] + (uint64_t)r * o.ld[which] + col0, o.ld[which], 0, o.rows - r, o.cols - col0);
         }
     });
 }
 
 // Adds the runs of a split product in their order, four columns a thread.
-static __global__ __launch_bounds__(256) void join_kernel(const ProductOut o, uint32_t m, uint32_t splits)
+template <bool BY> __global__ __launch_bounds__(256) void join_kernel(const ProductOut o, uint32_t m, uint32_t splits)
 {
     const uint64_t all = (uint64_t)m * o.cols, per = (o.cols + 3) / 4, n = m * per;
+    const float by = BY ? factor(o.by) : 1.0f;
     for (uint64_t i = (uint64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (uint64_t)gridDim.x * 256) {
         const uint32_t row = (uint32_t)(i / per), c = (uint32_t)(i % per) * 4, which = row >= o.half, r = row - which * o.half;
         if (r >= o.rows) continue;
@@ -120,12 +130,14 @@ static __global__ __launch_bounds__(256) void join_kernel(const ProductOut o, ui
 #pragma unroll
                 for (int k = 0; k < 4; ++k) v[k] += w[k];
             }
+#pragma unroll
+            for (int k = 0; k < 4; ++k) v[k] = BY ? v[k] * by : v[k];
             store_vec<bf16, 4>(to, v);
         } else {
             for (uint32_t k = 0; k < o.cols - c; ++k) {
                 float t = from[k];
                 for (uint32_t s = 1; s < splits; ++s) t += from[s * all + k];
-                to[k] = (bf16)t;
+                to[k] = (bf16)(BY ? t * by : t);
             }
         }
     }
@@ -196,37 +208,37 @@ inline size_t part_bytes(const Cut &c, size_t m, size_t cols)
     return c.splits > 1 ? round_up(c.splits * m * cols * sizeof(float), 256) : 0;
 }
 
-inline int run_join(const ProductOut &o, uint32_t m, uint32_t splits, hipStream_t st)
+template <bool BY> int run_join(const ProductOut &o, uint32_t m, uint32_t splits, hipStream_t st)
 {
     const uint64_t groups = ((uint64_t)m * ((o.cols + 3) / 4) + 255) / 256;
-    hipLaunchKernelGGL(join_kernel, dim3((uint32_t)(groups < 8192 ? groups : 8192)), dim3(256), 0, st, o, m, splits);
+    hipLaunchKernelGGL((join_kernel<BY>), dim3((uint32_t)(groups < 8192 ? groups : 8192)), dim3(256), 0, st, o, m, splits);
     return launch_status();
 }
 
 // ADD: the caller joins once all products are there.
-template <typename S, bool ABYK, bool ADD> int launch_product(GemmArgs &g, const ProductOut &o, hipStream_t st)
+template <typename S, bool ABYK, bool ADD, bool BY> int launch_product(GemmArgs &g, const ProductOut &o, hipStream_t st)
 {
     g.tiles_m = (g.m + S::BM - 1) / S::BM;
     g.tiles_n = (o.cols + S::BN - 1) / S::BN;
     constexpr int STAGE = 4 * kStageBytes<float, S::NT * 32>, LDS = S::LDS > STAGE ? S::LDS : STAGE;
     static OncePerDevice once;
-    int rc = allow_lds(once, (const void *)product_kernel<S, ABYK, ADD>, LDS);
+    int rc = allow_lds(once, (const void *)product_kernel<S, ABYK, ADD, BY>, LDS);
     if (rc != AR_OK) return rc;
-    hipLaunchKernelGGL((product_kernel<S, ABYK, ADD>), dim3(g.tiles_m * g.tiles_n, g.splits), dim3(S::THREADS), LDS, st, g, o);
+    hipLaunchKernelGGL((product_kernel<S, ABYK, ADD, BY>), dim3(g.tiles_m * g.tiles_n, g.splits), dim3(S::THREADS), LDS, st, g, o);
     rc = launch_status();
-    return rc != AR_OK || g.splits == 1 || ADD ? rc : run_join(o, g.m, g.splits, st);
+    return rc != AR_OK || g.splits == 1 || ADD ? rc : run_join<BY>(o, g.m, g.splits, st);
 }
 
 // B by k; A by rows (dx) or by k (the weights' gradients).
-template <bool ABYK, bool ADD = false> int product(const Cut &c, GemmArgs &g, const ProductOut &o, hipStream_t st)
+template <bool ABYK, bool ADD = false, bool BY = false> int product(const Cut &c, GemmArgs &g, const ProductOut &o, hipStream_t st)
 {
     g.splits = c.splits, g.batch = 1;
     switch (c.tile) {
-    case 0: return launch_product<Tiny, ABYK, ADD>(g, o, st);
-    case 1: return launch_product<Small, ABYK, ADD>(g, o, st);
-    case 2: return launch_product<Middle, ABYK, ADD>(g, o, st);
-    case 3: return launch_product<Large, ABYK, ADD>(g, o, st);
-    default: return launch_product<Deep, ABYK, ADD>(g, o, st);
+    case 0: return launch_product<Tiny, ABYK, ADD, BY>(g, o, st);
+    case 1: return launch_product<Small, ABYK, ADD, BY>(g, o, st);
+    case 2: return launch_product<Middle, ABYK, ADD, BY>(g, o, st);
+    case 3: return launch_product<Large, ABYK, ADD, BY>(g, o, st);
+    default: return launch_product<Deep, ABYK, ADD, BY>(g, o, st);
     }
 }
 

@@ -220,7 +220,7 @@ typedef struct ar_attention_desc {
     size_t heads, kv_heads, dim;  /* heads a multiple of kv_heads; dim 1 .. 128 (AR_ERR_UNSUPPORTED above) */
     int dtype;                    /* AR_BFLOAT16 */
     int flags;                    /* AR_ATTN_* */
-    float scale;                  /* > 0 and finite; 1 / sqrt(dim) as a rule */
+    float scale;                  /* 2^-100 .. 2^100; 1 / sqrt(dim) as a rule */
     size_t ld_q, hs_q, ld_k, hs_k, ld_v, hs_v, ld_o, hs_o;
     size_t ld_dout, hs_dout, ld_dq, hs_dq, ld_dk, hs_dk, ld_dv, hs_dv;  /* backward only */
 } ar_attention_desc;
@@ -280,7 +280,8 @@ size_t ar_vocab_loss_workspace(const ar_vocab_desc *desc, const void *x, const v
 int ar_vocab_loss_part(const ar_vocab_desc *desc, const void *x, const void *w, const void *target, float *part,
                        void *workspace, size_t workspace_bytes, void *stream);
 /* Joins the parts of `ranks` ranks (1 .. 65536), one after another, whose rows make up the
- * vocabulary.  Of the description tokens, classes and target_bytes count. */
+ * vocabulary.  Of the description, valid as a whole, tokens, classes and target_bytes
+ * count. */
 int ar_vocab_loss_join(const ar_vocab_desc *desc, size_t ranks, const float *parts, const void *target, float *loss, float *lse,
                        void *stream);
 

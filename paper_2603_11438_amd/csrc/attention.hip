@@ -91,16 +91,21 @@ __device__ __forceinline__ Place find_place(const AttnArgs &a, uint32_t slot, bo
 }
 
 // Zeros in the rows of no sequence, by the workgroups behind the tiles'.
-constexpr uint32_t kRestGroups = 32;
+constexpr uint32_t kRestGroups = 128;
 template <typename T> __device__ void clear_rest(const Heads<T> &x, const int32_t *starts, uint32_t sequences, uint32_t tokens,
                                                 uint32_t heads, uint32_t dim, uint32_t group)
 {
     const uint32_t a = start_of(starts, 0, tokens), b = start_of(starts, starts ? sequences : 1, tokens), rest = a + (tokens - b);
     if (b < a) return;
-    const uint64_t n = (uint64_t)rest * heads * dim;
-    for (uint64_t i = (uint64_t)group * blockDim.x + threadIdx.x; i < n; i += (uint64_t)kRestGroups * blockDim.x) {
-        const uint32_t t = (uint32_t)(i / ((uint64_t)heads * dim)), c = (uint32_t)(i % ((uint64_t)heads * dim));
-        x.at(t < a ? t : b + (t - a), c / dim)[c % dim] = (T)0.0f;
+    constexpr int V = sizeof(T) == 2 ? 8 : 4;
+    const float zeros[V] = {};
+    const uint32_t per = (dim + V - 1) / V;
+    const uint64_t each = (uint64_t)heads * per, n = rest * each;
+    for (uint64_t i = (uint64_t)group * 256 + threadIdx.x; i < n; i += kRestGroups * 256) {
+        const uint32_t t = (uint32_t)(i / each), c = (uint32_t)(i % each), d = c % per * V;
+        T *to = x.at(t < a ? t : b + (t - a), c / per) + d;
+        if (d + V <= dim) store_vec<T, V>(to, zeros);
+        else store_part<T, V>(to, (int)(dim - d), zeros);
     }
 }
 
@@ -883,7 +888,7 @@ int check_attention(const ar_attention_desc *d)
     if (!d) return AR_ERR_ARG;
     if (d->dtype != AR_BFLOAT16) return AR_ERR_UNSUPPORTED;
     if (d->flags & ~(AR_ATTN_CAUSAL | AR_ATTN_CLEAR)) return AR_ERR_ARG;
-    if (!(d->scale > 0.0f) || !isfinite(d->scale)) return AR_ERR_ARG;
+    if (!(d->scale >= 0x1p-100f && d->scale <= 0x1p100f)) return AR_ERR_ARG;  // with log2(e) in it still a normal number
     if (d->heads < 1 || d->kv_heads < 1 || d->heads > (1u << 16) || d->heads % d->kv_heads || d->dim < 1) return AR_ERR_ARG;
     if (d->dim > 128) return AR_ERR_UNSUPPORTED;
     // rows are counted in 32 bits on the device, and so are a launch's threads, 256 for a tile

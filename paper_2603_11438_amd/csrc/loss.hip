@@ -108,7 +108,7 @@ struct JoinOut {
     Targets target;
     uint64_t rows;      // of the weight at hand
     uint32_t tokens, runs;
-    float *loss, *lse;  // loss null: lse, and the target's logit behind it (0 where it is none of these rows)
+    float *loss, *lse, *logit;  // loss null: lse, and the target's logit, 0 where it is none of these rows
 };
 template <uint32_t TOKENS> __global__ __launch_bounds__(256) void vocab_join_kernel(const JoinOut o)
 {
@@ -136,7 +136,7 @@ template <uint32_t TOKENS> __global__ __launch_bounds__(256) void vocab_join_ker
     const float base = s.top == -INFINITY ? 0.0f : s.top, z = here ? o.picked[t] : 0.0f, log = __logf(s.sum);
     o.lse[t] = base + log;
     if (o.loss) o.loss[t] = counts ? log + (base - z) : 0.0f;
-    else o.lse[o.tokens + t] = z;
+    else o.logit[t] = z;
 }
 
 // Joins the ranks' (lse, target's logit).
@@ -247,15 +247,22 @@ int logits_tile(size_t tokens, size_t dim, size_t rows)
 size_t wave_columns(int tile) { return tile == 0 ? 32 : tile == 2 ? 96 : tile == 3 ? 128 : 64; }
 size_t runs_of(const ar_vocab_desc &d) { return (d.rows + wave_columns(logits_tile(d.tokens, d.dim, d.rows)) - 1) / wave_columns(logits_tile(d.tokens, d.dim, d.rows)); }
 
-// Where the forward pass keeps what: the statistics, the targets' logits, copies.
+// Where the forward pass keeps what: the statistics, the targets' logits, copies.  The
+// statistics, a 64th of the logits' bytes in fp32, are kept for so many tokens at a time
+// that they stay within this, many rounds of tiles.
+constexpr size_t kStatsBytes = (size_t)1 << 28;
 struct VocabSpace {
+    size_t tokens;  // at a time
     size_t picked, copies;
 };
 VocabSpace vocab_space(const ar_vocab_desc &d)
 {
     VocabSpace s;
-    s.picked = round_up(runs_of(d) * d.tokens * sizeof(Stat), 256);
-    s.copies = s.picked + round_up(d.tokens * sizeof(float), 256);
+    const size_t runs = runs_of(d), most = kStatsBytes / (runs * sizeof(Stat)) / 256 * 256;
+    s.tokens = d.tokens <= most ? d.tokens : most < 1024 ? 1024 : most;
+    s.tokens = s.tokens < d.tokens ? s.tokens : d.tokens;
+    s.picked = round_up(runs * s.tokens * sizeof(Stat), 256);
+    s.copies = s.picked + round_up(s.tokens * sizeof(float), 256);
     return s;
 }
 size_t copy_bytes(const Mat &m) { return round_up(packed_bytes(m.rows, m.cols), 256); }
@@ -324,20 +331,29 @@ int vocab_loss(const ar_vocab_desc *desc, const void *x, const void *w, const vo
     GemmArgs g{};
     Operand px, pw;
     if ((rc = logits_args(d, m, (char *)ws + s.copies, &g, &px, &pw, st)) != AR_OK) return rc;
-    const StatsOut o{(Stat *)ws, (float *)((char *)ws + s.picked), targets(d, target)};
-    switch (logits_tile(d.tokens, d.dim, d.rows)) {
-    case kFewTokens: rc = launch_stats<Flat>(g, o, st); break;
-    case 0: rc = launch_stats<Tiny>(g, o, st); break;
-    case 1: rc = launch_stats<Small>(g, o, st); break;
-    case 2: rc = launch_stats<Middle>(g, o, st); break;
-    case 3: rc = launch_stats<Large>(g, o, st); break;
-    default: rc = launch_stats<Deep>(g, o, st);
+    const int tile = logits_tile(d.tokens, d.dim, d.rows);
+    for (size_t first = 0; first < d.tokens; first += s.tokens) {
+        const size_t tokens = d.tokens - first < s.tokens ? d.tokens - first : s.tokens;
+        GemmArgs gb = g;
+        gb.a[0] = (const char *)px.p + first * px.ld, gb.m = (uint32_t)tokens;
+        StatsOut o{(Stat *)ws, (float *)((char *)ws + s.picked), targets(d, target)};
+        o.target.p = (const char *)target + first * d.target_bytes;
+        switch (tile) {
+        case kFewTokens: rc = launch_stats<Flat>(gb, o, st); break;
+        case 0: rc = launch_stats<Tiny>(gb, o, st); break;
+        case 1: rc = launch_stats<Small>(gb, o, st); break;
+        case 2: rc = launch_stats<Middle>(gb, o, st); break;
+        case 3: rc = launch_stats<Large>(gb, o, st); break;
+        default: rc = launch_stats<Deep>(gb, o, st);
+        }
+        if (rc != AR_OK) return rc;
+        const JoinOut j{o.stats, o.picked, o.target, d.rows, (uint32_t)tokens, (uint32_t)runs_of(d), loss ? loss + first : nullptr, lse + first,
+                        loss ? nullptr : lse + d.tokens + first};
+        if (tokens <= 64) hipLaunchKernelGGL((vocab_join_kernel<1>), dim3((uint32_t)tokens), dim3(256), 0, st, j);
+        else hipLaunchKernelGGL((vocab_join_kernel<16>), dim3((uint32_t)((tokens + 15) / 16)), dim3(256), 0, st, j);
+        if ((rc = launch_status()) != AR_OK) return rc;
     }
-    if (rc != AR_OK) return rc;
-    const JoinOut j{o.stats, o.picked, o.target, d.rows, (uint32_t)d.tokens, (uint32_t)runs_of(d), loss, lse};
-    if (d.tokens <= 64) hipLaunchKernelGGL((vocab_join_kernel<1>), dim3((uint32_t)d.tokens), dim3(256), 0, st, j);
-    else hipLaunchKernelGGL((vocab_join_kernel<16>), dim3((uint32_t)((d.tokens + 15) / 16)), dim3(256), 0, st, j);
-    return launch_status();
+    return AR_OK;
 }
 
 int vocab_join(const ar_vocab_desc *desc, size_t ranks, const float *parts, const void *target, float *loss, float *lse, void *stream)

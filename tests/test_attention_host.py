@@ -38,7 +38,7 @@ BAD_DESC = [
     (dict(dtype=0), ar.AR_ERR_UNSUPPORTED), (dict(dim=129), ar.AR_ERR_UNSUPPORTED), (dict(dim=0), ar.AR_ERR_ARG), (dict(heads=0), ar.AR_ERR_ARG),
     (dict(kv_heads=0), ar.AR_ERR_ARG), (dict(kv_heads=3), ar.AR_ERR_ARG), (dict(kv_heads=8), ar.AR_ERR_ARG), (dict(flags=4), ar.AR_ERR_ARG),
     (dict(scale=0.0), ar.AR_ERR_ARG), (dict(scale=-1.0), ar.AR_ERR_ARG), (dict(scale=float("nan")), ar.AR_ERR_ARG),
-    (dict(scale=float("inf")), ar.AR_ERR_ARG), (dict(tokens_q=1 << 30), ar.AR_ERR_ARG), (dict(tokens_k=1 << 31), ar.AR_ERR_ARG),
+    (dict(scale=float("inf")), ar.AR_ERR_ARG), (dict(scale=1e-38), ar.AR_ERR_ARG), (dict(scale=1e38), ar.AR_ERR_ARG), (dict(tokens_q=1 << 30), ar.AR_ERR_ARG), (dict(tokens_k=1 << 31), ar.AR_ERR_ARG),
     (dict(sequences=(1 << 20) + 1), ar.AR_ERR_ARG), (dict(tokens_q=(1 << 28) + 1), ar.AR_ERR_ARG), (dict(heads=1 << 17), ar.AR_ERR_ARG), (dict(sq=None), ar.AR_ERR_ARG), (dict(sk=None), ar.AR_ERR_ARG),
     (dict(sq=None, sk=None), ar.AR_ERR_ARG), (dict(sq=SQ + 2), ar.AR_ERR_ARG), (dict(q=None), ar.AR_ERR_ARG), (dict(q=Q + 1), ar.AR_ERR_ARG),
     (dict(v=None), ar.AR_ERR_ARG), (dict(hs_q=63), ar.AR_ERR_ARG), (dict(ld_k=63), ar.AR_ERR_ARG), (dict(ld_k=100), ar.AR_ERR_ARG),

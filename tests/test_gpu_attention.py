@@ -175,6 +175,22 @@ def test_tokens_of_no_sequence(lens):
         assert bool((t[:before] == 7).all()) and bool((t[sq[-1]:] == 7).all())
 
 
+@pytest.mark.parametrize("dim,heads", [(128, 8), (36, 5)])
+def test_much_padding(dim, heads):
+    """Far more padding than tokens, in every result."""
+    say("much padding", dim, heads)
+    sq = [3000, 3050]
+    x = torch.full((9001, heads, dim), math.nan, dtype=torch.bfloat16, device="cuda")
+    x[3000:3050] = draw((50, heads, dim), 51)
+    o, lse = ar.packed_attention(x, x, x, starts_q=on_gpu(sq), save=True)
+    grads = ar.packed_attention_backward(x, x, x, x, o, lse, starts_q=on_gpu(sq))
+    part = x[3000:3050]
+    o2, lse2 = ar.packed_attention(part, part, part, save=True)
+    grads2 = ar.packed_attention_backward(part, part, part, part, o2, lse2)
+    for t, t2 in zip((o, lse.t(), *grads), (o2, lse2.t(), *grads2)):
+        assert torch.equal(t[3000:3050], t2) and not t[:3000].any() and not t[3050:].any()
+
+
 def test_keys_behind_a_sequences_end_do_not_reach_it():
     """The next sequence's infinities and NaN lie in the same tiles."""
     say("neighbours")

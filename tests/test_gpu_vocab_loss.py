@@ -63,6 +63,20 @@ def test_pieces(size):
     check_all(*inputs(*size), device="cuda")
 
 
+def test_statistics_of_some_tokens_at_a_time():
+    """More tokens than the forward pass keeps statistics of at once, whole and as a rank's part."""
+    say("tokens at a time")
+    x, w, target, _ = inputs(36000, 16, 131072, 2)
+    want = oo.vocab_loss(x, w, target, device="cuda")
+    loss, lse = ar.vocab_loss(x, w, target)
+    check(loss, want["loss"], "loss")
+    check(lse, want["lse"], "lse")
+    part = ar.vocab_loss_part(x, w, target, first=0)
+    loss2, lse2 = ar.vocab_loss_join(part[None], target, classes=131072)
+    assert torch.equal(lse2, lse)
+    check(loss2, want["loss"], "loss of parts")
+
+
 @pytest.mark.parametrize("spread", [1e-3, 40.0])
 def test_even_and_certain(spread):
     """From a loss of log(classes) to targets that have all the weight or none."""

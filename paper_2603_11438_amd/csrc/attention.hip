@@ -504,17 +504,16 @@ __global__ __launch_bounds__(256) void attention_delta_kernel(const Heads<const 
 
 // dQ of a tile of rows, over the keys they see: dS^T = P^T * (V dO^T - delta) and
 // dQ^T += K^T dS^T, S^T as in the forward pass.
-template <int DP> __global__ __launch_bounds__(256, 2) void attention_dq_kernel(const AttnArgs a)
+template <int DP> __device__ __forceinline__ void backward_rows(const AttnArgs &a, uint32_t group, char *lds)
 {
     typedef Stage<DP> S;
-    extern __shared__ __attribute__((aligned(16))) char lds[];
     const uint32_t wave = uniform(threadIdx.x >> 6);
     const uint32_t tiles = a.slots * a.kv_heads * a.splits;
-    if (blockIdx.x >= tiles) {
-        clear_rest(a.dq, a.starts_q, a.sequences, a.tokens_q, a.heads, a.dim, blockIdx.x - tiles);
+    if (group >= tiles) {
+        clear_rest(a.dq, a.starts_q, a.sequences, a.tokens_q, a.heads, a.dim, group - tiles);
         return;
     }
-    const uint32_t kv_head = blockIdx.x % a.kv_heads, rest = blockIdx.x / a.kv_heads, split = rest % a.splits;
+    const uint32_t kv_head = group % a.kv_heads, rest = group / a.kv_heads, split = rest % a.splits;
     const Place p = find_place(a, a.slots - 1 - rest / a.splits, false, a.group, kRows);
     if (!p.some) return;
     const Rows r = rows_of(a, p, p.tile * kRows + wave * 32, kv_head);
@@ -590,18 +589,17 @@ template <int DP> __global__ __launch_bounds__(256, 2) void attention_dq_kernel(
 // dK and dV of 128 keys of a key head, 32 for each wave, over the queries that see
 // them, of every head of the group in turn: a lane holds one key.  dV^T += dO^T P and
 // dK^T += Q^T dS with P = e^(Q K^T - lse), dS = P * (dO V^T - delta).
-template <int DP> __global__ __launch_bounds__(256, 1) void attention_dkv_kernel(const AttnArgs a)
+template <int DP> __device__ __forceinline__ void backward_keys(const AttnArgs &a, uint32_t group, char *lds)
 {
     typedef Stage<DP> S;
-    extern __shared__ __attribute__((aligned(16))) char lds[];
     const uint32_t wave = uniform(threadIdx.x >> 6), lane = threadIdx.x & 63u, h = lane >> 5;
     const uint32_t tiles = a.slots * a.kv_heads * a.splits;
-    if (blockIdx.x >= tiles) {
-        clear_rest(a.dk, a.starts_k, a.sequences, a.tokens_k, a.kv_heads, a.dim, blockIdx.x - tiles);
-        clear_rest(a.dv, a.starts_k, a.sequences, a.tokens_k, a.kv_heads, a.dim, blockIdx.x - tiles);
+    if (group >= tiles) {
+        clear_rest(a.dk, a.starts_k, a.sequences, a.tokens_k, a.kv_heads, a.dim, group - tiles);
+        clear_rest(a.dv, a.starts_k, a.sequences, a.tokens_k, a.kv_heads, a.dim, group - tiles);
         return;
     }
-    const uint32_t kv_head = blockIdx.x % a.kv_heads, rest = blockIdx.x / a.kv_heads, split = rest % a.splits;
+    const uint32_t kv_head = group % a.kv_heads, rest = group / a.kv_heads, split = rest % a.splits;
     // the first tiles, which the most queries see, first
     const Place p = find_place(a, rest / a.splits, true, 1, kRows);
     if (!p.some) return;
@@ -775,28 +773,50 @@ template <int DP> __global__ __launch_bounds__(256, 1) void attention_dkv_kernel
     }
 }
 
-// Adds the runs of split gradients, in their order: [split][token][head][dim] of one,
-// then of the other.
-struct RunsOut {
-    Heads<bf16> to[2];
+template <int DP> __global__ __launch_bounds__(256, 2) void attention_dq_kernel(const AttnArgs a)
+{
+    extern __shared__ __attribute__((aligned(16))) char lds[];
+    backward_rows<DP>(a, blockIdx.x, lds);
+}
+template <int DP> __global__ __launch_bounds__(256, 1) void attention_dkv_kernel(const AttnArgs a)
+{
+    extern __shared__ __attribute__((aligned(16))) char lds[];
+    backward_keys<DP>(a, blockIdx.x, lds);
+}
+// Both where neither fills the device by itself: the first `groups` workgroups have the
+// keys' tiles, which take longer.
+template <int DP> __global__ __launch_bounds__(256, 1) void attention_backward_kernel(const AttnArgs keys, const AttnArgs rows, uint32_t groups)
+{
+    extern __shared__ __attribute__((aligned(16))) char lds[];
+    if (blockIdx.x < groups) backward_keys<DP>(keys, blockIdx.x, lds);
+    else backward_rows<DP>(rows, blockIdx.x - groups, lds);
+}
+
+// Adds the runs of split gradients, in their order: [split][token][head][dim].
+struct Runs {
+    Heads<bf16> to;
     const float *part;
     const int32_t *starts;
-    uint32_t sequences, tokens, heads, dim, splits;
+    uint32_t tokens, heads, splits;
 };
-__global__ __launch_bounds__(256) void attention_sum_kernel(const RunsOut o)
+struct RunsList {
+    Runs r[3];
+    uint32_t n, sequences, dim;
+};
+__global__ __launch_bounds__(256) void attention_sum_kernel(const RunsList list)
 {
-    const uint32_t from = start_of(o.starts, 0, o.tokens), until = start_of(o.starts, o.starts ? o.sequences : 1, o.tokens);
-    const uint32_t per = (o.dim + 3) / 4;
-    const uint64_t rows = (uint64_t)o.tokens * o.heads, n = rows * o.dim;
-    const float *part = o.part + blockIdx.y * o.splits * n;
+    const Runs o = list.r[blockIdx.y];
+    const uint32_t from = start_of(o.starts, 0, o.tokens), until = start_of(o.starts, o.starts ? list.sequences : 1, o.tokens);
+    const uint32_t dim = list.dim, per = (dim + 3) / 4;
+    const uint64_t rows = (uint64_t)o.tokens * o.heads, n = rows * dim;
     for (uint64_t i = (uint64_t)blockIdx.x * 256 + threadIdx.x; i < rows * per; i += (uint64_t)gridDim.x * 256) {
         const uint64_t row = i / per;
         const uint32_t token = (uint32_t)(row / o.heads), d = (uint32_t)(i % per) * 4;
         if (token < from || token >= until) continue;
-        bf16 *to = o.to[blockIdx.y].at(token, row % o.heads) + d;
-        const float *at = part + row * o.dim + d;
+        bf16 *to = o.to.at(token, row % o.heads) + d;
+        const float *at = o.part + row * dim + d;
         float v[4] = {0.0f, 0.0f, 0.0f, 0.0f}, w[4];
-        if (d + 4 <= o.dim) {
+        if (d + 4 <= dim) {
 #pragma unroll 8
             for (uint32_t s = 0; s < o.splits; ++s) {
                 load_vec<float, 4>(at + s * n, w);
@@ -805,7 +825,7 @@ __global__ __launch_bounds__(256) void attention_sum_kernel(const RunsOut o)
             }
             store_vec<bf16, 4>(to, v);
         } else {
-            for (uint32_t k = 0; k < o.dim - d; ++k) {
+            for (uint32_t k = 0; k < dim - d; ++k) {
                 for (uint32_t s = 0; s < o.splits; ++s) v[0] += at[s * n + k];
                 to[k] = (bf16)v[0], v[0] = 0.0f;
             }
@@ -1021,28 +1041,30 @@ AttnArgs attn_args(const ar_attention_desc &d, const int32_t *starts_q, const in
     return a;
 }
 
-template <typename K> int launch_tiles(OncePerDevice &once, K kernel, int lds, const AttnArgs &a, hipStream_t st)
+uint32_t groups_of(const AttnArgs &a) { return a.slots * a.kv_heads * a.splits + (a.rest ? kRestGroups : 0); }
+template <typename K, typename... A> int launch_tiles(OncePerDevice &once, K kernel, uint32_t groups, int lds, hipStream_t st, A... args)
 {
     const int rc = allow_lds(once, (const void *)kernel, lds);
     if (rc != AR_OK) return rc;
-    const uint32_t groups = a.slots * a.kv_heads * a.splits + (a.rest ? kRestGroups : 0);
-    hipLaunchKernelGGL(kernel, dim3(groups), dim3(256), lds, st, a);
+    hipLaunchKernelGGL(kernel, dim3(groups), dim3(256), lds, st, args...);
     return launch_status();
 }
 template <int DP> int launch_forward(const AttnArgs &a, hipStream_t st)
 {
     static OncePerDevice once;
-    return launch_tiles(once, attention_kernel<DP>, 4 * Stage<DP>::BYTES, a, st);
+    return launch_tiles(once, attention_kernel<DP>, groups_of(a), 4 * Stage<DP>::BYTES, st, a);
 }
-template <int DP> int launch_dq(const AttnArgs &a, hipStream_t st)
+// keys, rows: null where not wanted
+template <int DP> int launch_backward(const AttnArgs *keys, const AttnArgs *rows, bool together, hipStream_t st)
 {
-    static OncePerDevice once;
-    return launch_tiles(once, attention_dq_kernel<DP>, 4 * Stage<DP>::BYTES, a, st);
-}
-template <int DP> int launch_dkv(const AttnArgs &a, hipStream_t st)
-{
-    static OncePerDevice once;
-    return launch_tiles(once, attention_dkv_kernel<DP>, 4 * Stage<DP>::BYTES + 4 * kKeys * (int)sizeof(float), a, st);
+    constexpr int ROWS_LDS = 4 * Stage<DP>::BYTES, KEYS_LDS = ROWS_LDS + 4 * kKeys * (int)sizeof(float);
+    static OncePerDevice once[3];
+    if (together)
+        return launch_tiles(once[2], attention_backward_kernel<DP>, groups_of(*keys) + groups_of(*rows), KEYS_LDS, st, *keys, *rows, groups_of(*keys));
+    int rc = AR_OK;
+    if (keys) rc = launch_tiles(once[0], attention_dkv_kernel<DP>, groups_of(*keys), KEYS_LDS, st, *keys);
+    if (rows && rc == AR_OK) rc = launch_tiles(once[1], attention_dq_kernel<DP>, groups_of(*rows), ROWS_LDS, st, *rows);
+    return rc;
 }
 
 // What both passes refuse of the inputs.
@@ -1094,16 +1116,24 @@ int attention(const ar_attention_desc *desc, const void *q, const void *k, const
 
 // Where the backward pass keeps what; copies lie behind the rest.
 struct BackwardSpace {
-    size_t part, copies;  // delta lies at the start
+    size_t rows, keys, copies;  // the runs' sums of dq, and of dk and dv; delta lies at the start
 };
 BackwardSpace backward_space(const ar_attention_desc &d, bool dq, bool dkv)
 {
     BackwardSpace s{};
-    s.part = round_up(d.tokens_q * d.heads * sizeof(float), 256);
-    const size_t a = dq ? part_bytes(dq_splits(d), d.tokens_q * d.heads, d.dim) : 0;
-    const size_t b = dkv ? part_bytes(dkv_splits(d), 2 * d.tokens_k * d.kv_heads, d.dim) : 0;
-    s.copies = s.part + (a > b ? a : b);
+    s.rows = round_up(d.tokens_q * d.heads * sizeof(float), 256);
+    s.keys = s.rows + (dq ? part_bytes(dq_splits(d), d.tokens_q * d.heads, d.dim) : 0);
+    s.copies = s.keys + (dkv ? part_bytes(dkv_splits(d), 2 * d.tokens_k * d.kv_heads, d.dim) : 0);
     return s;
+}
+// Whether dq shares a launch with dk and dv: a workgroup has a unit to itself there, which
+// costs dq half of its rate once there are many.  All of a backward pass, in two launches
+// and in one: 1000 tokens, 8 heads of 128 56 and 44 us (160 workgroups), 1000 + 333 queries
+// over 1500 + 77 keys, 12 heads of 64, 57 and 40 (552); but 4 x 1024, 16 heads of 128, 124 and
+// 130 (1024), 2048, 16 heads over 2, 123 and 128 (928).
+bool in_one_launch(const ar_attention_desc &d)
+{
+    return tiles_for(d.tokens_q * (d.heads / d.kv_heads), d) * dq_splits(d) + tiles_for(d.tokens_k, d) * dkv_splits(d) <= 768;
 }
 size_t backward_bytes(const ar_attention_desc &d)
 {
@@ -1112,9 +1142,15 @@ size_t backward_bytes(const ar_attention_desc &d)
     return backward_space(d, true, true).copies + 2 * t.q.copy_bytes() + t.k.copy_bytes() + t.v.copy_bytes();
 }
 
-int sum_runs(const RunsOut &o, uint32_t results, hipStream_t st)
+int sum_runs(const RunsList &list, hipStream_t st)
 {
-    hipLaunchKernelGGL(attention_sum_kernel, dim3(groups_for((uint64_t)o.tokens * o.heads * ((o.dim + 3) / 4)), results), dim3(256), 0, st, o);
+    if (!list.n) return AR_OK;
+    uint64_t most = 0;
+    for (uint32_t k = 0; k < list.n; ++k) {
+        const uint64_t n = (uint64_t)list.r[k].tokens * list.r[k].heads;
+        most = n > most ? n : most;
+    }
+    hipLaunchKernelGGL(attention_sum_kernel, dim3(groups_for(most * ((list.dim + 3) / 4)), list.n), dim3(256), 0, st, list);
     return launch_status();
 }
 
@@ -1158,30 +1194,35 @@ int attention_backward(const ar_attention_desc *desc, const void *dout, const vo
     copies.dim = a.dim;
     a.q = readable(t.q, at, &copies), a.k = readable(t.k, at, &copies), a.v = readable(t.v, at, &copies), a.dout = readable(g, at, &copies);
     if ((rc = run_copies(copies, st)) != AR_OK) return rc;
-    a.lse = (float *)lse, a.delta = (float *)ws, a.part = (float *)((char *)ws + s.part);
+    a.lse = (float *)lse, a.delta = (float *)ws;
     if (d.tokens_q) {
         const uint64_t rows = (uint64_t)d.tokens_q * d.heads;
         hipLaunchKernelGGL(attention_delta_kernel, dim3(groups_for(rows * 16)), dim3(256), 0, st, heads_of<const bf16>(g),
                            heads_of<const bf16>(t.o), (float *)ws, rows, a.tokens_q, a.dim);
         if ((rc = launch_status()) != AR_OK) return rc;
     }
-    if (dk && d.tokens_k) {
-        a.dk = heads_of<bf16>(out[1]), a.dv = heads_of<bf16>(out[2]);
-        a.slots = (uint32_t)key_slots(d), a.splits = dkv_splits(d);
-        if ((rc = d.dim <= 64 ? launch_dkv<64>(a, st) : launch_dkv<128>(a, st)) != AR_OK) return rc;
-        if (a.splits > 1) {
-            const RunsOut o{{a.dk, a.dv}, a.part, starts_k, a.sequences, a.tokens_k, a.kv_heads, a.dim, a.splits};
-            if ((rc = sum_runs(o, 2, st)) != AR_OK) return rc;
+    const bool with_keys = dk && d.tokens_k, with_rows = dq && d.tokens_q;
+    AttnArgs keys = a, rows = a;
+    RunsList runs{};
+    runs.sequences = a.sequences, runs.dim = a.dim;
+    if (with_keys) {
+        keys.dk = heads_of<bf16>(out[1]), keys.dv = heads_of<bf16>(out[2]);
+        keys.slots = (uint32_t)key_slots(d), keys.splits = dkv_splits(d), keys.part = (float *)((char *)ws + s.keys);
+        if (keys.splits > 1) {
+            const uint64_t half = (uint64_t)keys.splits * d.tokens_k * d.kv_heads * d.dim;
+            runs.r[runs.n++] = {keys.dk, keys.part, starts_k, a.tokens_k, a.kv_heads, keys.splits};
+            runs.r[runs.n++] = {keys.dv, keys.part + half, starts_k, a.tokens_k, a.kv_heads, keys.splits};
         }
     }
-    if (dq && d.tokens_q) {
-        a.dq = heads_of<bf16>(out[0]);
-        a.slots = (uint32_t)row_slots(d), a.splits = dq_splits(d);
-        if ((rc = d.dim <= 64 ? launch_dq<64>(a, st) : launch_dq<128>(a, st)) != AR_OK) return rc;
-        const RunsOut o{{a.dq, a.dq}, a.part, starts_q, a.sequences, a.tokens_q, a.heads, a.dim, a.splits};
-        if (a.splits > 1 && (rc = sum_runs(o, 1, st)) != AR_OK) return rc;
+    if (with_rows) {
+        rows.dq = heads_of<bf16>(out[0]);
+        rows.slots = (uint32_t)row_slots(d), rows.splits = dq_splits(d), rows.part = (float *)((char *)ws + s.rows);
+        if (rows.splits > 1) runs.r[runs.n++] = {rows.dq, rows.part, starts_q, a.tokens_q, a.heads, rows.splits};
     }
-    return AR_OK;
+    const bool together = with_keys && with_rows && in_one_launch(d);
+    rc = d.dim <= 64 ? launch_backward<64>(with_keys ? &keys : nullptr, with_rows ? &rows : nullptr, together, st)
+                     : launch_backward<128>(with_keys ? &keys : nullptr, with_rows ? &rows : nullptr, together, st);
+    return rc != AR_OK ? rc : sum_runs(runs, st);
 }
 
 }  // namespace

@@ -614,7 +614,7 @@ template <int DP> __device__ __forceinline__ void backward_keys(const AttnArgs &
     const uint32_t begin = (uint32_t)(all * split / a.splits), end = (uint32_t)(all * (split + 1) / a.splits);
 
     const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)lds;
-    float *stats = (float *)(lds + 4 * S::BYTES);  // of a buffer's queries: lse, delta
+    float *stats = (float *)(lds + 4 * S::BYTES);  // of a buffer's queries: lse, -delta
     S qs, gs;
     Reads<DP> at;
     at.place(lds0);
@@ -646,7 +646,7 @@ template <int DP> __device__ __forceinline__ void backward_keys(const AttnArgs &
         }
     };
     auto keep = [&](uint32_t buf) {
-        const float kept = is_delta ? ahead : ahead == -INFINITY ? INFINITY : ahead * kLog2e;
+        const float kept = is_delta ? -ahead : ahead == -INFINITY ? INFINITY : ahead * kLog2e;
         if (threadIdx.x < 2 * kKeys) stats[buf * 2 * kKeys + threadIdx.x] = kept;
     };
     bf16x8 kf[DP / 16], vf[DP / 16];
@@ -673,41 +673,41 @@ template <int DP> __device__ __forceinline__ void backward_keys(const AttnArgs &
         if (here + kKeys > wave_from) {
             const float *st = stats + buffer.value * 2 * kKeys;
             // Each block of 32 queries in four parts, whose products have the matrix unit while
-            // the part's vector operations go on: S; dO V^T and P; dV and dS; dK.  The first
-            // fragments of each part are read in the one before.
+            // the part's vector operations go on: S; dO V^T - delta, and P; dV and dS; dK.  A
+            // part's fragments are read in the one before: it waits once, and not before each
+            // product.  (A wave that has a SIMD to itself issues an instruction in about 7
+            // cycles, waits among them, and a product takes 32.)
             constexpr int N = DP / 16;  // products of a part
-            bf16x8 first_rows[4], first_columns[4];
-            auto row_of = [&](int b, int d, int at_stage) { return d < 4 ? first_rows[d] : at.rows(b, d, at_stage); };
-            auto columns_of = [&](int b, int n, int at_stage) {
-                return n < 4 ? first_columns[n] : at.columns(n % (DP / 32), b * 2 + n / (DP / 32), at_stage);
+            typedef float f32x4 __attribute__((ext_vector_type(4)));
+            bf16x8 f[N], g[N];
+            f32x4 lse[4], delta[4];
+            auto read_rows = [&](bf16x8 (&to)[N], int b, int at_stage) {
+#pragma unroll
+                for (int d = 0; d < N; ++d) to[d] = at.rows(b, d, at_stage);
             };
-            auto read_rows = [&](int b, int at_stage) {
-#pragma unroll
-                for (int d = 0; d < 4; ++d) first_rows[d] = at.rows(b, d, at_stage);
-            };
-            auto read_columns = [&](int b, int at_stage) {
-#pragma unroll
-                for (int n = 0; n < 4; ++n) first_columns[n] = at.columns(n % (DP / 32), b * 2 + n / (DP / 32), at_stage);
-            };
-            read_rows(0, Q);
-#pragma unroll
-            for (int b = 0; b < 2; ++b) {
-                typedef float f32x4 __attribute__((ext_vector_type(4)));
-                f32x16 s{}, dp{};
-                bf16x8 f[N];
-                __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-                for (int d = 0; d < N; ++d) f[d] = row_of(b, d, Q);
-                read_rows(b, G);
-#pragma unroll
-                for (int d = 0; d < N; ++d) s = Frag<bf16>::mfma(f[d], kf[d], s);
-                f32x4 lse[4], delta[4];
+            auto columns = [&](int b, int n, int at_stage) { return at.columns(n % (DP / 32), b * 2 + n / (DP / 32), at_stage); };
+            auto read_stats = [&](int b) {
 #pragma unroll
                 for (int k = 0; k < 4; ++k) {
                     lse[k] = *(const f32x4 *)(st + b * 32 + 8 * k + 4 * h);
                     delta[k] = *(const f32x4 *)(st + kKeys + b * 32 + 8 * k + 4 * h);
                 }
-                interleave<N, 2, 0, 0>();
+            };
+            auto part = []() {
+                __builtin_amdgcn_sched_barrier(0);
+                __builtin_amdgcn_s_waitcnt(0xc07f);  // lgkmcnt(0) alone
+                __builtin_amdgcn_sched_barrier(0);
+            };
+            read_rows(f, 0, Q);
+            read_stats(0);
+#pragma unroll
+            for (int b = 0; b < 2; ++b) {
+                f32x16 s{}, dp;
+                part();
+                read_rows(g, b, G);
+#pragma unroll
+                for (int d = 0; d < N; ++d) s = Frag<bf16>::mfma(f[d], kf[d], s);
+                interleave<N, 1, 0, 0>();
                 here_now(s);
                 __builtin_amdgcn_sched_barrier(0);
                 if (here + b * 32 < wave_needs) {
@@ -715,42 +715,38 @@ template <int DP> __device__ __forceinline__ void backward_keys(const AttnArgs &
 #pragma unroll
                     for (int k = 0; k < 16; ++k) s[k] = 8 * (k / 4) + k % 4 >= hidden ? s[k] : -INFINITY;
                 }
-                __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-                for (int d = 0; d < N; ++d) f[d] = row_of(b, d, G);
-                read_columns(b, G);
+                part();
                 here_now(s);
 #pragma unroll
+                for (int k = 0; k < 16; ++k) dp[k] = delta[k / 4][k % 4];
+#pragma unroll
                 for (int d = 0; d < N; ++d) {
-                    dp = Frag<bf16>::mfma(f[d], vf[d], dp);
+                    dp = Frag<bf16>::mfma(g[d], vf[d], dp);
                     here_now(dp);
+                    f[d] = columns(b, d, G);
 #pragma unroll
                     for (int k = 0; k < 16 / N; ++k) {
                         const int n = d * (16 / N) + k;
                         s[n] = __builtin_amdgcn_exp2f(s[n] * c - lse[n / 4][n % 4]);
                     }
-                    here_now(s);
+                    __builtin_amdgcn_sched_barrier(0);
                 }
-                __builtin_amdgcn_sched_barrier(0);
                 const bf16x8 w[2] = {rounded(s, 0), rounded(s, 8)};
-#pragma unroll
-                for (int n = 0; n < N; ++n) f[n] = columns_of(b, n, G);
-                read_columns(b, Q);
+                part();
 #pragma unroll
                 for (int n = 0; n < N; ++n) {
                     dv[n % (DP / 32)] = Frag<bf16>::mfma(f[n], w[n / (DP / 32)], dv[n % (DP / 32)]);
                     here_now(dv[n % (DP / 32)]);
+                    g[n] = columns(b, n, Q);
 #pragma unroll
-                    for (int k = n * (16 / N); k < (n + 1) * (16 / N); ++k) dp[k] = s[k] * (dp[k] - delta[k / 4][k % 4]);
-                    here_now(dp);
+                    for (int k = n * (16 / N); k < (n + 1) * (16 / N); ++k) dp[k] *= s[k];
+                    __builtin_amdgcn_sched_barrier(0);
                 }
                 const bf16x8 u[2] = {rounded(dp, 0), rounded(dp, 8)};
-                __builtin_amdgcn_sched_barrier(0);
+                part();
+                if (b == 0) read_rows(f, 1, Q), read_stats(1);
 #pragma unroll
-                for (int n = 0; n < N; ++n) f[n] = columns_of(b, n, Q);
-                if (b == 0) read_rows(1, Q);
-#pragma unroll
-                for (int n = 0; n < N; ++n) dk[n % (DP / 32)] = Frag<bf16>::mfma(f[n], u[n / (DP / 32)], dk[n % (DP / 32)]);
+                for (int n = 0; n < N; ++n) dk[n % (DP / 32)] = Frag<bf16>::mfma(g[n], u[n / (DP / 32)], dk[n % (DP / 32)]);
                 interleave<N, 2, 0, 0>();
                 __builtin_amdgcn_sched_barrier(0);
             }

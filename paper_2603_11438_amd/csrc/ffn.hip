@@ -4,7 +4,7 @@
 // Compute-bound with many tokens: one product kernel (gemm_nt.h) whose waves
 // hold both projections of the same columns, so that the activation and the
 // product happen in registers and only h is written.  8192 x 4096 x 11264, silu:
-// 1230 us, 1230 TFLOP/s.  Bound by the weights' bytes with few: up to 64 tokens
+// 1200 us, 1260 TFLOP/s.  Bound by the weights' bytes with few: up to 64 tokens
 // share a tile of 64 columns of both, 1 x 4096 x 11264: 41 us, 4.5 TB/s.  Bound by the
 // length of k where there are few tiles, as in a rank's share of the columns: there
 // k is split, and a second kernel joins the runs and applies the activation (1 x
@@ -13,7 +13,7 @@
 // Backward: dG and dU by one pass over the saved projections (4096 x 11264: 128
 // us, 5.0 TB/s), dx as one product over both pairs of operands, both weights'
 // gradients as another, operands read by rows or by k where they lie.  Forward
-// with saved projections and backward, 4096 x 4096 x 11264: 2080 us, 1090
+// with saved projections and backward, 4096 x 4096 x 11264: 2060 us, 1100
 // TFLOP/s; a third of that the forward, a third the weights' gradients, 28 % dx.
 #include <type_traits>
 

@@ -27,10 +27,12 @@
 // chunks are rotated by 4 (k & 3) (64 columns: by 4 (k >> 1 & 1)): a transposing
 // read takes 64 bytes of each of four rows.
 //
-// Rate, bf16, 8192 x 8192 x 8192: 856 us, 1284 TFLOP/s with the 256 x 256 tile,
-// at 1.75 GHz: the board's power limit has the clock.  With every load an L2 hit
-// the same kernel takes 794 us, so the rest is misses that a stage's lead does
-// not cover.  Smaller tiles: 128 x 128 1020 us, 64 x 64 1525 us.
+// Rate, bf16, 8192 x 8192 x 8192: 856 us, 1284 TFLOP/s with the 256 x 256 tile and two
+// buffers, at 1.75 GHz: the board's power limit has the clock.  With every load an L2
+// hit the same kernel takes 794 us, so the rest is misses that a stage's lead does
+// not cover.  A third buffer for A (AHEAD) makes the waits 15 % of the cycles, from 25,
+// and the clock lower: 2 to 3 % less time (4096 x 4096 x 131072: 3540 us, from 3630).
+// Smaller tiles: 128 x 128 1020 us, 64 x 64 1525 us.
 #pragma once
 
 #include <type_traits>
@@ -175,13 +177,16 @@ constexpr int upto(int k, int steps, int things, int most)
 }
 
 // The shape of a workgroup's tile and pipeline: WM x 2 waves of MT x NT blocks of
-// 32 x 32, PLANES planes of each operand, k in stages of BK through BUFS buffers.
-template <int MT_, int NT_, int PLANES_, int BK_, int BUFS_, int WM_ = 2> struct Shape {
+// 32 x 32, PLANES planes of each operand, k in stages of BK through BUFS buffers, or
+// with AHEAD through one more for A.
+template <int MT_, int NT_, int PLANES_, int BK_, int BUFS_, int WM_ = 2, bool AHEAD_ = false> struct Shape {
     static constexpr int MT = MT_, NT = NT_, PLANES = PLANES_, BK = BK_, BUFS = BUFS_;
+    static constexpr bool AHEAD = AHEAD_;
     static constexpr int WM = WM_, WN = 2, WAVES = WM * WN, THREADS = 64 * WAVES, BM = WM * MT * 32, BN = WN * NT * 32;
     static constexpr int ROW = BK * 2;                        // bytes of a row in a buffer
     static constexpr int PLANE = (BM + BN) * ROW;             // A's rows, then B's
-    static constexpr int BUF = PLANES * PLANE, LDS = BUFS * BUF;
+    static constexpr int BUF = PLANES * PLANE, LDS = BUFS * BUF + (AHEAD ? BM * ROW : 0);
+    static_assert(!AHEAD || (PLANES == 1 && BUFS == 2 && LDS <= 160 * 1024), "one plane, and room for it");
     static_assert(BM * ROW % (1024 * WAVES) == 0 && BN * ROW % (1024 * WAVES) == 0, "whole loads");
 };
 
@@ -270,8 +275,8 @@ __device__ __forceinline__ uint64_t uniform_address(const void *p)
 //
 // With k split, a workgroup adds up run at.split of g.splits of the stages
 // (never empty: there are at least as many steps as splits).
-template <typename T, typename S, bool PAIRED, bool ABYK = false, bool BBYK = false>
-__device__ __forceinline__ void gemm_tile(const GemmArgs &g, const TileAt at, char *lds, f32x16 (&acc)[S::MT][S::NT])
+template <typename T, typename S, bool PAIRED, bool ABYK, bool BBYK>
+__device__ __forceinline__ void gemm_tile_even(const GemmArgs &g, const TileAt at, char *lds, f32x16 (&acc)[S::MT][S::NT])
 {
     constexpr int MT = S::MT, NT = S::NT, PLANES = S::PLANES, KQ = S::BK / 16, BUFS = S::BUFS;
     typedef Side<S, ABYK, S::BM> SideA;
@@ -464,6 +469,195 @@ __device__ __forceinline__ void gemm_tile(const GemmArgs &g, const TileAt at, ch
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     __syncthreads();
     settle(acc);
+}
+
+// The same with a third buffer for A: what a stage needs of B is loaded in the first half
+// of the one before, and of A in the second half of the one before that, so that the last
+// loads that a barrier waits for are half a stage old, not a quarter.  (Two buffers of both
+// are 128 KiB of a compute unit's 160 with the 256 x 256 tile: three of both do not fit.)
+template <typename T, typename S, bool PAIRED, bool ABYK, bool BBYK>
+__device__ __forceinline__ void gemm_tile_ahead(const GemmArgs &g, const TileAt at, char *lds, f32x16 (&acc)[S::MT][S::NT])
+{
+    constexpr int MT = S::MT, NT = S::NT, KQ = S::BK / 16;
+    typedef Side<S, ABYK, S::BM> SideA;
+    typedef Side<S, BBYK, S::BN> SideB;
+    constexpr int LOADS_A = SideA::LOADS, LOADS_B = SideB::LOADS, LOADS = LOADS_A + LOADS_B;
+    static_assert(!PAIRED || !BBYK, "pairs lie by rows");
+    constexpr uint32_t A_BYTES = S::BM * S::ROW, B_BYTES = S::BN * S::ROW, B_AT = 3 * A_BYTES;
+    typedef typename Frag<T>::type F;
+    const uint32_t lane = threadIdx.x & 63u, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const uint32_t wm = wave / S::WN, wn = wave % S::WN;
+    const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)lds;
+    const uint32_t m0 = at.m * S::BM, n0 = at.n * (PAIRED ? S::BN / 2 : S::BN);
+    constexpr int HALF = NT * 16;  // paired: columns of a wave
+
+    const uint32_t per = g.steps * (kStepK / S::BK), all = g.segments * per;
+    const uint32_t begin = (uint32_t)((uint64_t)all * at.split / g.splits);
+    const uint32_t total = (uint32_t)((uint64_t)all * (at.split + 1) / g.splits) - begin;
+
+    // where an operand's next loads are, and where in LDS they go
+    struct Next {
+        uint32_t segment, step, loaded, kbyte, slot, put;
+        u32x4v from;
+    };
+    SideA sa;
+    SideB sb;
+    Next na{begin / per, begin % per, 0, begin % per * S::ROW, 0, lds0 + wave * 1024}, nb = na;
+    nb.put += B_AT;
+    u32x4v rb2;
+    auto place_a = [&]() {
+        sa.place(wave, m0, g.m, [&](uint32_t row, uint32_t first) {
+            return ABYK ? row * g.lda : ((first + row < g.m ? first + row : g.m - 1) - first) * g.lda;
+        });
+        sa.base = uniform_address((const char *)g.a[na.segment] + at.batch * g.batch_a +
+                                  (ABYK ? (uint64_t)na.step * S::BK * g.lda + m0 * 2 : (uint64_t)m0 * g.lda));
+    };
+    auto place_b = [&]() {
+        sb.place(wave, n0, g.n, [&](uint32_t row, uint32_t first) {
+            if (BBYK) return row * g.ldb;
+            uint32_t ld = g.ldb, r = row;
+            if (PAIRED) {
+                const uint32_t in = row % (2 * HALF);
+                ld = in < HALF ? g.ldb : g.ldb2;
+                r = row / (2 * HALF) * HALF + in % HALF;
+            }
+            return ((first + r < g.n ? first + r : g.n - 1) - first) * ld;
+        });
+        sb.base = uniform_address((const char *)g.b[nb.segment] + at.batch * g.batch_b +
+                                  (BBYK ? (uint64_t)nb.step * S::BK * g.ldb + n0 * 2 : (uint64_t)n0 * g.ldb));
+    };
+    auto ready_a = [&]() {
+        na.from = tile_resource(sa.base);
+        if ((na.step + 1) * S::BK > g.ka) sa.stop_at(wave, (int)g.ka - (int)(na.step * S::BK));
+    };
+    auto ready_b = [&]() {
+        nb.from = tile_resource(sb.base);
+        if ((nb.step + 1) * S::BK > g.kb) sb.stop_at(wave, (int)g.kb - (int)(nb.step * S::BK));
+    };
+    place_a(), place_b(), ready_a(), ready_b();
+    if (PAIRED) rb2 = tile_resource(uniform_address((const char *)g.b2 + (uint64_t)n0 * g.ldb2));
+    // Past the last stage the loads go on, into buffers that are not read again, so that
+    // one constant count says which have landed.
+    auto next_a = [&]() {
+        na.slot = na.slot == 2 ? 0 : na.slot + 1;
+        na.put = lds0 + na.slot * A_BYTES + wave * 1024;
+        if (++na.loaded >= total) return;
+        na.kbyte += S::ROW;
+        if (++na.step == per) na.step = 0, na.kbyte = 0, ++na.segment, place_a();
+        else if (ABYK) sa.base += (uint64_t)S::BK * g.lda;
+        ready_a();
+    };
+    auto next_b = [&]() {
+        nb.slot ^= 1;
+        nb.put = lds0 + B_AT + nb.slot * B_BYTES + wave * 1024;
+        if (++nb.loaded >= total) return;
+        nb.kbyte += S::ROW;
+        if (++nb.step == per) nb.step = 0, nb.kbyte = 0, ++nb.segment, place_b();
+        else if (BBYK) sb.base += (uint64_t)S::BK * g.ldb;
+        ready_b();
+    };
+    auto load_a = [&](int i) { load_to_lds(na.put + i * S::WAVES * 1024, sa.off[i], na.from, ABYK ? 0u : na.kbyte); };
+    auto load_b = [&](int k) {
+        // a load of the four waves covers 32 rows (or 64): all of one half
+        static_assert(!PAIRED || HALF % (S::WAVES * 1024 / S::ROW) == 0, "loads do not straddle halves");
+        const bool second = PAIRED && k * S::WAVES * (1024 / S::ROW) % (2 * HALF) >= HALF;
+        load_to_lds(nb.put + k * S::WAVES * 1024, sb.off[k], second ? rb2 : nb.from, BBYK ? 0u : nb.kbyte);
+    };
+    auto load_one = [&](int n) {  // B's, then A's
+        if (n < LOADS_B) load_b(n);
+        else load_a(n - LOADS_B);
+    };
+
+    // Fragments, as above.
+    const uint32_t fr = lane & 31u, fc = lane >> 5;
+    const uint32_t rows_a = (wm * MT * 32 + fr) * S::ROW, rows_b = B_AT + (wn * NT * 32 + fr) * S::ROW;
+    const uint32_t tk = 8 * fc + (lane & 15u) / 4, tc = 2 * (lane >> 4 & 1u) + (lane >> 1 & 1u), te = (lane & 1u) * 8;
+    uint32_t cols_a[MT], cols_b[NT];
+    if (ABYK)
+#pragma unroll
+        for (int i = 0; i < MT; ++i)
+            cols_a[i] = tk * (S::BM * 2) + ((wm * MT + i) * 4 + tc + SideA::turn(tk)) % SideA::CHUNKS * 16 + te;
+    if (BBYK)
+#pragma unroll
+        for (int j = 0; j < NT; ++j)
+            cols_b[j] = B_AT + tk * (S::BN * 2) + ((wn * NT + j) * 4 + tc + SideB::turn(tk)) % SideB::CHUNKS * 16 + te;
+    auto transposed = [&](uint32_t at_byte, uint32_t pitch) {
+        typedef short s16x4 __attribute__((ext_vector_type(4)));
+        typedef __attribute__((address_space(3))) s16x4 *P;
+        const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((P)(uintptr_t)(lds0 + at_byte));
+        const s16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((P)(uintptr_t)(lds0 + at_byte + 4 * pitch));
+        return __builtin_bit_cast(F, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
+    };
+    constexpr int READS = MT + NT;
+    F fa[2][MT], fb[2][NT];
+    auto read_one = [&](uint32_t at_a, uint32_t at_b, int quarter, int to, int n) {
+        if (n < MT) {
+            if (ABYK) fa[to][n] = transposed(at_a + quarter * 16 * (S::BM * 2) + cols_a[n], S::BM * 2);
+            else fa[to][n] = *(const F *)(lds + at_a + rows_a + n * 32 * S::ROW + ((2 * quarter + fc) ^ SideA::swizzle(fr)) * 16);
+        } else {
+            const int j = n - MT;
+            if (BBYK) fb[to][j] = transposed(at_b + quarter * 16 * (S::BN * 2) + cols_b[j], S::BN * 2);
+            else fb[to][j] = *(const F *)(lds + at_b + rows_b + j * 32 * S::ROW + ((2 * quarter + fc) ^ SideB::swizzle(fr)) * 16);
+        }
+    };
+
+#pragma unroll
+    for (int i = 0; i < MT; ++i)
+#pragma unroll
+        for (int j = 0; j < NT; ++j)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.0f;
+
+    constexpr int PER_Q = (LOADS + KQ - 1) / KQ;
+    static_for<LOADS_A>([&](auto i) { load_a(i.value); });
+    static_for<LOADS_B>([&](auto i) { load_b(i.value); });
+    next_a(), next_b();
+    static_for<LOADS_A>([&](auto i) { load_a(i.value); });
+    next_a();
+    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(LOADS_A) : "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+    static_for<READS>([&](auto i) { read_one(0, 0, 0, 0, i.value); });
+    static_for<PER_Q>([&](auto i) { load_one(i.value); });
+    uint32_t buf_a = 0, buf_b = 0;
+    for (uint32_t t = 0; t < total; ++t) {
+        const uint32_t then_a = buf_a == 2 * A_BYTES ? 0 : buf_a + A_BYTES, then_b = B_BYTES - buf_b;
+        static_for<KQ>([&](auto quarter) {
+            constexpr int q = quarter.value, from = q & 1, to = from ^ 1;
+            constexpr bool last = q == KQ - 1;
+            if (last && t + 1 < total) {
+                // This wave has its last fragments of the buffers, and its loads of the
+                // next stage have landed, A's behind them not; past the barrier that holds
+                // for every wave.
+                asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(LOADS_A) : "memory");
+                __builtin_amdgcn_s_barrier();
+                asm volatile("" ::: "memory");
+                next_a(), next_b();
+            }
+            constexpr int PRODUCTS = MT * NT, FIRST = (q + 1) % KQ * PER_Q;
+            constexpr int HERE = FIRST >= LOADS ? 0 : LOADS - FIRST < PER_Q ? LOADS - FIRST : PER_Q;
+            static_for<PRODUCTS>([&](auto product) {
+                constexpr int k = product.value, r0 = upto(k, PRODUCTS, 2 * READS, READS), r1 = upto(k + 1, PRODUCTS, 2 * READS, READS);
+                constexpr int l0 = upto(k, PRODUCTS, HERE, HERE), l1 = upto(k + 1, PRODUCTS, HERE, HERE);
+                static_for<r1 - r0>([&](auto n) { read_one(last ? then_a : buf_a, last ? then_b : buf_b, last ? 0 : q + 1, to, r0 + n.value); });
+                static_for<l1 - l0>([&](auto n) { load_one(FIRST + l0 + n.value); });
+                __builtin_amdgcn_sched_barrier(0);
+                acc[k / NT][k % NT] = Frag<T>::mfma(fb[from][k % NT], fa[from][k / NT], acc[k / NT][k % NT]);
+                __builtin_amdgcn_sched_barrier(0);
+            });
+        });
+        buf_a = then_a, buf_b = then_b;
+    }
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+    settle(acc);
+}
+
+template <typename T, typename S, bool PAIRED, bool ABYK = false, bool BBYK = false>
+__device__ __forceinline__ void gemm_tile(const GemmArgs &g, const TileAt at, char *lds, f32x16 (&acc)[S::MT][S::NT])
+{
+    if constexpr (S::AHEAD) gemm_tile_ahead<T, S, PAIRED, ABYK, BBYK>(g, at, lds, acc);
+    else gemm_tile_even<T, S, PAIRED, ABYK, BBYK>(g, at, lds, acc);
 }
 
 // 32 rows of a wave's results in its own part of LDS, so that a row's bytes can

@@ -6,6 +6,11 @@
 // kernel joins these.  Backward: the logits again, a piece of the vocabulary at a time,
 // made into dz in registers and kept as bf16; then dx += dz W and dW = dz^T x of the
 // piece as products of operands that are read where they lie.
+//
+// Bound by the products, and those by the board's power: 4096 tokens of 4096, 131072
+// classes, forward 3540 us (1240 TFLOP/s), with gradients 14.5 ms (1210 TFLOP/s of what is
+// done, the logits twice).  A few tokens by the weights' bytes: one of 4096, 131072
+// classes, 200 us, 5.3 TB/s; 32768 classes 64 us, 4.2 TB/s.
 #include "products.h"
 
 #pragma clang fp contract(fast)

@@ -453,6 +453,180 @@ template <int DP> __global__ __launch_bounds__(256, 2) void attention_kernel(con
     }
 }
 
+// The forward pass where there are few rows, single tokens in a serving loop or a short
+// prompt: bound by the bytes of K and V, and by latency where those are few.  A tile has 32 rows, and each
+// wave of the workgroup every fourth block of 32 keys, which it loads into a part of LDS
+// of its own and waits for alone; at the end the waves' sums are joined through LDS.  By
+// tiles of 128 rows and so, 32 heads over 8 of 128: 1 query of 16000 keys 37 and 30 us, 32 of
+// 160 to 15000 210 and 195 us; 48 of 300, 8 heads over 1, 13.5 and 10.3 us.  A block takes
+// 0.9 us, the time of its loads, which are one block ahead: more do not fit the LDS.
+constexpr int kFewRows = 32;
+template <int DP> struct Few {
+    static constexpr int BLOCK = 32 * DP * 2, DEPTH = DP == 128 ? 2 : 4;  // bytes of a block of K or V; blocks of a wave
+    static constexpr int WAVE = 2 * DEPTH * BLOCK, LDS = 4 * WAVE;
+    static constexpr int LOADS = BLOCK / 1024;
+    static_assert(4 * (DP + 2) * 32 * (int)sizeof(float) <= LDS, "the waves' sums fit");
+};
+template <int DP> __global__ __launch_bounds__(256, 1) void attention_few_kernel(const AttnArgs a)
+{
+    typedef Few<DP> F;
+    typedef Stage<DP> S;
+    extern __shared__ __attribute__((aligned(16))) char lds[];
+    const uint32_t wave = uniform(threadIdx.x >> 6), lane = threadIdx.x & 63u, h = lane >> 5;
+    const uint32_t tiles = a.slots * a.kv_heads * a.splits;
+    if (blockIdx.x >= tiles) {
+        clear_rest(a.o, a.starts_q, a.sequences, a.tokens_q, a.heads, a.dim, blockIdx.x - tiles);
+        if (a.lse) clear_rest(Heads<float>{a.lse, 1, a.tokens_q}, a.starts_q, a.sequences, a.tokens_q, a.heads, 1, blockIdx.x - tiles);
+        return;
+    }
+    const uint32_t kv_head = blockIdx.x % a.kv_heads, rest = blockIdx.x / a.kv_heads, split = rest % a.splits;
+    const Place p = find_place(a, a.slots - 1 - rest / a.splits, false, a.group, kFewRows);
+    if (!p.some) return;
+    const Rows r = rows_of(a, p, p.tile * kFewRows, kv_head);
+    const uint32_t blocks = (r.most + 31) / 32;
+    const uint32_t begin = (uint32_t)((uint64_t)blocks * split / a.splits), end = (uint32_t)((uint64_t)blocks * (split + 1) / a.splits);
+
+    // this wave's loads: 1 KiB each, of K and then of V
+    const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)lds + wave * F::WAVE;
+    uint32_t off_k[F::LOADS], off_v[F::LOADS];
+#pragma unroll
+    for (int i = 0; i < F::LOADS; ++i) {
+        const uint32_t n = i * 64 + lane, row = n / S::CHUNKS, c = (n % S::CHUNKS) ^ S::turn(row);
+        off_k[i] = c * 8 < a.dim_in ? row * (uint32_t)a.k.ld * 2 + c * 16 : kOutOfRange;
+        off_v[i] = c * 8 < a.dim_in ? row * (uint32_t)a.v.ld * 2 + c * 16 : kOutOfRange;
+    }
+    uint64_t next_k = uniform_address(a.k.at(p.k0 + (begin + wave) * 32, kv_head)), next_v = uniform_address(a.v.at(p.k0 + (begin + wave) * 32, kv_head));
+    auto load = [&](uint32_t n, uint32_t slot) {
+        const uint32_t to = lds0 + slot * 2 * F::BLOCK, left = p.lk - n * 32;
+        const u32x4v from_k = tile_resource(next_k), from_v = tile_resource(next_v);
+        next_k += 4 * 32 * a.k.ld * 2, next_v += 4 * 32 * a.v.ld * 2;
+#pragma unroll
+        for (int i = 0; i < F::LOADS; ++i) load_to_lds(to + i * 1024, (i * 64 + lane) / S::CHUNKS < left ? off_k[i] : kOutOfRange, from_k, 0u);
+#pragma unroll
+        for (int i = 0; i < F::LOADS; ++i)
+            load_to_lds(to + F::BLOCK + i * 1024, (i * 64 + lane) / S::CHUNKS < left ? off_v[i] : kOutOfRange, from_v, 0u);
+    };
+    Reads<DP> at;
+    at.place(lds0);
+    bf16x8 q[DP / 16];
+    load_row<DP>(a.q.at(p.q0 + r.query, r.head), a.dim_in, q);
+    f32x16 o[DP / 32];
+#pragma unroll
+    for (int b = 0; b < DP / 32; ++b) o[b] = f32x16{};
+    const float c = a.scale * kLog2e;
+    float top = -INFINITY, part[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+
+    auto block = [&](uint32_t n, auto slot) {
+        constexpr int K = slot.value * 2 * F::BLOCK, V = K + F::BLOCK;
+        f32x16 s{};
+#pragma unroll
+        for (int d = 0; d < DP / 16; ++d) s = Frag<bf16>::mfma(at.rows(0, d, K), q[d], s);
+        if (n * 32 + 32 > r.least) {
+            const int32_t left = (int32_t)(r.limit - n * 32 - 4 * h);
+#pragma unroll
+            for (int k = 0; k < 16; ++k) s[k] = 8 * (k / 4) + k % 4 < left ? s[k] : -INFINITY;
+        }
+        float m = s[0];
+#pragma unroll
+        for (int k = 1; k < 16; ++k) m = __builtin_elementwise_maximum(m, s[k]);
+        const Halves both = halves(m);
+        m = __builtin_elementwise_maximum(both.a, both.b);
+        const bool rises = m * c > top * c + kSlack;
+        if (__any(rises)) {
+            const float next = rises ? m : top, to = next == -INFINITY ? 0.0f : next;
+            const float by = __builtin_amdgcn_exp2f((top - to) * c);
+            top = next;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) part[k] *= by;
+#pragma unroll
+            for (int b = 0; b < DP / 32; ++b)
+#pragma unroll
+                for (int k = 0; k < 16; ++k) o[b][k] *= by;
+        }
+        const float base = top == -INFINITY ? 0.0f : top * c;
+#pragma unroll
+        for (int k = 0; k < 16; ++k) s[k] = __builtin_amdgcn_exp2f(s[k] * c - base), part[k & 3] += s[k];
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            const bf16x8 w = rounded(s, k * 8);
+#pragma unroll
+            for (int d = 0; d < DP / 32; ++d) o[d] = Frag<bf16>::mfma(at.columns(d, k, V), w, o[d]);
+        }
+    };
+    // Behind the last block nothing is loaded: the last blocks wait for all that is.
+    uint32_t ahead = begin + wave;
+    static_for<F::DEPTH - 1>([&](auto slot) {
+        if (ahead < end) load(ahead, slot.value);
+        ahead += 4;
+    });
+    for (uint32_t n = begin + wave; n < end; n += 4 * F::DEPTH)
+        static_for<F::DEPTH>([&](auto slot) {
+            const uint32_t here = n + 4 * slot.value;
+            if (here >= end) return;
+            // the slot's last reads are done
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+            if (ahead < end) {
+                load(ahead, (slot.value + F::DEPTH - 1) % F::DEPTH);
+                asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * F::LOADS * (F::DEPTH - 1)) : "memory");
+            } else {
+                asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+            }
+            ahead += 4;
+            block(here, slot);
+        });
+
+    // the waves' sums: element d of row r at d * 32 + r, then the maxima and the sums
+    __syncthreads();
+    float *mine = (float *)lds + wave * (DP + 2) * 32;
+    const uint32_t row = lane & 31u;
+#pragma unroll
+    for (int b = 0; b < DP / 32; ++b)
+#pragma unroll
+        for (int k = 0; k < 16; ++k) mine[(b * 32 + 8 * (k / 4) + 4 * h + k % 4) * 32 + row] = o[b][k];
+    const Halves sums = halves((part[0] + part[1]) + (part[2] + part[3]));
+    if (h == 0) mine[DP * 32 + row] = top, mine[(DP + 1) * 32 + row] = sums.a + sums.b;
+    __syncthreads();
+    // eight threads a row, each with an eighth of its elements
+    constexpr int EACH = DP / 8;
+    const uint32_t to_row = threadIdx.x & 31u, d0 = threadIdx.x / 32 * EACH, index = p.tile * kFewRows + to_row;
+    if (index >= p.lq * a.group) return;
+    const float *all = (const float *)lds + to_row;
+    float most = -INFINITY, by[4], sum = 0.0f;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) most = fmaxf(most, all[(w * (DP + 2) + DP) * 32]);
+    const float base = most == -INFINITY ? 0.0f : most;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+        by[w] = __builtin_amdgcn_exp2f((all[(w * (DP + 2) + DP) * 32] - base) * c);
+        sum += by[w] * all[(w * (DP + 2) + DP + 1) * 32];
+    }
+    const float inverse = sum == 0.0f ? 0.0f : 1.0f / sum;
+    float v[EACH];
+#pragma unroll
+    for (int k = 0; k < EACH; ++k) {
+        v[k] = 0.0f;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) v[k] += by[w] * all[(w * (DP + 2) + d0 + k) * 32];
+        v[k] *= inverse;
+    }
+    const uint32_t query = index / a.group, head = kv_head * a.group + (index - query * a.group);
+    const uint64_t token = p.q0 + query;
+    const float lse = sum == 0.0f ? -INFINITY : base * a.scale + __logf(sum);
+    const int have = (int)a.dim - (int)d0;
+    if (a.splits > 1) {
+        const uint64_t at_row = ((uint64_t)split * a.tokens_q + token) * a.heads + head;
+        float *out = a.part + at_row * a.dim + d0;
+        if (have >= EACH) store_vec<float, EACH>(out, v);
+        else store_part<float, EACH>(out, have, v);
+        if (d0 == 0) a.part_lse[at_row] = lse;
+    } else {
+        bf16 *out = a.o.at(token, head) + d0;
+        if (have >= EACH) store_vec<bf16, EACH>(out, v);
+        else store_part<bf16, EACH>(out, have, v);
+        if (a.lse && d0 == 0) a.lse[(uint64_t)head * a.tokens_q + token] = lse;
+    }
+}
+
 // Joins the runs of keys of a split call: one wave for each row, lane s with the
 // statistics of run s, so that no load waits for another.
 constexpr uint32_t kMaxRuns = 64;
@@ -938,21 +1112,23 @@ AttnTensors attn_tensors(const ar_attention_desc &d, const void *q, const void *
 }
 
 // Tiles that the grid has room for: of queries' rows, and of keys.
-size_t row_slots(const ar_attention_desc &d) { return d.tokens_q * (d.heads / d.kv_heads) / kRows + d.sequences; }
+size_t row_slots(const ar_attention_desc &d, size_t rows = kRows) { return d.tokens_q * (d.heads / d.kv_heads) / rows + d.sequences; }
 size_t key_slots(const ar_attention_desc &d) { return d.tokens_k / kRows + d.sequences; }
 
 // How many runs the stages of each tile are split into: what makes the time of the
 // longest tile, whose stages follow one another, and of the join least.  `stages`: of a
 // tile, in the mean, half as many again where there are several sequences, some of them
-// longer; us: of a stage, alone; bytes: of a run's sums.  A join takes 5 us, 0.2 for each
-// run and the sums' way to memory and back at 3.4 TB/s.  Tiles of one length (one sequence,
+// longer; us: of a stage, alone; bytes: of a run's sums; work: the time of all tiles with
+// the device full.  A join takes 5 us, 0.2 for each run and the sums' way to memory and back
+// at 3.4 TB/s.  Tiles of one length (one sequence,
 // most of its keys seen by every query) come in rounds of `room` workgroups.  No more than
 // `most` times that in all: from there on the device is full and the sums are for nothing.
-// By sweeps of 1 to 64 runs over fourteen sizes, each in one piece, with the best, as
-// chosen: forward, 32 heads over 8 of 128, 1 query of 16000 keys 300, 34, 36 us, 32 of
-// 7600 408, 203, 206; 8 heads over 1, 512 of 33000 581, 89, 89; dk and dv of 2048 queries,
+// By sweeps of 1 to 64 runs over twenty sizes, each in one piece, with the best, as
+// chosen: forward, 32 heads over 8 of 128, 1 query of 16000 keys 120, 28, 31 us, 32 of
+// 7600 227, 194, 194; 8 heads over 1, 512 of 33000 581, 89, 89; dk and dv of 2048 queries,
 // 16 heads over 2, 485, 74, 76 us.
-uint32_t runs_for(size_t tiles, double stages, double us, double bytes, size_t room, size_t most, const ar_attention_desc &d)
+uint32_t runs_for(size_t tiles, double stages, double us, double bytes, size_t room, size_t most, const ar_attention_desc &d,
+                  double work = 0.0)
 {
     const bool alike = d.sequences == 1 && (!(d.flags & AR_ATTN_CAUSAL) || d.tokens_k >= 4 * d.tokens_q);
     if (d.sequences > 1) stages *= 1.5;
@@ -961,6 +1137,7 @@ uint32_t runs_for(size_t tiles, double stages, double us, double bytes, size_t r
     for (uint32_t s = 1; s <= kMaxRuns && (s == 1 || (s <= stages && s * tiles <= most * room)); ++s) {
         double t = stages / s * us;
         if (alike) t *= (tiles * s + room - 1) / room;
+        else if (t < work + t / 4) t = work + t / 4;
         if (s > 1) t += 5.0 + s * (0.2 + 2.0 * bytes / 3.4e6);
         if (s == 1 || t < time) best = s, time = t;
     }
@@ -969,15 +1146,33 @@ uint32_t runs_for(size_t tiles, double stages, double us, double bytes, size_t r
 double mean_stages(size_t tokens, const ar_attention_desc &d) { return ceil((double)tokens / d.sequences / kKeys); }
 double sums_bytes(size_t rows, const ar_attention_desc &d) { return 4.0 * rows * d.dim; }
 // Tiles that there are if the lengths are as even as they can be.
-size_t tiles_for(size_t rows, const ar_attention_desc &d)
+size_t tiles_for(size_t rows, const ar_attention_desc &d, size_t each = kRows)
 {
-    const size_t n = (rows + kRows - 1) / kRows;
+    const size_t n = (rows + each - 1) / each;
     return (n > d.sequences ? n : d.sequences) * d.kv_heads;
+}
+// Whether the forward pass takes its rows 32 at a time: where each such tile has a compute
+// unit, and there are no more of them than of 128 rows (no sequence has more than 32, if
+// they are even) or little to compute.  A tile of 32 takes nearly half the time of one of
+// 128.  By 128 and by 32 rows, in us: 8 queries of 1000 keys, 32 heads over 8 of 128, in
+// 127 sequences (1016 tiles of 32) 111, 165; one sequence of 8 heads over 1, 1000 queries
+// of 2000 keys (250 tiles of 32 stages) 33, 24, of 10000 keys 63, 84; 256 of 30000 (64 of
+// 469) 60, 70; 4 heads over 1 (32 of 469) 53, 44.
+bool few_rows(const ar_attention_desc &d)
+{
+    const size_t rows = d.tokens_q * (d.heads / d.kv_heads), tiles = tiles_for(rows, d, kFewRows);
+    return tiles <= 256 && (rows <= kFewRows * d.sequences || tiles * mean_stages(d.tokens_k, d) <= 16384);
 }
 uint32_t forward_splits(const ar_attention_desc &d)
 {
-    return runs_for(tiles_for(d.tokens_q * (d.heads / d.kv_heads), d), mean_stages(d.tokens_k, d), d.dim <= 64 ? 0.9 : 1.2,
-                    sums_bytes(d.tokens_q * d.heads, d), 512, 4, d);
+    const size_t rows = d.tokens_q * (d.heads / d.kv_heads);
+    const bool few = few_rows(d);
+    const size_t tiles = tiles_for(rows, d, few ? kFewRows : kRows);
+    const double stages = mean_stages(d.tokens_k, d), bytes = sums_bytes(d.tokens_q * d.heads, d);
+    // K and V of all stages, at 4.8 TB/s
+    const double work = tiles * stages * kKeys * 4.0 * d.dim / 4.8e6;
+    if (few) return runs_for(tiles, stages, d.dim <= 64 ? 0.3 : 0.5, bytes, 256, 4, d, work);
+    return runs_for(tiles, stages, d.dim <= 64 ? 0.9 : 1.2, bytes, 512, 4, d, work);
 }
 uint32_t dq_splits(const ar_attention_desc &d)
 {
@@ -1062,6 +1257,11 @@ template <int DP> int launch_forward(const AttnArgs &a, hipStream_t st)
     static OncePerDevice once;
     return launch_tiles(once, attention_kernel<DP>, groups_of(a), 4 * Stage<DP>::BYTES, st, a);
 }
+template <int DP> int launch_few(const AttnArgs &a, hipStream_t st)
+{
+    static OncePerDevice once;
+    return launch_tiles(once, attention_few_kernel<DP>, groups_of(a), Few<DP>::LDS, st, a);
+}
 // keys, rows: null where not wanted
 template <int DP> int launch_backward(const AttnArgs *keys, const AttnArgs *rows, bool together, hipStream_t st)
 {
@@ -1113,9 +1313,12 @@ int attention(const ar_attention_desc *desc, const void *q, const void *k, const
     a.q = readable(t.q, at, &copies), a.k = readable(t.k, at, &copies), a.v = readable(t.v, at, &copies);
     if ((rc = run_copies(copies, st)) != AR_OK) return rc;
     a.o = heads_of<bf16>(t.o), a.lse = lse;
-    a.slots = (uint32_t)row_slots(d), a.splits = forward_splits(d);
+    const bool few = few_rows(d);
+    a.slots = (uint32_t)row_slots(d, few ? kFewRows : kRows), a.splits = forward_splits(d);
     a.part = (float *)at, a.part_lse = a.part + a.splits * d.tokens_q * d.heads * d.dim;
-    if ((rc = d.dim <= 64 ? launch_forward<64>(a, st) : launch_forward<128>(a, st)) != AR_OK || a.splits == 1) return rc;
+    if (few) rc = d.dim <= 64 ? launch_few<64>(a, st) : launch_few<128>(a, st);
+    else rc = d.dim <= 64 ? launch_forward<64>(a, st) : launch_forward<128>(a, st);
+    if (rc != AR_OK || a.splits == 1) return rc;
     hipLaunchKernelGGL(attention_join_kernel, dim3(groups_for(d.tokens_q * d.heads * 64)), dim3(256), 0, st, a);
     return launch_status();
 }

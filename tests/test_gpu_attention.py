@@ -62,7 +62,23 @@ CASES = [
 ]
 
 
-@pytest.mark.parametrize("case", CASES, ids=str)
+# More tiles than the device has compute units: the forward pass takes 128 rows a tile.
+MANY = [
+    ([1], [1], 257, 257, 64, True), ([5], [5], 257, 257, 1, True), ([33], [32], 390, 130, 128, True), ([65], [63], 288, 96, 96, True),
+    ([127, 129], [128, 128], 80, 40, 128, True), ([300, 1, 77], [300, 1, 77], 72, 24, 80, True), ([0, 40, 0], [7, 70, 0], 260, 130, 64, True),
+    ([9, 9], [0, 200], 260, 260, 33, False), ([70] * 3, [3, 64, 71], 91, 91, 120, True), ([128], [700], 66, 66, 40, False),
+    ([20], [900], 257, 257, 127, True), ([600], [3000], 16, 1, 128, True), ([1] * 20, [60 * i for i in range(20)], 32, 16, 64, True),
+]
+# Some sequences of many rows among those of few, some keys more than one tile of them is worth.
+MIXED = [
+    ([100, 1, 1, 1, 1, 1], [100, 30, 1, 2000, 64, 65], 8, 2, 128, True), ([1, 1, 70, 0, 1], [300, 0, 500, 9, 33], 12, 2, 72, True),
+    ([33], [33], 4, 4, 128, True), ([16, 16], [1000, 1001], 2, 1, 64, True), ([17, 16], [1000, 1001], 2, 1, 64, False),
+    ([1], [31], 8, 1, 128, True), ([1] * 4, [127, 128, 129, 160], 8, 1, 128, True), ([1] * 4, [255, 256, 257, 513], 8, 1, 56, True),
+    ([256], [9000], 8, 1, 16, True),
+]
+
+
+@pytest.mark.parametrize("case", CASES + MANY + MIXED, ids=str)
 def test_against_the_definition(case):
     lq, lk, heads, kv_heads, dim, causal = case
     say("attention", case)
@@ -70,20 +86,22 @@ def test_against_the_definition(case):
     check_all(*inputs(sq, sk, heads, kv_heads, dim), sq, sk, causal)
 
 
+@pytest.mark.parametrize("heads,kv_heads", [(4, 2), (80, 40)])
 @pytest.mark.parametrize("scale", [1e-3, 1.0, 20.0])
-def test_scales(scale):
+def test_scales(scale, heads, kv_heads):
     """From nearly even weights to weights on one key alone."""
-    say("scale", scale)
+    say("scale", scale, heads)
     sq = starts([150, 60])
-    check_all(*inputs(sq, sq, 4, 2, 64, 9), sq, sq, True, scale)
+    check_all(*inputs(sq, sq, heads, kv_heads, 64, 9), sq, sq, True, scale)
 
 
-def test_a_maximum_that_keeps_rising_and_one_that_comes_first():
-    say("rising")
+@pytest.mark.parametrize("heads,kv_heads", [(2, 1), (22, 11)])
+def test_a_maximum_that_keeps_rising_and_one_that_comes_first(heads, kv_heads):
+    say("rising", heads)
     n, d = 400, 64
     for order in (1.0, -1.0):
         sq = starts([n])
-        q, k, v, do = inputs(sq, sq, 2, 1, d, 20)
+        q, k, v, do = inputs(sq, sq, heads, kv_heads, d, 20)
         q[..., 0], k[..., 0] = 8.0, (order * torch.linspace(-40, 40, n)).bfloat16().cuda()[:, None]
         check_all(q, k, v, do, sq, sq, False)
 
@@ -113,11 +131,12 @@ def layouts(t, name):
 
 
 @pytest.mark.parametrize("name", ["heads first", "unaligned", "apart", "odd apart"])
+@pytest.mark.parametrize("heads", [6, 270])
 @pytest.mark.parametrize("dim", [64, 100, 128])
-def test_layouts(name, dim):
-    say("layout", name, dim)
+def test_layouts(name, dim, heads):
+    say("layout", name, dim, heads)
     sq, sk = starts([70, 5]), starts([130, 5])
-    q, k, v, do = inputs(sq, sk, 6, 2, dim, 30)
+    q, k, v, do = inputs(sq, sk, heads, heads // 3, dim, 30)
     kw = dict(starts_q=on_gpu(sq), starts_k=on_gpu(sk))
     o, lse = ar.packed_attention(q, k, v, save=True, **kw)
     grads = ar.packed_attention_backward(do, q, k, v, o, lse, **kw)
@@ -175,7 +194,7 @@ def test_tokens_of_no_sequence(lens):
         assert bool((t[:before] == 7).all()) and bool((t[sq[-1]:] == 7).all())
 
 
-@pytest.mark.parametrize("dim,heads", [(128, 8), (36, 5)])
+@pytest.mark.parametrize("dim,heads", [(128, 8), (36, 5), (64, 1)])
 def test_much_padding(dim, heads):
     """Far more padding than tokens, in every result."""
     say("much padding", dim, heads)
@@ -185,17 +204,18 @@ def test_much_padding(dim, heads):
     o, lse = ar.packed_attention(x, x, x, starts_q=on_gpu(sq), save=True)
     grads = ar.packed_attention_backward(x, x, x, x, o, lse, starts_q=on_gpu(sq))
     part = x[3000:3050]
-    o2, lse2 = ar.packed_attention(part, part, part, save=True)
-    grads2 = ar.packed_attention_backward(part, part, part, part, o2, lse2)
-    for t, t2 in zip((o, lse.t(), *grads), (o2, lse2.t(), *grads2)):
-        assert torch.equal(t[3000:3050], t2) and not t[:3000].any() and not t[3050:].any()
+    want = oo.attention(part, part, part, [0, 50], [0, 50], do=part)
+    for t, name in zip((o, lse.t(), *grads), ("o", "lse", "dq", "dk", "dv")):
+        check(t[3000:3050], *want[name], name)
+        assert not t[:3000].any() and not t[3050:].any()
 
 
-def test_keys_behind_a_sequences_end_do_not_reach_it():
+@pytest.mark.parametrize("heads,kv_heads", [(2, 1), (160, 80)])
+def test_keys_behind_a_sequences_end_do_not_reach_it(heads, kv_heads):
     """The next sequence's infinities and NaN lie in the same tiles."""
-    say("neighbours")
+    say("neighbours", heads)
     sq = starts([50, 60, 30])
-    q, k, v, do = inputs(sq, sq, 2, 1, 64, 60)
+    q, k, v, do = inputs(sq, sq, heads, kv_heads, 64, 60)
     kw = dict(starts_q=on_gpu(sq))
     o, lse = ar.packed_attention(q, k, v, save=True, **kw)
     grads = ar.packed_attention_backward(do, q, k, v, o, lse, **kw)
@@ -208,9 +228,10 @@ def test_keys_behind_a_sequences_end_do_not_reach_it():
         assert torch.equal(a[:50], b[:50]) and torch.equal(a[110:], b[110:])
 
 
-def test_later_keys_do_not_reach_a_query():
-    say("causal")
-    q, k, v, _ = inputs([0, 500], [0, 500], 2, 1, 128, 61)
+@pytest.mark.parametrize("heads", [2, 34])
+def test_later_keys_do_not_reach_a_query(heads):
+    say("causal", heads)
+    q, k, v, _ = inputs([0, 500], [0, 500], heads, heads // 2, 128, 61)
     o = ar.packed_attention(q, k, v)
     for t in (q, k, v):
         t[300:] = draw(t[300:].shape, 62, 50.0)

@@ -14,7 +14,7 @@
 //
 // What bounds it, 32 heads over 8 of 128, bf16.  Prompts, 16384 tokens in four: 765 us,
 // 1050 TFLOP/s, the board's power (matrix units busy 57 % of the cycles, vector units 51 %,
-// at 1.7 GHz).  Single tokens over 160 to 15000 keys, 32 of them: 201 us, 4.8 TB/s of the
+// at 1.7 GHz).  Single tokens over 160 to 15000 keys, 32 of them: 193 us, 5.0 TB/s of the
 // cache.  Training, 2 x 4096: 1235 us; dq 1050 TFLOP/s as the forward, dk and dv 1000.
 #include <type_traits>
 

@@ -454,20 +454,22 @@ template <int DP> __global__ __launch_bounds__(256, 2) void attention_kernel(con
 }
 
 // The forward pass where there are few rows, single tokens in a serving loop or a short
-// prompt: bound by the bytes of K and V, and by latency where those are few.  A tile has 32 rows, and each
-// wave of the workgroup every fourth block of 32 keys, which it loads into a part of LDS
-// of its own and waits for alone; at the end the waves' sums are joined through LDS.  By
-// tiles of 128 rows and so, 32 heads over 8 of 128: 1 query of 16000 keys 37 and 30 us, 32 of
-// 160 to 15000 210 and 195 us; 48 of 300, 8 heads over 1, 13.5 and 10.3 us.  A block takes
-// 0.9 us, the time of its loads, which are one block ahead: more do not fit the LDS.
+// prompt: bound by the bytes of K and V, and by latency where those are few.  A tile has 32
+// rows, and each wave of the workgroup every fourth block of 32 keys, which it loads into a
+// part of LDS of its own and waits for alone; at the end the waves' sums are joined through
+// LDS.  A place in LDS is loaded again as soon as it has been read, K's while V is used, so
+// one place each is enough with dim above 64, and two workgroups fit a compute unit: with two
+// places each and one workgroup 504 tiles of 1200 keys took 34 us, so 26; dim 64, four places
+// and one workgroup, two and two: 23, 17 us (by tiles of 128 rows 34 and 32).  32 heads over
+// 8 of 128, by tiles of 128 rows and so: 1 query of 16000 keys 37 and 31 us, 32 of 160 to
+// 15000 210 and 195 us.
 constexpr int kFewRows = 32;
 template <int DP> struct Few {
-    static constexpr int BLOCK = 32 * DP * 2, DEPTH = DP == 128 ? 2 : 4;  // bytes of a block of K or V; blocks of a wave
-    static constexpr int WAVE = 2 * DEPTH * BLOCK, LDS = 4 * WAVE;
+    static constexpr int BLOCK = 32 * DP * 2, DEPTH = DP == 128 ? 1 : 2;  // bytes of a block of K or V; blocks of a wave
+    static constexpr int WAVE = 2 * DEPTH * BLOCK, SUMS = 4 * (DP + 2) * 32 * (int)sizeof(float), LDS = 4 * WAVE > SUMS ? 4 * WAVE : SUMS;
     static constexpr int LOADS = BLOCK / 1024;
-    static_assert(4 * (DP + 2) * 32 * (int)sizeof(float) <= LDS, "the waves' sums fit");
 };
-template <int DP> __global__ __launch_bounds__(256, 1) void attention_few_kernel(const AttnArgs a)
+template <int DP> __global__ __launch_bounds__(256, 2) void attention_few_kernel(const AttnArgs a)
 {
     typedef Few<DP> F;
     typedef Stage<DP> S;
@@ -496,16 +498,15 @@ template <int DP> __global__ __launch_bounds__(256, 1) void attention_few_kernel
         off_v[i] = c * 8 < a.dim_in ? row * (uint32_t)a.v.ld * 2 + c * 16 : kOutOfRange;
     }
     uint64_t next_k = uniform_address(a.k.at(p.k0 + (begin + wave) * 32, kv_head)), next_v = uniform_address(a.v.at(p.k0 + (begin + wave) * 32, kv_head));
-    auto load = [&](uint32_t n, uint32_t slot) {
-        const uint32_t to = lds0 + slot * 2 * F::BLOCK, left = p.lk - n * 32;
-        const u32x4v from_k = tile_resource(next_k), from_v = tile_resource(next_v);
-        next_k += 4 * 32 * a.k.ld * 2, next_v += 4 * 32 * a.v.ld * 2;
+    auto load = [&](uint32_t n, uint32_t to, uint64_t &next, uint64_t ld, const uint32_t *off) {
+        const uint32_t left = p.lk - n * 32;
+        const u32x4v from = tile_resource(next);
+        next += 4 * 32 * ld * 2;
 #pragma unroll
-        for (int i = 0; i < F::LOADS; ++i) load_to_lds(to + i * 1024, (i * 64 + lane) / S::CHUNKS < left ? off_k[i] : kOutOfRange, from_k, 0u);
-#pragma unroll
-        for (int i = 0; i < F::LOADS; ++i)
-            load_to_lds(to + F::BLOCK + i * 1024, (i * 64 + lane) / S::CHUNKS < left ? off_v[i] : kOutOfRange, from_v, 0u);
+        for (int i = 0; i < F::LOADS; ++i) load_to_lds(lds0 + to + i * 1024, (i * 64 + lane) / S::CHUNKS < left ? off[i] : kOutOfRange, from, 0u);
     };
+    auto load_k = [&](uint32_t n, uint32_t slot) { load(n, slot * 2 * F::BLOCK, next_k, a.k.ld, off_k); };
+    auto load_v = [&](uint32_t n, uint32_t slot) { load(n, slot * 2 * F::BLOCK + F::BLOCK, next_v, a.v.ld, off_v); };
     Reads<DP> at;
     at.place(lds0);
     bf16x8 q[DP / 16];
@@ -516,11 +517,21 @@ template <int DP> __global__ __launch_bounds__(256, 1) void attention_few_kernel
     const float c = a.scale * kLog2e;
     float top = -INFINITY, part[4] = {0.0f, 0.0f, 0.0f, 0.0f};
 
+    // Of the loads that are on their way, all but the newest DEPTH - 1 of K and of V and one
+    // more are there; where so many were not begun, all are.
+    auto landed = [&](bool all_begun) {
+        if (all_begun) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(F::LOADS * (2 * F::DEPTH - 1)) : "memory");
+        else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    };
     auto block = [&](uint32_t n, auto slot) {
         constexpr int K = slot.value * 2 * F::BLOCK, V = K + F::BLOCK;
+        landed(n + 4 * (F::DEPTH - 1) < end);
         f32x16 s{};
 #pragma unroll
         for (int d = 0; d < DP / 16; ++d) s = Frag<bf16>::mfma(at.rows(0, d, K), q[d], s);
+        const uint32_t ahead = n + 4 * F::DEPTH;
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // K's reads are done
+        if (ahead < end) load_k(ahead, slot.value);
         if (n * 32 + 32 > r.least) {
             const int32_t left = (int32_t)(r.limit - n * 32 - 4 * h);
 #pragma unroll
@@ -546,33 +557,23 @@ template <int DP> __global__ __launch_bounds__(256, 1) void attention_few_kernel
         const float base = top == -INFINITY ? 0.0f : top * c;
 #pragma unroll
         for (int k = 0; k < 16; ++k) s[k] = __builtin_amdgcn_exp2f(s[k] * c - base), part[k & 3] += s[k];
+        landed(ahead < end);
 #pragma unroll
         for (int k = 0; k < 2; ++k) {
             const bf16x8 w = rounded(s, k * 8);
 #pragma unroll
             for (int d = 0; d < DP / 32; ++d) o[d] = Frag<bf16>::mfma(at.columns(d, k, V), w, o[d]);
         }
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // V's are
+        if (ahead < end) load_v(ahead, slot.value);
     };
-    // Behind the last block nothing is loaded: the last blocks wait for all that is.
-    uint32_t ahead = begin + wave;
-    static_for<F::DEPTH - 1>([&](auto slot) {
-        if (ahead < end) load(ahead, slot.value);
-        ahead += 4;
+    static_for<F::DEPTH>([&](auto slot) {
+        const uint32_t n = begin + wave + 4 * slot.value;
+        if (n < end) load_k(n, slot.value), load_v(n, slot.value);
     });
     for (uint32_t n = begin + wave; n < end; n += 4 * F::DEPTH)
         static_for<F::DEPTH>([&](auto slot) {
-            const uint32_t here = n + 4 * slot.value;
-            if (here >= end) return;
-            // the slot's last reads are done
-            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-            if (ahead < end) {
-                load(ahead, (slot.value + F::DEPTH - 1) % F::DEPTH);
-                asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * F::LOADS * (F::DEPTH - 1)) : "memory");
-            } else {
-                asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-            }
-            ahead += 4;
-            block(here, slot);
+            if (n + 4 * slot.value < end) block(n + 4 * slot.value, slot);
         });
 
     // the waves' sums: element d of row r at d * 32 + r, then the maxima and the sums
@@ -1124,8 +1125,8 @@ size_t key_slots(const ar_attention_desc &d) { return d.tokens_k / kRows + d.seq
 // most of its keys seen by every query) come in rounds of `room` workgroups.  No more than
 // `most` times that in all: from there on the device is full and the sums are for nothing.
 // By sweeps of 1 to 64 runs over twenty sizes, each in one piece, with the best, as
-// chosen: forward, 32 heads over 8 of 128, 1 query of 16000 keys 120, 28, 31 us, 32 of
-// 7600 227, 194, 194; 8 heads over 1, 512 of 33000 581, 89, 89; dk and dv of 2048 queries,
+// chosen: forward, 32 heads over 8 of 128, 1 query of 16000 keys 146, 28, 31 us, 32 of
+// 7600 327, 194, 195; 8 heads over 1, 512 of 33000 581, 89, 89; dk and dv of 2048 queries,
 // 16 heads over 2, 485, 74, 76 us.
 uint32_t runs_for(size_t tiles, double stages, double us, double bytes, size_t room, size_t most, const ar_attention_desc &d,
                   double work = 0.0)
@@ -1151,17 +1152,21 @@ size_t tiles_for(size_t rows, const ar_attention_desc &d, size_t each = kRows)
     const size_t n = (rows + each - 1) / each;
     return (n > d.sequences ? n : d.sequences) * d.kv_heads;
 }
-// Whether the forward pass takes its rows 32 at a time: where each such tile has a compute
-// unit, and there are no more of them than of 128 rows (no sequence has more than 32, if
-// they are even) or little to compute.  A tile of 32 takes nearly half the time of one of
-// 128.  By 128 and by 32 rows, in us: 8 queries of 1000 keys, 32 heads over 8 of 128, in
-// 127 sequences (1016 tiles of 32) 111, 165; one sequence of 8 heads over 1, 1000 queries
-// of 2000 keys (250 tiles of 32 stages) 33, 24, of 10000 keys 63, 84; 256 of 30000 (64 of
-// 469) 60, 70; 4 heads over 1 (32 of 469) 53, 44.
+// Whether the forward pass takes its rows 32 at a time: nearly always where a sequence has
+// no more than eight, else where such workgroups find room at once, two on a compute unit
+// (or little more, if they have much to do), and there is little to compute in all.  Time by
+// 32 rows, of that by 128, means over 8 to 32 heads of dim 128, sequences of 100, 300, 500,
+// 1000 tiles: even, of 60 keys 0.92, 0.94, 0.98, 1.20, of 1000 keys 0.87, 0.67, 0.74, 1.03, of
+// 8000 keys 1.17, 1.23, 1.15, 1.30; uneven, of 1000 keys 0.91, 0.78, 0.79, 0.88; 32 rows each, of
+// 1000 keys 0.94, 0.87, 1.07, 1.04; one or eight rows each 0.7 to 1.1.  Of dim 64: one row each
+// of 60 keys 0.89, 0.91, 1.01, 1.26, even of 1000 keys 0.70, 0.50, 0.51, 0.93.
 bool few_rows(const ar_attention_desc &d)
 {
-    const size_t rows = d.tokens_q * (d.heads / d.kv_heads), tiles = tiles_for(rows, d, kFewRows);
-    return tiles <= 256 && (rows <= kFewRows * d.sequences || tiles * mean_stages(d.tokens_k, d) <= 16384);
+    const size_t rows = d.tokens_q * (d.heads / d.kv_heads), groups = row_slots(d, kFewRows) * d.kv_heads;
+    const double stages = mean_stages(d.tokens_k, d);
+    const bool some = groups <= 560 || (stages >= 8 && groups <= 700) || (stages >= 16 && d.dim <= 64 && groups <= 1100);
+    if (rows <= 8 * d.sequences) return some || stages >= 16 || d.dim > 64;
+    return some && tiles_for(rows, d, kFewRows) * stages <= (d.dim <= 64 ? 32000 : 16000);
 }
 uint32_t forward_splits(const ar_attention_desc &d)
 {
@@ -1169,9 +1174,10 @@ uint32_t forward_splits(const ar_attention_desc &d)
     const bool few = few_rows(d);
     const size_t tiles = tiles_for(rows, d, few ? kFewRows : kRows);
     const double stages = mean_stages(d.tokens_k, d), bytes = sums_bytes(d.tokens_q * d.heads, d);
-    // K and V of all stages, at 4.8 TB/s
-    const double work = tiles * stages * kKeys * 4.0 * d.dim / 4.8e6;
-    if (few) return runs_for(tiles, stages, d.dim <= 64 ? 0.3 : 0.5, bytes, 256, 4, d, work);
+    // K and V at 4.8 TB/s, or the tiles' stages with the device full
+    const double each = few ? d.dim <= 64 ? 0.9e-3 : 1.5e-3 : d.dim <= 64 ? 3e-3 : 4.5e-3;
+    const double work = fmax(4.0 * d.tokens_k * d.kv_heads * d.dim / 4.8e6, tiles * stages * each);
+    if (few) return runs_for(tiles, stages, d.dim <= 64 ? 0.37 : 0.6, bytes, 512, 4, d, work);
     return runs_for(tiles, stages, d.dim <= 64 ? 0.9 : 1.2, bytes, 512, 4, d, work);
 }
 uint32_t dq_splits(const ar_attention_desc &d)

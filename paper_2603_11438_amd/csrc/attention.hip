@@ -629,7 +629,8 @@ template <int DP> __global__ __launch_bounds__(256, 2) void attention_few_kernel
 }
 
 // Joins the runs of keys of a split call: one wave for each row, lane s with the
-// statistics of run s, so that no load waits for another.
+// statistics of run s, and the first sums on their way before those are there, so that no
+// load waits for another.
 constexpr uint32_t kMaxRuns = 64;
 __global__ __launch_bounds__(256) void attention_join_kernel(const AttnArgs a)
 {
@@ -639,16 +640,31 @@ __global__ __launch_bounds__(256) void attention_join_kernel(const AttnArgs a)
     for (uint64_t i = (uint64_t)blockIdx.x * 4 + uniform(threadIdx.x >> 6); i < rows; i += (uint64_t)gridDim.x * 4) {
         const uint32_t token = (uint32_t)(i / a.heads), head = (uint32_t)(i % a.heads);
         if (token < from || token >= until) continue;
+        const float *o = a.part + i * a.dim + d;
+        constexpr int FIRST = 16;
+        float early[FIRST][2];
         const float lse = lane < a.splits ? a.part_lse[lane * rows + i] : -INFINITY;
+#pragma unroll
+        for (int s = 0; s < FIRST; ++s) {
+            const float *from_run = o + (s < (int)a.splits ? s * rows * a.dim : 0);
+            early[s][0] = d < a.dim ? from_run[0] : 0.0f;
+            early[s][1] = d + 1 < a.dim ? from_run[1] : 0.0f;
+        }
         float top = lse;
 #pragma unroll
         for (int m = 32; m; m >>= 1) top = __builtin_elementwise_maximum(top, __shfl_xor(top, m));  // NaN stays
         const float base = top == -INFINITY ? 0.0f : top, w = __expf(lse - base), sum = wave_sum(w);
         float v[2] = {0.0f, 0.0f};
-        const float *o = a.part + i * a.dim + d;
+        auto weight = [&](uint32_t s) { return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, w), (int)s)); };
+#pragma unroll
+        for (int s = 0; s < FIRST; ++s) {
+            if (s >= (int)a.splits) break;
+            const float by = weight(s);
+            v[0] += by * early[s][0], v[1] += by * early[s][1];
+        }
 #pragma unroll 8
-        for (uint32_t s = 0; s < a.splits; ++s) {
-            const float by = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, w), (int)s));
+        for (uint32_t s = FIRST; s < a.splits; ++s) {
+            const float by = weight(s);
             const float *from_run = o + s * rows * a.dim;
             if (d < a.dim) v[0] += by * from_run[0];
             if (d + 1 < a.dim) v[1] += by * from_run[1];

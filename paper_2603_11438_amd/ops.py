@@ -714,11 +714,16 @@ def packed_attention_backward(do, q, k, v, o, lse, *, starts_q=None, starts_k=No
     return dq if need_dq else None, dk if need_dkv else None, dv if need_dkv else None
 
 
-def packed_attention_backward_workspace(queries: int, keys: int, heads: int, kv_heads: int, dim: int, sequences: int = 1) -> int:
-    """Bytes of packed_attention_backward's workspace."""
-    d = ar_attention_desc(sequences=sequences, tokens_q=queries, tokens_k=keys, heads=heads, kv_heads=kv_heads, dim=dim,
-                          dtype=_ar.AR_BFLOAT16, scale=1.0)
-    return _lib().ar_attention_backward_workspace(ctypes.byref(d))
+def packed_attention_backward_workspace(queries: int, keys: int, heads: int, kv_heads: int, dim: int, sequences: int = 1, *,
+                                        causal: Optional[bool] = None) -> int:
+    """Bytes of packed_attention_backward's workspace; enough for a causal call and for one
+    that is not, unless `causal` says which it is."""
+    L, most = _lib(), 0
+    for flags in (0, AR_ATTN_CAUSAL) if causal is None else (AR_ATTN_CAUSAL if causal else 0,):
+        d = ar_attention_desc(sequences=sequences, tokens_q=queries, tokens_k=keys, heads=heads, kv_heads=kv_heads, dim=dim,
+                              dtype=_ar.AR_BFLOAT16, flags=flags, scale=1.0)
+        most = max(most, L.ar_attention_backward_workspace(ctypes.byref(d)))
+    return most
 
 
 # ---- loss over a vocabulary -------------------------------------------------------

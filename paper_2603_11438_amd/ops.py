@@ -675,9 +675,9 @@ def packed_attention_backward(do, q, k, v, o, lse, *, starts_q=None, starts_k=No
     for those not needed (need_dq, need_dkv).
 
     o, lse: from packed_attention(save=True) on the same arguments.  out: the three
-    results to write to, which may be parts of one tensor; tokens of no sequence are
-    then left as they were, and are zeros otherwise.  workspace: a uint8 tensor to use in
-    place of a new one (packed_attention_backward_workspace)."""
+    results to write to, None for new ones, which may be parts of one tensor; tokens of no
+    sequence are left as they were in these, and are zeros in new ones.  workspace: a uint8
+    tensor to use in place of a new one (packed_attention_backward_workspace)."""
     import torch
 
     _tell_of_graphs(do, q, k, v)
@@ -689,7 +689,9 @@ def packed_attention_backward(do, q, k, v, o, lse, *, starts_q=None, starts_k=No
         if not lse.is_cuda or lse.device.index != dev or lse.dtype != torch.float32 or not lse.is_contiguous() or tuple(lse.shape) != (d.heads, d.tokens_q):
             raise ValueError("lse must be what packed_attention(save=True) returned for these tensors")
         dq, dk, dv = (None, None, None) if out is None else out
-        new = lambda like: torch.empty(like.shape, dtype=like.dtype, device=like.device)  # noqa: E731
+        # zeros where the library leaves tokens of no sequence as they are
+        make = torch.zeros if d.sequences == 0 or (out is not None and sq is not None) else torch.empty
+        new = lambda like: make(like.shape, dtype=like.dtype, device=like.device)  # noqa: E731
         if need_dq:
             dq = new(q) if dq is None else dq
             _, _, _, d.ld_dq, d.hs_dq = _heads(dq, "dq", dev, tuple(q.shape), q.dtype)
@@ -707,10 +709,6 @@ def packed_attention_backward(do, q, k, v, o, lse, *, starts_q=None, starts_k=No
             _ptr(dq) if need_dq else None, _ptr(dk) if need_dkv else None, _ptr(dv) if need_dkv else None, _ptr(ws),
             0 if ws is None else ws.numel() * ws.element_size(), on.ptr)
         _ar._check(rc, "ar_attention_backward")
-        if d.sequences == 0 and out is None:
-            for t in (dq, dk, dv):
-                if t is not None:
-                    t.zero_()
     return dq if need_dq else None, dk if need_dkv else None, dv if need_dkv else None
 
 

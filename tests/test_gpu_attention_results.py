@@ -1,0 +1,59 @@
+"""What attention's results hold where no sequence has a part in them: new results zeros,
+the caller's own what they held."""
+from __future__ import annotations
+
+import math
+
+import pytest
+import torch
+
+import paper_2603_11438_amd as ar
+from gpu_helpers import say
+
+pytestmark = pytest.mark.gpu
+
+TOKENS, HEADS, KV_HEADS, DIM = 400, 4, 2, 64
+STARTS = {"padding": [37, 97, 167], "one": [100, 300], "no sequences": [0], "none either": [60]}
+
+
+def on_gpu(at):
+    return torch.tensor(at, dtype=torch.int32).cuda()
+
+
+def draw(heads, seed):
+    return torch.randn(TOKENS, heads, DIM, generator=torch.Generator().manual_seed(seed)).bfloat16().cuda()
+
+
+def inputs():
+    return draw(HEADS, 1), draw(KV_HEADS, 2), draw(KV_HEADS, 3), draw(HEADS, 4)
+
+
+def leave_nan():
+    """NaN in the memory that the next new tensors of the results' sizes get."""
+    for heads, dtype in ((HEADS, torch.bfloat16), (KV_HEADS, torch.bfloat16)):
+        kept = [torch.full((TOKENS, heads, DIM), math.nan, dtype=dtype, device="cuda") for _ in range(64)]
+        del kept
+    kept = [torch.full((HEADS, TOKENS), math.nan, device="cuda") for _ in range(64)]
+    del kept
+
+
+def outside(t, at, dim=0):
+    """The tokens of no sequence."""
+    return torch.cat([t.narrow(dim, 0, at[0]), t.narrow(dim, at[-1], TOKENS - at[-1])], dim)
+
+
+@pytest.mark.parametrize("given", [(True, False, False), (False, True, True), (False, False, True), (False, False, False)], ids=str)
+@pytest.mark.parametrize("name", list(STARTS))
+def test_gradients_that_are_new_and_those_that_are_not(name, given):
+    say("gradients", name, given)
+    at, (q, k, v, do) = STARTS[name], inputs()
+    kw = dict(starts_q=on_gpu(at))
+    o, lse = ar.packed_attention(q, k, v, save=True, **kw)
+    want = ar.packed_attention_backward(do, q, k, v, o, lse, **kw)
+    out = tuple(torch.full_like(t, 7.0) if is_given else None for t, is_given in zip((q, k, v), given))
+    leave_nan()
+    got = ar.packed_attention_backward(do, q, k, v, o, lse, out=out, **kw)
+    for g, mine, w in zip(got, out, want):
+        assert mine is None or g is mine
+        assert torch.equal(g[at[0]:at[-1]], w[at[0]:at[-1]])
+        assert bool((outside(g, at) == (0.0 if mine is None else 7.0)).all())

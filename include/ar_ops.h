@@ -215,7 +215,7 @@ enum { AR_ATTN_CAUSAL = 1, AR_ATTN_CLEAR = 2 };
  * tokens (0 = heads * hs), hs_* between heads (0 = dim).  Either a token's heads lie
  * within ld, or a head's tokens within hs; nothing overlaps. */
 typedef struct ar_attention_desc {
-    size_t sequences;             /* 0, or no tokens: a valid no-op; times heads at most 2^22 */
+    size_t sequences;             /* 0, or no tokens: a valid no-op, with AR_ATTN_CLEAR too; times heads at most 2^22 */
     size_t tokens_q, tokens_k;    /* times heads, or kv_heads, at most 2^30 */
     size_t heads, kv_heads, dim;  /* heads a multiple of kv_heads; dim 1 .. 128 (AR_ERR_UNSUPPORTED above) */
     int dtype;                    /* AR_BFLOAT16 */

@@ -642,8 +642,8 @@ def packed_attention(q, k, v, *, starts_q=None, starts_k=None, causal: bool = Tr
     starts[i] .. starts[i + 1] - 1; starts_k left out is starts_q, both left out one
     sequence.  causal: a sequence's last query sees all its keys, each one before it one
     less; a query that sees none has o = 0.  scale: 1 / sqrt(dim) unless given; above 0.
-    out: o to write to; tokens of no sequence are then left as they were, and are zeros
-    otherwise.  lse: (heads, queries) fp32."""
+    out: o to write to; tokens of no sequence are then left as they were in it, and are
+    zeros in a new one.  lse: (heads, queries) fp32, zeros there."""
     import torch
 
     if out is None and stream is None and (nat := _native()) is not None:
@@ -657,7 +657,9 @@ def packed_attention(q, k, v, *, starts_q=None, starts_k=None, causal: bool = Tr
         d, sq, sk = _attention_desc(q, k, v, starts_q, starts_k, causal, scale, on.index, out is None)
         o = torch.empty(q.shape, dtype=q.dtype, device=q.device) if out is None else out
         _, _, _, d.ld_o, d.hs_o = _heads(o, "out", on.index, tuple(q.shape), q.dtype)
-        lse = torch.empty(q.shape[1], q.shape[0], dtype=torch.float32, device=q.device) if save else None
+        # zeros where the library leaves tokens of no sequence as they are
+        make = torch.zeros if d.sequences == 0 or (out is not None and sq is not None) else torch.empty
+        lse = make(q.shape[1], q.shape[0], dtype=torch.float32, device=q.device) if save else None
         L = _lib()
         need = L.ar_attention_workspace_for(ctypes.byref(d), q.data_ptr(), k.data_ptr(), v.data_ptr())
         ws = _workspace(need, q)

@@ -57,3 +57,21 @@ def test_gradients_that_are_new_and_those_that_are_not(name, given):
         assert mine is None or g is mine
         assert torch.equal(g[at[0]:at[-1]], w[at[0]:at[-1]])
         assert bool((outside(g, at) == (0.0 if mine is None else 7.0)).all())
+
+
+@pytest.mark.parametrize("with_out", (False, True))
+@pytest.mark.parametrize("name", list(STARTS))
+def test_the_logarithms_that_are_kept(name, with_out):
+    """lse is always a new result: zeros in tokens of no sequence, whatever is done to o there."""
+    say("lse", name, with_out)
+    at, (q, k, v, _) = STARTS[name], inputs()
+    mine = torch.full_like(q, 7.0) if with_out else None
+    leave_nan()
+    o, lse = ar.packed_attention(q, k, v, starts_q=on_gpu(at), save=True, out=mine)
+    assert mine is None or o is mine
+    assert not outside(lse, at, 1).any()
+    assert bool((outside(o, at) == (7.0 if with_out else 0.0)).all())
+    if at[-1] > at[0]:
+        part = [t[at[0]:at[-1]].clone() for t in (q, k, v)]
+        want = ar.packed_attention(*part, starts_q=on_gpu([s - at[0] for s in at]), save=True)
+        assert torch.equal(o[at[0]:at[-1]], want[0]) and torch.equal(lse[:, at[0]:at[-1]], want[1])

@@ -1093,6 +1093,17 @@ struct Tensor {
 };
 template <typename T> Heads<T> heads_of(const Tensor &t) { return {(T *)t.p, t.ld, t.hs}; }
 
+// Whether two tensors may share an element.  As matrices of rows, and where those meet and
+// the strides are the same, head by head: parts of one tensor whose heads take turns, as q,
+// k and v of (tokens, heads, 3, dim) do, share none.
+bool meet(const Tensor &a, const Tensor &b)
+{
+    if (!meet(a.mat(), b.mat())) return false;
+    if (a.ld != b.ld || a.hs != b.hs || a.heads != b.heads) return true;
+    auto by_head = [](const Tensor &t) { return Batch{Mat{t.p, t.tokens, t.dim, t.ld, 2}, t.heads, t.hs}; };
+    return meet(by_head(a), by_head(b));
+}
+
 // `heads` 0: a stride that is not given
 Tensor tensor(const void *p, size_t tokens, size_t heads, size_t dim, size_t ld, size_t hs)
 {
@@ -1316,7 +1327,9 @@ int attention(const ar_attention_desc *desc, const void *q, const void *k, const
     const AttnTensors t = attn_tensors(d, q, k, v, o);
     if (!inputs_ok(d, t, starts_q, starts_k) || (uintptr_t)lse % 4 != 0) return AR_ERR_ARG;
     const Mat om = t.o.mat(), lm = mat(lse, d.tokens_q, d.heads, 0, AR_FLOAT32);
-    for (const Mat &in : {t.q.mat(), t.k.mat(), t.v.mat(), starts_mat(starts_q, d.sequences), starts_mat(starts_k, d.sequences)})
+    for (const Tensor &in : {t.q, t.k, t.v})
+        if (meet(t.o, in) || meet(lm, in.mat())) return AR_ERR_ARG;
+    for (const Mat &in : {starts_mat(starts_q, d.sequences), starts_mat(starts_k, d.sequences)})
         if (meet(om, in) || meet(lm, in)) return AR_ERR_ARG;
     if (meet(om, lm)) return AR_ERR_ARG;
     const size_t need = attention_need(d, t);
@@ -1403,21 +1416,28 @@ int attention_backward(const ar_attention_desc *desc, const void *dout, const vo
                            tensor(dk, d.tokens_k, d.kv_heads, d.dim, d.ld_dk, d.hs_dk),
                            tensor(dv, d.tokens_k, d.kv_heads, d.dim, d.ld_dv, d.hs_dv)};
     const Mat lm = mat(lse, d.tokens_q, d.heads, 0, AR_FLOAT32);
+    const Tensor ins[] = {t.q, t.k, t.v, t.o, g};
+    const Mat others[] = {lm, starts_mat(starts_q, d.sequences), starts_mat(starts_k, d.sequences)};
+    for (int i = 0; i < 3; ++i) {
+        if (!out[i].p) continue;
+        if (!out[i].ok()) return AR_ERR_ARG;
+        for (const Tensor &in : ins)
+            if (meet(out[i], in)) return AR_ERR_ARG;
+        for (const Mat &in : others)
+            if (meet(out[i].mat(), in)) return AR_ERR_ARG;
+        for (int j = 0; j < i; ++j)
+            if (out[j].p && meet(out[i], out[j])) return AR_ERR_ARG;
+    }
     const size_t need = backward_bytes(d);
     if (!ws || ws_bytes < need) return AR_ERR_SCRATCH;
     if ((uintptr_t)ws % 256 != 0) return AR_ERR_ARG;
     const Mat wm{ws, 1, need, need, 1};
-    const Mat ins[] = {t.q.mat(), t.k.mat(), t.v.mat(), t.o.mat(), g.mat(), lm, starts_mat(starts_q, d.sequences), starts_mat(starts_k, d.sequences)};
-    for (const Mat &in : ins)
+    for (const Tensor &in : ins)
+        if (meet(wm, in.mat())) return AR_ERR_ARG;
+    for (const Mat &in : others)
         if (meet(wm, in)) return AR_ERR_ARG;
-    for (int i = 0; i < 3; ++i) {
-        if (!out[i].p) continue;
-        if (!out[i].ok() || meet(out[i].mat(), wm)) return AR_ERR_ARG;
-        for (const Mat &in : ins)
-            if (meet(out[i].mat(), in)) return AR_ERR_ARG;
-        for (int j = 0; j < i; ++j)
-            if (out[j].p && meet(out[i].mat(), out[j].mat())) return AR_ERR_ARG;
-    }
+    for (const Tensor &to : out)
+        if (to.p && meet(wm, to.mat())) return AR_ERR_ARG;
 
     hipStream_t st = (hipStream_t)stream;
     const BackwardSpace s = backward_space(d, dq != nullptr, dk != nullptr);

@@ -75,3 +75,33 @@ def test_the_logarithms_that_are_kept(name, with_out):
         part = [t[at[0]:at[-1]].clone() for t in (q, k, v)]
         want = ar.packed_attention(*part, starts_q=on_gpu([s - at[0] for s in at]), save=True)
         assert torch.equal(o[at[0]:at[-1]], want[0]) and torch.equal(lse[:, at[0]:at[-1]], want[1])
+
+
+@pytest.mark.parametrize("dim", [64, 100])
+@pytest.mark.parametrize("heads_first", (False, True))
+def test_parts_whose_heads_take_turns(heads_first, dim):
+    """(tokens, heads, 3, dim), its gradients laid out the same, o beside do; as in tensors of their own."""
+    say("in turn", heads_first, dim)
+    g = torch.Generator().manual_seed(9)
+
+    def fused(parts, fill=None):
+        shape = (3, 150, parts, dim) if heads_first else (150, 3, parts, dim)
+        t = torch.randn(*shape, generator=g).bfloat16().cuda() if fill is None else torch.full(shape, fill, dtype=torch.bfloat16, device="cuda")
+        t = t.transpose(0, 1) if heads_first else t
+        return [t[:, :, n] for n in range(parts)]
+
+    starts, (q, k, v), (do, mine) = on_gpu([0, 90, 150]), fused(3), fused(2)
+    before = do.clone()
+    grads = fused(3, math.nan)
+    assert ar.packed_attention(q, k, v, starts_q=starts, out=mine) is mine
+    o, lse = ar.packed_attention(q, k, v, starts_q=starts, save=True)
+    ar.packed_attention_backward(do, q, k, v, mine, lse, starts_q=starts, out=grads)
+    apart = [t.clone(memory_format=torch.contiguous_format) for t in (do, q, k, v)]
+    assert torch.equal(do, before) and torch.equal(mine, o) and torch.equal(ar.packed_attention(*apart[1:], starts_q=starts), o)
+    for a, b in zip(grads, ar.packed_attention_backward(*apart, o, lse, starts_q=starts)):
+        assert torch.equal(a, b)
+    pair = fused(2, math.nan)
+    ar.packed_attention_backward(do, q, k, v, o, lse, starts_q=starts, out=(None, *pair))
+    assert torch.equal(pair[0], grads[1]) and torch.equal(pair[1], grads[2])
+    with pytest.raises(ar.ARError):
+        ar.packed_attention_backward(do, q, k, v, o, lse, starts_q=starts, out=(pair[0], pair[0], pair[1]))

@@ -162,18 +162,76 @@ __global__ __launch_bounds__(256) void vocab_ranks_kernel(const float *parts, ui
     loss[t] = target.get(t, &unused) ? log + (base - z) : 0.0f;
 }
 
+// Which dloss gives dz its factor (below): that of the first token with a class whose
+// dloss is a number and not 0.
+struct LeadOf {
+    const float *dloss;
+    uint64_t stride;
+    Targets target;
+    uint32_t tokens;
+    // a token's dloss, 0 if it cannot lead; both loads are on their way at once
+    __device__ __forceinline__ float get(uint32_t t) const
+    {
+        const uint32_t at = t < tokens ? t : tokens - 1;
+        uint64_t unused;
+        const float v = dloss[at * stride];
+        return target.get(at, &unused) && t < tokens && significand(v) < 1.0f ? v : 0.0f;
+    }
+};
+// By a wave, 512 tokens at a time; 0 if there is none.
+__device__ __forceinline__ float find_lead(const LeadOf &o)
+{
+    const uint32_t lane = threadIdx.x & 63u;
+    for (uint32_t t0 = 0; t0 < o.tokens; t0 += 512) {
+        float v[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) v[k] = o.get(t0 + k * 64 + lane);
+#pragma unroll
+        for (int k = 0; k < 8; ++k)
+            if (const uint64_t found = __ballot(v[k] != 0.0f)) return __shfl(v[k], __ffsll((unsigned long long)found) - 1);
+    }
+    return 0.0f;
+}
+// By a workgroup, 4096 at a time, where there are more tokens, or more waves, than each
+// wave of the next kernel should look through.  3 to 4 us with the launch.
+__global__ __launch_bounds__(1024) void vocab_lead_kernel(const LeadOf o, float *lead)
+{
+    __shared__ uint32_t first;
+    if (threadIdx.x == 0) first = o.tokens;
+    __syncthreads();
+    for (uint32_t t0 = 0; t0 < o.tokens; t0 += 4096) {
+        float v[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) v[k] = o.get(t0 + k * 1024 + threadIdx.x);
+        uint32_t mine = o.tokens;  // the wave's first
+#pragma unroll
+        for (int k = 3; k >= 0; --k)
+            if (const uint64_t found = __ballot(v[k] != 0.0f)) mine = t0 + k * 1024 + (threadIdx.x & ~63u) + __ffsll((unsigned long long)found) - 1;
+        if (mine < o.tokens && (threadIdx.x & 63u) == 0) atomicMin(&first, mine);
+        __syncthreads();
+        const uint32_t found = first;
+        __syncthreads();  // all have read it before any goes on
+        if (found < o.tokens) break;
+    }
+    if (threadIdx.x == 0) *lead = first < o.tokens ? o.dloss[first * o.stride] : 0.0f;
+}
+
 // dz of a piece of the vocabulary: (e^(z - lse) - [target]) dloss / f, 0 for a token
 // without a loss and up to the next multiple of eight columns.  f is the significand of
-// the first token's dloss, and the products with dz are multiplied by it in fp32.  With one
+// one token's dloss, and the products with dz are multiplied by it in fp32.  With one
 // dloss for all tokens, the mean's, most of dz's weight lies in targets' elements, all of
 // them near -dloss: rounded to bf16, all would be off in one direction, and the gradients
-// by as much (777 tokens of 5001 classes: by 2.6e-3 of their norm, so by 1.7e-3).
+// by as much (777 tokens of 5001 classes: by 2.6e-3 of their norm, so by 1.7e-3).  So the
+// token has to be one that counts: tokens without a loss, a prompt's at the beginning
+// say, may hold 0 or anything.
 struct DzOut {
     bf16 *dz;
     uint64_t ld;
     const float *lse, *dloss;
     uint64_t dloss_stride;
     Targets target;  // first: of the piece
+    uint32_t search; // tokens that the lead is looked for in, and left at `lead`; 0: it is there
+    float *lead;
 };
 template <typename S> __global__ __launch_bounds__(S::THREADS) void vocab_dz_kernel(const GemmArgs g, const DzOut o)
 {
@@ -187,6 +245,8 @@ template <typename S> __global__ __launch_bounds__(S::THREADS) void vocab_dz_ker
     if (col0 >= g.n) return;
     const uint32_t cols = g.n - col0;
     char *stage = lds + wave * kStageBytes<bf16, COLS>;
+    const float lead = o.search ? find_lead({o.dloss, o.dloss_stride, o.target, o.search}) : *o.lead, f = significand(lead);
+    if (o.search && at.m == 0 && at.n == 0 && threadIdx.x == 0) *o.lead = lead;
     static_for<S::MT>([&](auto block) {
         constexpr int i = block.value;
         float v[NT][16];
@@ -198,7 +258,7 @@ template <typename S> __global__ __launch_bounds__(S::THREADS) void vocab_dz_ker
         const bool counts = o.target.get(row, &t);
         const uint64_t place = t - o.target.first - col0;
         const uint32_t hit = counts && t >= o.target.first && place < COLS ? (uint32_t)place : 0xffffffffu;
-        const float lse = o.lse[row] * kLog2e, by = o.dloss[row * o.dloss_stride] / factor(o.dloss);
+        const float lse = o.lse[row] * kLog2e, by = o.dloss[row * o.dloss_stride] / f;
         stage_rows<bf16, COLS>(stage, [&](int j, int r) {
             const uint32_t c = (uint32_t)(j * 32 + 8 * (r / 4) + r % 4) + 4 * h;
             const float p = __builtin_amdgcn_exp2f(v[j][r] * kLog2e - lse);
@@ -383,12 +443,19 @@ int vocab_join(const ar_vocab_desc *desc, size_t ranks, const float *parts, cons
 // device many times over and dx's sums, read and written by each, cost little.
 constexpr size_t kPieceBytes = (size_t)1 << 29;
 constexpr size_t kLeastPiece = 1024;
+// Whether each wave that makes dz looks for the lead by itself: where there are few tokens
+// to look through, eight looks at most, and few rounds of tiles that all do so, which is
+// less than a launch.  Gradients of 1025 x 1024 x 8192, 98.4 us with the first dloss taken as
+// it is: by waves 99, where only the last quarter of the tokens counts 96 (from 93.4); 4097 x
+// 512 x 4096, 114.5: by a launch 118.
+bool lead_by_waves(const ar_vocab_desc &d) { return d.tokens <= 4096 && d.tokens * d.rows <= (size_t)1 << 24; }
 
 // Where the backward pass keeps what; dz lies at the start, copies behind the rest.
 struct VocabBackwardSpace {
     size_t piece, pieces;  // rows of the weight in a piece (but the last)
     size_t ld;             // of dz
     Cut dx, dw;
+    size_t lead;                      // the dloss that gives dz its factor
     size_t part_dx, part_dw, copies;  // with one piece one place after the other
 };
 VocabBackwardSpace vocab_backward_space(const ar_vocab_desc &d, bool dx, bool dw)
@@ -400,7 +467,8 @@ VocabBackwardSpace vocab_backward_space(const ar_vocab_desc &d, bool dx, bool dw
     s.piece = s.pieces == 1 ? d.rows : round_up((d.rows + s.pieces - 1) / s.pieces, 256);
     s.pieces = (d.rows + s.piece - 1) / s.piece;
     s.ld = round_up(s.piece, kLine);
-    s.part_dx = s.part_dw = s.copies = round_up(d.tokens * s.ld * 2, 256);
+    s.lead = round_up(d.tokens * s.ld * 2, 256);
+    s.part_dx = s.part_dw = s.copies = s.lead + 256;
     const bool several = s.pieces > 1;  // dx's sums stay from piece to piece
     if (dx) {
         s.dx = cut_for(1, d.tokens, d.dim, s.ld / kStepK, 1, false, 0, 4, kMaxSplits);
@@ -449,13 +517,19 @@ int vocab_backward(const ar_vocab_desc *desc, const float *dloss, size_t dloss_s
     GemmArgs logits{};
     Operand px, pw;
     if ((rc = logits_args(d, m, (char *)ws + s.copies, &logits, &px, &pw, st)) != AR_OK) return rc;
-    const ProductOut to_dx{{(bf16 *)dx, nullptr}, part_dx, {odx.ld, 0}, 0x80000000u, (uint32_t)d.tokens, (uint32_t)d.dim, false, dloss};
+    float *lead = dloss_stride ? (float *)((char *)ws + s.lead) : (float *)dloss;  // one dloss for all leads itself
+    const bool by_waves = lead_by_waves(d);
+    if (dloss_stride && !by_waves) {
+        hipLaunchKernelGGL(vocab_lead_kernel, dim3(1), dim3(1024), 0, st, LeadOf{dloss, dloss_stride, targets(d, target), (uint32_t)d.tokens}, lead);
+        if ((rc = launch_status()) != AR_OK) return rc;
+    }
+    const ProductOut to_dx{{(bf16 *)dx, nullptr}, part_dx, {odx.ld, 0}, 0x80000000u, (uint32_t)d.tokens, (uint32_t)d.dim, false, lead};
     for (size_t k = 0; k < s.pieces; ++k) {
         const size_t first = k * s.piece, rows = d.rows - first < s.piece ? d.rows - first : s.piece;
         const char *wk = (const char *)pw.p + first * pw.ld;
         GemmArgs g = logits;
         g.b[0] = wk, g.n = (uint32_t)rows;
-        DzOut o{dz, s.ld, lse, dloss, dloss_stride, targets(d, target)};
+        DzOut o{dz, s.ld, lse, dloss, dloss_stride, targets(d, target), dloss_stride && by_waves ? (uint32_t)d.tokens : 0, lead};
         o.target.first += first;
         switch (logits_tile(d.tokens, d.dim, rows)) {
         case kFewTokens: rc = launch_dz<Flat>(g, o, st); break;
@@ -485,7 +559,7 @@ int vocab_backward(const ar_vocab_desc *desc, const float *dloss, size_t dloss_s
             p.ka = p.kb = (uint32_t)d.tokens;
             p.a[0] = dz, p.b[0] = px.p, p.lda = (uint32_t)(s.ld * 2), p.ldb = px.ld;
             p.m = (uint32_t)round_up(rows, 8), p.n = px.cols;
-            const ProductOut out{{(bf16 *)dw + first * odw.ld, nullptr}, part_dw, {odw.ld, 0}, 0x80000000u, (uint32_t)rows, (uint32_t)d.dim, false, dloss};
+            const ProductOut out{{(bf16 *)dw + first * odw.ld, nullptr}, part_dw, {odw.ld, 0}, 0x80000000u, (uint32_t)rows, (uint32_t)d.dim, false, lead};
             if ((rc = product<true, false, true>(s.dw, p, out, st)) != AR_OK) return rc;
         }
     }

@@ -72,12 +72,13 @@ struct ProductOut {
     bool more;
     const float *by;
 };
-// The significand, in [1/2, 1), of the value there; 1 for one that has none.
-__device__ __forceinline__ float factor(const float *p)
+// The significand, in [1/2, 1), of a value; 1 for one that has none (0, an infinity, NaN).
+__device__ __forceinline__ float significand(float v)
 {
-    const float m = fabsf(__builtin_amdgcn_frexp_mantf(*p));
+    const float m = fabsf(__builtin_amdgcn_frexp_mantf(v));
     return m >= 0.5f && m < 1.0f ? m : 1.0f;
 }
+__device__ __forceinline__ float factor(const float *p) { return significand(*p); }
 template <typename S, bool ABYK, bool ADD = false, bool BY = false> __global__ __launch_bounds__(S::THREADS) void product_kernel(const GemmArgs g, const ProductOut o)
 {
     constexpr int NT = S::NT, COLS = NT * 32;

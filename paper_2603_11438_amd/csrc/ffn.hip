@@ -198,11 +198,12 @@ template <typename S, int ACT> int launch_ffn(GemmArgs &g, const FfnOut &o, hipS
 
 size_t ffn_part_bytes(const ar_ffn_desc &d, const Cut &c) { return c.splits > 1 ? c.splits * 2 * d.tokens * d.hidden * sizeof(float) : 0; }
 
-template <int ACT> int launch_ffn_tiles(const Cut &c, GemmArgs &g, const FfnOut &o, hipStream_t st)
+template <int ACT> int launch_ffn_tiles(const Cut &c, bool ahead, GemmArgs &g, const FfnOut &o, hipStream_t st)
 {
     if (c.tile == kFlat) return launch_ffn<Flat, ACT>(g, o, st);
     if (c.tile == kPairDeep) return launch_ffn<Deep, ACT>(g, o, st);
-    return c.tile == kPairSmall ? launch_ffn<Small, ACT>(g, o, st) : launch_ffn<Large, ACT>(g, o, st);
+    if (c.tile == kPairSmall) return launch_ffn<Small, ACT>(g, o, st);
+    return ahead ? launch_ffn<Large, ACT>(g, o, st) : launch_ffn<LargeEven, ACT>(g, o, st);
 }
 
 struct FfnMats {
@@ -273,10 +274,11 @@ int ffn(const ar_ffn_desc *desc, const void *x, const void *wg, const void *wu, 
     g.ka = g.kb = (uint32_t)round_up(d.dim, 8);
     g.m = (uint32_t)d.tokens, g.n = (uint32_t)d.hidden, g.batch = 1, g.splits = cut.splits;
     const FfnOut o{(bf16 *)h, saved, (float *)at, m.h.ld};  // the runs' sums behind the copies
+    const bool ahead = pair_ahead(d.tokens, d.dim, d.hidden, saved != nullptr);
     switch (d.act) {
-    case AR_ACT_SILU: return launch_ffn_tiles<AR_ACT_SILU>(cut, g, o, st);
-    case AR_ACT_GELU: return launch_ffn_tiles<AR_ACT_GELU>(cut, g, o, st);
-    default: return launch_ffn_tiles<AR_ACT_RELU>(cut, g, o, st);
+    case AR_ACT_SILU: return launch_ffn_tiles<AR_ACT_SILU>(cut, ahead, g, o, st);
+    case AR_ACT_GELU: return launch_ffn_tiles<AR_ACT_GELU>(cut, ahead, g, o, st);
+    default: return launch_ffn_tiles<AR_ACT_RELU>(cut, ahead, g, o, st);
     }
 }
 

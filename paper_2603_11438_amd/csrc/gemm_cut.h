@@ -131,6 +131,16 @@ inline double pair_us(int tile, size_t tokens, size_t dim, size_t hidden, uint32
     return us;
 }
 
+// Whether the 256 x 256 tile takes a third buffer for A: where x, the weights and the
+// results do not stay in the 256 MiB of cache before the memory, so that loads take longer
+// than a stage covers.  Time by that of two buffers, without the projections saved: of 326 to
+// 372 MB 0.94 to 0.99 (8192 x 4096 x 11264, 343 MB, 1180 us and 1212), of 1 GB 0.95, of 234 to 284
+// MB 1.00 to 1.03 (8192 x 1024 x 11264, 247 MB, 367 and 357); saved, 8192 x 1024 x 11264 458 and 470.
+inline bool pair_ahead(size_t tokens, size_t dim, size_t hidden, bool saved)
+{
+    return 2.0 * ((double)tokens * dim + 2.0 * dim * hidden + (double)tokens * hidden) + (saved ? 8.0 * tokens * hidden : 0.0) > 3e8;
+}
+
 // The forward's tile and the runs of its k.  Few tiles, of a rank's share of the
 // hidden columns say, leave units idle that a split puts to work.  Flat: kFlatStep us
 // a step of 64 for a tile (1 x 4096 x 1408 in one piece 32 us), two tiles to a unit,

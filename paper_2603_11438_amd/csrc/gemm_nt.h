@@ -31,7 +31,8 @@
 // buffers, at 1.75 GHz: the board's power limit has the clock.  With every load an L2
 // hit the same kernel takes 794 us, so the rest is misses that a stage's lead does
 // not cover.  A third buffer for A (AHEAD) makes the waits 15 % of the cycles, from 25,
-// and the clock lower: 2 to 3 % less time (4096 x 4096 x 131072: 3540 us, from 3630).
+// and the clock lower: 2 to 3 % less time (4096 x 4096 x 131072: 3540 us, from 3630), but
+// paired and with all data in the cache 1 to 3 % more (`pair_ahead`).
 // Smaller tiles: 128 x 128 1020 us, 64 x 64 1525 us.
 #pragma once
 

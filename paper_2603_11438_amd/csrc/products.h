@@ -198,6 +198,7 @@ inline int run_packs(const PackList &list, hipStream_t st)
 }
 
 typedef Shape<4, 4, 1, 64, 2, 2, true> Large;
+typedef Shape<4, 4, 1, 64, 2> LargeEven;  // with two buffers of each operand
 typedef Shape<3, 3, 1, 64, 2> Middle;
 typedef Shape<2, 2, 1, 64, 2> Small;
 typedef Shape<1, 1, 1, 64, 4> Tiny;

@@ -97,6 +97,39 @@ inline Cut a_cut(int planes, size_t m, size_t np, size_t batch) { return cut_for
 inline Cut b_cut(int planes, size_t m, size_t mp, size_t batch) { return cut_for(planes, m, m, mp / kStepK, batch, true, 0, 3, 1); }
 inline Cut x_cut(int planes, size_t m, size_t n, size_t mp, size_t batch) { return cut_for(planes, m, n, mp / kStepK, batch, false, 0, 3, 1); }
 
+// The loss over a vocabulary.  The logits' tile, whose results an epilogue takes: up to 64
+// tokens the weights' bytes are what counts, 64 x 128.
+constexpr int kFewTokens = -1;
+inline int logits_tile(size_t tokens, size_t dim, size_t rows)
+{
+    if (tokens <= 64) return kFewTokens;
+    return cut_for(1, tokens, rows, (dim + kStepK - 1) / kStepK, 1, false, 0, 4, 1).tile;
+}
+// The backward pass: the rows of the weight in pieces, and both products with a piece's dz.
+// dz takes at most this much: large enough that a piece's products fill the device many
+// times over and dx's sums, read and written by each, cost little.
+constexpr size_t kPieceBytes = (size_t)1 << 29;
+constexpr size_t kLeastPiece = 1024;
+struct VocabCut {
+    size_t piece, pieces;  // rows in a piece (but the last)
+    size_t ld;             // of dz
+    Cut dx, dw;
+};
+inline VocabCut vocab_cut(size_t tokens, size_t dim, size_t rows)
+{
+    auto up = [](size_t v, size_t to) { return (v + to - 1) / to * to; };
+    VocabCut s{};
+    size_t most = kPieceBytes / (tokens * 2) / 256 * 256;
+    if (most < kLeastPiece) most = kLeastPiece;
+    s.pieces = (rows + most - 1) / most;
+    s.piece = s.pieces == 1 ? rows : up((rows + s.pieces - 1) / s.pieces, 256);
+    s.pieces = (rows + s.piece - 1) / s.piece;
+    s.ld = up(s.piece, 64);  // rows of dz begin at 128 bytes
+    s.dx = cut_for(1, tokens, dim, s.ld / kStepK, 1, false, 0, 4, kMaxSplits);
+    s.dw = cut_for(1, up(s.piece, 8), dim, (tokens + kStepK - 1) / kStepK, 1, false, 0, 4, kMaxSplits);
+    return s;
+}
+
 // ---- the gated feed-forward block's forward ----------------------------------
 
 // Paired tiles: a wave holds both projections of the same columns, so a tile has

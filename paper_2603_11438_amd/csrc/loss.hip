@@ -300,14 +300,6 @@ VocabMats vocab_mats(const ar_vocab_desc &d, const void *x, const void *w, const
 }
 Targets targets(const ar_vocab_desc &d, const void *p) { return {p, d.first, d.classes, d.target_bytes == 8}; }
 
-// The tile of a product whose results a kernel's epilogue takes, of those of `cut_for`.
-// Up to 64 tokens the weights' bytes are what counts: 64 x 128.
-constexpr int kFewTokens = -1;
-int logits_tile(size_t tokens, size_t dim, size_t rows)
-{
-    if (tokens <= 64) return kFewTokens;
-    return cut_for(1, tokens, rows, (dim + kStepK - 1) / kStepK, 1, false, 0, 4, 1).tile;
-}
 // Columns of a wave of the tile.
 size_t wave_columns(int tile) { return tile == 0 ? 32 : tile == 2 ? 96 : tile == 3 ? 128 : 64; }
 size_t runs_of(const ar_vocab_desc &d) { return (d.rows + wave_columns(logits_tile(d.tokens, d.dim, d.rows)) - 1) / wave_columns(logits_tile(d.tokens, d.dim, d.rows)); }
@@ -439,10 +431,6 @@ int vocab_join(const ar_vocab_desc *desc, size_t ranks, const float *parts, cons
 
 // ---- backward -------------------------------------------------------------------
 
-// dz of a piece takes at most this much: large enough that a piece's products fill the
-// device many times over and dx's sums, read and written by each, cost little.
-constexpr size_t kPieceBytes = (size_t)1 << 29;
-constexpr size_t kLeastPiece = 1024;
 // Whether each wave that makes dz looks for the lead by itself: where there are few tokens
 // to look through, eight looks at most, and few rounds of tiles that all do so, which is
 // less than a launch.  Gradients of 1025 x 1024 x 8192, 98.4 us with the first dloss taken as
@@ -451,32 +439,22 @@ constexpr size_t kLeastPiece = 1024;
 bool lead_by_waves(const ar_vocab_desc &d) { return d.tokens <= 4096 && d.tokens * d.rows <= (size_t)1 << 24; }
 
 // Where the backward pass keeps what; dz lies at the start, copies behind the rest.
-struct VocabBackwardSpace {
-    size_t piece, pieces;  // rows of the weight in a piece (but the last)
-    size_t ld;             // of dz
-    Cut dx, dw;
+struct VocabBackwardSpace : VocabCut {
     size_t lead;                      // the dloss that gives dz its factor
     size_t part_dx, part_dw, copies;  // with one piece one place after the other
 };
 VocabBackwardSpace vocab_backward_space(const ar_vocab_desc &d, bool dx, bool dw)
 {
     VocabBackwardSpace s{};
-    size_t most = kPieceBytes / (d.tokens * 2) / 256 * 256;
-    if (most < kLeastPiece) most = kLeastPiece;
-    s.pieces = (d.rows + most - 1) / most;
-    s.piece = s.pieces == 1 ? d.rows : round_up((d.rows + s.pieces - 1) / s.pieces, 256);
-    s.pieces = (d.rows + s.piece - 1) / s.piece;
-    s.ld = round_up(s.piece, kLine);
+    (VocabCut &)s = vocab_cut(d.tokens, d.dim, d.rows);
     s.lead = round_up(d.tokens * s.ld * 2, 256);
     s.part_dx = s.part_dw = s.copies = s.lead + 256;
     const bool several = s.pieces > 1;  // dx's sums stay from piece to piece
     if (dx) {
-        s.dx = cut_for(1, d.tokens, d.dim, s.ld / kStepK, 1, false, 0, 4, kMaxSplits);
         s.copies += several ? round_up(s.dx.splits * d.tokens * d.dim * sizeof(float), 256) : part_bytes(s.dx, d.tokens, d.dim);
         if (several) s.part_dw = s.copies;
     }
     if (dw) {
-        s.dw = cut_for(1, round_up(s.piece, 8), d.dim, (d.tokens + kStepK - 1) / kStepK, 1, false, 0, 4, kMaxSplits);
         const size_t end = s.part_dw + part_bytes(s.dw, round_up(s.piece, 8), d.dim);
         s.copies = end > s.copies ? end : s.copies;
     }

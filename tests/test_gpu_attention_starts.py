@@ -1,0 +1,124 @@
+"""Attention's starts: decreasing ones touch nothing outside the results, many sequences are
+all found, and tokens whose places pass 32 bits are read and written where they lie."""
+from __future__ import annotations
+
+import pytest
+import torch
+
+import paper_2603_11438_amd as ar
+from gpu_helpers import say
+from oracle import ops_oracle as oo
+from test_gpu_attention import check, draw, inputs, on_gpu, starts
+
+pytestmark = pytest.mark.gpu
+
+GUARD = 13.0
+
+
+def guarded(tokens, heads, dim):
+    """A tensor inside a larger one that is filled with a pattern."""
+    room = torch.full((tokens + 64, heads + 2, dim + 16), GUARD, dtype=torch.bfloat16, device="cuda")
+    return room, room[32:32 + tokens, 1:1 + heads, 8:8 + dim]
+
+
+def outside_is_kept(room, inner):
+    inner.fill_(GUARD)
+    return bool((room == GUARD).all())
+
+
+DECREASING = [
+    # queries, keys, starts_q, starts_k
+    (400, 500, [0, 300, 100, 250, 400], [0, 500, 20, 480, 10]), (400, 500, [400, 0], [500, 0]), (400, 500, [350, 20, 390, 0], [0, 100, 100, 500]),
+    (400, 500, [0, 100, 100, 400], [500, 200, 450, 30]), (90, 2000, [90, 10, 60, 0, 90], [2000, 0, 1999, 1, 5]),
+    (400, 500, [2 ** 31 - 1, -2 ** 31, 400, -1, 1 << 30], [-7, 600, -2 ** 31, 2 ** 31 - 1, 0]),
+    (3, 3000, [3, 2, 1, 0], [0, 3000, 0, 3000]), (1000, 1000, [1000 - (37 * i) % 1001 for i in range(200)], [(61 * i) % 1001 for i in range(200)]),
+]
+
+
+@pytest.mark.parametrize("heads,kv_heads,dim", [(4, 2, 64), (80, 40, 72)])
+@pytest.mark.parametrize("case", DECREASING, ids=lambda c: f"{c[0]}-{c[1]}-{len(c[2]) - 1}")
+@pytest.mark.parametrize("causal", [True, False])
+def test_decreasing_starts_touch_nothing_else(case, heads, kv_heads, dim, causal):
+    """No result is defined, but nothing around the results is written, and inputs stay."""
+    queries, keys, sq, sk = case
+    say("decreasing", queries, keys, len(sq) - 1, heads, dim, causal)
+    q, k, v, do = inputs([0, queries], [0, keys], heads, kv_heads, dim, 3)
+    before = [t.clone() for t in (q, k, v, do)]
+    rooms = [guarded(*t.shape) for t in (q, q, k, v)]
+    kw = dict(starts_q=on_gpu(sq), starts_k=on_gpu(sk), causal=causal)
+    _, lse = ar.packed_attention(q, k, v, save=True, out=rooms[0][1], **kw)
+    lse.nan_to_num_(0.0, 0.0, 0.0)
+    ar.packed_attention_backward(do, q, k, v, torch.zeros_like(q), lse, out=[inner for _, inner in rooms[1:]], **kw)
+    assert all(outside_is_kept(*r) for r in rooms)
+    assert all(torch.equal(a, b) for a, b in zip((q, k, v, do), before))
+
+
+@pytest.mark.parametrize("heads,kv_heads,dim", [(2, 1, 64), (3, 3, 40)])
+@pytest.mark.parametrize("count", [4095, 4097, 5000])
+def test_many_sequences(count, heads, kv_heads, dim):
+    """More than two rounds of the search find, short ones, empty ones and a few long ones among them."""
+    say("many", count, heads, dim)
+    lq = [(7 * i + i // 5) % 4 for i in range(count)]
+    lk = [(5 * i + i // 3) % 6 for i in range(count)]
+    for i, (a, b) in {17: (130, 200), count // 2: (70, 300), count - 2: (257, 257)}.items():
+        lq[i], lk[i] = a, b
+    sq, sk = starts(lq), starts(lk)
+    q, k, v, do = inputs(sq, sk, heads, kv_heads, dim, 5)
+    want = oo.attention(q, k, v, sq, sk, True, None, do)
+    kw = dict(starts_q=on_gpu(sq), starts_k=on_gpu(sk))
+    o, lse = ar.packed_attention(q, k, v, save=True, **kw)
+    check(o, *want["o"], "o")
+    check(lse.t(), *want["lse"], "lse")
+    for name, g in zip(("dq", "dk", "dv"), ar.packed_attention_backward(do, q, k, v, o, lse, **kw)):
+        check(g, *want[name], name)
+
+
+@pytest.mark.parametrize("heads,kv_heads", [(16, 8), (4, 2)])
+def test_rows_past_32_bits(heads, kv_heads):
+    """All tensors are column ranges of one, 2^20 elements from token to token: from token
+    2048 on places are 2^31 elements and more, in every pass, with tiles of 128 rows and of 32."""
+    say("far rows", heads)
+    tokens, dim, wide, at = 2600, 64, 1 << 20, [2000, 2300, 2570]
+    room = torch.full((tokens, wide), GUARD, dtype=torch.bfloat16, device="cuda")
+    place, parts = 0, {}
+    for name, h in (("q", heads), ("k", kv_heads), ("v", kv_heads), ("do", heads), ("o", heads), ("dq", heads), ("dk", kv_heads), ("dv", kv_heads)):
+        parts[name] = room[:, place:place + h * dim].unflatten(1, (h, dim))
+        place += h * dim + 8
+    inside = slice(at[0], at[-1])
+    near = [a - at[0] for a in at]
+    for t, x in zip((parts[n] for n in ("q", "k", "v", "do")), inputs(near, near, heads, kv_heads, dim, 7)):
+        t[inside] = x
+    for causal in (True, False):
+        kw = dict(starts_q=on_gpu(at), causal=causal)
+        q, k, v, do, o = (parts[n] for n in ("q", "k", "v", "do", "o"))
+        _, lse = ar.packed_attention(q, k, v, save=True, out=o, **kw)
+        ar.packed_attention_backward(do, q, k, v, o, lse, out=[parts[n] for n in ("dq", "dk", "dv")], **kw)
+        want = oo.attention(q[inside], k[inside], v[inside], near, near, causal, None, do[inside])
+        check(lse[:, inside].t(), *want["lse"], "lse")
+        for name in ("o", "dq", "dk", "dv"):
+            check(parts[name][inside], *want[name], name)
+    for t in parts.values():
+        t[inside] = GUARD
+    assert bool((room[:2000] == GUARD).all()) and bool((room[2000:] == GUARD).all())
+
+
+@pytest.mark.parametrize("heads_first", [False, True])
+def test_a_long_cache_past_32_bits(heads_first):
+    """Keys and values of more than 2^31 elements, whose gradients lie as they do, the last tokens in use."""
+    say("far tokens", heads_first)
+    hk, dim = 8, 128
+    tokens = (1 << 31) // (hk * dim) + 700
+    make = lambda: (torch.zeros(hk, tokens, dim, dtype=torch.bfloat16, device="cuda").transpose(0, 1) if heads_first  # noqa: E731
+                    else torch.zeros(tokens, hk, dim, dtype=torch.bfloat16, device="cuda"))
+    k, v, dk, dv = (make() for _ in range(4))
+    k[-600:], v[-600:] = draw((600, hk, dim), 120), draw((600, hk, dim), 121)
+    q, do = draw((200, 16, dim), 122), draw((200, 16, dim), 123)
+    kw = dict(starts_q=on_gpu([0, 0, 200]), starts_k=on_gpu([0, tokens - 600, tokens]))
+    o, lse = ar.packed_attention(q, k, v, save=True, **kw)
+    dq, _, _ = ar.packed_attention_backward(do, q, k, v, o, lse, out=(None, dk, dv), **kw)
+    want = oo.attention(q, k[-600:], v[-600:], [0, 200], [0, 600], True, None, do)
+    check(o, *want["o"], "o")
+    check(lse.t(), *want["lse"], "lse")
+    for name, t in (("dq", dq), ("dk", dk[-600:]), ("dv", dv[-600:])):
+        check(t, *want[name], name)
+    assert not dk[:-600].any() and not dv[:-600].any()

@@ -206,6 +206,9 @@ size_t ar_orthogonalize_workspace(const ar_ortho_desc *desc);
  * (before the first start, from the last one on) keep their o and lse, or get zeros
  * with AR_ATTN_CLEAR.  Values of `starts` outside the tokens are taken as the nearest
  * end of them; where they decrease, no output is defined, but nothing else is touched.
+ * A sequence may have no queries: unused places between caches that have room to grow are
+ * the keys of one such sequence each.  (They count in the mean length by which keys are
+ * split into runs, which is best where sequences are alike.)
  * A key that a query does not see has no part in it but for one thing: in a value (v)
  * or, backward, a k, q or dout that is infinite or NaN, 0 times it is NaN, which can
  * reach rows of the same sequence within 256 tokens. */

@@ -640,8 +640,9 @@ def packed_attention(q, k, v, *, starts_q=None, starts_k=None, causal: bool = Tr
     contiguous, so all three may be parts of one tensor.  starts_q, starts_k: int32, on
     the GPU, sequences + 1 values that do not decrease: sequence i has the tokens
     starts[i] .. starts[i + 1] - 1; starts_k left out is starts_q, both left out one
-    sequence.  causal: a sequence's last query sees all its keys, each one before it one
-    less; a query that sees none has o = 0.  scale: 1 / sqrt(dim) unless given; above 0.
+    sequence.  A sequence may have no queries, as unused places between caches.
+    causal: a sequence's last query sees all its keys, each one before it one less; a
+    query that sees none has o = 0.  scale: 1 / sqrt(dim) unless given; above 0.
     out: o to write to; tokens of no sequence are then left as they were in it, and are
     zeros in a new one.  lse: (heads, queries) fp32, zeros there."""
     import torch

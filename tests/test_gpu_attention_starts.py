@@ -122,3 +122,32 @@ def test_a_long_cache_past_32_bits(heads_first):
     for name, t in (("dq", dq), ("dk", dk[-600:]), ("dv", dv[-600:])):
         check(t, *want[name], name)
     assert not dk[:-600].any() and not dv[:-600].any()
+
+
+@pytest.mark.parametrize("room,heads,kv_heads,dim", [(700, 8, 2, 64), (4096, 32, 8, 128)])
+def test_caches_with_room_to_grow(room, heads, kv_heads, dim):
+    """A cache's unused places are the keys of a sequence without queries: new tokens are put
+    where the next one belongs, and nothing is packed again."""
+    say("room", room)
+    lens, count = [1, room, 0, 33, 300, room - 1, 64], 7
+    g = torch.Generator().manual_seed(8)
+    k, v = (torch.full((count, room, kv_heads, dim), float("nan"), dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    for i, n in enumerate(lens):
+        k[i, :n], v[i, :n] = (torch.randn(n, kv_heads, dim, generator=g).bfloat16().cuda() for _ in range(2))
+    q = draw((count, heads, dim), 9)
+    sq = torch.arange(count + 1).repeat_interleave(2)[1:]  # 0, 1, 1, 2, 2, ...
+    begin = torch.arange(count) * room
+    for step in range(3):
+        sk = torch.stack([begin, begin + torch.tensor(lens)], 1).flatten()  # a sequence, its room, the next
+        sk = torch.cat([sk, torch.tensor([count * room])])
+        kw = dict(starts_q=sq.int().cuda(), starts_k=sk.int().cuda())
+        assert len(sq) == len(sk) == 2 * count + 1
+        o, lse = ar.packed_attention(q, k.flatten(0, 1), v.flatten(0, 1), save=True, **kw)
+        packed = [torch.cat([t[i, :n] for i, n in enumerate(lens)]) for t in (k, v)]
+        want = oo.attention(q, *packed, list(range(count + 1)), starts(lens))
+        check(o, *want["o"], "o")
+        check(lse.t(), *want["lse"], "lse")
+        for i, n in enumerate(lens):  # a new token each, where there is room
+            if n < room:
+                k[i, n], v[i, n] = (torch.randn(kv_heads, dim, generator=g).bfloat16().cuda() for _ in range(2))
+                lens[i] = n + 1

@@ -15,7 +15,8 @@ constexpr int kStepK = 64;  // steps that k is counted in
 // us for the same when one tile has the unit to itself (its loads' way to the
 // L2 and back is then in the open); `fit`: tiles that share a unit; `ends`: us
 // before and after the products.  Measured on products of 1024 x 1024 x 4096
-// (alone) and 8192 x 8192 x 8192 (busy).  The last one has three buffers, for a
+// (alone) and 8192 x 8192 x 8192 (busy), the 256 tile's with two buffers of both operands:
+// the third for A, which it has since, takes 2 to 3 % off.  The last one has three, for a
 // tile alone on its unit: 768 x 1024 x 5376 in four runs 19.2 us, with two
 // buffers 23.7 and in 64 x 64 tiles 31.1; with two tiles to a unit it is slower
 // (5376 x 1024 x 768: 23.0 us, with two buffers 18.2).

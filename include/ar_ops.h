@@ -257,8 +257,9 @@ size_t ar_attention_backward_workspace(const ar_attention_desc *desc);
  *     lse_t = log sum_j e^z_tj,  loss_t = lse_t - z_t,target(t)
  * W is the whole vocabulary, or a rank's rows of it: the classes first .. first + rows - 1
  * of `classes`.  A token whose target is not one of 0 .. classes - 1, a negative one say,
- * has no loss (0) and no gradient; its row of x has to be finite all the same where dW
- * is wanted (0 times it is added there).  The logits are never in memory. */
+ * has no loss (0) and no gradient, whatever its dloss holds; its row of x has to be finite
+ * all the same where dW is wanted (0 times it is added there).  The logits are never in
+ * memory. */
 typedef struct ar_vocab_desc {
     size_t tokens;         /* 0 is a valid no-op (backward: zero weight gradient); at most
                               2^24, times rows 2^38 */
